@@ -392,6 +392,139 @@ int fcp_group_shard_args(const int32_t* group_of_seq, int32_t n_seqs, const int3
  */
 int fcp_scratch_status(const void* scratch, void* stream, int32_t* n_tiles, int32_t* n_rejected);
 
+/*
+ * Rotary positions.  Queries and keys are turned by angles that grow with their position before attention: with t = position * turns[i] (in full
+ * turns) and (a, b) the i-th pair of the first rot_dim channels,
+ *   y_a = magnitude (x_a cos 2 pi t - x_b sin 2 pi t),   y_b = magnitude (x_a sin 2 pi t + x_b cos 2 pi t);
+ * the other channels are copied.  The backward is the adjoint (the same with -t): it turns the gradients of rotated rows into those of the
+ * rows before.  Any rows at any positions: the packed rows of a rank, whose zigzag chunks lie apart in their sequences, or new tokens.
+ */
+#define FCP_BF16 0
+#define FCP_F32 1
+#define FCP_ROTARY_HALF 0        /* pair i: channels i and i + rot_dim / 2 */
+#define FCP_ROTARY_PAIRS 1       /* pair i: channels 2 i and 2 i + 1       */
+#define FCP_ROTARY_MAX_PARTS 4
+
+/* One tensor of rows: x[row * x_row + head * x_head + channel], strides in elements, channels next to each other. */
+typedef struct fcp_rotary_part {
+  const void* x;                 /* device, FCP_BF16 or FCP_F32 as x_type says                                        */
+  void* y;                       /* device, y_type; may be x with the same type and strides (in place), else apart    */
+  const int32_t* pos;            /* [rows] device: position of every row, any value                                   */
+  int64_t x_row, x_head, y_row, y_head;
+  int32_t rows, heads, x_type, y_type;
+} fcp_rotary_part;
+
+/*
+ * fcp_rotary_frequencies -- HOST ONLY.  turns[i], i < rot_dim / 2, in turns per position (radians / 2 pi), for contexts `factor` times as long
+ * as the `original_len` tokens that a model was trained on.  With f_i = base^(-2 i / rot_dim) / (2 pi):
+ *   FCP_ROTARY_PLAIN   f_i (factor, original_len, low, high are not used)
+ *   FCP_ROTARY_LINEAR  f_i / factor: positions are interpolated
+ *   FCP_ROTARY_BASE    f_i of the base that makes the slowest pair `factor` times as slow: base * factor^(rot_dim / (rot_dim - 2))
+ *   FCP_ROTARY_PARTS   pairs that turn fewer than `low` times in original_len tokens are interpolated, those that turn more than `high` times are
+ *                      left alone, those between are mixed in proportion
+ *   magnitude [1] out or NULL: 0.1 ln(factor) + 1 for FCP_ROTARY_PARTS and factor > 1, the usual correction of the scores' temperature
+ *   (pass it to fcp_rotary, or 1 for models without it); 1 otherwise.
+ */
+#define FCP_ROTARY_PLAIN 0
+#define FCP_ROTARY_LINEAR 1
+#define FCP_ROTARY_BASE 2
+#define FCP_ROTARY_PARTS 3
+int fcp_rotary_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor, double original_len, double low, double high,
+                           double* turns, float* magnitude);
+
+/*
+ * fcp_rotary -- up to FCP_ROTARY_MAX_PARTS tensors (queries and keys, say) in one launch.
+ *   parts [n_parts] host;  turns [rot_dim / 2] fp64 device;  rot_dim even, 2 <= rot_dim <= head_dim <= 1024
+ *   layout FCP_ROTARY_HALF or FCP_ROTARY_PAIRS;  magnitude > 0;  backward 0 or 1
+ * Angles are formed in 64 bits (position * turns loses the fraction of a turn in 32 bits at positions of 10^5), the products in 32, results are
+ * rounded once.  FCP_F32 in and FCP_BF16 out: gradient sums of fcp_attn_bwd_step become final gradients without a pass of their own.
+ * Rows whose pointers and strides are multiples of 16 bytes, with head_dim and rot_dim multiples of 16, move 16 bytes at a time; all others work too.
+ */
+int fcp_rotary(const fcp_rotary_part* parts, int32_t n_parts, const double* turns, int32_t head_dim, int32_t rot_dim, int32_t layout,
+               float magnitude, int32_t backward, void* stream);
+
+/*
+ * A paged cache of keys and values in 8 bits, for answering with what was trained: fcp_cache_append quantises new rows into it, fcp_cache_attn
+ * attends over it, fcp_cache_evict keeps the tokens that were attended to most.
+ * A page holds page_tokens tokens (16, 32, 64 or 128) of every KV head, and every (page, KV head) has one scale for its keys and one for its
+ * values; a stored code stands for code * scale.  Scales are powers of two, so that a rescaling loses nothing but what falls below the new step:
+ *   FCP_CACHE_E4M3  8-bit floating point (1 sign, 4 exponent, 3 mantissa bits, largest value 448, NaN but no infinity)
+ *   FCP_CACHE_INT8  -127 .. 127
+ * Keys lie as rows; values lie in groups of 16 tokens, the 16 codes of a channel together, which is how the matrix instructions take them.
+ * Sequence s owns the pages pages[s][0], pages[s][1], ...: its token t is slot t % page_tokens of page pages[s][t / page_tokens].  kv_len[s] tokens
+ * are cached; in every call below that takes queries or new rows, the n = cu_seqlens[s + 1] - cu_seqlens[s] rows of sequence s are its LAST n tokens,
+ * and kv_len counts them.  Both tables are device memory, so that a captured graph follows them.  A page number outside 0 .. n_pages - 1 is not
+ * followed: the tokens in it are not written, and seen by nobody.  kv_len is taken as at most max_pages * page_tokens.
+ */
+#define FCP_CACHE_E4M3 0
+#define FCP_CACHE_INT8 1
+typedef struct fcp_cache {
+  void* k;                 /* [n_pages][hkv][page_tokens][head_dim]           codes, device, 16-byte aligned */
+  void* v;                 /* [n_pages][hkv][page_tokens / 16][head_dim][16]  codes, device, 16-byte aligned */
+  float* k_scale;          /* [n_pages][hkv] device                                                          */
+  float* v_scale;          /* [n_pages][hkv] device                                                          */
+  float* weight;           /* [n_pages][hkv][page_tokens] device, 16-byte aligned: attention weight that each token got, or NULL (then no weigh, no evict) */
+  int32_t n_pages, hkv, head_dim, page_tokens, format;    /* head_dim 64 or 128 */
+} fcp_cache;
+
+/* Scratch size in bytes of fcp_cache_attn without / with weigh (queries: tq rows of hq heads) and of fcp_cache_evict (tq, hq not used), as
+ * fcp_scratch_bytes; 0 and fcp_last_error for arguments that the call would refuse.  A larger n_seqs, max_pages or tq never needs less. */
+#define FCP_SCRATCH_CACHE_ATTN 2
+#define FCP_SCRATCH_CACHE_WEIGH 3
+#define FCP_SCRATCH_CACHE_EVICT 4
+size_t fcp_cache_scratch_bytes(int which, const fcp_cache* cache, int32_t n_seqs, int32_t max_pages, int32_t tq, int32_t hq);
+
+/*
+ * fcp_cache_append -- quantise new key and value rows into the pages of their sequences.
+ *   k, v [n_rows, hkv, head_dim] bf16 device, rows k_row / v_row elements apart (multiples of 8), 16-byte aligned
+ *   cu_seqlens [n_seqs + 1], kv_len [n_seqs], pages [n_seqs][max_pages]  int32 device
+ * Per (page, KV head) written to: with no earlier token of the sequence in the page the scale is the least power of two (2^-110 at least) in whose
+ * units the new rows' largest finite magnitude is within the format; else the larger of that and the page's scale, and where it grows the
+ * earlier tokens are rounded again in the new units.  Codes are rounded to nearest even.  Infinities become the largest value; NaN stays NaN in
+ * FCP_CACHE_E4M3 and becomes 0 in FCP_CACHE_INT8.  The weights of the new tokens (if the cache has them) become 0.
+ * A page must not be written for two sequences, or read by another stream, at the same time.
+ */
+int fcp_cache_append(const fcp_cache* cache, const void* k, int64_t k_row, const void* v, int64_t v_row, int32_t n_rows, const int32_t* cu_seqlens,
+                     const int32_t* kv_len, const int32_t* pages, int32_t n_seqs, int32_t max_pages, void* stream);
+
+/*
+ * fcp_cache_attn -- attention of the last tokens of every sequence over its cache (their own keys and values appended before): row i of the n new
+ * rows of sequence s sees the tokens 0 .. kv_len[s] - n + i (causal).  One row per sequence, several, or the next piece of a prompt.
+ *   q [tq, hq, head_dim] bf16 device, rows q_row elements apart (a multiple of 8), 16-byte aligned;  cu_seqlens over its rows
+ *   o [tq, hq, head_dim] bf16, lse [hq, tq] fp32 (natural log of the scaled scores' sum; required): device, out.  A row that sees no token gets
+ *   O = 0, LSE = -inf.  Rows of no sequence are left unwritten.
+ *   weigh: 0, or 1 to add to cache->weight, for every token and KV head, the probabilities that the call's rows of that head's group give it.
+ *   scratch: device, 256-byte aligned, fcp_cache_scratch_bytes(FCP_SCRATCH_CACHE_ATTN or _WEIGH, ...); contents on entry irrelevant.
+ * Scores, statistics and sums are held in 32 bits; probabilities are rounded to bf16 for the product with V.  No atomics: results repeat bit for bit.
+ */
+int fcp_cache_attn(const fcp_cache* cache, const void* q, int64_t q_row, int32_t tq, int32_t hq, const int32_t* cu_seqlens, const int32_t* kv_len,
+                   const int32_t* pages, int32_t n_seqs, int32_t max_pages, float softmax_scale, int32_t weigh, void* o, float* lse,
+                   void* scratch, size_t scratch_bytes, void* stream);
+
+/*
+ * fcp_cache_weigh -- the weights of queries whose log-sum-exp is known, a prompt's after fcp_attn_fwd_step_direct say: adds exp(score - LSE) to
+ * cache->weight, as fcp_cache_attn with weigh does.  lse [hq, tq] fp32 device; rows with LSE = -inf add nothing.
+ */
+int fcp_cache_weigh(const fcp_cache* cache, const void* q, int64_t q_row, int32_t tq, int32_t hq, const float* lse, const int32_t* cu_seqlens,
+                    const int32_t* kv_len, const int32_t* pages, int32_t n_seqs, int32_t max_pages, float softmax_scale, void* stream);
+
+/*
+ * fcp_cache_evict -- cut every sequence to at most `budget` tokens, per KV head: its first n_first and last n_recent tokens stay, and of the others
+ * those with the greatest cache->weight (NaN counts as greatest; among equals the lowest token).  A sequence of at most `budget` tokens keeps all.
+ * The kept tokens, in their order, move with their weights to the pages new_pages[s][0], ...: pages of the same cache that no sequence of the
+ * call reads from (tokens move up, and many blocks move them at once); the old pages are free afterwards.  Every (new page, KV head) gets the least scale that
+ * holds its tokens, as in fcp_cache_append; slots after the last token hold 0.
+ *   new_pages [n_seqs][max_new_pages] int32 device; max_new_pages * page_tokens >= min(budget, max_pages * page_tokens)
+ *   budget >= n_first + n_recent, budget >= 1
+ *   kept [n_seqs][hkv][budget] int32 device out: the old token numbers, increasing, -1 after the last
+ *   new_len [n_seqs] int32 device out: min(kv_len, budget); not kv_len itself
+ *   scratch: device, 256-byte aligned, fcp_cache_scratch_bytes(FCP_SCRATCH_CACHE_EVICT, ...)
+ * Keys were turned to their positions before they were cached, so a token keeps its position whatever slot it moves to.
+ */
+int fcp_cache_evict(const fcp_cache* cache, const int32_t* pages, const int32_t* kv_len, int32_t n_seqs, int32_t max_pages, const int32_t* new_pages,
+                    int32_t max_new_pages, int32_t budget, int32_t n_first, int32_t n_recent, int32_t* kept, int32_t* new_len,
+                    void* scratch, size_t scratch_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

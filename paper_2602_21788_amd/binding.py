@@ -17,6 +17,12 @@ LIB_PATH = os.path.join(_PKG, "libfcp.so")
 
 FCP_OK, FCP_ERR_INVALID_ARG, FCP_ERR_CAPACITY, FCP_ERR_UNSUPPORTED, FCP_ERR_HIP, FCP_ERR_STALLED = 0, -1, -2, -3, -4, -5
 FCP_SCRATCH_FWD, FCP_SCRATCH_BWD = 0, 1
+FCP_SCRATCH_CACHE_ATTN, FCP_SCRATCH_CACHE_WEIGH, FCP_SCRATCH_CACHE_EVICT = 2, 3, 4
+FCP_BF16, FCP_F32 = 0, 1
+FCP_ROTARY_HALF, FCP_ROTARY_PAIRS = 0, 1
+FCP_ROTARY_PLAIN, FCP_ROTARY_LINEAR, FCP_ROTARY_BASE, FCP_ROTARY_PARTS = 0, 1, 2, 3
+FCP_ROTARY_MAX_PARTS = 4
+FCP_CACHE_E4M3, FCP_CACHE_INT8 = 0, 1
 
 CHUNK_DTYPE = np.dtype([("seq", "<i4"), ("rank", "<i4"), ("chunk", "<i4"),
                         ("seq_start", "<i4"), ("len", "<i4"), ("local_off", "<i4")])
@@ -28,7 +34,8 @@ SPAN_DTYPE = np.dtype([("seq", "<i4"), ("start", "<i4"), ("len", "<i4")])
 EXPORTS = ["fcp_last_error", "fcp_shard_plan", "fcp_plan_groups", "fcp_scratch_bytes", "fcp_attn_fwd_step", "fcp_lse_merge",
            "fcp_attn_bwd_delta", "fcp_attn_bwd_step", "fcp_grad_finalize", "fcp_scratch_status",
            "fcp_group_shard_args", "fcp_attn_fwd_step_running", "fcp_shard_plan_mixed", "fcp_mask_tables", "fcp_attn_fwd_step_mixed", "fcp_attn_bwd_step_mixed",
-           "fcp_attn_bwd_step_direct", "fcp_grad_finalize_direct", "fcp_attn_fwd_step_direct", "fcp_lse_merge_direct", "fcp_attn_fwd_step_static"]
+           "fcp_attn_bwd_step_direct", "fcp_grad_finalize_direct", "fcp_attn_fwd_step_direct", "fcp_lse_merge_direct", "fcp_attn_fwd_step_static",
+           "fcp_rotary_frequencies", "fcp_rotary", "fcp_cache_scratch_bytes", "fcp_cache_append", "fcp_cache_attn", "fcp_cache_weigh", "fcp_cache_evict"]
 
 
 class FcpError(RuntimeError):
@@ -96,6 +103,21 @@ def lib() -> ctypes.CDLL:
         L.fcp_attn_fwd_step_direct.argtypes = [P, P, P, P, I32, P, I64, I32, I32, I32, I32, I32, I32, F, P, P, P, P, P, P, SZ, P]
         L.fcp_lse_merge_direct.restype = ctypes.c_int
         L.fcp_lse_merge_direct.argtypes = [P, P, I32, I32, I32, I32, I32, P, P, P, I64, P]
+        D = ctypes.c_double
+        L.fcp_rotary_frequencies.restype = ctypes.c_int
+        L.fcp_rotary_frequencies.argtypes = [I32, D, I32, D, D, D, D, P, P]
+        L.fcp_rotary.restype = ctypes.c_int
+        L.fcp_rotary.argtypes = [P, I32, P, I32, I32, I32, F, I32, P]
+        L.fcp_cache_scratch_bytes.restype = SZ
+        L.fcp_cache_scratch_bytes.argtypes = [ctypes.c_int, P, I32, I32, I32, I32]
+        L.fcp_cache_append.restype = ctypes.c_int
+        L.fcp_cache_append.argtypes = [P, P, I64, P, I64, I32, P, P, P, I32, I32, P]
+        L.fcp_cache_attn.restype = ctypes.c_int
+        L.fcp_cache_attn.argtypes = [P, P, I64, I32, I32, P, P, P, I32, I32, F, I32, P, P, P, SZ, P]
+        L.fcp_cache_weigh.restype = ctypes.c_int
+        L.fcp_cache_weigh.argtypes = [P, P, I64, I32, I32, P, P, P, P, I32, I32, F, P]
+        L.fcp_cache_evict.restype = ctypes.c_int
+        L.fcp_cache_evict.argtypes = [P, P, P, I32, I32, P, I32, I32, I32, I32, P, P, P, SZ, P]
         _lib = L
     return _lib
 
@@ -393,3 +415,145 @@ def fcp_scratch_status(scratch, stream=None):
     a, b = ctypes.c_int32(0), ctypes.c_int32(0)
     _check(lib().fcp_scratch_status(_dev_ptr(scratch), _stream(stream), ctypes.byref(a), ctypes.byref(b)))
     return a.value, b.value
+
+
+# ---------------------------------------------------------------------------------------
+# Rotary positions and the paged 8-bit cache.  Tensors that the library reads by plain size are checked here for type and size, since
+# the C ABI sees addresses only.
+def _int_ptr(t, name, n=None):
+    import torch
+    if t.dtype != torch.int32 or (n is not None and t.numel() < n):
+        raise ValueError(f"{name} must be an int32 tensor" + ("" if n is None else f" of at least {n} entries"))
+    return _dev_ptr(t)
+
+
+def _row_stride(t, name):
+    """Elements between rows of a [rows, heads, D] bf16 tensor whose rows are whole (heads and channels next to each other)."""
+    import torch
+    if t.dtype != torch.bfloat16 or t.dim() != 3 or not t.is_cuda:
+        raise ValueError(f"{name} must be a bf16 device tensor [rows, heads, head_dim]")
+    n, h, d = t.shape
+    if n and ((d > 1 and t.stride(2) != 1) or (h > 1 and t.stride(1) != d)):
+        raise ValueError(f"{name}: the heads of a row must lie next to each other")
+    return t.stride(0) if n > 1 else h * d
+
+
+class RotaryPart(ctypes.Structure):
+    """fcp_rotary_part"""
+    _fields_ = [("x", ctypes.c_void_p), ("y", ctypes.c_void_p), ("pos", ctypes.c_void_p),
+                ("x_row", ctypes.c_int64), ("x_head", ctypes.c_int64), ("y_row", ctypes.c_int64), ("y_head", ctypes.c_int64),
+                ("rows", ctypes.c_int32), ("heads", ctypes.c_int32), ("x_type", ctypes.c_int32), ("y_type", ctypes.c_int32)]
+
+
+def fcp_rotary_frequencies(rot_dim, base=10000.0, scaling=FCP_ROTARY_PLAIN, factor=1.0, original_len=0.0, low=1.0, high=32.0):
+    """Host only.  (turns [rot_dim / 2] float64 in turns per position, magnitude); scaling: FCP_ROTARY_PLAIN, _LINEAR, _BASE or _PARTS."""
+    turns, magnitude = np.empty(max(int(rot_dim) // 2, 1), np.float64), ctypes.c_float(1.0)
+    _check(lib().fcp_rotary_frequencies(int(rot_dim), float(base), int(scaling), float(factor), float(original_len), float(low),
+                                        float(high), _np_ptr(turns), ctypes.byref(magnitude)))
+    return turns, magnitude.value
+
+
+def fcp_rotary(parts, turns, rot_dim, layout=FCP_ROTARY_HALF, magnitude=1.0, backward=False, stream=None):
+    """parts: up to four (x, y, pos), x and y [rows, heads, D] bf16 or fp32 device tensors with any row and head strides (y may be x), pos int32 [rows].
+    turns: fp64 device tensor [rot_dim / 2]."""
+    import torch
+    types = {torch.bfloat16: FCP_BF16, torch.float32: FCP_F32}
+    if turns.dtype != torch.float64 or turns.numel() * 2 < rot_dim:
+        raise ValueError("turns must be a float64 tensor of rot_dim / 2 entries")
+    arr, dim = (RotaryPart * max(len(parts), 1))(), None
+    for a, (x, y, pos) in zip(arr, parts):
+        if x.dtype not in types or y.dtype not in types or x.dim() != 3 or x.shape != y.shape or not (x.is_cuda and y.is_cuda):
+            raise ValueError("x and y must be bf16 or fp32 device tensors [rows, heads, head_dim] of one shape")
+        n, h, d = x.shape
+        if dim not in (None, d) or (d > 1 and (x.stride(2) != 1 or y.stride(2) != 1)):
+            raise ValueError("all parts have one head_dim, channels next to each other")
+        dim = d
+        a.x, a.y, a.pos = x.data_ptr(), y.data_ptr(), _int_ptr(pos, "pos", n)
+        a.x_row, a.x_head, a.y_row, a.y_head = x.stride(0), x.stride(1), y.stride(0), y.stride(1)
+        a.rows, a.heads, a.x_type, a.y_type = n, h, types[x.dtype], types[y.dtype]
+    _check(lib().fcp_rotary(arr, len(parts), _dev_ptr(turns), dim or max(int(rot_dim), 2), int(rot_dim), int(layout), float(magnitude), int(bool(backward)),
+                            _stream(stream)))
+
+
+class Cache(ctypes.Structure):
+    """fcp_cache: a view of the caller's tensors, kept as attributes' owner.  k [n_pages, hkv, page_tokens, D] and v [n_pages, hkv, page_tokens / 16, D, 16]
+    float8_e4m3fn or int8, k_scale and v_scale [n_pages, hkv] fp32, weight [n_pages, hkv, page_tokens] fp32 or None."""
+    _fields_ = [("_k", ctypes.c_void_p), ("_v", ctypes.c_void_p), ("_k_scale", ctypes.c_void_p), ("_v_scale", ctypes.c_void_p),
+                ("_weight", ctypes.c_void_p), ("n_pages", ctypes.c_int32), ("hkv", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("page_tokens", ctypes.c_int32), ("format", ctypes.c_int32)]
+
+    def __init__(self, k, v, k_scale, v_scale, weight=None):
+        import torch
+        formats = {torch.float8_e4m3fn: FCP_CACHE_E4M3, torch.int8: FCP_CACHE_INT8}
+        if k.dtype not in formats or v.dtype != k.dtype or k.dim() != 4:
+            raise ValueError("k and v must be float8_e4m3fn or int8 tensors, k [n_pages, hkv, page_tokens, head_dim]")
+        n, h, p, d = k.shape
+        if tuple(v.shape) != (n, h, p // 16, d, 16):
+            raise ValueError("v must be [n_pages, hkv, page_tokens / 16, head_dim, 16]")
+        for t, shape in ((k_scale, (n, h)), (v_scale, (n, h)), (weight, (n, h, p))):
+            if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != shape):
+                raise ValueError(f"scales and weights must be float32 tensors; expected the shape {shape}")
+        super().__init__(_dev_ptr(k), _dev_ptr(v), _dev_ptr(k_scale), _dev_ptr(v_scale), _dev_ptr(weight), n, h, d, p, formats[k.dtype])
+        self.k, self.v, self.k_scale, self.v_scale, self.weight = k, v, k_scale, v_scale, weight
+
+
+def fcp_cache_scratch_bytes(which, cache, n_seqs, max_pages, tq=0, hq=0) -> int:
+    n = int(lib().fcp_cache_scratch_bytes(int(which), ctypes.byref(cache), int(n_seqs), int(max_pages), int(tq), int(hq)))
+    if n == 0:
+        raise FcpError(FCP_ERR_INVALID_ARG, lib().fcp_last_error().decode())
+    return n
+
+
+def _seqs(cu_seqlens, kv_len, pages):
+    """(cu_seqlens, kv_len, pages) addresses, sequences, entries of a row of the table"""
+    if pages.dim() != 2:
+        raise ValueError("pages must be [n_seqs, max_pages]")
+    n, m = pages.shape
+    return _int_ptr(cu_seqlens, "cu_seqlens", n + 1) if cu_seqlens is not None else None, _int_ptr(kv_len, "kv_len", n), _int_ptr(pages, "pages"), n, m
+
+
+def fcp_cache_append(cache, k, v, cu_seqlens, kv_len, pages, stream=None):
+    """Quantises new rows k, v [n_rows, hkv, D] bf16, the last tokens of their sequences, into the cache (see include/fcp.h)."""
+    kr, vr = _row_stride(k, "k"), _row_stride(v, "v")
+    if k.shape != v.shape or tuple(k.shape[1:]) != (cache.hkv, cache.head_dim):
+        raise ValueError("k and v must be [n_rows, hkv, head_dim] of the cache")
+    cu, kl, pg, n, m = _seqs(cu_seqlens, kv_len, pages)
+    _check(lib().fcp_cache_append(ctypes.byref(cache), k.data_ptr(), kr, v.data_ptr(), vr, k.shape[0], cu, kl, pg, n, m, _stream(stream)))
+
+
+def _queries(cache, q, lse):
+    import torch
+    if q.dim() != 3 or q.shape[2] != cache.head_dim:
+        raise ValueError("q must be [tq, hq, head_dim] of the cache")
+    if lse.dtype != torch.float32 or tuple(lse.shape) != (q.shape[1], q.shape[0]):
+        raise ValueError("lse must be a float32 tensor [hq, tq]")
+    return _row_stride(q, "q")
+
+
+def fcp_cache_attn(cache, q, cu_seqlens, kv_len, pages, softmax_scale, o, lse, scratch, weigh=False, stream=None):
+    """Attention of the rows q [tq, hq, D], the last tokens of their sequences, over the cache: o [tq, hq, D] bf16, lse [hq, tq] fp32."""
+    import torch
+    qr = _queries(cache, q, lse)
+    if o.dtype != torch.bfloat16 or o.shape != q.shape:
+        raise ValueError("o must be a bf16 tensor of q's shape")
+    cu, kl, pg, n, m = _seqs(cu_seqlens, kv_len, pages)
+    _check(lib().fcp_cache_attn(ctypes.byref(cache), q.data_ptr(), qr, q.shape[0], q.shape[1], cu, kl, pg, n, m, float(softmax_scale), int(bool(weigh)),
+                                _dev_ptr(o), _dev_ptr(lse), _dev_ptr(scratch), scratch.numel() * scratch.element_size(), _stream(stream)))
+
+
+def fcp_cache_weigh(cache, q, lse, cu_seqlens, kv_len, pages, softmax_scale, stream=None):
+    """Adds the attention weights of the rows q, whose log-sum-exp lse [hq, tq] is known, to the cache's weights."""
+    qr = _queries(cache, q, lse)
+    cu, kl, pg, n, m = _seqs(cu_seqlens, kv_len, pages)
+    _check(lib().fcp_cache_weigh(ctypes.byref(cache), q.data_ptr(), qr, q.shape[0], q.shape[1], _dev_ptr(lse), cu, kl, pg, n, m, float(softmax_scale),
+                                 _stream(stream)))
+
+
+def fcp_cache_evict(cache, pages, kv_len, new_pages, budget, n_first, n_recent, kept, new_len, scratch, stream=None):
+    """Cuts every sequence to at most `budget` tokens per KV head and moves them to new_pages; kept [n_seqs, hkv, budget], new_len [n_seqs] int32 out."""
+    _, kl, pg, n, m = _seqs(None, kv_len, pages)
+    if new_pages.dim() != 2 or new_pages.shape[0] != n:
+        raise ValueError("new_pages must be [n_seqs, max_new_pages]")
+    _check(lib().fcp_cache_evict(ctypes.byref(cache), pg, kl, n, m, _int_ptr(new_pages, "new_pages"), new_pages.shape[1], int(budget), int(n_first),
+                                 int(n_recent), _int_ptr(kept, "kept", n * cache.hkv * int(budget)), _int_ptr(new_len, "new_len", n), _dev_ptr(scratch),
+                                 scratch.numel() * scratch.element_size(), _stream(stream)))
