@@ -48,14 +48,14 @@ __device__ inline int64_t block_of(const CacheView& c, int32_t page, int head) {
 // ---- codes --------------------------------------------------------------------------------------
 template <int Fmt> __device__ constexpr float most() { return Fmt == kE4m3 ? 448.f : 127.f; }
 
-// The least e with amax <= most 2^e: 448 = 0.875 * 2^9, 127 = (127 / 128) 2^7.  amax: finite, >= 0.
+// The least e with amax 2^more <= most 2^e: 448 = 0.875 * 2^9, 127 = (127 / 128) 2^7.  amax: finite, >= 0.
 template <int Fmt>
-__device__ inline int exponent_for(float amax) {
+__device__ inline int exponent_for(float amax, int more = 0) {
   if (!(amax > 0.f)) return kLeastExponent;
   const float m = __builtin_amdgcn_frexp_mantf(amax);
   const int x = __builtin_amdgcn_frexp_expf(amax);
   const int e = Fmt == kE4m3 ? x - 9 + (m > 0.875f) : x - 7 + (m > 127.f / 128.f);
-  return max(e, kLeastExponent);
+  return max(e + more, kLeastExponent);
 }
 // 2^e for -126 <= e <= 127, 0 below
 __device__ inline float power2(int e) { return e < -126 ? 0.f : __int_as_float((e + 127) << 23); }
@@ -80,6 +80,21 @@ template <int Fmt>
 __device__ inline f32x2 decode2(uint32_t u) {
   if constexpr (Fmt == kE4m3) return __builtin_amdgcn_cvt_pk_f32_fp8(u, false);
   else return f32x2{(float)(int8_t)u, (float)(int8_t)(u >> 8)};
+}
+// The two codes in the lower or upper half of a word as floats; two values, within the format, as codes in that half.
+template <int Fmt, bool Upper>
+__device__ inline f32x2 decode_half(uint32_t u) {
+  if constexpr (Fmt == kE4m3) return __builtin_amdgcn_cvt_pk_f32_fp8(u, Upper);
+  else return f32x2{(float)(int8_t)(u >> (Upper ? 16 : 0)), (float)(int8_t)(u >> (Upper ? 24 : 8))};
+}
+template <int Fmt, bool Upper>
+__device__ inline uint32_t encode_half(float a, float b, uint32_t word) {
+  if constexpr (Fmt == kE4m3) {
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(a, b, (int)word, Upper);
+  } else {
+    const uint32_t two = ((uint32_t)(int)rintf(a) & 0xffu) | ((uint32_t)(int)rintf(b) & 0xffu) << 8;
+    return Upper ? (word & 0xffffu) | two << 16 : (word & 0xffff0000u) | two;
+  }
 }
 // Eight codes in two words as bf16: both formats' values are exact there (4 and 7 significant bits).
 template <int Fmt>

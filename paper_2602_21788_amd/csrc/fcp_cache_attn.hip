@@ -39,6 +39,7 @@ struct Line {
   int64_t total;                       // tiles of all items
   int64_t before;                      // tiles of the sequences before `seq`
   int32_t seq;
+  int32_t sharers;                     // blocks that get a share
 };
 
 __device__ inline int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -48,7 +49,13 @@ __device__ inline int64_t cost_of(const SeqSizes& z, int hkv, int group, int row
   return z.n == 0 ? 0 : (int64_t)hkv * div_up((int64_t)z.n * group, rows) * tiles_of(z.len);
 }
 
-// The sequence that holds place `x` of the line (x < 0: sequence `want` is given and its `before` asked for).  Every thread of the block calls; 256 threads.
+// Blocks that get a share of the line: `blocks`, fewer where there are few tiles; and their shares.
+__device__ inline int32_t sharing(int64_t total, int32_t blocks) { return (int32_t)min((int64_t)blocks, div_up(total, kLeastTiles)); }
+__device__ inline int64_t share_begin(int64_t total, int32_t sharers, int32_t i) { return total * i / sharers; }
+__device__ inline int32_t sharer_of(int64_t total, int32_t sharers, int64_t x) { return (int32_t)(((x + 1) * sharers - 1) / total); }
+
+// The sequence that holds the beginning of share `block` (-1 if there is none), or, with want >= 0, sequence `want` and what lies before it.  Every thread of the block
+// (256) calls; a thread adds up a run of sequences.
 __device__ inline Line find_on_line(const SeqView& s, const CacheView& c, int group, int rows, int blocks, int block, int want) {
   __shared__ int64_t sums[kWaves];
   __shared__ int64_t found[2];
@@ -62,7 +69,6 @@ __device__ inline Line find_on_line(const SeqView& s, const CacheView& c, int gr
     const int64_t v = __shfl_up(upto, d);
     if (lane >= d) upto += v;
   }
-  __syncthreads();                     // (of an earlier call, everybody has what it found)
   if (lane == 63) sums[threadIdx.x >> 6] = upto;
   if (threadIdx.x == 0) found[0] = -1;
   __syncthreads();
@@ -71,8 +77,9 @@ __device__ inline Line find_on_line(const SeqView& s, const CacheView& c, int gr
     if (w < (int)(threadIdx.x >> 6)) upto += sums[w];
     total += sums[w];
   }
+  const int32_t sharers = sharing(total, blocks);
   int64_t at = upto - mine;            // of the thread's first sequence
-  const int64_t x = want >= 0 ? 0 : (int64_t)block * total / blocks;
+  const int64_t x = want >= 0 || block >= sharers ? -1 : share_begin(total, sharers, block);
   if (want >= 0 ? (want >= a && want < b) : (x >= at && x < upto)) {
     for (int i = a; i < b; ++i) {
       const int64_t n = cost_of(seq_sizes(s, i, c.page), c.hkv, group, rows);
@@ -85,13 +92,8 @@ __device__ inline Line find_on_line(const SeqView& s, const CacheView& c, int gr
     }
   }
   __syncthreads();
-  return {total, found[1], (int32_t)found[0]};
+  return {total, found[1], (int32_t)found[0], sharers};
 }
-
-// Blocks that get a share of the line: those of the grid, fewer where there are few tiles.
-__device__ inline int32_t sharing(int64_t total, int32_t blocks) { return (int32_t)min((int64_t)blocks, div_up(total, kLeastTiles)); }
-__device__ inline int64_t share_begin(int64_t total, int32_t sharers, int32_t i) { return total * i / sharers; }
-__device__ inline int32_t sharer_of(int64_t total, int32_t sharers, int64_t x) { return (int32_t)(((x + 1) * sharers - 1) / total); }
 
 template <int D>
 struct PartSlot { static constexpr int floats(int rows) { return rows * (D + 2); } };   // [rows][D] sums, [rows] maxima, [rows] sums of exponentials
@@ -103,35 +105,36 @@ struct RowState {
   float m[NB], l[NB];
 };
 
-// One wave's codes of a tile: keys, values, and the scales of the lane's 16 keys.
+// Pages of a tile for a lane: of the keys that its matrix row holds in the four key tiles, 16 (n / 4) + 4 i + n % 4, and of its 16 neighbouring keys 16 g ..; -1: not
+// there, or no cached token in it.
+struct TilePages { int32_t k, v; };
+template <class Args>
+__device__ inline TilePages pages_of(const Args& a, int seq, int len, int tile) {
+  const int lane = threadIdx.x & 63, kk = tile * kTile + 16 * ((lane & 15) >> 2), vk = tile * kTile + 16 * (lane >> 4);
+  return {kk < len ? page_at(a.s, a.c, seq, kk >> a.c.log_page) : -1, vk < len ? page_at(a.s, a.c, seq, vk >> a.c.log_page) : -1};
+}
 template <int D>
-struct TileCodes {
-  u32x4 k[4][D / 64], v[D / 16];
-  float ks, vs;
-  bool there;                          // the page of the lane's 16 keys exists and holds cached tokens
-};
-
-template <int D>
-__device__ inline void load_tile(const AttnArgs& a, int seq, int head, int len, int tile, TileCodes<D>& t) {
-  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
-  const int key0 = tile * kTile;
-  // keys: the lane's matrix row n holds, in key tile i, key 16 (n / 4) + 4 i + n % 4
-  const int kk = key0 + 16 * (n >> 2);
-  const int32_t kp = kk < len ? page_at(a.s, a.c, seq, kk >> a.c.log_page) : -1;
-  const uint8_t* kb = a.c.k + (block_of(a.c, max(kp, 0), head) * a.c.page + ((kk + (n & 3)) & (a.c.page - 1))) * D + 16 * g;
+__device__ inline void load_keys(const CacheView& c, int head, int tile, int32_t page, u32x4 (&k)[4][D / 64]) {
+  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4, kk = tile * kTile + 16 * (n >> 2) + (n & 3);
+  const uint8_t* p = c.k + (block_of(c, max(page, 0), head) * c.page + (kk & (c.page - 1))) * D + 16 * g;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int j = 0; j < D / 64; ++j) t.k[i][j] = *reinterpret_cast<const u32x4*>(kb + 4 * i * D + 64 * j);
-  const int vk = key0 + 16 * g;
-  const int32_t vp = vk < len ? page_at(a.s, a.c, seq, vk >> a.c.log_page) : -1;
-  const int64_t block = block_of(a.c, max(vp, 0), head);
-  const uint8_t* vb = a.c.v + (block * a.c.page + (vk & (a.c.page - 1))) * D + 16 * n;
+    for (int j = 0; j < D / 64; ++j) k[i][j] = *reinterpret_cast<const u32x4*>(p + 4 * i * D + 64 * j);
+}
+template <int D>
+__device__ inline void load_values(const CacheView& c, int head, int tile, int32_t page, u32x4 (&v)[D / 16]) {
+  const int lane = threadIdx.x & 63, vk = tile * kTile + 16 * (lane >> 4);
+  const uint8_t* p = c.v + (block_of(c, max(page, 0), head) * c.page + (vk & (c.page - 1))) * D + 16 * (lane & 15);
 #pragma unroll
-  for (int i = 0; i < D / 16; ++i) t.v[i] = *reinterpret_cast<const u32x4*>(vb + 256 * i);
-  t.there = vp >= 0;
-  t.ks = t.there ? a.c.k_scale[block] : 0.f;
-  t.vs = t.there ? a.c.v_scale[block] : 0.f;
+  for (int i = 0; i < D / 16; ++i) v[i] = *reinterpret_cast<const u32x4*>(p + 256 * i);
+}
+// scales of the lane's 16 neighbouring keys (1 where the page is not there: its scores are masked)
+struct TileScales { float k, v; };
+__device__ inline TileScales scales_of(const CacheView& c, int head, int32_t page) {
+  const int64_t block = block_of(c, max(page, 0), head);
+  const float k = c.k_scale[block], v = c.v_scale[block];
+  return {page >= 0 ? k : 1.f, page >= 0 ? v : 1.f};
 }
 
 __device__ inline float max_over_groups(float x) {
@@ -143,110 +146,157 @@ __device__ inline float sum_over_groups(float x) {
   return x + __shfl_xor(x, 32);
 }
 
-// Which of the lane's 16 values are NaN codes, as values codes of 1 (and 0): for the columns that a mask hides them from.
-__device__ inline uint32_t nan_bytes(uint32_t w) {         // 0x38 (1.0) where a byte is 0x7f or 0xff
-  const uint32_t x = (w & 0x7f7f7f7fu) + 0x01010101u;      // 0x80 exactly for 0x7f
-  return ((x & 0x80808080u) >> 7) * 0x38u;
-}
-
-// Scores, softmax and product of one tile for 16 rows (query fragments q, state of row block b).
+// S^T of one tile.
 template <int D, int Fmt, int NB>
-__device__ inline void work_tile(const AttnArgs& a, TileCodes<D>& t, const bf16x8 (&q)[NB][D / 32], RowState<D, NB>& r, int tile, const int (&last)[NB], int len,
-                                 bool full, float* scores) {
-  const int lane = threadIdx.x & 63, g = lane >> 4;
-  const int key0 = tile * kTile + 16 * g;                  // the lane's keys
-  f32x4 s[NB][4];
+__device__ inline void scores_of(const u32x4 (&k)[4][D / 64], const bf16x8 (&q)[NB][D / 32], f32x4 (&s)[NB][4]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
 #pragma unroll
     for (int b = 0; b < NB; ++b) s[b][i] = f32x4{0, 0, 0, 0};
 #pragma unroll
     for (int j = 0; j < D / 64; ++j) {
-      const bf16x8 k0 = decode8<Fmt>(t.k[i][j][0], t.k[i][j][1]), k1 = decode8<Fmt>(t.k[i][j][2], t.k[i][j][3]);
+      const bf16x8 k0 = decode8<Fmt>(k[i][j][0], k[i][j][1]), k1 = decode8<Fmt>(k[i][j][2], k[i][j][3]);
 #pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        s[b][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, q[b][2 * j], s[b][i], 0, 0, 0);
-        s[b][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, q[b][2 * j + 1], s[b][i], 0, 0, 0);
-      }
+      for (int b = 0; b < NB; ++b) s[b][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, q[b][2 * j], s[b][i], 0, 0, 0);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) s[b][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, q[b][2 * j + 1], s[b][i], 0, 0, 0);
     }
   }
-  const float c = a.scale * t.ks;
-  bf16x8 p[NB][2];
+}
+
+// Softmax of one tile and 16 rows: raw scores s become probabilities p (times the values' scale), the running maximum and sum follow.  c: what scales the scores.
+// Masked (not Full): the lane's key i is seen if i <= last.
+template <int D, bool Full>
+__device__ inline void softmax_of(f32x4 (&s)[4], float c, float vs, int last, f32x4 (&o)[D / 16], float& m, float& l, bf16x8 (&p)[2], float* scores) {
+  if (!Full)
 #pragma unroll
-  for (int b = 0; b < NB; ++b) {
-    float top = -INFINITY;
+    for (int i = 0; i < 16; ++i) s[i / 4][i % 4] = i <= last ? s[i / 4][i % 4] : -INFINITY;
+  float top = max3(s[0][0], s[0][1], s[0][2]);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      float x = s[b][i / 4][i % 4] * c;
-      if (!full) x = t.there && key0 + i <= last[b] ? x : -INFINITY;
-      s[b][i / 4][i % 4] = x;
-      top = fmaxf(top, x);
-    }
-    if (scores)
+  for (int i = 3; i < 15; i += 2) top = max3(top, s[i / 4][i % 4], s[(i + 1) / 4][(i + 1) % 4]);
+  top = __builtin_elementwise_maximum(top, s[3][3]) * c;
+  if (scores)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) *reinterpret_cast<f32x4*>(scores + (16 * b + (lane & 15)) * kTile + 16 * g + 4 * i) = s[b][i];
-    // the maximum only grows in steps of more than 2^8: probabilities stay below 256, and most tiles leave the sums alone
-    if (__ballot(top > r.m[b] + 8.f)) {
-      const float m = fmaxf(r.m[b], max_over_groups(top));
-      const float f = __builtin_amdgcn_exp2f(r.m[b] - m);
-      r.m[b] = m;
-      r.l[b] *= f;
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<f32x4*>(scores + 4 * i) = s[i] * c;
+  // the maximum only grows in steps of more than 2^8: probabilities stay below 256, and most tiles leave the sums alone
+  if (__ballot(top > m + 8.f)) {
+    const float grown = fmaxf(m, max_over_groups(top)), f = __builtin_amdgcn_exp2f(m - grown);
+    m = grown;
+    l *= f;
 #pragma unroll
-      for (int d = 0; d < D / 16; ++d) r.o[b][d] *= f;
-    }
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const float e = __builtin_amdgcn_exp2f(s[b][i / 4][i % 4] - r.m[b]);
-      r.l[b] += e;
-      p[b][i / 8][i % 8] = (__bf16)(e * t.vs);
-    }
+    for (int d = 0; d < D / 16; ++d) o[d] *= f;
   }
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 4][i % 4], c, -m));
+    l += e;
+    p[i / 8][i % 8] = (__bf16)(e * vs);
+  }
+}
+
+// Bytes that are NaN in FCP_CACHE_E4M3 as 0x38, the code of 1; 0 elsewhere.
+__device__ inline uint32_t nan_bytes(uint32_t w) {
+  const uint32_t x = (w & 0x7f7f7f7fu) + 0x01010101u;      // 0x80 exactly for 0x7f
+  return ((x & 0x80808080u) >> 7) * 0x38u;
+}
+
+// A tile that some row of the wave sees in part, values: codes past the last token are whatever the page holds, and 0 * NaN is NaN, so they are cleared.
+// Rare: a cached value that some rows do not see is NaN.  The rows that see it get NaN and the others do not: the NaN codes leave the product, and their number among
+// the keys that a row sees is counted by a product with 1.  live: cached tokens among the lane's 16.
+template <int D, int Fmt, int NB>
+__device__ inline void clear_hidden(u32x4 (&v)[D / 16], int live, const int (&last)[NB], RowState<D, NB>& r) {
   uint32_t odd = 0;
-  if (!full) {
-    // codes past the last token are whatever the page holds, and 0 * NaN is NaN: clear them
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i)
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const int live = t.there ? min(max(len - key0 - 4 * w, 0), 4) : 0;
-        t.v[i][w] = live == 4 ? t.v[i][w] : t.v[i][w] & ((1u << (8 * live)) - 1);
-        if (Fmt == kE4m3) odd |= nan_bytes(t.v[i][w]);
-      }
-  }
-  if (Fmt == kE4m3 && !full && __ballot(odd)) {
-    // Rare: a cached value is NaN in a tile that some row sees in part.  Its rows get NaN, and only they: the NaN codes leave the product, and their
-    // number among the keys that a row sees is counted by a product with 1.
+  for (int w = 0; w < 4; ++w) {
+    const int n = min(max(live - 4 * w, 0), 4);
+    const uint32_t keep = n == 4 ? 0xffffffffu : (1u << (8 * n)) - 1;
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) {
-      u32x4 bad;
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        bad[w] = nan_bytes(t.v[i][w]);
-        t.v[i][w] &= ~(((bad[w] >> 3) & 0x01010101u) * 0xffu);
-      }
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        f32x4 count = {0, 0, 0, 0};
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          bf16x8 seen;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) seen[j] = (__bf16)(t.there && key0 + 8 * h + j <= last[b] ? 1.f : 0.f);
-          count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8<Fmt>(bad[2 * h], bad[2 * h + 1]), seen, count, 0, 0, 0);
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) r.o[b][i][j] = count[j] > 0.f ? NAN : r.o[b][i][j];
-      }
+      v[i][w] &= keep;
+      if (Fmt == kE4m3) odd |= ((v[i][w] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
     }
   }
+  if (Fmt != kE4m3 || !__ballot(odd)) return;
 #pragma unroll
-  for (int i = 0; i < D / 16; ++i)
+  for (int i = 0; i < D / 16; ++i) {
+    __builtin_amdgcn_sched_barrier(0);                     // one channel tile after the other: this must not cost the common path registers
+    u32x4 bad;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const bf16x8 v = decode8<Fmt>(t.v[i][2 * h], t.v[i][2 * h + 1]);
-#pragma unroll
-      for (int b = 0; b < NB; ++b) r.o[b][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[b][h], r.o[b][i], 0, 0, 0);
+    for (int w = 0; w < 4; ++w) {
+      bad[w] = nan_bytes(v[i][w]);
+      v[i][w] &= ~(((bad[w] >> 3) & 0x01010101u) * 0xffu);
     }
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      f32x4 count = {0, 0, 0, 0};
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        bf16x8 seen;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) seen[j] = (__bf16)(8 * h + j <= last[b] ? 1.f : 0.f);
+        count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8<Fmt>(bad[2 * h], bad[2 * h + 1]), seen, count, 0, 0, 0);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) r.o[b][i][j] = count[j] > 0.f ? NAN : r.o[b][i][j];
+    }
+  }
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// Tiles first, first + step, ... below end for 16 * NB rows of one KV head.  last_tok: last token that the lane's row of a block sees; all_see: the wave's rows all see
+// the tokens up to it.  A tile's keys are asked for when the keys before them have become scores, its values when the values before them are in the sums, page numbers a tile
+// earlier still: a wave always has 8 to 16 KB on their way.
+template <int D, int Fmt, int NB>
+__device__ inline void walk(const AttnArgs& a, int seq, int head, int len, int first, int end, int step, const bf16x8 (&q)[NB][D / 32], const int (&last_tok)[NB],
+                            int all_see, RowState<D, NB>& r, float* scores, int score_rows) {
+  if (first >= end) return;
+  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  u32x4 k[4][D / 64], v[D / 16];
+  TilePages at = pages_of(a, seq, len, first), next = pages_of(a, seq, len, first + step);
+  load_keys<D>(a.c, head, first, at.k, k);
+  TileScales sc = scales_of(a.c, head, at.v);
+  load_values<D>(a.c, head, first, at.v, v);
+  for (int i = first; i < end; i += step) {
+    const bool more = i + step < end;
+    f32x4 s[NB][4];
+    scores_of<D, Fmt, NB>(k, q, s);
+    TileScales sc_next = sc;
+    if (more) {
+      load_keys<D>(a.c, head, i + step, next.k, k);
+      sc_next = scales_of(a.c, head, next.v);
+    }
+    const float c = a.scale * sc.k;
+    const bool full = i * kTile + kTile - 1 <= all_see && !__ballot(at.v < 0);
+    bf16x8 p[NB][2];
+    if (full) {
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+        softmax_of<D, true>(s[b], c, sc.v, 0, r.o[b], r.m[b], r.l[b], p[b], scores && n < score_rows ? scores + (int64_t)i * (16 * kTile) + n * kTile + 16 * g : nullptr);
+    } else {
+      int last[NB];
+      const int key0 = i * kTile + 16 * g;
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        last[b] = at.v < 0 ? -1 : last_tok[b] - key0;
+        softmax_of<D, false>(s[b], c, sc.v, last[b], r.o[b], r.m[b], r.l[b], p[b], scores && n < score_rows ? scores + (int64_t)i * (16 * kTile) + n * kTile + 16 * g : nullptr);
+      }
+      clear_hidden<D, Fmt, NB>(v, at.v < 0 ? 0 : len - key0, last, r);
+    }
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const bf16x8 x = decode8<Fmt>(v[d][2 * h], v[d][2 * h + 1]);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) r.o[b][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, p[b][h], r.o[b][d], 0, 0, 0);
+      }
+    if (more) {
+      load_values<D>(a.c, head, i + step, next.v, v);
+      at = next;
+      next = pages_of(a, seq, len, i + 2 * step);
+      sc = sc_next;
+    }
+  }
 }
 
 // Final row, or its part: o channels 16 i + 4 g + 0..3 of the lane's row.
@@ -266,20 +316,17 @@ __device__ inline void write_row(const AttnArgs& a, int row, int head, const f32
 
 // Waves of a block divide the tiles of a piece (Keys) or take rows of their own.
 template <int D, int Fmt, int NB, bool Keys>
-__global__ __launch_bounds__(256) void attn_kernel(AttnArgs a) {
+__global__ __launch_bounds__(256, Keys ? 2 : 1) void attn_kernel(AttnArgs a) {
   constexpr int kRows = 16 * NB * (Keys ? 1 : kWaves);     // of a block
   constexpr int kStride = D + 4;                           // floats of a staged row: rows on different banks
   __shared__ float stage[Keys ? kWaves * 16 * NB * kStride : 1];
   __shared__ float stage_m[kWaves * 16 * NB], stage_l[kWaves * 16 * NB];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
-  // total first: how many blocks share the line depends on it
-  Line line = find_on_line(a.s, a.c, a.group, kRows, 1, 0, -1);
-  if (line.total == 0) return;
-  const int32_t sharers = sharing(line.total, a.blocks), me = blockIdx.x;
-  if (me >= sharers) return;
-  int64_t at = share_begin(line.total, sharers, me);
-  const int64_t end = share_begin(line.total, sharers, me + 1);
-  line = find_on_line(a.s, a.c, a.group, kRows, sharers, me, -1);
+  const int32_t me = blockIdx.x;
+  const Line line = find_on_line(a.s, a.c, a.group, kRows, a.blocks, me, -1);
+  if (line.seq < 0) return;
+  int64_t at = share_begin(line.total, line.sharers, me);
+  const int64_t end = share_begin(line.total, line.sharers, me + 1);
   int seq = line.seq;
   int64_t base = line.before;
   SeqSizes z = seq_sizes(a.s, seq, a.c.page);
@@ -328,15 +375,12 @@ __global__ __launch_bounds__(256) void attn_kernel(AttnArgs a) {
     const int last_row = min(rb * kRows + kRows, all_rows) - 1, seen = z.len - z.n + last_row / a.group;
     const int t_end = min(t1, seen < 0 ? 0 : seen / kTile + 1);
     if (Keys || __ballot(any)) {
-      TileCodes<D> t;
-      for (int i = t0 + (Keys ? wave : 0); i < t_end; i += Keys ? kWaves : 1) {
-        load_tile<D>(a, seq, head, z.len, i, t);
-        const bool full = i * kTile + kTile - 1 <= first_seen && __ballot(!t.there) == 0;
-        work_tile<D, Fmt, NB>(a, t, q, r, i, last, z.len, full, a.scores ? a.scores + (at0 - t0 + i) * (16 * kTile) : nullptr);
-      }
-      if (Keys && a.scores)                                // tiles of the piece that nobody sees
+      float* const scores = Keys && a.scores ? a.scores + (at0 - t0) * (16 * kTile) : nullptr;
+      const int score_rows = min(all_rows - rb * kRows, 16);
+      walk<D, Fmt, NB>(a, seq, head, z.len, t0 + (Keys ? wave : 0), t_end, Keys ? kWaves : 1, q, last, first_seen, r, scores, score_rows);
+      if (scores)                                          // tiles of the piece that nobody sees
         for (int i = max(t_end, t0) + wave; i < t1; i += kWaves)
-          for (int j = lane; j < 16 * kTile; j += 64) a.scores[(at0 - t0 + i) * (16 * kTile) + j] = -INFINITY;
+          for (int j = lane; j < score_rows * kTile; j += 64) scores[(int64_t)i * (16 * kTile) + j] = -INFINITY;
     }
 #pragma unroll
     for (int b = 0; b < NB; ++b) r.l[b] = sum_over_groups(r.l[b]);
@@ -397,50 +441,76 @@ __global__ __launch_bounds__(256) void attn_kernel(AttnArgs a) {
   }
 }
 
-// The items that several blocks worked: a block per (row, KV head), a wave per query head of the group, two or four channels a lane.
-template <int D>
-__global__ __launch_bounds__(256) void attn_merge_kernel(AttnArgs a, int rows_of_block) {
-  const int tok = blockIdx.x / a.c.hkv, head = blockIdx.x % a.c.hkv, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  // the row's sequence: the last one that begins at or before it and has rows
-  int lo = 0, n = a.s.n_seqs;
+// The sequence of a row: the last one that begins at or before it.  (64 ways at a time; every lane gets it.)
+__device__ inline int32_t seq_of_row(const SeqView& s, int row) {
+  int lo = 0, n = s.n_seqs;
   while (n > 1) {
-    const int step = (n + 63) / 64, at = lo + lane * step;
-    const int k = __popcll(__ballot(at < lo + n && a.s.cu[at] <= tok)) - 1, next = lo + max(k, 0) * step;
+    const int step = (n + 63) / 64, at = lo + (int)(threadIdx.x & 63) * step;
+    const int k = __popcll(__ballot(at < lo + n && s.cu[at] <= row)) - 1, next = lo + max(k, 0) * step;
     n = min(step, lo + n - next);
     lo = next;
   }
-  const int seq = lo;
-  const SeqSizes z = seq_sizes(a.s, seq, a.c.page);
-  if (tok < z.row0 || tok >= z.row0 + z.n) return;         // (uniform over the block)
-  const Line line = find_on_line(a.s, a.c, a.group, rows_of_block, 1, 0, seq);
-  const int32_t sharers = sharing(line.total, a.blocks);
-  const int tiles = tiles_of(z.len), row_blocks = (z.n * a.group + rows_of_block - 1) / rows_of_block;
-  for (int h = wave; h < a.group; h += kWaves) {
-    const int row = (tok - z.row0) * a.group + h, rb = row / rows_of_block, lr = row % rows_of_block;
-    const int64_t x = line.before + ((int64_t)head * row_blocks + rb) * tiles;
-    const int32_t w0 = sharer_of(line.total, sharers, x), w1 = sharer_of(line.total, sharers, x + tiles - 1);
-    if (w0 == w1) continue;
-    const int floats = PartSlot<D>::floats(rows_of_block);
-    auto slot = [&](int w) { return a.part + (int64_t)(2 * w + (w == w0 ? 1 : 0)) * floats; };
-    float m = kLow;
-    for (int w = w0 + lane; w <= w1; w += 64) m = fmaxf(m, slot(w)[rows_of_block * D + lr]);
-    m = wave_maxf(m);
-    float l = 0.f;
-    constexpr int kCh = D / 64;
-    float o[kCh] = {};
-#pragma unroll 4
-    for (int w = w0; w <= w1; ++w) {
-      const float* s = slot(w);
-      const float f = __builtin_amdgcn_exp2f(s[rows_of_block * D + lr] - m);
-      l += f * s[rows_of_block * (D + 1) + lr];
-#pragma unroll
-      for (int i = 0; i < kCh; ++i) o[i] += f * s[lr * D + kCh * lane + i];
+  return lo;
+}
+
+// The items that several blocks worked.  Few rows: a block per (row, query head) whose waves divide the pieces, of which a long sequence has many.
+// Many rows: a block per (eight rows, KV head) whose waves take query heads; there are two or three pieces then.
+constexpr int kMergeRows = 8;
+template <int D, bool Keys>
+__global__ __launch_bounds__(256) void attn_merge_kernel(AttnArgs a) {
+  constexpr int kCh = D / 64, kRows = Keys ? 16 : 128, kFloats = PartSlot<D>::floats(kRows);
+  __shared__ float sum_o[Keys ? kWaves : 1][D], sum_l[kWaves];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int heads = Keys ? a.hq : a.c.hkv, head = Keys ? (int)(blockIdx.x % heads) / a.group : (int)(blockIdx.x % heads);
+  const int tok0 = (int)(blockIdx.x / heads) * (Keys ? 1 : kMergeRows), tok1 = min(tok0 + (Keys ? 1 : kMergeRows), a.s.n_rows);
+  int seq = -1;
+  SeqSizes z = {0, 0, 0};
+  Line line = {};
+  for (int tok = tok0; tok < tok1; ++tok) {
+    if (seq < 0 || tok >= z.row0 + z.n) {                  // (all of this is the same for the whole block)
+      seq = seq_of_row(a.s, tok);
+      z = seq_sizes(a.s, seq, a.c.page);
+      if (tok < z.row0 || tok >= z.row0 + z.n) { seq = -1; continue; }
+      __syncthreads();
+      line = find_on_line(a.s, a.c, a.group, kRows, a.blocks, 0, seq);
     }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    __bf16* y = a.o + ((int64_t)tok * a.hq + head * a.group + h) * D + kCh * lane;
+    const int tiles = tiles_of(z.len), row_blocks = (z.n * a.group + kRows - 1) / kRows;
+    for (int h = Keys ? (int)(blockIdx.x % heads) % a.group : wave; h < a.group; h += Keys ? a.group : kWaves) {
+      const int row = (tok - z.row0) * a.group + h, rb = row / kRows, lr = row % kRows, qh = head * a.group + h;
+      const int64_t x = line.before + ((int64_t)head * row_blocks + rb) * tiles;
+      const int32_t w0 = sharer_of(line.total, line.sharers, x), w1 = sharer_of(line.total, line.sharers, x + tiles - 1);
+      if (w0 == w1) continue;
+      auto slot = [&](int w) { return a.part + (int64_t)(2 * w + (w == w0 ? 1 : 0)) * kFloats; };
+      float m = kLow;
+      for (int w = w0 + lane; w <= w1; w += 64) m = fmaxf(m, slot(w)[kRows * D + lr]);
+      m = wave_maxf(m);
+      float l = 0.f, o[kCh] = {};
+#pragma unroll 8
+      for (int w = w0 + (Keys ? wave : 0); w <= w1; w += Keys ? kWaves : 1) {
+        const float* s = slot(w);
+        const float f = __builtin_amdgcn_exp2f(s[kRows * D + lr] - m);
+        l += f * s[kRows * (D + 1) + lr];
 #pragma unroll
-    for (int i = 0; i < kCh; ++i) y[i] = (__bf16)(o[i] * inv);
-    if (lane == 0) a.lse[(int64_t)(head * a.group + h) * a.s.n_rows + tok] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+        for (int i = 0; i < kCh; ++i) o[i] += f * s[lr * D + kCh * lane + i];
+      }
+      __bf16* const y = a.o + ((int64_t)tok * a.hq + qh) * D;
+      float* const lse = a.lse + (int64_t)qh * a.s.n_rows + tok;
+      if constexpr (Keys) {
+#pragma unroll
+        for (int i = 0; i < kCh; ++i) sum_o[wave][kCh * lane + i] = o[i];
+        if (lane == 0) sum_l[wave] = l;
+        __syncthreads();                                   // (one row: once in a block)
+        l = (sum_l[0] + sum_l[1]) + (sum_l[2] + sum_l[3]);
+        const int ch = threadIdx.x;
+        if (ch < D) y[ch] = (__bf16)(l == 0.f ? 0.f : ((sum_o[0][ch] + sum_o[1][ch]) + (sum_o[2][ch] + sum_o[3][ch])) * (1.f / l));
+        if (ch == 0) *lse = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+      } else {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+        for (int i = 0; i < kCh; ++i) y[kCh * lane + i] = (__bf16)(o[i] * inv);
+        if (lane == 0) *lse = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+      }
+    }
   }
 }
 
@@ -465,7 +535,7 @@ __global__ __launch_bounds__(256) void weigh_kernel(WeighArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
   // the line with one block of rows per KV head
   const int kAll = INT32_MAX;
-  const Line line = find_on_line(a.s, a.c, 1, kAll, 1, 0, -1);
+  const Line line = find_on_line(a.s, a.c, 1, kAll, 1, 0, -1);       // (its length)
   int seq = 0;
   int64_t base = 0;
   SeqSizes z = seq_sizes(a.s, 0, a.c.page);
@@ -476,30 +546,22 @@ __global__ __launch_bounds__(256) void weigh_kernel(WeighArgs a) {
       z = seq_sizes(a.s, ++seq, a.c.page);
     }
     const int tile = (int)((u - base) / a.c.hkv), head = (int)((u - base) % a.c.hkv);
-    TileCodes<D> t;
-    const int key0 = tile * kTile;
+    const int key0 = tile * kTile, mine0 = key0 + 16 * g;
+    const TilePages at = pages_of(a, seq, z.len, tile);
+    const TileScales sc = scales_of(a.c, head, at.v);
+    bf16x8 k[4][D / 32];
     {
-      const int kk = key0 + 16 * (n >> 2);
-      const int32_t kp = kk < z.len ? page_at(a.s, a.c, seq, kk >> a.c.log_page) : -1;
-      const uint8_t* kb = a.c.k + (block_of(a.c, max(kp, 0), head) * a.c.page + ((kk + (n & 3)) & (a.c.page - 1))) * D + 16 * g;
+      u32x4 raw[4][D / 64];
+      load_keys<D>(a.c, head, tile, at.k, raw);
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < D / 64; ++j) t.k[i][j] = *reinterpret_cast<const u32x4*>(kb + 4 * i * D + 64 * j);
-      const int vk = key0 + 16 * g;
-      const int32_t vp = vk < z.len ? page_at(a.s, a.c, seq, vk >> a.c.log_page) : -1;
-      t.there = vp >= 0;
-      t.ks = t.there ? a.c.k_scale[block_of(a.c, vp, head)] : 0.f;
+        for (int j = 0; j < D / 64; ++j) {
+          k[i][2 * j] = decode8<Fmt>(raw[i][j][0], raw[i][j][1]);
+          k[i][2 * j + 1] = decode8<Fmt>(raw[i][j][2], raw[i][j][3]);
+        }
     }
-    bf16x8 k[4][D / 32];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int j = 0; j < D / 64; ++j) {
-        k[i][2 * j] = decode8<Fmt>(t.k[i][j][0], t.k[i][j][1]);
-        k[i][2 * j + 1] = decode8<Fmt>(t.k[i][j][2], t.k[i][j][3]);
-      }
-    const float c = a.scale * t.ks;
+    const float c = a.scale * sc.k;
     float got[16] = {};
     const int all_rows = z.n * a.group;
     // the first token that sees the tile's first key
@@ -521,7 +583,7 @@ __global__ __launch_bounds__(256) void weigh_kernel(WeighArgs a) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const float p = __builtin_amdgcn_exp2f(s[i / 4][i % 4] * c - lse2);
-        got[i] += t.there && key0 + 16 * g + i <= last && lse2 != -INFINITY ? p : 0.f;
+        got[i] += at.v >= 0 && mine0 + i <= last && lse2 != -INFINITY ? p : 0.f;
       }
     }
 #pragma unroll
@@ -546,13 +608,11 @@ __global__ __launch_bounds__(256) void weigh_kernel(WeighArgs a) {
 // The same from the scores that the attention kernel left (few rows): a wave per (sequence, KV head, tile), a key per lane.
 __global__ __launch_bounds__(256) void weigh_scores_kernel(AttnArgs a, int rows_of_block) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  Line line = find_on_line(a.s, a.c, a.group, rows_of_block, 1, 0, -1);
-  if (line.total == 0) return;
-  const int32_t sharers = sharing(line.total, a.blocks * kWaves), me = blockIdx.x;   // (a share has a few tiles of its own)
-  if (me >= sharers) return;
-  int64_t at = share_begin(line.total, sharers, me);
-  const int64_t end = share_begin(line.total, sharers, me + 1);
-  line = find_on_line(a.s, a.c, a.group, rows_of_block, sharers, me, -1);
+  const int32_t me = blockIdx.x;
+  const Line line = find_on_line(a.s, a.c, a.group, rows_of_block, a.blocks * kWaves, me, -1);   // (a share of its own)
+  if (line.seq < 0) return;
+  int64_t at = share_begin(line.total, line.sharers, me);
+  const int64_t end = share_begin(line.total, line.sharers, me + 1);
   int seq = line.seq;
   int64_t base = line.before;
   SeqSizes z = seq_sizes(a.s, seq, a.c.page);
@@ -605,7 +665,8 @@ int launch_attn(const AttnArgs& a, const AttnPlan& p, bool weigh, hipStream_t st
   if (p.keys) attn_kernel<D, Fmt, 1, true><<<dim3(kBlocks), dim3(256), 0, st>>>(a);
   else attn_kernel<D, Fmt, 2, false><<<dim3(kBlocks), dim3(256), 0, st>>>(a);
   FCP_HIP_CHECK(hipGetLastError());
-  attn_merge_kernel<D><<<dim3((unsigned)a.s.n_rows * a.c.hkv), dim3(256), 0, st>>>(a, p.rows);
+if (p.keys) attn_merge_kernel<D, true><<<dim3((unsigned)a.s.n_rows * a.hq), dim3(256), 0, st>>>(a);
+  else attn_merge_kernel<D, false><<<dim3((unsigned)((a.s.n_rows + kMergeRows - 1) / kMergeRows) * a.c.hkv), dim3(256), 0, st>>>(a);
   FCP_HIP_CHECK(hipGetLastError());
   if (p.stored) {
     weigh_scores_kernel<<<dim3(kBlocks * kWaves), dim3(256), 0, st>>>(a, p.rows);
@@ -629,7 +690,7 @@ int check_heads(const char* who, const CacheView& c, int32_t hq) {
 int check_rows(const char* who, const fcp_cache* cache, const void* q, int64_t q_row, int32_t tq, int32_t hq) {
   if (!q || q_row < (int64_t)hq * cache->head_dim || q_row % 8 || (uintptr_t)q % 16)
     return fail(FCP_ERR_INVALID_ARG, "%s: query rows must be at least hq * head_dim elements apart, a multiple of 8, and 16-byte aligned", who);
-  if ((int64_t)tq * cache->hkv > INT32_MAX || (int64_t)tq * (hq / cache->hkv) > INT32_MAX - 256)
+  if ((int64_t)tq * hq > INT32_MAX - 256)
     return fail(FCP_ERR_UNSUPPORTED, "%s: more than 2^31 rows of all heads", who);
   return FCP_OK;
 }

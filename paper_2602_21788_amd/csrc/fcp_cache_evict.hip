@@ -1,14 +1,19 @@
 // fcp_cache_evict: the cached tokens with the greatest attention weight kept, per KV head, and moved to new pages.
 //
-// Two launches.  The first finds, for a (sequence, KV head), the k-th greatest weight among the tokens that are neither among the first nor the most recent, by
-// counting 8 bits of an ordered integer at a time, and lists the kept tokens in order.  The second moves them: a wave per (new page, KV head, keys or
-// values) gathers the page's tokens from wherever they lie, finds the page's scale and writes the codes in its units.
+// First the k-th greatest weight among the tokens of a (sequence, KV head) that are neither among the first nor the most recent is found, by counting an ordered integer's
+// upper 11 bits and then, among the tokens that share those of the k-th, the next 11 and the last 10; the kept tokens are listed in order.  A block does that alone for
+// short tables.  One CU takes about 20 us to look at 131072 weights once, so long ones are cut into chunks: one launch counts, one lists each chunk's tokens with the k-th's
+// upper bits, one finds the border among those (every block for itself) and writes the chunk's part of the list.
+// The last launch moves the tokens: a wave per (new page, KV head, keys or values).
 #include "fcp_cache.h"
 
 namespace fcp {
 namespace {
 
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
+constexpr int kBins = 2048;
+constexpr int kListed = 16384;         // candidates that a block keeps in LDS: 64 KB; a table of as many tokens is a block's
+constexpr int kMaxChunks = 32;
 
 struct EvictArgs {
   CacheView c;
@@ -17,6 +22,12 @@ struct EvictArgs {
   int32_t max_new, budget, first, recent;
   int32_t* kept;
   int32_t* new_len;
+  // long tables: tokens of a chunk, chunks; per (sequence, KV head): counts of each chunk, candidates, of each chunk the tokens above their upper bits, border
+  int32_t chunk, chunks;
+  int32_t* counts;                     // [chunks][kBins]
+  uint32_t* list;                      // [max_pages * page]
+  int32_t* above;                      // [chunks]
+  int32_t* border;                     // upper bits, places left, candidates, unused
 };
 
 // An integer that orders weights: greater weight, greater integer; -0 and 0 are equal, every NaN is greatest.
@@ -31,170 +42,463 @@ __device__ inline int32_t cached(const EvictArgs& a, int seq) {
   const int32_t n = max(a.s.kv_len[seq], 0);
   return n < room ? n : (int32_t)room;
 }
-// weight of token t (0 where its page is missing)
-__device__ inline uint32_t order_at(const EvictArgs& a, int seq, int head, int t) {
-  const int32_t p = page_at(a.s, a.c, seq, t >> a.c.log_page);
-  return p < 0 ? order_of(0.f) : order_of(a.c.weight[block_of(a.c, p, head) * a.c.page + (t & (a.c.page - 1))]);
+// Weights of tokens t .. t + 3 (t a multiple of 4) as ordered integers; where the page is missing, of 0.
+struct Quad { uint32_t u[4]; };
+__device__ inline Quad orders_of(const EvictArgs& a, int32_t page, int head, int t) {
+  f32x4 w = {0, 0, 0, 0};
+  if (page >= 0) w = *reinterpret_cast<const f32x4*>(a.c.weight + block_of(a.c, page, head) * a.c.page + (t & (a.c.page - 1)));
+  return {{order_of(w[0]), order_of(w[1]), order_of(w[2]), order_of(w[3])}};
+}
+// f(order, whether it is one) of the tokens of [from, to) that lie in [lo, hi), in any order; from is a multiple of 4.  A thread has several loads of the page table, then of
+// weights, on their way.
+template <int Unroll, class F>
+__device__ inline void for_weights(const EvictArgs& a, int seq, int head, int from, int to, int lo, int hi, F f) {
+  constexpr int kStep = 4 * kSelectThreads;
+  to = min(to, hi);
+  for (int t0 = from + 4 * (int)threadIdx.x; t0 < to; t0 += Unroll * kStep) {
+    int32_t page[Unroll];
+    Quad q[Unroll];
+#pragma unroll
+    for (int i = 0; i < Unroll; ++i) page[i] = t0 + i * kStep < to ? page_at(a.s, a.c, seq, (t0 + i * kStep) >> a.c.log_page) : -1;
+#pragma unroll
+    for (int i = 0; i < Unroll; ++i) q[i] = orders_of(a, page[i], head, t0 + i * kStep);
+#pragma unroll
+    for (int i = 0; i < Unroll; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) f(q[i].u[j], t0 + i * kStep + j >= lo && t0 + i * kStep + j < to);
+  }
+}
+// One more in a bin.  Weights are often equal, and additions to one address wait for each other: the lanes that share the first lane's bin add once.
+__device__ inline void count_in(int32_t* bins, uint32_t bin, bool in) {
+  const uint64_t all = __ballot(in);
+  if (!all) return;
+  const uint32_t first = __builtin_amdgcn_readlane(bin, __ffsll((unsigned long long)all) - 1);
+  const uint64_t same = __ballot(in && bin == first);
+  if (in && bin != first) atomicAdd(&bins[bin], 1);
+  if ((int)(threadIdx.x & 63) == __ffsll((unsigned long long)same) - 1) atomicAdd(&bins[first], (int32_t)__popcll(same));
 }
 
-__global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictArgs a) {
-  __shared__ int32_t bins[256];
+// The bin that holds the want-th greatest, how many of it are wanted, and how many it holds.  The block's threads take two bins each, from the greatest down.
+struct Found { int32_t bin, want, held; };
+__device__ inline Found find_bin(const int32_t* bins, int32_t want) {
+  __shared__ int32_t sums[kSelectWaves];
+  __shared__ Found found;
+  const int tid = threadIdx.x, wave = tid >> 6, b = kBins - 1 - 2 * tid;
+  const int32_t x = bins[b], y = bins[b - 1], upto_wave = wave_prefix_sum(x + y);
+  if ((tid & 63) == 63) sums[wave] = upto_wave;
+  __syncthreads();
+  int32_t over = upto_wave - x - y;
+  for (int w = 0; w < wave; ++w) over += sums[w];
+  if (over < want && want <= over + x) found = {b, want - over, x};
+  else if (over + x < want && want <= over + x + y) found = {b - 1, want - over - x, y};
+  __syncthreads();
+  return found;
+}
+static_assert(kBins == 2 * kSelectThreads, "two bins a thread");
+
+// Writes the kept tokens of [c0, c1) to the list from `place` on: the protected ones, those above the border, and of those at it the first ones while `want` lasts; `equals` of them
+// came before.  none: no other than the protected.  A wave lists a run of tokens; how many the runs before it keep comes from a count first.
+__device__ inline void emit(const EvictArgs& a, int seq, int head, int32_t* kept, int c0, int c1, int lo, int hi, bool none, uint32_t border, int32_t want, int32_t place, int32_t equals) {
   __shared__ int32_t waves[2][kSelectWaves];
-  __shared__ uint32_t s_prefix;
-  __shared__ int32_t s_want;
-  const int seq = blockIdx.x / a.c.hkv, head = blockIdx.x % a.c.hkv, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int n = cached(a, seq), n_new = min(n, a.budget);
-  int32_t* const kept = a.kept + ((int64_t)seq * a.c.hkv + head) * a.budget;
-  if (head == 0 && tid == 0) a.new_len[seq] = n_new;
-  for (int i = n_new + tid; i < a.budget; i += kSelectThreads) kept[i] = -1;
-  if (n <= a.budget) {
-    for (int i = tid; i < n; i += kSelectThreads) kept[i] = i;
-    return;
-  }
-  // tokens lo .. hi - 1 compete for `want` places
-  const int lo = a.first, hi = n - a.recent;
-  int32_t want = a.budget - a.first - a.recent;
-  uint32_t prefix = 0;                             // upper bits of the last kept weight
-  for (int shift = 24; shift >= 0 && want > 0; shift -= 8) {
-    if (tid < 256) bins[tid] = 0;
-    __syncthreads();
-    for (int t = lo + tid; t < hi; t += kSelectThreads) {
-      const uint32_t u = order_at(a, seq, head, t);
-      if (shift == 24 || (u >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&bins[(u >> shift) & 255], 1);
-    }
-    __syncthreads();
-    // the bin that holds the want-th greatest: wave 0, four bins a lane, from the greatest down
-    if (wave == 0) {
-      int32_t mine[4], sum = 0;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int run = ((c1 - c0 + kSelectWaves - 1) / kSelectWaves + 255) & ~255, t0 = min(c0 + wave * run, c1), t1 = min(t0 + run, c1);
+  // of four tokens: bit j set if token t + j is kept whatever the others are, bit 4 + j if it lies at the border
+  auto look = [&](const Quad& q, int t) {
+    uint32_t r = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) sum += mine[i] = bins[255 - 4 * lane - i];
-      int32_t upto = wave_prefix_sum(sum), above = upto - sum;
-      if (above < want && want <= upto) {
-        int i = 0;
-        while (above + mine[i] < want) above += mine[i++];
-        s_prefix = prefix | (uint32_t)(255 - 4 * lane - i) << shift;
-        s_want = want - above;
-      }
+    for (int j = 0; j < 4; ++j) {
+      const bool in = t + j < t1, safe = t + j < lo || t + j >= hi;
+      r |= (uint32_t)(in && (safe || (!none && q.u[j] > border))) << j;
+      r |= (uint32_t)(in && !safe && !none && q.u[j] == border) << (4 + j);
     }
-    __syncthreads();
-    prefix = s_prefix;
-    want = s_want;
-  }
-  // kept: the protected, those above the border, and the first `want` at it.  A wave lists a run of tokens; how many the runs before it keep comes from a count first
-  const bool none = a.budget == a.first + a.recent;
-  const int run = ((n + kSelectWaves - 1) / kSelectWaves + 63) & ~63, t0 = min(wave * run, n), t1 = min(t0 + run, n);
+    return r;
+  };
+  constexpr int kUnroll = 2;
+  auto walk = [&](auto f) {
+    for (int t = t0 + 4 * lane; t - 4 * lane < t1; t += kUnroll * 256) {
+      int32_t page[kUnroll];
+      Quad q[kUnroll];
+#pragma unroll
+      for (int i = 0; i < kUnroll; ++i) page[i] = t + 256 * i < t1 ? page_at(a.s, a.c, seq, (t + 256 * i) >> a.c.log_page) : -1;
+#pragma unroll
+      for (int i = 0; i < kUnroll; ++i) q[i] = orders_of(a, page[i], head, t + 256 * i);
+#pragma unroll
+      for (int i = 0; i < kUnroll; ++i) f(look(q[i], t + 256 * i), t + 256 * i);
+    }
+  };
   int32_t above = 0, equal = 0;
-  for (int t = t0 + lane; t < t1; t += 64) {
-    const bool safe = t < lo || t >= hi;
-    const uint32_t u = safe || none ? 0 : order_at(a, seq, head, t);
-    above += safe || (!none && u > prefix);
-    equal += !safe && !none && u == prefix;
-  }
+  walk([&](uint32_t r, int) {
+    above += __popc(r & 15);
+    equal += __popc(r >> 4);
+  });
   above = __builtin_amdgcn_readlane(wave_prefix_sum(above), 63);
   equal = __builtin_amdgcn_readlane(wave_prefix_sum(equal), 63);
   if (lane == 0) { waves[0][wave] = above; waves[1][wave] = equal; }
   __syncthreads();
-  int32_t place = 0, equals = 0;                   // listed and equal ones before the run
   for (int w = 0; w < wave; ++w) {
     place += waves[0][w] + min(waves[1][w], max(want - equals, 0));
     equals += waves[1][w];
   }
-  const uint64_t below = ((uint64_t)1 << lane) - 1;
-  for (int t = t0 + lane; t - lane < t1; t += 64) {
-    const bool in = t < t1, safe = in && (t < lo || t >= hi);
-    const uint32_t u = !in || safe || none ? 0 : order_at(a, seq, head, t);
-    const bool eq = in && !safe && !none && u == prefix;
-    const uint64_t eqs = __ballot(eq);
-    const bool keep = safe || (in && !none && u > prefix) || (eq && equals + __popcll(eqs & below) < want);
-    const uint64_t keeps = __ballot(keep);
-    if (keep) kept[place + __popcll(keeps & below)] = t;
-    place += __popcll(keeps);
-    equals += __popcll(eqs);
+  walk([&](uint32_t r, int t) {
+    // equal ones before the lane's, then the kept ones before it
+    const int32_t eq = __popc(r >> 4), eq_upto = wave_prefix_sum(eq);
+    int32_t room = want - equals - (eq_upto - eq);  // places that are left for the lane's equal ones
+    uint32_t keep = r & 15;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (r >> (4 + j) & 1) {
+        if (room > 0) keep |= 1u << j;
+        --room;
+      }
+    const int32_t mine = __popc(keep), upto = wave_prefix_sum(mine);
+    int32_t to = place + upto - mine;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (keep >> j & 1) kept[to++] = t + j;
+    place += __builtin_amdgcn_readlane(upto, 63);
+    equals += __builtin_amdgcn_readlane(eq_upto, 63);
+  });
+}
+
+// What all blocks of a (sequence, KV head) begin with; the first writes the new length and the list's ends.  done: every token is kept.
+struct Select { int32_t n, lo, hi, want; int32_t* kept; bool done; };
+__device__ inline Select open_select(const EvictArgs& a, int seq, int head, bool writes) {
+  const int n = cached(a, seq), n_new = min(n, a.budget), tid = threadIdx.x;
+  int32_t* const kept = a.kept + ((int64_t)seq * a.c.hkv + head) * a.budget;
+  if (writes) {
+    if (head == 0 && tid == 0) a.new_len[seq] = n_new;
+    for (int i = n_new + tid; i < a.budget; i += kSelectThreads) kept[i] = -1;
+    if (n <= a.budget)
+      for (int i = tid; i < n; i += kSelectThreads) kept[i] = i;
+  }
+  return {n, a.first, n - a.recent, a.budget - a.first - a.recent, kept, n <= a.budget};
+}
+
+// Short tables: a block per (sequence, KV head).
+__global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictArgs a) {
+  __shared__ int32_t bins[kBins];
+  __shared__ uint32_t list[kListed];
+  __shared__ int32_t s_listed;
+  const int seq = blockIdx.x / a.c.hkv, head = blockIdx.x % a.c.hkv, tid = threadIdx.x, lane = tid & 63;
+  const Select z = open_select(a, seq, head, true);
+  if (z.done) return;
+  int32_t want = z.want, m = 0;
+  uint32_t border = 0;
+  if (want > 0) {
+    bins[tid] = bins[tid + kSelectThreads] = 0;
+    if (tid == 0) s_listed = 0;
+    __syncthreads();
+    for_weights<2>(a, seq, head, 0, z.hi, z.lo, z.hi, [&](uint32_t u, bool in) { count_in(bins, u >> 21, in); });
+    __syncthreads();
+    Found f = find_bin(bins, want);
+    for_weights<2>(a, seq, head, 0, z.hi, z.lo, z.hi, [&](uint32_t u, bool in) {
+      if (in && (int)(u >> 21) == f.bin) list[atomicAdd(&s_listed, 1)] = u;
+    });
+    border = (uint32_t)f.bin << 21;
+    want = f.want;
+    m = f.held;
+    for (int shift = 10; shift >= 0; shift -= 10) {        // bits 20 .. 10, then 9 .. 0
+      bins[tid] = bins[tid + kSelectThreads] = 0;
+      __syncthreads();
+      for (int i = tid; i - lane < m; i += kSelectThreads) {
+        const uint32_t u = i < m ? list[i] : 0;
+        const bool in = i < m && (shift == 10 || (u >> 10) == (border >> 10));
+        count_in(bins, shift == 10 ? (u >> 10) & 2047 : u & 1023, in);
+      }
+      __syncthreads();
+      f = find_bin(bins, want);
+      border |= (uint32_t)f.bin << shift;
+      want = f.want;
+    }
+  }
+  emit(a, seq, head, z.kept, 0, z.n, z.lo, z.hi, z.want == 0, border, want, 0, 0);
+}
+
+// Long tables, a block per (sequence and KV head, chunk).  First: the chunk's tokens by their upper 11 bits.
+__global__ __launch_bounds__(kSelectThreads) void count_kernel(EvictArgs a) {
+  __shared__ int32_t bins[kBins];
+  const int chunk = blockIdx.y, sh = blockIdx.x, seq = sh / a.c.hkv, head = sh % a.c.hkv, tid = threadIdx.x;
+  const Select z = open_select(a, seq, head, chunk == 0);
+  if (z.done || z.want == 0 || chunk * a.chunk >= z.n) return;
+  bins[tid] = bins[tid + kSelectThreads] = 0;
+  __syncthreads();
+  for_weights<2>(a, seq, head, chunk * a.chunk, (chunk + 1) * a.chunk, z.lo, z.hi, [&](uint32_t u, bool in) { count_in(bins, u >> 21, in); });
+  __syncthreads();
+  int32_t* const to = a.counts + ((int64_t)sh * a.chunks + chunk) * kBins;
+  to[tid] = bins[tid];
+  to[tid + kSelectThreads] = bins[tid + kSelectThreads];
+}
+
+// Second: the chunk's tokens that share the k-th greatest's upper bits, listed behind those of the chunks before; and how many tokens of the chunk lie above them.
+__global__ __launch_bounds__(kSelectThreads) void list_kernel(EvictArgs a) {
+  __shared__ int32_t bins[kBins];
+  __shared__ int32_t s_listed, s_above;
+  const int chunk = blockIdx.y, sh = blockIdx.x, seq = sh / a.c.hkv, head = sh % a.c.hkv, tid = threadIdx.x;
+  const Select z = open_select(a, seq, head, false);
+  if (z.done || z.want == 0 || chunk * a.chunk >= z.n) return;
+  const int used = (z.n + a.chunk - 1) / a.chunk;
+  const int32_t* const counts = a.counts + (int64_t)sh * a.chunks * kBins;
+  int32_t x = 0, y = 0;
+#pragma unroll 8
+  for (int c = 0; c < used; ++c) {
+    x += counts[(int64_t)c * kBins + tid];
+    y += counts[(int64_t)c * kBins + tid + kSelectThreads];
+  }
+  bins[tid] = x;
+  bins[tid + kSelectThreads] = y;
+  if (tid == 0) s_listed = s_above = 0;
+  __syncthreads();
+  const Found f = find_bin(bins, z.want);
+  int32_t base = 0;
+  for (int c = 0; c < chunk; ++c) base += counts[(int64_t)c * kBins + f.bin];
+  const int32_t* const own = counts + (int64_t)chunk * kBins;
+  const int32_t above = (tid > f.bin ? own[tid] : 0) + (tid + kSelectThreads > f.bin ? own[tid + kSelectThreads] : 0);
+  if (above) atomicAdd(&s_above, above);
+  uint32_t* const list = a.list + (int64_t)sh * a.s.max_pages * a.c.page + base;
+  for_weights<2>(a, seq, head, chunk * a.chunk, (chunk + 1) * a.chunk, z.lo, z.hi, [&](uint32_t u, bool in) {
+    if (in && (int)(u >> 21) == f.bin) list[atomicAdd(&s_listed, 1)] = u;
+  });
+  __syncthreads();
+  if (tid == 0) {
+    a.above[(int64_t)sh * a.chunks + chunk] = s_above;
+    if (chunk == 0) {
+      int32_t* const b = a.border + (int64_t)sh * 4;
+      b[0] = f.bin;
+      b[1] = f.want;
+      b[2] = f.held;
+    }
   }
 }
 
-template <int D, int Fmt>
+// Third: the border among the candidates, and the chunk's part of the list.
+__global__ __launch_bounds__(kSelectThreads) void emit_kernel(EvictArgs a) {
+  __shared__ int32_t bins[kBins];
+  __shared__ int32_t s_above, s_equal;
+  const int chunk = blockIdx.y, sh = blockIdx.x, seq = sh / a.c.hkv, head = sh % a.c.hkv, tid = threadIdx.x, lane = tid & 63;
+  const Select z = open_select(a, seq, head, false);
+  const int c0 = chunk * a.chunk, c1 = min(c0 + a.chunk, z.n);
+  if (z.done || c0 >= z.n) return;
+  // the protected before the chunk
+  int32_t place = min(c0, z.lo) + max(c0 - z.hi, 0), want = z.want, equals = 0;
+  uint32_t border = 0;
+  if (want > 0) {
+    const int32_t* const b = a.border + (int64_t)sh * 4;
+    const int32_t m = b[2];
+    border = (uint32_t)b[0] << 21;
+    want = b[1];
+    const uint32_t* const list = a.list + (int64_t)sh * a.s.max_pages * a.c.page;
+    for (int shift = 10; shift >= 0; shift -= 10) {        // bits 20 .. 10, then 9 .. 0
+      bins[tid] = bins[tid + kSelectThreads] = 0;
+      if (tid == 0) s_above = s_equal = 0;
+      __syncthreads();
+#pragma unroll 4
+      for (int i = tid; i - lane < m; i += kSelectThreads) {
+        const uint32_t u = i < m ? list[i] : 0;
+        const bool in = i < m && (shift == 10 || (u >> 10) == (border >> 10));
+        count_in(bins, shift == 10 ? (u >> 10) & 2047 : u & 1023, in);
+      }
+      __syncthreads();
+      const Found f = find_bin(bins, want);
+      border |= (uint32_t)f.bin << shift;
+      want = f.want;
+    }
+    // candidates of the chunks before that are kept, and all of their tokens above the candidates
+    const int32_t* const counts = a.counts + (int64_t)sh * a.chunks * kBins;
+    int32_t before = 0;
+    for (int c = 0; c < chunk; ++c) {
+      before += counts[(int64_t)c * kBins + b[0]];
+      place += a.above[(int64_t)sh * a.chunks + c];
+    }
+    int32_t above = 0, equal = 0;
+    for (int i = tid; i < before; i += kSelectThreads) {
+      const uint32_t u = list[i];
+      above += u > border;
+      equal += u == border;
+    }
+    above = __builtin_amdgcn_readlane(wave_prefix_sum(above), 63);
+    equal = __builtin_amdgcn_readlane(wave_prefix_sum(equal), 63);
+    if (lane == 0 && above) atomicAdd(&s_above, above);
+    if (lane == 0 && equal) atomicAdd(&s_equal, equal);
+    __syncthreads();
+    equals = s_equal;
+    place += s_above + min(equals, want);
+  }
+  emit(a, seq, head, z.kept, c0, c1, z.lo, z.hi, z.want == 0, border, want, place, equals);
+}
+
+// Lane `from`'s value; with one row of lanes in a wave the number is the same for all.
+template <int TPW> __device__ inline int32_t pick(int32_t x, int from) { return TPW == 1 ? __builtin_amdgcn_readlane(x, from) : __shfl(x, from); }
+template <int TPW> __device__ inline float pick(float x, int from) { return __int_as_float(pick<TPW>(__float_as_int(x), from)); }
+
+// Codes of a word (four tokens of a channel, or four channels of a token) in other units: the largest magnitude (in units 2^16 times as large, which no value leaves), and
+// the codes.  A token's scale is multiplied in 2^-16 times.  NaN is no magnitude, and stays.
+constexpr float kFar = 0x1p-16f;
+template <int Fmt>
+__device__ inline float largest(uint32_t w, float s0, float s1, float s2, float s3, float top) {
+  const f32x2 a = decode_half<Fmt, false>(w), b = decode_half<Fmt, true>(w);
+  top = fmaxf(fmaxf(top, fabsf(a[0] * s0)), fabsf(a[1] * s1));
+  return fmaxf(fmaxf(top, fabsf(b[0] * s2)), fabsf(b[1] * s3));
+}
+template <int Fmt>
+__device__ inline uint32_t in_units(uint32_t w, float s0, float s1, float s2, float s3) {
+  const f32x2 a = decode_half<Fmt, false>(w), b = decode_half<Fmt, true>(w);
+  return encode_half<Fmt, true>(b[0] * s2, b[1] * s3, encode_half<Fmt, false>(a[0] * s0, a[1] * s1, 0));
+}
+
+// A wave per (new page, KV head, keys or values).  Lane j first finds where slot j's token lies and its scale, so that the tokens' codes can all be asked for at
+// once; they stay in registers until the page's scale is known.  Keys move as 16 bytes of a row; of the values, which lie 16 tokens together, a lane takes single bytes of
+// two channels and keeps them in the order in which they leave.  Groups: of 16 slots in a page.
+template <int D, int Fmt, int Groups>
 __global__ __launch_bounds__(256) void move_kernel(EvictArgs a) {
-  constexpr int LPR = D / 2, TPW = 64 / LPR;
+  constexpr int P = Groups * kGroup, kPer = (P + 63) / 64;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int job = blockIdx.y * 4 + wave;
   if (job >= 2 * a.c.hkv) return;
-  const int head = job >> 1, P = a.c.page, seq = blockIdx.x / a.max_new, place = blockIdx.x % a.max_new;
+  const int head = job >> 1, seq = blockIdx.x / a.max_new, place = blockIdx.x % a.max_new;
   const bool value = job & 1;
   const int n_new = min(cached(a, seq), a.budget), count = min(P, n_new - place * P);
   if (count <= 0) return;
   const int32_t page = a.new_pages[(int64_t)seq * a.max_new + place];
   if ((uint32_t)page >= (uint32_t)a.c.n_pages) return;
   const int32_t* const kept = a.kept + ((int64_t)seq * a.c.hkv + head) * a.budget + place * P;
-  const int sub = lane / LPR, ch = 2 * (lane % LPR);
-  const uint8_t* const from = value ? a.c.v : a.c.k;
-  const float* const scales = value ? a.c.v_scale : a.c.k_scale;
-  // the lane's two channels of the token in slot j, as they stand (0 past the last and where a page is missing)
-  auto fetch = [&](int j) -> f32x2 {
-    if (j >= count) return f32x2{0.f, 0.f};
-    const int t = kept[j];
-    const int32_t p = page_at(a.s, a.c, seq, t >> a.c.log_page);
-    if (p < 0) return f32x2{0.f, 0.f};
-    const int64_t block = block_of(a.c, p, head);
-    const int slot = t & (P - 1);
-    const float s = scales[block];
-    uint32_t two;
-    if (!value) {
-      two = *reinterpret_cast<const uint16_t*>(from + (block * P + slot) * D + ch);
-    } else {
-      const uint8_t* b = from + (block * P + (slot & ~(kGroup - 1))) * D + ch * kGroup + (slot & (kGroup - 1));
-      two = b[0] | (uint32_t)b[kGroup] << 8;
-    }
-    const f32x2 f = decode2<Fmt>(two);
-    return f32x2{f[0] * s, f[1] * s};
-  };
-  float top = 0.f;
-#pragma unroll 4
-  for (int j = sub; j < count; j += TPW) {
-    const f32x2 f = fetch(j);
-    const float x = fabsf(f[0]), y = fabsf(f[1]);
-    top = fmaxf(top, fmaxf(x < INFINITY ? x : 0.f, y < INFINITY ? y : 0.f));
-  }
-  const int e = exponent_for<Fmt>(wave_maxf(top));
-  const float to_units = power2(-e);
   const int64_t block = block_of(a.c, page, head);
-  if (lane == 0) (value ? a.c.v_scale : a.c.k_scale)[block] = power2(e);
+  // slot lane + 64 i: token's page, slot there, scale; past the last token and where a page is missing: scale 0
+  int32_t from_page[kPer], from_slot[kPer];
+  float scale[kPer];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int j = lane + 64 * i;
+    const int t = j < count ? kept[j] : 0;
+    const int32_t p = j < count ? page_at(a.s, a.c, seq, t >> a.c.log_page) : -1;
+    from_page[i] = max(p, 0);
+    from_slot[i] = t & (P - 1);
+    const int64_t b = block_of(a.c, from_page[i], head);
+    const float s = (value ? a.c.v_scale : a.c.k_scale)[b];
+    scale[i] = p < 0 ? 0.f : s;
+    if (!value && j < P) a.c.weight[block * P + j] = p < 0 ? 0.f : a.c.weight[b * P + from_slot[i]];
+  }
   uint8_t* const codes = (value ? a.c.v : a.c.k) + block * P * D;
+  float top = 0.f;
   if (!value) {
-#pragma unroll 4
-    for (int j = sub; j < P; j += TPW) {
-      const f32x2 f = fetch(j);
-      *reinterpret_cast<uint16_t*>(codes + j * D + ch) = (uint16_t)encode2<Fmt>(f[0] * to_units, f[1] * to_units);
+    constexpr int LPR = D / 16, RPI = 64 / LPR, N = (P + RPI - 1) / RPI;       // lanes of a row, rows of a load, loads
+    const int sub = lane / LPR, ch = 16 * (lane % LPR);
+    u32x4 w[N];
+    float s[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int slot = min(RPI * i + sub, P - 1);
+      const int32_t fp = __shfl(from_page[RPI * i / 64], slot & 63), fs = __shfl(from_slot[RPI * i / 64], slot & 63);
+      s[i] = __shfl(scale[RPI * i / 64], slot & 63);
+      w[i] = *reinterpret_cast<const u32x4*>(a.c.k + (block_of(a.c, fp, head) * P + fs) * D + ch);
     }
-    for (int j = lane; j < P; j += 64) {
-      float w = 0.f;
-      if (j < count) {
-        const int t = kept[j];
-        const int32_t p = page_at(a.s, a.c, seq, t >> a.c.log_page);
-        if (p >= 0) w = a.c.weight[block_of(a.c, p, head) * P + (t & (P - 1))];
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        w[i][j] = s[i] == 0.f ? 0u : w[i][j];
+        const float f = s[i] * kFar;
+        top = largest<Fmt>(w[i][j], f, f, f, f, top);
       }
-      a.c.weight[block * P + j] = w;
+    top = wave_maxf(top);
+    const int e = exponent_for<Fmt>(top, 16);
+    if (lane == 0) a.c.k_scale[block] = power2(e);
+    const float to_units = power2(-e);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int slot = RPI * i + sub;
+      const float f = fmaxf(s[i] * to_units, 0x1p-126f);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[i][j] = in_units<Fmt>(w[i][j], f, f, f, f);
+      if (slot < P) *reinterpret_cast<u32x4*>(codes + slot * D + ch) = w[i];
     }
   } else {
-    for (int g = sub; g * kGroup < P; g += TPW) {
-      u32x4 w0 = {0, 0, 0, 0}, w1 = {0, 0, 0, 0};
+    constexpr int LPR = D / 2, TPW = 64 / LPR, N = (Groups + TPW - 1) / TPW;   // lanes of a token, groups of a step, steps
+    const int sub = lane / LPR, ch = 2 * (lane % LPR);
+    u32x4 w[N][2];
 #pragma unroll
-      for (int j = 0; j < kGroup; ++j) {
-        const f32x2 f = fetch(g * kGroup + j);
-        const uint32_t two = encode2<Fmt>(f[0] * to_units, f[1] * to_units);
-        w0[j / 4] |= (two & 0xffu) << (8 * (j % 4));
-        w1[j / 4] |= (two >> 8) << (8 * (j % 4));
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        uint32_t w0 = 0, w1 = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int slot = min((sub + TPW * i) * kGroup + 4 * q + j, P - 1), at = TPW * i * kGroup / 64;
+          const int32_t fp = pick<TPW>(from_page[at], slot & 63), fs = pick<TPW>(from_slot[at], slot & 63);
+          const uint8_t* v = a.c.v + (block_of(a.c, fp, head) * P + (fs & ~(kGroup - 1))) * D + (fs & (kGroup - 1)) + ch * kGroup;
+          w0 |= (uint32_t)v[0] << (8 * j);
+          w1 |= (uint32_t)v[kGroup] << (8 * j);
+        }
+        w[i][0][q] = w0;
+        w[i][1][q] = w1;
       }
-      u32x4* const c = reinterpret_cast<u32x4*>(codes + (g * D + ch) * kGroup);
-      c[0] = w0;
-      c[1] = w1;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        float s[4];
+        uint32_t gone = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          s[j] = pick<TPW>(scale[TPW * i * kGroup / 64], min((sub + TPW * i) * kGroup + 4 * q + j, P - 1) & 63);
+          gone |= s[j] == 0.f ? 0xffu << (8 * j) : 0u;
+          s[j] *= kFar;
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          w[i][c][q] &= ~gone;
+          top = largest<Fmt>(w[i][c][q], s[0], s[1], s[2], s[3], top);
+        }
+      }
+    top = wave_maxf(top);
+    const int e = exponent_for<Fmt>(top, 16);
+    if (lane == 0) a.c.v_scale[block] = power2(e);
+    const float to_units = power2(-e);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int g = sub + TPW * i;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        float s[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[j] = fmaxf(pick<TPW>(scale[TPW * i * kGroup / 64], min(g * kGroup + 4 * q + j, P - 1) & 63) * to_units, 0x1p-126f);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) w[i][c][q] = in_units<Fmt>(w[i][c][q], s[0], s[1], s[2], s[3]);
+      }
+      if (g < Groups) {
+        u32x4* const y = reinterpret_cast<u32x4*>(codes + (g * D + ch) * kGroup);
+        y[0] = w[i][0];
+        y[1] = w[i][1];
+      }
     }
   }
 }
 
+template <int D, int Fmt>
+void launch_move(const EvictArgs& a, dim3 grid, hipStream_t st) {
+  auto kernel = a.c.page == 16 ? move_kernel<D, Fmt, 1> : a.c.page == 32 ? move_kernel<D, Fmt, 2> : a.c.page == 64 ? move_kernel<D, Fmt, 4> : move_kernel<D, Fmt, 8>;
+  kernel<<<grid, dim3(256), 0, st>>>(a);
+}
+
+// Where the parts of scratch lie.  A table of up to kListed tokens needs none of them.
+struct EvictPlan { int32_t chunk, chunks; size_t counts, list, above, border, bytes; };
+EvictPlan plan_evict(const CacheView& c, int32_t n_seqs, int32_t max_pages) {
+  EvictPlan p = {};
+  const int64_t room = (int64_t)max_pages * c.page, lists = (int64_t)n_seqs * c.hkv;
+  if (room <= kListed) { p.bytes = 256; return p; }
+  const int64_t step = 4 * kSelectThreads;
+  p.chunk = (int32_t)(((room + kMaxChunks - 1) / kMaxChunks + step - 1) / step * step);
+  if (p.chunk < 2 * step) p.chunk = 2 * step;
+  p.chunks = (int32_t)((room + p.chunk - 1) / p.chunk);
+  p.list = pad_to((size_t)lists * p.chunks * kBins * 4, 256);
+  p.above = p.list + pad_to((size_t)lists * room * 4, 256);
+  p.border = p.above + pad_to((size_t)lists * p.chunks * 4, 256);
+  p.bytes = p.border + pad_to((size_t)lists * 16, 256);
+  return p;
+}
+
 }  // namespace
 
-size_t evict_scratch_bytes(const CacheView&, int32_t, int32_t) { return 256; }
+size_t evict_scratch_bytes(const CacheView& c, int32_t n_seqs, int32_t max_pages) { return plan_evict(c, n_seqs, max_pages).bytes; }
 
 }  // namespace fcp
 
@@ -217,9 +521,11 @@ extern "C" int fcp_cache_evict(const fcp_cache* cache, const int32_t* pages, con
   if ((int64_t)max_new_pages * a.c.page < most)
     return fail(FCP_ERR_CAPACITY, "%s: %d new pages of %d tokens for up to %lld", who, max_new_pages, a.c.page, (long long)most);
   if (!scratch || (uintptr_t)scratch % 256) return fail(FCP_ERR_INVALID_ARG, "%s: scratch must be 256-byte aligned", who);
-  const size_t need = evict_scratch_bytes(a.c, n_seqs, max_pages);
+  const EvictPlan p = plan_evict(a.c, n_seqs, max_pages);
+  const size_t need = p.bytes;
   if (scratch_bytes < need) return fail(FCP_ERR_CAPACITY, "%s: scratch has %zu bytes, %zu are needed", who, scratch_bytes, need);
   const int64_t use = (most + a.c.page - 1) / a.c.page;      // (further entries of new_pages are not used)
+  if (room > 1 << 30) return fail(FCP_ERR_UNSUPPORTED, "%s: a table of more than 2^30 tokens", who);
   if ((int64_t)n_seqs * a.c.hkv > INT32_MAX || (int64_t)n_seqs * max_new_pages > INT32_MAX)
     return fail(FCP_ERR_UNSUPPORTED, "%s: more than 2^31 - 1 pages or heads of all sequences", who);
   a.s = {nullptr, kv_len, pages, n_seqs, max_pages, 0};
@@ -231,13 +537,28 @@ extern "C" int fcp_cache_evict(const fcp_cache* cache, const int32_t* pages, con
   a.kept = kept;
   a.new_len = new_len;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  select_kernel<<<dim3((unsigned)(n_seqs * a.c.hkv)), dim3(kSelectThreads), 0, st>>>(a);
+  if (p.chunks == 0) {
+    select_kernel<<<dim3((unsigned)(n_seqs * a.c.hkv)), dim3(kSelectThreads), 0, st>>>(a);
+  } else {
+    char* const area = static_cast<char*>(scratch);
+    a.chunk = p.chunk;
+    a.chunks = p.chunks;
+    a.counts = reinterpret_cast<int32_t*>(area + p.counts);
+    a.list = reinterpret_cast<uint32_t*>(area + p.list);
+    a.above = reinterpret_cast<int32_t*>(area + p.above);
+    a.border = reinterpret_cast<int32_t*>(area + p.border);
+    const dim3 grid((unsigned)(n_seqs * a.c.hkv), (unsigned)p.chunks);
+    count_kernel<<<grid, dim3(kSelectThreads), 0, st>>>(a);
+    FCP_HIP_CHECK(hipGetLastError());
+    list_kernel<<<grid, dim3(kSelectThreads), 0, st>>>(a);
+    FCP_HIP_CHECK(hipGetLastError());
+    emit_kernel<<<grid, dim3(kSelectThreads), 0, st>>>(a);
+  }
   FCP_HIP_CHECK(hipGetLastError());
   if (use == 0) return FCP_OK;
   const dim3 grid((unsigned)(n_seqs * max_new_pages), (unsigned)((2 * a.c.hkv + 3) / 4));
   const bool e4m3 = cache->format == FCP_CACHE_E4M3;
-  auto kernel = cache->head_dim == 128 ? (e4m3 ? move_kernel<128, kE4m3> : move_kernel<128, kInt8>) : (e4m3 ? move_kernel<64, kE4m3> : move_kernel<64, kInt8>);
-  kernel<<<grid, dim3(256), 0, st>>>(a);
+  (cache->head_dim == 128 ? (e4m3 ? launch_move<128, kE4m3> : launch_move<128, kInt8>) : (e4m3 ? launch_move<64, kE4m3> : launch_move<64, kInt8>))(a, grid, st);
   FCP_HIP_CHECK(hipGetLastError());
   return FCP_OK;
 }

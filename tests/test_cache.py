@@ -343,7 +343,8 @@ def test_attention_repeats_and_follows_its_tables_in_a_graph(news):
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("P,D,hkv,kv_len,budget,first,recent", [
     (16, 64, 2, [1], 1, 0, 0), (16, 64, 2, [100, 40, 0, 41], 40, 2, 8), (64, 128, 1, [700], 65, 0, 1), (32, 128, 3, [333, 64, 90], 64, 4, 60),
-    (128, 64, 2, [1000, 129], 300, 8, 100), (64, 64, 1, [5000], 1111, 4, 200), (16, 128, 2, [77, 77], 77, 0, 77), (16, 64, 1, [60], 17, 0, 0)])
+    (128, 64, 2, [1000, 129], 300, 8, 100), (64, 64, 1, [5000], 1111, 4, 200), (16, 128, 2, [77, 77], 77, 0, 77), (16, 64, 1, [60], 17, 0, 0),
+    (32, 64, 2, [40000, 30, 16389, 9001], 9000, 5, 100), (128, 64, 1, [33000], 32000, 0, 0), (16, 64, 1, [70001, 69000], 20, 4, 16)])
 def test_evict(P, D, hkv, kv_len, budget, first, recent, fmt):
     import torch
     rng = np.random.default_rng(budget)
@@ -370,6 +371,30 @@ def test_evict(P, D, hkv, kv_len, budget, first, recent, fmt):
     assert np.array_equal(kept.cpu().numpy(), want_kept)
     w = R.check_content(cache, ref)
     assert np.array_equal(w, ref.weight.astype(np.float32), equal_nan=True)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [5000, 30000])
+@pytest.mark.parametrize("kind", ["equal", "two", "near"])
+def test_evict_of_weights_that_share_their_upper_bits(n, kind):
+    """One value, two values, and values whose upper bits are all alike: the kept are the greatest, and of equal ones the lowest."""
+    import torch
+    P, D, budget, first, recent = 64, 64, n // 3, 3, 50
+    counts, new = -(-n // P), -(-budget // P)
+    rng = np.random.default_rng(n)
+    w = {"equal": np.zeros(n), "two": rng.integers(0, 2, n) * 0.5, "near": 1 + rng.integers(0, 3000, n) * 2.0 ** -23}[kind].astype(np.float32)
+    weight = np.zeros((counts + new, 1, P), np.float32)
+    weight.reshape(-1)[:n] = w
+    z = lambda *s, dt=torch.int8: torch.zeros(*s, dtype=dt, device="cuda")
+    cache = B.Cache(z(counts + new, 1, P, D), z(counts + new, 1, P // 16, D, 16), z(counts + new, 1, dt=torch.float32) + 1, z(counts + new, 1, dt=torch.float32) + 1,
+                    torch.from_numpy(weight).cuda())
+    pages, new_pages = dev(np.arange(counts)[None]), dev(np.arange(counts, counts + new)[None])
+    kept, new_len = z(1, 1, budget, dt=torch.int32), z(1, dt=torch.int32)
+    scratch = torch.full((B.fcp_cache_scratch_bytes(B.FCP_SCRATCH_CACHE_EVICT, cache, 1, counts),), 255, dtype=torch.uint8, device="cuda")
+    B.fcp_cache_evict(cache, pages, dev([n]), new_pages, budget, first, recent, kept, new_len, scratch)
+    order = np.argsort(-w[first: n - recent], kind="stable")[: budget - first - recent] + first
+    assert np.array_equal(kept.cpu().numpy()[0, 0], np.sort(np.concatenate([np.arange(first), order, np.arange(n - recent, n)])))
+    assert np.array_equal(cache.weight.cpu().numpy()[counts:].reshape(-1)[:budget], w[kept.cpu().numpy()[0, 0]])
 
 
 @pytest.mark.gpu
