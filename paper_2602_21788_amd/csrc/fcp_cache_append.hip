@@ -3,8 +3,8 @@
 // A unit is one page that gets new tokens, for one KV head, keys or values: a wave works it alone, since all of the page's codes share one
 // scale 2^e, e the least exponent that holds the largest magnitude.  Reads 2 bytes and writes 1 per element: the memory bounds long prompts, the chain
 // table -> page -> scale -> codes single tokens.
-// A lane owns two neighbouring channels.  Key rows are written as they come; for the values a lane collects a group of 16 tokens, which in the
-// cache's order is 16 bytes for each of its channels, so the transposition costs nothing.
+// The page's new rows stay in registers while their scale is found.  Key rows are written as they come; of the values a lane holds a group of 16 tokens of two
+// channels, which in the cache's order are 16 bytes for each, so the transposition costs nothing.
 #include "fcp_cache.h"
 
 namespace fcp {
@@ -21,104 +21,238 @@ struct AppendArgs {
 // Which sequence holds unit u: units are numbered so that a sequence's begin at cu / page + 2 seq, which leaves every sequence room for all pages that its rows
 // can touch, (n - 1) / page + 2 at most.  The numbers grow with the sequence: a search, 64 ways at a time.
 __device__ inline int64_t first_unit(const SeqView& s, int log_page, int seq) { return (int64_t)(min(max(s.cu[seq], 0), s.n_rows) >> log_page) + 2 * (int64_t)seq; }
-__device__ inline int seq_of_unit(const SeqView& s, int log_page, int u) {
+struct UnitSeq { int32_t seq; int64_t first_unit; SeqSizes z; };
+__device__ inline UnitSeq seq_of_unit(const SeqView& s, int log_page, int u) {
+  const int lane = threadIdx.x & 63;
+  if (s.n_seqs <= 64) {
+    // a sequence per lane, all of its numbers at once: with the search and then its sizes a single token's chain of loads is one longer
+    const int i = min(lane, s.n_seqs - 1);
+    const SeqSizes z = seq_sizes(s, i, 1 << log_page);
+    const int64_t first = first_unit(s, log_page, i);
+    const int k = max((int)__popcll(__ballot(lane < s.n_seqs && first <= u)) - 1, 0);
+    return {k, (int64_t)__builtin_amdgcn_readlane((int32_t)first, k), {__builtin_amdgcn_readlane(z.row0, k), __builtin_amdgcn_readlane(z.n, k), __builtin_amdgcn_readlane(z.len, k)}};
+  }
   int lo = 0, n = s.n_seqs;                        // the sequence is in lo .. lo + n - 1
   while (n > 1) {
-    const int step = (n + 63) / 64, at = lo + (int)(threadIdx.x & 63) * step;
+    const int step = (n + 63) / 64, at = lo + lane * step;
     const bool below = at < lo + n && first_unit(s, log_page, at) <= u;
     const int k = __popcll(__ballot(below)) - 1;   // (true for a run of lanes from the first on; lane 0's always is)
     const int next = lo + max(k, 0) * step;
     n = min(step, lo + n - next);
     lo = next;
   }
-  return lo;
+  return {lo, first_unit(s, log_page, lo), seq_sizes(s, lo, 1 << log_page)};
 }
 
-template <int D, int Fmt>
-__global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
-  constexpr int LPR = D / 2, TPW = 64 / LPR;       // lanes of a row; rows (keys), groups (values) a wave works at a time
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int job = blockIdx.y * 4 + wave;           // (KV head, keys or values)
-  if (job >= 2 * a.c.hkv) return;
-  const int head = job >> 1, P = a.c.page, u = blockIdx.x;
-  const bool value = job & 1;
-  const int seq = seq_of_unit(a.s, a.c.log_page, u);
-  const SeqSizes z = seq_sizes(a.s, seq, P);
-  // tokens len - n .. len - 1; those before the first slot (a caller's error) are not written
-  const int64_t first = (int64_t)z.len - z.n;
-  if (z.n == 0 || z.len == 0) return;
-  const int32_t place = (int32_t)((first > 0 ? first : 0) >> a.c.log_page) + (int32_t)(u - first_unit(a.s, a.c.log_page, seq));
-  const int64_t t0 = (int64_t)place << a.c.log_page;
-  if (t0 >= z.len) return;
-  const int32_t page = page_at(a.s, a.c, seq, place);
-  if (page < 0) return;
-  const int lo = (int)max(first - t0, (int64_t)0), hi = (int)min((int64_t)P, z.len - t0);
-  const int sub = lane / LPR, ch = 2 * (lane % LPR);
-  // row of slot j: row0 + (t0 + j - first)
-  const __bf16* const x = a.x[value] + ((int64_t)z.row0 + t0 - first) * a.row[value] + head * D + ch;
-  const int64_t block = block_of(a.c, page, head);
-  uint8_t* const codes = (value ? a.c.v : a.c.k) + block * P * D;
-  float* const scale = (value ? a.c.v_scale : a.c.k_scale) + block;
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 
-  // largest finite magnitude: bf16 magnitudes are ordered as integers
-  uint32_t top = 0;
-#pragma unroll 8
-  for (int j = lo + sub; j < hi; j += TPW) {
-    const uint32_t w = *reinterpret_cast<const uint32_t*>(x + j * a.row[value]);
-    const uint32_t p = w & 0x7fffu, q = (w >> 16) & 0x7fffu;
-    top = max(top, max(p < 0x7f80u ? p : 0u, q < 0x7f80u ? q : 0u));
+// Largest of the finite magnitudes in a word of two bf16; these are ordered as integers.
+__device__ inline uint32_t finite2(uint32_t w) {
+  const uint32_t p = w & 0x7fffu, q = (w >> 16) & 0x7fffu;
+  return max(p < 0x7f80u ? p : 0u, q < 0x7f80u ? q : 0u);
+}
+__device__ inline uint32_t wave_max16(uint32_t x) {
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) x = max(x, (uint32_t)__shfl_xor((int)x, d));
+  return x;
+}
+// Two bf16 as codes in the lower 16 bits.  Odd: there are values that are not finite.
+template <int Fmt, bool Odd>
+__device__ inline uint32_t code2(uint32_t w, float to_units) {
+  const float a = __uint_as_float(w << 16) * to_units, b = __uint_as_float(w & 0xffff0000u) * to_units;
+  return Odd ? encode2<Fmt>(a, b) : encode_half<Fmt, false>(a, b, 0) & 0xffffu;
+}
+
+// The largest finite magnitude of a wave's words w[0 .. N - 1] of bf16 pairs as a float; odd: some are not finite.
+template <int N>
+__device__ inline float top_of(const uint32_t (&w)[N], bool& odd) {
+  u16x2 t = {0, 0};
+#pragma unroll
+  for (int i = 0; i < N; ++i) t = __builtin_elementwise_max(t, __builtin_bit_cast(u16x2, w[i] & 0x7fff7fffu));
+  uint32_t top = wave_max16(max((uint32_t)t[0], (uint32_t)t[1]));
+  odd = top >= 0x7f80u;
+  if (odd) {                                       // rare: once more without them
+    top = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) top = max(top, finite2(w[i]));
+    top = wave_max16(top);
   }
-  int e = exponent_for<Fmt>(wave_maxf(__uint_as_float(top << 16)));
-  float again = 1.f;                               // units of the earlier tokens' codes, in new units
-  if (lo > 0) {
+  return __uint_as_float(top << 16);
+}
+
+// Exponent of the page's scale after new values of magnitude `top`, and the earlier tokens' units in the new ones (1: they stay as they are).
+template <int Fmt>
+__device__ inline int grow(float top, bool earlier, float* scale, float& again) {
+  int e = exponent_for<Fmt>(top);
+  again = 1.f;
+  if (earlier) {
     const int before = exponent_of(*scale);
     e = max(e, before);
     again = power2(before - e);
   }
-  const float to_units = power2(-e);
-  if (lane == 0) *scale = power2(e);
+  if ((threadIdx.x & 63) == 0) *scale = power2(e);
+  return e;
+}
 
+template <int D, int Fmt, int Groups>
+__global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
+  constexpr int P = Groups * kGroup;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int job = blockIdx.y * 4 + wave;           // (KV head, keys or values)
+  if (job >= 2 * a.c.hkv) return;
+  const int head = job >> 1, u = blockIdx.x;
+  const bool value = job & 1;
+  const UnitSeq of = seq_of_unit(a.s, a.c.log_page, u);
+  const int seq = of.seq;
+  const SeqSizes z = of.z;
+  // tokens len - n .. len - 1; those before the first slot (a caller's error) are not written
+  const int64_t first = (int64_t)z.len - z.n;
+  if (z.n == 0 || z.len == 0) return;
+  const int32_t place = (int32_t)((first > 0 ? first : 0) >> a.c.log_page) + (int32_t)(u - of.first_unit);
+  const int64_t t0 = (int64_t)place * P;
+  if (t0 >= z.len) return;
+  const int32_t page = page_at(a.s, a.c, seq, place);
+  if (page < 0) return;
+  const int lo = __builtin_amdgcn_readfirstlane((int)max(first - t0, (int64_t)0)), hi = __builtin_amdgcn_readfirstlane((int)min((int64_t)P, z.len - t0));
+  const int64_t row = a.row[value];
+  // row of slot j: row0 + (t0 + j - first)
+  const __bf16* const x = a.x[value] + ((int64_t)z.row0 + t0 - first) * row + head * D;
+  const int64_t block = block_of(a.c, page, head);
+  uint8_t* const codes = (value ? a.c.v : a.c.k) + block * P * D;
+  bool odd;
+  float again;
   if (!value) {
+    // a lane: eight channels of a row, every RPI-th row.  Slots that get no new row repeat the nearest one that does, which changes no maximum.
+    constexpr int LPR = D / 8, RPI = 64 / LPR, N = P / RPI;
+    const int sub = lane / LPR, ch = 8 * (lane % LPR);
+    uint32_t w[4 * N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      u32x4 r = {0, 0, 0, 0};
+      if (RPI * i < hi && RPI * (i + 1) > lo) r = *reinterpret_cast<const u32x4*>(x + min(max(RPI * i + sub, lo), hi - 1) * row + ch);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w[4 * i + j] = r[j];
+    }
+    const float top = top_of(w, odd);
+    const int e = grow<Fmt>(top, lo > 0, a.c.k_scale + block, again);
+    const float to_units = power2(-e);
     if (again != 1.f)
-      for (int j = sub; j < lo; j += TPW) {
-        uint16_t* const c = reinterpret_cast<uint16_t*>(codes + j * D + ch);
-        const f32x2 f = decode2<Fmt>(*c);
-        *c = (uint16_t)encode2<Fmt>(f[0] * again, f[1] * again);
+#pragma unroll 1
+      for (int j = sub; j < lo; j += RPI) {
+        uint32_t* const c = reinterpret_cast<uint32_t*>(codes + j * D + ch);
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          const f32x2 f = decode_half<Fmt, false>(c[q]), g = decode_half<Fmt, true>(c[q]);
+          c[q] = encode2<Fmt>(f[0] * again, f[1] * again) | encode2<Fmt>(g[0] * again, g[1] * again) << 16;
+        }
       }
-#pragma unroll 8
-    for (int j = lo + sub; j < hi; j += TPW) {
-      const uint32_t w = *reinterpret_cast<const uint32_t*>(x + j * a.row[0]);
-      *reinterpret_cast<uint16_t*>(codes + j * D + ch) = (uint16_t)encode2<Fmt>(__uint_as_float(w << 16) * to_units, __uint_as_float(w & 0xffff0000u) * to_units);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int slot = RPI * i + sub;
+      u32x2 c;
+#pragma unroll
+      for (int q = 0; q < 2; ++q)
+        c[q] = odd ? code2<Fmt, true>(w[4 * i + 2 * q], to_units) | code2<Fmt, true>(w[4 * i + 2 * q + 1], to_units) << 16
+                   : code2<Fmt, false>(w[4 * i + 2 * q], to_units) | code2<Fmt, false>(w[4 * i + 2 * q + 1], to_units) << 16;
+      if (slot >= lo && slot < hi) *reinterpret_cast<u32x2*>(codes + slot * D + ch) = c;
     }
     if (a.c.weight)
       for (int j = lo + lane; j < hi; j += 64) a.c.weight[block * P + j] = 0.f;
   } else {
-    for (int g = sub; g * kGroup < hi; g += TPW) {
-      const int j0 = g * kGroup;
-      if (j0 + kGroup <= lo && again == 1.f) continue;
-      u32x4* const c = reinterpret_cast<u32x4*>(codes + (g * D + ch) * kGroup);     // the two channels' 16 bytes lie next to each other
-      u32x4 w0 = {0, 0, 0, 0}, w1 = {0, 0, 0, 0};
-      if (j0 < lo || j0 + kGroup > hi) { w0 = c[0]; w1 = c[1]; }                    // codes that stay
+    // a lane: two neighbouring channels of all tokens (64 channels: of every second group), which the cache holds as 16 bytes a group each
+    constexpr int LPR = D / 2, TPW = 64 / LPR, N = (Groups + TPW - 1) / TPW;
+    const int sub = lane / LPR, ch = 2 * (lane % LPR);
+    uint32_t w[N * kGroup];
+    u32x4 old[N][2];
 #pragma unroll
-      for (int j = 0; j < kGroup; ++j) {
-        const int slot = j0 + j, word = j / 4, shift = 8 * (j % 4);
-        uint32_t two = ((w0[word] >> shift) & 0xffu) | (((w1[word] >> shift) & 0xffu) << 8);
-        if (slot < lo) {
-          if (again != 1.f) {
-            const f32x2 f = decode2<Fmt>(two);
-            two = encode2<Fmt>(f[0] * again, f[1] * again);
-          }
-        } else if (slot < hi) {
-          const uint32_t r = *reinterpret_cast<const uint32_t*>(x + slot * a.row[1]);
-          two = encode2<Fmt>(__uint_as_float(r << 16) * to_units, __uint_as_float(r & 0xffff0000u) * to_units);
-        }
-        w0[word] = (w0[word] & ~(0xffu << shift)) | ((two & 0xffu) << shift);
-        w1[word] = (w1[word] & ~(0xffu << shift)) | ((two >> 8) << shift);
+    for (int i = 0; i < N; ++i) {
+      const int g = min(sub + TPW * i, Groups - 1);
+      const bool any = TPW * i * kGroup < hi && TPW * (i + 1) * kGroup > lo;
+      if (any) {
+#pragma unroll
+        for (int j = 0; j < kGroup; ++j) w[kGroup * i + j] = *reinterpret_cast<const uint32_t*>(x + min(max(g * kGroup + j, lo), hi - 1) * row + ch);
+      } else {
+#pragma unroll
+        for (int j = 0; j < kGroup; ++j) w[kGroup * i + j] = 0;
       }
-      c[0] = w0;
-      c[1] = w1;
+      old[i][0] = old[i][1] = u32x4{0, 0, 0, 0};
+      if (any && (TPW * i * kGroup < lo || TPW * (i + 1) * kGroup > hi)) {                // codes that stay
+        const u32x4* const c = reinterpret_cast<const u32x4*>(codes + (g * D + ch) * kGroup);
+        old[i][0] = c[0];
+        old[i][1] = c[1];
+      }
+    }
+    const float top = top_of(w, odd);
+    const int e = grow<Fmt>(top, lo > 0, a.c.v_scale + block, again);
+    const float to_units = power2(-e);
+    if (again != 1.f) {
+      // the earlier tokens' groups in the new units (of a group with new tokens: below)
+#pragma unroll 1
+      for (int g = sub; (g + 1) * kGroup <= lo; g += TPW) {
+        u32x4* const c = reinterpret_cast<u32x4*>(codes + (g * D + ch) * kGroup);
+        if (TPW * (g / TPW + 1) * kGroup > lo) continue;   // (its step is below)
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+          u32x4 o = c[m];
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const f32x2 f = decode_half<Fmt, false>(o[q]), h = decode_half<Fmt, true>(o[q]);
+            o[q] = encode2<Fmt>(f[0] * again, f[1] * again) | encode2<Fmt>(h[0] * again, h[1] * again) << 16;
+          }
+          c[m] = o;
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int g = sub + TPW * i;
+      if (TPW * i * kGroup < hi && TPW * (i + 1) * kGroup > lo) {
+        u32x4 c0, c1;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          uint32_t t[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t r = w[kGroup * i + 4 * q + j];
+            t[j] = odd ? code2<Fmt, true>(r, to_units) : code2<Fmt, false>(r, to_units);
+          }
+          // bytes of the first channel, of the second
+          const uint32_t p = __builtin_amdgcn_perm(t[1], t[0], 0x05010400u), r = __builtin_amdgcn_perm(t[3], t[2], 0x05010400u);
+          c0[q] = (p & 0xffffu) | r << 16;
+          c1[q] = (p >> 16) | (r & 0xffff0000u);
+        }
+        if (TPW * i * kGroup < lo || TPW * (i + 1) * kGroup > hi) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const int s0 = g * kGroup + 4 * q;     // slots s0 .. s0 + 3: the first `before` hold earlier tokens, from `end` on nothing new
+            const int before = min(max(lo - s0, 0), 4), end = min(max(hi - s0, 0), 4);
+            const uint32_t early = before == 4 ? ~0u : (1u << (8 * before)) - 1, upto = end == 4 ? ~0u : (1u << (8 * end)) - 1, fresh_bytes = upto & ~early;
+            uint32_t o0 = old[i][0][q], o1 = old[i][1][q];
+            if (again != 1.f) {
+              const f32x2 f0 = decode_half<Fmt, false>(o0), h0 = decode_half<Fmt, true>(o0), f1 = decode_half<Fmt, false>(o1), h1 = decode_half<Fmt, true>(o1);
+              const uint32_t n0 = encode2<Fmt>(f0[0] * again, f0[1] * again) | encode2<Fmt>(h0[0] * again, h0[1] * again) << 16;
+              const uint32_t n1 = encode2<Fmt>(f1[0] * again, f1[1] * again) | encode2<Fmt>(h1[0] * again, h1[1] * again) << 16;
+              o0 = (n0 & early) | (o0 & ~early);
+              o1 = (n1 & early) | (o1 & ~early);
+            }
+            c0[q] = (c0[q] & fresh_bytes) | (o0 & ~fresh_bytes);
+            c1[q] = (c1[q] & fresh_bytes) | (o1 & ~fresh_bytes);
+          }
+        }
+        if (g < Groups) {
+          u32x4* const c = reinterpret_cast<u32x4*>(codes + (g * D + ch) * kGroup);
+          c[0] = c0;
+          c[1] = c1;
+        }
+      }
     }
   }
+}
+
+template <int D, int Fmt>
+void launch_append(const AppendArgs& a, dim3 grid, hipStream_t st) {
+  auto kernel = a.c.page == 16 ? append_kernel<D, Fmt, 1> : a.c.page == 32 ? append_kernel<D, Fmt, 2> : a.c.page == 64 ? append_kernel<D, Fmt, 4> : append_kernel<D, Fmt, 8>;
+  kernel<<<grid, dim3(256), 0, st>>>(a);
 }
 
 }  // namespace
@@ -172,8 +306,7 @@ extern "C" int fcp_cache_append(const fcp_cache* cache, const void* k, int64_t k
   hipStream_t st = static_cast<hipStream_t>(stream);
   const dim3 grid((unsigned)a.units, (unsigned)((2 * a.c.hkv + 3) / 4));
   const bool e4m3 = cache->format == FCP_CACHE_E4M3;
-  auto kernel = cache->head_dim == 128 ? (e4m3 ? append_kernel<128, kE4m3> : append_kernel<128, kInt8>) : (e4m3 ? append_kernel<64, kE4m3> : append_kernel<64, kInt8>);
-  kernel<<<grid, dim3(256), 0, st>>>(a);
+  (cache->head_dim == 128 ? (e4m3 ? launch_append<128, kE4m3> : launch_append<128, kInt8>) : (e4m3 ? launch_append<64, kE4m3> : launch_append<64, kInt8>))(a, grid, st);
   FCP_HIP_CHECK(hipGetLastError());
   return FCP_OK;
 }

@@ -605,7 +605,7 @@ __global__ __launch_bounds__(256) void weigh_kernel(WeighArgs a) {
   }
 }
 
-// The same from the scores that the attention kernel left (few rows): a wave per (sequence, KV head, tile), a key per lane.
+// The same from the scores that the attention kernel left (few rows): a wave takes four rows of a tile at a time, four keys a lane, and four tiles.
 __global__ __launch_bounds__(256) void weigh_scores_kernel(AttnArgs a, int rows_of_block) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int32_t me = blockIdx.x;
@@ -625,19 +625,43 @@ __global__ __launch_bounds__(256) void weigh_scores_kernel(AttnArgs a, int rows_
     const int item = (int)((at - base) / tiles), t0 = (int)((at - base) % tiles), t1 = (int)min((int64_t)tiles, t0 + end - at);
     const int head = item / row_blocks, rb = item % row_blocks;
     // the rows of all blocks of a head add to the same weights: those of the first block's share do it, so that no two do
-    if (rb == 0)
-      for (int i = t0 + wave; i < t1; i += kWaves) {
-        const int key = i * kTile + lane;
-        float got = 0.f;
-        for (int row = 0; row < all_rows; ++row) {
-          const float lse = a.lse[(int64_t)(head * a.group + row % a.group) * a.s.n_rows + z.row0 + row / a.group];
-          if (lse == -INFINITY) continue;
-          const float* s = a.scores + (base + ((int64_t)head * row_blocks + row / rows_of_block) * tiles + i) * (16 * kTile);
-          got += __builtin_amdgcn_exp2f(s[(row % rows_of_block) * kTile + lane] - lse * kLog2e);
+    if (rb == 0) {
+      constexpr int kUnroll = 4;
+      const int sub = lane >> 4, key4 = 4 * (lane & 15);   // row of four, keys of the tile
+      for (int i = t0 + wave; i < t1; i += kWaves * kUnroll) {
+        f32x4 got[kUnroll] = {};
+        for (int r0 = 0; r0 < all_rows; r0 += 4) {
+          const int row = min(r0 + sub, all_rows - 1);
+          const float lse = a.lse[(int64_t)(head * a.group + row % a.group) * a.s.n_rows + z.row0 + row / a.group] * kLog2e;
+          const bool live = r0 + sub < all_rows && lse != -INFINITY;
+          const float* const s0 = a.scores + (base + ((int64_t)head * row_blocks + row / rows_of_block) * tiles) * (16 * kTile) + (row % rows_of_block) * kTile + key4;
+          f32x4 s[kUnroll];
+#pragma unroll
+          for (int j = 0; j < kUnroll; ++j) s[j] = *reinterpret_cast<const f32x4*>(s0 + (int64_t)min(i + kWaves * j, t1 - 1) * (16 * kTile));
+#pragma unroll
+          for (int j = 0; j < kUnroll; ++j)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) got[j][k] += live ? __builtin_amdgcn_exp2f(s[j][k] - lse) : 0.f;
         }
-        const int32_t p = key < z.len ? page_at(a.s, a.c, seq, key >> a.c.log_page) : -1;
-        if (p >= 0) a.c.weight[block_of(a.c, p, head) * a.c.page + (key & (a.c.page - 1))] += got;
+#pragma unroll
+        for (int j = 0; j < kUnroll; ++j)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) got[j][k] = sum_over_groups(got[j][k]);
+        if (sub == 0)
+#pragma unroll
+          for (int j = 0; j < kUnroll; ++j) {
+            const int key = (i + kWaves * j) * kTile + key4;
+            const int32_t p = i + kWaves * j < t1 && key < z.len ? page_at(a.s, a.c, seq, key >> a.c.log_page) : -1;
+            if (p >= 0) {
+              f32x4* const w = reinterpret_cast<f32x4*>(a.c.weight + block_of(a.c, p, head) * a.c.page + (key & (a.c.page - 1)));
+              f32x4 v = *w;
+#pragma unroll
+              for (int k = 0; k < 4; ++k) v[k] += key + k < z.len ? got[j][k] : 0.f;
+              *w = v;
+            }
+          }
       }
+    }
     at += t1 - t0;
   }
 }

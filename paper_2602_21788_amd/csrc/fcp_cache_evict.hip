@@ -326,9 +326,8 @@ __global__ __launch_bounds__(kSelectThreads) void emit_kernel(EvictArgs a) {
   emit(a, seq, head, z.kept, c0, c1, z.lo, z.hi, z.want == 0, border, want, place, equals);
 }
 
-// Lane `from`'s value; with one row of lanes in a wave the number is the same for all.
-template <int TPW> __device__ inline int32_t pick(int32_t x, int from) { return TPW == 1 ? __builtin_amdgcn_readlane(x, from) : __shfl(x, from); }
-template <int TPW> __device__ inline float pick(float x, int from) { return __int_as_float(pick<TPW>(__float_as_int(x), from)); }
+// Lane `from`'s value.
+__device__ inline float pick(float x, int from) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), from)); }
 
 // Codes of a word (four tokens of a channel, or four channels of a token) in other units: the largest magnitude (in units 2^16 times as large, which no value leaves), and
 // the codes.  A token's scale is multiplied in 2^-16 times.  NaN is no magnitude, and stays.
@@ -346,8 +345,8 @@ __device__ inline uint32_t in_units(uint32_t w, float s0, float s1, float s2, fl
 }
 
 // A wave per (new page, KV head, keys or values).  Lane j first finds where slot j's token lies and its scale, so that the tokens' codes can all be asked for at
-// once; they stay in registers until the page's scale is known.  Keys move as 16 bytes of a row; of the values, which lie 16 tokens together, a lane takes single bytes of
-// two channels and keeps them in the order in which they leave.  Groups: of 16 slots in a page.
+// once; they stay in registers until the page's scale is known.  Keys move as 16 bytes of a row; of the values, which lie 16 tokens together, a lane takes its channels'
+// 16 bytes and picks the token's.  Groups: of 16 slots in a page.
 template <int D, int Fmt, int Groups>
 __global__ __launch_bounds__(256) void move_kernel(EvictArgs a) {
   constexpr int P = Groups * kGroup, kPer = (P + 63) / 64;
@@ -412,41 +411,49 @@ __global__ __launch_bounds__(256) void move_kernel(EvictArgs a) {
       if (slot < P) *reinterpret_cast<u32x4*>(codes + slot * D + ch) = w[i];
     }
   } else {
-    constexpr int LPR = D / 2, TPW = 64 / LPR, N = (Groups + TPW - 1) / TPW;   // lanes of a token, groups of a step, steps
-    const int sub = lane / LPR, ch = 2 * (lane % LPR);
-    u32x4 w[N][2];
+    // The word of four tokens that holds the token is asked for, for 32 tokens at once: a group's lines are fetched once, by whichever token comes first, and nearly every group of a
+    // long sequence cut to an eighth has one.  (131072 tokens to 16384, 8 heads: values alone 74 us, keys alone 30.  Single bytes of channels that lie 32 bytes apart are a
+    // request each: 131 us for the whole launch instead of 94.)
+    constexpr int NC = D / 64, kBatch = P < 32 ? P : 32;   // channels of a lane: lane, lane + 64; tokens on their way
+    u32x4 w[Groups][NC];
 #pragma unroll
-    for (int i = 0; i < N; ++i)
+    for (int b = 0; b < P / kBatch; ++b) {
+      uint32_t x[kBatch][NC];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        uint32_t w0 = 0, w1 = 0;
+      for (int j = 0; j < kBatch; ++j) {
+        const int slot = kBatch * b + j;
+        const int32_t fp = __builtin_amdgcn_readlane(from_page[slot / 64], slot & 63), at = __builtin_amdgcn_readlane(from_slot[slot / 64], slot & 63);
+        const uint8_t* v = a.c.v + (block_of(a.c, fp, head) * P + (at & ~(kGroup - 1))) * D + (at & 12);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int slot = min((sub + TPW * i) * kGroup + 4 * q + j, P - 1), at = TPW * i * kGroup / 64;
-          const int32_t fp = pick<TPW>(from_page[at], slot & 63), fs = pick<TPW>(from_slot[at], slot & 63);
-          const uint8_t* v = a.c.v + (block_of(a.c, fp, head) * P + (fs & ~(kGroup - 1))) * D + (fs & (kGroup - 1)) + ch * kGroup;
-          w0 |= (uint32_t)v[0] << (8 * j);
-          w1 |= (uint32_t)v[kGroup] << (8 * j);
-        }
-        w[i][0][q] = w0;
-        w[i][1][q] = w1;
+        for (int c = 0; c < NC; ++c) x[j][c] = *reinterpret_cast<const uint32_t*>(v + 16 * lane + 1024 * c);
       }
 #pragma unroll
-    for (int i = 0; i < N; ++i)
+      for (int j = 0; j < kBatch; ++j) {
+        const int slot = kBatch * b + j, g = slot / kGroup, q = slot % kGroup / 4, byte = slot % 4;
+        const int32_t at = __builtin_amdgcn_readlane(from_slot[slot / 64], slot & 63);
+        // byte `byte` of the result's word is byte at % 4 of the token's word; the others stay
+        const uint32_t sel = (0x07060504u & ~(0xffu << (8 * byte))) | (uint32_t)(at & 3) << (8 * byte);
+#pragma unroll
+        for (int c = 0; c < NC; ++c) w[g][c][q] = __builtin_amdgcn_perm(byte == 0 ? 0u : w[g][c][q], x[j][c], sel);
+      }
+    }
+#pragma unroll
+    for (int g = 0; g < Groups; ++g)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         float s[4];
         uint32_t gone = 0;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          s[j] = pick<TPW>(scale[TPW * i * kGroup / 64], min((sub + TPW * i) * kGroup + 4 * q + j, P - 1) & 63);
+          const int slot = g * kGroup + 4 * q + j;
+          s[j] = pick(scale[slot / 64], slot & 63);
           gone |= s[j] == 0.f ? 0xffu << (8 * j) : 0u;
           s[j] *= kFar;
         }
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          w[i][c][q] &= ~gone;
-          top = largest<Fmt>(w[i][c][q], s[0], s[1], s[2], s[3], top);
+        for (int c = 0; c < NC; ++c) {
+          w[g][c][q] &= ~gone;
+          top = largest<Fmt>(w[g][c][q], s[0], s[1], s[2], s[3], top);
         }
       }
     top = wave_maxf(top);
@@ -454,21 +461,20 @@ __global__ __launch_bounds__(256) void move_kernel(EvictArgs a) {
     if (lane == 0) a.c.v_scale[block] = power2(e);
     const float to_units = power2(-e);
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int g = sub + TPW * i;
+    for (int g = 0; g < Groups; ++g) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         float s[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s[j] = fmaxf(pick<TPW>(scale[TPW * i * kGroup / 64], min(g * kGroup + 4 * q + j, P - 1) & 63) * to_units, 0x1p-126f);
+        for (int j = 0; j < 4; ++j) {
+          const int slot = g * kGroup + 4 * q + j;
+          s[j] = fmaxf(pick(scale[slot / 64], slot & 63) * to_units, 0x1p-126f);
+        }
 #pragma unroll
-        for (int c = 0; c < 2; ++c) w[i][c][q] = in_units<Fmt>(w[i][c][q], s[0], s[1], s[2], s[3]);
+        for (int c = 0; c < NC; ++c) w[g][c][q] = in_units<Fmt>(w[g][c][q], s[0], s[1], s[2], s[3]);
       }
-      if (g < Groups) {
-        u32x4* const y = reinterpret_cast<u32x4*>(codes + (g * D + ch) * kGroup);
-        y[0] = w[i][0];
-        y[1] = w[i][1];
-      }
+#pragma unroll
+      for (int c = 0; c < NC; ++c) *reinterpret_cast<u32x4*>(codes + (g * D + lane + 64 * c) * kGroup) = w[g][c];
     }
   }
 }
