@@ -30,69 +30,78 @@ struct AttnArgs {
   __bf16* o;
   float* lse;
   float* part;                         // two slots per block: rows x (D + 2) floats
-  float* scores;                       // weigh: [tile][16 rows][64 keys], scaled by log2(e); or NULL
+  float* scores;                       // weigh: [tile][4 key tiles][16 rows][4 groups][4 keys], in the order in which waves hold them, scaled by log2(e); or NULL
   int32_t blocks;                      // that share the line
 };
 
-// An item's sequence, and the line's length.
+// The line of the tiles of all items, and its division among blocks.  Sequence s has, for every KV head and every block of `rows` rows, all of its tiles (a sequence without
+// cached tokens one empty tile, which writes O = 0).  Short: an item is one place on the line, whatever its tiles, so that it lies in one block.
+// Places are 32-bit numbers: the host sees to it that there are fewer than 2^31.
 struct Line {
-  int64_t total;                       // tiles of all items
-  int64_t before;                      // tiles of the sequences before `seq`
+  int32_t total;                       // places
+  int32_t before;                      // those of the sequences before `seq`
   int32_t seq;
+  SeqSizes z;                          // of `seq`
   int32_t sharers;                     // blocks that get a share
+  // share i begins at i * size + min(i, larger): the first `larger` shares have size + 1 places
+  __device__ int32_t size() const { return total / sharers; }
+  __device__ int32_t larger() const { return total % sharers; }
+  __device__ int32_t begin(int32_t i) const { return i * size() + min(i, larger()); }
+  __device__ int32_t owner(int32_t x) const {
+    const int32_t q = size(), r = larger(), first = r * (q + 1);
+    return x < first ? x / (q + 1) : r + (x - first) / q;
+  }
 };
 
-__device__ inline int64_t div_up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 __device__ inline int32_t tiles_of(int len) { return max((len + kTile - 1) / kTile, 1); }
-// tiles on the line of a sequence: every block of `rows` rows of every KV head walks all of them (a sequence without cached tokens: one empty tile, which writes O = 0)
-__device__ inline int64_t cost_of(const SeqSizes& z, int hkv, int group, int rows) {
-  return z.n == 0 ? 0 : (int64_t)hkv * div_up((int64_t)z.n * group, rows) * tiles_of(z.len);
+template <bool Short> __device__ inline int32_t places_of(int len) { return Short ? 1 : tiles_of(len); }
+template <bool Short>
+__device__ inline int32_t cost_of(const SeqSizes& z, int hkv, int group, int rows) {
+  return z.n == 0 ? 0 : hkv * ((z.n * group + rows - 1) / rows) * places_of<Short>(z.len);
 }
 
-// Blocks that get a share of the line: `blocks`, fewer where there are few tiles; and their shares.
-__device__ inline int32_t sharing(int64_t total, int32_t blocks) { return (int32_t)min((int64_t)blocks, div_up(total, kLeastTiles)); }
-__device__ inline int64_t share_begin(int64_t total, int32_t sharers, int32_t i) { return total * i / sharers; }
-__device__ inline int32_t sharer_of(int64_t total, int32_t sharers, int64_t x) { return (int32_t)(((x + 1) * sharers - 1) / total); }
-
-// The sequence that holds the beginning of share `block` (-1 if there is none), or, with want >= 0, sequence `want` and what lies before it.  Every thread of the block
-// (256) calls; a thread adds up a run of sequences.
-__device__ inline Line find_on_line(const SeqView& s, const CacheView& c, int group, int rows, int blocks, int block, int want) {
-  __shared__ int64_t sums[kWaves];
-  __shared__ int64_t found[2];
-  const int per = (s.n_seqs + 255) / 256, a = min((int)threadIdx.x * per, s.n_seqs), b = min(a + per, s.n_seqs);
-  int64_t mine = 0;
-  for (int i = a; i < b; ++i) mine += cost_of(seq_sizes(s, i, c.page), c.hkv, group, rows);
-  int64_t upto = mine;
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int64_t v = __shfl_up(upto, d);
-    if (lane >= d) upto += v;
-  }
-  if (lane == 63) sums[threadIdx.x >> 6] = upto;
+// The sequence that holds the beginning of share `block`, or, with tok >= 0, query row `tok`; seq = -1 if there is none.  Every thread of the block (256, 512) calls; a thread
+// looks at a run of sequences, all of which are asked for at once.  At most `blocks` shares, fewer where a share would have fewer than kLeastTiles places.
+template <bool Short, int Threads = 256>
+__device__ inline Line find_on_line(const SeqView& s, const CacheView& c, int group, int rows, int blocks, int block, int tok) {
+  __shared__ int32_t sums[Threads / 64];
+  __shared__ int32_t found[5];
+  const int per = (s.n_seqs + Threads - 1) / Threads, a = min((int)threadIdx.x * per, s.n_seqs), b = min(a + per, s.n_seqs);
+  int32_t mine = 0;
+  for (int i = a; i < b; ++i) mine += cost_of<Short>(seq_sizes(s, i, c.page), c.hkv, group, rows);
+  int32_t upto = wave_prefix_sum(mine);
+  if ((threadIdx.x & 63) == 63) sums[threadIdx.x >> 6] = upto;
   if (threadIdx.x == 0) found[0] = -1;
   __syncthreads();
-  int64_t total = 0;
-  for (int w = 0; w < kWaves; ++w) {
+  Line line = {};
+  for (int w = 0; w < Threads / 64; ++w) {
     if (w < (int)(threadIdx.x >> 6)) upto += sums[w];
-    total += sums[w];
+    line.total += sums[w];
   }
-  const int32_t sharers = sharing(total, blocks);
-  int64_t at = upto - mine;            // of the thread's first sequence
-  const int64_t x = want >= 0 || block >= sharers ? -1 : share_begin(total, sharers, block);
-  if (want >= 0 ? (want >= a && want < b) : (x >= at && x < upto)) {
+  const int least = Short ? 1 : kLeastTiles;
+  line.sharers = min(blocks, (line.total + least - 1) / least);
+  int32_t at = upto - mine;            // of the thread's first sequence
+  const int32_t x = tok >= 0 || block >= line.sharers ? -1 : line.begin(block);
+  if (tok >= 0 || (x >= at && x < upto)) {
     for (int i = a; i < b; ++i) {
-      const int64_t n = cost_of(seq_sizes(s, i, c.page), c.hkv, group, rows);
-      if (want >= 0 ? i == want : x < at + n) {
+      const SeqSizes z = seq_sizes(s, i, c.page);
+      const int32_t n = cost_of<Short>(z, c.hkv, group, rows);
+      if (tok >= 0 ? tok >= z.row0 && tok < z.row0 + z.n : x < at + n) {
         found[0] = i;
         found[1] = at;
+        found[2] = z.row0;
+        found[3] = z.n;
+        found[4] = z.len;
         break;
       }
       at += n;
     }
   }
   __syncthreads();
-  return {total, found[1], (int32_t)found[0], sharers};
+  line.seq = found[0];
+  line.before = found[1];
+  line.z = {found[2], found[3], found[4]};
+  return line;
 }
 
 template <int D>
@@ -177,7 +186,7 @@ __device__ inline void softmax_of(f32x4 (&s)[4], float c, float vs, int last, f3
   top = __builtin_elementwise_maximum(top, s[3][3]) * c;
   if (scores)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) *reinterpret_cast<f32x4*>(scores + 4 * i) = s[i] * c;
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<f32x4*>(scores + 16 * 16 * i) = s[i] * c;
   // the maximum only grows in steps of more than 2^8: probabilities stay below 256, and most tiles leave the sums alone
   if (__ballot(top > m + 8.f)) {
     const float grown = fmaxf(m, max_over_groups(top)), f = __builtin_amdgcn_exp2f(m - grown);
@@ -271,14 +280,14 @@ __device__ inline void walk(const AttnArgs& a, int seq, int head, int len, int f
     if (full) {
 #pragma unroll
       for (int b = 0; b < NB; ++b)
-        softmax_of<D, true>(s[b], c, sc.v, 0, r.o[b], r.m[b], r.l[b], p[b], scores && n < score_rows ? scores + (int64_t)i * (16 * kTile) + n * kTile + 16 * g : nullptr);
+        softmax_of<D, true>(s[b], c, sc.v, 0, r.o[b], r.m[b], r.l[b], p[b], scores && n < score_rows ? scores + (int64_t)i * (16 * kTile) + 16 * n + 4 * g : nullptr);
     } else {
       int last[NB];
       const int key0 = i * kTile + 16 * g;
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
         last[b] = at.v < 0 ? -1 : last_tok[b] - key0;
-        softmax_of<D, false>(s[b], c, sc.v, last[b], r.o[b], r.m[b], r.l[b], p[b], scores && n < score_rows ? scores + (int64_t)i * (16 * kTile) + n * kTile + 16 * g : nullptr);
+        softmax_of<D, false>(s[b], c, sc.v, last[b], r.o[b], r.m[b], r.l[b], p[b], scores && n < score_rows ? scores + (int64_t)i * (16 * kTile) + 16 * n + 4 * g : nullptr);
       }
       clear_hidden<D, Fmt, NB>(v, at.v < 0 ? 0 : len - key0, last, r);
     }
@@ -315,7 +324,7 @@ __device__ inline void write_row(const AttnArgs& a, int row, int head, const f32
 }
 
 // Waves of a block divide the tiles of a piece (Keys) or take rows of their own.
-template <int D, int Fmt, int NB, bool Keys>
+template <int D, int Fmt, int NB, bool Keys, bool Short>
 __global__ __launch_bounds__(256, Keys ? 2 : 1) void attn_kernel(AttnArgs a) {
   constexpr int kRows = 16 * NB * (Keys ? 1 : kWaves);     // of a block
   constexpr int kStride = D + 4;                           // floats of a staged row: rows on different banks
@@ -323,24 +332,24 @@ __global__ __launch_bounds__(256, Keys ? 2 : 1) void attn_kernel(AttnArgs a) {
   __shared__ float stage_m[kWaves * 16 * NB], stage_l[kWaves * 16 * NB];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
   const int32_t me = blockIdx.x;
-  const Line line = find_on_line(a.s, a.c, a.group, kRows, a.blocks, me, -1);
+  const Line line = find_on_line<Short>(a.s, a.c, a.group, kRows, a.blocks, me, -1);
   if (line.seq < 0) return;
-  int64_t at = share_begin(line.total, line.sharers, me);
-  const int64_t end = share_begin(line.total, line.sharers, me + 1);
+  int32_t at = line.begin(me);
+  const int32_t end = line.begin(me + 1);
   int seq = line.seq;
-  int64_t base = line.before;
-  SeqSizes z = seq_sizes(a.s, seq, a.c.page);
+  int32_t base = line.before;
+  SeqSizes z = line.z;
   while (at < end) {
-    while (at >= base + cost_of(z, a.c.hkv, a.group, kRows)) {      // the next sequence with rows
-      base += cost_of(z, a.c.hkv, a.group, kRows);
+    while (at >= base + cost_of<Short>(z, a.c.hkv, a.group, kRows)) {      // the next sequence with rows
+      base += cost_of<Short>(z, a.c.hkv, a.group, kRows);
       z = seq_sizes(a.s, ++seq, a.c.page);
     }
     const int tiles = tiles_of(z.len), all_rows = z.n * a.group, row_blocks = (all_rows + kRows - 1) / kRows;
-    const int item = (int)((at - base) / tiles), t0 = (int)((at - base) % tiles);
-    const int t1 = (int)min((int64_t)tiles, t0 + end - at);
+    const int item = Short ? at - base : (at - base) / tiles, t0 = Short ? 0 : (at - base) % tiles;
+    const int t1 = Short ? tiles : min(tiles, t0 + end - at);
     const int head = item / row_blocks, rb = item % row_blocks;
-    const int64_t at0 = at;
-    at += t1 - t0;
+    const int32_t at0 = at;
+    at += Short ? 1 : t1 - t0;
 
     bf16x8 q[NB][D / 32];
     RowState<D, NB> r;
@@ -375,12 +384,12 @@ __global__ __launch_bounds__(256, Keys ? 2 : 1) void attn_kernel(AttnArgs a) {
     const int last_row = min(rb * kRows + kRows, all_rows) - 1, seen = z.len - z.n + last_row / a.group;
     const int t_end = min(t1, seen < 0 ? 0 : seen / kTile + 1);
     if (Keys || __ballot(any)) {
-      float* const scores = Keys && a.scores ? a.scores + (at0 - t0) * (16 * kTile) : nullptr;
+      float* const scores = Keys && a.scores ? a.scores + ((int64_t)at0 - t0) * (16 * kTile) : nullptr;
       const int score_rows = min(all_rows - rb * kRows, 16);
       walk<D, Fmt, NB>(a, seq, head, z.len, t0 + (Keys ? wave : 0), t_end, Keys ? kWaves : 1, q, last, first_seen, r, scores, score_rows);
       if (scores)                                          // tiles of the piece that nobody sees
         for (int i = max(t_end, t0) + wave; i < t1; i += kWaves)
-          for (int j = lane; j < score_rows * kTile; j += 64) scores[(int64_t)i * (16 * kTile) + j] = -INFINITY;
+          for (int j = lane; j < 16 * kTile; j += 64) scores[(int64_t)i * (16 * kTile) + j] = -INFINITY;
     }
 #pragma unroll
     for (int b = 0; b < NB; ++b) r.l[b] = sum_over_groups(r.l[b]);
@@ -441,18 +450,6 @@ __global__ __launch_bounds__(256, Keys ? 2 : 1) void attn_kernel(AttnArgs a) {
   }
 }
 
-// The sequence of a row: the last one that begins at or before it.  (64 ways at a time; every lane gets it.)
-__device__ inline int32_t seq_of_row(const SeqView& s, int row) {
-  int lo = 0, n = s.n_seqs;
-  while (n > 1) {
-    const int step = (n + 63) / 64, at = lo + (int)(threadIdx.x & 63) * step;
-    const int k = __popcll(__ballot(at < lo + n && s.cu[at] <= row)) - 1, next = lo + max(k, 0) * step;
-    n = min(step, lo + n - next);
-    lo = next;
-  }
-  return lo;
-}
-
 // The items that several blocks worked.  Few rows: a block per (row, query head) whose waves divide the pieces, of which a long sequence has many.
 // Many rows: a block per (eight rows, KV head) whose waves take query heads; there are two or three pieces then.
 constexpr int kMergeRows = 8;
@@ -463,22 +460,19 @@ __global__ __launch_bounds__(256) void attn_merge_kernel(AttnArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int heads = Keys ? a.hq : a.c.hkv, head = Keys ? (int)(blockIdx.x % heads) / a.group : (int)(blockIdx.x % heads);
   const int tok0 = (int)(blockIdx.x / heads) * (Keys ? 1 : kMergeRows), tok1 = min(tok0 + (Keys ? 1 : kMergeRows), a.s.n_rows);
-  int seq = -1;
-  SeqSizes z = {0, 0, 0};
   Line line = {};
+  line.seq = -1;
   for (int tok = tok0; tok < tok1; ++tok) {
-    if (seq < 0 || tok >= z.row0 + z.n) {                  // (all of this is the same for the whole block)
-      seq = seq_of_row(a.s, tok);
-      z = seq_sizes(a.s, seq, a.c.page);
-      if (tok < z.row0 || tok >= z.row0 + z.n) { seq = -1; continue; }
+    if (line.seq < 0 || tok >= line.z.row0 + line.z.n) {   // (the same for the whole block)
       __syncthreads();
-      line = find_on_line(a.s, a.c, a.group, kRows, a.blocks, 0, seq);
+      line = find_on_line<false>(a.s, a.c, a.group, kRows, a.blocks, 0, tok);
+      if (line.seq < 0) continue;
     }
+    const SeqSizes z = line.z;
     const int tiles = tiles_of(z.len), row_blocks = (z.n * a.group + kRows - 1) / kRows;
     for (int h = Keys ? (int)(blockIdx.x % heads) % a.group : wave; h < a.group; h += Keys ? a.group : kWaves) {
       const int row = (tok - z.row0) * a.group + h, rb = row / kRows, lr = row % kRows, qh = head * a.group + h;
-      const int64_t x = line.before + ((int64_t)head * row_blocks + rb) * tiles;
-      const int32_t w0 = sharer_of(line.total, line.sharers, x), w1 = sharer_of(line.total, line.sharers, x + tiles - 1);
+      const int32_t x = line.before + (head * row_blocks + rb) * tiles, w0 = line.owner(x), w1 = line.owner(x + tiles - 1);
       if (w0 == w1) continue;
       auto slot = [&](int w) { return a.part + (int64_t)(2 * w + (w == w0 ? 1 : 0)) * kFloats; };
       float m = kLow;
@@ -516,8 +510,9 @@ __global__ __launch_bounds__(256) void attn_merge_kernel(AttnArgs a) {
 
 // ---- weights ------------------------------------------------------------------------------------
 
-// Adds exp(score - LSE), summed over the rows of the group, to the tokens' weights.  A block takes one (sequence, KV head, tile) at a time, the longest-seen
-// first; its waves divide the rows.  The 16 sums of a lane (its keys) over its column's rows are added over the 16 columns, then over the waves.
+// Adds exp(score - LSE), summed over the rows of the group, to the tokens' weights: the products bound it, and the exponentials, which take longer than they do.  A block takes one
+// (sequence, KV head, tile) at a time, those with the most rows first; its waves hold the tile's keys and divide the rows, 16 at a time, the next ones on their way.  The 16 sums of a
+// lane (its keys) over its column's rows are added over the 16 columns, then over the waves.
 struct WeighArgs {
   CacheView c;
   SeqView s;
@@ -528,27 +523,44 @@ struct WeighArgs {
   const float* lse;
   int64_t lse_head;                    // floats between heads
 };
+constexpr int kWeighThreads = 512, kWeighWaves = kWeighThreads / 64;
 
 template <int D, int Fmt>
-__global__ __launch_bounds__(256) void weigh_kernel(WeighArgs a) {
-  __shared__ float sum[kWaves][kTile];
+__global__ __launch_bounds__(kWeighThreads, 2) void weigh_kernel(WeighArgs a) {
+  __shared__ float sum[kWeighWaves][kTile];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
   // the line with one block of rows per KV head
-  const int kAll = INT32_MAX;
-  const Line line = find_on_line(a.s, a.c, 1, kAll, 1, 0, -1);       // (its length)
-  int seq = 0;
-  int64_t base = 0;
-  SeqSizes z = seq_sizes(a.s, 0, a.c.page);
-  for (int64_t u = blockIdx.x; u < line.total; u += gridDim.x) {
+  const int kAll = 1 << 30;
+  const Line line = find_on_line<false, kWeighThreads>(a.s, a.c, 1, kAll, 1, 0, -1);
+  if (line.seq < 0) return;
+  int seq = line.seq;
+  int32_t base = line.before;
+  SeqSizes z = line.z;
+  for (int32_t u = blockIdx.x; u < line.total; u += gridDim.x) {
     __syncthreads();                   // (everybody has read the sums of the tile before)
-    while (u >= base + cost_of(z, a.c.hkv, 1, kAll)) {
-      base += cost_of(z, a.c.hkv, 1, kAll);
+    while (u >= base + cost_of<false>(z, a.c.hkv, 1, kAll)) {
+      base += cost_of<false>(z, a.c.hkv, 1, kAll);
       z = seq_sizes(a.s, ++seq, a.c.page);
     }
-    const int tile = (int)((u - base) / a.c.hkv), head = (int)((u - base) % a.c.hkv);
-    const int key0 = tile * kTile, mine0 = key0 + 16 * g;
+    const int tile = (u - base) / a.c.hkv, head = (u - base) % a.c.hkv;
+    const int key0 = tile * kTile, all_rows = z.n * a.group;
+    // the first token that sees the tile's first key
+    const int tok0 = max(key0 - (z.len - z.n), 0), rb0 = (int)((int64_t)tok0 * a.group / 16);
     const TilePages at = pages_of(a, seq, z.len, tile);
     const TileScales sc = scales_of(a.c, head, at.v);
+    struct Rows { bf16x8 q[D / 32]; float lse2; int last; };
+    auto rows_at = [&](int rb, Rows& r) {
+      const int row = min(rb * 16 + n, all_rows - 1), tok = row / a.group, h = head * a.group + row % a.group;
+      const __bf16* x = a.q + (int64_t)(z.row0 + tok) * a.q_row + h * D + 16 * g;
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j) r.q[j] = *reinterpret_cast<const bf16x8*>(x + 64 * (j / 2) + 8 * (j % 2));
+      const float lse = a.lse[h * a.lse_head + z.row0 + tok];
+      // rows that are not there, and rows that saw nothing, add exp2(-inf)
+      r.lse2 = rb * 16 + n < all_rows && lse != -INFINITY ? lse * kLog2e : INFINITY;
+      r.last = z.len - z.n + tok - key0 - 16 * g;          // of the lane's keys, those up to it are seen
+    };
+    Rows r;
+    if (16 * (rb0 + wave) < all_rows) rows_at(rb0 + wave, r);
     bf16x8 k[4][D / 32];
     {
       u32x4 raw[4][D / 64];
@@ -562,28 +574,25 @@ __global__ __launch_bounds__(256) void weigh_kernel(WeighArgs a) {
         }
     }
     const float c = a.scale * sc.k;
+    const int there = at.v < 0 ? -1 : 15;                  // (keys of a page that is not there are not seen)
     float got[16] = {};
-    const int all_rows = z.n * a.group;
-    // the first token that sees the tile's first key
-    const int tok0 = max(key0 - (z.len - z.n), 0), rb0 = (int)((int64_t)tok0 * a.group / 16);
-    for (int rb = rb0 + wave; rb * 16 < all_rows; rb += kWaves) {
-      const int row = rb * 16 + n;
-      const bool live = row < all_rows;
-      const int tok = live ? row / a.group : 0, h = head * a.group + (live ? row % a.group : 0);
-      const int last = live ? z.len - z.n + tok : -1;
-      const float lse2 = live ? a.lse[h * a.lse_head + z.row0 + tok] * kLog2e : -INFINITY;
-      const __bf16* x = a.q + (int64_t)(z.row0 + tok) * a.q_row + h * D + 16 * g;
+    for (int rb = rb0 + wave; rb * 16 < all_rows; rb += kWeighWaves) {
       f32x4 s[4] = {};
 #pragma unroll
-      for (int j = 0; j < D / 32; ++j) {
-        const bf16x8 q = *reinterpret_cast<const bf16x8*>(x + 64 * (j / 2) + 8 * (j % 2));
+      for (int j = 0; j < D / 32; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[i][j], q, s[i], 0, 0, 0);
-      }
+        for (int i = 0; i < 4; ++i) s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[i][j], r.q[j], s[i], 0, 0, 0);
+      const float lse2 = r.lse2;
+      const int last = min(r.last, there);
+      if (16 * (rb + kWeighWaves) < all_rows) rows_at(rb + kWeighWaves, r);
+      if (__ballot(last < 15)) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float p = __builtin_amdgcn_exp2f(s[i / 4][i % 4] * c - lse2);
-        got[i] += at.v >= 0 && mine0 + i <= last && lse2 != -INFINITY ? p : 0.f;
+        for (int i = 0; i < 16; ++i) s[i / 4][i % 4] = i <= last ? s[i / 4][i % 4] * c : -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) got[i] += __builtin_amdgcn_exp2f(s[i / 4][i % 4] - lse2);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) got[i] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 4][i % 4], c, -lse2));
       }
     }
 #pragma unroll
@@ -599,7 +608,10 @@ __global__ __launch_bounds__(256) void weigh_kernel(WeighArgs a) {
       const int32_t p = page_at(a.s, a.c, seq, key >> a.c.log_page);
       if (p >= 0) {
         float* w = a.c.weight + block_of(a.c, p, head) * a.c.page + (key & (a.c.page - 1));
-        *w += (sum[0][threadIdx.x] + sum[1][threadIdx.x]) + (sum[2][threadIdx.x] + sum[3][threadIdx.x]);
+        float all = 0.f;
+#pragma unroll
+        for (int i = 0; i < kWeighWaves; ++i) all += sum[i][threadIdx.x];
+        *w += all;
       }
     }
   }
@@ -609,32 +621,32 @@ __global__ __launch_bounds__(256) void weigh_kernel(WeighArgs a) {
 __global__ __launch_bounds__(256) void weigh_scores_kernel(AttnArgs a, int rows_of_block) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int32_t me = blockIdx.x;
-  const Line line = find_on_line(a.s, a.c, a.group, rows_of_block, a.blocks * kWaves, me, -1);   // (a share of its own)
+  const Line line = find_on_line<false>(a.s, a.c, a.group, rows_of_block, a.blocks * kWaves, me, -1);   // (a share of its own)
   if (line.seq < 0) return;
-  int64_t at = share_begin(line.total, line.sharers, me);
-  const int64_t end = share_begin(line.total, line.sharers, me + 1);
+  int32_t at = line.begin(me);
+  const int32_t end = line.begin(me + 1);
   int seq = line.seq;
-  int64_t base = line.before;
-  SeqSizes z = seq_sizes(a.s, seq, a.c.page);
+  int32_t base = line.before;
+  SeqSizes z = line.z;
   while (at < end) {
-    while (at >= base + cost_of(z, a.c.hkv, a.group, rows_of_block)) {
-      base += cost_of(z, a.c.hkv, a.group, rows_of_block);
+    while (at >= base + cost_of<false>(z, a.c.hkv, a.group, rows_of_block)) {
+      base += cost_of<false>(z, a.c.hkv, a.group, rows_of_block);
       z = seq_sizes(a.s, ++seq, a.c.page);
     }
     const int tiles = tiles_of(z.len), all_rows = z.n * a.group, row_blocks = (all_rows + rows_of_block - 1) / rows_of_block;
-    const int item = (int)((at - base) / tiles), t0 = (int)((at - base) % tiles), t1 = (int)min((int64_t)tiles, t0 + end - at);
+    const int item = (at - base) / tiles, t0 = (at - base) % tiles, t1 = min(tiles, t0 + end - at);
     const int head = item / row_blocks, rb = item % row_blocks;
     // the rows of all blocks of a head add to the same weights: those of the first block's share do it, so that no two do
     if (rb == 0) {
       constexpr int kUnroll = 4;
-      const int sub = lane >> 4, key4 = 4 * (lane & 15);   // row of four, keys of the tile
+      const int sub = lane >> 4, i4 = (lane >> 2) & 3, g = lane & 3, key4 = 16 * g + 4 * i4;   // row of four, keys of the tile
       for (int i = t0 + wave; i < t1; i += kWaves * kUnroll) {
         f32x4 got[kUnroll] = {};
         for (int r0 = 0; r0 < all_rows; r0 += 4) {
           const int row = min(r0 + sub, all_rows - 1);
           const float lse = a.lse[(int64_t)(head * a.group + row % a.group) * a.s.n_rows + z.row0 + row / a.group] * kLog2e;
           const bool live = r0 + sub < all_rows && lse != -INFINITY;
-          const float* const s0 = a.scores + (base + ((int64_t)head * row_blocks + row / rows_of_block) * tiles) * (16 * kTile) + (row % rows_of_block) * kTile + key4;
+          const float* const s0 = a.scores + ((int64_t)base + ((int64_t)head * row_blocks + row / rows_of_block) * tiles) * (16 * kTile) + 256 * i4 + 16 * (row % rows_of_block) + 4 * g;
           f32x4 s[kUnroll];
 #pragma unroll
           for (int j = 0; j < kUnroll; ++j) s[j] = *reinterpret_cast<const f32x4*>(s0 + (int64_t)min(i + kWaves * j, t1 - 1) * (16 * kTile));
@@ -669,9 +681,11 @@ __global__ __launch_bounds__(256) void weigh_scores_kernel(AttnArgs a, int rows_
 // ---- host ---------------------------------------------------------------------------------------
 
 constexpr int kBlocks = 512;           // that share the line: two per CU
+// Tables of up to this many tiles: an item is not divided among blocks, which saves the second launch.  One sequence of 512 tokens, 4 heads of 64 channels: MEASURED.
+constexpr int kShortTiles = 16;
 
 // How a call is worked.  Up to 16 rows per sequence and KV head on average: a block of 16 rows whose waves divide the keys; more: 128 rows, a wave 32.
-struct AttnPlan { int rows; bool keys; bool stored; int64_t part_floats, score_floats; };
+struct AttnPlan { int rows; bool keys; bool stored; bool whole; int64_t part_floats, score_floats, places; };
 AttnPlan plan_attn(const CacheView& c, int head_dim, int32_t n_seqs, int32_t max_pages, int32_t tq, int32_t hq, bool weigh) {
   const int group = hq / c.hkv;
   AttnPlan p;
@@ -680,18 +694,25 @@ AttnPlan plan_attn(const CacheView& c, int head_dim, int32_t n_seqs, int32_t max
   p.stored = weigh && p.keys;
   p.part_floats = (int64_t)2 * kBlocks * p.rows * (head_dim + 2);
   const int64_t tiles = max(((int64_t)max_pages * c.page + kTile - 1) / kTile, (int64_t)1);
-  p.score_floats = p.stored ? tiles * c.hkv * (n_seqs + (int64_t)tq * group / 16) * 16 * kTile : 0;
+  p.whole = tiles <= kShortTiles && !p.stored;
+  p.places = tiles * c.hkv * (n_seqs + (int64_t)tq * group / p.rows);
+  p.score_floats = p.stored ? p.places * 16 * kTile : 0;
   return p;
 }
 
 template <int D, int Fmt>
 int launch_attn(const AttnArgs& a, const AttnPlan& p, bool weigh, hipStream_t st) {
-  if (p.keys) attn_kernel<D, Fmt, 1, true><<<dim3(kBlocks), dim3(256), 0, st>>>(a);
-  else attn_kernel<D, Fmt, 2, false><<<dim3(kBlocks), dim3(256), 0, st>>>(a);
+  const dim3 grid(kBlocks), block(256);
+  if (p.keys && p.whole) attn_kernel<D, Fmt, 1, true, true><<<grid, block, 0, st>>>(a);
+  else if (p.keys) attn_kernel<D, Fmt, 1, true, false><<<grid, block, 0, st>>>(a);
+  else if (p.whole) attn_kernel<D, Fmt, 2, false, true><<<grid, block, 0, st>>>(a);
+  else attn_kernel<D, Fmt, 2, false, false><<<grid, block, 0, st>>>(a);
   FCP_HIP_CHECK(hipGetLastError());
-if (p.keys) attn_merge_kernel<D, true><<<dim3((unsigned)a.s.n_rows * a.hq), dim3(256), 0, st>>>(a);
-  else attn_merge_kernel<D, false><<<dim3((unsigned)((a.s.n_rows + kMergeRows - 1) / kMergeRows) * a.c.hkv), dim3(256), 0, st>>>(a);
-  FCP_HIP_CHECK(hipGetLastError());
+  if (!p.whole) {
+    if (p.keys) attn_merge_kernel<D, true><<<dim3((unsigned)a.s.n_rows * a.hq), block, 0, st>>>(a);
+    else attn_merge_kernel<D, false><<<dim3((unsigned)((a.s.n_rows + kMergeRows - 1) / kMergeRows) * a.c.hkv), block, 0, st>>>(a);
+    FCP_HIP_CHECK(hipGetLastError());
+  }
   if (p.stored) {
     weigh_scores_kernel<<<dim3(kBlocks * kWaves), dim3(256), 0, st>>>(a, p.rows);
     FCP_HIP_CHECK(hipGetLastError());
@@ -702,7 +723,7 @@ if (p.keys) attn_merge_kernel<D, true><<<dim3((unsigned)a.s.n_rows * a.hq), dim3
 int launch_weigh(const WeighArgs& a, int head_dim, int format, hipStream_t st) {
   auto kernel = head_dim == 128 ? (format == kE4m3 ? weigh_kernel<128, kE4m3> : weigh_kernel<128, kInt8>)
                                 : (format == kE4m3 ? weigh_kernel<64, kE4m3> : weigh_kernel<64, kInt8>);
-  kernel<<<dim3(4 * kBlocks), dim3(256), 0, st>>>(a);
+  kernel<<<dim3(2 * kBlocks), dim3(kWeighThreads), 0, st>>>(a);
   FCP_HIP_CHECK(hipGetLastError());
   return FCP_OK;
 }
@@ -757,6 +778,7 @@ extern "C" int fcp_cache_attn(const fcp_cache* cache, const void* q, int64_t q_r
   if (!o || !lse || (uintptr_t)o % 16 || (uintptr_t)lse % 4) return fail(FCP_ERR_INVALID_ARG, "%s: o and lse are required and must be aligned", who);
   if (!scratch || (uintptr_t)scratch % 256) return fail(FCP_ERR_INVALID_ARG, "%s: scratch must be 256-byte aligned", who);
   const AttnPlan p = plan_attn(a.c, cache->head_dim, n_seqs, max_pages, tq, hq, weigh);
+  if (p.places > INT32_MAX) return fail(FCP_ERR_UNSUPPORTED, "%s: tables and rows that may make 2^31 tiles of work", who);
   const size_t need = pad_to((size_t)p.part_floats * 4, 256) + pad_to((size_t)p.score_floats * 4, 256);
   if (scratch_bytes < need) return fail(FCP_ERR_CAPACITY, "%s: scratch has %zu bytes, %zu are needed", who, scratch_bytes, need);
   a.s = {cu_seqlens, kv_len, pages, n_seqs, max_pages, tq};
@@ -793,6 +815,8 @@ extern "C" int fcp_cache_weigh(const fcp_cache* cache, const void* q, int64_t q_
   if (tq == 0 || n_seqs == 0) return FCP_OK;
   if (int rc = check_rows(who, cache, q, q_row, tq, hq)) return rc;
   if (!lse || (uintptr_t)lse % 4) return fail(FCP_ERR_INVALID_ARG, "%s: lse is required", who);
+  if (plan_attn(a.c, cache->head_dim, n_seqs, max_pages, tq, hq, false).places > INT32_MAX)
+    return fail(FCP_ERR_UNSUPPORTED, "%s: tables and rows that may make 2^31 tiles of work", who);
   a.s = {cu_seqlens, kv_len, pages, n_seqs, max_pages, tq};
   a.q = static_cast<const __bf16*>(q);
   a.q_row = q_row;
