@@ -10,6 +10,8 @@
 //     of two) the probabilities.  The wave needs no LDS and no barrier in its loop.
 // All (sequence, KV head, block of rows, key tile) form one line, cut into equal pieces for the blocks: a long sequence is split over many blocks and short ones
 // share one, however ragged the lengths, which only the device knows.  The pieces of an item that does not lie in one block meet in a second launch.
+#include <type_traits>
+
 #include "fcp_cache.h"
 
 namespace fcp {
@@ -60,7 +62,7 @@ __device__ inline int32_t cost_of(const SeqSizes& z, int hkv, int group, int row
   return z.n == 0 ? 0 : hkv * ((z.n * group + rows - 1) / rows) * places_of<Short>(z.len);
 }
 
-// The sequence that holds the beginning of share `block`, or, with tok >= 0, query row `tok`; seq = -1 if there is none.  Every thread of the block (256, 512) calls; a thread
+// The sequence that holds the beginning of share `block` (blocks = 0: place `block` itself), or, with tok >= 0, query row `tok`; seq = -1 if there is none.  Every thread of the block (256, 512) calls; a thread
 // looks at a run of sequences, all of which are asked for at once.  At most `blocks` shares, fewer where a share would have fewer than kLeastTiles places.
 template <bool Short, int Threads = 256>
 __device__ inline Line find_on_line(const SeqView& s, const CacheView& c, int group, int rows, int blocks, int block, int tok) {
@@ -81,7 +83,7 @@ __device__ inline Line find_on_line(const SeqView& s, const CacheView& c, int gr
   const int least = Short ? 1 : kLeastTiles;
   line.sharers = min(blocks, (line.total + least - 1) / least);
   int32_t at = upto - mine;            // of the thread's first sequence
-  const int32_t x = tok >= 0 || block >= line.sharers ? -1 : line.begin(block);
+  const int32_t x = blocks == 0 ? block : tok >= 0 || block >= line.sharers ? -1 : line.begin(block);
   if (tok >= 0 || (x >= at && x < upto)) {
     for (int i = a; i < b; ++i) {
       const SeqSizes z = seq_sizes(s, i, c.page);
@@ -265,12 +267,12 @@ __device__ inline void walk(const AttnArgs& a, int seq, int head, int len, int f
   load_keys<D>(a.c, head, first, at.k, k);
   TileScales sc = scales_of(a.c, head, at.v);
   load_values<D>(a.c, head, first, at.v, v);
-  for (int i = first; i < end; i += step) {
-    const bool more = i + step < end;
+  // (The last tile apart: loads under a condition would all be waited for where it ends.)
+  auto tile = [&](int i, auto more) {
     f32x4 s[NB][4];
     scores_of<D, Fmt, NB>(k, q, s);
     TileScales sc_next = sc;
-    if (more) {
+    if constexpr (more) {
       load_keys<D>(a.c, head, i + step, next.k, k);
       sc_next = scales_of(a.c, head, next.v);
     }
@@ -299,13 +301,16 @@ __device__ inline void walk(const AttnArgs& a, int seq, int head, int len, int f
 #pragma unroll
         for (int b = 0; b < NB; ++b) r.o[b][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, p[b][h], r.o[b][d], 0, 0, 0);
       }
-    if (more) {
+    if constexpr (more) {
       load_values<D>(a.c, head, i + step, next.v, v);
       at = next;
       next = pages_of(a, seq, len, i + 2 * step);
       sc = sc_next;
     }
-  }
+  };
+  int i = first;
+  for (; i + step < end; i += step) tile(i, std::true_type{});
+  tile(i, std::false_type{});
 }
 
 // Final row, or its part: o channels 16 i + 4 g + 0..3 of the lane's row.
@@ -523,6 +528,10 @@ struct WeighArgs {
   const float* lse;
   int64_t lse_head;                    // floats between heads
 };
+// Sum over the 16 lanes of a row.
+template <int Ctrl> __device__ inline float plus_dpp(float x) { return x + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), Ctrl, 0xf, 0xf, false)); }
+__device__ inline float sum_of_16(float x) { return plus_dpp<0x121>(plus_dpp<0x122>(plus_dpp<0x124>(plus_dpp<0x128>(x)))); }   // turned by 8, 4, 2, 1 lanes
+
 constexpr int kWeighThreads = 512, kWeighWaves = kWeighThreads / 64;
 
 template <int D, int Fmt>
@@ -531,7 +540,7 @@ __global__ __launch_bounds__(kWeighThreads, 2) void weigh_kernel(WeighArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
   // the line with one block of rows per KV head
   const int kAll = 1 << 30;
-  const Line line = find_on_line<false, kWeighThreads>(a.s, a.c, 1, kAll, 1, 0, -1);
+  const Line line = find_on_line<false, kWeighThreads>(a.s, a.c, 1, kAll, 0, blockIdx.x, -1);
   if (line.seq < 0) return;
   int seq = line.seq;
   int32_t base = line.before;
@@ -548,19 +557,23 @@ __global__ __launch_bounds__(kWeighThreads, 2) void weigh_kernel(WeighArgs a) {
     const int tok0 = max(key0 - (z.len - z.n), 0), rb0 = (int)((int64_t)tok0 * a.group / 16);
     const TilePages at = pages_of(a, seq, z.len, tile);
     const TileScales sc = scales_of(a.c, head, at.v);
-    struct Rows { bf16x8 q[D / 32]; float lse2; int last; };
-    auto rows_at = [&](int rb, Rows& r) {
-      const int row = min(rb * 16 + n, all_rows - 1), tok = row / a.group, h = head * a.group + row % a.group;
-      const __bf16* x = a.q + (int64_t)(z.row0 + tok) * a.q_row + h * D + 16 * g;
+    // the lane's row of a block of 16: token and query head of the group, and where its query and its LSE lie, stepped without products; what is asked for a block ahead
+    struct Rows { bf16x8 q[D / 32]; float lse; };
+    const int step = 16 * kWeighWaves, step_tok = step / a.group, step_h = step % a.group;
+    int row = 16 * (rb0 + wave) + n, tok = row / a.group, h = row % a.group;
+    const __bf16* const q0 = a.q + (int64_t)z.row0 * a.q_row + head * a.group * D + 16 * g;
+    const float* const lse0 = a.lse + head * a.group * a.lse_head + z.row0;
+    int64_t q_at = (int64_t)tok * a.q_row + h * D, lse_at = h * a.lse_head + tok;
+    const int64_t q_step = step_tok * a.q_row + step_h * D, q_wrap = a.q_row - a.group * D, lse_step = step_h * a.lse_head + step_tok, lse_wrap = 1 - a.group * a.lse_head;
+    auto rows_at = [&](Rows& r) {
+      const bool live = row < all_rows;                    // (else: the first row)
+      const __bf16* x = q0 + (live ? q_at : 0);
 #pragma unroll
       for (int j = 0; j < D / 32; ++j) r.q[j] = *reinterpret_cast<const bf16x8*>(x + 64 * (j / 2) + 8 * (j % 2));
-      const float lse = a.lse[h * a.lse_head + z.row0 + tok];
-      // rows that are not there, and rows that saw nothing, add exp2(-inf)
-      r.lse2 = rb * 16 + n < all_rows && lse != -INFINITY ? lse * kLog2e : INFINITY;
-      r.last = z.len - z.n + tok - key0 - 16 * g;          // of the lane's keys, those up to it are seen
+      r.lse = lse0[live ? lse_at : 0];
     };
-    Rows r;
-    if (16 * (rb0 + wave) < all_rows) rows_at(rb0 + wave, r);
+    Rows r[2];
+    rows_at(r[0]);
     bf16x8 k[4][D / 32];
     {
       u32x4 raw[4][D / 64];
@@ -576,15 +589,24 @@ __global__ __launch_bounds__(kWeighThreads, 2) void weigh_kernel(WeighArgs a) {
     const float c = a.scale * sc.k;
     const int there = at.v < 0 ? -1 : 15;                  // (keys of a page that is not there are not seen)
     float got[16] = {};
-    for (int rb = rb0 + wave; rb * 16 < all_rows; rb += kWeighWaves) {
+    auto add = [&](const Rows& now, Rows& next) {
+      // rows that are not there, and rows that saw nothing, add exp2(-inf)
+      const float lse2 = row < all_rows && now.lse != -INFINITY ? now.lse * kLog2e : INFINITY;
+      const int last = min(z.len - z.n + tok - key0 - 16 * g, there);          // of the lane's keys, those up to it are seen
+      row += step;
+      tok += step_tok;
+      h += step_h;
+      const bool wraps = h >= a.group;
+      h -= wraps ? a.group : 0;
+      tok += wraps;
+      q_at += q_step + (wraps ? q_wrap : 0);
+      lse_at += lse_step + (wraps ? lse_wrap : 0);
+      rows_at(next);                                       // (always: loads under a condition would be waited for where it ends)
       f32x4 s[4] = {};
 #pragma unroll
       for (int j = 0; j < D / 32; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[i][j], r.q[j], s[i], 0, 0, 0);
-      const float lse2 = r.lse2;
-      const int last = min(r.last, there);
-      if (16 * (rb + kWeighWaves) < all_rows) rows_at(rb + kWeighWaves, r);
+        for (int i = 0; i < 4; ++i) s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[i][j], now.q[j], s[i], 0, 0, 0);
       if (__ballot(last < 15)) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i / 4][i % 4] = i <= last ? s[i / 4][i % 4] * c : -INFINITY;
@@ -594,11 +616,13 @@ __global__ __launch_bounds__(kWeighThreads, 2) void weigh_kernel(WeighArgs a) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) got[i] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 4][i % 4], c, -lse2));
       }
+    };
+    for (int rb = rb0 + wave; rb * 16 < all_rows; rb += 2 * kWeighWaves) {
+      add(r[0], r[1]);
+      add(r[1], r[0]);
     }
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-#pragma unroll
-      for (int d = 8; d > 0; d >>= 1) got[i] += __shfl_xor(got[i], d);
+    for (int i = 0; i < 16; ++i) got[i] = sum_of_16(got[i]);
     if (n == 0)
 #pragma unroll
       for (int i = 0; i < 16; ++i) sum[wave][16 * g + i] = got[i];
@@ -721,9 +745,10 @@ int launch_attn(const AttnArgs& a, const AttnPlan& p, bool weigh, hipStream_t st
 }
 
 int launch_weigh(const WeighArgs& a, int head_dim, int format, hipStream_t st) {
+  const int64_t most = max(((int64_t)a.s.max_pages * a.c.page + kTile - 1) / kTile, (int64_t)1) * a.c.hkv * a.s.n_seqs;
   auto kernel = head_dim == 128 ? (format == kE4m3 ? weigh_kernel<128, kE4m3> : weigh_kernel<128, kInt8>)
                                 : (format == kE4m3 ? weigh_kernel<64, kE4m3> : weigh_kernel<64, kInt8>);
-  kernel<<<dim3(2 * kBlocks), dim3(kWeighThreads), 0, st>>>(a);
+  kernel<<<dim3((unsigned)min(most, (int64_t)2 * kBlocks)), dim3(kWeighThreads), 0, st>>>(a);
   FCP_HIP_CHECK(hipGetLastError());
   return FCP_OK;
 }
