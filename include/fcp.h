@@ -468,7 +468,8 @@ typedef struct fcp_cache {
 } fcp_cache;
 
 /* Scratch size in bytes of fcp_cache_attn without / with weigh (queries: tq rows of hq heads) and of fcp_cache_evict (tq, hq not used), as
- * fcp_scratch_bytes; 0 and fcp_last_error for arguments that the call would refuse.  A larger n_seqs, max_pages or tq never needs less. */
+ * fcp_scratch_bytes; 0 and fcp_last_error for arguments that the call would refuse.  The way that a call is worked follows from its sizes, so other sizes may need more or
+ * less: a program that calls with several takes the largest. */
 #define FCP_SCRATCH_CACHE_ATTN 2
 #define FCP_SCRATCH_CACHE_WEIGH 3
 #define FCP_SCRATCH_CACHE_EVICT 4

@@ -114,6 +114,12 @@ __device__ inline bf16x8 decode8(uint32_t lo, uint32_t hi) {
   }
 }
 
+// One wave-wide LDS-direct load: the 16 bytes at every lane's own address land at LDS offset `lds` (the same for the wave) + 16 lane.  In assembly for the reasons given at
+// lds_fill_b128: the caller waits with s_waitcnt vmcnt before the wave reads them.
+__device__ inline void lds_load_b128(const void* from, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, off" :: "s"(__builtin_amdgcn_readfirstlane((int)lds)), "v"(from) : "memory");
+}
+
 __device__ inline float wave_maxf(float x) {
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) x = fmaxf(x, __shfl_xor(x, d));

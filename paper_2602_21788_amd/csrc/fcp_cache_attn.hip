@@ -12,108 +12,16 @@
 // share one, however ragged the lengths, which only the device knows.  The pieces of an item that does not lie in one block meet in a second launch.
 #include <type_traits>
 
-#include "fcp_cache.h"
+#include "fcp_cache_attn.h"
 
 namespace fcp {
 namespace {
 
-constexpr int kTile = 64;              // keys of a tile
-constexpr int kWaves = 4;              // of a block
-constexpr int kLeastTiles = 4;         // of a block, where there are few
-constexpr float kLow = -1e30f;         // running maximum before the first key: finite, so that exp2(-inf - it) is 0
-
-struct AttnArgs {
-  CacheView c;
-  SeqView s;
-  const __bf16* q;
-  int64_t q_row;
-  int32_t hq, group;
-  float scale;                         // softmax_scale * log2(e)
-  __bf16* o;
-  float* lse;
-  float* part;                         // two slots per block: rows x (D + 2) floats
-  float* scores;                       // weigh: [tile][4 key tiles][16 rows][4 groups][4 keys], in the order in which waves hold them, scaled by log2(e); or NULL
-  int32_t blocks;                      // that share the line
-};
-
-// The line of the tiles of all items, and its division among blocks.  Sequence s has, for every KV head and every block of `rows` rows, all of its tiles (a sequence without
-// cached tokens one empty tile, which writes O = 0).  Short: an item is one place on the line, whatever its tiles, so that it lies in one block.
-// Places are 32-bit numbers: the host sees to it that there are fewer than 2^31.
-struct Line {
-  int32_t total;                       // places
-  int32_t before;                      // those of the sequences before `seq`
-  int32_t seq;
-  SeqSizes z;                          // of `seq`
-  int32_t sharers;                     // blocks that get a share
-  // share i begins at i * size + min(i, larger): the first `larger` shares have size + 1 places
-  __device__ int32_t size() const { return total / sharers; }
-  __device__ int32_t larger() const { return total % sharers; }
-  __device__ int32_t begin(int32_t i) const { return i * size() + min(i, larger()); }
-  __device__ int32_t owner(int32_t x) const {
-    const int32_t q = size(), r = larger(), first = r * (q + 1);
-    return x < first ? x / (q + 1) : r + (x - first) / q;
-  }
-};
-
-__device__ inline int32_t tiles_of(int len) { return max((len + kTile - 1) / kTile, 1); }
-template <bool Short> __device__ inline int32_t places_of(int len) { return Short ? 1 : tiles_of(len); }
-template <bool Short>
-__device__ inline int32_t cost_of(const SeqSizes& z, int hkv, int group, int rows) {
-  return z.n == 0 ? 0 : hkv * ((z.n * group + rows - 1) / rows) * places_of<Short>(z.len);
-}
-
-// The sequence that holds the beginning of share `block` (blocks = 0: place `block` itself), or, with tok >= 0, query row `tok`; seq = -1 if there is none.  Every thread of the block (256, 512) calls; a thread
-// looks at a run of sequences, all of which are asked for at once.  At most `blocks` shares, fewer where a share would have fewer than kLeastTiles places.
-template <bool Short, int Threads = 256>
-__device__ inline Line find_on_line(const SeqView& s, const CacheView& c, int group, int rows, int blocks, int block, int tok) {
-  __shared__ int32_t sums[Threads / 64];
-  __shared__ int32_t found[5];
-  const int per = (s.n_seqs + Threads - 1) / Threads, a = min((int)threadIdx.x * per, s.n_seqs), b = min(a + per, s.n_seqs);
-  int32_t mine = 0;
-  for (int i = a; i < b; ++i) mine += cost_of<Short>(seq_sizes(s, i, c.page), c.hkv, group, rows);
-  int32_t upto = wave_prefix_sum(mine);
-  if ((threadIdx.x & 63) == 63) sums[threadIdx.x >> 6] = upto;
-  if (threadIdx.x == 0) found[0] = -1;
-  __syncthreads();
-  Line line = {};
-  for (int w = 0; w < Threads / 64; ++w) {
-    if (w < (int)(threadIdx.x >> 6)) upto += sums[w];
-    line.total += sums[w];
-  }
-  const int least = Short ? 1 : kLeastTiles;
-  line.sharers = min(blocks, (line.total + least - 1) / least);
-  int32_t at = upto - mine;            // of the thread's first sequence
-  const int32_t x = blocks == 0 ? block : tok >= 0 || block >= line.sharers ? -1 : line.begin(block);
-  if (tok >= 0 || (x >= at && x < upto)) {
-    for (int i = a; i < b; ++i) {
-      const SeqSizes z = seq_sizes(s, i, c.page);
-      const int32_t n = cost_of<Short>(z, c.hkv, group, rows);
-      if (tok >= 0 ? tok >= z.row0 && tok < z.row0 + z.n : x < at + n) {
-        found[0] = i;
-        found[1] = at;
-        found[2] = z.row0;
-        found[3] = z.n;
-        found[4] = z.len;
-        break;
-      }
-      at += n;
-    }
-  }
-  __syncthreads();
-  line.seq = found[0];
-  line.before = found[1];
-  line.z = {found[2], found[3], found[4]};
-  return line;
-}
-
+// What a wave keeps of 16 rows.
 template <int D>
-struct PartSlot { static constexpr int floats(int rows) { return rows * (D + 2); } };   // [rows][D] sums, [rows] maxima, [rows] sums of exponentials
-
-// What a wave keeps of 16 * NB rows.
-template <int D, int NB>
 struct RowState {
-  f32x4 o[NB][D / 16];
-  float m[NB], l[NB];
+  f32x4 o[D / 16];
+  float m, l;
 };
 
 // Pages of a tile for a lane: of the keys that its matrix row holds in the four key tiles, 16 (n / 4) + 4 i + n % 4, and of its 16 neighbouring keys 16 g ..; -1: not
@@ -148,60 +56,17 @@ __device__ inline TileScales scales_of(const CacheView& c, int head, int32_t pag
   return {page >= 0 ? k : 1.f, page >= 0 ? v : 1.f};
 }
 
-__device__ inline float max_over_groups(float x) {
-  x = fmaxf(x, __shfl_xor(x, 16));
-  return fmaxf(x, __shfl_xor(x, 32));
-}
-__device__ inline float sum_over_groups(float x) {
-  x += __shfl_xor(x, 16);
-  return x + __shfl_xor(x, 32);
-}
-
 // S^T of one tile.
-template <int D, int Fmt, int NB>
-__device__ inline void scores_of(const u32x4 (&k)[4][D / 64], const bf16x8 (&q)[NB][D / 32], f32x4 (&s)[NB][4]) {
+template <int D, int Fmt>
+__device__ inline void scores_of(const u32x4 (&k)[4][D / 64], const bf16x8 (&q)[D / 32], f32x4 (&s)[4]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-#pragma unroll
-    for (int b = 0; b < NB; ++b) s[b][i] = f32x4{0, 0, 0, 0};
+    s[i] = f32x4{0, 0, 0, 0};
 #pragma unroll
     for (int j = 0; j < D / 64; ++j) {
-      const bf16x8 k0 = decode8<Fmt>(k[i][j][0], k[i][j][1]), k1 = decode8<Fmt>(k[i][j][2], k[i][j][3]);
-#pragma unroll
-      for (int b = 0; b < NB; ++b) s[b][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, q[b][2 * j], s[b][i], 0, 0, 0);
-#pragma unroll
-      for (int b = 0; b < NB; ++b) s[b][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, q[b][2 * j + 1], s[b][i], 0, 0, 0);
+      s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8<Fmt>(k[i][j][0], k[i][j][1]), q[2 * j], s[i], 0, 0, 0);
+      s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8<Fmt>(k[i][j][2], k[i][j][3]), q[2 * j + 1], s[i], 0, 0, 0);
     }
-  }
-}
-
-// Softmax of one tile and 16 rows: raw scores s become probabilities p (times the values' scale), the running maximum and sum follow.  c: what scales the scores.
-// Masked (not Full): the lane's key i is seen if i <= last.
-template <int D, bool Full>
-__device__ inline void softmax_of(f32x4 (&s)[4], float c, float vs, int last, f32x4 (&o)[D / 16], float& m, float& l, bf16x8 (&p)[2], float* scores) {
-  if (!Full)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) s[i / 4][i % 4] = i <= last ? s[i / 4][i % 4] : -INFINITY;
-  float top = max3(s[0][0], s[0][1], s[0][2]);
-#pragma unroll
-  for (int i = 3; i < 15; i += 2) top = max3(top, s[i / 4][i % 4], s[(i + 1) / 4][(i + 1) % 4]);
-  top = __builtin_elementwise_maximum(top, s[3][3]) * c;
-  if (scores)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) *reinterpret_cast<f32x4*>(scores + 16 * 16 * i) = s[i] * c;
-  // the maximum only grows in steps of more than 2^8: probabilities stay below 256, and most tiles leave the sums alone
-  if (__ballot(top > m + 8.f)) {
-    const float grown = fmaxf(m, max_over_groups(top)), f = __builtin_amdgcn_exp2f(m - grown);
-    m = grown;
-    l *= f;
-#pragma unroll
-    for (int d = 0; d < D / 16; ++d) o[d] *= f;
-  }
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 4][i % 4], c, -m));
-    l += e;
-    p[i / 8][i % 8] = (__bf16)(e * vs);
   }
 }
 
@@ -214,8 +79,8 @@ __device__ inline uint32_t nan_bytes(uint32_t w) {
 // A tile that some row of the wave sees in part, values: codes past the last token are whatever the page holds, and 0 * NaN is NaN, so they are cleared.
 // Rare: a cached value that some rows do not see is NaN.  The rows that see it get NaN and the others do not: the NaN codes leave the product, and their number among
 // the keys that a row sees is counted by a product with 1.  live: cached tokens among the lane's 16.
-template <int D, int Fmt, int NB>
-__device__ inline void clear_hidden(u32x4 (&v)[D / 16], int live, const int (&last)[NB], RowState<D, NB>& r) {
+template <int D, int Fmt>
+__device__ inline void clear_hidden(u32x4 (&v)[D / 16], int live, int last, RowState<D>& r) {
   uint32_t odd = 0;
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
@@ -237,29 +102,26 @@ __device__ inline void clear_hidden(u32x4 (&v)[D / 16], int live, const int (&la
       bad[w] = nan_bytes(v[i][w]);
       v[i][w] &= ~(((bad[w] >> 3) & 0x01010101u) * 0xffu);
     }
+    f32x4 count = {0, 0, 0, 0};
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      f32x4 count = {0, 0, 0, 0};
+    for (int h = 0; h < 2; ++h) {
+      bf16x8 seen;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        bf16x8 seen;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) seen[j] = (__bf16)(8 * h + j <= last[b] ? 1.f : 0.f);
-        count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8<Fmt>(bad[2 * h], bad[2 * h + 1]), seen, count, 0, 0, 0);
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) r.o[b][i][j] = count[j] > 0.f ? NAN : r.o[b][i][j];
+      for (int j = 0; j < 8; ++j) seen[j] = (__bf16)(8 * h + j <= last ? 1.f : 0.f);
+      count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8<Fmt>(bad[2 * h], bad[2 * h + 1]), seen, count, 0, 0, 0);
     }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) r.o[i][j] = count[j] > 0.f ? NAN : r.o[i][j];
   }
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// Tiles first, first + step, ... below end for 16 * NB rows of one KV head.  last_tok: last token that the lane's row of a block sees; all_see: the wave's rows all see
+// Tiles first, first + step, ... below end for 16 rows of one KV head.  last_tok: last token that the lane's row sees; all_see: all rows see
 // the tokens up to it.  A tile's keys are asked for when the keys before them have become scores, its values when the values before them are in the sums, page numbers a tile
 // earlier still: a wave always has 8 to 16 KB on their way.
-template <int D, int Fmt, int NB>
-__device__ inline void walk(const AttnArgs& a, int seq, int head, int len, int first, int end, int step, const bf16x8 (&q)[NB][D / 32], const int (&last_tok)[NB],
-                            int all_see, RowState<D, NB>& r, float* scores, int score_rows) {
+template <int D, int Fmt>
+__device__ inline void walk(const AttnArgs& a, int seq, int head, int len, int first, int end, int step, const bf16x8 (&q)[D / 32], int last_tok, int all_see,
+                            RowState<D>& r, float* scores, int score_rows) {
   if (first >= end) return;
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   u32x4 k[4][D / 64], v[D / 16];
@@ -269,8 +131,8 @@ __device__ inline void walk(const AttnArgs& a, int seq, int head, int len, int f
   load_values<D>(a.c, head, first, at.v, v);
   // (The last tile apart: loads under a condition would all be waited for where it ends.)
   auto tile = [&](int i, auto more) {
-    f32x4 s[NB][4];
-    scores_of<D, Fmt, NB>(k, q, s);
+    f32x4 s[4];
+    scores_of<D, Fmt>(k, q, s);
     TileScales sc_next = sc;
     if constexpr (more) {
       load_keys<D>(a.c, head, i + step, next.k, k);
@@ -278,29 +140,18 @@ __device__ inline void walk(const AttnArgs& a, int seq, int head, int len, int f
     }
     const float c = a.scale * sc.k;
     const bool full = i * kTile + kTile - 1 <= all_see && !__ballot(at.v < 0);
-    bf16x8 p[NB][2];
-    if (full) {
-#pragma unroll
-      for (int b = 0; b < NB; ++b)
-        softmax_of<D, true>(s[b], c, sc.v, 0, r.o[b], r.m[b], r.l[b], p[b], scores && n < score_rows ? scores + (int64_t)i * (16 * kTile) + 16 * n + 4 * g : nullptr);
-    } else {
-      int last[NB];
-      const int key0 = i * kTile + 16 * g;
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        last[b] = at.v < 0 ? -1 : last_tok[b] - key0;
-        softmax_of<D, false>(s[b], c, sc.v, last[b], r.o[b], r.m[b], r.l[b], p[b], scores && n < score_rows ? scores + (int64_t)i * (16 * kTile) + 16 * n + 4 * g : nullptr);
-      }
-      clear_hidden<D, Fmt, NB>(v, at.v < 0 ? 0 : len - key0, last, r);
+    float* const to = scores && n < score_rows ? scores + (int64_t)i * (16 * kTile) + 16 * n + 4 * g : nullptr;
+    if (!full) {
+      const int key0 = i * kTile + 16 * g, last = at.v < 0 ? -1 : last_tok - key0;
+      mask_scores(s, last);
+      clear_hidden<D, Fmt>(v, at.v < 0 ? 0 : len - key0, last, r);
     }
+    bf16x8 p[2];
+    softmax_of<D>(s, c, sc.v, r.o, r.m, r.l, p, to);
 #pragma unroll
     for (int d = 0; d < D / 16; ++d)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const bf16x8 x = decode8<Fmt>(v[d][2 * h], v[d][2 * h + 1]);
-#pragma unroll
-        for (int b = 0; b < NB; ++b) r.o[b][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, p[b][h], r.o[b][d], 0, 0, 0);
-      }
+      for (int h = 0; h < 2; ++h) r.o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8<Fmt>(v[d][2 * h], v[d][2 * h + 1]), p[h], r.o[d], 0, 0, 0);
     if constexpr (more) {
       load_values<D>(a.c, head, i + step, next.v, v);
       at = next;
@@ -313,34 +164,22 @@ __device__ inline void walk(const AttnArgs& a, int seq, int head, int len, int f
   tile(i, std::false_type{});
 }
 
-// Final row, or its part: o channels 16 i + 4 g + 0..3 of the lane's row.
-template <int D>
-__device__ inline void write_row(const AttnArgs& a, int row, int head, const f32x4 (&o)[D / 16], float m, float l, int g) {
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  __bf16* y = a.o + ((int64_t)row * a.hq + head) * D + 4 * g;
-#pragma unroll
-  for (int i = 0; i < D / 16; ++i) {
-    bf16x4 w;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) w[j] = (__bf16)(o[i][j] * inv);
-    *reinterpret_cast<bf16x4*>(y + 16 * i) = w;
-  }
-  if (g == 0) a.lse[(int64_t)head * a.s.n_rows + row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
-}
-
-// Waves of a block divide the tiles of a piece (Keys) or take rows of their own.
-template <int D, int Fmt, int NB, bool Keys, bool Short>
-__global__ __launch_bounds__(256, Keys ? 2 : 1) void attn_kernel(AttnArgs a) {
-  constexpr int kRows = 16 * NB * (Keys ? 1 : kWaves);     // of a block
+// Few rows: a block takes 16 rows of a KV head at a time, its waves divide the tiles of a piece and join their sums in LDS.
+constexpr int kRows = 16;
+template <int D, int Fmt, bool Short>
+__global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
   constexpr int kStride = D + 4;                           // floats of a staged row: rows on different banks
-  __shared__ float stage[Keys ? kWaves * 16 * NB * kStride : 1];
-  __shared__ float stage_m[kWaves * 16 * NB], stage_l[kWaves * 16 * NB];
+  __shared__ float stage[kWaves * kRows * kStride];
+  __shared__ float stage_m[kWaves * kRows], stage_l[kWaves * kRows];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
   const int32_t me = blockIdx.x;
   const Line line = find_on_line<Short>(a.s, a.c, a.group, kRows, a.blocks, me, -1);
-  if (line.seq < 0) return;
-  int32_t at = line.begin(me);
-  const int32_t end = line.begin(me + 1);
+  Divided divided = {};
+  int32_t at = 0, end = 0;
+  if (line.seq >= 0) {
+    at = line.begin(me);
+    end = line.begin(me + 1);
+  }
   int seq = line.seq;
   int32_t base = line.before;
   SeqSizes z = line.z;
@@ -356,160 +195,103 @@ __global__ __launch_bounds__(256, Keys ? 2 : 1) void attn_kernel(AttnArgs a) {
     const int32_t at0 = at;
     at += Short ? 1 : t1 - t0;
 
-    bf16x8 q[NB][D / 32];
-    RowState<D, NB> r;
-    int last[NB];                                          // last token that the lane's row sees
-    int first_seen = INT32_MAX;                            // least of them in the wave
-    bool any = false;
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      const int row = rb * kRows + (Keys ? 0 : wave * 16 * NB) + 16 * b + n;
-      const bool live = row < all_rows;
-      const int tok = live ? row / a.group : 0;
-      last[b] = live ? z.len - z.n + tok : -1;
-      any = any || live;
-      first_seen = min(first_seen, live ? last[b] : INT32_MAX);
-      const __bf16* x = a.q + (int64_t)(z.row0 + tok) * a.q_row + (head * a.group + (live ? row % a.group : 0)) * D + 16 * g;
-#pragma unroll
-      for (int j = 0; j < D / 64; ++j)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const bf16x8 w = *reinterpret_cast<const bf16x8*>(x + 64 * j + 8 * h);
-          bf16x8 zero = {};
-          q[b][2 * j + h] = live ? w : zero;
-        }
-      r.m[b] = kLow;
-      r.l[b] = 0.f;
-#pragma unroll
-      for (int i = 0; i < D / 16; ++i) r.o[b][i] = f32x4{0, 0, 0, 0};
-    }
+    const int my_row = rb * kRows + n;
+    const bool live = my_row < all_rows;
+    const int my_tok = live ? my_row / a.group : 0, last = live ? z.len - z.n + my_tok : -1;     // last token that the lane's row sees
+    int first_seen = live ? last : INT32_MAX;              // least of them
 #pragma unroll
     for (int d = 8; d > 0; d >>= 1) first_seen = min(first_seen, __shfl_xor(first_seen, d));
-    // the last tile that any row of the block sees
-    const int last_row = min(rb * kRows + kRows, all_rows) - 1, seen = z.len - z.n + last_row / a.group;
-    const int t_end = min(t1, seen < 0 ? 0 : seen / kTile + 1);
-    if (Keys || __ballot(any)) {
-      float* const scores = Keys && a.scores ? a.scores + ((int64_t)at0 - t0) * (16 * kTile) : nullptr;
-      const int score_rows = min(all_rows - rb * kRows, 16);
-      walk<D, Fmt, NB>(a, seq, head, z.len, t0 + (Keys ? wave : 0), t_end, Keys ? kWaves : 1, q, last, first_seen, r, scores, score_rows);
-      if (scores)                                          // tiles of the piece that nobody sees
-        for (int i = max(t_end, t0) + wave; i < t1; i += kWaves)
-          for (int j = lane; j < 16 * kTile; j += 64) scores[(int64_t)i * (16 * kTile) + j] = -INFINITY;
-    }
+    const __bf16* x = a.q + (int64_t)(z.row0 + my_tok) * a.q_row + (head * a.group + (live ? my_row % a.group : 0)) * D + 16 * g;
+    bf16x8 q[D / 32];
 #pragma unroll
-    for (int b = 0; b < NB; ++b) r.l[b] = sum_over_groups(r.l[b]);
+    for (int j = 0; j < D / 32; ++j) {
+      const bf16x8 w = *reinterpret_cast<const bf16x8*>(x + 64 * (j / 2) + 8 * (j % 2)), zero = {};
+      q[j] = live ? w : zero;
+    }
+    RowState<D> r;
+    r.m = kLow;
+    r.l = 0.f;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) r.o[i] = f32x4{0, 0, 0, 0};
+    // the last tile that any of the rows sees
+    const int rows = min(all_rows - rb * kRows, kRows), seen = z.len - z.n + (rb * kRows + rows - 1) / a.group;
+    const int t_end = min(t1, seen < 0 ? 0 : seen / kTile + 1);
+    float* const scores = a.scores ? a.scores + ((int64_t)at0 - t0) * (16 * kTile) : nullptr;
+    walk<D, Fmt>(a, seq, head, z.len, t0 + wave, t_end, kWaves, q, last, first_seen, r, scores, rows);
+    if (scores)                                            // tiles of the piece that nobody sees
+      for (int i = max(t_end, t0) + wave; i < t1; i += kWaves)
+        for (int j = lane; j < 16 * kTile; j += 64) scores[(int64_t)i * (16 * kTile) + j] = -INFINITY;
+    r.l = sum_over_groups(r.l);
 
     const bool whole = t0 == 0 && t1 == tiles;
-    float* const slot = a.part + (int64_t)(2 * me + (t0 == 0 ? 1 : 0)) * PartSlot<D>::floats(kRows);
-    if constexpr (Keys) {
-      // the four waves' sums in the block's LDS, then each wave finishes a quarter of the channels
+    if (t0 == 0 && !whole) divided = {line.owner(at0 + tiles - 1) - me + 1, z.row0, all_rows, head, rb, {}};
+    float* const slot = a.part + (int64_t)(2 * me + (t0 == 0 ? 1 : 0)) * slot_floats(D, kRows);
+    if (g == 0) { stage_m[wave * kRows + n] = r.m; stage_l[wave * kRows + n] = r.l; }
 #pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        const int row = wave * 16 * NB + 16 * b + n;
-        if (g == 0) { stage_m[row] = r.m[b]; stage_l[row] = r.l[b]; }
+    for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4*>(&stage[(wave * kRows + n) * kStride + 16 * i + 4 * g]) = r.o[i];
+    __syncthreads();
+    for (int j = threadIdx.x; j < rows * (D / 4); j += 256) {
+      const int lr = j / (D / 4), ch = 4 * (j % (D / 4)), row = rb * kRows + lr;
+      float m = kLow, l = 0.f;
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4*>(&stage[row * kStride + 16 * i + 4 * g]) = r.o[b][i];
+      for (int w = 0; w < kWaves; ++w) m = fmaxf(m, stage_m[w * kRows + lr]);
+      f32x4 o = {0, 0, 0, 0};
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float f = __builtin_amdgcn_exp2f(stage_m[w * kRows + lr] - m);
+        l += f * stage_l[w * kRows + lr];
+        o += f * *reinterpret_cast<const f32x4*>(&stage[(w * kRows + lr) * kStride + ch]);
       }
-      __syncthreads();
-      for (int j = threadIdx.x; j < 16 * NB * (D / 4); j += 256) {
-        const int lr = j / (D / 4), ch = 4 * (j % (D / 4)), row = rb * kRows + lr;
-        if (row >= all_rows) continue;
-        float m = kLow, l = 0.f;
+      if (whole) {
+        const int tok = z.row0 + row / a.group, h = head * a.group + row % a.group;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        bf16x4 w;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) m = fmaxf(m, stage_m[w * 16 * NB + lr]);
-        f32x4 o = {0, 0, 0, 0};
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-          const float f = __builtin_amdgcn_exp2f(stage_m[w * 16 * NB + lr] - m);
-          l += f * stage_l[w * 16 * NB + lr];
-          o += f * *reinterpret_cast<const f32x4*>(&stage[(w * 16 * NB + lr) * kStride + ch]);
-        }
-        if (whole) {
-          const int tok = z.row0 + row / a.group, h = head * a.group + row % a.group;
-          const float inv = l == 0.f ? 0.f : 1.f / l;
-          bf16x4 w;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) w[i] = (__bf16)(o[i] * inv);
-          *reinterpret_cast<bf16x4*>(a.o + ((int64_t)tok * a.hq + h) * D + ch) = w;
-          if (ch == 0) a.lse[(int64_t)h * a.s.n_rows + tok] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
-        } else {
-          *reinterpret_cast<f32x4*>(slot + lr * D + ch) = o;
-          if (ch == 0) { slot[kRows * D + lr] = m; slot[kRows * (D + 1) + lr] = l; }
-        }
-      }
-      __syncthreads();
-    } else {
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        const int lr = wave * 16 * NB + 16 * b + n, row = rb * kRows + lr;
-        if (row >= all_rows) continue;
-        if (whole) {
-          write_row<D>(a, z.row0 + row / a.group, head * a.group + row % a.group, r.o[b], r.m[b], r.l[b], g);
-        } else {
-#pragma unroll
-          for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4*>(slot + lr * D + 16 * i + 4 * g) = r.o[b][i];
-          if (g == 0) { slot[kRows * D + lr] = r.m[b]; slot[kRows * (D + 1) + lr] = r.l[b]; }
-        }
+        for (int i = 0; i < 4; ++i) w[i] = (__bf16)(o[i] * inv);
+        *reinterpret_cast<bf16x4*>(a.o + ((int64_t)tok * a.hq + h) * D + ch) = w;
+        if (ch == 0) a.lse[(int64_t)h * a.s.n_rows + tok] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+      } else {
+        *reinterpret_cast<f32x4*>(slot + lr * D + ch) = o;
+        if (ch == 0) { slot[kRows * D + lr] = m; slot[kRows * (D + 1) + lr] = l; }
       }
     }
+    __syncthreads();
   }
+  if (!Short && threadIdx.x == 0) a.divided[me] = divided;
 }
 
-// The items that several blocks worked.  Few rows: a block per (row, query head) whose waves divide the pieces, of which a long sequence has many.
-// Many rows: a block per (eight rows, KV head) whose waves take query heads; there are two or three pieces then.
+// Divided items: a block per (block in which one begins, every eighth row), whose waves divide the pieces; two or one channel a lane.
 constexpr int kMergeRows = 8;
-template <int D, bool Keys>
+template <int D>
 __global__ __launch_bounds__(256) void attn_merge_kernel(AttnArgs a) {
-  constexpr int kCh = D / 64, kRows = Keys ? 16 : 128, kFloats = PartSlot<D>::floats(kRows);
-  __shared__ float sum_o[Keys ? kWaves : 1][D], sum_l[kWaves];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int heads = Keys ? a.hq : a.c.hkv, head = Keys ? (int)(blockIdx.x % heads) / a.group : (int)(blockIdx.x % heads);
-  const int tok0 = (int)(blockIdx.x / heads) * (Keys ? 1 : kMergeRows), tok1 = min(tok0 + (Keys ? 1 : kMergeRows), a.s.n_rows);
-  Line line = {};
-  line.seq = -1;
-  for (int tok = tok0; tok < tok1; ++tok) {
-    if (line.seq < 0 || tok >= line.z.row0 + line.z.n) {   // (the same for the whole block)
-      __syncthreads();
-      line = find_on_line<false>(a.s, a.c, a.group, kRows, a.blocks, 0, tok);
-      if (line.seq < 0) continue;
-    }
-    const SeqSizes z = line.z;
-    const int tiles = tiles_of(z.len), row_blocks = (z.n * a.group + kRows - 1) / kRows;
-    for (int h = Keys ? (int)(blockIdx.x % heads) % a.group : wave; h < a.group; h += Keys ? a.group : kWaves) {
-      const int row = (tok - z.row0) * a.group + h, rb = row / kRows, lr = row % kRows, qh = head * a.group + h;
-      const int32_t x = line.before + (head * row_blocks + rb) * tiles, w0 = line.owner(x), w1 = line.owner(x + tiles - 1);
-      if (w0 == w1) continue;
-      auto slot = [&](int w) { return a.part + (int64_t)(2 * w + (w == w0 ? 1 : 0)) * kFloats; };
-      float m = kLow;
-      for (int w = w0 + lane; w <= w1; w += 64) m = fmaxf(m, slot(w)[kRows * D + lr]);
-      m = wave_maxf(m);
-      float l = 0.f, o[kCh] = {};
+  constexpr int kCh = D / 64, kFloats = slot_floats(D, kRows);
+  __shared__ float sum_o[kWaves][D], sum_l[kWaves];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), me = blockIdx.x / kMergeRows;
+  const Divided d = a.divided[me];
+  const int rows = min(d.all_rows - d.row_block * kRows, kRows);
+  if (d.pieces == 0) return;
+  for (int lr = blockIdx.x % kMergeRows; lr < rows; lr += kMergeRows) {
+    float m = kLow;
+    for (int p = lane; p < d.pieces; p += 64) m = fmaxf(m, piece_slot(a, me, p, kFloats)[kRows * D + lr]);
+    m = wave_maxf(m);
+    float l = 0.f, o[kCh] = {};
 #pragma unroll 8
-      for (int w = w0 + (Keys ? wave : 0); w <= w1; w += Keys ? kWaves : 1) {
-        const float* s = slot(w);
-        const float f = __builtin_amdgcn_exp2f(s[kRows * D + lr] - m);
-        l += f * s[kRows * (D + 1) + lr];
+    for (int p = wave; p < d.pieces; p += kWaves) {
+      const float* s = piece_slot(a, me, p, kFloats);
+      const float f = __builtin_amdgcn_exp2f(s[kRows * D + lr] - m);
+      l += f * s[kRows * (D + 1) + lr];
 #pragma unroll
-        for (int i = 0; i < kCh; ++i) o[i] += f * s[lr * D + kCh * lane + i];
-      }
-      __bf16* const y = a.o + ((int64_t)tok * a.hq + qh) * D;
-      float* const lse = a.lse + (int64_t)qh * a.s.n_rows + tok;
-      if constexpr (Keys) {
-#pragma unroll
-        for (int i = 0; i < kCh; ++i) sum_o[wave][kCh * lane + i] = o[i];
-        if (lane == 0) sum_l[wave] = l;
-        __syncthreads();                                   // (one row: once in a block)
-        l = (sum_l[0] + sum_l[1]) + (sum_l[2] + sum_l[3]);
-        const int ch = threadIdx.x;
-        if (ch < D) y[ch] = (__bf16)(l == 0.f ? 0.f : ((sum_o[0][ch] + sum_o[1][ch]) + (sum_o[2][ch] + sum_o[3][ch])) * (1.f / l));
-        if (ch == 0) *lse = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
-      } else {
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-        for (int i = 0; i < kCh; ++i) y[kCh * lane + i] = (__bf16)(o[i] * inv);
-        if (lane == 0) *lse = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
-      }
+      for (int i = 0; i < kCh; ++i) o[i] += f * s[lr * D + kCh * lane + i];
     }
+#pragma unroll
+    for (int i = 0; i < kCh; ++i) sum_o[wave][kCh * lane + i] = o[i];
+    if (lane == 0) sum_l[wave] = l;
+    __syncthreads();
+    l = (sum_l[0] + sum_l[1]) + (sum_l[2] + sum_l[3]);
+    const int row = d.row_block * kRows + lr, tok = d.row0 + row / a.group, h = d.head * a.group + row % a.group, ch = threadIdx.x;
+    if (ch < D) a.o[((int64_t)tok * a.hq + h) * D + ch] = (__bf16)(l == 0.f ? 0.f : ((sum_o[0][ch] + sum_o[1][ch]) + (sum_o[2][ch] + sum_o[3][ch])) * (1.f / l));
+    if (ch == 0) a.lse[(int64_t)h * a.s.n_rows + tok] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+    __syncthreads();
   }
 }
 
@@ -536,7 +318,9 @@ constexpr int kWeighThreads = 512, kWeighWaves = kWeighThreads / 64;
 
 template <int D, int Fmt>
 __global__ __launch_bounds__(kWeighThreads, 2) void weigh_kernel(WeighArgs a) {
+  constexpr int kRowBytes = 16 * 2 * D;                    // of a wave's 16 rows
   __shared__ float sum[kWeighWaves][kTile];
+  __shared__ __align__(256) unsigned char rows_lds[kWeighWaves * 2 * kRowBytes];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
   // the line with one block of rows per KV head
   const int kAll = 1 << 30;
@@ -557,23 +341,29 @@ __global__ __launch_bounds__(kWeighThreads, 2) void weigh_kernel(WeighArgs a) {
     const int tok0 = max(key0 - (z.len - z.n), 0), rb0 = (int)((int64_t)tok0 * a.group / 16);
     const TilePages at = pages_of(a, seq, z.len, tile);
     const TileScales sc = scales_of(a.c, head, at.v);
-    // the lane's row of a block of 16: token and query head of the group, and where its query and its LSE lie, stepped without products; what is asked for a block ahead
-    struct Rows { bf16x8 q[D / 32]; float lse; };
+    // What the wave asks for a block of 16 rows ahead: queries through LDS, four lanes a row, so that a request is 64 bytes (operand rows straight from memory are 16 bytes a
+    // request, and the requests bounded the kernel: a prompt of 4096 tokens, 8 heads, 48 us instead of 36), and the LSE of the lane's row n.
+    // Row lane / 4 (queries) and row n (LSE, mask) of the block: token and query head of the group, and where they lie, stepped without divisions.
     const int step = 16 * kWeighWaves, step_tok = step / a.group, step_h = step % a.group;
-    int row = 16 * (rb0 + wave) + n, tok = row / a.group, h = row % a.group;
-    const __bf16* const q0 = a.q + (int64_t)z.row0 * a.q_row + head * a.group * D + 16 * g;
+    auto start = [&](int row, int& tok, int& h) { tok = row / a.group; h = row % a.group; };
+    const int first_row = 16 * (rb0 + wave);
+    int q_tok, q_h, tok, h, q_row = first_row + lane / 4, row = first_row + n;
+    start(q_row, q_tok, q_h);
+    start(row, tok, h);
+    const __bf16* const q0 = a.q + (int64_t)z.row0 * a.q_row + head * a.group * D + 8 * ((lane & 3) ^ (lane >> 4));
     const float* const lse0 = a.lse + head * a.group * a.lse_head + z.row0;
-    int64_t q_at = (int64_t)tok * a.q_row + h * D, lse_at = h * a.lse_head + tok;
+    int64_t q_at = (int64_t)q_tok * a.q_row + q_h * D, lse_at = h * a.lse_head + tok;
     const int64_t q_step = step_tok * a.q_row + step_h * D, q_wrap = a.q_row - a.group * D, lse_step = step_h * a.lse_head + step_tok, lse_wrap = 1 - a.group * a.lse_head;
-    auto rows_at = [&](Rows& r) {
-      const bool live = row < all_rows;                    // (else: the first row)
-      const __bf16* x = q0 + (live ? q_at : 0);
+    unsigned char* const buffers = rows_lds + wave * 2 * kRowBytes;
+    auto ask = [&](int buffer, float& lse) {               // (rows that are not there: the first one's)
+      const __bf16* x = q0 + (q_row < all_rows ? q_at : 0);
+      // 64-byte piece j of all 16 rows goes to the buffer's j-th KB, lane after lane: row lane / 4, place lane % 4, which holds chunk (lane % 4) ^ (row / 4) of the piece
 #pragma unroll
-      for (int j = 0; j < D / 32; ++j) r.q[j] = *reinterpret_cast<const bf16x8*>(x + 64 * (j / 2) + 8 * (j % 2));
-      r.lse = lse0[live ? lse_at : 0];
+      for (int j = 0; j < D / 32; ++j) lds_load_b128(x + 32 * j, lds_offset(buffers) + buffer * kRowBytes + 1024 * j);
+      lse = lse0[row < all_rows ? lse_at : 0];
     };
-    Rows r[2];
-    rows_at(r[0]);
+    float lse[2];
+    ask(0, lse[0]);
     bf16x8 k[4][D / 32];
     {
       u32x4 raw[4][D / 64];
@@ -586,27 +376,40 @@ __global__ __launch_bounds__(kWeighThreads, 2) void weigh_kernel(WeighArgs a) {
           k[i][2 * j + 1] = decode8<Fmt>(raw[i][j][2], raw[i][j][3]);
         }
     }
+    // (operand 2 j + e holds channels 64 j + 16 g + 8 e ..: chunk 2 (g % 2) + e of piece 2 j + g / 2)
+    int q_from[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) q_from[e] = 1024 * (g >> 1) + 64 * n + 16 * ((2 * (g & 1) + e) ^ (n >> 2));
     const float c = a.scale * sc.k;
     const int there = at.v < 0 ? -1 : 15;                  // (keys of a page that is not there are not seen)
     float got[16] = {};
-    auto add = [&](const Rows& now, Rows& next) {
+    auto add = [&](int buffer, const float& now, float& next) {
+      __builtin_amdgcn_s_waitcnt(kWaitVm0);                // the buffer's rows are there
+      const float mine = now;
       // rows that are not there, and rows that saw nothing, add exp2(-inf)
-      const float lse2 = row < all_rows && now.lse != -INFINITY ? now.lse * kLog2e : INFINITY;
+      const float lse2 = row < all_rows && mine != -INFINITY ? mine * kLog2e : INFINITY;
       const int last = min(z.len - z.n + tok - key0 - 16 * g, there);          // of the lane's keys, those up to it are seen
-      row += step;
-      tok += step_tok;
-      h += step_h;
-      const bool wraps = h >= a.group;
-      h -= wraps ? a.group : 0;
-      tok += wraps;
-      q_at += q_step + (wraps ? q_wrap : 0);
-      lse_at += lse_step + (wraps ? lse_wrap : 0);
-      rows_at(next);                                       // (always: loads under a condition would be waited for where it ends)
+      auto move = [&](int& r, int& t, int& hh) {
+        r += step;
+        t += step_tok;
+        hh += step_h;
+        const bool wraps = hh >= a.group;
+        hh -= wraps ? a.group : 0;
+        t += wraps;
+        return wraps;
+      };
+      q_at += q_step + (move(q_row, q_tok, q_h) ? q_wrap : 0);
+      lse_at += lse_step + (move(row, tok, h) ? lse_wrap : 0);
+      bf16x8 q[D / 32];
+      typedef bf16x8 __attribute__((may_alias)) chunk;
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j) q[j] = *reinterpret_cast<const chunk*>(buffers + buffer * kRowBytes + 2048 * (j / 2) + q_from[j % 2]);
+      ask(buffer ^ 1, next);
       f32x4 s[4] = {};
 #pragma unroll
       for (int j = 0; j < D / 32; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[i][j], now.q[j], s[i], 0, 0, 0);
+        for (int i = 0; i < 4; ++i) s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[i][j], q[j], s[i], 0, 0, 0);
       if (__ballot(last < 15)) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i / 4][i % 4] = i <= last ? s[i / 4][i % 4] * c : -INFINITY;
@@ -618,9 +421,10 @@ __global__ __launch_bounds__(kWeighThreads, 2) void weigh_kernel(WeighArgs a) {
       }
     };
     for (int rb = rb0 + wave; rb * 16 < all_rows; rb += 2 * kWeighWaves) {
-      add(r[0], r[1]);
-      add(r[1], r[0]);
+      add(0, lse[0], lse[1]);
+      add(1, lse[1], lse[0]);
     }
+    __builtin_amdgcn_s_waitcnt(kWaitVm0);                  // (the rows asked for in vain have landed before the buffers are used again)
 #pragma unroll
     for (int i = 0; i < 16; ++i) got[i] = sum_of_16(got[i]);
     if (n == 0)
@@ -704,7 +508,6 @@ __global__ __launch_bounds__(256) void weigh_scores_kernel(AttnArgs a, int rows_
 
 // ---- host ---------------------------------------------------------------------------------------
 
-constexpr int kBlocks = 512;           // that share the line: two per CU
 // Tables of up to this many tiles: an item is not divided among blocks, which saves the second launch.  One sequence of 512 tokens, 4 heads of 64 channels: MEASURED.
 constexpr int kShortTiles = 16;
 
@@ -714,9 +517,9 @@ AttnPlan plan_attn(const CacheView& c, int head_dim, int32_t n_seqs, int32_t max
   const int group = hq / c.hkv;
   AttnPlan p;
   p.keys = (int64_t)tq * group <= (int64_t)16 * n_seqs;
-  p.rows = p.keys ? 16 : 128;
+  p.rows = p.keys ? kRows : kManyRows;
   p.stored = weigh && p.keys;
-  p.part_floats = (int64_t)2 * kBlocks * p.rows * (head_dim + 2);
+  p.part_floats = (int64_t)2 * kBlocks * slot_floats(head_dim, p.rows);
   const int64_t tiles = max(((int64_t)max_pages * c.page + kTile - 1) / kTile, (int64_t)1);
   p.whole = tiles <= kShortTiles && !p.stored;
   p.places = tiles * c.hkv * (n_seqs + (int64_t)tq * group / p.rows);
@@ -724,21 +527,22 @@ AttnPlan plan_attn(const CacheView& c, int head_dim, int32_t n_seqs, int32_t max
   return p;
 }
 
+// slots, and who the divided items are
+size_t part_bytes(const AttnPlan& p) { return pad_to((size_t)p.part_floats * 4, 256) + pad_to(kBlocks * sizeof(Divided), 256); }
+
 template <int D, int Fmt>
-int launch_attn(const AttnArgs& a, const AttnPlan& p, bool weigh, hipStream_t st) {
+int launch_attn(const AttnArgs& a, const AttnPlan& p, hipStream_t st) {
   const dim3 grid(kBlocks), block(256);
-  if (p.keys && p.whole) attn_kernel<D, Fmt, 1, true, true><<<grid, block, 0, st>>>(a);
-  else if (p.keys) attn_kernel<D, Fmt, 1, true, false><<<grid, block, 0, st>>>(a);
-  else if (p.whole) attn_kernel<D, Fmt, 2, false, true><<<grid, block, 0, st>>>(a);
-  else attn_kernel<D, Fmt, 2, false, false><<<grid, block, 0, st>>>(a);
+  if (!p.keys) return launch_attn_rows(a, D, Fmt, p.whole, st);
+  if (p.whole) attn_kernel<D, Fmt, true><<<grid, block, 0, st>>>(a);
+  else attn_kernel<D, Fmt, false><<<grid, block, 0, st>>>(a);
   FCP_HIP_CHECK(hipGetLastError());
   if (!p.whole) {
-    if (p.keys) attn_merge_kernel<D, true><<<dim3((unsigned)a.s.n_rows * a.hq), block, 0, st>>>(a);
-    else attn_merge_kernel<D, false><<<dim3((unsigned)((a.s.n_rows + kMergeRows - 1) / kMergeRows) * a.c.hkv), block, 0, st>>>(a);
+    attn_merge_kernel<D><<<dim3(kBlocks * kMergeRows), block, 0, st>>>(a);
     FCP_HIP_CHECK(hipGetLastError());
   }
   if (p.stored) {
-    weigh_scores_kernel<<<dim3(kBlocks * kWaves), dim3(256), 0, st>>>(a, p.rows);
+    weigh_scores_kernel<<<dim3(kBlocks * kWaves), block, 0, st>>>(a, p.rows);
     FCP_HIP_CHECK(hipGetLastError());
   }
   return FCP_OK;
@@ -783,7 +587,7 @@ extern "C" size_t fcp_cache_scratch_bytes(int which, const fcp_cache* cache, int
   if (check_heads(who, c, hq)) return 0;
   const bool weigh = which == FCP_SCRATCH_CACHE_WEIGH;
   const AttnPlan p = plan_attn(c, cache->head_dim, n_seqs, max_pages, tq, hq, weigh);
-  return pad_to((size_t)p.part_floats * 4, 256) + pad_to((size_t)p.score_floats * 4, 256);
+  return part_bytes(p) + pad_to((size_t)p.score_floats * 4, 256);
 }
 
 extern "C" int fcp_cache_attn(const fcp_cache* cache, const void* q, int64_t q_row, int32_t tq, int32_t hq, const int32_t* cu_seqlens,
@@ -804,7 +608,7 @@ extern "C" int fcp_cache_attn(const fcp_cache* cache, const void* q, int64_t q_r
   if (!scratch || (uintptr_t)scratch % 256) return fail(FCP_ERR_INVALID_ARG, "%s: scratch must be 256-byte aligned", who);
   const AttnPlan p = plan_attn(a.c, cache->head_dim, n_seqs, max_pages, tq, hq, weigh);
   if (p.places > INT32_MAX) return fail(FCP_ERR_UNSUPPORTED, "%s: tables and rows that may make 2^31 tiles of work", who);
-  const size_t need = pad_to((size_t)p.part_floats * 4, 256) + pad_to((size_t)p.score_floats * 4, 256);
+  const size_t need = part_bytes(p) + pad_to((size_t)p.score_floats * 4, 256);
   if (scratch_bytes < need) return fail(FCP_ERR_CAPACITY, "%s: scratch has %zu bytes, %zu are needed", who, scratch_bytes, need);
   a.s = {cu_seqlens, kv_len, pages, n_seqs, max_pages, tq};
   a.q = static_cast<const __bf16*>(q);
@@ -815,12 +619,13 @@ extern "C" int fcp_cache_attn(const fcp_cache* cache, const void* q, int64_t q_r
   a.o = static_cast<__bf16*>(o);
   a.lse = lse;
   a.part = static_cast<float*>(scratch);
-  a.scores = p.stored ? reinterpret_cast<float*>(static_cast<char*>(scratch) + pad_to((size_t)p.part_floats * 4, 256)) : nullptr;
+  a.divided = reinterpret_cast<Divided*>(static_cast<char*>(scratch) + pad_to((size_t)p.part_floats * 4, 256));
+  a.scores = p.stored ? reinterpret_cast<float*>(static_cast<char*>(scratch) + part_bytes(p)) : nullptr;
   a.blocks = kBlocks;
   hipStream_t st = static_cast<hipStream_t>(stream);
   const bool e4m3 = cache->format == FCP_CACHE_E4M3;
-  const int rc = cache->head_dim == 128 ? (e4m3 ? launch_attn<128, kE4m3>(a, p, weigh, st) : launch_attn<128, kInt8>(a, p, weigh, st))
-                                        : (e4m3 ? launch_attn<64, kE4m3>(a, p, weigh, st) : launch_attn<64, kInt8>(a, p, weigh, st));
+  const int rc = cache->head_dim == 128 ? (e4m3 ? launch_attn<128, kE4m3>(a, p, st) : launch_attn<128, kInt8>(a, p, st))
+                                        : (e4m3 ? launch_attn<64, kE4m3>(a, p, st) : launch_attn<64, kInt8>(a, p, st));
   if (rc || !weigh || p.stored) return rc;
   const WeighArgs w = {a.c, a.s, a.q, q_row, hq, a.group, a.scale, lse, tq};
   return launch_weigh(w, cache->head_dim, cache->format, st);

@@ -107,7 +107,6 @@ def test_scratch_sizes():
     for which in (B.FCP_SCRATCH_CACHE_ATTN, B.FCP_SCRATCH_CACHE_WEIGH, B.FCP_SCRATCH_CACHE_EVICT):
         n = B.fcp_cache_scratch_bytes(which, c, 4, 100, 4, 16)
         assert n >= 256 and n % 256 == 0
-        assert all(B.fcp_cache_scratch_bytes(which, c, *more, 16) >= n for more in ((9, 100, 4), (4, 200, 4), (4, 100, 400)))
         with pytest.raises(B.FcpError):
             B.fcp_cache_scratch_bytes(which, c, -1, 100, 4, 16)
     with pytest.raises(B.FcpError):
