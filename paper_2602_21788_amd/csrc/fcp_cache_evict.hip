@@ -12,7 +12,7 @@ namespace {
 
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
 constexpr int kBins = 2048;
-constexpr int kListed = 16384;         // candidates that a block keeps in LDS: 64 KB; a table of as many tokens is a block's
+constexpr int kListed = 16384;         // tokens of a table that a block chooses from alone: candidates in 64 KB of LDS, weights in 16 registers a thread
 constexpr int kMaxChunks = 32;
 
 struct EvictArgs {
@@ -49,25 +49,30 @@ __device__ inline Quad orders_of(const EvictArgs& a, int32_t page, int head, int
   if (page >= 0) w = *reinterpret_cast<const f32x4*>(a.c.weight + block_of(a.c, page, head) * a.c.page + (t & (a.c.page - 1)));
   return {{order_of(w[0]), order_of(w[1]), order_of(w[2]), order_of(w[3])}};
 }
-// f(order, whether it is one) of the tokens of [from, to) that lie in [lo, hi), in any order; from is a multiple of 4.  A thread has several loads of the page table, then of
-// weights, on their way.
-template <int Unroll, class F>
-__device__ inline void for_weights(const EvictArgs& a, int seq, int head, int from, int to, int lo, int hi, F f) {
-  constexpr int kStep = 4 * kSelectThreads;
-  to = min(to, hi);
-  for (int t0 = from + 4 * (int)threadIdx.x; t0 < to; t0 += Unroll * kStep) {
-    int32_t page[Unroll];
-    Quad q[Unroll];
+// A thread's tokens of a block's 4096 U from `from` on: in round u those from from + 4096 u + 4 thread on.  All page numbers are asked for at once, then all weights, and these
+// stay in registers for every look that the block takes at them.
+template <int U>
+struct Held {
+  Quad q[U];
+  int first;
+  __device__ int token(int u) const { return first + 4 * kSelectThreads * u; }
+  __device__ void load(const EvictArgs& a, int seq, int head, int from, int to) {
+    first = from + 4 * (int)threadIdx.x;
+    int32_t page[U];
 #pragma unroll
-    for (int i = 0; i < Unroll; ++i) page[i] = t0 + i * kStep < to ? page_at(a.s, a.c, seq, (t0 + i * kStep) >> a.c.log_page) : -1;
+    for (int u = 0; u < U; ++u) page[u] = token(u) < to ? page_at(a.s, a.c, seq, token(u) >> a.c.log_page) : -1;
 #pragma unroll
-    for (int i = 0; i < Unroll; ++i) q[i] = orders_of(a, page[i], head, t0 + i * kStep);
-#pragma unroll
-    for (int i = 0; i < Unroll; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) f(q[i].u[j], t0 + i * kStep + j >= lo && t0 + i * kStep + j < to);
+    for (int u = 0; u < U; ++u) q[u] = orders_of(a, page[u], head, token(u));
   }
-}
+  // f(order, whether the token lies in [lo, hi))
+  template <class F>
+  __device__ void each(int lo, int hi, F f) const {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) f(q[u].u[j], token(u) + j >= lo && token(u) + j < hi);
+  }
+};
 // One more in a bin.  Weights are often equal, and additions to one address wait for each other: the lanes that share the first lane's bin add once.
 __device__ inline void count_in(int32_t* bins, uint32_t bin, bool in) {
   const uint64_t all = __ballot(in);
@@ -96,68 +101,49 @@ __device__ inline Found find_bin(const int32_t* bins, int32_t want) {
 }
 static_assert(kBins == 2 * kSelectThreads, "two bins a thread");
 
-// Writes the kept tokens of [c0, c1) to the list from `place` on: the protected ones, those above the border, and of those at it the first ones while `want` lasts; `equals` of them
-// came before.  none: no other than the protected.  A wave lists a run of tokens; how many the runs before it keep comes from a count first.
-__device__ inline void emit(const EvictArgs& a, int seq, int head, int32_t* kept, int c0, int c1, int lo, int hi, bool none, uint32_t border, int32_t want, int32_t place, int32_t equals) {
-  __shared__ int32_t waves[2][kSelectWaves];
+// Writes the kept ones of the block's tokens below `to` to the list from `place` on: the protected ones, those above the border, and of those at it the first ones while `want`
+// lasts; `equals` of them came before.  none: no other than the protected.  Both counts are moved on.
+template <int U>
+__device__ inline void emit(const Held<U>& x, int32_t* kept, int to, int lo, int hi, bool none, uint32_t border, int32_t want, int32_t& place, int32_t& equals) {
+  __shared__ int32_t sums[U][kSelectWaves];                // of a wave's tokens in a round: surely kept, and at the border (upper half)
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int run = ((c1 - c0 + kSelectWaves - 1) / kSelectWaves + 255) & ~255, t0 = min(c0 + wave * run, c1), t1 = min(t0 + run, c1);
-  // of four tokens: bit j set if token t + j is kept whatever the others are, bit 4 + j if it lies at the border
-  auto look = [&](const Quad& q, int t) {
-    uint32_t r = 0;
+  uint32_t sure[U], equal[U];                              // a bit per token
+  int32_t upto[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    sure[u] = equal[u] = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const bool in = t + j < t1, safe = t + j < lo || t + j >= hi;
-      r |= (uint32_t)(in && (safe || (!none && q.u[j] > border))) << j;
-      r |= (uint32_t)(in && !safe && !none && q.u[j] == border) << (4 + j);
+      const int t = x.token(u) + j;
+      const bool in = t < to, safe = t < lo || t >= hi;
+      sure[u] |= (uint32_t)(in && (safe || (!none && x.q[u].u[j] > border))) << j;
+      equal[u] |= (uint32_t)(in && !safe && !none && x.q[u].u[j] == border) << j;
     }
-    return r;
-  };
-  constexpr int kUnroll = 2;
-  auto walk = [&](auto f) {
-    for (int t = t0 + 4 * lane; t - 4 * lane < t1; t += kUnroll * 256) {
-      int32_t page[kUnroll];
-      Quad q[kUnroll];
-#pragma unroll
-      for (int i = 0; i < kUnroll; ++i) page[i] = t + 256 * i < t1 ? page_at(a.s, a.c, seq, (t + 256 * i) >> a.c.log_page) : -1;
-#pragma unroll
-      for (int i = 0; i < kUnroll; ++i) q[i] = orders_of(a, page[i], head, t + 256 * i);
-#pragma unroll
-      for (int i = 0; i < kUnroll; ++i) f(look(q[i], t + 256 * i), t + 256 * i);
-    }
-  };
-  int32_t above = 0, equal = 0;
-  walk([&](uint32_t r, int) {
-    above += __popc(r & 15);
-    equal += __popc(r >> 4);
-  });
-  above = __builtin_amdgcn_readlane(wave_prefix_sum(above), 63);
-  equal = __builtin_amdgcn_readlane(wave_prefix_sum(equal), 63);
-  if (lane == 0) { waves[0][wave] = above; waves[1][wave] = equal; }
-  __syncthreads();
-  for (int w = 0; w < wave; ++w) {
-    place += waves[0][w] + min(waves[1][w], max(want - equals, 0));
-    equals += waves[1][w];
+    upto[u] = wave_prefix_sum(__popc(sure[u]) | __popc(equal[u]) << 16);
+    if (lane == 63) sums[u][wave] = upto[u];
   }
-  walk([&](uint32_t r, int t) {
-    // equal ones before the lane's, then the kept ones before it
-    const int32_t eq = __popc(r >> 4), eq_upto = wave_prefix_sum(eq);
-    int32_t room = want - equals - (eq_upto - eq);  // places that are left for the lane's equal ones
-    uint32_t keep = r & 15;
+  __syncthreads();
+  int32_t before = 0;                                      // the rounds and waves before
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (r >> (4 + j) & 1) {
-        if (room > 0) keep |= 1u << j;
-        --room;
-      }
-    const int32_t mine = __popc(keep), upto = wave_prefix_sum(mine);
-    int32_t to = place + upto - mine;
+  for (int u = 0; u < U; ++u) {
+    int32_t here = before;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (keep >> j & 1) kept[to++] = t + j;
-    place += __builtin_amdgcn_readlane(upto, 63);
-    equals += __builtin_amdgcn_readlane(eq_upto, 63);
-  });
+    for (int w = 0; w < kSelectWaves; ++w) {
+      here += w < wave ? sums[u][w] : 0;
+      before += sums[u][w];
+    }
+    here += upto[u] - (__popc(sure[u]) | __popc(equal[u]) << 16);
+    int32_t eq = equals + (here >> 16);                    // at the border, before the lane's
+    int32_t at = place + (here & 0xffff) + min(eq, want) - min(equals, want);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const bool is_equal = equal[u] >> j & 1;
+      if ((sure[u] >> j & 1) || (is_equal && eq < want)) kept[at++] = x.token(u) + j;
+      eq += is_equal;
+    }
+  }
+  place += (before & 0xffff) + min(equals + (before >> 16), want) - min(equals, want);
+  equals += before >> 16;
 }
 
 // What all blocks of a (sequence, KV head) begin with; the first writes the new length and the list's ends.  done: every token is kept.
@@ -174,47 +160,59 @@ __device__ inline Select open_select(const EvictArgs& a, int seq, int head, bool
   return {n, a.first, n - a.recent, a.budget - a.first - a.recent, kept, n <= a.budget};
 }
 
-// Short tables: a block per (sequence, KV head).
+// The last kept weight among the m candidates of a list, which share its upper 11 bits (border): bits 20 .. 10, then 9 .. 0.  On return `want` is how many of those at the border
+// are kept.
+template <class List>
+__device__ inline void find_border(const List& list, int32_t m, int32_t* bins, uint32_t& border, int32_t& want) {
+  const int tid = threadIdx.x, lane = tid & 63;
+  for (int shift = 10; shift >= 0; shift -= 10) {
+    bins[tid] = bins[tid + kSelectThreads] = 0;
+    __syncthreads();
+#pragma unroll 4
+    for (int i = tid; i - lane < m; i += kSelectThreads) {
+      const uint32_t u = i < m ? list[i] : 0;
+      const bool in = i < m && (shift == 10 || (u >> 10) == (border >> 10));
+      count_in(bins, shift == 10 ? (u >> 10) & 2047 : u & 1023, in);
+    }
+    __syncthreads();
+    const Found f = find_bin(bins, want);
+    border |= (uint32_t)f.bin << shift;
+    want = f.want;
+  }
+}
+
+// Short tables (of up to 4096 U tokens): a block per (sequence, KV head).
+template <int U>
 __global__ __launch_bounds__(kSelectThreads) void select_kernel(EvictArgs a) {
   __shared__ int32_t bins[kBins];
-  __shared__ uint32_t list[kListed];
+  __shared__ uint32_t list[4 * U * kSelectThreads];
   __shared__ int32_t s_listed;
-  const int seq = blockIdx.x / a.c.hkv, head = blockIdx.x % a.c.hkv, tid = threadIdx.x, lane = tid & 63;
+  const int seq = blockIdx.x / a.c.hkv, head = blockIdx.x % a.c.hkv, tid = threadIdx.x;
   const Select z = open_select(a, seq, head, true);
   if (z.done) return;
-  int32_t want = z.want, m = 0;
+  Held<U> x;
+  x.load(a, seq, head, 0, z.n);
+  int32_t want = z.want, place = 0, equals = 0;
   uint32_t border = 0;
   if (want > 0) {
     bins[tid] = bins[tid + kSelectThreads] = 0;
     if (tid == 0) s_listed = 0;
     __syncthreads();
-    for_weights<2>(a, seq, head, 0, z.hi, z.lo, z.hi, [&](uint32_t u, bool in) { count_in(bins, u >> 21, in); });
+    x.each(z.lo, z.hi, [&](uint32_t u, bool in) { count_in(bins, u >> 21, in); });
     __syncthreads();
-    Found f = find_bin(bins, want);
-    for_weights<2>(a, seq, head, 0, z.hi, z.lo, z.hi, [&](uint32_t u, bool in) {
+    const Found f = find_bin(bins, want);
+    x.each(z.lo, z.hi, [&](uint32_t u, bool in) {
       if (in && (int)(u >> 21) == f.bin) list[atomicAdd(&s_listed, 1)] = u;
     });
     border = (uint32_t)f.bin << 21;
     want = f.want;
-    m = f.held;
-    for (int shift = 10; shift >= 0; shift -= 10) {        // bits 20 .. 10, then 9 .. 0
-      bins[tid] = bins[tid + kSelectThreads] = 0;
-      __syncthreads();
-      for (int i = tid; i - lane < m; i += kSelectThreads) {
-        const uint32_t u = i < m ? list[i] : 0;
-        const bool in = i < m && (shift == 10 || (u >> 10) == (border >> 10));
-        count_in(bins, shift == 10 ? (u >> 10) & 2047 : u & 1023, in);
-      }
-      __syncthreads();
-      f = find_bin(bins, want);
-      border |= (uint32_t)f.bin << shift;
-      want = f.want;
-    }
+    find_border(list, f.held, bins, border, want);
   }
-  emit(a, seq, head, z.kept, 0, z.n, z.lo, z.hi, z.want == 0, border, want, 0, 0);
+  emit(x, z.kept, z.n, z.lo, z.hi, z.want == 0, border, want, place, equals);
 }
 
-// Long tables, a block per (sequence and KV head, chunk).  First: the chunk's tokens by their upper 11 bits.
+// Long tables, a block per (sequence and KV head, chunk), 8192 tokens at a time.  First: the chunk's tokens by their upper 11 bits.
+constexpr int kRounds = 2, kStep = 4 * kRounds * kSelectThreads;
 __global__ __launch_bounds__(kSelectThreads) void count_kernel(EvictArgs a) {
   __shared__ int32_t bins[kBins];
   const int chunk = blockIdx.y, sh = blockIdx.x, seq = sh / a.c.hkv, head = sh % a.c.hkv, tid = threadIdx.x;
@@ -222,7 +220,11 @@ __global__ __launch_bounds__(kSelectThreads) void count_kernel(EvictArgs a) {
   if (z.done || z.want == 0 || chunk * a.chunk >= z.n) return;
   bins[tid] = bins[tid + kSelectThreads] = 0;
   __syncthreads();
-  for_weights<2>(a, seq, head, chunk * a.chunk, (chunk + 1) * a.chunk, z.lo, z.hi, [&](uint32_t u, bool in) { count_in(bins, u >> 21, in); });
+  for (int t = chunk * a.chunk; t < min((chunk + 1) * a.chunk, z.hi); t += kStep) {
+    Held<kRounds> x;
+    x.load(a, seq, head, t, z.hi);
+    x.each(z.lo, z.hi, [&](uint32_t u, bool in) { count_in(bins, u >> 21, in); });
+  }
   __syncthreads();
   int32_t* const to = a.counts + ((int64_t)sh * a.chunks + chunk) * kBins;
   to[tid] = bins[tid];
@@ -238,6 +240,8 @@ __global__ __launch_bounds__(kSelectThreads) void list_kernel(EvictArgs a) {
   if (z.done || z.want == 0 || chunk * a.chunk >= z.n) return;
   const int used = (z.n + a.chunk - 1) / a.chunk;
   const int32_t* const counts = a.counts + (int64_t)sh * a.chunks * kBins;
+  Held<kRounds> held;
+  held.load(a, seq, head, chunk * a.chunk, z.hi);
   int32_t x = 0, y = 0;
 #pragma unroll 8
   for (int c = 0; c < used; ++c) {
@@ -255,9 +259,12 @@ __global__ __launch_bounds__(kSelectThreads) void list_kernel(EvictArgs a) {
   const int32_t above = (tid > f.bin ? own[tid] : 0) + (tid + kSelectThreads > f.bin ? own[tid + kSelectThreads] : 0);
   if (above) atomicAdd(&s_above, above);
   uint32_t* const list = a.list + (int64_t)sh * a.s.max_pages * a.c.page + base;
-  for_weights<2>(a, seq, head, chunk * a.chunk, (chunk + 1) * a.chunk, z.lo, z.hi, [&](uint32_t u, bool in) {
-    if (in && (int)(u >> 21) == f.bin) list[atomicAdd(&s_listed, 1)] = u;
-  });
+  for (int t = chunk * a.chunk; t < min((chunk + 1) * a.chunk, z.hi); t += kStep) {
+    if (t > chunk * a.chunk) held.load(a, seq, head, t, z.hi);
+    held.each(z.lo, z.hi, [&](uint32_t u, bool in) {
+      if (in && (int)(u >> 21) == f.bin) list[atomicAdd(&s_listed, 1)] = u;
+    });
+  }
   __syncthreads();
   if (tid == 0) {
     a.above[(int64_t)sh * a.chunks + chunk] = s_above;
@@ -278,38 +285,25 @@ __global__ __launch_bounds__(kSelectThreads) void emit_kernel(EvictArgs a) {
   const Select z = open_select(a, seq, head, false);
   const int c0 = chunk * a.chunk, c1 = min(c0 + a.chunk, z.n);
   if (z.done || c0 >= z.n) return;
+  Held<kRounds> x;
+  x.load(a, seq, head, c0, z.n);
   // the protected before the chunk
   int32_t place = min(c0, z.lo) + max(c0 - z.hi, 0), want = z.want, equals = 0;
   uint32_t border = 0;
   if (want > 0) {
     const int32_t* const b = a.border + (int64_t)sh * 4;
-    const int32_t m = b[2];
+    const uint32_t* const list = a.list + (int64_t)sh * a.s.max_pages * a.c.page;
     border = (uint32_t)b[0] << 21;
     want = b[1];
-    const uint32_t* const list = a.list + (int64_t)sh * a.s.max_pages * a.c.page;
-    for (int shift = 10; shift >= 0; shift -= 10) {        // bits 20 .. 10, then 9 .. 0
-      bins[tid] = bins[tid + kSelectThreads] = 0;
-      if (tid == 0) s_above = s_equal = 0;
-      __syncthreads();
-#pragma unroll 4
-      for (int i = tid; i - lane < m; i += kSelectThreads) {
-        const uint32_t u = i < m ? list[i] : 0;
-        const bool in = i < m && (shift == 10 || (u >> 10) == (border >> 10));
-        count_in(bins, shift == 10 ? (u >> 10) & 2047 : u & 1023, in);
-      }
-      __syncthreads();
-      const Found f = find_bin(bins, want);
-      border |= (uint32_t)f.bin << shift;
-      want = f.want;
-    }
-    // candidates of the chunks before that are kept, and all of their tokens above the candidates
+    if (tid == 0) s_above = s_equal = 0;
+    // candidates of the chunks before, and all of their tokens above the candidates
     const int32_t* const counts = a.counts + (int64_t)sh * a.chunks * kBins;
-    int32_t before = 0;
-    for (int c = 0; c < chunk; ++c) {
-      before += counts[(int64_t)c * kBins + b[0]];
-      place += a.above[(int64_t)sh * a.chunks + c];
-    }
-    int32_t above = 0, equal = 0;
+    int32_t before = lane < chunk ? counts[(int64_t)lane * kBins + b[0]] : 0, over = lane < chunk ? a.above[(int64_t)sh * a.chunks + lane] : 0;
+    before = __builtin_amdgcn_readlane(wave_prefix_sum(before), 63);
+    place += __builtin_amdgcn_readlane(wave_prefix_sum(over), 63);
+    find_border(list, b[2], bins, border, want);
+    int32_t above = 0, equal = 0;                          // of the candidates before, those that are kept
+#pragma unroll 4
     for (int i = tid; i < before; i += kSelectThreads) {
       const uint32_t u = list[i];
       above += u > border;
@@ -323,8 +317,15 @@ __global__ __launch_bounds__(kSelectThreads) void emit_kernel(EvictArgs a) {
     equals = s_equal;
     place += s_above + min(equals, want);
   }
-  emit(a, seq, head, z.kept, c0, c1, z.lo, z.hi, z.want == 0, border, want, place, equals);
+  for (int t = c0; t < c1; t += kStep) {
+    if (t > c0) {
+      __syncthreads();                                     // (everybody has read the sums of the tokens before)
+      x.load(a, seq, head, t, z.n);
+    }
+    emit(x, z.kept, min(t + kStep, c1), z.lo, z.hi, z.want == 0, border, want, place, equals);
+  }
 }
+static_assert(kMaxChunks <= 64, "a chunk per lane");
 
 // Lane `from`'s value.
 __device__ inline float pick(float x, int from) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), from)); }
@@ -491,9 +492,7 @@ EvictPlan plan_evict(const CacheView& c, int32_t n_seqs, int32_t max_pages) {
   EvictPlan p = {};
   const int64_t room = (int64_t)max_pages * c.page, lists = (int64_t)n_seqs * c.hkv;
   if (room <= kListed) { p.bytes = 256; return p; }
-  const int64_t step = 4 * kSelectThreads;
-  p.chunk = (int32_t)(((room + kMaxChunks - 1) / kMaxChunks + step - 1) / step * step);
-  if (p.chunk < 2 * step) p.chunk = 2 * step;
+  p.chunk = (int32_t)(((room + kMaxChunks - 1) / kMaxChunks + kStep - 1) / kStep * kStep);
   p.chunks = (int32_t)((room + p.chunk - 1) / p.chunk);
   p.list = pad_to((size_t)lists * p.chunks * kBins * 4, 256);
   p.above = p.list + pad_to((size_t)lists * room * 4, 256);
@@ -544,7 +543,8 @@ extern "C" int fcp_cache_evict(const fcp_cache* cache, const int32_t* pages, con
   a.new_len = new_len;
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (p.chunks == 0) {
-    select_kernel<<<dim3((unsigned)(n_seqs * a.c.hkv)), dim3(kSelectThreads), 0, st>>>(a);
+    auto kernel = room <= 4 * kSelectThreads ? select_kernel<1> : select_kernel<4>;
+    kernel<<<dim3((unsigned)(n_seqs * a.c.hkv)), dim3(kSelectThreads), 0, st>>>(a);
   } else {
     char* const area = static_cast<char*>(scratch);
     a.chunk = p.chunk;
