@@ -53,8 +53,8 @@ __device__ inline int32_t cost_of(const SeqSizes& z, int hkv, int group, int row
 }
 
 // The sequence that holds the beginning of share `block` (blocks = 0: place `block` itself), or, with tok >= 0, query row `tok`; seq = -1 if there is none.  Every thread of the block (256, 512) calls; a thread
-// looks at a run of sequences, all of which are asked for at once.  At most `blocks` shares, fewer where a share would have fewer than kLeastTiles places.
-template <bool Short, int Threads = 256>
+// looks at a run of sequences, all of which are asked for at once.  At most `blocks` shares, fewer where a share would have fewer than Least places.
+template <bool Short, int Threads = 256, int Least = Short ? 1 : kLeastTiles>
 static __device__ inline Line find_on_line(const SeqView& s, const CacheView& c, int group, int rows, int blocks, int block, int tok) {
   __shared__ int32_t sums[Threads / 64];
   __shared__ int32_t found[5];
@@ -70,8 +70,7 @@ static __device__ inline Line find_on_line(const SeqView& s, const CacheView& c,
     if (w < (int)(threadIdx.x >> 6)) upto += sums[w];
     line.total += sums[w];
   }
-  const int least = Short ? 1 : kLeastTiles;
-  line.sharers = min(blocks, (line.total + least - 1) / least);
+  line.sharers = min(blocks, (line.total + Least - 1) / Least);
   int32_t at = upto - mine;            // of the thread's first sequence
   const int32_t x = blocks == 0 ? block : tok >= 0 || block >= line.sharers ? -1 : line.begin(block);
   if (tok >= 0 || (x >= at && x < upto)) {

@@ -446,10 +446,11 @@ __global__ __launch_bounds__(kWeighThreads, 2) void weigh_kernel(WeighArgs a) {
 }
 
 // The same from the scores that the attention kernel left (few rows): a wave takes four rows of a tile at a time, four keys a lane, and four tiles.
+constexpr int kScoreTiles = 4 * kWaves;   // that a block works at once
 __global__ __launch_bounds__(256) void weigh_scores_kernel(AttnArgs a, int rows_of_block) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int32_t me = blockIdx.x;
-  const Line line = find_on_line<false>(a.s, a.c, a.group, rows_of_block, a.blocks * kWaves, me, -1);   // (a share of its own)
+  const Line line = find_on_line<false, 256, kScoreTiles>(a.s, a.c, a.group, rows_of_block, gridDim.x, me, -1);
   if (line.seq < 0) return;
   int32_t at = line.begin(me);
   const int32_t end = line.begin(me + 1);
@@ -466,40 +467,48 @@ __global__ __launch_bounds__(256) void weigh_scores_kernel(AttnArgs a, int rows_
     const int head = item / row_blocks, rb = item % row_blocks;
     // the rows of all blocks of a head add to the same weights: those of the first block's share do it, so that no two do
     if (rb == 0) {
-      constexpr int kUnroll = 4;
+      constexpr int kUnroll = kScoreTiles / kWaves;
       const int sub = lane >> 4, i4 = (lane >> 2) & 3, g = lane & 3, key4 = 16 * g + 4 * i4;   // row of four, keys of the tile
       for (int i = t0 + wave; i < t1; i += kWaves * kUnroll) {
-        f32x4 got[kUnroll] = {};
-        for (int r0 = 0; r0 < all_rows; r0 += 4) {
+        // everything is asked for before anything is waited for: the first four rows' scores and LSE, the pages, then where the sums go (only the first 16 lanes' are used)
+        f32x4 s[kUnroll], got[kUnroll] = {}, sum[kUnroll];
+        float lse = 0.f;
+        auto rows_at = [&](int r0) {
           const int row = min(r0 + sub, all_rows - 1);
-          const float lse = a.lse[(int64_t)(head * a.group + row % a.group) * a.s.n_rows + z.row0 + row / a.group] * kLog2e;
-          const bool live = r0 + sub < all_rows && lse != -INFINITY;
+          lse = a.lse[(int64_t)(head * a.group + row % a.group) * a.s.n_rows + z.row0 + row / a.group];
           const float* const s0 = a.scores + ((int64_t)base + ((int64_t)head * row_blocks + row / rows_of_block) * tiles) * (16 * kTile) + 256 * i4 + 16 * (row % rows_of_block) + 4 * g;
-          f32x4 s[kUnroll];
 #pragma unroll
           for (int j = 0; j < kUnroll; ++j) s[j] = *reinterpret_cast<const f32x4*>(s0 + (int64_t)min(i + kWaves * j, t1 - 1) * (16 * kTile));
+        };
+        rows_at(0);
+        f32x4* to[kUnroll];
+#pragma unroll
+        for (int j = 0; j < kUnroll; ++j) {
+          const int key = (i + kWaves * j) * kTile + key4;
+          const int32_t p = sub == 0 && i + kWaves * j < t1 && key < z.len ? page_at(a.s, a.c, seq, key >> a.c.log_page) : -1;
+          to[j] = p < 0 ? nullptr : reinterpret_cast<f32x4*>(a.c.weight + block_of(a.c, p, head) * a.c.page + (key & (a.c.page - 1)));
+        }
+#pragma unroll
+        for (int j = 0; j < kUnroll; ++j) sum[j] = to[j] ? *to[j] : f32x4{0, 0, 0, 0};
+        for (int r0 = 0; r0 < all_rows; r0 += 4) {
+          if (r0 > 0) rows_at(r0);
+          const float lse2 = r0 + sub < all_rows && lse != -INFINITY ? lse * kLog2e : INFINITY;       // (else nothing is added)
 #pragma unroll
           for (int j = 0; j < kUnroll; ++j)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) got[j][k] += live ? __builtin_amdgcn_exp2f(s[j][k] - lse) : 0.f;
+            for (int k = 0; k < 4; ++k) got[j][k] += __builtin_amdgcn_exp2f(s[j][k] - lse2);
         }
 #pragma unroll
         for (int j = 0; j < kUnroll; ++j)
 #pragma unroll
           for (int k = 0; k < 4; ++k) got[j][k] = sum_over_groups(got[j][k]);
-        if (sub == 0)
 #pragma unroll
-          for (int j = 0; j < kUnroll; ++j) {
-            const int key = (i + kWaves * j) * kTile + key4;
-            const int32_t p = i + kWaves * j < t1 && key < z.len ? page_at(a.s, a.c, seq, key >> a.c.log_page) : -1;
-            if (p >= 0) {
-              f32x4* const w = reinterpret_cast<f32x4*>(a.c.weight + block_of(a.c, p, head) * a.c.page + (key & (a.c.page - 1)));
-              f32x4 v = *w;
+        for (int j = 0; j < kUnroll; ++j) {
+          const int key = (i + kWaves * j) * kTile + key4;
 #pragma unroll
-              for (int k = 0; k < 4; ++k) v[k] += key + k < z.len ? got[j][k] : 0.f;
-              *w = v;
-            }
-          }
+          for (int k = 0; k < 4; ++k) sum[j][k] += key + k < z.len ? got[j][k] : 0.f;
+          if (to[j]) *to[j] = sum[j];
+        }
       }
     }
     at += t1 - t0;
@@ -508,7 +517,9 @@ __global__ __launch_bounds__(256) void weigh_scores_kernel(AttnArgs a, int rows_
 
 // ---- host ---------------------------------------------------------------------------------------
 
-// Tables of up to this many tiles: an item is not divided among blocks, which saves the second launch.  One sequence of 512 tokens, 4 heads of 64 channels: MEASURED.
+// Tables of up to this many tiles: an item is not divided among blocks, which saves the second launch (one sequence of 512 tokens, 4 heads of 64 channels: 6.0 us, divided 13.5).  Twice
+// as many where there are items for all blocks: shares would end inside items of a few tiles, and leave most of a block's waves without one.  64 ragged sequences of up to 1025 tokens, 8
+// KV heads, not divided / divided: 18.7 / 33.1 us; of up to 2000 31.7 / 37.2; but of up to 4000 63.7 / 54.0, and 16 sequences of up to 2000 23.4 / 19.4.
 constexpr int kShortTiles = 16;
 
 // How a call is worked.  Up to 16 rows per sequence and KV head on average: a block of 16 rows whose waves divide the keys; more: 128 rows, a wave 32.
@@ -521,7 +532,7 @@ AttnPlan plan_attn(const CacheView& c, int head_dim, int32_t n_seqs, int32_t max
   p.stored = weigh && p.keys;
   p.part_floats = (int64_t)2 * kBlocks * slot_floats(head_dim, p.rows);
   const int64_t tiles = max(((int64_t)max_pages * c.page + kTile - 1) / kTile, (int64_t)1);
-  p.whole = tiles <= kShortTiles && !p.stored;
+  p.whole = !p.stored && tiles <= ((int64_t)n_seqs * c.hkv >= kBlocks ? 2 : 1) * kShortTiles;
   p.places = tiles * c.hkv * (n_seqs + (int64_t)tq * group / p.rows);
   p.score_floats = p.stored ? p.places * 16 * kTile : 0;
   return p;
@@ -542,7 +553,7 @@ int launch_attn(const AttnArgs& a, const AttnPlan& p, hipStream_t st) {
     FCP_HIP_CHECK(hipGetLastError());
   }
   if (p.stored) {
-    weigh_scores_kernel<<<dim3(kBlocks * kWaves), block, 0, st>>>(a, p.rows);
+    weigh_scores_kernel<<<dim3((unsigned)min((p.places + kScoreTiles - 1) / kScoreTiles, (int64_t)5 * kBlocks / 2)), block, 0, st>>>(a, p.rows);
     FCP_HIP_CHECK(hipGetLastError());
   }
   return FCP_OK;
