@@ -99,6 +99,33 @@ class RankAttention:
         self.dk = torch.empty(self.tkv, hkv, D, dtype=torch.bfloat16, device=dev)
         self.dv = torch.empty(self.tkv, hkv, D, dtype=torch.bfloat16, device=dev)
 
+    # -- rotary positions -------------------------------------------------------------
+    def set_rotary(self, turns, rot_dim=None, layout=B.FCP_ROTARY_HALF, magnitude=1.0):
+        """Queries and keys come unrotated: rotate_inputs() turns them by their positions in their sequences (a rank's zigzag chunks lie apart in them), and
+        finalize_rotary() / rotate_grads() turn the gradients back.  turns: what fcp_rotary_frequencies gives."""
+        self.turns = torch.as_tensor(turns, dtype=torch.float64).to(self.device)
+        self.rot = (self.D if rot_dim is None else int(rot_dim), layout, float(magnitude))
+        pos = np.arange(self.tkv) - np.repeat(self.cu[:-1], self.seq_lens)
+        self.k_pos = torch.from_numpy(pos.astype(np.int32)).to(self.device)
+        self.q_pos = torch.from_numpy(pos[self.rows].astype(np.int32)).to(self.device)
+
+    def _rotate(self, parts, backward, stream):
+        rot_dim, layout, magnitude = self.rot
+        B.fcp_rotary(parts, self.turns, rot_dim, layout, magnitude, backward, stream)
+
+    def rotate_inputs(self, stream=None):
+        """Q and K in place, once after set_inputs."""
+        self._rotate([(self.q, self.q, self.q_pos), (self.k, self.k, self.k_pos)], False, stream)
+
+    def rotate_grads(self, stream=None):
+        """After backward_direct: dQ and dK in place, from those of the rotated rows to those of the rows that set_inputs took."""
+        self._rotate([(self.dq, self.dq, self.q_pos), (self.dk, self.dk, self.k_pos)], True, stream)
+
+    def finalize_rotary(self, stream=None):
+        """After backward_steps, in the place of finalize: the fp32 sums of dQ and dK turned back and rounded to bf16 once, dV rounded."""
+        self._rotate([(self.dq_acc, self.dq, self.q_pos), (self.dk_acc, self.dk, self.k_pos)], True, stream)
+        B.fcp_grad_finalize(self.dv_acc, self.dv, stream)
+
     # -- passes -----------------------------------------------------------------------
     def forward_steps(self, stream=None):
         if self.spans is not None:

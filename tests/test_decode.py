@@ -1,0 +1,90 @@
+"""Prompts, new tokens and eviction together: the decoder against attention in 64 bits over what its cache holds, token for token."""
+import numpy as np
+import pytest
+
+import cache_ref as R
+from paper_2602_21788_amd import binding as B
+
+
+def bf16_rows(torch, g, n, h, D):
+    return torch.randn(n, h, D, generator=g, device="cuda").to(torch.bfloat16)
+
+
+def held(dec, fmt):
+    """The cache's content as the reference's."""
+    k, v, ks, vs, w = R.from_device(dec.cache)
+    ref = object.__new__(R.RefCache)
+    ref.P, ref.D, ref.hkv, ref.fmt, ref.n_pages = dec.P, dec.D, dec.hkv, fmt, k.shape[0]
+    ref.k, ref.v, ref.k_e, ref.v_e, ref.weight = k, v, np.log2(ks).astype(int), np.log2(vs).astype(int), w.astype(np.float64)
+    return ref
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt,P,D,hq,hkv", [("e4m3", 64, 128, 8, 2), ("int8", 16, 64, 4, 4)])
+def test_prompts_tokens_and_eviction(fmt, P, D, hq, hkv):
+    import torch
+    from paper_2602_21788_amd.decode import CacheDecoder
+    g = torch.Generator(device="cuda").manual_seed(1)
+    lens = [150, 3, 0, 64]
+    dec = CacheDecoder(4, 64, 24, hq, hkv, D, page_tokens=P, fmt=fmt)
+    n = sum(lens)
+    q, k, v = bf16_rows(torch, g, n, hq, D), bf16_rows(torch, g, n, hkv, D), bf16_rows(torch, g, n, hkv, D)
+    before = held(dec, fmt)
+    o, lse = dec.prefill(q, k, v, lens)
+    f64 = lambda t: t.double().cpu().numpy()
+    cu = np.concatenate([[0], np.cumsum(lens)])
+    # the cache holds the prompts' rotated keys and values, and the weights of the prompts' own attention
+    before.append(f64(k), f64(v), cu, dec.kv_len, dec.pages)
+    w = R.check_content(dec.cache, before)
+    _, _, want, _, units = before.attn(f64(q), cu, dec.kv_len, dec.pages, dec.scale, lse_in=f64(lse))
+    assert np.abs(w - want).max() <= 1e-5 * max(lens) and (want > 0).any()
+
+    def check_step(news):
+        rows = sum(news)
+        q, k, v = bf16_rows(torch, g, rows, hq, D), bf16_rows(torch, g, rows, hkv, D), bf16_rows(torch, g, rows, hkv, D)
+        ref = held(dec, fmt)
+        o, lse = dec.step(q, k, v, news)
+        cu = np.concatenate([[0], np.cumsum(news)])
+        ref.append(f64(k), f64(v), cu, dec.kv_len, dec.pages)
+        O, LSE, W, absv, units = ref.attn(f64(q), cu, dec.kv_len, dec.pages, dec.scale)
+        eps = (units + 8 * np.abs(LSE) + 16) * 2.0 ** -24
+        assert (np.abs(f64(lse) - LSE) <= eps).all()
+        assert (np.abs(f64(o) - O) <= absv * (2.0 ** -8 + 2 * eps.T[..., None]) + np.abs(O) * 2.0 ** -8 + 1e-30).all()
+        w = R.check_content(dec.cache, ref)
+        assert (np.abs(w - ref.weight - W) <= 1e-4 * W + (ref.weight + W) * 2.0 ** -22 + 1e-30).all()
+
+    for news in ([1, 1, 1, 1], [1, 1, 0, 1], [0, 7, 2, 1]):
+        check_step(news)
+    assert dec.next_pos.tolist() == [152, 12, 3, 67]
+    ref = held(dec, fmt)
+    lens, pages, free = dec.kv_len.copy(), dec.pages.copy(), len(dec.free)
+    kept = dec.evict(60, n_first=2, n_recent=16)
+    want_kept, want_len = ref.evict(pages, lens, dec.pages, 60, 2, 16)
+    assert np.array_equal(kept.cpu().numpy(), want_kept) and np.array_equal(dec.kv_len, want_len)
+    assert len(dec.free) == free + (pages >= 0).sum() - (dec.pages >= 0).sum()
+    assert dec.next_pos.tolist() == [152, 12, 3, 67]
+    for news in ([1, 1, 1, 1], [2, 0, 1, 30]):
+        check_step(news)
+    dec.close(0)
+    assert dec.kv_len[0] == 0 and (dec.pages[0] == -1).all()
+    check_step([5, 1, 1, 1])
+
+
+@pytest.mark.gpu
+def test_the_decoder_says_when_pages_are_short():
+    import torch
+    from paper_2602_21788_amd.decode import CacheDecoder
+    g = torch.Generator(device="cuda").manual_seed(2)
+    dec = CacheDecoder(2, 6, 4, 2, 2, 64, page_tokens=16)
+    rows = lambda n: (bf16_rows(torch, g, n, 2, 64) for _ in range(3))
+    dec.prefill(*rows(64), [40, 24])
+    with pytest.raises(MemoryError):
+        dec.step(*rows(30), [30, 0])
+    with pytest.raises(MemoryError):
+        dec.evict(32, 1, 1)
+    assert dec.kv_len.tolist() == [40, 24]
+    dec.close(1)
+    dec.evict(16, 1, 4)
+    assert dec.kv_len.tolist() == [16, 0] and len(dec.free) == 5
+    with pytest.raises(ValueError):
+        dec.prefill(*rows(4), [2, 2])
