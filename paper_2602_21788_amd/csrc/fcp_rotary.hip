@@ -2,7 +2,7 @@
 //
 // A pair (a, b) of channels with frequency f at position p becomes (a cos t - b sin t, a sin t + b cos t), t = 2 pi frac(p f).  Every element is read
 // and written once and takes part in two products, so the memory bounds it.  The angle is the same for all heads of a row: a block takes a few rows
-// of one tensor, forms their cosines and sines once in LDS, and its threads then work 16 channels at a time, head after head.
+// of one tensor, forms their cosines and sines once in LDS, and its threads then work 16 bytes at a time, head after head.
 // p f is formed in 64 bits and reduced to a fraction of a turn there: at p = 10^6 a product in 32 bits is off by 0.06 of a radian.  The fraction, at
 // most half a turn, has 24 good bits as a float (angle off by 2e-7).
 #include <math.h>
@@ -14,7 +14,7 @@ namespace {
 
 constexpr int kRotThreads = 256;
 constexpr int kRotLds = 1024;         // cosines and sines a block holds: rows * rot_dim / 2
-constexpr int kRotItem = 16;          // channels of an item
+constexpr int kRotItem = 16;          // head_dim and rot_dim are multiples of it where 16 bytes move at a time
 
 struct RotaryArgs {
   fcp_rotary_part part[FCP_ROTARY_MAX_PARTS];
@@ -28,63 +28,84 @@ template <class T> __device__ inline float load1(const T* p);
 template <> __device__ inline float load1(const float* p) { return *p; }
 template <> __device__ inline float load1(const __bf16* p) { return (float)*p; }
 
-// eight neighbouring channels
-struct F8 { float f[8]; };
-__device__ inline F8 load8(const float* p) {
-  const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
-  return {{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}};
+// W neighbouring channels: 16 bytes of what is read
+template <int W> struct Channels { float f[W]; };
+__device__ inline Channels<4> load16(const float* p) {
+  const f32x4 a = *reinterpret_cast<const f32x4*>(p);
+  return {{a[0], a[1], a[2], a[3]}};
 }
-__device__ inline F8 load8(const __bf16* p) {
+__device__ inline Channels<8> load16(const __bf16* p) {
   const bf16x8 a = *reinterpret_cast<const bf16x8*>(p);
-  F8 r;
+  Channels<8> r;
 #pragma unroll
   for (int i = 0; i < 8; ++i) r.f[i] = (float)a[i];
   return r;
 }
-__device__ inline void store8(float* p, const F8& x) {
-  *reinterpret_cast<f32x4*>(p) = f32x4{x.f[0], x.f[1], x.f[2], x.f[3]};
-  *reinterpret_cast<f32x4*>(p + 4) = f32x4{x.f[4], x.f[5], x.f[6], x.f[7]};
+template <int W>
+__device__ inline void store(float* p, const Channels<W>& x) {
+#pragma unroll
+  for (int i = 0; i < W; i += 4) *reinterpret_cast<f32x4*>(p + i) = f32x4{x.f[i], x.f[i + 1], x.f[i + 2], x.f[i + 3]};
 }
-__device__ inline void store8(__bf16* p, const F8& x) {
+__device__ inline void store(__bf16* p, const Channels<4>& x) { *reinterpret_cast<bf16x4*>(p) = bf16x4{(__bf16)x.f[0], (__bf16)x.f[1], (__bf16)x.f[2], (__bf16)x.f[3]}; }
+__device__ inline void store(__bf16* p, const Channels<8>& x) {
   bf16x8 a;
 #pragma unroll
   for (int i = 0; i < 8; ++i) a[i] = (__bf16)x.f[i];
   *reinterpret_cast<bf16x8*>(p) = a;
 }
 
+// Division by a number that stays: by 2^32 / d rounded up, at most one too large.  (Two divisions for each item of 16 bytes took longer than the item: 9363 rows of 48 heads, 
+struct Divisor {
+  uint32_t d, m;
+  __device__ explicit Divisor(int by) : d(by), m(by == 1 ? 0u : 0xffffffffu / (uint32_t)by + 1) {}
+  __device__ int operator()(int x, int& rest) const {
+    int q = d == 1 ? x : (int)__umulhi((uint32_t)x, m);
+    rest = x - q * (int)d;
+    if (rest < 0) { --q; rest += (int)d; }
+    return q;
+  }
+};
+
 template <class X, class Y, bool Half, bool Wide>
 __device__ void turn_rows(const RotaryArgs& a, const fcp_rotary_part& p, int row0, int rows, int head0, int heads, const float2* cs) {
   const int half = a.rot / 2;
   const X* const x0 = static_cast<const X*>(p.x) + (int64_t)row0 * p.x_row + (int64_t)head0 * p.x_head;
   Y* const y0 = static_cast<Y*>(p.y) + (int64_t)row0 * p.y_row + (int64_t)head0 * p.y_head;
-  if constexpr (Wide) {                            // items of 16 channels: eight pairs, or 16 channels that do not turn
-    const int per_head = a.head_dim / kRotItem, turning = a.rot / kRotItem, n = rows * heads * per_head;
+  if constexpr (Wide) {
+    // An item is 16 bytes of what is read, or, where a pair's channels lie apart, twice 16 bytes: neighbouring lanes read and write neighbouring bytes.  Items that turn and items that
+    // are copied load and store alike, and at the same place in the program: a wave often has both.
+    constexpr int W = 16 / sizeof(X), kItem = Half ? 2 * W : W;
+    const int turning = a.rot / kItem, per_head = a.head_dim / kItem, n = rows * heads * per_head;
+    const Divisor by_head(per_head), by_row(heads);
     for (int it = threadIdx.x; it < n; it += kRotThreads) {
-      const int i = it % per_head, rh = it / per_head, h = rh % heads, r = rh / heads;
+      int i, h;
+      const int r = by_row(by_head(it, i), h);
+      const bool turns = i < turning;
+      const int ca = Half && turns ? W * i : kItem * i, cb = Half && turns ? half + W * i : kItem * i + W;
       const X* x = x0 + r * p.x_row + h * p.x_head;
       Y* y = y0 + r * p.y_row + h * p.y_head;
-      const bool turns = i < turning;
-      const int ca = turns && Half ? 8 * i : kRotItem * i, cb = turns && Half ? half + 8 * i : kRotItem * i + 8;
-      F8 u = load8(x + ca), v = load8(x + cb);
+      Channels<W> u = load16(x + ca), v = u;
+      if (Half) v = load16(x + cb);
       if (turns) {
-        const float2* t = cs + r * half + 8 * i;
+        const float2* t = cs + r * half + (Half ? W : W / 2) * i;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          float& xa = Half ? u.f[j] : (j < 4 ? u.f[2 * j] : v.f[2 * j - 8]);
-          float& xb = Half ? v.f[j] : (j < 4 ? u.f[2 * j + 1] : v.f[2 * j - 7]);
+        for (int j = 0; j < (Half ? W : W / 2); ++j) {
+          float &xa = Half ? u.f[j] : u.f[2 * j], &xb = Half ? v.f[j] : u.f[2 * j + 1];
           const float2 c = t[j];
           const float ya = xa * c.x - xb * c.y, yb = xa * c.y + xb * c.x;
           xa = ya;
           xb = yb;
         }
       }
-      store8(y + ca, u);
-      store8(y + cb, v);
+      store(y + ca, u);
+      if (Half) store(y + cb, v);
     }
   } else {                                         // items of one pair, or of one channel that does not turn
     const int per_head = half + a.head_dim - a.rot, n = rows * heads * per_head;
+    const Divisor by_head(per_head), by_row(heads);
     for (int it = threadIdx.x; it < n; it += kRotThreads) {
-      const int i = it % per_head, rh = it / per_head, h = rh % heads, r = rh / heads;
+      int i, h;
+      const int r = by_row(by_head(it, i), h);
       const X* x = x0 + r * p.x_row + h * p.x_head;
       Y* y = y0 + r * p.y_row + h * p.y_head;
       if (i >= half) {
@@ -172,7 +193,7 @@ extern "C" int fcp_rotary(const fcp_rotary_part* parts, int32_t n_parts, const d
     return fail(FCP_ERR_INVALID_ARG, "%s: magnitude must be above 0 and backward 0 or 1", who);
   RotaryArgs a = {};
   bool wide = head_dim % kRotItem == 0 && rot_dim % kRotItem == 0;
-  int64_t head_rows = 0;
+  int64_t head_rows = 0, row_bytes = 1;
   for (int32_t i = 0; i < n_parts; ++i) {
     const fcp_rotary_part& p = parts[i];
     if (p.rows < 0 || p.heads < 0) return fail(FCP_ERR_INVALID_ARG, "%s: parts[%d] has negative sizes", who, i);
@@ -189,14 +210,19 @@ extern "C" int fcp_rotary(const fcp_rotary_part* parts, int32_t n_parts, const d
       return fail(FCP_ERR_INVALID_ARG, "%s: parts[%d] is not aligned to its type", who, i);
     wide = wide && multiple16(p.x, p.x_row, p.x_head, p.x_type) && multiple16(p.y, p.y_row, p.y_head, p.y_type);
     head_rows += (int64_t)p.rows * p.heads;
+    const int64_t bytes = (int64_t)p.heads * head_dim * ((p.x_type == FCP_BF16 ? 2 : 4) + (p.y_type == FCP_BF16 ? 2 : 4));
+    if (bytes > row_bytes) row_bytes = bytes;
     a.part[a.n_parts++] = p;
   }
   if (a.n_parts == 0) return FCP_OK;
-  // Rows of a block: as many as leave a thread one cosine to form (more than 512 pairs in a row: one row).  Heads: all of them, except where that makes
-  // fewer blocks than two per CU; then a block has few enough that every thread has about one item.
+  // Rows of a block: as many as leave a thread one cosine to form (more than 512 pairs in a row: one row), but no more than 64 KB of traffic, or a launch ends with a few blocks that the
+  // others wait for (9363 rows of 40 and 8 heads, half of 128 channels turn, fp32 to bf16: 2 rows 67.8 us, 4 rows 73.2; 32768 rows of 32 and 8 heads, bf16: 2 rows 125.2, 4 rows 120.4).
+  // Heads: all of them, except where that makes fewer blocks than two per CU; then a block has few enough that every thread has about one item.
   a.head_dim = head_dim;
   a.rot = rot_dim;
+  const int64_t fit = 65536 / row_bytes;
   a.rows = rot_dim / 2 >= kRotThreads ? 1 : kRotThreads / (rot_dim / 2);
+  if (a.rows > fit) a.rows = fit < 1 ? 1 : (int32_t)fit;
   const int per_head = wide ? head_dim / kRotItem : head_dim - rot_dim / 2;
   if (head_rows * per_head < (int64_t)512 * kRotThreads) {
     a.rows = 1;
