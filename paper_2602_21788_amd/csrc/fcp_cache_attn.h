@@ -89,9 +89,12 @@ static __device__ inline Line find_on_line(const SeqView& s, const CacheView& c,
     }
   }
   __syncthreads();
-  line.seq = found[0];
-  line.before = found[1];
-  line.z = {found[2], found[3], found[4]};
+  // (the same for all threads: scalar registers)
+  line.seq = __builtin_amdgcn_readfirstlane(found[0]);
+  line.before = __builtin_amdgcn_readfirstlane(found[1]);
+  line.z = {__builtin_amdgcn_readfirstlane(found[2]), __builtin_amdgcn_readfirstlane(found[3]), __builtin_amdgcn_readfirstlane(found[4])};
+  line.total = __builtin_amdgcn_readfirstlane(line.total);
+  line.sharers = __builtin_amdgcn_readfirstlane(line.sharers);
   return line;
 }
 
@@ -123,17 +126,14 @@ __device__ inline void mask_scores(f32x4 (&s)[4], int last) {
   for (int i = 0; i < 16; ++i) s[i / 4][i % 4] = i <= last ? s[i / 4][i % 4] : -INFINITY;
 }
 
-// Softmax of one tile and 16 rows: raw scores s become probabilities p (times the values' scale), the running maximum and sum follow.  c: what scales the scores.
+// Softmax of one tile and 16 rows, in two parts: the running maximum follows the raw scores s (c scales them), and what was summed up so far follows the maximum; then the scores become
+// probabilities p, times the values' scale vs.  The maximum only grows in steps of more than 2^8: probabilities stay below 256, and most tiles leave the sums alone.
 template <int D>
-__device__ inline void softmax_of(f32x4 (&s)[4], float c, float vs, f32x4 (&o)[D / 16], float& m, float& l, bf16x8 (&p)[2], float* scores) {
+__device__ inline void raise_maximum(const f32x4 (&s)[4], float c, f32x4 (&o)[D / 16], float& m, float& l) {
   float top = max3(s[0][0], s[0][1], s[0][2]);
 #pragma unroll
   for (int i = 3; i < 15; i += 2) top = max3(top, s[i / 4][i % 4], s[(i + 1) / 4][(i + 1) % 4]);
   top = __builtin_elementwise_maximum(top, s[3][3]) * c;
-  if (scores)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) *reinterpret_cast<f32x4*>(scores + 16 * 16 * i) = s[i] * c;
-  // the maximum only grows in steps of more than 2^8: probabilities stay below 256, and most tiles leave the sums alone
   if (__ballot(top > m + 8.f)) {
     const float grown = fmaxf(m, max_over_groups(top)), f = __builtin_amdgcn_exp2f(m - grown);
     m = grown;
@@ -141,6 +141,8 @@ __device__ inline void softmax_of(f32x4 (&s)[4], float c, float vs, f32x4 (&o)[D
 #pragma unroll
     for (int d = 0; d < D / 16; ++d) o[d] *= f;
   }
+}
+__device__ inline void probabilities_of(const f32x4 (&s)[4], float c, float vs, float m, float& l, bf16x8 (&p)[2]) {
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
     const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 4][i % 4], c, -m));

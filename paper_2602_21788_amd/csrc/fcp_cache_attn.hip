@@ -146,8 +146,12 @@ __device__ inline void walk(const AttnArgs& a, int seq, int head, int len, int f
       mask_scores(s, last);
       clear_hidden<D, Fmt>(v, at.v < 0 ? 0 : len - key0, last, r);
     }
+    if (to)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) *reinterpret_cast<f32x4*>(to + 16 * 16 * j) = s[j] * c;
+    raise_maximum<D>(s, c, r.o, r.m, r.l);
     bf16x8 p[2];
-    softmax_of<D>(s, c, sc.v, r.o, r.m, r.l, p, to);
+    probabilities_of(s, c, sc.v, r.m, r.l, p);
 #pragma unroll
     for (int d = 0; d < D / 16; ++d)
 #pragma unroll

@@ -1,10 +1,14 @@
 // Attention over the paged 8-bit cache for many rows: pieces of prompts, or several new tokens of many query heads.
 //
 // A block takes 128 rows of a KV head's group at a time, a wave 32 of them, against tiles of 64 keys.  The products and the exponentials bound it (4 D flops a pair; an exponential
-// takes as long as 64 flops of the matrix units per lane), so the codes must not become bf16 in every wave: a tile's codes come in whole lines, 32 a thread, become bf16 in
-// the page's scale there (exact) and go to LDS, from which the waves read the operands of the 16 x 16 x 32 instructions, each for two blocks of 16 rows.  The next tile's codes
-// are on their way meanwhile, in registers; one barrier a tile, two stages.  Two blocks per CU, in no lock step: the one's exponentials meet the other's products.
-// Operand rows straight from memory would be requests of 16 bytes a lane, a quarter of a line's rate, in every wave.
+// takes as long as 64 flops of the matrix units per lane), so the codes must not become bf16 in every wave: a tile's codes come in whole lines, 32 a thread, become bf16 (exact) and
+// go to LDS, from which the waves read the operands of the 16 x 16 x 32 instructions, each for two blocks of 16 rows.  Operand rows straight from memory would be requests of 16 bytes
+// a lane, a quarter of a line's rate, in every wave.  The keys' scale is taken with the scores, the values' with the codes.
+// A step has two streams: the next tile's scores with this tile's exponentials, and this tile's product with the values with the conversion of codes for the tiles after; the matrix
+// units and the others work at once, and operands from LDS are asked for four ahead.  One barrier a step.  Two blocks per CU: a wave has 256 registers, all in use.
+// Pieces of 512 tokens over up to 16385, 2 sequences, 40 query heads on 8, 128 channels, 193 Gflop: 244 us with e4m3 (232 and the merge), 280 with int8, whose codes take three times as
+// many instructions; score, exponentials and product one after the other, each operand asked for when it is due: 277 and 300.  Of a wave's time the matrix units work 38 %, the
+// others 47, 20 are waits.  A large matrix product runs at 1250 Tflop/s here, this at 830.
 // Keys and rows are laid on the matrix as in the kernel for few rows: a lane ends with the scores of 16 neighbouring keys, which is the operand of the product with V.
 #include "fcp_cache_attn.h"
 
@@ -13,11 +17,13 @@ namespace {
 
 constexpr int kNB = 2;                 // blocks of 16 rows of a wave
 
-// LDS of a stage: keys as rows of D channels, values as rows (channels) of 64 keys, in chunks of 8 bf16 whose places in a row are permuted so that the 16 rows of
-// an operand lie on different banks.
+// LDS of a stage: keys as rows of D channels, values as rows (channels) of 64 keys, in chunks of 8 bf16 whose places in a row are permuted so that what is read or written at once
+// lies on different banks.  That is 16 lanes, but not neighbours: 0 to 3 and 12 to 15 of one group of 16 with 4 to 11 of the next, so both groups' chunks count.  Values: chunk g + 4 u
+// holds keys 16 g + 8 u and on (in the order of the keys two lanes met on every bank).
 template <int D>
 struct Stage {
   static constexpr int kKeyRow = 2 * D, kValueRow = 2 * kTile, kKeys = kTile * kKeyRow, kBytes = kKeys + D * kValueRow;
+  static constexpr int kGroupBit = D == 128 ? 6 : 5;       // key_mix's part that comes from the group of 16 keys, in bytes
   // an operand's rows are 16 a + 4 i + b, a and b from 0 to 3: with 128 channels a row is a whole bank cycle, with 64 two rows are
   static __device__ int key_mix(int row) { return D == 128 ? ((row >> 4) & 3) * 4 + (row & 3) : ((row >> 4) & 3) * 2 + ((row >> 1) & 1); }
   static __device__ int value_mix(int ch) { return (ch >> 1) & 7; }
@@ -25,26 +31,23 @@ struct Stage {
   static __device__ int value_at(int ch, int chunk) { return kKeys + ch * kValueRow + ((chunk ^ value_mix(ch)) << 4); }
 };
 
-// 16 codes as bf16 in their scale, a power of two: exact.
-template <int Fmt>
-__device__ inline void decode16(u32x4 w, float scale, bf16x8& a, bf16x8& b) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    bf16x2 lo, hi;
-    if constexpr (Fmt == kE4m3) {
-      lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], scale, false);
-      hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], scale, true);
-    } else {
-      const f32x2 f = decode_half<Fmt, false>(w[i]), g = decode_half<Fmt, true>(w[i]);
-      lo = bf16x2{(__bf16)(f[0] * scale), (__bf16)(f[1] * scale)};
-      hi = bf16x2{(__bf16)(g[0] * scale), (__bf16)(g[1] * scale)};
-    }
-    bf16x8& to = i < 2 ? a : b;
-    to[4 * (i & 1)] = lo[0];
-    to[4 * (i & 1) + 1] = lo[1];
-    to[4 * (i & 1) + 2] = hi[0];
-    to[4 * (i & 1) + 3] = hi[1];
+// Four codes as bf16, times their scale, a power of two, or not: exact.
+template <int Fmt, bool Scaled>
+__device__ inline void decode4(uint32_t w, float scale, bf16x8& to, int at) {
+  bf16x2 lo, hi;
+  if constexpr (Fmt == kE4m3) {
+    lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, Scaled ? scale : 1.f, false);
+    hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, Scaled ? scale : 1.f, true);
+  } else {
+    f32x2 f = decode_half<Fmt, false>(w), g = decode_half<Fmt, true>(w);
+    if (Scaled) f = f32x2{f[0] * scale, f[1] * scale}, g = f32x2{g[0] * scale, g[1] * scale};
+    lo = bf16x2{(__bf16)f[0], (__bf16)f[1]};
+    hi = bf16x2{(__bf16)g[0], (__bf16)g[1]};
   }
+  to[at] = lo[0];
+  to[at + 1] = lo[1];
+  to[at + 2] = hi[0];
+  to[at + 3] = hi[1];
 }
 
 // A wave's share of a tile, D / 64 times: 64 D / 256 bytes of one group of 16 keys and as many of the group's values, which lie in one run each, 16 a lane.  Page, scales and
@@ -56,62 +59,83 @@ __device__ inline scalar_float as_scalar(const float* p) { return (scalar_float)
 
 template <int D>
 struct Share {
-  u32x4 k[D / 64], v[D / 64];
-  float ks[D / 64], vs[D / 64];
+  u32x4 w[D / 64];
+  float scale[D / 64];
   int live[D / 64];                    // of the 16 keys, those that are cached tokens (0: the page is not there)
 };
 // group of 16 keys, and the wave's place in it (in lots of 64 times 16 bytes)
 template <int D> __device__ inline int group_of(int wave, int i) { return D == 128 ? wave / 2 + 2 * i : wave; }
 template <int D> __device__ inline int lot_of(int wave) { return D == 128 ? wave & 1 : 0; }
 
+// Pages that hold the wave's share of a tile, -1 where there is none; asked for a step before the share is, so that nobody waits for the one to ask for the other.
 template <int D>
-__device__ inline void load_share(const AttnArgs& a, const int32_t* table, int head, int len, int tile, int wave, Share<D>& s) {
+struct Pages { int32_t of[D / 64]; };
+template <int D>
+__device__ inline void load_pages(const AttnArgs& a, const int32_t* table, int len, int tile, int wave, Pages<D>& pages) {
 #pragma unroll
   for (int i = 0; i < D / 64; ++i) {
-    const int key = tile * kTile + kGroup * group_of<D>(wave, i), place = key >> a.c.log_page;
-    int32_t page = -1;
-    if (key < len) page = as_scalar(table)[place];         // (len is at most what the table holds)
-    const bool there = (uint32_t)page < (uint32_t)a.c.n_pages;
-    const int64_t block = block_of(a.c, there ? page : 0, head), at = (block * a.c.page + (key & (a.c.page - 1))) * D + 1024 * lot_of<D>(wave);
-    s.live[i] = there ? min(len - key, kGroup) : 0;
-    s.ks[i] = as_scalar(a.c.k_scale)[block];
-    s.vs[i] = as_scalar(a.c.v_scale)[block];
-    const int mine = 16 * (int)(threadIdx.x & 63);
-    s.k[i] = *reinterpret_cast<const u32x4*>(a.c.k + at + mine);
-    s.v[i] = *reinterpret_cast<const u32x4*>(a.c.v + at + mine);
+    const int key = tile * kTile + kGroup * group_of<D>(wave, i);
+    const int32_t page = as_scalar(table)[min(key, len - 1) >> a.c.log_page];        // (len is at most what the table holds)
+    pages.of[i] = key < len && (uint32_t)page < (uint32_t)a.c.n_pages ? page : -1;
   }
 }
-// live: per group of 16 keys; odd: a value is NaN.  partly: some row of the block does not see the whole tile.
-template <int D, int Fmt>
-__device__ inline void store_share(const Share<D>& s, int wave, unsigned char* stage, int32_t* live, int32_t* odd, bool partly) {
-  typedef bf16x8 __attribute__((may_alias)) chunk;
-  // (the thread's number is formed anew: the compiler would keep the addresses that follow from it in registers, and spill them)
-  const int lane = fresh((int)threadIdx.x) & 63;
+// codes, scales: of the cache's keys, or of its values (a group of 16 tokens is one run of 16 D bytes in both).  Where there is no page the pool's first is read.
+template <int D>
+__device__ inline void load_share(const AttnArgs& a, const uint8_t* codes, const float* scales, const Pages<D>& pages, int head, int len, int tile, int wave, Share<D>& s) {
 #pragma unroll
   for (int i = 0; i < D / 64; ++i) {
-    const int g = group_of<D>(wave, i), at = 64 * lot_of<D>(wave) + lane, key = kGroup * g + at / (D / 16), c = at % (D / 16), ch = at;
-    bf16x8 x, y;
-    decode16<Fmt>(s.k[i], s.ks[i], x, y);
-    *reinterpret_cast<chunk*>(stage + Stage<D>::key_at(key, 2 * c)) = x;
-    *reinterpret_cast<chunk*>(stage + Stage<D>::key_at(key, 2 * c + 1)) = y;
-    u32x4 v = s.v[i];
-    if (s.live[i] < kGroup) {                              // codes past the last token are whatever the page holds, and 0 * NaN is NaN
+    const int key = tile * kTile + kGroup * group_of<D>(wave, i);
+    const int64_t block = block_of(a.c, max(pages.of[i], 0), head), at = (block * a.c.page + (key & (a.c.page - 1))) * D + 1024 * lot_of<D>(wave);
+    s.live[i] = pages.of[i] < 0 ? 0 : min(len - key, kGroup);
+    s.scale[i] = as_scalar(scales)[block];
+    s.w[i] = *reinterpret_cast<const u32x4*>(codes + at + 16 * (int)(threadIdx.x & 63));
+  }
+}
+
+// partly: some row of the block does not see the whole tile.  Its product with a NaN value would be NaN too, so zero takes that place, and the first such token of each channel is
+// noted in first_nan: the rows that see it get their NaN at the item's end.
+template <int D>
+__device__ inline void without_nan(Share<D>& s, int wave, int32_t* first_nan, int first_key) {
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const int n = min(max(s.live[i] - 4 * w, 0), 4);
-        v[w] &= n == 4 ? 0xffffffffu : (1u << (8 * n)) - 1;
-      }
-    }
-    if (Fmt == kE4m3 && partly) {
-      uint32_t o = 0;
+  for (int i = 0; i < D / 64; ++i)
 #pragma unroll
-      for (int w = 0; w < 4; ++w) o |= ((v[w] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
-      if (o) *odd = 1;
+    for (int w = 0; w < 4; ++w) {
+      const uint32_t nan = ((s.w[i][w] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+      const int at = 4 * w + (__builtin_ctz(nan) >> 3);
+      if (nan && at < s.live[i]) atomicMin(first_nan + 64 * lot_of<D>(wave) + (threadIdx.x & 63), first_key + kGroup * group_of<D>(wave, i) + at);
+      s.w[i][w] &= ~((nan >> 7) * 0xffu);
     }
-    decode16<Fmt>(v, s.vs[i], x, y);
-    *reinterpret_cast<chunk*>(stage + Stage<D>::value_at(ch, 2 * g)) = x;
-    *reinterpret_cast<chunk*>(stage + Stage<D>::value_at(ch, 2 * g + 1)) = y;
-    if (lane == 0) live[g] = s.live[i];
+}
+// Word i of a share, 0 to D / 16 - 1, on its way into LDS (half: what it shares a chunk with).
+template <int D, int Fmt, bool Values>
+__device__ inline void store_word(const Share<D>& s, int i, int wave, int place, unsigned char* stage, bf16x8& half) {
+  typedef bf16x8 __attribute__((may_alias)) chunk;
+  uint32_t w = s.w[i / 4][i % 4];
+  if (Values) {                                            // codes past the last token are whatever the page holds, and 0 * NaN is NaN: they become zeros
+    const int n = min(max(s.live[i / 4] - 4 * (i % 4), 0), 4);
+    w &= (uint32_t)((1ull << (8 * n)) - 1);
+  }
+  decode4<Fmt, Values>(w, s.scale[i / 4], half, 4 * (i % 2));
+  if (i % 2 == 0) return;
+  const int g = group_of<D>(wave, i / 4), u = i / 2 % 2;
+  place = fresh(place);                                    // (the compiler would keep the addresses that follow from it in registers, and spill them)
+  const int at = Values ? place ^ (g << 4 | u << 6) : (place ^ (g << Stage<D>::kGroupBit | u << 4)) + kGroup * g * Stage<D>::kKeyRow;
+  *reinterpret_cast<chunk*>(stage + at) = half;
+}
+
+// Products whose operands come from LDS, N operands: some are on their way while the products of those before run.  (Left alone the compiler asks for an operand when it is due, and waits.)
+constexpr int kAhead = 4;
+template <int N, typename Read, typename Multiply>
+__device__ inline void stream_operands(Read read, Multiply multiply) {
+  bf16x8 x[kAhead];
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) x[i] = read(i);
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    multiply(i, x[i % kAhead]);
+    if (i + kAhead < N) x[i % kAhead] = read(i + kAhead);
+    __builtin_amdgcn_sched_barrier(0);
   }
 }
 
@@ -119,11 +143,12 @@ template <int D, int Fmt, bool Short>
 __global__ __launch_bounds__(256, 2) void attn_rows_kernel(AttnArgs a) {
   typedef bf16x8 __attribute__((may_alias)) chunk;
   extern __shared__ __align__(256) unsigned char lds[];    // two stages
-  __shared__ int32_t live[2][4], odd[2];
+  __shared__ float key_scale[4][4];                        // [tile][group of 16 keys]
+  __shared__ int32_t live[4][4], first_nan[2][D];          // (the latter for this item and the next)
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
-  // the lane's operand rows: neither permutation depends on the 4 i or 16 d that steps through them
-  const int key_first = 16 * (n >> 2) + (n & 3), key_row = key_first * Stage<D>::kKeyRow, key_mix = Stage<D>::key_mix(key_first);
-  const int value_row = Stage<D>::kKeys + n * Stage<D>::kValueRow, value_mix = Stage<D>::value_mix(n);
+  // Where the lane's operands and codes lie in a stage.  The chunk's number only flips bits below a row's size, so what steps through chunks is an exclusive or with a constant.
+  const int key_first = 16 * (n >> 2) + (n & 3), key_operand = Stage<D>::key_at(key_first, g), value_operand = Stage<D>::value_at(n, g);
+  const int mine = 64 * lot_of<D>(wave) + lane, key_place = Stage<D>::key_at(mine / (D / 16), 2 * (mine % (D / 16))), value_place = Stage<D>::value_at(mine, 0);
   const int32_t me = blockIdx.x;
   const Line line = find_on_line<Short>(a.s, a.c, a.group, kManyRows, a.blocks, me, -1);
   Divided divided = {};
@@ -135,6 +160,8 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(AttnArgs a) {
   int seq = line.seq;
   int32_t base = line.before;
   SeqSizes z = line.z;
+  if (Fmt == kE4m3 && threadIdx.x < D) first_nan[1][threadIdx.x] = INT32_MAX;
+  int parity = 1;                                          // of the items that see a tile
   while (at < end) {
     while (at >= base + cost_of<Short>(z, a.c.hkv, a.group, kManyRows)) {  // the next sequence with rows
       base += cost_of<Short>(z, a.c.hkv, a.group, kManyRows);
@@ -173,40 +200,69 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(AttnArgs a) {
     const int seen = z.len - z.n + (rb * kManyRows + rows - 1) / a.group;
     const int t_end = min(t1, seen < 0 ? 0 : seen / kTile + 1);
     if (t0 < t_end) {
-      Share<D> share;
+      // Tile t's scores are formed a step ahead, so that its exponentials and the products for the next scores are one stream of instructions, and so are its product with the values
+      // and the conversion of codes: no pipe waits for another.  Step t writes the keys of tile t + 2 and the values of tile t + 1 where those of tiles t and t - 1 lay.
+      Share<D> keys, values;
       const int32_t* const table = a.s.pages + (int64_t)seq * a.s.max_pages;
-      load_share<D>(a, table, head, z.len, t0, wave, share);
-      if (threadIdx.x < 2) odd[threadIdx.x] = 0;
+      Pages<D> ahead = {}, at_hand;                            // of tiles t + 3 and t + 2 in step t
+      auto ask_pages = [&](int t) {
+        at_hand = ahead;
+        load_pages<D>(a, table, z.len, t, wave, ahead);
+      };
+      auto ask_keys = [&](int t) { load_share<D>(a, a.c.k, a.c.k_scale, ahead, head, z.len, t, wave, keys); };
+      auto ask_values = [&](int t) { load_share<D>(a, a.c.v, a.c.v_scale, at_hand, head, z.len, t, wave, values); };
+      auto stage_of = [&](int t) { return lds + ((t - t0) & 1) * Stage<D>::kBytes; };
+      auto tidy = [&](int t) {
+        if (Fmt == kE4m3 && t * kTile + kTile - 1 > all_see) without_nan<D>(values, wave, first_nan[parity], t * kTile);
+      };
+      auto note_live = [&](int t) {
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i)
+          if (lane == 0) live[t & 3][group_of<D>(wave, i)] = keys.live[i], key_scale[t & 3][group_of<D>(wave, i)] = keys.live[i] ? keys.scale[i] : 1.f;
+      };
+      auto store_keys = [&](int t) {
+        bf16x8 half;
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) store_word<D, Fmt, false>(keys, i, wave, key_place, stage_of(t), half);
+        note_live(t);
+      };
+      ask_pages(t0);
+      ask_keys(t0);
+      ask_pages(t0 + 1);
+      ask_values(t0);
       __syncthreads();                                     // (the stages of the item before have been read)
-      store_share<D, Fmt>(share, wave, lds, live[0], &odd[0], t0 * kTile + kTile - 1 > all_see);
-      load_share<D>(a, table, head, z.len, t0 + 1, wave, share);     // (past the last tile: pages that are not there, the pool's first is read)
-      for (int t = t0; t < t_end; ++t) {
-        const int st = (t - t0) & 1;
-        unsigned char* const stage = lds + st * Stage<D>::kBytes;
-        __syncthreads();
-        if (t + 1 < t_end) store_share<D, Fmt>(share, wave, lds + (st ^ 1) * Stage<D>::kBytes, live[st ^ 1], &odd[st ^ 1], (t + 1) * kTile + kTile - 1 > all_see);
-        load_share<D>(a, table, head, z.len, t + 2, wave, share);
-        __builtin_amdgcn_sched_barrier(0);                 // (the compiler would keep operands of all parts of the step in registers, and spill)
-
-        f32x4 s[kNB][4];
-        const unsigned char* const keys = stage + fresh(key_row);
+      if (Fmt == kE4m3 && threadIdx.x < D) first_nan[parity ^ 1][threadIdx.x] = INT32_MAX;
+      store_keys(t0);
+      ask_keys(t0 + 1);
+      tidy(t0);
+      bf16x8 half;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < D / 16; ++i) store_word<D, Fmt, true>(values, i, wave, value_place, stage_of(t0), half);
+      store_keys(t0 + 1);
+      ask_pages(t0 + 2);
+      ask_keys(t0 + 2);
+      ask_values(t0 + 1);
+      __syncthreads();
+      // 16 keys after the other: their scores take the registers that the exponentials of as many leave
+      auto scores = [&](int t, f32x4 (&s)[kNB][4], auto meanwhile) {
+        const int k0 = fresh(key_operand);
+        constexpr int kSteps = D / 32;
+        stream_operands<D / 8>([&](int i) { return *reinterpret_cast<const chunk*>(stage_of(t) + (k0 ^ (i % kSteps << 6)) + 4 * (i / kSteps) * Stage<D>::kKeyRow); },
+                               [&](int i, bf16x8 k) {
 #pragma unroll
-          for (int b = 0; b < kNB; ++b) s[b][i] = f32x4{0, 0, 0, 0};
-#pragma unroll
-          for (int j = 0; j < D / 32; ++j) {
-            const bf16x8 k = *reinterpret_cast<const chunk*>(keys + 4 * i * Stage<D>::kKeyRow + (((4 * j + g) ^ key_mix) << 4));
-#pragma unroll
-            for (int b = 0; b < kNB; ++b) s[b][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[b][j], s[b][i], 0, 0, 0);
-          }
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        bf16x8 p[kNB][2];
-        const int live_here = live[st][g];
+                                 for (int b = 0; b < kNB; ++b) {
+                                   const f32x4 zero = {0, 0, 0, 0};
+                                   s[b][i / kSteps] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[b][i % kSteps], i % kSteps == 0 ? zero : s[b][i / kSteps], 0, 0, 0);
+                                 }
+                                 meanwhile(i);
+                               });
+      };
+      auto step = [&](int t, f32x4 (&s)[kNB][4], f32x4 (&s_next)[kNB][4]) {
+        tidy(t + 1);
+        ask_pages(t + 3);
+        const int live_here = live[t & 3][g];
+        const float c = a.scale * key_scale[t & 3][g];
         const bool full = t * kTile + kTile - 1 <= all_see && !__ballot(live_here < kGroup);
-        const unsigned char* const values = stage + fresh(value_row);
-        auto value = [&](int d, int u) { return *reinterpret_cast<const chunk*>(values + 16 * d * Stage<D>::kValueRow + (((2 * g + u) ^ value_mix) << 4)); };
         int sees[kNB];
 #pragma unroll
         for (int b = 0; b < kNB; ++b) sees[b] = min(last[b] - t * kTile - 16 * g, live_here - 1);
@@ -214,45 +270,53 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(AttnArgs a) {
 #pragma unroll
           for (int b = 0; b < kNB; ++b) mask_scores(s[b], sees[b]);
 #pragma unroll
-        for (int b = 0; b < kNB; ++b) softmax_of<D>(s[b], a.scale, 1.f, o[b], m[b], l[b], p[b], nullptr);
+        for (int b = 0; b < kNB; ++b) raise_maximum<D>(s[b], c, o[b], m[b], l[b]);
+        __syncthreads();
+        bf16x8 p[kNB][2];
+        scores(t + 1, s_next, [&](int i) {
+#pragma unroll
+          for (int j = 256 / D * i; j < 256 / D * (i + 1); ++j) {
+            const int b = j / 16, x = j % 16;
+            const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][x / 4][x % 4], c, -m[b]));
+            l[b] += e;
+            p[b][x / 8][x % 8] = (__bf16)e;
+          }
+          // (left alone the compiler adds them up where the sum is due, and keeps them all until then)
+#pragma unroll
+          for (int b = 0; b < kNB; ++b) asm volatile("" : "+v"(l[b]));
+        });
         __builtin_amdgcn_sched_barrier(0);
-        if (Fmt == kE4m3 && !full && odd[st]) {
-          // Rare: a value that some rows do not see is NaN.  The rows that see it get NaN and the others do not: the product with the probabilities takes zeros in its place,
-          // and its number among the keys that a row sees is counted by a product with 1.
+        const int v0 = fresh(value_operand);
+        stream_operands<D / 8>([&](int i) { return *reinterpret_cast<const chunk*>(stage_of(t) + (v0 ^ (i / 4 % 2 << 6)) + 16 * (i / 8 * 4 + i % 4) * Stage<D>::kValueRow); },
+                               [&](int i, bf16x8 v) {
 #pragma unroll
-          for (int b = 0; b < kNB; ++b)
-#pragma unroll
-            for (int d = 0; d < D / 16; ++d) {
-              __builtin_amdgcn_sched_barrier(0);
-              f32x4 count = {0, 0, 0, 0};
-#pragma unroll
-              for (int u = 0; u < 2; ++u) {
-                bf16x8 v = value(d, u), bad, one;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                  const bool nan = __builtin_isnan((float)v[j]);
-                  bad[j] = (__bf16)(nan ? 1.f : 0.f);
-                  one[j] = (__bf16)(8 * u + j <= fresh(sees[b]) ? 1.f : 0.f);
-                  v[j] = nan ? (__bf16)0.f : v[j];
-                }
-                count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bad, one, count, 0, 0, 0);
-                o[b][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[b][u], o[b][d], 0, 0, 0);
-              }
-#pragma unroll
-              for (int j = 0; j < 4; ++j) o[b][d][j] = count[j] > 0.f ? NAN : o[b][d][j];
-            }
-          __builtin_amdgcn_sched_barrier(0);
-        } else {
-#pragma unroll
-          for (int d = 0; d < D / 16; ++d)
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-              const bf16x8 v = value(d, u);
-#pragma unroll
-              for (int b = 0; b < kNB; ++b) o[b][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[b][u], o[b][d], 0, 0, 0);
-            }
-        }
+                                 for (int b = 0; b < kNB; ++b) {
+                                   f32x4& sum = o[b][i / 8 * 4 + i % 4];
+                                   sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[b][i / 4 % 2], sum, 0, 0, 0);
+                                 }
+                                 if (i < D / 16) store_word<D, Fmt, false>(keys, i, wave, key_place, stage_of(t), half);
+                                 else store_word<D, Fmt, true>(values, i - D / 16, wave, value_place, stage_of(t + 1), half);
+                               });
+        note_live(t + 2);
+        ask_keys(t + 3);
+        ask_values(t + 2);
+      };
+      f32x4 s[2][kNB][4];
+      scores(t0, s[0], [](int) {});
+      for (int t = t0; t < t_end; t += 2) {
+        step(t, s[0], s[1]);
+        if (t + 1 < t_end) step(t + 1, s[1], s[0]);
       }
+      if (Fmt == kE4m3)
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int first = first_nan[parity][16 * i + 4 * g + j];
+#pragma unroll
+            for (int b = 0; b < kNB; ++b) o[b][i][j] = first <= last[b] ? NAN : o[b][i][j];
+          }
+      parity ^= 1;
     }
 #pragma unroll
     for (int b = 0; b < kNB; ++b) l[b] = sum_over_groups(l[b]);

@@ -301,6 +301,24 @@ def test_nan_in_the_cache_reaches_only_the_rows_that_see_it(news, bad_key):
 
 
 @pytest.mark.gpu
+def test_nan_among_many_items():
+    """More (sequence, KV head, block of rows) than blocks run at once, so blocks work several in turn: what one saw does not reach the next.  Some sequences are shorter than
+    their new rows, so that whole blocks of rows see nothing."""
+    import torch
+    kv_len = [8 if i % 9 == 4 else 80 + 13 * i % 110 for i in range(60)]
+    news = [90 if i % 9 == 4 else 70 for i in range(60)]
+    ref, cache, pages, cu, q, scale = attn_case(32, 64, 10, 5, kv_len, news, "e4m3")
+    for i in range(0, 60, 2):
+        t, head, channel = kv_len[i] - 1 - i % 3, i % 5, 7 * i % 64
+        ref.v[pages[i, t // 32], head, t % 32, channel] = 127
+    cache = R.to_device(ref, torch, B)
+    got = run_attn(cache, q, cu, kv_len, pages, scale, False)
+    want = ref.attn(q, cu, kv_len, pages, scale)
+    assert 60 < np.isnan(want[0]).sum() < 400 and np.isneginf(want[1]).any()
+    check_attn(got, want)
+
+
+@pytest.mark.gpu
 def test_scores_that_differ_widely():
     """The running maximum rises many times and falls behind by far: e^-80 beside 1."""
     ref, cache, pages, cu, q, scale = attn_case(64, 64, 4, 4, [1000, 640], [1, 1], "e4m3", scale=2.0)
