@@ -129,6 +129,6 @@ __device__ inline float wave_maxf(float x) {
 // ---- host ---------------------------------------------------------------------------------------
 // Checks what every call of the cache checks, and fills the view.  needs_weight: the call reads or writes weights.
 int check_cache(const char* who, const fcp_cache* cache, bool needs_weight, CacheView* out);
-int check_seqs(const char* who, const int32_t* cu, bool needs_cu, const int32_t* kv_len, const int32_t* pages, int32_t n_seqs, int32_t max_pages, int32_t n_rows);
+int check_seqs(const char* who, const fcp_cache& c, const int32_t* cu, bool needs_cu, const int32_t* kv_len, const int32_t* pages, int32_t n_seqs, int32_t max_pages, int32_t n_rows);
 
 }  // namespace fcp

@@ -615,7 +615,7 @@ extern "C" int fcp_cache_attn(const fcp_cache* cache, const void* q, int64_t q_r
   if (weigh != 0 && weigh != 1) return fail(FCP_ERR_INVALID_ARG, "%s: weigh must be 0 or 1", who);
   if (int rc = check_cache(who, cache, weigh, &a.c)) return rc;
   if (int rc = check_heads(who, a.c, hq)) return rc;
-  if (int rc = check_seqs(who, cu_seqlens, true, kv_len, pages, n_seqs, max_pages, tq)) return rc;
+  if (int rc = check_seqs(who, *cache, cu_seqlens, true, kv_len, pages, n_seqs, max_pages, tq)) return rc;
   if (!(softmax_scale > 0.f) || !__builtin_isfinite(softmax_scale)) return fail(FCP_ERR_INVALID_ARG, "%s: softmax_scale must be above 0", who);
   if (tq == 0 || n_seqs == 0) return FCP_OK;
   if (int rc = check_rows(who, cache, q, q_row, tq, hq)) return rc;
@@ -655,7 +655,7 @@ extern "C" int fcp_cache_weigh(const fcp_cache* cache, const void* q, int64_t q_
   WeighArgs a = {};
   if (int rc = check_cache(who, cache, true, &a.c)) return rc;
   if (int rc = check_heads(who, a.c, hq)) return rc;
-  if (int rc = check_seqs(who, cu_seqlens, true, kv_len, pages, n_seqs, max_pages, tq)) return rc;
+  if (int rc = check_seqs(who, *cache, cu_seqlens, true, kv_len, pages, n_seqs, max_pages, tq)) return rc;
   if (!(softmax_scale > 0.f) || !__builtin_isfinite(softmax_scale)) return fail(FCP_ERR_INVALID_ARG, "%s: softmax_scale must be above 0", who);
   if (tq == 0 || n_seqs == 0) return FCP_OK;
   if (int rc = check_rows(who, cache, q, q_row, tq, hq)) return rc;

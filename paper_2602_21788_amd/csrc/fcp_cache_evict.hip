@@ -515,7 +515,7 @@ extern "C" int fcp_cache_evict(const fcp_cache* cache, const int32_t* pages, con
   const char* who = "fcp_cache_evict";
   EvictArgs a = {};
   if (int rc = check_cache(who, cache, true, &a.c)) return rc;
-  if (int rc = check_seqs(who, nullptr, false, kv_len, pages, n_seqs, max_pages, 0)) return rc;
+  if (int rc = check_seqs(who, *cache, nullptr, false, kv_len, pages, n_seqs, max_pages, 0)) return rc;
   if (n_first < 0 || n_recent < 0 || budget < 1 || (int64_t)n_first + n_recent > budget)
     return fail(FCP_ERR_INVALID_ARG, "%s: budget must be at least 1 and n_first + n_recent, which must not be negative", who);
   if (max_new_pages < 0) return fail(FCP_ERR_INVALID_ARG, "%s: negative size", who);
@@ -530,7 +530,6 @@ extern "C" int fcp_cache_evict(const fcp_cache* cache, const int32_t* pages, con
   const size_t need = p.bytes;
   if (scratch_bytes < need) return fail(FCP_ERR_CAPACITY, "%s: scratch has %zu bytes, %zu are needed", who, scratch_bytes, need);
   const int64_t use = (most + a.c.page - 1) / a.c.page;      // (further entries of new_pages are not used)
-  if (room > 1 << 30) return fail(FCP_ERR_UNSUPPORTED, "%s: a table of more than 2^30 tokens", who);
   if ((int64_t)n_seqs * a.c.hkv > INT32_MAX || (int64_t)n_seqs * max_new_pages > INT32_MAX)
     return fail(FCP_ERR_UNSUPPORTED, "%s: more than 2^31 - 1 pages or heads of all sequences", who);
   a.s = {nullptr, kv_len, pages, n_seqs, max_pages, 0};

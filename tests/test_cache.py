@@ -102,6 +102,13 @@ def test_refusals_come_before_any_device_work():
     assert Call(max_new=1).evict() == full and Call(scratch=Call.fake + 1).evict() == bad and Call(bytes=1).evict() == full
 
 
+def test_tables_are_bounded():
+    """A token's place is a 32-bit number, and tiles past the last one are looked at."""
+    for op in ("append", "attn", "weigh", "evict"):
+        for page, pages in ((128, (1 << 23) + 1), (16, (1 << 26) + 1), (16, 1 << 30)):
+            assert getattr(Call(page_tokens=page, max_pages=pages), op)() == B.FCP_ERR_UNSUPPORTED and b"2^30 tokens" in B.lib().fcp_last_error()
+
+
 def test_scratch_sizes():
     c = Call().c
     for which in (B.FCP_SCRATCH_CACHE_ATTN, B.FCP_SCRATCH_CACHE_WEIGH, B.FCP_SCRATCH_CACHE_EVICT):
