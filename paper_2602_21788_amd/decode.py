@@ -55,6 +55,8 @@ class CacheDecoder:
 
     def _grow(self, news):
         """Room for news[s] more tokens of every sequence; (cu_seqlens, positions) of the new rows."""
+        if news.shape != self.kv_len.shape or (news < 0).any():
+            raise ValueError("a number of tokens, 0 or more, is needed for every sequence")
         need = [-(-(int(n) + int(m)) // self.P) - int((row >= 0).sum()) for n, m, row in zip(self.kv_len, news, self.pages)]
         if sum(max(n, 0) for n in need) > len(self.free) or (self.kv_len + news > self.pages.shape[1] * self.P).any():
             raise MemoryError("no page left: evict, or close a sequence")
@@ -81,6 +83,8 @@ class CacheDecoder:
     def prefill(self, q, k, v, lens):
         """Prompts of lens[s] tokens for empty sequences: bf16 rows q [sum, hq, D], k, v [sum, hkv, D] (turned in place).  Returns O [sum, hq, D], LSE [hq, sum]."""
         lens = np.asarray(lens, np.int32)
+        if not q.shape[0] == k.shape[0] == v.shape[0] == lens.sum():
+            raise ValueError("q, k and v must have sum(lens) rows")
         if self.kv_len.any():
             raise ValueError("prefill is for empty sequences; step() takes the next piece of a prompt")
         cu, pos = self._grow(lens)
@@ -97,6 +101,8 @@ class CacheDecoder:
     def step(self, q, k, v, news, weigh=True):
         """news[s] new tokens of every sequence (0, 1, or more): bf16 rows as in prefill.  Returns O [sum, hq, D], LSE [hq, sum]."""
         news = np.asarray(news, np.int32)
+        if not q.shape[0] == k.shape[0] == v.shape[0] == news.sum():
+            raise ValueError("q, k and v must have sum(news) rows")
         cu, pos = self._grow(news)
         self._rotate(q, k, pos)
         B.fcp_cache_append(self.cache, k, v, cu, self.kv_len_d, self.pages_d)
@@ -108,6 +114,8 @@ class CacheDecoder:
 
     def evict(self, budget, n_first=4, n_recent=64):
         """Cuts every sequence to `budget` tokens; the old pages are free.  Returns the kept token numbers [n_seqs, hkv, budget] (-1 past the last)."""
+        if budget < max(1, n_first + n_recent) or min(n_first, n_recent) < 0:
+            raise ValueError("budget must be at least 1 and n_first + n_recent, which must not be negative")
         self._upload()
         new_len = np.minimum(self.kv_len, budget).astype(np.int32)
         counts = -(-new_len // self.P)

@@ -88,3 +88,22 @@ def test_the_decoder_says_when_pages_are_short():
     assert dec.kv_len.tolist() == [16, 0] and len(dec.free) == 5
     with pytest.raises(ValueError):
         dec.prefill(*rows(4), [2, 2])
+
+
+@pytest.mark.gpu
+def test_refusals_change_nothing():
+    import torch
+    from paper_2602_21788_amd.decode import CacheDecoder
+    dec = CacheDecoder(2, 8, 4, 4, 2, 64, page_tokens=16)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    rows = lambda n, h: bf16_rows(torch, g, n, h, 64)
+    dec.prefill(rows(50, 4), rows(50, 2), rows(50, 2), [40, 10])
+    free, lens, pages = list(dec.free), dec.kv_len.copy(), dec.pages.copy()
+    for call in (lambda: dec.evict(20, n_first=4, n_recent=64), lambda: dec.evict(0, 0, 0), lambda: dec.evict(20, -1, 4),
+                 lambda: dec.step(rows(3, 4), rows(3, 2), rows(3, 2), [1, 1]), lambda: dec.step(rows(1, 4), rows(1, 2), rows(1, 2), [2, -1]),
+                 lambda: dec.step(rows(1, 4), rows(1, 2), rows(1, 2), [1]), lambda: dec.prefill(rows(1, 4), rows(1, 2), rows(1, 2), [1, 0])):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(MemoryError):
+        dec.step(rows(90, 4), rows(90, 2), rows(90, 2), [20, 70])
+    assert dec.free == free and np.array_equal(dec.kv_len, lens) and np.array_equal(dec.pages, pages)
