@@ -454,7 +454,8 @@ int fcp_rotary(const fcp_rotary_part* parts, int32_t n_parts, const double* turn
  * Sequence s owns the pages pages[s][0], pages[s][1], ...: its token t is slot t % page_tokens of page pages[s][t / page_tokens].  kv_len[s] tokens
  * are cached; in every call below that takes queries or new rows, the n = cu_seqlens[s + 1] - cu_seqlens[s] rows of sequence s are its LAST n tokens,
  * and kv_len counts them.  Both tables are device memory, so that a captured graph follows them.  A page number outside 0 .. n_pages - 1 is not
- * followed: the tokens in it are not written, and seen by nobody.  kv_len is taken as at most max_pages * page_tokens, which is at most 2^30 (FCP_ERR_UNSUPPORTED beyond).
+ * followed: the tokens in it are not written, and seen by nobody.  cu_seqlens must not fall: where it does, the calls that take queries do nothing at all.
+ * softmax_scale: finite, at least 2^-32.  kv_len is taken as at most max_pages * page_tokens, which is at most 2^30 (FCP_ERR_UNSUPPORTED beyond).
  */
 #define FCP_CACHE_E4M3 0
 #define FCP_CACHE_INT8 1

@@ -49,35 +49,43 @@ __device__ inline int32_t tiles_of(int len) { return max((len + kTile - 1) / kTi
 template <bool Short> __device__ inline int32_t places_of(int len) { return Short ? 1 : tiles_of(len); }
 template <bool Short>
 __device__ inline int32_t cost_of(const SeqSizes& z, int hkv, int group, int rows) {
-  return z.n == 0 ? 0 : hkv * ((z.n * group + rows - 1) / rows) * places_of<Short>(z.len);
+  return z.n == 0 ? 0 : hkv * ((z.n * group - 1) / rows + 1) * places_of<Short>(z.len);
 }
 
-// The sequence that holds the beginning of share `block` (blocks = 0: place `block` itself), or, with tok >= 0, query row `tok`; seq = -1 if there is none.  Every thread of the block (256, 512) calls; a thread
+// The sequence that holds the beginning of share `block` (blocks = 0: place `block` itself); seq = -1 if there is none.  Every thread of the block (256, 512) calls; a thread
 // looks at a run of sequences, all of which are asked for at once.  At most `blocks` shares, fewer where a share would have fewer than Least places.
+// Where cu_seqlens falls, rows would belong to several sequences and there could be more places than the host counted: then there is no work at all.
 template <bool Short, int Threads = 256, int Least = Short ? 1 : kLeastTiles>
-static __device__ inline Line find_on_line(const SeqView& s, const CacheView& c, int group, int rows, int blocks, int block, int tok) {
+static __device__ inline Line find_on_line(const SeqView& s, const CacheView& c, int group, int rows, int blocks, int block) {
   __shared__ int32_t sums[Threads / 64];
   __shared__ int32_t found[5];
   const int per = (s.n_seqs + Threads - 1) / Threads, a = min((int)threadIdx.x * per, s.n_seqs), b = min(a + per, s.n_seqs);
   int32_t mine = 0;
-  for (int i = a; i < b; ++i) mine += cost_of<Short>(seq_sizes(s, i, c.page), c.hkv, group, rows);
+  bool falls = false;
+  for (int i = a; i < b; ++i) {
+    falls |= s.cu[i + 1] < s.cu[i];
+    mine += cost_of<Short>(seq_sizes(s, i, c.page), c.hkv, group, rows);
+  }
+  falls = __ballot(falls);
   int32_t upto = wave_prefix_sum(mine);
-  if ((threadIdx.x & 63) == 63) sums[threadIdx.x >> 6] = upto;
+  if ((threadIdx.x & 63) == 63) sums[threadIdx.x >> 6] = falls ? -1 : upto;
   if (threadIdx.x == 0) found[0] = -1;
   __syncthreads();
   Line line = {};
   for (int w = 0; w < Threads / 64; ++w) {
     if (w < (int)(threadIdx.x >> 6)) upto += sums[w];
     line.total += sums[w];
+    falls |= sums[w] < 0;
   }
+  if (falls) line.total = 0;
   line.sharers = min(blocks, (line.total + Least - 1) / Least);
   int32_t at = upto - mine;            // of the thread's first sequence
-  const int32_t x = blocks == 0 ? block : tok >= 0 || block >= line.sharers ? -1 : line.begin(block);
-  if (tok >= 0 || (x >= at && x < upto)) {
+  const int32_t x = falls ? -1 : blocks == 0 ? block : block >= line.sharers ? -1 : line.begin(block);
+  if (x >= 0 && x >= at && x < upto) {
     for (int i = a; i < b; ++i) {
       const SeqSizes z = seq_sizes(s, i, c.page);
       const int32_t n = cost_of<Short>(z, c.hkv, group, rows);
-      if (tok >= 0 ? tok >= z.row0 && tok < z.row0 + z.n : x < at + n) {
+      if (x < at + n) {
         found[0] = i;
         found[1] = at;
         found[2] = z.row0;

@@ -177,7 +177,7 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
   __shared__ float stage_m[kWaves * kRows], stage_l[kWaves * kRows];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
   const int32_t me = blockIdx.x;
-  const Line line = find_on_line<Short>(a.s, a.c, a.group, kRows, a.blocks, me, -1);
+  const Line line = find_on_line<Short>(a.s, a.c, a.group, kRows, a.blocks, me);
   Divided divided = {};
   int32_t at = 0, end = 0;
   if (line.seq >= 0) {
@@ -327,8 +327,8 @@ __global__ __launch_bounds__(kWeighThreads, 2) void weigh_kernel(WeighArgs a) {
   __shared__ __align__(256) unsigned char rows_lds[kWeighWaves * 2 * kRowBytes];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
   // the line with one block of rows per KV head
-  const int kAll = 1 << 30;
-  const Line line = find_on_line<false, kWeighThreads>(a.s, a.c, 1, kAll, 0, blockIdx.x, -1);
+  const int kAll = INT32_MAX;
+  const Line line = find_on_line<false, kWeighThreads>(a.s, a.c, 1, kAll, 0, blockIdx.x);
   if (line.seq < 0) return;
   int seq = line.seq;
   int32_t base = line.before;
@@ -454,7 +454,7 @@ constexpr int kScoreTiles = 4 * kWaves;   // that a block works at once
 __global__ __launch_bounds__(256) void weigh_scores_kernel(AttnArgs a, int rows_of_block) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int32_t me = blockIdx.x;
-  const Line line = find_on_line<false, 256, kScoreTiles>(a.s, a.c, a.group, rows_of_block, gridDim.x, me, -1);
+  const Line line = find_on_line<false, 256, kScoreTiles>(a.s, a.c, a.group, rows_of_block, gridDim.x, me);
   if (line.seq < 0) return;
   int32_t at = line.begin(me);
   const int32_t end = line.begin(me + 1);
@@ -576,6 +576,11 @@ int check_heads(const char* who, const CacheView& c, int32_t hq) {
   if (hq < 1 || hq % c.hkv) return fail(FCP_ERR_UNSUPPORTED, "%s: %d query heads on %d KV heads", who, hq, c.hkv);
   return FCP_OK;
 }
+// (times log2(e) and a scale of 2^-110 it must not become 0: a masked score, -inf, times 0 is NaN)
+int check_scale(const char* who, float scale) {
+  if (!(scale >= 0x1p-32f) || !__builtin_isfinite(scale)) return fail(FCP_ERR_INVALID_ARG, "%s: softmax_scale must be finite and at least 2^-32", who);
+  return FCP_OK;
+}
 int check_rows(const char* who, const fcp_cache* cache, const void* q, int64_t q_row, int32_t tq, int32_t hq) {
   if (!q || q_row < (int64_t)hq * cache->head_dim || q_row % 8 || (uintptr_t)q % 16)
     return fail(FCP_ERR_INVALID_ARG, "%s: query rows must be at least hq * head_dim elements apart, a multiple of 8, and 16-byte aligned", who);
@@ -616,7 +621,7 @@ extern "C" int fcp_cache_attn(const fcp_cache* cache, const void* q, int64_t q_r
   if (int rc = check_cache(who, cache, weigh, &a.c)) return rc;
   if (int rc = check_heads(who, a.c, hq)) return rc;
   if (int rc = check_seqs(who, *cache, cu_seqlens, true, kv_len, pages, n_seqs, max_pages, tq)) return rc;
-  if (!(softmax_scale > 0.f) || !__builtin_isfinite(softmax_scale)) return fail(FCP_ERR_INVALID_ARG, "%s: softmax_scale must be above 0", who);
+  if (int rc = check_scale(who, softmax_scale)) return rc;
   if (tq == 0 || n_seqs == 0) return FCP_OK;
   if (int rc = check_rows(who, cache, q, q_row, tq, hq)) return rc;
   if (!o || !lse || (uintptr_t)o % 16 || (uintptr_t)lse % 4) return fail(FCP_ERR_INVALID_ARG, "%s: o and lse are required and must be aligned", who);
@@ -656,7 +661,7 @@ extern "C" int fcp_cache_weigh(const fcp_cache* cache, const void* q, int64_t q_
   if (int rc = check_cache(who, cache, true, &a.c)) return rc;
   if (int rc = check_heads(who, a.c, hq)) return rc;
   if (int rc = check_seqs(who, *cache, cu_seqlens, true, kv_len, pages, n_seqs, max_pages, tq)) return rc;
-  if (!(softmax_scale > 0.f) || !__builtin_isfinite(softmax_scale)) return fail(FCP_ERR_INVALID_ARG, "%s: softmax_scale must be above 0", who);
+  if (int rc = check_scale(who, softmax_scale)) return rc;
   if (tq == 0 || n_seqs == 0) return FCP_OK;
   if (int rc = check_rows(who, cache, q, q_row, tq, hq)) return rc;
   if (!lse || (uintptr_t)lse % 4) return fail(FCP_ERR_INVALID_ARG, "%s: lse is required", who);

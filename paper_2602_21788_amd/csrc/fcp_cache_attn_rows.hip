@@ -150,7 +150,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(AttnArgs a) {
   const int key_first = 16 * (n >> 2) + (n & 3), key_operand = Stage<D>::key_at(key_first, g), value_operand = Stage<D>::value_at(n, g);
   const int mine = 64 * lot_of<D>(wave) + lane, key_place = Stage<D>::key_at(mine / (D / 16), 2 * (mine % (D / 16))), value_place = Stage<D>::value_at(mine, 0);
   const int32_t me = blockIdx.x;
-  const Line line = find_on_line<Short>(a.s, a.c, a.group, kManyRows, a.blocks, me, -1);
+  const Line line = find_on_line<Short>(a.s, a.c, a.group, kManyRows, a.blocks, me);
   Divided divided = {};
   int32_t at = 0, end = 0;
   if (line.seq >= 0) {

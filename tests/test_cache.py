@@ -441,3 +441,120 @@ def test_evict_of_equal_weights_and_of_bad_tables():
         assert int(new_len[0]) == min(max(lens[0], 0), 40)
     k, _, _, _, _ = R.from_device(cache)
     assert np.array_equal(k[:6], ref.k[:6]) and np.array_equal(k[6:8], ref.k[6:8])
+
+
+def test_scales_that_would_vanish_are_refused():
+    """softmax_scale times the least scale of a page must stay above 0, or a masked score, -inf, becomes NaN."""
+    for op in ("attn", "weigh"):
+        call = lambda v: getattr(Call(scale=v, n_seqs=0), op)()
+        assert call(2.0 ** -33) == B.FCP_ERR_INVALID_ARG and call(float("inf")) == B.FCP_ERR_INVALID_ARG and call(-1.0) == B.FCP_ERR_INVALID_ARG
+        assert call(2.0 ** -32) == 0 and call(1.0) == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows", [1, 40])
+def test_least_scales_beside_masked_tokens(rows):
+    """Pages of zeros (scale 2^-110) with the least softmax_scale: every seen token gets the same weight."""
+    import torch
+    P, D, n = 16, 64, 75
+    pages = -(-n // P)
+    z = lambda *s, dt=torch.int8: torch.zeros(*s, dtype=dt, device="cuda")
+    cache = B.Cache(z(pages, 1, P, D), z(pages, 1, P // 16, D, 16), z(pages, 1, dt=torch.float32), z(pages, 1, dt=torch.float32), z(pages, 1, P, dt=torch.float32))
+    cache.k_scale.fill_(2.0 ** -110), cache.v_scale.fill_(2.0 ** -110)
+    q = np.ones((rows, 2, D))
+    o, lse = run_attn(cache, q, np.array([0, rows]), [n], np.arange(pages, dtype=np.int32)[None], 2.0 ** -32, True)
+    seen = n - rows + 1 + np.arange(rows)
+    # the sum of n ones is exact; its logarithm is off by a few steps of itself
+    assert (o == 0).all() and (np.abs(lse - np.log(seen)) <= np.log(seen) * 8 * 2.0 ** -24).all()
+    want = sum(2.0 / s * (np.arange(pages * P) < s) for s in seen)
+    got = cache.weight.double().cpu().numpy().reshape(-1)
+    assert (np.abs(got - want) <= want * (2 * rows + 40) * 2.0 ** -24).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("news", [[1, 1, 1], [50, 60, 70]])
+def test_rows_of_several_sequences_are_not_worked(news):
+    """cu_seqlens that falls: more places than the host counted, so nothing is computed and nothing is written, in scratch neither."""
+    import torch
+    kv_len = [150, 130, 140]
+    ref, cache, pages, cu, q, scale = attn_case(32, 64, 4, 2, kv_len, news, "int8")
+    total = int(cu[-1])
+    for bad in ([0, total, 0, total], [0, 2, 1, total], [total, 0, 0, 0], [0, 2147483647, -2147483648, total]):
+        for which, weigh in ((B.FCP_SCRATCH_CACHE_ATTN, False), (B.FCP_SCRATCH_CACHE_WEIGH, True)):
+            n = B.fcp_cache_scratch_bytes(which, cache, 3, pages.shape[1], total, 4)
+            scratch = torch.full((n + 4096,), 77, dtype=torch.uint8, device="cuda")
+            o, lse = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device="cuda"), torch.full((4, total), 7.0, device="cuda")
+            B.fcp_cache_attn(cache, dev_bf16(q), dev(bad), dev(kv_len), dev(pages), scale, o, lse, scratch[:n], weigh=weigh)
+            assert (o == 7).all() and (lse == 7).all() and (scratch[n:] == 77).all()
+        B.fcp_cache_weigh(cache, dev_bf16(q), torch.zeros(4, total, device="cuda"), dev(bad), dev(kv_len), dev(pages), scale)
+        assert np.array_equal(R.check_content(cache, ref), ref.weight.astype(np.float32))
+    # and the same call with good ones works
+    check_attn(run_attn(cache, q, cu, kv_len, pages, scale, False), ref.attn(q, cu, kv_len, pages, scale))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("news", [[1, 1], [3, 2], [40, 65]])
+def test_queries_that_are_slices_of_wider_rows(news):
+    """Rows of the fused projection's output: bit for bit the results of rows that lie together."""
+    import torch
+    kv_len = [300, 90]
+    _, cache, pages, cu, q, scale = attn_case(64, 128, 6, 2, kv_len, news, "e4m3")
+    n = int(cu[-1])
+    wide = torch.full((n, 6 * 128 + 520), float("nan"), dtype=torch.bfloat16, device="cuda")
+    sliced = wide[:, 8: 8 + 768].unflatten(1, (6, 128))
+    sliced.copy_(dev_bf16(q))
+    out = []
+    for x in (dev_bf16(q), sliced):
+        cache.weight.zero_()
+        o, lse = torch.empty(n, 6, 128, dtype=torch.bfloat16, device="cuda"), torch.empty(6, n, device="cuda")
+        scratch = torch.empty(B.fcp_cache_scratch_bytes(B.FCP_SCRATCH_CACHE_WEIGH, cache, 2, pages.shape[1], n, 6), dtype=torch.uint8, device="cuda")
+        B.fcp_cache_attn(cache, x, dev(cu), dev(kv_len), dev(pages), scale, o, lse, scratch, weigh=True)
+        first = cache.weight.clone()
+        B.fcp_cache_weigh(cache, x, lse, dev(cu), dev(kv_len), dev(pages), scale)
+        out.append((o, lse, first, cache.weight.clone()))
+    assert all(torch.equal(a, b) for a, b in zip(*out))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_pages_past_the_32nd_bit(fmt):
+    """The last pages of a pool whose keys take more than 2^32 bytes: bit for bit what the same pages give in a small pool."""
+    import torch
+    P, D, hkv, hq, kv_len = 128, 128, 8, 8, [700, 260]
+    dt = torch.int8
+    used = 16
+    n_big = (1 << 32) // (P * D * hkv) + used
+    view = lambda t: t.view(torch.float8_e4m3fn) if fmt == "e4m3" else t
+    g = torch.Generator(device="cuda").manual_seed(3)
+    rows = lambda n, h: torch.randn(n, h, D, generator=g, device="cuda").to(torch.bfloat16)
+    cu, cu1 = np.array([0, 700, 960]), np.array([0, 70, 71])
+    k, v, q = rows(960, hkv), rows(960, hkv), rows(71, hq)
+    lse_in = torch.full((hq, 71), 6.0, device="cuda")
+    results = []
+    for n in (used, n_big):
+        at = n - used
+        mk = lambda *s: view(torch.empty(*s, dtype=dt, device="cuda"))
+        cache = B.Cache(mk(n, hkv, P, D), mk(n, hkv, P // 16, D, 16), torch.empty(n, hkv, device="cuda"), torch.empty(n, hkv, device="cuda"), torch.empty(n, hkv, P, device="cuda"))
+        for t in (cache.k, cache.v, cache.weight):
+            (t.view(torch.int8) if t.element_size() == 1 else t)[at:].zero_()
+        cache.k_scale[at:].fill_(1.0), cache.v_scale[at:].fill_(1.0)
+        pages = dev(np.array([[5, 0, 3, 7, 1, 9], [2, 8, 4, -1, -1, -1]], np.int32) + at * np.array([[1] * 6, [1, 1, 1, 0, 0, 0]], np.int32))
+        new_pages = dev(np.array([[12, 10], [15, 6]], np.int32) + at)
+        B.fcp_cache_append(cache, k, v, dev(cu), dev(kv_len), pages)
+        got = []
+        for rows_cu, x in ((cu1, q), (np.array([0, 1, 2]), q[:2])):
+            m = x.shape[0]
+            o, lse = torch.empty(m, hq, D, dtype=torch.bfloat16, device="cuda"), torch.empty(hq, m, device="cuda")
+            scratch = torch.empty(B.fcp_cache_scratch_bytes(B.FCP_SCRATCH_CACHE_WEIGH, cache, 2, 6, m, hq), dtype=torch.uint8, device="cuda")
+            B.fcp_cache_attn(cache, x, dev(rows_cu), dev(kv_len), pages, 0.09, o, lse, scratch, weigh=True)
+            got += [o, lse]
+        B.fcp_cache_weigh(cache, q, lse_in, dev(cu1), dev(kv_len), pages, 0.09)
+        kept, new_len = torch.empty(2, hkv, 200, dtype=torch.int32, device="cuda"), torch.empty(2, dtype=torch.int32, device="cuda")
+        scratch = torch.empty(B.fcp_cache_scratch_bytes(B.FCP_SCRATCH_CACHE_EVICT, cache, 2, 6), dtype=torch.uint8, device="cuda")
+        B.fcp_cache_evict(cache, pages, dev(kv_len), new_pages, 200, 4, 30, kept, new_len, scratch)
+        got += [kept, new_len, cache.k_scale[at:].clone(), cache.v_scale[at:].clone(), cache.weight[at:].clone()]
+        got += [t.view(torch.int8)[at:].clone() for t in (cache.k, cache.v)]
+        results.append(got)
+        del cache
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+    assert float(results[0][8].sum()) > 100 and not torch.isnan(results[0][0].float()).any()
