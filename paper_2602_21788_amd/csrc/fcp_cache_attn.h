@@ -22,7 +22,7 @@ struct AttnArgs {
   float* lse;
   float* part;                         // two slots per block: rows x (D + 2) floats
   struct Divided* divided;             // per block: the item that begins in it and goes on in the blocks after it
-  float* scores;                       // weigh: [tile][4 key tiles][16 rows][4 groups][4 keys], in the order in which waves hold them, scaled by log2(e); or NULL
+  float* scores;                       // weigh: 16 x 64 for every place on the line, scaled by log2(e), in the order in which waves hold them; or NULL
   int32_t blocks;                      // that share the line
 };
 

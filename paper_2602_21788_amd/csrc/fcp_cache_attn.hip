@@ -27,10 +27,19 @@ struct RowState {
 // Pages of a tile for a lane: of the keys that its matrix row holds in the four key tiles, 16 (n / 4) + 4 i + n % 4, and of its 16 neighbouring keys 16 g ..; -1: not
 // there, or no cached token in it.
 struct TilePages { int32_t k, v; };
+// The table's entries, of a sequence with cached tokens (past the last token the last one's: a load under a condition is waited for at once, and everything before it too) ..
 template <class Args>
-__device__ inline TilePages pages_of(const Args& a, int seq, int len, int tile) {
+__device__ inline TilePages ask_pages(const Args& a, int seq, int len, int tile) {
   const int lane = threadIdx.x & 63, kk = tile * kTile + 16 * ((lane & 15) >> 2), vk = tile * kTile + 16 * (lane >> 4);
-  return {kk < len ? page_at(a.s, a.c, seq, kk >> a.c.log_page) : -1, vk < len ? page_at(a.s, a.c, seq, vk >> a.c.log_page) : -1};
+  const int32_t* const table = a.s.pages + (int64_t)seq * a.s.max_pages;
+  return {table[min(kk, len - 1) >> a.c.log_page], table[min(vk, len - 1) >> a.c.log_page]};
+}
+// .. and what they say.
+template <class Args>
+__device__ inline TilePages pages_of(const Args& a, const TilePages& entries, int len, int tile) {
+  const int lane = threadIdx.x & 63, kk = tile * kTile + 16 * ((lane & 15) >> 2), vk = tile * kTile + 16 * (lane >> 4);
+  const uint32_t n = a.c.n_pages;
+  return {kk < len && (uint32_t)entries.k < n ? entries.k : -1, vk < len && (uint32_t)entries.v < n ? entries.v : -1};
 }
 template <int D>
 __device__ inline void load_keys(const CacheView& c, int head, int tile, int32_t page, u32x4 (&k)[4][D / 64]) {
@@ -64,9 +73,11 @@ __device__ inline void scores_of(const u32x4 (&k)[4][D / 64], const bf16x8 (&q)[
     s[i] = f32x4{0, 0, 0, 0};
 #pragma unroll
     for (int j = 0; j < D / 64; ++j) {
-      s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8<Fmt>(k[i][j][0], k[i][j][1]), q[2 * j], s[i], 0, 0, 0);
-      s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8<Fmt>(k[i][j][2], k[i][j][3]), q[2 * j + 1], s[i], 0, 0, 0);
+      const u32x4 w = k[i][j];
+      s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8<Fmt>(w[0], w[1]), q[2 * j], s[i], 0, 0, 0);
+      s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8<Fmt>(w[2], w[3]), q[2 * j + 1], s[i], 0, 0, 0);
     }
+    if (Fmt == kInt8) __builtin_amdgcn_sched_barrier(0);   // (left alone the compiler converts a tile's codes all at once, which takes 60 registers more and no less time)
   }
 }
 
@@ -116,52 +127,85 @@ __device__ inline void clear_hidden(u32x4 (&v)[D / 16], int live, int last, RowS
   __builtin_amdgcn_sched_barrier(0);
 }
 
+// Scores kept of a tile of an item: [rows / 4][4 key tiles][4 groups][4 rows][4 keys], tiles next to each other in the item's part of the line (which has room for 16 rows each).
+// 16 neighbouring lanes of a store hold one group, so 4 rows of them are 64 bytes at one place; with rows outside groups they were four places, and that bounded the kernel.
+__device__ inline int score_floats(int rows) { return (rows + 3) / 4 * (4 * kTile); }
+constexpr int kRing = 16 * 4 * kTile;  // floats of a wave's ring: 16 tiles of four rows, 4 of 16
+__device__ inline int score_at(int row) { return row / 4 * (4 * kTile) + row % 4 * 4; }
+
 // Tiles first, first + step, ... below end for 16 rows of one KV head.  last_tok: last token that the lane's row sees; all_see: all rows see
-// the tokens up to it.  A tile's keys are asked for when the keys before them have become scores, its values when the values before them are in the sums, page numbers a tile
-// earlier still: a wave always has 8 to 16 KB on their way.
-template <int D, int Fmt>
+// the tokens up to it.  A tile's keys are asked for when the keys before them have become scores, its values when the values before them are in the sums: a wave always has 8 to 16 KB
+// on their way.  Page numbers are asked for a tile earlier, right behind keys: loads come back in order, so those behind values would be waited for with the values.
+// Scored: the scores are kept (score_rows rows), in `ring` until it is full: stores between the loads hold these up, and that costs less in few long bursts.  64 sequences of 4700 tokens,
+// int8, 32 heads on 8, 128 channels, with weights: 168 us, stored tile by tile 178; lengths from 819 to 16384: 186 and 188.
+template <int D, int Fmt, bool Scored>
 __device__ inline void walk(const AttnArgs& a, int seq, int head, int len, int first, int end, int step, const bf16x8 (&q)[D / 32], int last_tok, int all_see,
-                            RowState<D>& r, float* scores, int score_rows) {
+                            RowState<D>& r, float* scores, int score_rows, float* ring) {
   if (first >= end) return;
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   u32x4 k[4][D / 64], v[D / 16];
-  TilePages at = pages_of(a, seq, len, first), next = pages_of(a, seq, len, first + step);
+  TilePages at = pages_of(a, ask_pages(a, seq, len, first), len, first), next = ask_pages(a, seq, len, first + step);
   load_keys<D>(a.c, head, first, at.k, k);
   TileScales sc = scales_of(a.c, head, at.v);
   load_values<D>(a.c, head, first, at.v, v);
+  asm volatile("");                                        // (these loads and the loop's own must not become one at its head: the compiler then copies all that it carries, and spills)
+  int kept = 0;                                            // tiles in the ring, the last of them at hand
+  auto flush = [&](int last) {
+    const int lots = score_floats(score_rows) / 256;       // of 1 KB a tile
+    wave_exchange();
+    for (int t = 0; t < kept; ++t) {
+      float* const to = scores + (int64_t)(last - (kept - 1 - t) * step) * (256 * lots) + 4 * lane;
+      for (int x = 0; x < lots; ++x) *reinterpret_cast<f32x4*>(to + 256 * x) = *reinterpret_cast<const f32x4*>(ring + 256 * (t * lots + x) + 4 * lane);
+    }
+    wave_exchange();
+  };
   // (The last tile apart: loads under a condition would all be waited for where it ends.)
   auto tile = [&](int i, auto more) {
     f32x4 s[4];
     scores_of<D, Fmt>(k, q, s);
     TileScales sc_next = sc;
+    TilePages at_next = at;
     if constexpr (more) {
-      load_keys<D>(a.c, head, i + step, next.k, k);
-      sc_next = scales_of(a.c, head, next.v);
+      at_next = pages_of(a, next, len, i + step);
+      load_keys<D>(a.c, head, i + step, at_next.k, k);
+      sc_next = scales_of(a.c, head, at_next.v);
+      next = ask_pages(a, seq, len, i + 2 * step);
     }
     const float c = a.scale * sc.k;
     const bool full = i * kTile + kTile - 1 <= all_see && !__ballot(at.v < 0);
-    float* const to = scores && n < score_rows ? scores + (int64_t)i * (16 * kTile) + 16 * n + 4 * g : nullptr;
     if (!full) {
       const int key0 = i * kTile + 16 * g, last = at.v < 0 ? -1 : last_tok - key0;
       mask_scores(s, last);
       clear_hidden<D, Fmt>(v, at.v < 0 ? 0 : len - key0, last, r);
     }
-    if (to)
+    if constexpr (Scored) {
+      if (n < score_rows) {
+        float* const to = ring + kept * score_floats(score_rows) + score_at(n) + 16 * g;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) *reinterpret_cast<f32x4*>(to + 16 * 16 * j) = s[j] * c;
+        for (int j = 0; j < 4; ++j) *reinterpret_cast<f32x4*>(to + 64 * j) = s[j] * c;
+      }
+      ++kept;
+    }
     raise_maximum<D>(s, c, r.o, r.m, r.l);
     bf16x8 p[2];
     probabilities_of(s, c, sc.v, r.m, r.l, p);
 #pragma unroll
-    for (int d = 0; d < D / 16; ++d)
+    for (int d = 0; d < D / 16; ++d) {
+      const u32x4 w = v[d];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) r.o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8<Fmt>(v[d][2 * h], v[d][2 * h + 1]), p[h], r.o[d], 0, 0, 0);
+      for (int h = 0; h < 2; ++h) r.o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8<Fmt>(w[2 * h], w[2 * h + 1]), p[h], r.o[d], 0, 0, 0);
+      if (Fmt == kInt8) __builtin_amdgcn_sched_barrier(0);
+    }
     if constexpr (more) {
-      load_values<D>(a.c, head, i + step, next.v, v);
-      at = next;
-      next = pages_of(a, seq, len, i + 2 * step);
+      load_values<D>(a.c, head, i + step, at_next.v, v);
+      at = at_next;
       sc = sc_next;
     }
+    if constexpr (Scored)
+      if (!more || (kept + 1) * score_floats(score_rows) > kRing) {
+        flush(i);
+        kept = 0;
+      }
   };
   int i = first;
   for (; i + step < end; i += step) tile(i, std::true_type{});
@@ -170,10 +214,15 @@ __device__ inline void walk(const AttnArgs& a, int seq, int head, int len, int f
 
 // Few rows: a block takes 16 rows of a KV head at a time, its waves divide the tiles of a piece and join their sums in LDS.
 constexpr int kRows = 16;
-template <int D, int Fmt, bool Short>
+// Short: items are whole.  Scored: scores are kept for the weights (items may be divided).
+template <int D, int Fmt, bool Short, bool Scored>
 __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
+  static_assert(!(Short && Scored), "scores are kept of items on the line of tiles");
   constexpr int kStride = D + 4;                           // floats of a staged row: rows on different banks
-  __shared__ float stage[kWaves * kRows * kStride];
+  // a wave's sums for the others, or, before it writes them, its ring of scores
+  constexpr int kWaveFloats = Scored ? kRing : kRows * kStride;
+  static_assert(kWaveFloats >= kRows * kStride, "the sums fit");
+  __shared__ __align__(16) float stage[kWaves * kWaveFloats];
   __shared__ float stage_m[kWaves * kRows], stage_l[kWaves * kRows];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
   const int32_t me = blockIdx.x;
@@ -220,11 +269,11 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
     // the last tile that any of the rows sees
     const int rows = min(all_rows - rb * kRows, kRows), seen = z.len - z.n + (rb * kRows + rows - 1) / a.group;
     const int t_end = min(t1, seen < 0 ? 0 : seen / kTile + 1);
-    float* const scores = a.scores ? a.scores + ((int64_t)at0 - t0) * (16 * kTile) : nullptr;
-    walk<D, Fmt>(a, seq, head, z.len, t0 + wave, t_end, kWaves, q, last, first_seen, r, scores, rows);
-    if (scores)                                            // tiles of the piece that nobody sees
+    float* const scores = Scored ? a.scores + ((int64_t)at0 - t0) * (16 * kTile) : nullptr;
+    walk<D, Fmt, Scored>(a, seq, head, z.len, t0 + wave, t_end, kWaves, q, last, first_seen, r, scores, rows, stage + wave * kWaveFloats);
+    if constexpr (Scored)                                  // tiles of the piece that nobody sees
       for (int i = max(t_end, t0) + wave; i < t1; i += kWaves)
-        for (int j = lane; j < 16 * kTile; j += 64) scores[(int64_t)i * (16 * kTile) + j] = -INFINITY;
+        for (int j = lane; j < score_floats(rows); j += 64) scores[(int64_t)i * score_floats(rows) + j] = -INFINITY;
     r.l = sum_over_groups(r.l);
 
     const bool whole = t0 == 0 && t1 == tiles;
@@ -232,7 +281,7 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
     float* const slot = a.part + (int64_t)(2 * me + (t0 == 0 ? 1 : 0)) * slot_floats(D, kRows);
     if (g == 0) { stage_m[wave * kRows + n] = r.m; stage_l[wave * kRows + n] = r.l; }
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4*>(&stage[(wave * kRows + n) * kStride + 16 * i + 4 * g]) = r.o[i];
+    for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4*>(&stage[wave * kWaveFloats + n * kStride + 16 * i + 4 * g]) = r.o[i];
     __syncthreads();
     for (int j = threadIdx.x; j < rows * (D / 4); j += 256) {
       const int lr = j / (D / 4), ch = 4 * (j % (D / 4)), row = rb * kRows + lr;
@@ -244,7 +293,7 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
       for (int w = 0; w < kWaves; ++w) {
         const float f = __builtin_amdgcn_exp2f(stage_m[w * kRows + lr] - m);
         l += f * stage_l[w * kRows + lr];
-        o += f * *reinterpret_cast<const f32x4*>(&stage[(w * kRows + lr) * kStride + ch]);
+        o += f * *reinterpret_cast<const f32x4*>(&stage[w * kWaveFloats + lr * kStride + ch]);
       }
       if (whole) {
         const int tok = z.row0 + row / a.group, h = head * a.group + row % a.group;
@@ -343,7 +392,7 @@ __global__ __launch_bounds__(kWeighThreads, 2) void weigh_kernel(WeighArgs a) {
     const int key0 = tile * kTile, all_rows = z.n * a.group;
     // the first token that sees the tile's first key
     const int tok0 = max(key0 - (z.len - z.n), 0), rb0 = (int)((int64_t)tok0 * a.group / 16);
-    const TilePages at = pages_of(a, seq, z.len, tile);
+    const TilePages at = pages_of(a, z.len > 0 ? ask_pages(a, seq, z.len, tile) : TilePages{-1, -1}, z.len, tile);
     const TileScales sc = scales_of(a.c, head, at.v);
     // What the wave asks for a block of 16 rows ahead: queries through LDS, four lanes a row, so that a request is 64 bytes (operand rows straight from memory are 16 bytes a
     // request, and the requests bounded the kernel: a prompt of 4096 tokens, 8 heads, 48 us instead of 36), and the LSE of the lane's row n.
@@ -449,7 +498,12 @@ __global__ __launch_bounds__(kWeighThreads, 2) void weigh_kernel(WeighArgs a) {
   }
 }
 
-// The same from the scores that the attention kernel left (few rows): a wave takes four rows of a tile at a time, four keys a lane, and four tiles.
+// The same from the scores that the attention kernel left (few rows): a wave takes four rows of a tile at a time, which are 1 KB at one place, four keys a lane, and four tiles.  The sums
+// over a quad's four rows then go to the lanes in the order of the keys, so that weights are read and written 256 bytes at a time.
+__device__ inline float sum_of_quad(float x) {             // neighbours (1 0 3 2), then pairs (2 3 0 1)
+  x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0xb1, 0xf, 0xf, false));
+  return x + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x4e, 0xf, 0xf, false));
+}
 constexpr int kScoreTiles = 4 * kWaves;   // that a block works at once
 __global__ __launch_bounds__(256) void weigh_scores_kernel(AttnArgs a, int rows_of_block) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -470,30 +524,36 @@ __global__ __launch_bounds__(256) void weigh_scores_kernel(AttnArgs a, int rows_
     const int item = (at - base) / tiles, t0 = (at - base) % tiles, t1 = min(tiles, t0 + end - at);
     const int head = item / row_blocks, rb = item % row_blocks;
     // the rows of all blocks of a head add to the same weights: those of the first block's share do it, so that no two do
-    if (rb == 0) {
+    if (rb == 0 && z.len > 0) {
+      const int32_t* const table = a.s.pages + (int64_t)seq * a.s.max_pages;
       constexpr int kUnroll = kScoreTiles / kWaves;
-      const int sub = lane >> 4, i4 = (lane >> 2) & 3, g = lane & 3, key4 = 16 * g + 4 * i4;   // row of four, keys of the tile
+      // lane 16 i + 4 g + r holds row r of keys 16 g + 4 i ..; key 16 g + 4 i + k's sum is element k there
+      const int sub = lane & 3, from = 16 * ((lane >> 2) & 3) + 4 * (lane >> 4) + sub;
       for (int i = t0 + wave; i < t1; i += kWaves * kUnroll) {
-        // everything is asked for before anything is waited for: the first four rows' scores and LSE, the pages, then where the sums go (only the first 16 lanes' are used)
-        f32x4 s[kUnroll], got[kUnroll] = {}, sum[kUnroll];
-        float lse = 0.f;
+        // everything is asked for before anything is waited for: the first four rows' scores and LSE, the pages, then the weights so far
+        f32x4 s[kUnroll], got[kUnroll] = {};
+        float sum[kUnroll], lse = 0.f;
         auto rows_at = [&](int r0) {
           const int row = min(r0 + sub, all_rows - 1);
           lse = a.lse[(int64_t)(head * a.group + row % a.group) * a.s.n_rows + z.row0 + row / a.group];
-          const float* const s0 = a.scores + ((int64_t)base + ((int64_t)head * row_blocks + row / rows_of_block) * tiles) * (16 * kTile) + 256 * i4 + 16 * (row % rows_of_block) + 4 * g;
+          const int b = row / rows_of_block, floats = score_floats(min(all_rows - b * rows_of_block, rows_of_block));
+          const float* const s0 = a.scores + ((int64_t)base + ((int64_t)head * row_blocks + b) * tiles) * (16 * kTile) + score_at(row % rows_of_block) + 16 * (lane >> 2);
 #pragma unroll
-          for (int j = 0; j < kUnroll; ++j) s[j] = *reinterpret_cast<const f32x4*>(s0 + (int64_t)min(i + kWaves * j, t1 - 1) * (16 * kTile));
+          for (int j = 0; j < kUnroll; ++j) s[j] = *reinterpret_cast<const f32x4*>(s0 + (int64_t)min(i + kWaves * j, t1 - 1) * floats);
         };
         rows_at(0);
-        f32x4* to[kUnroll];
+        int32_t page[kUnroll];
+        float* to[kUnroll];
+#pragma unroll
+        for (int j = 0; j < kUnroll; ++j) page[j] = table[min((i + kWaves * j) * kTile + lane, z.len - 1) >> a.c.log_page];
 #pragma unroll
         for (int j = 0; j < kUnroll; ++j) {
-          const int key = (i + kWaves * j) * kTile + key4;
-          const int32_t p = sub == 0 && i + kWaves * j < t1 && key < z.len ? page_at(a.s, a.c, seq, key >> a.c.log_page) : -1;
-          to[j] = p < 0 ? nullptr : reinterpret_cast<f32x4*>(a.c.weight + block_of(a.c, p, head) * a.c.page + (key & (a.c.page - 1)));
+          const int key = (i + kWaves * j) * kTile + lane;
+          const bool there = (uint32_t)page[j] < (uint32_t)a.c.n_pages;
+          to[j] = a.c.weight + block_of(a.c, there ? page[j] : 0, head) * a.c.page + (key & (a.c.page - 1));
+          sum[j] = *to[j];
+          if (!there || i + kWaves * j >= t1 || key >= z.len) to[j] = nullptr;
         }
-#pragma unroll
-        for (int j = 0; j < kUnroll; ++j) sum[j] = to[j] ? *to[j] : f32x4{0, 0, 0, 0};
         for (int r0 = 0; r0 < all_rows; r0 += 4) {
           if (r0 > 0) rows_at(r0);
           const float lse2 = r0 + sub < all_rows && lse != -INFINITY ? lse * kLog2e : INFINITY;       // (else nothing is added)
@@ -503,15 +563,12 @@ __global__ __launch_bounds__(256) void weigh_scores_kernel(AttnArgs a, int rows_
             for (int k = 0; k < 4; ++k) got[j][k] += __builtin_amdgcn_exp2f(s[j][k] - lse2);
         }
 #pragma unroll
-        for (int j = 0; j < kUnroll; ++j)
-#pragma unroll
-          for (int k = 0; k < 4; ++k) got[j][k] = sum_over_groups(got[j][k]);
-#pragma unroll
         for (int j = 0; j < kUnroll; ++j) {
-          const int key = (i + kWaves * j) * kTile + key4;
 #pragma unroll
-          for (int k = 0; k < 4; ++k) sum[j][k] += key + k < z.len ? got[j][k] : 0.f;
-          if (to[j]) *to[j] = sum[j];
+          for (int k = 0; k < 4; ++k) got[j][k] = sum_of_quad(got[j][k]);
+          const float mine = sub < 2 ? (sub == 0 ? got[j][0] : got[j][1]) : (sub == 2 ? got[j][2] : got[j][3]);
+          const float all = __shfl(mine, from);
+          if (to[j]) *to[j] = sum[j] + all;
         }
       }
     }
@@ -549,8 +606,8 @@ template <int D, int Fmt>
 int launch_attn(const AttnArgs& a, const AttnPlan& p, hipStream_t st) {
   const dim3 grid(kBlocks), block(256);
   if (!p.keys) return launch_attn_rows(a, D, Fmt, p.whole, st);
-  if (p.whole) attn_kernel<D, Fmt, true><<<grid, block, 0, st>>>(a);
-  else attn_kernel<D, Fmt, false><<<grid, block, 0, st>>>(a);
+  auto kernel = p.whole ? attn_kernel<D, Fmt, true, false> : p.stored ? attn_kernel<D, Fmt, false, true> : attn_kernel<D, Fmt, false, false>;
+  kernel<<<grid, block, 0, st>>>(a);
   FCP_HIP_CHECK(hipGetLastError());
   if (!p.whole) {
     attn_merge_kernel<D><<<dim3(kBlocks * kMergeRows), block, 0, st>>>(a);
