@@ -27,7 +27,8 @@ struct AttnArgs {
 };
 
 // The line of the tiles of all items, and its division among blocks.  Sequence s has, for every KV head and every block of `rows` rows, all of its tiles (a sequence without
-// cached tokens one empty tile, which writes O = 0).  Short: an item is one place on the line, whatever its tiles, so that it lies in one block.
+// cached tokens one empty tile, which writes O = 0).  Lead: places before an item's first tile, for what a block does for an item whatever its tiles; kWhole: an item is one place on the
+// line, so that it lies in one block.
 // Places are 32-bit numbers: the host sees to it that there are fewer than 2^31.
 struct Line {
   int32_t total;                       // places
@@ -46,16 +47,21 @@ struct Line {
 };
 
 __device__ inline int32_t tiles_of(int len) { return max((len + kTile - 1) / kTile, 1); }
-template <bool Short> __device__ inline int32_t places_of(int len) { return Short ? 1 : tiles_of(len); }
-template <bool Short>
+constexpr int kWhole = -1;
+// Rows, first loads and the waves' meeting take a block about as long as four tiles.  Lead of 0 / 2 / 4 / 8, few rows: 64 sequences of up to 16384 tokens with weights 185 / 182 / 180 / 182 us, of
+// up to 4000 48.5 / 46.4 / 44.5 / 46.6, 16 of up to 8000 27.9 / 27.7 / 26.2 / 27.7, 5 of up to 2000 14.2 / 13.6 / 11.3 / 11.2; 64 of 4700 150 each.  0 / 2 / 4 / 6 / 10, many: 30 of up to 4000,
+// 40 new tokens 99 / 84 / 78 / 80 / 85, 8 of up to 16000, 100 new 155 / 153 / 149 / 148 / 152, 2 of up to 16385, 512 new 264 / 259 / 258 / 257 / 266.
+constexpr int kItemLead = 4;
+template <int Lead> __device__ inline int32_t places_of(int len) { return Lead == kWhole ? 1 : tiles_of(len) + Lead; }
+template <int Lead>
 __device__ inline int32_t cost_of(const SeqSizes& z, int hkv, int group, int rows) {
-  return z.n == 0 ? 0 : hkv * ((z.n * group - 1) / rows + 1) * places_of<Short>(z.len);
+  return z.n == 0 ? 0 : hkv * ((z.n * group - 1) / rows + 1) * places_of<Lead>(z.len);
 }
 
 // The sequence that holds the beginning of share `block` (blocks = 0: place `block` itself); seq = -1 if there is none.  Every thread of the block (256, 512) calls; a thread
 // looks at a run of sequences, all of which are asked for at once.  At most `blocks` shares, fewer where a share would have fewer than Least places.
 // Where cu_seqlens falls, rows would belong to several sequences and there could be more places than the host counted: then there is no work at all.
-template <bool Short, int Threads = 256, int Least = Short ? 1 : kLeastTiles>
+template <int Lead, int Threads = 256, int Least = Lead == kWhole ? 1 : kLeastTiles>
 static __device__ inline Line find_on_line(const SeqView& s, const CacheView& c, int group, int rows, int blocks, int block) {
   __shared__ int32_t sums[Threads / 64];
   __shared__ int32_t found[5];
@@ -64,7 +70,7 @@ static __device__ inline Line find_on_line(const SeqView& s, const CacheView& c,
   bool falls = false;
   for (int i = a; i < b; ++i) {
     falls |= s.cu[i + 1] < s.cu[i];
-    mine += cost_of<Short>(seq_sizes(s, i, c.page), c.hkv, group, rows);
+    mine += cost_of<Lead>(seq_sizes(s, i, c.page), c.hkv, group, rows);
   }
   falls = __ballot(falls);
   int32_t upto = wave_prefix_sum(mine);
@@ -84,7 +90,7 @@ static __device__ inline Line find_on_line(const SeqView& s, const CacheView& c,
   if (x >= 0 && x >= at && x < upto) {
     for (int i = a; i < b; ++i) {
       const SeqSizes z = seq_sizes(s, i, c.page);
-      const int32_t n = cost_of<Short>(z, c.hkv, group, rows);
+      const int32_t n = cost_of<Lead>(z, c.hkv, group, rows);
       if (x < at + n) {
         found[0] = i;
         found[1] = at;
@@ -104,6 +110,15 @@ static __device__ inline Line find_on_line(const SeqView& s, const CacheView& c,
   line.total = __builtin_amdgcn_readfirstlane(line.total);
   line.sharers = __builtin_amdgcn_readfirstlane(line.sharers);
   return line;
+}
+
+// A block's share of an item, from place `at` on (`from` places after the item's first) to place `end` at most: tiles first .. last - 1, and the places that they and the lead take.
+struct Piece { int32_t first, last, places; };
+template <int Lead>
+__device__ inline Piece piece_of(int32_t tiles, int32_t from, int32_t room) {
+  if (Lead == kWhole) return {0, tiles, 1};
+  const int32_t n = min(tiles + Lead - from, room);
+  return {max(from - Lead, 0), max(from + n - Lead, 0), n};
 }
 
 // An item that several blocks work: the block in which it begins says who it is and how many pieces it has; piece p lies in slot 2 (block + p), the first in slot

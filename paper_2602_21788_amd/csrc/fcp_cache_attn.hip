@@ -218,6 +218,7 @@ constexpr int kRows = 16;
 template <int D, int Fmt, bool Short, bool Scored>
 __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
   static_assert(!(Short && Scored), "scores are kept of items on the line of tiles");
+  constexpr int kLead = Short ? kWhole : kItemLead;
   constexpr int kStride = D + 4;                           // floats of a staged row: rows on different banks
   // a wave's sums for the others, or, before it writes them, its ring of scores
   constexpr int kWaveFloats = Scored ? kRing : kRows * kStride;
@@ -226,7 +227,7 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
   __shared__ float stage_m[kWaves * kRows], stage_l[kWaves * kRows];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
   const int32_t me = blockIdx.x;
-  const Line line = find_on_line<Short>(a.s, a.c, a.group, kRows, a.blocks, me);
+  const Line line = find_on_line<kLead>(a.s, a.c, a.group, kRows, a.blocks, me);
   Divided divided = {};
   int32_t at = 0, end = 0;
   if (line.seq >= 0) {
@@ -237,16 +238,17 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
   int32_t base = line.before;
   SeqSizes z = line.z;
   while (at < end) {
-    while (at >= base + cost_of<Short>(z, a.c.hkv, a.group, kRows)) {      // the next sequence with rows
-      base += cost_of<Short>(z, a.c.hkv, a.group, kRows);
+    while (at >= base + cost_of<kLead>(z, a.c.hkv, a.group, kRows)) {      // the next sequence with rows
+      base += cost_of<kLead>(z, a.c.hkv, a.group, kRows);
       z = seq_sizes(a.s, ++seq, a.c.page);
     }
     const int tiles = tiles_of(z.len), all_rows = z.n * a.group, row_blocks = (all_rows + kRows - 1) / kRows;
-    const int item = Short ? at - base : (at - base) / tiles, t0 = Short ? 0 : (at - base) % tiles;
-    const int t1 = Short ? tiles : min(tiles, t0 + end - at);
-    const int head = item / row_blocks, rb = item % row_blocks;
-    const int32_t at0 = at;
-    at += Short ? 1 : t1 - t0;
+    const int places = places_of<kLead>(z.len), item = (at - base) / places, from = (at - base) % places;
+    const Piece piece = piece_of<kLead>(tiles, from, end - at);
+    const int head = item / row_blocks, rb = item % row_blocks, t0 = piece.first, t1 = piece.last;
+    const int32_t item0 = at - from;
+    at += piece.places;
+    if (t0 == t1) continue;                                // (the item's lead alone)
 
     const int my_row = rb * kRows + n;
     const bool live = my_row < all_rows;
@@ -269,7 +271,7 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
     // the last tile that any of the rows sees
     const int rows = min(all_rows - rb * kRows, kRows), seen = z.len - z.n + (rb * kRows + rows - 1) / a.group;
     const int t_end = min(t1, seen < 0 ? 0 : seen / kTile + 1);
-    float* const scores = Scored ? a.scores + ((int64_t)at0 - t0) * (16 * kTile) : nullptr;
+    float* const scores = Scored ? a.scores + (int64_t)item0 * (16 * kTile) : nullptr;
     walk<D, Fmt, Scored>(a, seq, head, z.len, t0 + wave, t_end, kWaves, q, last, first_seen, r, scores, rows, stage + wave * kWaveFloats);
     if constexpr (Scored)                                  // tiles of the piece that nobody sees
       for (int i = max(t_end, t0) + wave; i < t1; i += kWaves)
@@ -277,7 +279,7 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
     r.l = sum_over_groups(r.l);
 
     const bool whole = t0 == 0 && t1 == tiles;
-    if (t0 == 0 && !whole) divided = {line.owner(at0 + tiles - 1) - me + 1, z.row0, all_rows, head, rb, {}};
+    if (t0 == 0 && !whole) divided = {line.owner(item0 + kItemLead + tiles - 1) - me + 1, z.row0, all_rows, head, rb, {}};
     float* const slot = a.part + (int64_t)(2 * me + (t0 == 0 ? 1 : 0)) * slot_floats(D, kRows);
     if (g == 0) { stage_m[wave * kRows + n] = r.m; stage_l[wave * kRows + n] = r.l; }
 #pragma unroll
@@ -377,15 +379,15 @@ __global__ __launch_bounds__(kWeighThreads, 2) void weigh_kernel(WeighArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
   // the line with one block of rows per KV head
   const int kAll = INT32_MAX;
-  const Line line = find_on_line<false, kWeighThreads>(a.s, a.c, 1, kAll, 0, blockIdx.x);
+  const Line line = find_on_line<0, kWeighThreads>(a.s, a.c, 1, kAll, 0, blockIdx.x);
   if (line.seq < 0) return;
   int seq = line.seq;
   int32_t base = line.before;
   SeqSizes z = line.z;
   for (int32_t u = blockIdx.x; u < line.total; u += gridDim.x) {
     __syncthreads();                   // (everybody has read the sums of the tile before)
-    while (u >= base + cost_of<false>(z, a.c.hkv, 1, kAll)) {
-      base += cost_of<false>(z, a.c.hkv, 1, kAll);
+    while (u >= base + cost_of<0>(z, a.c.hkv, 1, kAll)) {
+      base += cost_of<0>(z, a.c.hkv, 1, kAll);
       z = seq_sizes(a.s, ++seq, a.c.page);
     }
     const int tile = (u - base) / a.c.hkv, head = (u - base) % a.c.hkv;
@@ -508,7 +510,7 @@ constexpr int kScoreTiles = 4 * kWaves;   // that a block works at once
 __global__ __launch_bounds__(256) void weigh_scores_kernel(AttnArgs a, int rows_of_block) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int32_t me = blockIdx.x;
-  const Line line = find_on_line<false, 256, kScoreTiles>(a.s, a.c, a.group, rows_of_block, gridDim.x, me);
+  const Line line = find_on_line<kItemLead, 256, kScoreTiles>(a.s, a.c, a.group, rows_of_block, gridDim.x, me);
   if (line.seq < 0) return;
   int32_t at = line.begin(me);
   const int32_t end = line.begin(me + 1);
@@ -516,13 +518,14 @@ __global__ __launch_bounds__(256) void weigh_scores_kernel(AttnArgs a, int rows_
   int32_t base = line.before;
   SeqSizes z = line.z;
   while (at < end) {
-    while (at >= base + cost_of<false>(z, a.c.hkv, a.group, rows_of_block)) {
-      base += cost_of<false>(z, a.c.hkv, a.group, rows_of_block);
+    while (at >= base + cost_of<kItemLead>(z, a.c.hkv, a.group, rows_of_block)) {
+      base += cost_of<kItemLead>(z, a.c.hkv, a.group, rows_of_block);
       z = seq_sizes(a.s, ++seq, a.c.page);
     }
     const int tiles = tiles_of(z.len), all_rows = z.n * a.group, row_blocks = (all_rows + rows_of_block - 1) / rows_of_block;
-    const int item = (at - base) / tiles, t0 = (at - base) % tiles, t1 = min(tiles, t0 + end - at);
-    const int head = item / row_blocks, rb = item % row_blocks;
+    const int places = places_of<kItemLead>(z.len), item = (at - base) / places, from = (at - base) % places;
+    const Piece piece = piece_of<kItemLead>(tiles, from, end - at);
+    const int head = item / row_blocks, rb = item % row_blocks, t0 = piece.first, t1 = piece.last;
     // the rows of all blocks of a head add to the same weights: those of the first block's share do it, so that no two do
     if (rb == 0 && z.len > 0) {
       const int32_t* const table = a.s.pages + (int64_t)seq * a.s.max_pages;
@@ -537,7 +540,7 @@ __global__ __launch_bounds__(256) void weigh_scores_kernel(AttnArgs a, int rows_
           const int row = min(r0 + sub, all_rows - 1);
           lse = a.lse[(int64_t)(head * a.group + row % a.group) * a.s.n_rows + z.row0 + row / a.group];
           const int b = row / rows_of_block, floats = score_floats(min(all_rows - b * rows_of_block, rows_of_block));
-          const float* const s0 = a.scores + ((int64_t)base + ((int64_t)head * row_blocks + b) * tiles) * (16 * kTile) + score_at(row % rows_of_block) + 16 * (lane >> 2);
+          const float* const s0 = a.scores + ((int64_t)base + ((int64_t)head * row_blocks + b) * places) * (16 * kTile) + score_at(row % rows_of_block) + 16 * (lane >> 2);
 #pragma unroll
           for (int j = 0; j < kUnroll; ++j) s[j] = *reinterpret_cast<const f32x4*>(s0 + (int64_t)min(i + kWaves * j, t1 - 1) * floats);
         };
@@ -572,7 +575,7 @@ __global__ __launch_bounds__(256) void weigh_scores_kernel(AttnArgs a, int rows_
         }
       }
     }
-    at += t1 - t0;
+    at += piece.places;
   }
 }
 
@@ -594,7 +597,7 @@ AttnPlan plan_attn(const CacheView& c, int head_dim, int32_t n_seqs, int32_t max
   p.part_floats = (int64_t)2 * kBlocks * slot_floats(head_dim, p.rows);
   const int64_t tiles = max(((int64_t)max_pages * c.page + kTile - 1) / kTile, (int64_t)1);
   p.whole = !p.stored && tiles <= ((int64_t)n_seqs * c.hkv >= kBlocks ? 2 : 1) * kShortTiles;
-  p.places = tiles * c.hkv * (n_seqs + (int64_t)tq * group / p.rows);
+  p.places = (tiles + kItemLead) * c.hkv * (n_seqs + (int64_t)tq * group / p.rows);
   p.score_floats = p.stored ? p.places * 16 * kTile : 0;
   return p;
 }

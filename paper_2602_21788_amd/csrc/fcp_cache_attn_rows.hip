@@ -150,7 +150,8 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(AttnArgs a) {
   const int key_first = 16 * (n >> 2) + (n & 3), key_operand = Stage<D>::key_at(key_first, g), value_operand = Stage<D>::value_at(n, g);
   const int mine = 64 * lot_of<D>(wave) + lane, key_place = Stage<D>::key_at(mine / (D / 16), 2 * (mine % (D / 16))), value_place = Stage<D>::value_at(mine, 0);
   const int32_t me = blockIdx.x;
-  const Line line = find_on_line<Short>(a.s, a.c, a.group, kManyRows, a.blocks, me);
+  constexpr int kLead = Short ? kWhole : kItemLead;
+  const Line line = find_on_line<kLead>(a.s, a.c, a.group, kManyRows, a.blocks, me);
   Divided divided = {};
   int32_t at = 0, end = 0;
   if (line.seq >= 0) {
@@ -163,16 +164,17 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(AttnArgs a) {
   if (Fmt == kE4m3 && threadIdx.x < D) first_nan[1][threadIdx.x] = INT32_MAX;
   int parity = 1;                                          // of the items that see a tile
   while (at < end) {
-    while (at >= base + cost_of<Short>(z, a.c.hkv, a.group, kManyRows)) {  // the next sequence with rows
-      base += cost_of<Short>(z, a.c.hkv, a.group, kManyRows);
+    while (at >= base + cost_of<kLead>(z, a.c.hkv, a.group, kManyRows)) {  // the next sequence with rows
+      base += cost_of<kLead>(z, a.c.hkv, a.group, kManyRows);
       z = seq_sizes(a.s, ++seq, a.c.page);
     }
     const int tiles = tiles_of(z.len), all_rows = z.n * a.group, row_blocks = (all_rows + kManyRows - 1) / kManyRows;
-    const int item = Short ? at - base : (at - base) / tiles, t0 = Short ? 0 : (at - base) % tiles;
-    const int t1 = Short ? tiles : min(tiles, t0 + end - at);
-    const int head = item / row_blocks, rb = item % row_blocks;
-    const int32_t at0 = at;
-    at += Short ? 1 : t1 - t0;
+    const int places = places_of<kLead>(z.len), item = (at - base) / places, from = (at - base) % places;
+    const Piece piece = piece_of<kLead>(tiles, from, end - at);
+    const int head = item / row_blocks, rb = item % row_blocks, t0 = piece.first, t1 = piece.last;
+    const int32_t item0 = at - from;
+    at += piece.places;
+    if (t0 == t1) continue;                                // (the item's lead alone)
 
     bf16x8 q[kNB][D / 32];
     f32x4 o[kNB][D / 16];
@@ -322,7 +324,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(AttnArgs a) {
     for (int b = 0; b < kNB; ++b) l[b] = sum_over_groups(l[b]);
 
     const bool whole = t0 == 0 && t1 == tiles;
-    if (t0 == 0 && !whole) divided = {line.owner(at0 + tiles - 1) - me + 1, z.row0, all_rows, head, rb, {}};
+    if (t0 == 0 && !whole) divided = {line.owner(item0 + kItemLead + tiles - 1) - me + 1, z.row0, all_rows, head, rb, {}};
     float* const slot = a.part + (int64_t)(2 * me + (t0 == 0 ? 1 : 0)) * slot_floats(D, kManyRows);
 #pragma unroll
     for (int b = 0; b < kNB; ++b) {
