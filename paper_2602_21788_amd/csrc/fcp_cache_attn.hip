@@ -10,6 +10,8 @@
 //     of two) the probabilities.  The wave needs no LDS and no barrier in its loop.
 // All (sequence, KV head, block of rows, key tile) form one line, cut into equal pieces for the blocks: a long sequence is split over many blocks and short ones
 // share one, however ragged the lengths, which only the device knows.  The pieces of an item that does not lie in one block meet in a second launch.
+// One token over 131072, 32 heads on 8, e4m3, 269 MB: 57 to 60 us, 4.6 TB/s, where a large copy reaches 4.9 (the join is 7 of them, mostly its launch); 64 of lengths 819 to 16384, int8: 136 us,
+// 4.9 TB/s, with weights 180 (scores go out and come back).
 #include <type_traits>
 
 #include "fcp_cache_attn.h"

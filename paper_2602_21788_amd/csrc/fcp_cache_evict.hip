@@ -5,6 +5,7 @@
 // short tables.  One CU takes about 20 us to look at 131072 weights once, so long ones are cut into chunks: one launch counts, one lists each chunk's tokens with the k-th's
 // upper bits, one finds the border among those (every block for itself) and writes the chunk's part of the list.
 // The last launch moves the tokens: a wave per (new page, KV head, keys or values).
+// 4 sequences of up to 131072 tokens, 8 heads: choosing 7.5 + 10 + 18 us, chains of loads and barriers; moving 94 (the kernel says why).  4 of up to 600, 4 heads of 64 channels: 7 and 4.
 #include "fcp_cache.h"
 
 namespace fcp {
