@@ -317,35 +317,67 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
   if (!Short && threadIdx.x == 0) a.divided[me] = divided;
 }
 
-// Divided items: blocks_of_item blocks for each block in which one may begin, a row at a time, whose waves divide the pieces; two or one channel a lane.
+// Pieces p, p + kWaves, ... of a row joined by a wave, N asked for at a time; kCh channels a lane.  What was summed up so far follows the maximum.
+template <int D, int N>
+__device__ inline void join_pieces(const AttnArgs& a, int me, int pieces, int p, int row, float& m, float& l, float (&o)[D / 64]) {
+  constexpr int kCh = D / 64, kFloats = slot_floats(D, kRows);
+  const int ch = kCh * (threadIdx.x & 63);
+  for (; p < pieces; p += N * kWaves) {
+    float pm[N], pl[N], po[N][kCh];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float* const s = piece_slot(a, me, min(p + i * kWaves, pieces - 1), kFloats);
+      pm[i] = s[kRows * D + row];
+      pl[i] = s[kRows * (D + 1) + row];
+#pragma unroll
+      for (int c = 0; c < kCh; ++c) po[i][c] = s[row * D + ch + c];
+    }
+    float top = m;
+#pragma unroll
+    for (int i = 0; i < N; ++i) top = fmaxf(top, pm[i]);   // (the last one again where there are no more)
+    const float before = __builtin_amdgcn_exp2f(m - top);
+    m = top;
+    l *= before;
+#pragma unroll
+    for (int c = 0; c < kCh; ++c) o[c] *= before;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const bool there = p + i * kWaves < pieces;
+      const float f = __builtin_amdgcn_exp2f(pm[i] - m);
+      l += there ? f * pl[i] : 0.f;
+#pragma unroll
+      for (int c = 0; c < kCh; ++c) o[c] += there ? f * po[i][c] : 0.f;
+    }
+  }
+}
+
+// Divided items: blocks_of_item blocks for each block in which one may begin, a row at a time, whose waves divide the pieces.  Everything of eight pieces is asked for at once.
 template <int D>
 __global__ __launch_bounds__(256) void attn_merge_kernel(AttnArgs a, int blocks_of_item) {
-  constexpr int kCh = D / 64, kFloats = slot_floats(D, kRows);
-  __shared__ float sum_o[kWaves][D], sum_l[kWaves];
+  constexpr int kCh = D / 64;
+  __shared__ float sum_o[kWaves][D], sum_m[kWaves], sum_l[kWaves];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), me = blockIdx.x / blocks_of_item;
   const Divided d = a.divided[me];
   const int rows = min(d.all_rows - d.row_block * kRows, kRows);
   if (d.pieces == 0) return;
   for (int lr = blockIdx.x % blocks_of_item; lr < rows; lr += blocks_of_item) {
-    float m = kLow;
-    for (int p = lane; p < d.pieces; p += 64) m = fmaxf(m, piece_slot(a, me, p, kFloats)[kRows * D + lr]);
-    m = wave_maxf(m);
-    float l = 0.f, o[kCh] = {};
-#pragma unroll 8
-    for (int p = wave; p < d.pieces; p += kWaves) {
-      const float* s = piece_slot(a, me, p, kFloats);
-      const float f = __builtin_amdgcn_exp2f(s[kRows * D + lr] - m);
-      l += f * s[kRows * (D + 1) + lr];
-#pragma unroll
-      for (int i = 0; i < kCh; ++i) o[i] += f * s[lr * D + kCh * lane + i];
-    }
+    float m = kLow, l = 0.f, o[kCh] = {};
+    if (d.pieces <= kWaves) join_pieces<D, 1>(a, me, d.pieces, wave, lr, m, l, o);
+    else join_pieces<D, 8>(a, me, d.pieces, wave, lr, m, l, o);
 #pragma unroll
     for (int i = 0; i < kCh; ++i) sum_o[wave][kCh * lane + i] = o[i];
-    if (lane == 0) sum_l[wave] = l;
+    if (lane == 0) { sum_m[wave] = m; sum_l[wave] = l; }
     __syncthreads();
-    l = (sum_l[0] + sum_l[1]) + (sum_l[2] + sum_l[3]);
+    float f[kWaves];
+    m = fmaxf(fmaxf(sum_m[0], sum_m[1]), fmaxf(sum_m[2], sum_m[3]));
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) f[w] = __builtin_amdgcn_exp2f(sum_m[w] - m);
+    l = (f[0] * sum_l[0] + f[1] * sum_l[1]) + (f[2] * sum_l[2] + f[3] * sum_l[3]);
     const int row = d.row_block * kRows + lr, tok = d.row0 + row / a.group, h = d.head * a.group + row % a.group, ch = threadIdx.x;
-    if (ch < D) a.o[((int64_t)tok * a.hq + h) * D + ch] = (__bf16)(l == 0.f ? 0.f : ((sum_o[0][ch] + sum_o[1][ch]) + (sum_o[2][ch] + sum_o[3][ch])) * (1.f / l));
+    if (ch < D) {
+      const float sum = (f[0] * sum_o[0][ch] + f[1] * sum_o[1][ch]) + (f[2] * sum_o[2][ch] + f[3] * sum_o[3][ch]);
+      a.o[((int64_t)tok * a.hq + h) * D + ch] = (__bf16)(l == 0.f ? 0.f : sum * (1.f / l));
+    }
     if (ch == 0) a.lse[(int64_t)h * a.s.n_rows + tok] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
     __syncthreads();
   }
