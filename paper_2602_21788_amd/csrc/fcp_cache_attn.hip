@@ -31,21 +31,21 @@ struct RowState {
 struct TilePages { int32_t k, v; };
 // The table's entries, of a sequence with cached tokens (past the last token the last one's: a load under a condition is waited for at once, and everything before it too) ..
 template <class Args>
-__device__ inline TilePages ask_pages(const Args& a, int seq, int len, int tile) {
-  const int lane = threadIdx.x & 63, kk = tile * kTile + 16 * ((lane & 15) >> 2), vk = tile * kTile + 16 * (lane >> 4);
+__device__ inline TilePages ask_pages(const Args& a, int lane, int seq, int len, int tile) {
+  const int kk = tile * kTile + 16 * ((lane & 15) >> 2), vk = tile * kTile + 16 * (lane >> 4);
   const int32_t* const table = a.s.pages + (int64_t)seq * a.s.max_pages;
   return {table[min(kk, len - 1) >> a.c.log_page], table[min(vk, len - 1) >> a.c.log_page]};
 }
 // .. and what they say.
 template <class Args>
-__device__ inline TilePages pages_of(const Args& a, const TilePages& entries, int len, int tile) {
-  const int lane = threadIdx.x & 63, kk = tile * kTile + 16 * ((lane & 15) >> 2), vk = tile * kTile + 16 * (lane >> 4);
+__device__ inline TilePages pages_of(const Args& a, int lane, const TilePages& entries, int len, int tile) {
+  const int kk = tile * kTile + 16 * ((lane & 15) >> 2), vk = tile * kTile + 16 * (lane >> 4);
   const uint32_t n = a.c.n_pages;
   return {kk < len && (uint32_t)entries.k < n ? entries.k : -1, vk < len && (uint32_t)entries.v < n ? entries.v : -1};
 }
 template <int D>
-__device__ inline void load_keys(const CacheView& c, int head, int tile, int32_t page, u32x4 (&k)[4][D / 64]) {
-  const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4, kk = tile * kTile + 16 * (n >> 2) + (n & 3);
+__device__ inline void load_keys(const CacheView& c, int lane, int head, int tile, int32_t page, u32x4 (&k)[4][D / 64]) {
+  const int n = lane & 15, g = lane >> 4, kk = tile * kTile + 16 * (n >> 2) + (n & 3);
   const uint8_t* p = c.k + (block_of(c, max(page, 0), head) * c.page + (kk & (c.page - 1))) * D + 16 * g;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
@@ -53,8 +53,8 @@ __device__ inline void load_keys(const CacheView& c, int head, int tile, int32_t
     for (int j = 0; j < D / 64; ++j) k[i][j] = *reinterpret_cast<const u32x4*>(p + 4 * i * D + 64 * j);
 }
 template <int D>
-__device__ inline void load_values(const CacheView& c, int head, int tile, int32_t page, u32x4 (&v)[D / 16]) {
-  const int lane = threadIdx.x & 63, vk = tile * kTile + 16 * (lane >> 4);
+__device__ inline void load_values(const CacheView& c, int lane, int head, int tile, int32_t page, u32x4 (&v)[D / 16]) {
+  const int vk = tile * kTile + 16 * (lane >> 4);
   const uint8_t* p = c.v + (block_of(c, max(page, 0), head) * c.page + (vk & (c.page - 1))) * D + 16 * (lane & 15);
 #pragma unroll
   for (int i = 0; i < D / 16; ++i) v[i] = *reinterpret_cast<const u32x4*>(p + 256 * i);
@@ -68,32 +68,27 @@ __device__ inline TileScales scales_of(const CacheView& c, int head, int32_t pag
 }
 
 // S^T of one tile.
-template <int D, int Fmt>
-__device__ inline void scores_of(const u32x4 (&k)[4][D / 64], const bf16x8 (&q)[D / 32], f32x4 (&s)[4]) {
+template <int D, int Fmt, int NB>
+__device__ inline void scores_of(const u32x4 (&k)[4][D / 64], const bf16x8 (&q)[NB][D / 32], f32x4 (&s)[NB][4]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    s[i] = f32x4{0, 0, 0, 0};
 #pragma unroll
-    for (int j = 0; j < D / 64; ++j) {
-      const u32x4 w = k[i][j];
-      s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8<Fmt>(w[0], w[1]), q[2 * j], s[i], 0, 0, 0);
-      s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8<Fmt>(w[2], w[3]), q[2 * j + 1], s[i], 0, 0, 0);
+    for (int b = 0; b < NB; ++b) s[b][i] = f32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j) {
+      const bf16x8 x = decode8<Fmt>(k[i][j / 2][2 * (j % 2)], k[i][j / 2][2 * (j % 2) + 1]);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) s[b][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, q[b][j], s[b][i], 0, 0, 0);
     }
-    if (Fmt == kInt8) __builtin_amdgcn_sched_barrier(0);   // (left alone the compiler converts a tile's codes all at once, which takes 60 registers more and no less time)
+    if (Fmt == kInt8 || NB > 1) __builtin_amdgcn_sched_barrier(0);       // (left alone the compiler converts a tile's codes all at once, which takes 60 registers more and no less time)
   }
 }
 
-// Bytes that are NaN in FCP_CACHE_E4M3 as 0x38, the code of 1; 0 elsewhere.
-__device__ inline uint32_t nan_bytes(uint32_t w) {
-  const uint32_t x = (w & 0x7f7f7f7fu) + 0x01010101u;      // 0x80 exactly for 0x7f
-  return ((x & 0x80808080u) >> 7) * 0x38u;
-}
-
-// A tile that some row of the wave sees in part, values: codes past the last token are whatever the page holds, and 0 * NaN is NaN, so they are cleared.
-// Rare: a cached value that some rows do not see is NaN.  The rows that see it get NaN and the others do not: the NaN codes leave the product, and their number among
-// the keys that a row sees is counted by a product with 1.  live: cached tokens among the lane's 16.
+// A tile that some row of the wave sees in part, values: codes past the last token are whatever the page holds, and 0 * NaN is NaN, so they are cleared.  live: cached tokens among the
+// lane's 16, from key0 on.  Rare: one that some rows do not see is NaN.  It leaves the product, and the first such token of each channel is noted in first_nan (of the wave, prepared at
+// its first use; noted: there are some): the rows that see it get their NaN when the wave's tiles are done.
 template <int D, int Fmt>
-__device__ inline void clear_hidden(u32x4 (&v)[D / 16], int live, int last, RowState<D>& r) {
+__device__ inline void clear_hidden(u32x4 (&v)[D / 16], int live, int key0, int32_t* first_nan, bool& noted) {
   uint32_t odd = 0;
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
@@ -106,27 +101,23 @@ __device__ inline void clear_hidden(u32x4 (&v)[D / 16], int live, int last, RowS
     }
   }
   if (Fmt != kE4m3 || !__ballot(odd)) return;
+  const int lane = lane_id();                              // (formed here: the compiler would keep addresses that follow from it in registers, and spill)
+  if (!noted)
+#pragma unroll
+    for (int c = 0; c < D; c += 64) first_nan[c + lane] = INT32_MAX;
+  noted = true;
+  wave_exchange();
 #pragma unroll
   for (int i = 0; i < D / 16; ++i) {
-    __builtin_amdgcn_sched_barrier(0);                     // one channel tile after the other: this must not cost the common path registers
-    u32x4 bad;
+    int at = INT32_MAX;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      bad[w] = nan_bytes(v[i][w]);
-      v[i][w] &= ~(((bad[w] >> 3) & 0x01010101u) * 0xffu);
+    for (int w = 3; w >= 0; --w) {
+      const uint32_t nan = ((v[i][w] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;        // 0x80 exactly for 0x7f
+      if (nan) at = key0 + 4 * w + (__builtin_ctz(nan) >> 3);
+      v[i][w] &= ~((nan >> 7) * 0xffu);
     }
-    f32x4 count = {0, 0, 0, 0};
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      bf16x8 seen;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) seen[j] = (__bf16)(8 * h + j <= last ? 1.f : 0.f);
-      count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8<Fmt>(bad[2 * h], bad[2 * h + 1]), seen, count, 0, 0, 0);
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) r.o[i][j] = count[j] > 0.f ? NAN : r.o[i][j];
+    if (at != INT32_MAX) atomicMin(first_nan + 16 * i + (lane & 15), at);
   }
-  __builtin_amdgcn_sched_barrier(0);
 }
 
 // Scores kept of a tile of an item: [rows / 4][4 key tiles][4 groups][4 rows][4 keys], tiles next to each other in the item's part of the line (which has room for 16 rows each).
@@ -135,22 +126,25 @@ __device__ inline int score_floats(int rows) { return (rows + 3) / 4 * (4 * kTil
 constexpr int kRing = 16 * 4 * kTile;  // floats of a wave's ring: 16 tiles of four rows, 4 of 16
 __device__ inline int score_at(int row) { return row / 4 * (4 * kTile) + row % 4 * 4; }
 
-// Tiles first, first + step, ... below end for 16 rows of one KV head.  last_tok: last token that the lane's row sees; all_see: all rows see
+// Tiles first, first + step, ... below end for NB blocks of 16 rows of one KV head.  last_tok: last tokens that the lane's rows see; all_see: all rows see
 // the tokens up to it.  A tile's keys are asked for when the keys before them have become scores, its values when the values before them are in the sums: a wave always has 8 to 16 KB
 // on their way.  Page numbers are asked for a tile earlier, right behind keys: loads come back in order, so those behind values would be waited for with the values.
 // Scored: the scores are kept (score_rows rows), in `ring` until it is full: stores between the loads hold these up, and that costs less in few long bursts.  64 sequences of 4700 tokens,
 // int8, 32 heads on 8, 128 channels, with weights: 168 us, stored tile by tile 178; lengths from 819 to 16384: 186 and 188.
-template <int D, int Fmt, bool Scored>
-__device__ inline void walk(const AttnArgs& a, int seq, int head, int len, int first, int end, int step, const bf16x8 (&q)[D / 32], int last_tok, int all_see,
-                            RowState<D>& r, float* scores, int score_rows, float* ring) {
+template <int D, int Fmt, bool Scored, int NB>
+__device__ inline void walk(const AttnArgs& a, int seq, int head, int len, int first, int end, int step, const bf16x8 (&q)[NB][D / 32], const int (&last_tok)[NB], int all_see,
+                            RowState<D> (&r)[NB], float* scores, int score_rows, float* ring, int32_t* first_nan) {
   if (first >= end) return;
   const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   u32x4 k[4][D / 64], v[D / 16];
-  TilePages at = pages_of(a, ask_pages(a, seq, len, first), len, first), next = ask_pages(a, seq, len, first + step);
-  load_keys<D>(a.c, head, first, at.k, k);
+  TilePages at = pages_of(a, lane, ask_pages(a, lane, seq, len, first), len, first), next = ask_pages(a, lane, seq, len, first + step);
+  load_keys<D>(a.c, lane, head, first, at.k, k);
   TileScales sc = scales_of(a.c, head, at.v);
-  load_values<D>(a.c, head, first, at.v, v);
+  load_values<D>(a.c, lane, head, first, at.v, v);
   asm volatile("");                                        // (these loads and the loop's own must not become one at its head: the compiler then copies all that it carries, and spills)
+  // With 32 rows and e4m3 the registers are full: what follows from the lane is formed at every tile (64 sequences of up to 16384 tokens, 5 new: 176 us, else 186; int8 154 without, 159 with).
+  auto form_lane = [&] { return NB > 1 && Fmt == kE4m3 ? lane_id() : lane; };
+  bool noted = false;
   int kept = 0;                                            // tiles in the ring, the last of them at hand
   auto flush = [&](int last) {
     const int lots = score_floats(score_rows) / 256;       // of 1 KB a tile
@@ -163,43 +157,51 @@ __device__ inline void walk(const AttnArgs& a, int seq, int head, int len, int f
   };
   // (The last tile apart: loads under a condition would all be waited for where it ends.)
   auto tile = [&](int i, auto more) {
-    f32x4 s[4];
+    f32x4 s[NB][4];
     scores_of<D, Fmt>(k, q, s);
     TileScales sc_next = sc;
     TilePages at_next = at;
     if constexpr (more) {
-      at_next = pages_of(a, next, len, i + step);
-      load_keys<D>(a.c, head, i + step, at_next.k, k);
+      const int lane = form_lane();
+      at_next = pages_of(a, lane, next, len, i + step);
+      load_keys<D>(a.c, lane, head, i + step, at_next.k, k);
       sc_next = scales_of(a.c, head, at_next.v);
-      next = ask_pages(a, seq, len, i + 2 * step);
+      next = ask_pages(a, lane, seq, len, i + 2 * step);
     }
     const float c = a.scale * sc.k;
     const bool full = i * kTile + kTile - 1 <= all_see && !__ballot(at.v < 0);
     if (!full) {
-      const int key0 = i * kTile + 16 * g, last = at.v < 0 ? -1 : last_tok - key0;
-      mask_scores(s, last);
-      clear_hidden<D, Fmt>(v, at.v < 0 ? 0 : len - key0, last, r);
+      const int key0 = i * kTile + 16 * g;
+#pragma unroll
+      for (int b = 0; b < NB; ++b) mask_scores(s[b], at.v < 0 ? -1 : last_tok[b] - key0);
+      clear_hidden<D, Fmt>(v, at.v < 0 ? 0 : len - key0, key0, first_nan, noted);
     }
     if constexpr (Scored) {
       if (n < score_rows) {
         float* const to = ring + kept * score_floats(score_rows) + score_at(n) + 16 * g;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) *reinterpret_cast<f32x4*>(to + 64 * j) = s[j] * c;
+        for (int j = 0; j < 4; ++j) *reinterpret_cast<f32x4*>(to + 64 * j) = s[0][j] * c;
       }
       ++kept;
     }
-    raise_maximum<D>(s, c, r.o, r.m, r.l);
-    bf16x8 p[2];
-    probabilities_of(s, c, sc.v, r.m, r.l, p);
+    bf16x8 p[NB][2];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      raise_maximum<D>(s[b], c, r[b].o, r[b].m, r[b].l);
+      probabilities_of(s[b], c, sc.v, r[b].m, r[b].l, p[b]);
+    }
 #pragma unroll
     for (int d = 0; d < D / 16; ++d) {
-      const u32x4 w = v[d];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) r.o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8<Fmt>(w[2 * h], w[2 * h + 1]), p[h], r.o[d], 0, 0, 0);
-      if (Fmt == kInt8) __builtin_amdgcn_sched_barrier(0);
+      for (int h = 0; h < 2; ++h) {
+        const bf16x8 x = decode8<Fmt>(v[d][2 * h], v[d][2 * h + 1]);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) r[b].o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, p[b][h], r[b].o[d], 0, 0, 0);
+      }
+      if (Fmt == kInt8 || NB > 1) __builtin_amdgcn_sched_barrier(0);
     }
     if constexpr (more) {
-      load_values<D>(a.c, head, i + step, at_next.v, v);
+      load_values<D>(a.c, form_lane(), head, i + step, at_next.v, v);
       at = at_next;
       sc = sc_next;
     }
@@ -212,14 +214,26 @@ __device__ inline void walk(const AttnArgs& a, int seq, int head, int len, int f
   int i = first;
   for (; i + step < end; i += step) tile(i, std::true_type{});
   tile(i, std::false_type{});
+  if (Fmt == kE4m3 && noted) {
+    wave_exchange();
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int first_bad = first_nan[16 * d + 4 * g + j];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) r[b].o[d][j] = first_bad <= last_tok[b] ? NAN : r[b].o[d][j];
+      }
+    wave_exchange();
+  }
 }
 
-// Few rows: a block takes 16 rows of a KV head at a time, its waves divide the tiles of a piece and join their sums in LDS.
-constexpr int kRows = 16;
+// Few rows: a block takes 16 NB rows of a KV head at a time, its waves divide the tiles of a piece and join their sums in LDS.
 // Short: items are whole.  Scored: scores are kept for the weights (items may be divided).
-template <int D, int Fmt, bool Short, bool Scored>
+template <int D, int Fmt, bool Short, bool Scored, int NB>
 __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
-  static_assert(!(Short && Scored), "scores are kept of items on the line of tiles");
+  static_assert(!(Scored && (Short || NB > 1)), "scores are kept of items on the line of tiles, 16 rows of each");
+  constexpr int kRows = 16 * NB;
   constexpr int kLead = Short ? kWhole : kItemLead;
   constexpr int kStride = D + 4;                           // floats of a staged row: rows on different banks
   // a wave's sums for the others, or, before it writes them, its ring of scores
@@ -227,6 +241,7 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
   static_assert(kWaveFloats >= kRows * kStride, "the sums fit");
   __shared__ __align__(16) float stage[kWaves * kWaveFloats];
   __shared__ float stage_m[kWaves * kRows], stage_l[kWaves * kRows];
+  __shared__ int32_t first_nan[kWaves][Fmt == kE4m3 ? D : 1];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
   const int32_t me = blockIdx.x;
   const Line line = find_on_line<kLead>(a.s, a.c, a.group, kRows, a.blocks, me);
@@ -252,40 +267,49 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
     at += piece.places;
     if (t0 == t1) continue;                                // (the item's lead alone)
 
-    const int my_row = rb * kRows + n;
-    const bool live = my_row < all_rows;
-    const int my_tok = live ? my_row / a.group : 0, last = live ? z.len - z.n + my_tok : -1;     // last token that the lane's row sees
-    int first_seen = live ? last : INT32_MAX;              // least of them
+    int last[NB], first_seen = INT32_MAX;                  // last tokens that the lane's rows see; the first of those of all rows
+    bf16x8 q[NB][D / 32];
+    RowState<D> r[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const int my_row = rb * kRows + 16 * b + n;
+      const bool live = my_row < all_rows;
+      const int my_tok = live ? my_row / a.group : 0;
+      last[b] = live ? z.len - z.n + my_tok : -1;
+      first_seen = min(first_seen, live ? last[b] : INT32_MAX);
+      const __bf16* x = a.q + (int64_t)(z.row0 + my_tok) * a.q_row + (head * a.group + (live ? my_row % a.group : 0)) * D + 16 * g;
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j) {
+        const bf16x8 w = *reinterpret_cast<const bf16x8*>(x + 64 * (j / 2) + 8 * (j % 2)), zero = {};
+        q[b][j] = live ? w : zero;
+      }
+      r[b].m = kLow;
+      r[b].l = 0.f;
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) r[b].o[i] = f32x4{0, 0, 0, 0};
+    }
 #pragma unroll
     for (int d = 8; d > 0; d >>= 1) first_seen = min(first_seen, __shfl_xor(first_seen, d));
-    const __bf16* x = a.q + (int64_t)(z.row0 + my_tok) * a.q_row + (head * a.group + (live ? my_row % a.group : 0)) * D + 16 * g;
-    bf16x8 q[D / 32];
-#pragma unroll
-    for (int j = 0; j < D / 32; ++j) {
-      const bf16x8 w = *reinterpret_cast<const bf16x8*>(x + 64 * (j / 2) + 8 * (j % 2)), zero = {};
-      q[j] = live ? w : zero;
-    }
-    RowState<D> r;
-    r.m = kLow;
-    r.l = 0.f;
-#pragma unroll
-    for (int i = 0; i < D / 16; ++i) r.o[i] = f32x4{0, 0, 0, 0};
     // the last tile that any of the rows sees
     const int rows = min(all_rows - rb * kRows, kRows), seen = z.len - z.n + (rb * kRows + rows - 1) / a.group;
     const int t_end = min(t1, seen < 0 ? 0 : seen / kTile + 1);
     float* const scores = Scored ? a.scores + (int64_t)item0 * (16 * kTile) : nullptr;
-    walk<D, Fmt, Scored>(a, seq, head, z.len, t0 + wave, t_end, kWaves, q, last, first_seen, r, scores, rows, stage + wave * kWaveFloats);
+    walk<D, Fmt, Scored>(a, seq, head, z.len, t0 + wave, t_end, kWaves, q, last, first_seen, r, scores, rows, stage + wave * kWaveFloats, first_nan[wave]);
     if constexpr (Scored)                                  // tiles of the piece that nobody sees
       for (int i = max(t_end, t0) + wave; i < t1; i += kWaves)
         for (int j = lane; j < score_floats(rows); j += 64) scores[(int64_t)i * score_floats(rows) + j] = -INFINITY;
-    r.l = sum_over_groups(r.l);
 
     const bool whole = t0 == 0 && t1 == tiles;
     if (t0 == 0 && !whole) divided = {line.owner(item0 + kItemLead + tiles - 1) - me + 1, z.row0, all_rows, head, rb, {}};
     float* const slot = a.part + (int64_t)(2 * me + (t0 == 0 ? 1 : 0)) * slot_floats(D, kRows);
-    if (g == 0) { stage_m[wave * kRows + n] = r.m; stage_l[wave * kRows + n] = r.l; }
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4*>(&stage[wave * kWaveFloats + n * kStride + 16 * i + 4 * g]) = r.o[i];
+    for (int b = 0; b < NB; ++b) {
+      const int lr = 16 * b + n;
+      r[b].l = sum_over_groups(r[b].l);
+      if (g == 0) { stage_m[wave * kRows + lr] = r[b].m; stage_l[wave * kRows + lr] = r[b].l; }
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4*>(&stage[wave * kWaveFloats + lr * kStride + 16 * i + 4 * g]) = r[b].o[i];
+    }
     __syncthreads();
     for (int j = threadIdx.x; j < rows * (D / 4); j += 256) {
       const int lr = j / (D / 4), ch = 4 * (j % (D / 4)), row = rb * kRows + lr;
@@ -318,7 +342,7 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
 }
 
 // Pieces p, p + kWaves, ... of a row joined by a wave, N asked for at a time; kCh channels a lane.  What was summed up so far follows the maximum.
-template <int D, int N>
+template <int D, int kRows, int N>
 __device__ inline void join_pieces(const AttnArgs& a, int me, int pieces, int p, int row, float& m, float& l, float (&o)[D / 64]) {
   constexpr int kCh = D / 64, kFloats = slot_floats(D, kRows);
   const int ch = kCh * (threadIdx.x & 63);
@@ -352,7 +376,7 @@ __device__ inline void join_pieces(const AttnArgs& a, int me, int pieces, int p,
 }
 
 // Divided items: blocks_of_item blocks for each block in which one may begin, a row at a time, whose waves divide the pieces.  Everything of eight pieces is asked for at once.
-template <int D>
+template <int D, int kRows>
 __global__ __launch_bounds__(256) void attn_merge_kernel(AttnArgs a, int blocks_of_item) {
   constexpr int kCh = D / 64;
   __shared__ float sum_o[kWaves][D], sum_m[kWaves], sum_l[kWaves];
@@ -362,8 +386,8 @@ __global__ __launch_bounds__(256) void attn_merge_kernel(AttnArgs a, int blocks_
   if (d.pieces == 0) return;
   for (int lr = blockIdx.x % blocks_of_item; lr < rows; lr += blocks_of_item) {
     float m = kLow, l = 0.f, o[kCh] = {};
-    if (d.pieces <= kWaves) join_pieces<D, 1>(a, me, d.pieces, wave, lr, m, l, o);
-    else join_pieces<D, 8>(a, me, d.pieces, wave, lr, m, l, o);
+    if (d.pieces <= kWaves) join_pieces<D, kRows, 1>(a, me, d.pieces, wave, lr, m, l, o);
+    else join_pieces<D, kRows, 8>(a, me, d.pieces, wave, lr, m, l, o);
 #pragma unroll
     for (int i = 0; i < kCh; ++i) sum_o[wave][kCh * lane + i] = o[i];
     if (lane == 0) { sum_m[wave] = m; sum_l[wave] = l; }
@@ -427,7 +451,7 @@ __global__ __launch_bounds__(kWeighThreads, 2) void weigh_kernel(WeighArgs a) {
     const int key0 = tile * kTile, all_rows = z.n * a.group;
     // the first token that sees the tile's first key
     const int tok0 = max(key0 - (z.len - z.n), 0), rb0 = (int)((int64_t)tok0 * a.group / 16);
-    const TilePages at = pages_of(a, z.len > 0 ? ask_pages(a, seq, z.len, tile) : TilePages{-1, -1}, z.len, tile);
+    const TilePages at = pages_of(a, lane, z.len > 0 ? ask_pages(a, lane, seq, z.len, tile) : TilePages{-1, -1}, z.len, tile);
     const TileScales sc = scales_of(a.c, head, at.v);
     // What the wave asks for a block of 16 rows ahead: queries through LDS, four lanes a row, so that a request is 64 bytes (operand rows straight from memory are 16 bytes a
     // request, and the requests bounded the kernel: a prompt of 4096 tokens, 8 heads, 48 us instead of 36), and the LSE of the lane's row n.
@@ -455,7 +479,7 @@ __global__ __launch_bounds__(kWeighThreads, 2) void weigh_kernel(WeighArgs a) {
     bf16x8 k[4][D / 32];
     {
       u32x4 raw[4][D / 64];
-      load_keys<D>(a.c, head, tile, at.k, raw);
+      load_keys<D>(a.c, lane, head, tile, at.k, raw);
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -533,7 +557,7 @@ __global__ __launch_bounds__(kWeighThreads, 2) void weigh_kernel(WeighArgs a) {
   }
 }
 
-// The same from the scores that the attention kernel left (few rows): a wave takes four rows of a tile at a time, which are 1 KB at one place, four keys a lane, and four tiles.  The sums
+// The same from the scores that the attention kernel left (blocks of 16 rows): a wave takes four rows of a tile at a time, which are 1 KB at one place, four keys a lane, and four tiles.  The sums
 // over a quad's four rows then go to the lanes in the order of the keys, so that weights are read and written 256 bytes at a time.
 __device__ inline float sum_of_quad(float x) {             // neighbours (1 0 3 2), then pairs (2 3 0 1)
   x += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0xb1, 0xf, 0xf, false));
@@ -619,14 +643,15 @@ __global__ __launch_bounds__(256) void weigh_scores_kernel(AttnArgs a, int rows_
 // KV heads, not divided / divided: 18.7 / 33.1 us; of up to 2000 31.7 / 37.2; but of up to 4000 63.7 / 54.0, and 16 sequences of up to 2000 23.4 / 19.4.
 constexpr int kShortTiles = 16;
 
-// How a call is worked.  Up to 16 rows per sequence and KV head on average: a block of 16 rows whose waves divide the keys; more: 128 rows, a wave 32.
-struct AttnPlan { int rows; bool keys; bool stored; bool whole; int64_t part_floats, score_floats, places; };
+// How a call is worked.  Up to 16 or 32 rows per sequence and KV head on average: a block of as many rows, whose waves divide the keys; more: 128 rows, a wave 32.  64 sequences of up to 16384
+// tokens, int8, 32 heads on 8, 5 new tokens each (20 rows): 32 rows a block 154 us, 128 rows 252; of up to 1000 21 / 44; 8 of up to 8000 28 / 40.
+struct AttnPlan { int rows; bool stored; bool whole; int64_t part_floats, score_floats, places; };
 AttnPlan plan_attn(const CacheView& c, int head_dim, int32_t n_seqs, int32_t max_pages, int32_t tq, int32_t hq, bool weigh) {
   const int group = hq / c.hkv;
   AttnPlan p;
-  p.keys = (int64_t)tq * group <= (int64_t)16 * n_seqs;
-  p.rows = p.keys ? kRows : kManyRows;
-  p.stored = weigh && p.keys;
+  const int64_t all_rows = (int64_t)tq * group;
+  p.rows = all_rows <= (int64_t)16 * n_seqs ? 16 : all_rows <= (int64_t)32 * n_seqs ? 32 : kManyRows;
+  p.stored = weigh && p.rows == 16;
   p.part_floats = (int64_t)2 * kBlocks * slot_floats(head_dim, p.rows);
   const int64_t tiles = max(((int64_t)max_pages * c.page + kTile - 1) / kTile, (int64_t)1);
   p.whole = !p.stored && tiles <= ((int64_t)n_seqs * c.hkv >= kBlocks ? 2 : 1) * kShortTiles;
@@ -641,16 +666,18 @@ size_t part_bytes(const AttnPlan& p) { return pad_to((size_t)p.part_floats * 4, 
 template <int D, int Fmt>
 int launch_attn(const AttnArgs& a, const AttnPlan& p, hipStream_t st) {
   const dim3 grid(kBlocks), block(256);
-  if (!p.keys) return launch_attn_rows(a, D, Fmt, p.whole, st);
-  auto kernel = p.whole ? attn_kernel<D, Fmt, true, false> : p.stored ? attn_kernel<D, Fmt, false, true> : attn_kernel<D, Fmt, false, false>;
+  if (p.rows == kManyRows) return launch_attn_rows(a, D, Fmt, p.whole, st);
+  auto kernel = p.rows == 32 ? (p.whole ? attn_kernel<D, Fmt, true, false, 2> : attn_kernel<D, Fmt, false, false, 2>)
+                             : p.whole ? attn_kernel<D, Fmt, true, false, 1> : p.stored ? attn_kernel<D, Fmt, false, true, 1> : attn_kernel<D, Fmt, false, false, 1>;
   kernel<<<grid, block, 0, st>>>(a);
   FCP_HIP_CHECK(hipGetLastError());
   if (!p.whole) {
-    // A block for each row that an item has on average, but 4 at least and 16 (all) at most.  4 / 8 / 16 blocks: 64 sequences of up to 4000 tokens, 4 rows 42.9 / 44.7 / 47.0 us; 16 of up to
+    // A block for each row that an item has on average, but 4 at least.  4 / 8 / 16 blocks: 64 sequences of up to 4000 tokens, 4 rows 42.9 / 44.7 / 47.0 us; 16 of up to
     // 8000, 16 rows 21.3 / 16.6 / 14.2.
     const int64_t rows = ((int64_t)a.s.n_rows * a.group + a.s.n_seqs - 1) / a.s.n_seqs;
-    const int of_item = rows <= 4 ? 4 : rows <= 8 ? 8 : kRows;
-    attn_merge_kernel<D><<<dim3((unsigned)(kBlocks * of_item)), block, 0, st>>>(a, of_item);
+    const int of_item = rows <= 4 ? 4 : rows <= 8 ? 8 : rows <= 16 ? 16 : 32;
+    auto merge = p.rows == 32 ? attn_merge_kernel<D, 32> : attn_merge_kernel<D, 16>;
+    merge<<<dim3((unsigned)(kBlocks * of_item)), block, 0, st>>>(a, of_item);
     FCP_HIP_CHECK(hipGetLastError());
   }
   if (p.stored) {

@@ -558,3 +558,62 @@ def test_pages_past_the_32nd_bit(fmt):
         del cache
     assert all(torch.equal(a, b) for a, b in zip(*results))
     assert float(results[0][8].sum()) > 100 and not torch.isnan(results[0][0].float()).any()
+
+
+SEVERAL = [  # P, D, hq, hkv, kv_len, news: 17 to 32 rows of a KV head per sequence on average, more and fewer in some
+    (16, 64, 8, 2, [100, 37], [7, 4]), (64, 128, 16, 1, [1300], [2]), (32, 128, 8, 1, [2500, 40, 0, 700], [3, 2, 1, 4]), (128, 64, 24, 1, [5, 900], [1, 1]),
+    (64, 128, 8, 2, [150, 64, 1], [15, 3, 1]), (16, 128, 8, 8, [600, 19, 5], [32, 21, 9]), (32, 64, 40, 8, [1100, 1090], [5, 6])]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("weigh", [False, True])
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("P,D,hq,hkv,kv_len,news", SEVERAL)
+def test_attention_of_several_tokens(P, D, hq, hkv, kv_len, news, fmt, weigh):
+    assert 16 < sum(news) * hq / hkv / len(news) <= 32
+    ref, cache, pages, cu, q, scale = attn_case(P, D, hq, hkv, kv_len, news, fmt, seed=7)
+    got = run_attn(cache, q, cu, kv_len, pages, scale, weigh)
+    want = ref.attn(q, cu, kv_len, pages, scale)
+    eps = check_attn(got, want)
+    w = R.check_content(cache, ref)
+    if weigh:
+        check_weight(w, ref.weight, want[2], eps, max(news) * hq // hkv)
+    else:
+        assert np.array_equal(w, ref.weight.astype(np.float32))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n", [90, 1500])
+@pytest.mark.parametrize("news", [1, 5, 12])
+def test_nan_values_reach_only_the_rows_that_see_them(D, n, news):
+    """NaN in values of the last tokens, in several channels and tiles' waves, and past the last token; short tables, and long ones whose items are divided."""
+    ref, cache, pages, cu, q, scale = attn_case(64, D, 4, 2, [n, n - 7], [news, news], "e4m3", seed=3)
+    for s, length in ((0, n), (1, n - 7)):
+        ref.v[pages[s, (length - 1) // 64], :, (length - 1) % 64 + 1:] = 127
+        for back, head, channel in ((1, 0, 3), (2, 1, 17), (1, 1, 40), (5, 1, 40), (11, 0, 63)):
+            t = length - back
+            ref.v[pages[s, t // 64], head, t % 64, channel] = 255 if back % 2 else 127
+    import torch
+    cache = R.to_device(ref, torch, B)
+    got = run_attn(cache, q, cu, [n, n - 7], pages, scale, False)
+    want = ref.attn(q, cu, [n, n - 7], pages, scale)
+    assert np.isnan(want[0]).any() and (news == 1 or not np.isnan(want[0][:, 0, 3]).all())
+    check_attn(got, want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("news", [1, 5])
+@pytest.mark.parametrize("hkv", [1, 4])
+def test_nothing_is_written_past_scratch(news, hkv):
+    """Scratch of exactly the size that is asked for, in a longer tensor whose other bytes stay."""
+    import torch
+    kv_len = [1000, 64, 1, 0, 1999]
+    ref, cache, pages, cu, q, scale = attn_case(32, 64, 4, hkv, kv_len, [news] * 5, "int8", seed=5)
+    for which, weigh in ((B.FCP_SCRATCH_CACHE_ATTN, False), (B.FCP_SCRATCH_CACHE_WEIGH, True)):
+        n = B.fcp_cache_scratch_bytes(which, cache, 5, pages.shape[1], q.shape[0], 4)
+        scratch = torch.full((n + 65536,), 77, dtype=torch.uint8, device="cuda")
+        o, lse = torch.empty(q.shape, dtype=torch.bfloat16, device="cuda"), torch.empty(4, q.shape[0], device="cuda")
+        B.fcp_cache_attn(cache, dev_bf16(q), dev(cu), dev(kv_len), dev(pages), scale, o, lse, scratch[:n], weigh=weigh)
+        assert (scratch[n:] == 77).all()
+        check_attn((o.double().cpu().numpy(), lse.double().cpu().numpy()), ref.attn(q, cu, kv_len, pages, scale))
