@@ -643,14 +643,15 @@ __global__ __launch_bounds__(256) void weigh_scores_kernel(AttnArgs a, int rows_
 // KV heads, not divided / divided: 18.7 / 33.1 us; of up to 2000 31.7 / 37.2; but of up to 4000 63.7 / 54.0, and 16 sequences of up to 2000 23.4 / 19.4.
 constexpr int kShortTiles = 16;
 
-// How a call is worked.  Up to 16 or 32 rows per sequence and KV head on average: a block of as many rows, whose waves divide the keys; more: 128 rows, a wave 32.  64 sequences of up to 16384
-// tokens, int8, 32 heads on 8, 5 new tokens each (20 rows): 32 rows a block 154 us, 128 rows 252; of up to 1000 21 / 44; 8 of up to 8000 28 / 40.
+// How a call is worked.  Up to 16 or 32 rows per sequence and KV head on average: a block of as many rows, whose waves divide the keys; more: 64 or 128 rows, which its waves divide.
+// 64 sequences of up to 16384 tokens, int8, 32 heads on 8: 5 new tokens each (20 rows), 32 rows a block 154 us, 128 rows 252; 16 new (64 rows), 64 rows a block 221 us, 128 rows 262.  Of up
+// to 1000: 21 / 44, 38 / 46; 8 of up to 8000: 28 / 40, 39 / 45.
 struct AttnPlan { int rows; bool stored; bool whole; int64_t part_floats, score_floats, places; };
 AttnPlan plan_attn(const CacheView& c, int head_dim, int32_t n_seqs, int32_t max_pages, int32_t tq, int32_t hq, bool weigh) {
   const int group = hq / c.hkv;
   AttnPlan p;
   const int64_t all_rows = (int64_t)tq * group;
-  p.rows = all_rows <= (int64_t)16 * n_seqs ? 16 : all_rows <= (int64_t)32 * n_seqs ? 32 : kManyRows;
+  p.rows = all_rows <= (int64_t)16 * n_seqs ? 16 : all_rows <= (int64_t)32 * n_seqs ? 32 : all_rows <= (int64_t)64 * n_seqs ? kManyRows / 2 : kManyRows;
   p.stored = weigh && p.rows == 16;
   p.part_floats = (int64_t)2 * kBlocks * slot_floats(head_dim, p.rows);
   const int64_t tiles = max(((int64_t)max_pages * c.page + kTile - 1) / kTile, (int64_t)1);
@@ -666,7 +667,7 @@ size_t part_bytes(const AttnPlan& p) { return pad_to((size_t)p.part_floats * 4, 
 template <int D, int Fmt>
 int launch_attn(const AttnArgs& a, const AttnPlan& p, hipStream_t st) {
   const dim3 grid(kBlocks), block(256);
-  if (p.rows == kManyRows) return launch_attn_rows(a, D, Fmt, p.whole, st);
+  if (p.rows > 32) return launch_attn_rows(a, D, Fmt, p.rows, p.whole, st);
   auto kernel = p.rows == 32 ? (p.whole ? attn_kernel<D, Fmt, true, false, 2> : attn_kernel<D, Fmt, false, false, 2>)
                              : p.whole ? attn_kernel<D, Fmt, true, false, 1> : p.stored ? attn_kernel<D, Fmt, false, true, 1> : attn_kernel<D, Fmt, false, false, 1>;
   kernel<<<grid, block, 0, st>>>(a);

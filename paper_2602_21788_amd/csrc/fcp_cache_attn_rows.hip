@@ -1,8 +1,8 @@
 // Attention over the paged 8-bit cache for many rows: pieces of prompts, or several new tokens of many query heads.
 //
-// A block takes 128 rows of a KV head's group at a time, a wave 32 of them, against tiles of 64 keys.  The products and the exponentials bound it (4 D flops a pair; an exponential
+// A block takes 128 rows (or 64, where there are no more) of a KV head's group at a time, a wave 32 (16) of them, against tiles of 64 keys.  The products and the exponentials bound it (4 D flops a pair; an exponential
 // takes as long as 64 flops of the matrix units per lane), so the codes must not become bf16 in every wave: a tile's codes come in whole lines, 32 a thread, become bf16 (exact) and
-// go to LDS, from which the waves read the operands of the 16 x 16 x 32 instructions, each for two blocks of 16 rows.  Operand rows straight from memory would be requests of 16 bytes
+// go to LDS, from which the waves read the operands of the 16 x 16 x 32 instructions, each for all of its rows.  Operand rows straight from memory would be requests of 16 bytes
 // a lane, a quarter of a line's rate, in every wave.  The keys' scale is taken with the scores, the values' with the codes.
 // A step has two streams: the next tile's scores with this tile's exponentials, and this tile's product with the values with the conversion of codes for the tiles after; the matrix
 // units and the others work at once, and operands from LDS are asked for four ahead.  One barrier a step.  Two blocks per CU: a wave has 256 registers, all in use.
@@ -14,8 +14,6 @@
 
 namespace fcp {
 namespace {
-
-constexpr int kNB = 2;                 // blocks of 16 rows of a wave
 
 // LDS of a stage: keys as rows of D channels, values as rows (channels) of 64 keys, in chunks of 8 bf16 whose places in a row are permuted so that what is read or written at once
 // lies on different banks.  That is 16 lanes, but not neighbours: 0 to 3 and 12 to 15 of one group of 16 with 4 to 11 of the next, so both groups' chunks count.  Values: chunk g + 4 u
@@ -139,8 +137,10 @@ __device__ inline void stream_operands(Read read, Multiply multiply) {
   }
 }
 
-template <int D, int Fmt, bool Short>
+// kNB: blocks of 16 rows of a wave.
+template <int D, int Fmt, bool Short, int kNB>
 __global__ __launch_bounds__(256, 2) void attn_rows_kernel(AttnArgs a) {
+  constexpr int kRows = 64 * kNB;
   typedef bf16x8 __attribute__((may_alias)) chunk;
   extern __shared__ __align__(256) unsigned char lds[];    // two stages
   __shared__ float key_scale[4][4];                        // [tile][group of 16 keys]
@@ -151,7 +151,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(AttnArgs a) {
   const int mine = 64 * lot_of<D>(wave) + lane, key_place = Stage<D>::key_at(mine / (D / 16), 2 * (mine % (D / 16))), value_place = Stage<D>::value_at(mine, 0);
   const int32_t me = blockIdx.x;
   constexpr int kLead = Short ? kWhole : kItemLead;
-  const Line line = find_on_line<kLead>(a.s, a.c, a.group, kManyRows, a.blocks, me);
+  const Line line = find_on_line<kLead>(a.s, a.c, a.group, kRows, a.blocks, me);
   Divided divided = {};
   int32_t at = 0, end = 0;
   if (line.seq >= 0) {
@@ -164,11 +164,11 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(AttnArgs a) {
   if (Fmt == kE4m3 && threadIdx.x < D) first_nan[1][threadIdx.x] = INT32_MAX;
   int parity = 1;                                          // of the items that see a tile
   while (at < end) {
-    while (at >= base + cost_of<kLead>(z, a.c.hkv, a.group, kManyRows)) {  // the next sequence with rows
-      base += cost_of<kLead>(z, a.c.hkv, a.group, kManyRows);
+    while (at >= base + cost_of<kLead>(z, a.c.hkv, a.group, kRows)) {  // the next sequence with rows
+      base += cost_of<kLead>(z, a.c.hkv, a.group, kRows);
       z = seq_sizes(a.s, ++seq, a.c.page);
     }
-    const int tiles = tiles_of(z.len), all_rows = z.n * a.group, row_blocks = (all_rows + kManyRows - 1) / kManyRows;
+    const int tiles = tiles_of(z.len), all_rows = z.n * a.group, row_blocks = (all_rows + kRows - 1) / kRows;
     const int places = places_of<kLead>(z.len), item = (at - base) / places, from = (at - base) % places;
     const Piece piece = piece_of<kLead>(tiles, from, end - at);
     const int head = item / row_blocks, rb = item % row_blocks, t0 = piece.first, t1 = piece.last;
@@ -182,7 +182,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(AttnArgs a) {
     int last[kNB];                                         // last token that the lane's row sees
 #pragma unroll
     for (int b = 0; b < kNB; ++b) {
-      const int row = rb * kManyRows + (wave * kNB + b) * 16 + n;
+      const int row = rb * kRows + (wave * kNB + b) * 16 + n;
       const bool there = row < all_rows;
       const int tok = there ? row / a.group : 0;
       last[b] = there ? z.len - z.n + tok : -1;
@@ -198,8 +198,8 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(AttnArgs a) {
       for (int i = 0; i < D / 16; ++i) o[b][i] = f32x4{0, 0, 0, 0};
     }
     // all of the block's rows see the tokens up to all_see; tiles from t_end on nobody sees
-    const int rows = min(all_rows - rb * kManyRows, kManyRows), all_see = z.len - z.n + rb * kManyRows / a.group;
-    const int seen = z.len - z.n + (rb * kManyRows + rows - 1) / a.group;
+    const int rows = min(all_rows - rb * kRows, kRows), all_see = z.len - z.n + rb * kRows / a.group;
+    const int seen = z.len - z.n + (rb * kRows + rows - 1) / a.group;
     const int t_end = min(t1, seen < 0 ? 0 : seen / kTile + 1);
     if (t0 < t_end) {
       // Tile t's scores are formed a step ahead, so that its exponentials and the products for the next scores are one stream of instructions, and so are its product with the values
@@ -277,7 +277,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(AttnArgs a) {
         bf16x8 p[kNB][2];
         scores(t + 1, s_next, [&](int i) {
 #pragma unroll
-          for (int j = 256 / D * i; j < 256 / D * (i + 1); ++j) {
+          for (int j = 128 * kNB / D * i; j < 128 * kNB / D * (i + 1); ++j) {
             const int b = j / 16, x = j % 16;
             const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][x / 4][x % 4], c, -m[b]));
             l[b] += e;
@@ -325,14 +325,14 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(AttnArgs a) {
 
     const bool whole = t0 == 0 && t1 == tiles;
     if (t0 == 0 && !whole) divided = {line.owner(item0 + kItemLead + tiles - 1) - me + 1, z.row0, all_rows, head, rb, {}};
-    float* const slot = a.part + (int64_t)(2 * me + (t0 == 0 ? 1 : 0)) * slot_floats(D, kManyRows);
+    float* const slot = a.part + (int64_t)(2 * me + (t0 == 0 ? 1 : 0)) * slot_floats(D, kRows);
 #pragma unroll
     for (int b = 0; b < kNB; ++b) {
-      const int lr = (wave * kNB + b) * 16 + n, row = rb * kManyRows + lr;
+      const int lr = (wave * kNB + b) * 16 + n, row = rb * kRows + lr;
       if (!whole) {                                        // sums as they lie in the registers: the merge divides them the same way
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4*>(slot + (((wave * kNB + b) * (D / 16) + i) * 64 + lane) * 4) = o[b][i];
-        if (g == 0) { slot[kManyRows * D + lr] = m[b]; slot[kManyRows * (D + 1) + lr] = l[b]; }
+        if (g == 0) { slot[kRows * D + lr] = m[b]; slot[kRows * (D + 1) + lr] = l[b]; }
       } else if (row < all_rows) {
         const int tok = z.row0 + row / a.group, h = head * a.group + row % a.group;
         const float inv = l[b] == 0.f ? 0.f : 1.f / l[b];
@@ -352,16 +352,16 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(AttnArgs a) {
 }
 
 // Divided items: a block per (block in which one begins, 16 rows), four channels of a row a thread, in the order in which the sums lie.
-template <int D>
+template <int D, int kRows>
 __global__ __launch_bounds__(256) void attn_rows_merge_kernel(AttnArgs a) {
-  constexpr int kFloats = slot_floats(D, kManyRows);
+  constexpr int kFloats = slot_floats(D, kRows);
   const int me = blockIdx.x, part = blockIdx.y, lane = threadIdx.x & 63;
   const Divided d = a.divided[me];
-  const int lr = part * 16 + (lane & 15), row = d.row_block * kManyRows + lr;
+  const int lr = part * 16 + (lane & 15), row = d.row_block * kRows + lr;
   if (d.pieces == 0 || row >= d.all_rows) return;
   float m = kLow;
 #pragma unroll 4
-  for (int p = 0; p < d.pieces; ++p) m = fmaxf(m, piece_slot(a, me, p, kFloats)[kManyRows * D + lr]);
+  for (int p = 0; p < d.pieces; ++p) m = fmaxf(m, piece_slot(a, me, p, kFloats)[kRows * D + lr]);
   f32x4 o[D / 64];
 #pragma unroll
   for (int i = 0; i < D / 64; ++i) o[i] = f32x4{0, 0, 0, 0};
@@ -369,8 +369,8 @@ __global__ __launch_bounds__(256) void attn_rows_merge_kernel(AttnArgs a) {
 #pragma unroll 4
   for (int p = 0; p < d.pieces; ++p) {
     const float* s = piece_slot(a, me, p, kFloats);
-    const float f = __builtin_amdgcn_exp2f(s[kManyRows * D + lr] - m);
-    l += f * s[kManyRows * (D + 1) + lr];
+    const float f = __builtin_amdgcn_exp2f(s[kRows * D + lr] - m);
+    l += f * s[kRows * (D + 1) + lr];
 #pragma unroll
     for (int i = 0; i < D / 64; ++i) o[i] += f * *reinterpret_cast<const f32x4*>(s + ((part * (D / 16) + 4 * i + (int)(threadIdx.x >> 6)) * 64 + lane) * 4);
   }
@@ -387,16 +387,18 @@ __global__ __launch_bounds__(256) void attn_rows_merge_kernel(AttnArgs a) {
 }
 
 template <int D, int Fmt>
-int launch(const AttnArgs& a, bool whole, hipStream_t st) {
+int launch(const AttnArgs& a, int rows, bool whole, hipStream_t st) {
   constexpr int kLds = 2 * Stage<D>::kBytes;
-  static std::atomic<uint64_t> raised[2];
-  auto kernel = whole ? attn_rows_kernel<D, Fmt, true> : attn_rows_kernel<D, Fmt, false>;
+  static std::atomic<uint64_t> raised[4];
+  const bool half = rows == kManyRows / 2;
+  auto kernel = half ? (whole ? attn_rows_kernel<D, Fmt, true, 1> : attn_rows_kernel<D, Fmt, false, 1>) : whole ? attn_rows_kernel<D, Fmt, true, 2> : attn_rows_kernel<D, Fmt, false, 2>;
   if (kLds > 64 * 1024 - 1024)
-    if (int rc = raise_lds_limit(reinterpret_cast<const void*>(kernel), kLds, raised[whole])) return rc;
+    if (int rc = raise_lds_limit(reinterpret_cast<const void*>(kernel), kLds, raised[2 * half + whole])) return rc;
   kernel<<<dim3(kBlocks), dim3(256), kLds, st>>>(a);
   FCP_HIP_CHECK(hipGetLastError());
   if (!whole) {
-    attn_rows_merge_kernel<D><<<dim3(kBlocks, kManyRows / 16), dim3(256), 0, st>>>(a);
+    auto merge = half ? attn_rows_merge_kernel<D, kManyRows / 2> : attn_rows_merge_kernel<D, kManyRows>;
+    merge<<<dim3(kBlocks, (unsigned)(rows / 16)), dim3(256), 0, st>>>(a);
     FCP_HIP_CHECK(hipGetLastError());
   }
   return FCP_OK;
@@ -404,9 +406,9 @@ int launch(const AttnArgs& a, bool whole, hipStream_t st) {
 
 }  // namespace
 
-int launch_attn_rows(const AttnArgs& a, int head_dim, int format, bool whole, hipStream_t st) {
-  if (head_dim == 128) return format == kE4m3 ? launch<128, kE4m3>(a, whole, st) : launch<128, kInt8>(a, whole, st);
-  return format == kE4m3 ? launch<64, kE4m3>(a, whole, st) : launch<64, kInt8>(a, whole, st);
+int launch_attn_rows(const AttnArgs& a, int head_dim, int format, int rows, bool whole, hipStream_t st) {
+  if (head_dim == 128) return format == kE4m3 ? launch<128, kE4m3>(a, rows, whole, st) : launch<128, kInt8>(a, rows, whole, st);
+  return format == kE4m3 ? launch<64, kE4m3>(a, rows, whole, st) : launch<64, kInt8>(a, rows, whole, st);
 }
 
 }  // namespace fcp

@@ -617,3 +617,38 @@ def test_nothing_is_written_past_scratch(news, hkv):
         B.fcp_cache_attn(cache, dev_bf16(q), dev(cu), dev(kv_len), dev(pages), scale, o, lse, scratch[:n], weigh=weigh)
         assert (scratch[n:] == 77).all()
         check_attn((o.double().cpu().numpy(), lse.double().cpu().numpy()), ref.attn(q, cu, kv_len, pages, scale))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("weigh", [False, True])
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("P,D,hq,hkv,kv_len,news", [   # 33 to 64 rows of a KV head per sequence on average
+    (64, 128, 40, 8, [600, 90], [10, 9]), (16, 64, 6, 2, [1200], [20]), (32, 128, 16, 1, [2300, 77, 5], [7, 2, 1]), (128, 64, 4, 4, [70, 1500], [64, 33])])
+def test_attention_of_tens_of_rows(P, D, hq, hkv, kv_len, news, fmt, weigh):
+    assert 32 < sum(news) * hq / hkv / len(news) <= 64
+    ref, cache, pages, cu, q, scale = attn_case(P, D, hq, hkv, kv_len, news, fmt, seed=9)
+    got = run_attn(cache, q, cu, kv_len, pages, scale, weigh)
+    want = ref.attn(q, cu, kv_len, pages, scale)
+    eps = check_attn(got, want)
+    w = R.check_content(cache, ref)
+    if weigh:
+        check_weight(w, ref.weight, want[2], eps, max(news) * hq // hkv)
+    else:
+        assert np.array_equal(w, ref.weight.astype(np.float32))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n", [90, 1500])
+def test_nan_values_among_tens_of_rows(D, n):
+    import torch
+    ref, cache, pages, cu, q, scale = attn_case(64, D, 4, 2, [n, n - 7], [24, 24], "e4m3", seed=3)
+    for s, length in ((0, n), (1, n - 7)):
+        for back, head, channel in ((1, 0, 3), (2, 1, 17), (5, 1, 40), (21, 0, 63)):
+            t = length - back
+            ref.v[pages[s, t // 64], head, t % 64, channel] = 255
+    cache = R.to_device(ref, torch, B)
+    got = run_attn(cache, q, cu, [n, n - 7], pages, scale, False)
+    want = ref.attn(q, cu, [n, n - 7], pages, scale)
+    assert np.isnan(want[0]).any() and not np.isnan(want[0][0]).any()
+    check_attn(got, want)
