@@ -638,10 +638,12 @@ __global__ __launch_bounds__(256) void weigh_scores_kernel(AttnArgs a, int rows_
 
 // ---- host ---------------------------------------------------------------------------------------
 
-// Tables of up to this many tiles: an item is not divided among blocks, which saves the second launch (one sequence of 512 tokens, 4 heads of 64 channels: 6.0 us, divided 13.5).  Twice
-// as many where there are items for all blocks: shares would end inside items of a few tiles, and leave most of a block's waves without one.  64 ragged sequences of up to 1025 tokens, 8
-// KV heads, not divided / divided: 18.7 / 33.1 us; of up to 2000 31.7 / 37.2; but of up to 4000 63.7 / 54.0, and 16 sequences of up to 2000 23.4 / 19.4.
-constexpr int kShortTiles = 16;
+// Tables of up to this many tiles: an item is not divided among blocks, which saves the second launch.  Few rows (not divided / divided; one token of each sequence, 32 heads on 8, 128
+// channels): one sequence of 500 tokens 8.2 / 10.5 us, of 1000 11.2 / 10.8, of 1500 14.4 / 11.0; 16 of up to 1000 11.6 / 12.8, of up to 1500 14.9 / 13.7.  Twice as many where there are
+// items for all blocks, since shares would end inside items of a few tiles: 64 of up to 1000 16.1 / 19.6, of up to 1500 21.4 / 22.2, of up to 2000 26.2 / 25.7 (with 5 new tokens each 32.8 / 39).
+// Many rows: a tile costs more, so fewer.  40 new tokens each (blocks of 128 rows): 8 of up to 250 16.1 / 21.5, of 380 20.1 / 22.1, of 500 24.2 / 22.7; 16 new (64 rows, 64 channels): 8 of
+// up to 500 12.4 / 13.5, 64 of up to 500 16.0 / 20.6.
+int whole_tiles(int rows, int64_t items) { return rows == kManyRows ? 6 : rows == kManyRows / 2 ? 8 : items >= kBlocks ? 32 : 16; }
 
 // How a call is worked.  Up to 16 or 32 rows per sequence and KV head on average: a block of as many rows, whose waves divide the keys; more: 64 or 128 rows, which its waves divide.
 // 64 sequences of up to 16384 tokens, int8, 32 heads on 8: 5 new tokens each (20 rows), 32 rows a block 154 us, 128 rows 252; 16 new (64 rows), 64 rows a block 221 us, 128 rows 262.  Of up
@@ -655,7 +657,7 @@ AttnPlan plan_attn(const CacheView& c, int head_dim, int32_t n_seqs, int32_t max
   p.stored = weigh && p.rows == 16;
   p.part_floats = (int64_t)2 * kBlocks * slot_floats(head_dim, p.rows);
   const int64_t tiles = max(((int64_t)max_pages * c.page + kTile - 1) / kTile, (int64_t)1);
-  p.whole = !p.stored && tiles <= ((int64_t)n_seqs * c.hkv >= kBlocks ? 2 : 1) * kShortTiles;
+  p.whole = !p.stored && tiles <= whole_tiles(p.rows, (int64_t)n_seqs * c.hkv);
   p.places = (tiles + kItemLead) * c.hkv * (n_seqs + (int64_t)tq * group / p.rows);
   p.score_floats = p.stored ? p.places * 16 * kTile : 0;
   return p;
