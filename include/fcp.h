@@ -497,7 +497,8 @@ int fcp_cache_append(const fcp_cache* cache, const void* k, int64_t k_row, const
  *   O = 0, LSE = -inf.  Rows of no sequence are left unwritten.
  *   weigh: 0, or 1 to add to cache->weight, for every token and KV head, the probabilities that the call's rows of that head's group give it.
  *   scratch: device, 256-byte aligned, fcp_cache_scratch_bytes(FCP_SCRATCH_CACHE_ATTN or _WEIGH, ...); contents on entry irrelevant.
- * Scores, statistics and sums are held in 32 bits; probabilities are rounded to bf16 for the product with V.  No atomics: results repeat bit for bit.
+ * Scores, statistics and sums are held in 32 bits; for the product with V probabilities are rounded to bf16 (|dO| <= 2^-8 sum p |v|), and with
+ * up to 32 rows per sequence and KV head on average what that leaves is multiplied too.  No atomics: results repeat bit for bit.
  */
 int fcp_cache_attn(const fcp_cache* cache, const void* q, int64_t q_row, int32_t tq, int32_t hq, const int32_t* cu_seqlens, const int32_t* kv_len,
                    const int32_t* pages, int32_t n_seqs, int32_t max_pages, float softmax_scale, int32_t weigh, void* o, float* lse,

@@ -149,8 +149,8 @@ __device__ inline void mask_scores(f32x4 (&s)[4], int last) {
   for (int i = 0; i < 16; ++i) s[i / 4][i % 4] = i <= last ? s[i / 4][i % 4] : -INFINITY;
 }
 
-// Softmax of one tile and 16 rows, in two parts: the running maximum follows the raw scores s (c scales them), and what was summed up so far follows the maximum; then the scores become
-// probabilities p, times the values' scale vs.  The maximum only grows in steps of more than 2^8: probabilities stay below 256, and most tiles leave the sums alone.
+// Softmax of one tile and 16 rows, its first part: the running maximum follows the raw scores s (c scales them), and what was summed up so far follows the maximum.  It only grows in steps of
+// more than 2^8: probabilities stay below 256, and most tiles leave the sums alone.
 template <int D>
 __device__ inline void raise_maximum(const f32x4 (&s)[4], float c, f32x4 (&o)[D / 16], float& m, float& l) {
   float top = max3(s[0][0], s[0][1], s[0][2]);
@@ -163,14 +163,6 @@ __device__ inline void raise_maximum(const f32x4 (&s)[4], float c, f32x4 (&o)[D 
     l *= f;
 #pragma unroll
     for (int d = 0; d < D / 16; ++d) o[d] *= f;
-  }
-}
-__device__ inline void probabilities_of(const f32x4 (&s)[4], float c, float vs, float m, float& l, bf16x8 (&p)[2]) {
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 4][i % 4], c, -m));
-    l += e;
-    p[i / 8][i % 8] = (__bf16)(e * vs);
   }
 }
 
