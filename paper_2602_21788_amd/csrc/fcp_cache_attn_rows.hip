@@ -85,7 +85,8 @@ __device__ inline void load_share(const AttnArgs& a, const uint8_t* codes, const
     const int key = tile * kTile + kGroup * group_of<D>(wave, i);
     const int64_t block = block_of(a.c, max(pages.of[i], 0), head), at = (block * a.c.page + (key & (a.c.page - 1))) * D + 1024 * lot_of<D>(wave);
     s.live[i] = pages.of[i] < 0 ? 0 : min(len - key, kGroup);
-    s.scale[i] = as_scalar(scales)[block];
+    const float scale = as_scalar(scales)[block];
+    s.scale[i] = pages.of[i] < 0 ? 1.f : scale;            // (that of an unused page is whatever it holds, and 0 * NaN is NaN)
     s.w[i] = *reinterpret_cast<const u32x4*>(codes + at + 16 * (int)(threadIdx.x & 63));
   }
 }
@@ -220,7 +221,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(AttnArgs a) {
       auto note_live = [&](int t) {
 #pragma unroll
         for (int i = 0; i < D / 64; ++i)
-          if (lane == 0) live[t & 3][group_of<D>(wave, i)] = keys.live[i], key_scale[t & 3][group_of<D>(wave, i)] = keys.live[i] ? keys.scale[i] : 1.f;
+          if (lane == 0) live[t & 3][group_of<D>(wave, i)] = keys.live[i], key_scale[t & 3][group_of<D>(wave, i)] = keys.scale[i];
       };
       auto store_keys = [&](int t) {
         bf16x8 half;

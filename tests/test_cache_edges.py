@@ -1,0 +1,45 @@
+"""The paged 8-bit cache at the edges of what it takes: what unused pages hold, the ends of the range of scales and scores, queries that are not finite, limits."""
+import numpy as np
+import pytest
+
+import cache_ref as R
+from paper_2602_21788_amd import binding as B
+from test_cache import FORMATS, Call, attn_case, check_attn, dev, dev_bf16, run_attn
+
+
+# ---- GPU ------------------------------------------------------------------------------------------------------------------------------------
+def check_weights(got, before, W, eps, rows):
+    """As test_cache.check_weight where the sums are finite; elsewhere the same NaN and infinity."""
+    want = before + W
+    fine = np.isfinite(want)
+    assert np.array_equal(np.isfinite(got), fine) and np.array_equal(got[~fine], want[~fine], equal_nan=True)
+    tol = W[fine] * (2 * eps[np.isfinite(eps)].max() + 1e-6) + want[fine] * (rows + 2) * 2.0 ** -24 + 1e-30
+    assert (np.abs(got[fine] - want[fine]) <= tol).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bad", [np.nan, np.inf])
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("P,D,hq,hkv,kv_len,news", [   # rows of a KV head per sequence on average: up to 16, 32, 64, more; whole and divided items
+    (16, 64, 4, 2, [150, 70], [1, 2]), (32, 128, 8, 2, [1500, 40], [6, 6]), (16, 64, 4, 2, [150, 70], [20, 20]), (32, 128, 8, 2, [1500, 40], [16, 10]),
+    (16, 64, 4, 2, [150, 70], [50, 60]), (64, 128, 4, 1, [1500, 129], [40, 40]), (128, 128, 4, 2, [65], [65])])
+def test_scales_of_unused_pages_are_not_looked_at(P, D, hq, hkv, kv_len, news, fmt, bad):
+    """Nobody has to fill the scales of pages that hold no token: NaN and infinity there reach nothing.  Page 0 is unused, and a page in the middle is missing."""
+    import torch
+    ref, _, pages, cu, q, scale = attn_case(P, D, hq, hkv, kv_len, news, fmt, seed=11)
+    grown = R.RefCache(np.random.default_rng(0), ref.n_pages + 1, hkv, P, D, fmt)
+    for name in ("k", "v", "k_e", "v_e", "weight"):
+        getattr(grown, name)[1:] = getattr(ref, name)
+    pages = np.where(pages >= 0, pages + 1, -1).astype(np.int32)
+    if (pages[0] >= 0).sum() > 2:
+        pages[0, 1] = -1
+    cache = R.to_device(grown, torch, B)
+    unused = torch.from_numpy(np.setdiff1d(np.arange(grown.n_pages), pages)).cuda()
+    assert 0 in unused
+    cache.k_scale[unused], cache.v_scale[unused] = bad, bad
+    for weigh in (False, True):
+        got = run_attn(cache, q, cu, kv_len, pages, scale, weigh)
+        want = grown.attn(q, cu, kv_len, pages, scale)
+        assert np.isfinite(want[0]).all()
+        eps = check_attn(got, want)
+    check_weights(R.from_device(cache)[4], grown.weight, want[2], eps, max(news) * hq // hkv)
