@@ -333,6 +333,9 @@ __device__ inline float pick(float x, int from) { return __int_as_float(__builti
 // Codes of a word (four tokens of a channel, or four channels of a token) in other units: the largest magnitude (in units 2^16 times as large, which no value leaves), and
 // the codes.  A token's scale is multiplied in 2^-16 times.  NaN is no magnitude, and stays.
 constexpr float kFar = 0x1p-16f;
+// The factor from a token's units to the new page's.  A code other than 0 leaves the format with a factor above 2^18, so only zeros meet a greater one; it stays finite, since 0 times
+// infinity is NaN.  (Below 2^-126 all codes become zeros.)
+__device__ inline float unit_factor(float scale, float to_units) { return fminf(fmaxf(scale * to_units, 0x1p-126f), 0x1p126f); }
 template <int Fmt>
 __device__ inline float largest(uint32_t w, float s0, float s1, float s2, float s3, float top) {
   const f32x2 a = decode_half<Fmt, false>(w), b = decode_half<Fmt, true>(w);
@@ -406,7 +409,7 @@ __global__ __launch_bounds__(256) void move_kernel(EvictArgs a) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int slot = RPI * i + sub;
-      const float f = fmaxf(s[i] * to_units, 0x1p-126f);
+      const float f = unit_factor(s[i], to_units);
 #pragma unroll
       for (int j = 0; j < 4; ++j) w[i][j] = in_units<Fmt>(w[i][j], f, f, f, f);
       if (slot < P) *reinterpret_cast<u32x4*>(codes + slot * D + ch) = w[i];
@@ -469,7 +472,7 @@ __global__ __launch_bounds__(256) void move_kernel(EvictArgs a) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const int slot = g * kGroup + 4 * q + j;
-          s[j] = fmaxf(pick(scale[slot / 64], slot & 63) * to_units, 0x1p-126f);
+          s[j] = unit_factor(pick(scale[slot / 64], slot & 63), to_units);
         }
 #pragma unroll
         for (int c = 0; c < NC; ++c) w[g][c][q] = in_units<Fmt>(w[g][c][q], s[0], s[1], s[2], s[3]);

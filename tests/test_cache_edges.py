@@ -43,3 +43,29 @@ def test_scales_of_unused_pages_are_not_looked_at(P, D, hq, hkv, kv_len, news, f
         assert np.isfinite(want[0]).all()
         eps = check_attn(got, want)
     check_weights(R.from_device(cache)[4], grown.weight, want[2], eps, max(news) * hq // hkv)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("P,D", [(16, 64), (64, 128)])
+@pytest.mark.parametrize("far", [17, 18, 60, 119])
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_eviction_keeps_zeros_of_pages_of_great_scales(fmt, far, P, D):
+    """Tokens of nothing but zeros from a page whose scale is 2^far: alone in a new page, whose scale is the least, and beside tokens of the least magnitudes."""
+    import torch
+    rng = np.random.default_rng(far)
+    ref = R.RefCache(rng, 10, 2, P, D, fmt)
+    pages, new_pages = np.array([[0, 1, 2], [3, 4, 5]], np.int32), np.array([[6], [7]], np.int32)
+    kv_len, budget = [3 * P, 3 * P], P
+    ref.weight[:] = 0
+    for codes, es in ((ref.k, ref.k_e), (ref.v, ref.v_e)):
+        es[[0, 3]], es[1] = far, -108
+        codes[0, :, ::2] = codes[3] = 0
+        codes[3, :, 1, 5] = 0 if fmt == "int8" else 128          # minus zero
+    ref.weight[0, :, ::2], ref.weight[1, :, ::2], ref.weight[3] = 2, 1, 1
+    cache = R.to_device(ref, torch, B)
+    kept, new_len = torch.empty(2, 2, budget, dtype=torch.int32, device="cuda"), torch.empty(2, dtype=torch.int32, device="cuda")
+    scratch = torch.empty(B.fcp_cache_scratch_bytes(B.FCP_SCRATCH_CACHE_EVICT, cache, 2, 3), dtype=torch.uint8, device="cuda")
+    B.fcp_cache_evict(cache, dev(pages), dev(kv_len), dev(new_pages), budget, 0, 0, kept, new_len, scratch)
+    want_kept, _ = ref.evict(pages, kv_len, new_pages, budget, 0, 0)
+    assert np.array_equal(kept.cpu().numpy(), want_kept) and ref.k_e[7, 0] == R.LEAST and ref.k_e[6, 0] < -90
+    R.check_content(cache, ref)
