@@ -508,9 +508,9 @@ __global__ __launch_bounds__(kWeighThreads, 2) void weigh_kernel(WeighArgs a) {
     auto add = [&](int buffer, const float& now, float& next) {
       __builtin_amdgcn_s_waitcnt(kWaitVm0);                // the buffer's rows are there
       const float mine = now;
-      // rows that are not there, and rows that saw nothing, add exp2(-inf)
-      const float lse2 = row < all_rows && mine != -INFINITY ? mine * kLog2e : INFINITY;
-      const int last = min(z.len - z.n + tok - key0 - 16 * g, there);          // of the lane's keys, those up to it are seen
+      const float lse2 = mine * kLog2e;
+      // of the lane's keys, those up to `last` are seen; none by rows that are not there, and by rows that saw nothing
+      const int last = row < all_rows && mine != -INFINITY ? min(z.len - z.n + tok - key0 - 16 * g, there) : -1;
       auto move = [&](int& r, int& t, int& hh) {
         r += step;
         t += step_tok;
@@ -533,10 +533,12 @@ __global__ __launch_bounds__(kWeighThreads, 2) void weigh_kernel(WeighArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[i][j], q[j], s[i], 0, 0, 0);
       if (__ballot(last < 15)) {
+        // (chosen behind the exponential: a score or an LSE that is NaN must not reach keys that the row does not see)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[i / 4][i % 4] = i <= last ? s[i / 4][i % 4] * c : -INFINITY;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) got[i] += __builtin_amdgcn_exp2f(s[i / 4][i % 4] - lse2);
+        for (int i = 0; i < 16; ++i) {
+          const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 4][i % 4], c, -lse2));
+          got[i] += i <= last ? e : 0.f;
+        }
       } else {
 #pragma unroll
         for (int i = 0; i < 16; ++i) got[i] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[i / 4][i % 4], c, -lse2));
@@ -627,6 +629,13 @@ __global__ __launch_bounds__(256) void weigh_scores_kernel(AttnArgs a, int rows_
         for (int r0 = 0; r0 < all_rows; r0 += 4) {
           if (r0 > 0) rows_at(r0);
           const float lse2 = r0 + sub < all_rows && lse != -INFINITY ? lse * kLog2e : INFINITY;       // (else nothing is added)
+          if (__ballot(lse2 != lse2)) {                    // rare: a row's NaN must not reach keys that it does not see, whose scores are -inf
+#pragma unroll
+            for (int j = 0; j < kUnroll; ++j)
+#pragma unroll
+              for (int k = 0; k < 4; ++k) got[j][k] += s[j][k] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s[j][k] - lse2);
+            continue;
+          }
 #pragma unroll
           for (int j = 0; j < kUnroll; ++j)
 #pragma unroll

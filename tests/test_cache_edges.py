@@ -69,3 +69,64 @@ def test_eviction_keeps_zeros_of_pages_of_great_scales(fmt, far, P, D):
     want_kept, _ = ref.evict(pages, kv_len, new_pages, budget, 0, 0)
     assert np.array_equal(kept.cpu().numpy(), want_kept) and ref.k_e[7, 0] == R.LEAST and ref.k_e[6, 0] < -90
     R.check_content(cache, ref)
+
+
+MANY = [  # P, D, hq, hkv, kv_len, news of calls of fcp_cache_weigh
+    (64, 128, 4, 4, [100], [100]), (16, 64, 8, 2, [70, 130], [70, 130]), (32, 128, 6, 2, [300, 20, 90], [40, 20, 1]), (128, 64, 2, 2, [1000], [3]), (64, 128, 3, 1, [200], [17])]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
+@pytest.mark.parametrize("P,D,hq,hkv,kv_len,news", MANY)
+def test_weights_of_queries_that_are_not_finite(P, D, hq, hkv, kv_len, news, bad):
+    """Such a row reaches the weights of the tokens that it sees and no others."""
+    import torch
+    ref, cache, pages, cu, q, scale = attn_case(P, D, hq, hkv, kv_len, news, "int8", seed=21)
+    _, LSE, _, _, units = ref.attn(q, cu, kv_len, pages, scale)
+    lse = LSE.astype(np.float32)
+    q[0, 0, 3] = bad
+    B.fcp_cache_weigh(cache, dev_bf16(q), torch.from_numpy(lse).cuda(), dev(cu), dev(kv_len), dev(pages), scale)
+    with np.errstate(all="ignore"):
+        W = ref.attn(q, cu, kv_len, pages, scale, lse_in=lse.astype(np.float64))[2]
+    eps = (units + 8 * np.abs(LSE) + 16) * 2.0 ** -24
+    check_weights(R.from_device(cache)[4], ref.weight, W, eps, max(news) * hq // hkv)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("P,D,hq,hkv,kv_len,news", MANY)
+def test_weights_of_rows_whose_sum_is_nan_or_of_nothing(P, D, hq, hkv, kv_len, news):
+    """A row whose LSE is -inf adds nothing, whatever its query holds; one whose LSE is NaN reaches the tokens that it sees and no others."""
+    import torch
+    ref, cache, pages, cu, q, scale = attn_case(P, D, hq, hkv, kv_len, news, "e4m3", seed=22)
+    _, LSE, _, _, units = ref.attn(q, cu, kv_len, pages, scale)
+    lse, n = LSE.astype(np.float32), q.shape[0]
+    given, seen_by, sums = q.copy(), q.copy(), lse.astype(np.float64)
+    for row, value in ((n - 1, np.nan), (n // 2, np.inf)):
+        given[row], seen_by[row], lse[:, row], sums[:, row] = value, 0, -np.inf, np.inf          # (exp(score - inf) is 0)
+    lse[0, 0] = sums[0, 0] = np.nan
+    B.fcp_cache_weigh(cache, dev_bf16(given), torch.from_numpy(lse).cuda(), dev(cu), dev(kv_len), dev(pages), scale)
+    W = ref.attn(seen_by, cu, kv_len, pages, scale, lse_in=sums)[2]
+    eps = (units + 8 * np.abs(LSE) + 16) * 2.0 ** -24
+    check_weights(R.from_device(cache)[4], ref.weight, W, eps, max(news) * hq // hkv)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bad", [np.nan, np.inf])
+@pytest.mark.parametrize("P,D,hq,hkv,kv_len,news", MANY + [(16, 64, 4, 2, [90, 33], [3, 2]), (64, 128, 2, 1, [1500], [6]), (32, 64, 1, 1, [70, 200], [5, 9])])
+def test_attention_that_weighs_queries_that_are_not_finite(P, D, hq, hkv, kv_len, news, bad):
+    """A row whose query is not finite spoils its own output and sum, and the weights of the tokens that it sees; nothing else."""
+    import torch
+    ref, cache, pages, cu, q, scale = attn_case(P, D, hq, hkv, kv_len, news, "int8", seed=23)
+    q[0, 0] = 0                                            # (the reference's row: what it adds lies on the tokens that are left out below)
+    want = ref.attn(q, cu, kv_len, pages, scale)
+    q[0, 0, 3] = bad
+    o, lse = run_attn(cache, q, cu, kv_len, pages, scale, True)
+    assert bad == np.inf or (np.isnan(o[0, 0]).all() and np.isnan(lse[0, 0]))
+    o[0, 0], lse[0, 0] = want[0][0, 0], want[1][0, 0]
+    eps = check_attn((o, lse), want)
+    got, mine = R.from_device(cache)[4].astype(np.float64), np.zeros(ref.weight.shape, bool)
+    for t in range(kv_len[0] - news[0] + 1):
+        mine[pages[0, t // P], 0, t % P] = True
+    assert bad == np.inf or np.isnan(got[mine]).all()
+    got[mine] = (ref.weight + want[2])[mine]
+    check_weights(got, ref.weight, want[2], eps, max(news) * hq // hkv)
