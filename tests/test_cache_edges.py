@@ -130,3 +130,59 @@ def test_attention_that_weighs_queries_that_are_not_finite(P, D, hq, hkv, kv_len
     assert bad == np.inf or np.isnan(got[mine]).all()
     got[mine] = (ref.weight + want[2])[mine]
     check_weights(got, ref.weight, want[2], eps, max(news) * hq // hkv)
+
+
+PARTS = [  # P, D, hq, hkv, kv_len, news, softmax scale: up to 32 rows of a KV head per sequence on average; items whole, and (more than 2048 tokens in the table, or weights) divided
+    (16, 64, 4, 2, [100, 37], [1, 1], 0.125), (64, 128, 8, 1, [300, 90], [1, 2], 0.09), (32, 128, 4, 4, [2500], [1], 0.3), (64, 64, 8, 2, [2300, 3000], [2, 4], 0.4),
+    (16, 64, 8, 2, [100, 37], [7, 4], 0.125), (64, 128, 24, 1, [200], [1], 0.09), (32, 128, 8, 1, [2500], [4], 0.3)]
+
+
+def part_bound(q, ref, want, kv_len, news, bits):
+    """What O may be off by: half a step of bf16 of itself; of sum p |v| the `bits` that the probabilities in the product have, twice what a score may be off by, and the roundings of the sums of
+    numerator and denominator.  On its way through both a term meets at most 16 additions for each tile of its wave, 64 in a product and 64 where waves and pieces are joined."""
+    O, LSE, _, absv, units = want
+    eps = (units + 8 * np.abs(LSE) + 16) * 2.0 ** -24
+    sums = 2 * (max(kv_len) // 16 + 128) * 2.0 ** -24
+    return absv * (2.0 ** -bits + 2 * eps.T[..., None] + sums) + np.abs(O) * 2.0 ** -8 + 1e-30
+
+
+def parts_case(P, D, hq, hkv, kv_len, news, scale, fmt):
+    assert sum(news) * hq / hkv / len(news) <= 32
+    ref, cache, pages, cu, q, scale = attn_case(P, D, hq, hkv, kv_len, news, fmt, seed=31, scale=scale)
+    return ref, cache, pages, cu, q, scale, ref.attn(q, cu, kv_len, pages, scale)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("weigh", [False, True])
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("P,D,hq,hkv,kv_len,news,scale", PARTS)
+def test_probabilities_of_few_rows_have_two_parts(P, D, hq, hkv, kv_len, news, scale, fmt, weigh):
+    """Two bf16 parts: what a part leaves is at most 2^-8 of what it is a part of."""
+    ref, cache, pages, cu, q, scale, want = parts_case(P, D, hq, hkv, kv_len, news, scale, fmt)
+    o, _ = run_attn(cache, q, cu, kv_len, pages, scale, weigh)
+    assert (np.abs(o - want[0]) <= part_bound(q, ref, want, kv_len, news, 16)).all()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("P,D,hq,hkv,kv_len,news,scale", PARTS)
+def test_the_bound_tells_one_part_from_two(P, D, hq, hkv, kv_len, news, scale, fmt, monkeypatch):
+    """On the CPU, exactly but for the probabilities: in two parts they are within the bound, in one they are not."""
+    monkeypatch.setattr(R, "to_device", lambda *a: None)
+    ref, _, pages, cu, q, scale, want = parts_case(P, D, hq, hkv, kv_len, news, scale, fmt)
+
+    def bf16(x):
+        u = np.asarray(x, np.float32).view(np.uint32)
+        return ((u + 0x7fff + ((u >> 16) & 1)) & np.uint32(0xffff0000)).view(np.float32).astype(np.float64)
+
+    off = {1: np.zeros(want[0].shape), 2: np.zeros(want[0].shape)}
+    for s, n in enumerate(kv_len):
+        for h in range(hq):
+            K, V = (ref.rows(w, pages[s], n, h // (hq // hkv))[0] for w in "kv")
+            for i in range(news[s]):
+                x = scale * (K @ q[cu[s] + i, h])
+                e = np.exp(x - x[: n - news[s] + i + 1].max()) * (np.arange(n) <= n - news[s] + i)
+                one = bf16(e)
+                for parts, p in ((1, one), (2, one + bf16(e - one))):
+                    off[parts][cu[s] + i, h] = bf16(p @ V / e.sum()) - want[0][cu[s] + i, h]
+    bound = part_bound(q, ref, want, kv_len, news, 16)
+    assert (np.abs(off[2]) <= bound).all() and (np.abs(off[1]) > bound).any()
