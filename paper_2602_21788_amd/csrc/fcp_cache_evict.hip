@@ -154,7 +154,7 @@ __device__ inline Select open_select(const EvictArgs& a, int seq, int head, bool
   int32_t* const kept = a.kept + ((int64_t)seq * a.c.hkv + head) * a.budget;
   if (writes) {
     if (head == 0 && tid == 0) a.new_len[seq] = n_new;
-    for (int i = n_new + tid; i < a.budget; i += kSelectThreads) kept[i] = -1;
+    for (int64_t i = n_new + tid; i < a.budget; i += kSelectThreads) kept[i] = -1;     // (64 bits: a budget may be 2^31 - 1)
     if (n <= a.budget)
       for (int i = tid; i < n; i += kSelectThreads) kept[i] = i;
   }

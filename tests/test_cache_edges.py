@@ -186,3 +186,19 @@ def test_the_bound_tells_one_part_from_two(P, D, hq, hkv, kv_len, news, scale, f
                     off[parts][cu[s] + i, h] = bf16(p @ V / e.sum()) - want[0][cu[s] + i, h]
     bound = part_bound(q, ref, want, kv_len, news, 16)
     assert (np.abs(off[2]) <= bound).all() and (np.abs(off[1]) > bound).any()
+
+
+@pytest.mark.gpu
+def test_eviction_with_a_budget_of_the_last_32_bit_number():
+    """A budget far above what the tables can hold keeps everything; the list's end is -1 to the last place."""
+    import torch
+    ref = R.RefCache(np.random.default_rng(3), 5, 1, 16, 64, "int8")
+    cache = R.to_device(ref, torch, B)
+    pages, new_pages, budget = np.array([[0, 1]], np.int32), np.array([[3, 2]], np.int32), 2 ** 31 - 1
+    kept, new_len = torch.zeros(1, 1, budget, dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    scratch = torch.empty(B.fcp_cache_scratch_bytes(B.FCP_SCRATCH_CACHE_EVICT, cache, 1, 2), dtype=torch.uint8, device="cuda")
+    B.fcp_cache_evict(cache, dev(pages), dev([21]), dev(new_pages), budget, 4, 8, kept, new_len, scratch)
+    assert int(new_len[0]) == 21 and kept[0, 0, :21].tolist() == list(range(21))
+    assert all(bool((x == -1).all()) for x in kept[0, 0, 21:].split(1 << 28))
+    ref.evict(pages, [21], new_pages, 24, 4, 8)
+    R.check_content(cache, ref)
