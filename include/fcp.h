@@ -439,6 +439,7 @@ int fcp_rotary_frequencies(int32_t rot_dim, double base, int32_t scaling, double
  * Angles are formed in 64 bits (position * turns loses the fraction of a turn in 32 bits at positions of 10^5), the products in 32, results are
  * rounded once.  FCP_F32 in and FCP_BF16 out: gradient sums of fcp_attn_bwd_step become final gradients without a pass of their own.
  * Rows whose pointers and strides are multiples of 16 bytes, with head_dim and rot_dim multiples of 16, move 16 bytes at a time; all others work too.
+ * Tensors that make 2^24 blocks or more (a block takes at least one row, and 512 / rot_dim rows of up to 64 KB read and written) are FCP_ERR_UNSUPPORTED.
  */
 int fcp_rotary(const fcp_rotary_part* parts, int32_t n_parts, const double* turns, int32_t head_dim, int32_t rot_dim, int32_t layout,
                float magnitude, int32_t backward, void* stream);
@@ -484,7 +485,7 @@ size_t fcp_cache_scratch_bytes(int which, const fcp_cache* cache, int32_t n_seqs
  * units the new rows' largest finite magnitude is within the format; else the larger of that and the page's scale, and where it grows the
  * earlier tokens are rounded again in the new units.  Codes are rounded to nearest even.  Infinities become the largest value; NaN stays NaN in
  * FCP_CACHE_E4M3 and becomes 0 in FCP_CACHE_INT8.  The weights of the new tokens (if the cache has them) become 0.
- * A page must not be written for two sequences, or read by another stream, at the same time.
+ * A page must not be written for two sequences, or read by another stream, at the same time.  n_rows / page_tokens + 2 n_seqs must be below 2^24 (FCP_ERR_UNSUPPORTED).
  */
 int fcp_cache_append(const fcp_cache* cache, const void* k, int64_t k_row, const void* v, int64_t v_row, int32_t n_rows, const int32_t* cu_seqlens,
                      const int32_t* kv_len, const int32_t* pages, int32_t n_seqs, int32_t max_pages, void* stream);
@@ -518,7 +519,7 @@ int fcp_cache_weigh(const fcp_cache* cache, const void* q, int64_t q_row, int32_
  * call reads from (tokens move up, and many blocks move them at once); the old pages are free afterwards.  Every (new page, KV head) gets the least scale that
  * holds its tokens, as in fcp_cache_append; slots after the last token hold 0.
  *   new_pages [n_seqs][max_new_pages] int32 device; max_new_pages * page_tokens >= min(budget, max_pages * page_tokens)
- *   budget >= n_first + n_recent, budget >= 1
+ *   budget >= n_first + n_recent, budget >= 1;  n_seqs * hkv below 2^22, n_seqs times the pages of min(budget, max_pages * page_tokens) tokens below 2^24 (FCP_ERR_UNSUPPORTED)
  *   kept [n_seqs][hkv][budget] int32 device out: the old token numbers, increasing, -1 after the last
  *   new_len [n_seqs] int32 device out: min(kv_len, budget); not kv_len itself
  *   scratch: device, 256-byte aligned, fcp_cache_scratch_bytes(FCP_SCRATCH_CACHE_EVICT, ...)

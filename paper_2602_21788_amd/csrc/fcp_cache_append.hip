@@ -305,6 +305,7 @@ extern "C" int fcp_cache_append(const fcp_cache* cache, const void* k, int64_t k
   a.row[0] = k_row;
   a.row[1] = v_row;
   a.units = (n_rows >> a.c.log_page) + 2 * n_seqs;
+  if (!fits_axis(a.units, 256)) return fail(FCP_ERR_UNSUPPORTED, "%s: rows that may lie in 2^24 pages or more", who);
   hipStream_t st = static_cast<hipStream_t>(stream);
   const dim3 grid((unsigned)a.units, (unsigned)((2 * a.c.hkv + 3) / 4));
   const bool e4m3 = cache->format == FCP_CACHE_E4M3;

@@ -20,7 +20,7 @@ struct EvictArgs {
   CacheView c;
   SeqView s;                           // (no rows)
   const int32_t* new_pages;
-  int32_t max_new, budget, first, recent;
+  int32_t max_new, places, budget, first, recent;          // entries of a row of new_pages, those of them that can get a token
   int32_t* kept;
   int32_t* new_len;
   // long tables: tokens of a chunk, chunks; per (sequence, KV head): counts of each chunk, candidates, of each chunk the tokens above their upper bits, border
@@ -357,7 +357,7 @@ __global__ __launch_bounds__(256) void move_kernel(EvictArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int job = blockIdx.y * 4 + wave;
   if (job >= 2 * a.c.hkv) return;
-  const int head = job >> 1, seq = blockIdx.x / a.max_new, place = blockIdx.x % a.max_new;
+  const int head = job >> 1, seq = blockIdx.x / a.places, place = blockIdx.x % a.places;
   const bool value = job & 1;
   const int n_new = min(cached(a, seq), a.budget), count = min(P, n_new - place * P);
   if (count <= 0) return;
@@ -533,11 +533,12 @@ extern "C" int fcp_cache_evict(const fcp_cache* cache, const int32_t* pages, con
   const size_t need = p.bytes;
   if (scratch_bytes < need) return fail(FCP_ERR_CAPACITY, "%s: scratch has %zu bytes, %zu are needed", who, scratch_bytes, need);
   const int64_t use = (most + a.c.page - 1) / a.c.page;      // (further entries of new_pages are not used)
-  if ((int64_t)n_seqs * a.c.hkv > INT32_MAX || (int64_t)n_seqs * max_new_pages > INT32_MAX)
-    return fail(FCP_ERR_UNSUPPORTED, "%s: more than 2^31 - 1 pages or heads of all sequences", who);
+  if (!fits_axis((int64_t)n_seqs * a.c.hkv, kSelectThreads) || !fits_axis((int64_t)n_seqs * use, 256))
+    return fail(FCP_ERR_UNSUPPORTED, "%s: 2^22 KV heads or 2^24 new pages of all sequences, or more", who);
   a.s = {nullptr, kv_len, pages, n_seqs, max_pages, 0};
   a.new_pages = new_pages;
   a.max_new = max_new_pages;
+  a.places = (int32_t)use;
   a.budget = budget;
   a.first = n_first;
   a.recent = n_recent;
@@ -564,7 +565,7 @@ extern "C" int fcp_cache_evict(const fcp_cache* cache, const int32_t* pages, con
   }
   FCP_HIP_CHECK(hipGetLastError());
   if (use == 0) return FCP_OK;
-  const dim3 grid((unsigned)(n_seqs * max_new_pages), (unsigned)((2 * a.c.hkv + 3) / 4));
+  const dim3 grid((unsigned)(n_seqs * use), (unsigned)((2 * a.c.hkv + 3) / 4));
   const bool e4m3 = cache->format == FCP_CACHE_E4M3;
   (cache->head_dim == 128 ? (e4m3 ? launch_move<128, kE4m3> : launch_move<128, kInt8>) : (e4m3 ? launch_move<64, kE4m3> : launch_move<64, kInt8>))(a, grid, st);
   FCP_HIP_CHECK(hipGetLastError());

@@ -20,6 +20,9 @@ void clear_error();
       return ::fcp::fail(FCP_ERR_HIP, "%s failed: %s", #expr, hipGetErrorString(e__)); \
   } while (0)
 
+// A launch has fewer than 2^32 threads along an axis; HIP refuses larger ones, which a call that has launched something before would find out too late.
+inline bool fits_axis(int64_t blocks, int threads) { return blocks < ((int64_t)1 << 32) / threads; }
+
 // A kernel that uses more than 64 KB of dynamic LDS needs its limit raised once per device; `done` keeps one bit
 // per device (devices past 63 raise it on every call).  Safe to call from several threads.
 inline int raise_lds_limit(const void* kernel, int bytes, std::atomic<uint64_t>& done) {

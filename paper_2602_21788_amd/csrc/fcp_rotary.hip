@@ -236,7 +236,7 @@ extern "C" int fcp_rotary(const fcp_rotary_part* parts, int32_t n_parts, const d
     a.first[i] = (int32_t)blocks;
     const fcp_rotary_part& p = a.part[i];
     blocks += ((int64_t)p.rows + a.rows - 1) / a.rows * (a.heads >= p.heads ? 1 : ((int64_t)p.heads + a.heads - 1) / a.heads);
-    if (blocks > INT32_MAX) return fail(FCP_ERR_UNSUPPORTED, "%s: more than 2^31 - 1 blocks of rows", who);
+    if (!fits_axis(blocks, kRotThreads)) return fail(FCP_ERR_UNSUPPORTED, "%s: 2^24 blocks of rows or more", who);
   }
   a.first[a.n_parts] = (int32_t)blocks;
   a.turns = turns;

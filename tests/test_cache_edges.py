@@ -7,6 +7,19 @@ from paper_2602_21788_amd import binding as B
 from test_cache import FORMATS, Call, attn_case, check_attn, dev, dev_bf16, run_attn
 
 
+# ---- CPU ------------------------------------------------------------------------------------------------------------------------------------
+def test_launches_of_too_many_threads_are_refused_before_any_device_work():
+    no = B.FCP_ERR_UNSUPPORTED
+    assert Call(page_tokens=16, n_rows=1 << 28).append() == no and Call(page_tokens=16, n_rows=2 ** 31 - 1, n_seqs=1).append() == no
+    assert Call(n_seqs=1 << 20).evict() == no and b"2^22" in B.lib().fcp_last_error()
+    assert Call(hkv=1, page_tokens=16, n_seqs=1 << 20, max_pages=16, max_new=16, budget=256).evict() == no
+    p = (B.RotaryPart * 1)()
+    p[0].x = p[0].y = p[0].pos = Call.fake
+    p[0].x_row = p[0].y_row = p[0].x_head = p[0].y_head = 1024
+    p[0].rows, p[0].heads = 1 << 24, 1
+    assert B.lib().fcp_rotary(p, 1, Call.fake, 1024, 1024, 0, 1.0, 0, None) == no and b"2^24" in B.lib().fcp_last_error()
+
+
 # ---- GPU ------------------------------------------------------------------------------------------------------------------------------------
 def check_weights(got, before, W, eps, rows):
     """As test_cache.check_weight where the sums are finite; elsewhere the same NaN and infinity."""
@@ -201,4 +214,20 @@ def test_eviction_with_a_budget_of_the_last_32_bit_number():
     assert int(new_len[0]) == 21 and kept[0, 0, :21].tolist() == list(range(21))
     assert all(bool((x == -1).all()) for x in kept[0, 0, 21:].split(1 << 28))
     ref.evict(pages, [21], new_pages, 24, 4, 8)
+    R.check_content(cache, ref)
+
+
+@pytest.mark.gpu
+def test_eviction_with_a_long_table_of_new_pages():
+    """Only as many entries as the budget fills are launched for."""
+    import torch
+    ref = R.RefCache(np.random.default_rng(4), 9, 2, 16, 64, "e4m3")
+    cache = R.to_device(ref, torch, B)
+    pages, new_pages, kv_len = np.array([[0, 1, 2], [3, 4, -1]], np.int32), np.full((2, 1 << 23), -1, np.int32), [41, 19]
+    new_pages[:, :2] = [[8, 5], [6, 7]]
+    kept, new_len = torch.empty(2, 2, 20, dtype=torch.int32, device="cuda"), torch.empty(2, dtype=torch.int32, device="cuda")
+    scratch = torch.empty(B.fcp_cache_scratch_bytes(B.FCP_SCRATCH_CACHE_EVICT, cache, 2, 3), dtype=torch.uint8, device="cuda")
+    B.fcp_cache_evict(cache, dev(pages), dev(kv_len), dev(new_pages), 20, 1, 4, kept, new_len, scratch)
+    want_kept, want_len = ref.evict(pages, kv_len, new_pages, 20, 1, 4)
+    assert np.array_equal(kept.cpu().numpy(), want_kept) and np.array_equal(new_len.cpu().numpy(), want_len)
     R.check_content(cache, ref)
