@@ -29,7 +29,7 @@ struct AttnArgs {
 // The line of the tiles of all items, and its division among blocks.  Sequence s has, for every KV head and every block of `rows` rows, all of its tiles (a sequence without
 // cached tokens one empty tile, which writes O = 0).  Lead: places before an item's first tile, for what a block does for an item whatever its tiles; kWhole: an item is one place on the
 // line, so that it lies in one block.
-// Places are 32-bit numbers: the host sees to it that there are fewer than 2^31.
+// Places are 32-bit numbers: the host sees to it that there are at most kMostPlaces.
 struct Line {
   int32_t total;                       // places
   int32_t before;                      // those of the sequences before `seq`

@@ -682,6 +682,9 @@ AttnPlan plan_attn(const CacheView& c, int head_dim, int32_t n_seqs, int32_t max
   return p;
 }
 
+// Places are 32-bit numbers, and so is the one that a block of the weights' kernel, one of up to 2 kBlocks, steps to past the last.
+constexpr int64_t kMostPlaces = INT32_MAX - 2 * kBlocks;
+
 // slots, and who the divided items are
 size_t part_bytes(const AttnPlan& p) { return pad_to((size_t)p.part_floats * 4, 256) + pad_to(kBlocks * sizeof(Divided), 256); }
 
@@ -773,7 +776,7 @@ extern "C" int fcp_cache_attn(const fcp_cache* cache, const void* q, int64_t q_r
   if (!o || !lse || (uintptr_t)o % 16 || (uintptr_t)lse % 4) return fail(FCP_ERR_INVALID_ARG, "%s: o and lse are required and must be aligned", who);
   if (!scratch || (uintptr_t)scratch % 256) return fail(FCP_ERR_INVALID_ARG, "%s: scratch must be 256-byte aligned", who);
   const AttnPlan p = plan_attn(a.c, cache->head_dim, n_seqs, max_pages, tq, hq, weigh);
-  if (p.places > INT32_MAX) return fail(FCP_ERR_UNSUPPORTED, "%s: tables and rows that may make 2^31 tiles of work", who);
+  if (p.places > kMostPlaces) return fail(FCP_ERR_UNSUPPORTED, "%s: tables and rows that may make 2^31 tiles of work", who);
   const size_t need = part_bytes(p) + pad_to((size_t)p.score_floats * 4, 256);
   if (scratch_bytes < need) return fail(FCP_ERR_CAPACITY, "%s: scratch has %zu bytes, %zu are needed", who, scratch_bytes, need);
   a.s = {cu_seqlens, kv_len, pages, n_seqs, max_pages, tq};
@@ -811,7 +814,7 @@ extern "C" int fcp_cache_weigh(const fcp_cache* cache, const void* q, int64_t q_
   if (tq == 0 || n_seqs == 0) return FCP_OK;
   if (int rc = check_rows(who, cache, q, q_row, tq, hq)) return rc;
   if (!lse || (uintptr_t)lse % 4) return fail(FCP_ERR_INVALID_ARG, "%s: lse is required", who);
-  if (plan_attn(a.c, cache->head_dim, n_seqs, max_pages, tq, hq, false).places > INT32_MAX)
+  if (plan_attn(a.c, cache->head_dim, n_seqs, max_pages, tq, hq, false).places > kMostPlaces)
     return fail(FCP_ERR_UNSUPPORTED, "%s: tables and rows that may make 2^31 tiles of work", who);
   a.s = {cu_seqlens, kv_len, pages, n_seqs, max_pages, tq};
   a.q = static_cast<const __bf16*>(q);

@@ -20,6 +20,14 @@ def test_launches_of_too_many_threads_are_refused_before_any_device_work():
     assert B.lib().fcp_rotary(p, 1, Call.fake, 1024, 1024, 0, 1.0, 0, None) == no and b"2^24" in B.lib().fcp_last_error()
 
 
+def test_places_that_a_step_would_take_past_32_bits_are_refused():
+    """A block of the weights' kernel steps 1024 places at a time, past the last one too: 2^31 - 128 places and their likes were let through."""
+    call = lambda op, pages, heads: getattr(Call(hkv=heads, hq=heads, q_row=128 * heads, n_seqs=1, tq=1, max_pages=pages, bytes=0), op)()
+    for pages, heads in (((1 << 24) - 5, 128), ((1 << 23) - 5, 256)):
+        assert call("attn", pages, heads) == call("weigh", pages, heads) == B.FCP_ERR_UNSUPPORTED, (pages, heads)
+    assert call("attn", (1 << 20) - 5, 2048) == B.FCP_ERR_CAPACITY             # 2^31 - 2048: scratch is what is missing
+
+
 # ---- GPU ------------------------------------------------------------------------------------------------------------------------------------
 def check_weights(got, before, W, eps, rows):
     """As test_cache.check_weight where the sums are finite; elsewhere the same NaN and infinity."""
