@@ -127,8 +127,9 @@ __device__ inline float wave_maxf(float x) {
 }
 
 // ---- host ---------------------------------------------------------------------------------------
-// Checks what every call of the cache checks, and fills the view.  needs_weight: the call reads or writes weights.
+// Checks what every call of the cache checks, and fills the view.  needs_weight: the call reads or writes weights.  Sizes apart: those who only ask for scratch have no tables yet.
 int check_cache(const char* who, const fcp_cache* cache, bool needs_weight, CacheView* out);
-int check_seqs(const char* who, const fcp_cache& c, const int32_t* cu, bool needs_cu, const int32_t* kv_len, const int32_t* pages, int32_t n_seqs, int32_t max_pages, int32_t n_rows);
+int check_sizes(const char* who, const CacheView& c, int32_t n_seqs, int32_t max_pages, int32_t n_rows);
+int check_seqs(const char* who, const CacheView& c, const int32_t* cu, bool needs_cu, const int32_t* kv_len, const int32_t* pages, int32_t n_seqs, int32_t max_pages, int32_t n_rows);
 
 }  // namespace fcp

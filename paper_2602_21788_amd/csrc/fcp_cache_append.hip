@@ -276,11 +276,16 @@ int check_cache(const char* who, const fcp_cache* cache, bool needs_weight, Cach
   return FCP_OK;
 }
 
-int check_seqs(const char* who, const fcp_cache& c, const int32_t* cu, bool needs_cu, const int32_t* kv_len, const int32_t* pages, int32_t n_seqs, int32_t max_pages, int32_t n_rows) {
+int check_sizes(const char* who, const CacheView& c, int32_t n_seqs, int32_t max_pages, int32_t n_rows) {
   if (n_seqs < 0 || max_pages < 0 || n_rows < 0) return fail(FCP_ERR_INVALID_ARG, "%s: negative size", who);
-  if (n_seqs > 0 && ((needs_cu && !cu) || !kv_len || (max_pages > 0 && !pages))) return fail(FCP_ERR_INVALID_ARG, "%s: null argument", who);
   if (n_seqs > 1 << 20) return fail(FCP_ERR_UNSUPPORTED, "%s: more than 2^20 sequences", who);
-  if ((int64_t)max_pages * c.page_tokens > 1 << 30) return fail(FCP_ERR_UNSUPPORTED, "%s: a table of more than 2^30 tokens", who);
+  if ((int64_t)max_pages * c.page > 1 << 30) return fail(FCP_ERR_UNSUPPORTED, "%s: a table of more than 2^30 tokens", who);
+  return FCP_OK;
+}
+
+int check_seqs(const char* who, const CacheView& c, const int32_t* cu, bool needs_cu, const int32_t* kv_len, const int32_t* pages, int32_t n_seqs, int32_t max_pages, int32_t n_rows) {
+  if (int rc = check_sizes(who, c, n_seqs, max_pages, n_rows)) return rc;
+  if (n_seqs > 0 && ((needs_cu && !cu) || !kv_len || (max_pages > 0 && !pages))) return fail(FCP_ERR_INVALID_ARG, "%s: null argument", who);
   return FCP_OK;
 }
 
@@ -293,7 +298,7 @@ extern "C" int fcp_cache_append(const fcp_cache* cache, const void* k, int64_t k
   const char* who = "fcp_cache_append";
   AppendArgs a = {};
   if (int rc = check_cache(who, cache, false, &a.c)) return rc;
-  if (int rc = check_seqs(who, *cache, cu_seqlens, true, kv_len, pages, n_seqs, max_pages, n_rows)) return rc;
+  if (int rc = check_seqs(who, a.c, cu_seqlens, true, kv_len, pages, n_seqs, max_pages, n_rows)) return rc;
   if (n_rows == 0 || n_seqs == 0 || max_pages == 0) return FCP_OK;
   if (!k || !v) return fail(FCP_ERR_INVALID_ARG, "%s: null argument", who);
   const int64_t width = (int64_t)cache->hkv * cache->head_dim;

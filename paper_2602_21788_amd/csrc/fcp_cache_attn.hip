@@ -687,6 +687,8 @@ constexpr int64_t kMostPlaces = INT32_MAX - 2 * kBlocks;
 
 // slots, and who the divided items are
 size_t part_bytes(const AttnPlan& p) { return pad_to((size_t)p.part_floats * 4, 256) + pad_to(kBlocks * sizeof(Divided), 256); }
+// .. and kept scores
+size_t attn_bytes(const AttnPlan& p) { return part_bytes(p) + pad_to((size_t)p.score_floats * 4, 256); }
 
 template <int D, int Fmt>
 int launch_attn(const AttnArgs& a, const AttnPlan& p, hipStream_t st) {
@@ -730,17 +732,23 @@ int check_scale(const char* who, float scale) {
   if (!(scale >= 0x1p-32f) || !__builtin_isfinite(scale)) return fail(FCP_ERR_INVALID_ARG, "%s: softmax_scale must be finite and at least 2^-32", who);
   return FCP_OK;
 }
+int check_row_count(const char* who, int32_t tq, int32_t hq) {
+  if ((int64_t)tq * hq > INT32_MAX - 256) return fail(FCP_ERR_UNSUPPORTED, "%s: more than 2^31 rows of all heads", who);
+  return FCP_OK;
+}
 int check_rows(const char* who, const fcp_cache* cache, const void* q, int64_t q_row, int32_t tq, int32_t hq) {
   if (!q || q_row < (int64_t)hq * cache->head_dim || q_row % 8 || (uintptr_t)q % 16)
     return fail(FCP_ERR_INVALID_ARG, "%s: query rows must be at least hq * head_dim elements apart, a multiple of 8, and 16-byte aligned", who);
-  if ((int64_t)tq * hq > INT32_MAX - 256)
-    return fail(FCP_ERR_UNSUPPORTED, "%s: more than 2^31 rows of all heads", who);
+  return check_row_count(who, tq, hq);
+}
+int check_places(const char* who, const AttnPlan& p) {
+  if (p.places > kMostPlaces) return fail(FCP_ERR_UNSUPPORTED, "%s: tables and rows that may make 2^31 tiles of work", who);
   return FCP_OK;
 }
 
 }  // namespace
 
-size_t evict_scratch_bytes(const CacheView& c, int32_t n_seqs, int32_t max_pages);
+size_t evict_scratch_bytes(const char* who, const CacheView& c, int32_t n_seqs, int32_t max_pages);       // 0: refused
 
 }  // namespace fcp
 
@@ -750,13 +758,14 @@ extern "C" size_t fcp_cache_scratch_bytes(int which, const fcp_cache* cache, int
   const char* who = "fcp_cache_scratch_bytes";
   CacheView c;
   if (check_cache(who, cache, which != FCP_SCRATCH_CACHE_ATTN, &c)) return 0;
-  if (n_seqs < 0 || max_pages < 0 || tq < 0) { fail(FCP_ERR_INVALID_ARG, "%s: negative size", who); return 0; }
-  if (which == FCP_SCRATCH_CACHE_EVICT) return evict_scratch_bytes(c, n_seqs, max_pages);
+  if (check_sizes(who, c, n_seqs, max_pages, tq)) return 0;
+  if (which == FCP_SCRATCH_CACHE_EVICT) return evict_scratch_bytes(who, c, n_seqs, max_pages);
   if (which != FCP_SCRATCH_CACHE_ATTN && which != FCP_SCRATCH_CACHE_WEIGH) { fail(FCP_ERR_INVALID_ARG, "%s: which = %d is not known", who, which); return 0; }
   if (check_heads(who, c, hq)) return 0;
   const bool weigh = which == FCP_SCRATCH_CACHE_WEIGH;
   const AttnPlan p = plan_attn(c, cache->head_dim, n_seqs, max_pages, tq, hq, weigh);
-  return part_bytes(p) + pad_to((size_t)p.score_floats * 4, 256);
+  if (n_seqs > 0 && tq > 0 && (check_row_count(who, tq, hq) || check_places(who, p))) return 0;
+  return attn_bytes(p);
 }
 
 extern "C" int fcp_cache_attn(const fcp_cache* cache, const void* q, int64_t q_row, int32_t tq, int32_t hq, const int32_t* cu_seqlens,
@@ -769,15 +778,15 @@ extern "C" int fcp_cache_attn(const fcp_cache* cache, const void* q, int64_t q_r
   if (weigh != 0 && weigh != 1) return fail(FCP_ERR_INVALID_ARG, "%s: weigh must be 0 or 1", who);
   if (int rc = check_cache(who, cache, weigh, &a.c)) return rc;
   if (int rc = check_heads(who, a.c, hq)) return rc;
-  if (int rc = check_seqs(who, *cache, cu_seqlens, true, kv_len, pages, n_seqs, max_pages, tq)) return rc;
+  if (int rc = check_seqs(who, a.c, cu_seqlens, true, kv_len, pages, n_seqs, max_pages, tq)) return rc;
   if (int rc = check_scale(who, softmax_scale)) return rc;
   if (tq == 0 || n_seqs == 0) return FCP_OK;
   if (int rc = check_rows(who, cache, q, q_row, tq, hq)) return rc;
   if (!o || !lse || (uintptr_t)o % 16 || (uintptr_t)lse % 4) return fail(FCP_ERR_INVALID_ARG, "%s: o and lse are required and must be aligned", who);
   if (!scratch || (uintptr_t)scratch % 256) return fail(FCP_ERR_INVALID_ARG, "%s: scratch must be 256-byte aligned", who);
   const AttnPlan p = plan_attn(a.c, cache->head_dim, n_seqs, max_pages, tq, hq, weigh);
-  if (p.places > kMostPlaces) return fail(FCP_ERR_UNSUPPORTED, "%s: tables and rows that may make 2^31 tiles of work", who);
-  const size_t need = part_bytes(p) + pad_to((size_t)p.score_floats * 4, 256);
+  if (int rc = check_places(who, p)) return rc;
+  const size_t need = attn_bytes(p);
   if (scratch_bytes < need) return fail(FCP_ERR_CAPACITY, "%s: scratch has %zu bytes, %zu are needed", who, scratch_bytes, need);
   a.s = {cu_seqlens, kv_len, pages, n_seqs, max_pages, tq};
   a.q = static_cast<const __bf16*>(q);
@@ -809,13 +818,12 @@ extern "C" int fcp_cache_weigh(const fcp_cache* cache, const void* q, int64_t q_
   WeighArgs a = {};
   if (int rc = check_cache(who, cache, true, &a.c)) return rc;
   if (int rc = check_heads(who, a.c, hq)) return rc;
-  if (int rc = check_seqs(who, *cache, cu_seqlens, true, kv_len, pages, n_seqs, max_pages, tq)) return rc;
+  if (int rc = check_seqs(who, a.c, cu_seqlens, true, kv_len, pages, n_seqs, max_pages, tq)) return rc;
   if (int rc = check_scale(who, softmax_scale)) return rc;
   if (tq == 0 || n_seqs == 0) return FCP_OK;
   if (int rc = check_rows(who, cache, q, q_row, tq, hq)) return rc;
   if (!lse || (uintptr_t)lse % 4) return fail(FCP_ERR_INVALID_ARG, "%s: lse is required", who);
-  if (plan_attn(a.c, cache->head_dim, n_seqs, max_pages, tq, hq, false).places > kMostPlaces)
-    return fail(FCP_ERR_UNSUPPORTED, "%s: tables and rows that may make 2^31 tiles of work", who);
+  if (int rc = check_places(who, plan_attn(a.c, cache->head_dim, n_seqs, max_pages, tq, hq, false))) return rc;
   a.s = {cu_seqlens, kv_len, pages, n_seqs, max_pages, tq};
   a.q = static_cast<const __bf16*>(q);
   a.q_row = q_row;

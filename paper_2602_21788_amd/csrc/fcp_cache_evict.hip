@@ -504,9 +504,16 @@ EvictPlan plan_evict(const CacheView& c, int32_t n_seqs, int32_t max_pages) {
   return p;
 }
 
+int check_lists(const char* who, const CacheView& c, int32_t n_seqs) {
+  if (!fits_axis((int64_t)n_seqs * c.hkv, kSelectThreads)) return fail(FCP_ERR_UNSUPPORTED, "%s: 2^22 KV heads of all sequences or more", who);
+  return FCP_OK;
+}
+
 }  // namespace
 
-size_t evict_scratch_bytes(const CacheView& c, int32_t n_seqs, int32_t max_pages) { return plan_evict(c, n_seqs, max_pages).bytes; }
+size_t evict_scratch_bytes(const char* who, const CacheView& c, int32_t n_seqs, int32_t max_pages) {
+  return check_lists(who, c, n_seqs) ? 0 : plan_evict(c, n_seqs, max_pages).bytes;
+}
 
 }  // namespace fcp
 
@@ -518,7 +525,7 @@ extern "C" int fcp_cache_evict(const fcp_cache* cache, const int32_t* pages, con
   const char* who = "fcp_cache_evict";
   EvictArgs a = {};
   if (int rc = check_cache(who, cache, true, &a.c)) return rc;
-  if (int rc = check_seqs(who, *cache, nullptr, false, kv_len, pages, n_seqs, max_pages, 0)) return rc;
+  if (int rc = check_seqs(who, a.c, nullptr, false, kv_len, pages, n_seqs, max_pages, 0)) return rc;
   if (n_first < 0 || n_recent < 0 || budget < 1 || (int64_t)n_first + n_recent > budget)
     return fail(FCP_ERR_INVALID_ARG, "%s: budget must be at least 1 and n_first + n_recent, which must not be negative", who);
   if (max_new_pages < 0) return fail(FCP_ERR_INVALID_ARG, "%s: negative size", who);
@@ -533,8 +540,8 @@ extern "C" int fcp_cache_evict(const fcp_cache* cache, const int32_t* pages, con
   const size_t need = p.bytes;
   if (scratch_bytes < need) return fail(FCP_ERR_CAPACITY, "%s: scratch has %zu bytes, %zu are needed", who, scratch_bytes, need);
   const int64_t use = (most + a.c.page - 1) / a.c.page;      // (further entries of new_pages are not used)
-  if (!fits_axis((int64_t)n_seqs * a.c.hkv, kSelectThreads) || !fits_axis((int64_t)n_seqs * use, 256))
-    return fail(FCP_ERR_UNSUPPORTED, "%s: 2^22 KV heads or 2^24 new pages of all sequences, or more", who);
+  if (int rc = check_lists(who, a.c, n_seqs)) return rc;
+  if (!fits_axis((int64_t)n_seqs * use, 256)) return fail(FCP_ERR_UNSUPPORTED, "%s: 2^24 new pages of all sequences or more", who);
   a.s = {nullptr, kv_len, pages, n_seqs, max_pages, 0};
   a.new_pages = new_pages;
   a.max_new = max_new_pages;

@@ -28,6 +28,25 @@ def test_places_that_a_step_would_take_past_32_bits_are_refused():
     assert call("attn", (1 << 20) - 5, 2048) == B.FCP_ERR_CAPACITY             # 2^31 - 2048: scratch is what is missing
 
 
+def test_scratch_is_refused_where_the_call_is():
+    f = B.fcp_cache_scratch_bytes
+    sizes = lambda which, n_seqs, max_pages, tq=4, hq=16, **c: f(which, Call(**c).c, n_seqs, max_pages, tq, hq)
+    which = (B.FCP_SCRATCH_CACHE_ATTN, B.FCP_SCRATCH_CACHE_WEIGH, B.FCP_SCRATCH_CACHE_EVICT)
+    for w in which:
+        for n_seqs, max_pages in (((1 << 20) + 1, 4), (4, (1 << 24) + 1), (-1, 4), (4, -1)):
+            with pytest.raises(B.FcpError):
+                sizes(w, n_seqs, max_pages)
+        assert sizes(w, 4, 1 << 24, hkv=1, hq=1) > 0 and sizes(w, 0, 4) > 0
+    for w in which[:2]:
+        for n_seqs, max_pages, tq, hq in ((4, 4, 1 << 27, 16), (1 << 20, 1 << 10, 4, 16), (4, 4, 4, 6)):
+            with pytest.raises(B.FcpError):
+                sizes(w, n_seqs, max_pages, tq, hq)
+            assert Call(n_seqs=n_seqs, max_pages=max_pages, tq=tq, hq=hq, q_row=128 * hq).attn() == B.FCP_ERR_UNSUPPORTED
+        assert sizes(w, 4, 4, tq=0) > 0
+    with pytest.raises(B.FcpError):
+        sizes(which[2], 1 << 20, 1)
+
+
 # ---- GPU ------------------------------------------------------------------------------------------------------------------------------------
 def check_weights(got, before, W, eps, rows):
     """As test_cache.check_weight where the sums are finite; elsewhere the same NaN and infinity."""
