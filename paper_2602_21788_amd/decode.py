@@ -8,6 +8,8 @@ Only buffers and tables live here (which pages a sequence owns, how long it is, 
 """
 from __future__ import annotations
 
+from contextlib import contextmanager
+
 import numpy as np
 import torch
 
@@ -53,22 +55,46 @@ class CacheDecoder:
             self._scratch[which] = torch.empty(n, dtype=torch.uint8, device=self.device)
         return self._scratch[which]
 
-    def _grow(self, news):
-        """Room for news[s] more tokens of every sequence; (cu_seqlens, positions) of the new rows."""
+    def _counts(self, news):
+        news = np.asarray(news, np.int32)
         if news.shape != self.kv_len.shape or (news < 0).any():
             raise ValueError("a number of tokens, 0 or more, is needed for every sequence")
+        return news
+
+    def _fit(self, q, k, v, rows, whole=False):
+        """Refuses rows that a call of the path would refuse, before pages change hands.  whole: nothing between rows, as prompts' attention takes them."""
+        for name, x, h in (("q", q, self.hq), ("k", k, self.hkv), ("v", v, self.hkv)):
+            at, row = B._rows(x, h, self.D, name)
+            if x.shape[0] != rows:
+                raise ValueError(f"{name} must have {rows} rows, one for each new token")
+            if x.device != self.cache.k.device or row < h * self.D or row % 8 or at % 16 or (whole and not x.is_contiguous()):
+                raise ValueError(f"{name} must be on the cache's device, 16-byte aligned, {'contiguous' if whole else 'its rows a multiple of 8 elements apart'}")
+
+    @contextmanager
+    def _grown(self, news):
+        """Room for news[s] more tokens of every sequence: (cu_seqlens, positions) of the new rows.  Where something fails inside, the tables are as they were."""
         need = [-(-(int(n) + int(m)) // self.P) - int((row >= 0).sum()) for n, m, row in zip(self.kv_len, news, self.pages)]
         if sum(max(n, 0) for n in need) > len(self.free) or (self.kv_len + news > self.pages.shape[1] * self.P).any():
             raise MemoryError("no page left: evict, or close a sequence")
+        taken = []
         for s, n in enumerate(need):
             at = int((self.pages[s] >= 0).sum())
             for i in range(n):
                 self.pages[s, at + i] = self.free.pop()
+                taken.append((s, at + i))
         pos = np.concatenate([np.arange(p, p + m) for p, m in zip(self.next_pos, news)]) if sum(news) else np.zeros(0)
         self.kv_len += news
         self.next_pos += news
-        self._upload()
-        return self._to(np.concatenate([[0], np.cumsum(news)])), self._to(pos)
+        try:
+            self._upload()
+            yield self._to(np.concatenate([[0], np.cumsum(news)])), self._to(pos)
+        except BaseException:
+            for at in reversed(taken):
+                self.free.append(int(self.pages[at]))
+                self.pages[at] = -1
+            self.kv_len -= news
+            self.next_pos -= news
+            raise
 
     def close(self, seq):
         """Forgets a sequence; its pages are free."""
@@ -82,34 +108,33 @@ class CacheDecoder:
     # -- the path ----------------------------------------------------------------------------------------------------------
     def prefill(self, q, k, v, lens):
         """Prompts of lens[s] tokens for empty sequences: bf16 rows q [sum, hq, D], k, v [sum, hkv, D] (turned in place).  Returns O [sum, hq, D], LSE [hq, sum]."""
-        lens = np.asarray(lens, np.int32)
-        if not q.shape[0] == k.shape[0] == v.shape[0] == lens.sum():
-            raise ValueError("q, k and v must have sum(lens) rows")
+        lens = self._counts(lens)
+        self._fit(q, k, v, int(lens.sum()), whole=True)
         if self.kv_len.any():
             raise ValueError("prefill is for empty sequences; step() takes the next piece of a prompt")
-        cu, pos = self._grow(lens)
-        self._rotate(q, k, pos)
         some = lens[lens > 0]
         ra = RankAttention(some, np.ones(len(some), np.int32), 0, self.hq, self.hkv, self.D, self.scale, device=self.device)
         ra.q, ra.k, ra.v, ra.d_o = q, k, v, None
         ra._alloc_outputs()
-        ra.forward_direct()
-        B.fcp_cache_append(self.cache, k, v, cu, self.kv_len_d, self.pages_d)
-        B.fcp_cache_weigh(self.cache, q, ra.lse, cu, self.kv_len_d, self.pages_d, self.scale)
+        with self._grown(lens) as (cu, pos):
+            self._rotate(q, k, pos)
+            ra.forward_direct()
+            B.fcp_cache_append(self.cache, k, v, cu, self.kv_len_d, self.pages_d)
+            B.fcp_cache_weigh(self.cache, q, ra.lse, cu, self.kv_len_d, self.pages_d, self.scale)
         return ra.o, ra.lse
 
     def step(self, q, k, v, news, weigh=True):
         """news[s] new tokens of every sequence (0, 1, or more): bf16 rows as in prefill.  Returns O [sum, hq, D], LSE [hq, sum]."""
-        news = np.asarray(news, np.int32)
-        if not q.shape[0] == k.shape[0] == v.shape[0] == news.sum():
-            raise ValueError("q, k and v must have sum(news) rows")
-        cu, pos = self._grow(news)
-        self._rotate(q, k, pos)
-        B.fcp_cache_append(self.cache, k, v, cu, self.kv_len_d, self.pages_d)
+        news = self._counts(news)
+        self._fit(q, k, v, int(news.sum()))
         o = torch.empty(q.shape, dtype=torch.bfloat16, device=self.device)
         lse = torch.empty(q.shape[1], q.shape[0], dtype=torch.float32, device=self.device)
         which = B.FCP_SCRATCH_CACHE_WEIGH if weigh else B.FCP_SCRATCH_CACHE_ATTN
-        B.fcp_cache_attn(self.cache, q, cu, self.kv_len_d, self.pages_d, self.scale, o, lse, self._work(which, q.shape[0]), weigh=weigh)
+        scratch = self._work(which, q.shape[0])
+        with self._grown(news) as (cu, pos):
+            self._rotate(q, k, pos)
+            B.fcp_cache_append(self.cache, k, v, cu, self.kv_len_d, self.pages_d)
+            B.fcp_cache_attn(self.cache, q, cu, self.kv_len_d, self.pages_d, self.scale, o, lse, scratch, weigh=weigh)
         return o, lse
 
     def evict(self, budget, n_first=4, n_recent=64):
@@ -123,13 +148,15 @@ class CacheDecoder:
         if counts.sum() > len(self.free):
             raise MemoryError("eviction moves tokens to new pages, and there are too few")
         new_pages = np.full((len(new_len), width), -1, np.int32)
+        taken = 0
         for s, n in enumerate(counts):
             for i in range(n):
-                new_pages[s, i] = self.free.pop()
+                taken += 1
+                new_pages[s, i] = self.free[-taken]
         kept = torch.empty(len(new_len), self.hkv, budget, dtype=torch.int32, device=self.device)
         B.fcp_cache_evict(self.cache, self.pages_d, self.kv_len_d, self._to(new_pages), budget, n_first, n_recent, kept,
                           torch.empty(len(new_len), dtype=torch.int32, device=self.device), self._work(B.FCP_SCRATCH_CACHE_EVICT))
-        self.free += [int(p) for p in self.pages[self.pages >= 0]]
+        self.free = self.free[: len(self.free) - taken] + [int(p) for p in self.pages[self.pages >= 0]]
         self.pages[:] = -1
         self.pages[:, :width] = new_pages[:, : self.pages.shape[1]]
         self.kv_len = new_len

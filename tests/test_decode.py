@@ -107,3 +107,65 @@ def test_refusals_change_nothing():
     with pytest.raises(MemoryError):
         dec.step(rows(90, 4), rows(90, 2), rows(90, 2), [20, 70])
     assert dec.free == free and np.array_equal(dec.kv_len, lens) and np.array_equal(dec.pages, pages)
+
+
+def state(dec):
+    return list(dec.free), dec.kv_len.tolist(), dec.next_pos.tolist(), dec.pages.tolist()
+
+
+@pytest.mark.gpu
+def test_rows_of_another_kind_change_nothing():
+    """Heads, channels, types and layouts that do not fit are refused before tokens are counted, pages taken or rows turned."""
+    import torch
+    from paper_2602_21788_amd.decode import CacheDecoder
+    g = torch.Generator(device="cuda").manual_seed(6)
+    rows = lambda n, h, d=64: bf16_rows(torch, g, n, h, d)
+    good = rows(40, 4), rows(40, 2), rows(40, 2)
+    for begun in (False, True):
+        dec = CacheDecoder(2, 12, 6, 4, 2, 64, page_tokens=16)
+        if begun:
+            dec.prefill(*(x.clone() for x in good), [30, 10])
+        before = state(dec)
+        call = dec.step if begun else dec.prefill
+        for at, heads in ((0, 4), (1, 2), (2, 2)):
+            h = heads
+            wide = rows(40, h + 1)
+            for bad in (rows(40, h + 1), rows(40, h, 128), rows(40, h).float(), rows(40, h).cpu(), rows(40, h).reshape(40, -1), wide.transpose(1, 2), rows(39, h),
+                        rows(40, h, 65)[:, :, 1:], torch.zeros(40 * (h * 64 + 4), dtype=torch.bfloat16, device="cuda").as_strided((40, h, 64), (h * 64 + 4, 64, 1))):
+                args = [x.clone() for x in good]
+                args[at] = bad
+                with pytest.raises(ValueError):
+                    call(*args, [15, 25])
+                assert state(dec) == before
+                assert all(torch.equal(x, y) for i, (x, y) in enumerate(zip(args, good)) if i != at)
+        o, _ = call(*(x.clone() for x in good), [15, 25])
+        assert torch.isfinite(o.float()).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("where", ["_work", "fcp_rotary", "fcp_cache_append", "fcp_cache_attn", "fcp_cache_weigh", "fcp_cache_evict", "_to"])
+def test_failures_leave_the_tables_as_they_were(where, monkeypatch):
+    """Memory that is not there, or a call that fails: the decoder counts no token that it does not answer, and the next call works."""
+    import torch
+    from paper_2602_21788_amd import decode
+    g = torch.Generator(device="cuda").manual_seed(7)
+    rows = lambda n: (bf16_rows(torch, g, n, 4, 64), bf16_rows(torch, g, n, 2, 64), bf16_rows(torch, g, n, 2, 64))
+    dec = decode.CacheDecoder(2, 24, 6, 4, 2, 64, page_tokens=16)
+    calls = {"prefill": lambda: dec.prefill(*rows(40), [30, 10]), "step": lambda: dec.step(*rows(9), [4, 5]), "evict": lambda: dec.evict(20, 1, 4)}
+    failing = {"fcp_rotary": ("prefill", "step"), "_to": ("prefill", "step", "evict"), "fcp_cache_append": ("prefill", "step"), "fcp_cache_attn": ("step",),
+               "fcp_cache_weigh": ("prefill",), "fcp_cache_evict": ("evict",), "_work": ("step", "evict")}[where]
+    for name, call in calls.items():
+        if name in failing:
+            before = state(dec)
+
+            def fail(*a, **kw):
+                raise torch.OutOfMemoryError("none left")
+
+            with monkeypatch.context() as m:
+                m.setattr(decode.B if where.startswith("fcp") else dec, where, fail)
+                with pytest.raises(torch.OutOfMemoryError):
+                    call()
+            assert state(dec) == before, name
+        call()
+    lens, pages = dec.kv_len.tolist(), dec.pages
+    assert lens == [20, 15] and sorted(dec.free + pages[pages >= 0].tolist()) == list(range(24))
