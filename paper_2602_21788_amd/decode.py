@@ -113,6 +113,8 @@ class CacheDecoder:
         if self.kv_len.any():
             raise ValueError("prefill is for empty sequences; step() takes the next piece of a prompt")
         some = lens[lens > 0]
+        if not len(some):
+            return torch.empty_like(q), torch.empty(self.hq, 0, dtype=torch.float32, device=self.device)
         ra = RankAttention(some, np.ones(len(some), np.int32), 0, self.hq, self.hkv, self.D, self.scale, device=self.device)
         ra.q, ra.k, ra.v, ra.d_o = q, k, v, None
         ra._alloc_outputs()

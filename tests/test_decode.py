@@ -169,3 +169,15 @@ def test_failures_leave_the_tables_as_they_were(where, monkeypatch):
         call()
     lens, pages = dec.kv_len.tolist(), dec.pages
     assert lens == [20, 15] and sorted(dec.free + pages[pages >= 0].tolist()) == list(range(24))
+
+
+@pytest.mark.gpu
+def test_no_tokens_at_all():
+    import torch
+    from paper_2602_21788_amd.decode import CacheDecoder
+    dec = CacheDecoder(2, 8, 4, 4, 2, 64, page_tokens=16)
+    none = lambda h: torch.empty(0, h, 64, dtype=torch.bfloat16, device="cuda")
+    for call in (dec.prefill, dec.step):
+        o, lse = call(none(4), none(2), none(2), [0, 0])
+        assert o.shape == (0, 4, 64) and lse.shape == (4, 0)
+    assert dec.evict(16, 1, 4).eq(-1).all() and dec.kv_len.tolist() == [0, 0] and len(dec.free) == 8
