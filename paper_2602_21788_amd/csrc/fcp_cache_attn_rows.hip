@@ -85,10 +85,17 @@ __device__ inline void load_share(const AttnArgs& a, const uint8_t* codes, const
     const int key = tile * kTile + kGroup * group_of<D>(wave, i);
     const int64_t block = block_of(a.c, max(pages.of[i], 0), head), at = (block * a.c.page + (key & (a.c.page - 1))) * D + 1024 * lot_of<D>(wave);
     s.live[i] = pages.of[i] < 0 ? 0 : min(len - key, kGroup);
-    const float scale = as_scalar(scales)[block];
-    s.scale[i] = pages.of[i] < 0 ? 1.f : scale;            // (that of an unused page is whatever it holds, and 0 * NaN is NaN)
+    s.scale[i] = as_scalar(scales)[block];
     s.w[i] = *reinterpret_cast<const u32x4*>(codes + at + 16 * (int)(threadIdx.x & 63));
   }
+}
+
+// The scale of a page that is not there is whatever the pool's first page holds, and 0 * NaN is NaN: 1 takes its place.  (Where the share is used: done where it is asked for this would wait
+// for the load.  64 sequences of up to 16384 tokens, 16 new each, int8: 216 us, 228 there.)
+template <int D>
+__device__ inline void settle_scales(Share<D>& s) {
+#pragma unroll
+  for (int i = 0; i < D / 64; ++i) s.scale[i] = s.live[i] ? s.scale[i] : 1.f;
 }
 
 // partly: some row of the block does not see the whole tile.  Its product with a NaN value would be NaN too, so zero takes that place, and the first such token of each channel is
@@ -219,6 +226,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(AttnArgs a) {
         if (Fmt == kE4m3 && t * kTile + kTile - 1 > all_see) without_nan<D>(values, wave, first_nan[parity], t * kTile);
       };
       auto note_live = [&](int t) {
+        settle_scales<D>(keys);
 #pragma unroll
         for (int i = 0; i < D / 64; ++i)
           if (lane == 0) live[t & 3][group_of<D>(wave, i)] = keys.live[i], key_scale[t & 3][group_of<D>(wave, i)] = keys.scale[i];
@@ -238,6 +246,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(AttnArgs a) {
       store_keys(t0);
       ask_keys(t0 + 1);
       tidy(t0);
+      settle_scales<D>(values);
       bf16x8 half;
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) store_word<D, Fmt, true>(values, i, wave, value_place, stage_of(t0), half);
@@ -289,6 +298,7 @@ __global__ __launch_bounds__(256, 2) void attn_rows_kernel(AttnArgs a) {
           for (int b = 0; b < kNB; ++b) asm volatile("" : "+v"(l[b]));
         });
         __builtin_amdgcn_sched_barrier(0);
+        settle_scales<D>(values);
         const int v0 = fresh(value_operand);
         stream_operands<D / 8>([&](int i) { return *reinterpret_cast<const chunk*>(stage_of(t) + (v0 ^ (i / 4 % 2 << 6)) + 16 * (i / 8 * 4 + i % 4) * Stage<D>::kValueRow); },
                                [&](int i, bf16x8 v) {
