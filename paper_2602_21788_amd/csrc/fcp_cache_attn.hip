@@ -533,6 +533,7 @@ __global__ __launch_bounds__(kWeighThreads, 2) void weigh_kernel(WeighArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[i][j], q[j], s[i], 0, 0, 0);
       if (__ballot(last < 15)) {
+        if (!__ballot(last >= 0)) return;
         // (chosen behind the exponential: a score or an LSE that is NaN must not reach keys that the row does not see)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
