@@ -455,7 +455,10 @@ int fcp_rotary(const fcp_rotary_part* parts, int32_t n_parts, const double* turn
  * Sequence s owns the pages pages[s][0], pages[s][1], ...: its token t is slot t % page_tokens of page pages[s][t / page_tokens].  kv_len[s] tokens
  * are cached; in every call below that takes queries or new rows, the n = cu_seqlens[s + 1] - cu_seqlens[s] rows of sequence s are its LAST n tokens,
  * and kv_len counts them.  Both tables are device memory, so that a captured graph follows them.  A page number outside 0 .. n_pages - 1 is not
- * followed: the tokens in it are not written, and seen by nobody.  cu_seqlens must not fall: where it does, the calls that take queries do nothing at all.
+ * followed: the tokens in it are not written, and seen by nobody.  The scales of pages that hold no token are not looked at.  cu_seqlens must not fall: where it does, the calls that take queries do nothing at all.
+ * Sequences may share the pages of a common beginning as long as these are only read: fcp_cache_attn without weigh, the old pages of fcp_cache_evict.  A page whose weights are
+ * added to (weigh, fcp_cache_weigh) must belong to one place of one sequence of the call: what two add at the same time is lost in part, differently each time.
+ * Scaled scores of a magnitude up to 2^26 and values up to 2^80 keep all sums within 32-bit floats' range; beyond, rows may become infinite or NaN.
  * softmax_scale: finite, at least 2^-32.  kv_len is taken as at most max_pages * page_tokens, which is at most 2^30 (FCP_ERR_UNSUPPORTED beyond).
  */
 #define FCP_CACHE_E4M3 0
@@ -496,7 +499,8 @@ int fcp_cache_append(const fcp_cache* cache, const void* k, int64_t k_row, const
  *   q [tq, hq, head_dim] bf16 device, rows q_row elements apart (a multiple of 8), 16-byte aligned;  cu_seqlens over its rows
  *   o [tq, hq, head_dim] bf16, lse [hq, tq] fp32 (natural log of the scaled scores' sum; required): device, out.  A row that sees no token gets
  *   O = 0, LSE = -inf.  Rows of no sequence are left unwritten.
- *   weigh: 0, or 1 to add to cache->weight, for every token and KV head, the probabilities that the call's rows of that head's group give it.
+ *   weigh: 0, or 1 to add to cache->weight, for every token and KV head, the probabilities that the call's rows of that head's group give it.  A row whose query is not
+ *   finite reaches the weights of the tokens that it sees, and no others.
  *   scratch: device, 256-byte aligned, fcp_cache_scratch_bytes(FCP_SCRATCH_CACHE_ATTN or _WEIGH, ...); contents on entry irrelevant.
  * Scores, statistics and sums are held in 32 bits; for the product with V probabilities are rounded to bf16 (|dO| <= 2^-8 sum p |v|), and with
  * up to 32 rows per sequence and KV head on average what that leaves is multiplied too.  No atomics: results repeat bit for bit.
@@ -507,7 +511,8 @@ int fcp_cache_attn(const fcp_cache* cache, const void* q, int64_t q_row, int32_t
 
 /*
  * fcp_cache_weigh -- the weights of queries whose log-sum-exp is known, a prompt's after fcp_attn_fwd_step_direct say: adds exp(score - LSE) to
- * cache->weight, as fcp_cache_attn with weigh does.  lse [hq, tq] fp32 device; rows with LSE = -inf add nothing.
+ * cache->weight, as fcp_cache_attn with weigh does.  lse [hq, tq] fp32 device; rows with LSE = -inf add nothing, whatever their queries hold.
+ * The scores are those of the cached, 8-bit keys: with the LSE of attention over keys as they were before, a row's weights add up to 1 but for the keys' rounding.
  */
 int fcp_cache_weigh(const fcp_cache* cache, const void* q, int64_t q_row, int32_t tq, int32_t hq, const float* lse, const int32_t* cu_seqlens,
                     const int32_t* kv_len, const int32_t* pages, int32_t n_seqs, int32_t max_pages, float softmax_scale, void* stream);

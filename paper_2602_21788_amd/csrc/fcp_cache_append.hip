@@ -6,6 +6,7 @@
 // The page's new rows stay in registers while their scale is found.  Key rows are written as they come; of the values a lane holds a group of 16 tokens of two
 // channels, which in the cache's order are 16 bytes for each, so the transposition costs nothing.
 // 24 prompts of up to 4001 tokens, 8 heads of 128 channels, int8, 199 MB: 46 us, 4.3 TB/s, where a large copy reaches 4.9.  One token of each of 64 sequences: 6.6 us.
+// Pages of 128 tokens take 221 to 245 registers for a page's rows, two waves a SIMD instead of three or four: the prompts 59 us.
 #include "fcp_cache.h"
 
 namespace fcp {

@@ -48,9 +48,9 @@ struct Line {
 
 __device__ inline int32_t tiles_of(int len) { return max((len + kTile - 1) / kTile, 1); }
 constexpr int kWhole = -1;
-// Rows, first loads and the waves' meeting take a block about as long as four tiles.  Lead of 0 / 2 / 4 / 8, few rows: 64 sequences of up to 16384 tokens with weights 185 / 182 / 180 / 182 us, of
-// up to 4000 48.5 / 46.4 / 44.5 / 46.6, 16 of up to 8000 27.9 / 27.7 / 26.2 / 27.7, 5 of up to 2000 14.2 / 13.6 / 11.3 / 11.2; 64 of 4700 150 each.  0 / 2 / 4 / 6 / 10, many: 30 of up to 4000,
-// 40 new tokens 99 / 84 / 78 / 80 / 85, 8 of up to 16000, 100 new 155 / 153 / 149 / 148 / 152, 2 of up to 16385, 512 new 264 / 259 / 258 / 257 / 266.
+// Rows, first loads and the waves' meeting take a block about as long as four tiles.  Lead of 0 / 2 / 4 / 8, few rows, int8: 64 sequences of up to 16384 tokens with weights 186 / 181 / 180 / 181 us, of
+// up to 4000 47.6 / 44.7 / 43.1 / 45.4, 16 of up to 8000 28.6 / 28.3 / 26.8 / 27.9, 5 of up to 2000 13.9 / 13.3 / 11.0 / 11.0; 64 of 4700 113 each.  0 / 2 / 4 / 6 / 10, many: 30 of up to 4000,
+// 40 new tokens 96 / 84 / 85 / 89 / 96, 8 of up to 16000, 100 new 168 / 164 / 165 / 166 / 170; e4m3, 2 of up to 16385, 512 new 248 / 243 / 243 / 244 / 247.
 constexpr int kItemLead = 4;
 template <int Lead> __device__ inline int32_t places_of(int len) { return Lead == kWhole ? 1 : tiles_of(len) + Lead; }
 template <int Lead>

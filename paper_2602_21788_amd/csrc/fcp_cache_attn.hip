@@ -7,11 +7,11 @@
 //     neighbouring keys 16 g .. 16 g + 15, in order, which is the operand that the product with V needs, without any exchange.
 //   * O^T += V^T P^T, P in two bf16 parts: the cache holds values in groups of 16 tokens, a channel's 16 codes together, so a lane's 16 bytes are its channel's codes of its keys.
 //   * Codes go from memory to registers in 16-byte loads and become bf16 there (exact); the keys' scale multiplies the scores, the values' scale (a power
-//     of two) the probabilities.  The wave needs no LDS and no barrier in its loop.
+//     of two) the probabilities.  The wave needs no barrier in its loop, and LDS only for the scores that it keeps for the weights (a ring of its own).
 // All (sequence, KV head, block of rows, key tile) form one line, cut into equal pieces for the blocks: a long sequence is split over many blocks and short ones
 // share one, however ragged the lengths, which only the device knows.  The pieces of an item that does not lie in one block meet in a second launch.
-// One token over 131072, 32 heads on 8, e4m3, 269 MB: 57 to 60 us, 4.6 TB/s, where a large copy reaches 4.9 (the join is 7 of them, mostly its launch); 64 of lengths 819 to 16384, int8: 136 us,
-// 4.9 TB/s, with weights 180 (scores go out and come back).
+// One token over 131072, 32 heads on 8, e4m3, 269 MB: 60 us, 4.5 TB/s, where a large copy reaches 4.9 (the join is 8 of them, mostly its launch); 64 of lengths 819 to 16384, int8: 132 us,
+// 5.2 TB/s, with weights 180 (scores go out and come back).
 #include <type_traits>
 
 #include "fcp_cache_attn.h"
@@ -130,7 +130,7 @@ __device__ inline int score_at(int row) { return row / 4 * (4 * kTile) + row % 4
 // the tokens up to it.  A tile's keys are asked for when the keys before them have become scores, its values when the values before them are in the sums: a wave always has 8 to 16 KB
 // on their way.  Page numbers are asked for a tile earlier, right behind keys: loads come back in order, so those behind values would be waited for with the values.
 // Scored: the scores are kept (score_rows rows), in `ring` until it is full: stores between the loads hold these up, and that costs less in few long bursts.  64 sequences of 4700 tokens,
-// int8, 32 heads on 8, 128 channels, with weights: 168 us, stored tile by tile 178; lengths from 819 to 16384: 186 and 188.
+// int8, 32 heads on 8, 128 channels, with weights: 150 us, stored tile by tile 161; lengths from 819 to 16384: 180 and 186.
 template <int D, int Fmt, bool Scored, int NB>
 __device__ inline void walk(const AttnArgs& a, int seq, int head, int len, int first, int end, int step, const bf16x8 (&q)[NB][D / 32], const int (&last_tok)[NB], int all_see,
                             RowState<D> (&r)[NB], float* scores, int score_rows, float* ring, int32_t* first_nan) {
@@ -142,7 +142,8 @@ __device__ inline void walk(const AttnArgs& a, int seq, int head, int len, int f
   TileScales sc = scales_of(a.c, head, at.v);
   load_values<D>(a.c, lane, head, first, at.v, v);
   asm volatile("");                                        // (these loads and the loop's own must not become one at its head: the compiler then copies all that it carries, and spills)
-  // With 32 rows and e4m3 the registers are full: what follows from the lane is formed at every tile (64 sequences of up to 16384 tokens, 5 new: 176 us, else 186; int8 154 without, 159 with).
+  // With 32 rows and e4m3 the registers are full: what follows from the lane is formed at every tile (64 sequences of up to 16384 tokens, 5 new: 177 us, else 181; int8 157 without, 162 with).
+  // With 128 channels some 24 to 29 registers lie in memory all the same: the second part of the probabilities took their place.
   auto form_lane = [&] { return NB > 1 && Fmt == kE4m3 ? lane_id() : lane; };
   bool noted = false;
   int kept = 0;                                            // tiles in the ring, the last of them at hand
@@ -422,6 +423,8 @@ __global__ __launch_bounds__(256) void attn_merge_kernel(AttnArgs a, int blocks_
 // Adds exp(score - LSE), summed over the rows of the group, to the tokens' weights: the products bound it, and the exponentials, which take longer than they do.  A block takes one
 // (sequence, KV head, tile) at a time, those with the most rows first; its waves hold the tile's keys and divide the rows, 16 at a time, the next ones on their way.  The 16 sums of a
 // lane (its keys) over its column's rows are added over the 16 columns, then over the waves.
+// It is made for prompts: one of 4096 tokens, 8 heads on 8 of 128 channels, 31 us, 555 Tflop/s.  Of a head's few rows it has work for some of its waves only, each with the tile's keys: 64
+// sequences of up to 16384 tokens, int8, 32 heads on 8, 5 new tokens each (20 rows) 758 us with weights, 157 without; 16 new (64 rows) 880 and 219.
 struct WeighArgs {
   CacheView c;
   SeqView s;
@@ -659,15 +662,15 @@ __global__ __launch_bounds__(256) void weigh_scores_kernel(AttnArgs a, int rows_
 // ---- host ---------------------------------------------------------------------------------------
 
 // Tables of up to this many tiles: an item is not divided among blocks, which saves the second launch.  Few rows (not divided / divided; one token of each sequence, 32 heads on 8, 128
-// channels): one sequence of 500 tokens 8.2 / 10.5 us, of 1000 11.2 / 10.8, of 1500 14.4 / 11.0; 16 of up to 1000 11.6 / 12.8, of up to 1500 14.9 / 13.7.  Twice as many where there are
-// items for all blocks, since shares would end inside items of a few tiles: 64 of up to 1000 16.1 / 19.6, of up to 1500 21.4 / 22.2, of up to 2000 26.2 / 25.7 (with 5 new tokens each 32.8 / 39).
-// Many rows: a tile costs more, so fewer.  40 new tokens each (blocks of 128 rows): 8 of up to 250 16.1 / 21.5, of 380 20.1 / 22.1, of 500 24.2 / 22.7; 16 new (64 rows, 64 channels): 8 of
-// up to 500 12.4 / 13.5, 64 of up to 500 16.0 / 20.6.
+// channels, int8): one sequence of 500 tokens 8.6 / 10.4 us, of 1000 11.8 / 10.6, of 1500 15.3 / 11.0; 16 of up to 1000 12.3 / 13.1, of up to 1500 15.8 / 13.9.  Twice as many where there are
+// items for all blocks, since shares would end inside items of a few tiles: 64 of up to 1000 17.5 / 20.3, of up to 1500 22.6 / 23.2, of up to 2000 27.7 / 26.9 (with 5 new tokens each 37.7 / 41.5).
+// Many rows: a tile costs more, so fewer.  40 new tokens each (blocks of 128 rows): 8 of up to 250 15.9 / 21.3, of 380 20.1 / 22.2, of 500 23.6 / 22.8; 16 new (64 rows, 64 channels, e4m3): 8 of
+// up to 500 12.5 / 13.4, 64 of up to 500 16.2 / 21.1.
 int whole_tiles(int rows, int64_t items) { return rows == kManyRows ? 6 : rows == kManyRows / 2 ? 8 : items >= kBlocks ? 32 : 16; }
 
 // How a call is worked.  Up to 16 or 32 rows per sequence and KV head on average: a block of as many rows, whose waves divide the keys; more: 64 or 128 rows, which its waves divide.
-// 64 sequences of up to 16384 tokens, int8, 32 heads on 8: 5 new tokens each (20 rows), 32 rows a block 154 us, 128 rows 252; 16 new (64 rows), 64 rows a block 221 us, 128 rows 262.  Of up
-// to 1000: 21 / 44, 38 / 46; 8 of up to 8000: 28 / 40, 39 / 45.
+// 64 sequences of up to 16384 tokens, int8, 32 heads on 8: 5 new tokens each (20 rows), 32 rows a block 157 us, 128 rows 250; 16 new (64 rows), 64 rows a block 219 us, 128 rows 264.  Of up
+// to 1000: 24 / 39, 36 / 42; 8 of up to 8000: 29 / 40, 39 / 44.
 struct AttnPlan { int rows; bool stored; bool whole; int64_t part_floats, score_floats, places; };
 AttnPlan plan_attn(const CacheView& c, int head_dim, int32_t n_seqs, int32_t max_pages, int32_t tq, int32_t hq, bool weigh) {
   const int group = hq / c.hkv;
@@ -700,8 +703,8 @@ int launch_attn(const AttnArgs& a, const AttnPlan& p, hipStream_t st) {
   kernel<<<grid, block, 0, st>>>(a);
   FCP_HIP_CHECK(hipGetLastError());
   if (!p.whole) {
-    // A block for each row that an item has on average, but 4 at least.  4 / 8 / 16 blocks: 64 sequences of up to 4000 tokens, 4 rows 42.9 / 44.7 / 47.0 us; 16 of up to
-    // 8000, 16 rows 21.3 / 16.6 / 14.2.
+    // A block for each row that an item has on average, but 4 at least.  4 / 8 / 16 / 32 blocks: 64 sequences of up to 4000 tokens, 4 rows 43.1 / 44.5 / 46.6 / 50.4 us; 16 of up to
+    // 8000, 16 rows 16.3 / 14.1 / 13.3 / 13.8.
     const int64_t rows = ((int64_t)a.s.n_rows * a.group + a.s.n_seqs - 1) / a.s.n_seqs;
     const int of_item = rows <= 4 ? 4 : rows <= 8 ? 8 : rows <= 16 ? 16 : 32;
     auto merge = p.rows == 32 ? attn_merge_kernel<D, 32> : attn_merge_kernel<D, 16>;

@@ -6,8 +6,8 @@
 // a lane, a quarter of a line's rate, in every wave.  The keys' scale is taken with the scores, the values' with the codes.
 // A step has two streams: the next tile's scores with this tile's exponentials, and this tile's product with the values with the conversion of codes for the tiles after; the matrix
 // units and the others work at once, and operands from LDS are asked for four ahead.  One barrier a step.  Two blocks per CU: a wave has 256 registers, all in use.
-// Pieces of 512 tokens over up to 16385, 2 sequences, 40 query heads on 8, 128 channels, 193 Gflop: 237 to 243 us with e4m3 (11 of them the merge), 7 % more with int8, whose codes take
-// three times as many instructions; with score, exponentials and product one after the other, each operand asked for when it is due, 277 and 300 where this took 244 and 280.  Counted:
+// Pieces of 512 tokens over up to 16385, 2 sequences, 40 query heads on 8, 128 channels, 193 Gflop: 239 to 244 us with e4m3 (11 of them the merge), 270 with int8, whose codes take
+// three times as many instructions; with score, exponentials and product one after the other, each operand asked for when it is due, 277 and 300 where this took 244 and 280 then.  Counted:
 // the matrix units work 38 % of the CUs' time, 22 % of a wave's time are waits.  A large matrix product runs at 1213 Tflop/s here, this at 800.
 // Keys and rows are laid on the matrix as in the kernel for few rows: a lane ends with the scores of 16 neighbouring keys, which is the operand of the product with V.
 #include "fcp_cache_attn.h"

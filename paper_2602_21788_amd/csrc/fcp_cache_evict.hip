@@ -5,7 +5,8 @@
 // short tables.  One CU takes about 20 us to look at 131072 weights once, so long ones are cut into chunks: one launch counts, one lists each chunk's tokens with the k-th's
 // upper bits, one finds the border among those (every block for itself) and writes the chunk's part of the list.
 // The last launch moves the tokens: a wave per (new page, KV head, keys or values).
-// 4 sequences of up to 131072 tokens, 8 heads: choosing 7.5 + 10 + 18 us, chains of loads and barriers; moving 94 (the kernel says why).  4 of up to 600, 4 heads of 64 channels: 7 and 4.
+// 4 sequences of up to 131072 tokens, 8 heads: choosing 7.5 + 10 + 18 us, chains of loads and barriers; moving 95 (the kernel says why).  4 of up to 600, 4 heads of 64 channels: 7 and 4.
+// Pages of 128 tokens and 128 channels take more than 256 registers for a page's codes, one wave a SIMD instead of three: the long sequences 205 us altogether, with pages of 64 131.
 #include "fcp_cache.h"
 
 namespace fcp {
@@ -416,7 +417,7 @@ __global__ __launch_bounds__(256) void move_kernel(EvictArgs a) {
     }
   } else {
     // The word of four tokens that holds the token is asked for, for 32 tokens at once: a group's lines are fetched once, by whichever token comes first, and nearly every group of a
-    // long sequence cut to an eighth has one.  4 sequences of up to 131072 tokens to 16384, 8 heads: 290 MB read and 124 written in 94 us, 4.4 TB/s, where a large copy reaches 5.2;
+    // long sequence cut to an eighth has one.  4 sequences of up to 131072 tokens to 16384, 8 heads: 290 MB read and 124 written in 95 us, 4.4 TB/s, where a large copy reaches 4.9;
     // values alone 74 us, keys alone 30.  (Two waves a page and half the chain of loads: 91.  Single bytes of channels that lie 32 bytes apart are a request each: 131.)
     constexpr int NC = D / 64, kBatch = P < 32 ? P : 32;   // channels of a lane: lane, lane + 64; tokens on their way
     u32x4 w[Groups][NC];

@@ -107,7 +107,9 @@ class CacheDecoder:
 
     # -- the path ----------------------------------------------------------------------------------------------------------
     def prefill(self, q, k, v, lens):
-        """Prompts of lens[s] tokens for empty sequences: bf16 rows q [sum, hq, D], k, v [sum, hkv, D] (turned in place).  Returns O [sum, hq, D], LSE [hq, sum]."""
+        """Prompts of lens[s] tokens for empty sequences: bf16 rows q [sum, hq, D], k, v [sum, hkv, D] (turned in place).  Returns O [sum, hq, D], LSE [hq, sum].
+        O and LSE are those of the keys and values as given.  The cached tokens' weights are exp(score - LSE) with the scores of the cached, 8-bit keys: a row's add up to 1 but for the keys'
+        rounding."""
         lens = self._counts(lens)
         self._fit(q, k, v, int(lens.sum()), whole=True)
         if self.kv_len.any():
