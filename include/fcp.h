@@ -478,6 +478,8 @@ typedef struct fcp_cache {
 #define FCP_SCRATCH_CACHE_ATTN 2
 #define FCP_SCRATCH_CACHE_WEIGH 3
 #define FCP_SCRATCH_CACHE_EVICT 4
+#define FCP_SCRATCH_CACHE_FORK 6      /* n_seqs: sequences of the next step; tq, hq not used */
+#define FCP_SCRATCH_CACHE_COMPACT 7   /* tq, hq not used                                      */
 size_t fcp_cache_scratch_bytes(int which, const fcp_cache* cache, int32_t n_seqs, int32_t max_pages, int32_t tq, int32_t hq);
 
 /*
@@ -533,6 +535,62 @@ int fcp_cache_weigh(const fcp_cache* cache, const void* q, int64_t q_row, int32_
 int fcp_cache_evict(const fcp_cache* cache, const int32_t* pages, const int32_t* kv_len, int32_t n_seqs, int32_t max_pages, const int32_t* new_pages,
                     int32_t max_new_pages, int32_t budget, int32_t n_first, int32_t n_recent, int32_t* kept, int32_t* new_len,
                     void* scratch, size_t scratch_bytes, void* stream);
+
+/*
+ * Answering a prompt with several continuations: fcp_beam_select says which beams go on with which tokens, fcp_cache_fork gives every one of them its table.
+ *
+ * fcp_cache_fork -- the tables of the next step's sequences out of those of this step's.  Sequence i of the next step has the tokens of sequence parent[i] (a number outside
+ * 0 .. n_seqs - 1: none) and room for news[i] more (negative: 0); new_len[i] counts both, at most max_pages * page_tokens.  One sequence may have several children (beams, samples; a
+ * prompt's first continuations), one child (it goes on) or none (it ends).
+ *   - Pages that are only read are shared.
+ *   - A page that holds tokens of the parent and gets new ones must belong to one sequence: where several would write it the lowest keeps it, but none does if others only read it or it is
+ *     busy.  The others get a copy of the parent's tokens in it: codes (values in whole groups of 16 tokens), scales, weights if the cache has them.
+ *   - Fresh pages, for copies and for new tokens, are handed out in increasing order to the sequences in order, and within one in the order of its table: the lowest numbers that no sequence of
+ *     this step holds and that are not busy.  If there are too few the rest of the entries are -1 (such tokens are not written, and seen by nobody).
+ *   - Pages that only sequences without children held are free afterwards, for the next call: this one does not write them.
+ * Entries of parents' tables that are no page's number become -1.  Entries behind a sequence's last page are -1.
+ *   pages [n_seqs][max_pages], kv_len [n_seqs];  parent, news [n_new];  new_pages [n_new][max_pages], new_len [n_new] out, apart from the old tables: int32 device
+ *   busy [n_pages] bytes, device, or NULL: not 0 for pages that others hold, sequences outside the call say
+ *   counts [3] int32 device out: pages handed out, pages that were lacking, pages that neither the new tables nor others hold
+ *   scratch: device, 256-byte aligned, fcp_cache_scratch_bytes(FCP_SCRATCH_CACHE_FORK, cache, n_new, max_pages, ...); contents on entry irrelevant
+ * While the call runs nobody else may write the pages of its sequences or use free ones.  2^24 blocks of work or more (one for 256 entries of a table, one for each (new sequence, KV head))
+ * are FCP_ERR_UNSUPPORTED.
+ */
+int fcp_cache_fork(const fcp_cache* cache, const int32_t* pages, const int32_t* kv_len, int32_t n_seqs, int32_t max_pages, const int32_t* parent,
+                   const int32_t* news, int32_t n_new, const uint8_t* busy, int32_t* new_pages, int32_t* new_len, int32_t* counts,
+                   void* scratch, size_t scratch_bytes, void* stream);
+
+/*
+ * fcp_cache_compact -- the pages in use (entries of the tables that hold cached tokens) move to the lowest numbers, so that the pool's end is free.  Those that are not busy get the
+ * lowest numbers that are not busy: pages there already stay, the others, in increasing order, take the free numbers in increasing order.  A page that several entries name moves once, whole.
+ *   new_pages [n_seqs][max_pages] int32 device out (may be pages itself): the tables with the new numbers, -1 where there is no cached token or no page
+ *   busy as above: such pages stay where they are
+ *   counts [3] int32 device out: pages moved, pages in use, the first number past all pages that are in use or busy
+ *   scratch: fcp_cache_scratch_bytes(FCP_SCRATCH_CACHE_COMPACT, cache, n_seqs, max_pages, ...)
+ * Old pages keep their contents until somebody writes them.  Limits as above.
+ */
+int fcp_cache_compact(const fcp_cache* cache, const int32_t* pages, const int32_t* kv_len, int32_t n_seqs, int32_t max_pages, const uint8_t* busy,
+                      int32_t* new_pages, int32_t* counts, void* scratch, size_t scratch_bytes, void* stream);
+
+/*
+ * fcp_beam_select -- the `keep` best continuations of every prompt.  A prompt has `beams` rows of logits; token t behind beam b has the score
+ *   score_b + x_bt - ln sum_u exp x_bu.
+ * NaN counts as -inf and +inf as the largest finite value; a logit of -inf is no candidate (a grammar's mask), nor is any of a beam whose score is -inf or NaN (beams that begin with the same
+ * tokens: all but one).  Of a beam at most its `keep` greatest logits are candidates, among equal ones the lowest tokens.  A beam that is done has one candidate, end_token, at its score.
+ * Sums and scores are held and compared in 64 bits; among equal scores the lowest beam comes first, then the lowest token.
+ *   logits [n_prompts * beams, vocab] FCP_BF16 or FCP_F32 device, rows logits_row elements apart, aligned to their type
+ *   score [n_prompts * beams] fp32 device;  done [n_prompts * beams] bytes device, or NULL;  end_token: the token that ends a beam, or -1
+ *   parent, token [n_prompts, keep] int32, new_score [n_prompts, keep] fp32, new_done [n_prompts, keep] bytes (or NULL): device out, best first.  parent: the row of the beam, what
+ *   fcp_cache_fork takes; new_done: the beam is done, or token is end_token.  Where there are fewer candidates: -1, -1, -inf, 0.  Outputs lie apart from inputs.
+ *   scratch: device, 256-byte aligned, fcp_beam_scratch_bytes (0 and fcp_last_error for arguments that the call would refuse); contents on entry irrelevant
+ * Limits (FCP_ERR_UNSUPPORTED): beams, keep, vocab up to FCP_BEAM_MAX_BEAMS, FCP_BEAM_MAX_KEEP, 2^30; fewer than 2^24 chunks of 2048 logits of a row.
+ */
+#define FCP_BEAM_MAX_BEAMS 256
+#define FCP_BEAM_MAX_KEEP 64
+size_t fcp_beam_scratch_bytes(int32_t n_prompts, int32_t beams, int32_t vocab, int32_t keep);
+int fcp_beam_select(const void* logits, int32_t type, int64_t logits_row, int32_t n_prompts, int32_t beams, int32_t vocab, const float* score,
+                    const uint8_t* done, int32_t end_token, int32_t keep, int32_t* parent, int32_t* token, float* new_score,
+                    uint8_t* new_done, void* scratch, size_t scratch_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -19,6 +19,8 @@ LIB_PATH = os.path.join(_PKG, "libfcp.so")
 FCP_OK, FCP_ERR_INVALID_ARG, FCP_ERR_CAPACITY, FCP_ERR_UNSUPPORTED, FCP_ERR_HIP, FCP_ERR_STALLED = 0, -1, -2, -3, -4, -5
 FCP_SCRATCH_FWD, FCP_SCRATCH_BWD = 0, 1
 FCP_SCRATCH_CACHE_ATTN, FCP_SCRATCH_CACHE_WEIGH, FCP_SCRATCH_CACHE_EVICT = 2, 3, 4
+FCP_SCRATCH_CACHE_FORK, FCP_SCRATCH_CACHE_COMPACT = 6, 7
+FCP_BEAM_MAX_BEAMS, FCP_BEAM_MAX_KEEP = 256, 64
 FCP_BF16, FCP_F32 = 0, 1
 FCP_ROTARY_HALF, FCP_ROTARY_PAIRS = 0, 1
 FCP_ROTARY_PLAIN, FCP_ROTARY_LINEAR, FCP_ROTARY_BASE, FCP_ROTARY_PARTS = 0, 1, 2, 3
@@ -36,7 +38,8 @@ EXPORTS = ["fcp_last_error", "fcp_shard_plan", "fcp_plan_groups", "fcp_scratch_b
            "fcp_attn_bwd_delta", "fcp_attn_bwd_step", "fcp_grad_finalize", "fcp_scratch_status",
            "fcp_group_shard_args", "fcp_attn_fwd_step_running", "fcp_shard_plan_mixed", "fcp_mask_tables", "fcp_attn_fwd_step_mixed", "fcp_attn_bwd_step_mixed",
            "fcp_attn_bwd_step_direct", "fcp_grad_finalize_direct", "fcp_attn_fwd_step_direct", "fcp_lse_merge_direct", "fcp_attn_fwd_step_static",
-           "fcp_rotary_frequencies", "fcp_rotary", "fcp_cache_scratch_bytes", "fcp_cache_append", "fcp_cache_attn", "fcp_cache_weigh", "fcp_cache_evict"]
+           "fcp_rotary_frequencies", "fcp_rotary", "fcp_cache_scratch_bytes", "fcp_cache_append", "fcp_cache_attn", "fcp_cache_weigh", "fcp_cache_evict",
+           "fcp_cache_fork", "fcp_cache_compact", "fcp_beam_scratch_bytes", "fcp_beam_select"]
 
 
 class FcpError(RuntimeError):
@@ -119,6 +122,14 @@ def lib() -> ctypes.CDLL:
         L.fcp_cache_weigh.argtypes = [P, P, I64, I32, I32, P, P, P, P, I32, I32, F, P]
         L.fcp_cache_evict.restype = ctypes.c_int
         L.fcp_cache_evict.argtypes = [P, P, P, I32, I32, P, I32, I32, I32, I32, P, P, P, SZ, P]
+        L.fcp_cache_fork.restype = ctypes.c_int
+        L.fcp_cache_fork.argtypes = [P, P, P, I32, I32, P, P, I32, P, P, P, P, P, SZ, P]
+        L.fcp_cache_compact.restype = ctypes.c_int
+        L.fcp_cache_compact.argtypes = [P, P, P, I32, I32, P, P, P, P, SZ, P]
+        L.fcp_beam_scratch_bytes.restype = SZ
+        L.fcp_beam_scratch_bytes.argtypes = [I32, I32, I32, I32]
+        L.fcp_beam_select.restype = ctypes.c_int
+        L.fcp_beam_select.argtypes = [P, I32, I64, I32, I32, I32, P, P, I32, I32, P, P, P, P, P, SZ, P]
         _lib = L
     return _lib
 
@@ -422,15 +433,15 @@ def fcp_scratch_status(scratch, stream=None):
 # Rotary positions and the paged 8-bit cache.  Tensors that the library reads by plain size are checked here for type and size, since
 # the C ABI sees addresses only.  The smallest calls take the GPU 4 to 7 us, so what the checks cost on the host shows: torch and its types are looked up once,
 # descriptors are packed as bytes (rotary positions of 16 rows of queries and keys 8.6 -> 6.7 us a call, one token of 64 sequences appended 7.0 -> 6.6).
-_bf16 = _f32 = _f64 = _i32 = None
+_bf16 = _f32 = _f64 = _i32 = _u8 = None
 
 
 def _types():
-    global _bf16, _f32, _f64, _i32
+    global _bf16, _f32, _f64, _i32, _u8
     if _bf16 is None:
         import torch
         lib()
-        _f32, _f64, _i32, _bf16 = torch.float32, torch.float64, torch.int32, torch.bfloat16
+        _f32, _f64, _i32, _u8, _bf16 = torch.float32, torch.float64, torch.int32, torch.uint8, torch.bfloat16
     return _bf16
 
 
@@ -570,3 +581,60 @@ def fcp_cache_evict(cache, pages, kv_len, new_pages, budget, n_first, n_recent, 
     _check(lib().fcp_cache_evict(ctypes.byref(cache), pg, kl, n, m, _int_ptr(new_pages, "new_pages"), new_pages.shape[1], budget, n_first,
                                  n_recent, _int_ptr(kept, "kept", n * cache.hkv * budget), _int_ptr(new_len, "new_len", n), _dev_ptr(scratch),
                                  scratch.numel() * scratch.element_size(), _stream(stream)))
+
+
+# ---------------------------------------------------------------------------------------
+# Several continuations of a prompt: who holds which page, and which beams go on.
+def _bytes_ptr(t, name, n):
+    if t is not None and (t.dtype is not _u8 or t.numel() < n):
+        raise ValueError(f"{name} must be a uint8 tensor of at least {n} entries")
+    return _dev_ptr(t)
+
+
+def fcp_cache_fork(cache, pages, kv_len, parent, news, new_pages, new_len, counts, scratch, busy=None, stream=None):
+    """Tables of the sequences that continue those of pages [n_seqs, max_pages], kv_len: sequence i has the tokens of sequence parent[i] and room for news[i] more.  new_pages [n_new,
+    max_pages], new_len [n_new], counts [3] (pages handed out, lacking, free) int32 out; busy: uint8 [n_pages] or None (see include/fcp.h)."""
+    _, kl, pg, n, m = _seqs(None, kv_len, pages)
+    if len(new_pages.shape) != 2 or new_pages.shape[1] != m:
+        raise ValueError("new_pages must be [n_new, max_pages], its rows as long as those of pages")
+    n_new = new_pages.shape[0]
+    _check(lib().fcp_cache_fork(ctypes.byref(cache), pg, kl, n, m, _int_ptr(parent, "parent", n_new), _int_ptr(news, "news", n_new), n_new,
+                                _bytes_ptr(busy, "busy", cache.n_pages), _int_ptr(new_pages, "new_pages"), _int_ptr(new_len, "new_len", n_new), _int_ptr(counts, "counts", 3),
+                                _dev_ptr(scratch), scratch.numel() * scratch.element_size(), _stream(stream)))
+
+
+def fcp_cache_compact(cache, pages, kv_len, new_pages, counts, scratch, busy=None, stream=None):
+    """Moves the pages in use to the lowest numbers: new_pages [n_seqs, max_pages] (may be pages), counts [3] (pages moved, in use, first number past all) int32 out."""
+    _, kl, pg, n, m = _seqs(None, kv_len, pages)
+    if tuple(new_pages.shape) != (n, m):
+        raise ValueError("new_pages must have the shape of pages")
+    _check(lib().fcp_cache_compact(ctypes.byref(cache), pg, kl, n, m, _bytes_ptr(busy, "busy", cache.n_pages), _int_ptr(new_pages, "new_pages"),
+                                   _int_ptr(counts, "counts", 3), _dev_ptr(scratch), scratch.numel() * scratch.element_size(), _stream(stream)))
+
+
+def fcp_beam_scratch_bytes(n_prompts, beams, vocab, keep) -> int:
+    n = int(lib().fcp_beam_scratch_bytes(int(n_prompts), int(beams), int(vocab), int(keep)))
+    if n == 0:
+        raise FcpError(FCP_ERR_INVALID_ARG, lib().fcp_last_error().decode())
+    return n
+
+
+def fcp_beam_select(logits, score, beams, parent, token, new_score, scratch, done=None, end_token=-1, new_done=None, stream=None):
+    """The best continuations of every prompt: logits [n_prompts * beams, vocab] bf16 or fp32 (rows with any stride), score [n_prompts * beams] fp32, done uint8 or None.  parent, token int32,
+    new_score fp32, new_done uint8 or None, all [n_prompts, keep]: out, best first (see include/fcp.h)."""
+    _bf16 or _types()
+    if len(logits.shape) != 2 or (logits.dtype is not _bf16 and logits.dtype is not _f32) or not logits.is_cuda or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError("logits must be a bf16 or fp32 device tensor [rows, vocab], the logits of a row next to each other")
+    rows, vocab = logits.shape
+    n = parent.shape[0] if len(parent.shape) == 2 else -1
+    if n < 0 or n * beams != rows:
+        raise ValueError("parent must be [n_prompts, keep], with n_prompts * beams rows of logits")
+    keep = parent.shape[1]
+    for t, name in ((token, "token"), (new_score, "new_score"), (new_done, "new_done")):
+        if t is not None and t.shape != parent.shape:
+            raise ValueError(f"{name} must have the shape of parent")
+    if score.dtype is not _f32 or score.numel() != rows or new_score.dtype is not _f32:
+        raise ValueError("score and new_score must be float32 tensors, score with an entry for every row")
+    _check(lib().fcp_beam_select(logits.data_ptr(), 1 if logits.dtype is _f32 else 0, logits.stride(0) if rows > 1 else vocab, n, int(beams), vocab, _dev_ptr(score),
+                                 _bytes_ptr(done, "done", rows), int(end_token), keep, _int_ptr(parent, "parent"), _int_ptr(token, "token"), _dev_ptr(new_score),
+                                 _bytes_ptr(new_done, "new_done", n * keep), _dev_ptr(scratch), scratch.numel() * scratch.element_size(), _stream(stream)))

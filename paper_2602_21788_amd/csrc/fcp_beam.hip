@@ -1,0 +1,372 @@
+// fcp_beam_select: the best continuations of every prompt, over its beams and the vocabulary.
+//
+// The score of token t behind beam b is score_b + x_bt - ln sum_u exp x_bu.  The order of a beam's tokens is that of its logits, so a beam offers its `keep` greatest logits, and the
+// logarithm is needed only to put beams beside each other.  Candidates of different beams can lie as near as they like: sums and scores are held in 64 bits.
+//
+// First launch: a block takes a chunk of a row, 32 neighbouring logits a thread (8 where there are few rows), which stay in registers for three looks:
+//   * the greatest of every four threads, 64 in all; the keep-th greatest of those 64, T: at least `keep` logits of the chunk are T or more;
+//   * the sum of exp(x - greatest): the exponential as a polynomial in 64 bits, which this card multiplies as fast as 32;
+//   * logits beyond T, and those equal to it in T's four threads and earlier ones, go to a list in LDS.  Whatever the logits, they lie in `keep` groups of four threads, which bounds
+//     the list; as a rule it is little longer than `keep`.  The list is put in order by counting, where it is long by a bitonic sort.
+// Second launch: a block for each prompt joins the sums and finds the best candidates of all lists the same way.
+#include <float.h>
+
+#include "fcp_device.h"
+
+namespace fcp {
+namespace {
+
+constexpr int kThreads = 256, kGroups = 64;   // groups of neighbouring threads whose greatest element stands for them: a lane each
+constexpr int kPerGroup = kThreads / kGroups;
+
+struct BeamArgs {
+  const void* logits;
+  int64_t row;
+  int32_t rows, beams, vocab, chunks, keep, end_token;
+  const float* score;
+  const uint8_t* done;
+  int32_t* parent;
+  int32_t* token;
+  float* new_score;
+  uint8_t* new_done;
+  uint64_t* lists;                     // [rows][chunks][keep]: ordered logit, then ~token; 0: none
+  double* sums;                        // [rows][chunks]: sum of exp(x - greatest)
+  float* tops;                         // [rows][chunks]: greatest logit, -inf: none
+};
+
+// Integers that order floats: greater value, greater integer (never 0).  No NaN, no -0.
+__device__ inline uint32_t order_of(float x) {
+  const uint32_t u = __float_as_uint(x);
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ inline float value_of(uint32_t order) { return __uint_as_float(order & 0x80000000u ? order & 0x7fffffffu : ~order); }
+__device__ inline uint64_t order_of(double x) {
+  const uint64_t u = (uint64_t)__double_as_longlong(x + 0.0);
+  return u >> 63 ? ~u : u | (uint64_t)1 << 63;
+}
+__device__ inline double score_of(uint64_t order) { return __longlong_as_double((long long)(order >> 63 ? order & ~((uint64_t)1 << 63) : ~order)); }
+
+// A logit as it counts: NaN as -inf, +inf as the largest finite value, -0 as 0.
+__device__ inline float counted(float x) { return (x != x ? -INFINITY : fminf(x, FLT_MAX)) + 0.f; }
+
+// exp(x - top), x <= top: 2^n times a polynomial in f, n + f = (x - top) log2(e), |f| <= 1/2.  The coefficients are a least-squares fit on Chebyshev nodes with weights 2^-f; the
+// relative error is at most 4.1e-11, which is how far the logarithm of a sum may be off.  2^-1000 stands for everything below it.
+__device__ inline double exp_below(float x, double top) {
+  constexpr double kLog2E = 1.4426950408889634074, kShift = 6755399441055744.0;       // 1.5 * 2^52: the sum's low bits are the rounded number
+  const double t = fmax(((double)x - top) * kLog2E, -1000.0), shifted = t + kShift, f = t - (shifted - kShift);
+  double p = 0x1.fde1039ee67bfp-17;
+  p = __builtin_fma(p, f, 0x1.4469d4b220e3bp-13);
+  p = __builtin_fma(p, f, 0x1.5d8a9fcfc7546p-10);
+  p = __builtin_fma(p, f, 0x1.3b29dcb134a69p-7);
+  p = __builtin_fma(p, f, 0x1.c6b08a80840e9p-5);
+  p = __builtin_fma(p, f, 0x1.ebfbe0a416e10p-3);
+  p = __builtin_fma(p, f, 0x1.62e42ff12cfc5p-1);
+  p = __builtin_fma(p, f, 0x1.ffffffffac502p-1);
+  const int n = (int)(uint32_t)__double_as_longlong(shifted);
+  return __longlong_as_double(__double_as_longlong(p) + ((long long)n << 52));
+}
+
+__device__ inline double sum_of_wave(double x) {
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
+  return x;
+}
+
+// E elements from `from` on, of which those at 0 .. there - 1 exist; the others count as -inf.
+template <class T, int E>
+__device__ inline void load_row(const T* from, int there, float (&v)[E]) {
+  if (there >= E) {
+    constexpr int W = 16 / sizeof(T);
+    struct __attribute__((packed, aligned(sizeof(T)))) Words { uint32_t w[4]; };     // (rows may begin at any element)
+#pragma unroll
+    for (int i = 0; i < E / W; ++i) {
+      const Words r = *reinterpret_cast<const Words*>(from + W * i);
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        if constexpr (sizeof(T) == 2) v[W * i + j] = __uint_as_float(j % 2 ? r.w[j / 2] & 0xffff0000u : r.w[j / 2] << 16);
+        else v[W * i + j] = __uint_as_float(r.w[j]);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < E; ++i) v[i] = i < there ? (float)from[i] : -INFINITY;
+  }
+#pragma unroll
+  for (int i = 0; i < E; ++i) v[i] = counted(v[i]);
+}
+
+// One of the 64 elements that a wave holds, a lane each: the rank-th greatest, of equal ones the lowest lane first.  Returns its lane.
+template <class Greater>
+__device__ inline int lane_of_rank(int rank, Greater greater) {
+  const int lane = threadIdx.x & 63;
+  int above = 0;
+#pragma unroll 8
+  for (int j = 0; j < 64; ++j) above += greater(j, lane);
+  return __builtin_ctzll(__ballot(above == rank));
+}
+
+// Puts list[0 .. n - 1], different from each other, in order, greatest first, as far as the first `keep`; the list has room for the next power of two.  Every thread calls.
+template <class K, class Greater, class Out>
+__device__ inline void best_of(K* list, int n, int keep, const K& least, Greater greater, Out out) {
+  if (n <= kThreads) {
+    if ((int)threadIdx.x < n) {
+      const K mine = list[threadIdx.x];
+      int above = 0;
+#pragma unroll 4
+      for (int j = 0; j < n; ++j) above += greater(list[j], mine);
+      if (above < keep) out(above, mine);
+    }
+    return;
+  }
+  int size = 1;
+  while (size < n) size *= 2;
+  for (int i = n + threadIdx.x; i < size; i += kThreads) list[i] = least;
+  __syncthreads();
+  for (int run = 2; run <= size; run *= 2)
+    for (int d = run / 2; d > 0; d /= 2) {
+      for (int i = threadIdx.x; i < size / 2; i += kThreads) {
+        const int a = 2 * i - (i & (d - 1)), b = a + d;    // (the pair's lower place has the bit d clear)
+        const K x = list[a], y = list[b];
+        const bool falling = (a & run) == 0;
+        if (greater(y, x) == falling) { list[a] = y; list[b] = x; }
+      }
+      __syncthreads();
+    }
+  for (int i = threadIdx.x; i < min(keep, n); i += kThreads) out(i, list[i]);
+}
+
+// Room of the list of a block whose threads hold E elements: those of `keep` groups, and a power of two for the sort.
+__host__ __device__ constexpr int list_room(int keep, int E) {
+  int n = 1;
+  while (n < keep) n *= 2;
+  return n * kPerGroup * E;
+}
+
+template <class T, int E>
+__global__ __launch_bounds__(kThreads) void beam_rows_kernel(BeamArgs a) {
+  extern __shared__ __align__(16) uint64_t list[];
+  __shared__ float groups[kGroups];
+  __shared__ double sums[kThreads / 64];
+  __shared__ int32_t listed;
+  const int row = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const float score = a.score[row];
+  if (!(score > -INFINITY) || (a.done && a.done[row])) return;           // offers nothing, or one candidate whatever its logits
+  const int first = chunk * (kThreads * E) + (int)threadIdx.x * E;
+  float v[E];
+  load_row<T, E>(static_cast<const T*>(a.logits) + (int64_t)row * a.row + first, a.vocab - first, v);
+  float top = v[0];
+#pragma unroll
+  for (int i = 1; i < E; ++i) top = fmaxf(top, v[i]);
+  top = fmaxf(top, __shfl_xor(top, 1));
+  top = fmaxf(top, __shfl_xor(top, 2));
+  if (threadIdx.x % kPerGroup == 0) groups[threadIdx.x / kPerGroup] = top;
+  if (threadIdx.x == 0) listed = 0;
+  __syncthreads();
+  const float mine = groups[lane];
+  const int at = lane_of_rank(a.keep - 1, [&](int j, int i) {
+    const float other = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(mine), j));
+    return other > mine || (other == mine && j < i);
+  });
+  const float border = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(mine), at));
+  float most = mine;
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
+  double sum = 0;
+  if (most > -INFINITY) {
+#pragma unroll
+    for (int i = 0; i < E; ++i) sum += exp_below(v[i], (double)most);
+    const float equal = (int)threadIdx.x / kPerGroup <= at ? border : INFINITY;          // the border itself counts in its own group and earlier ones
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+      if ((v[i] > border || v[i] == equal) && v[i] > -INFINITY)
+        list[atomicAdd(&listed, 1)] = (uint64_t)order_of(v[i]) << 32 | (uint32_t)~(first + i);
+  }
+  sum = sum_of_wave(sum);
+  if (lane == 0) sums[wave] = sum;
+  __syncthreads();
+  const int n = listed;
+  uint64_t* const out = a.lists + (int64_t)blockIdx.x * a.keep;
+  best_of(list, n, a.keep, (uint64_t)0, [](uint64_t x, uint64_t y) { return x > y; }, [&](int i, uint64_t k) { out[i] = k; });
+  if ((int)threadIdx.x >= n && (int)threadIdx.x < a.keep) out[threadIdx.x] = 0;
+  if (threadIdx.x == 0) {
+    a.sums[blockIdx.x] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+    a.tops[blockIdx.x] = most;
+  }
+}
+
+// A candidate: its score's order, then the beam and the token, both so that lower is greater.
+struct Candidate { uint64_t score, place; };
+__device__ inline bool greater(const Candidate& x, const Candidate& y) { return x.score > y.score || (x.score == y.score && x.place > y.place); }
+
+constexpr int kJoined = 8;             // candidates that a thread holds
+
+__global__ __launch_bounds__(kThreads) void beam_join_kernel(BeamArgs a) {
+  extern __shared__ __align__(16) Candidate found[];       // the best so far, then those that may replace them
+  __shared__ double lse[FCP_BEAM_MAX_BEAMS];
+  __shared__ Candidate groups[kGroups], best[FCP_BEAM_MAX_KEEP];
+  __shared__ int32_t listed;
+  const int row0 = blockIdx.x * a.beams, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for (int b = wave; b < a.beams; b += kThreads / 64) {    // a wave joins the sums of a beam
+    const float score = a.score[row0 + b];
+    if (!(score > -INFINITY) || (a.done && a.done[row0 + b])) continue;
+    const int64_t at = (int64_t)(row0 + b) * a.chunks;
+    float most = -INFINITY;
+    for (int c = lane; c < a.chunks; c += 64) most = fmaxf(most, a.tops[at + c]);
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
+    double sum = 0;
+    for (int c = lane; c < a.chunks; c += 64) {
+      const float top = a.tops[at + c];
+      if (top > -INFINITY) sum += a.sums[at + c] * exp((double)top - (double)most);
+    }
+    sum = sum_of_wave(sum);
+    if (lane == 0) lse[b] = (double)most + log(sum);
+  }
+  if (threadIdx.x == 0) listed = 0;
+  __syncthreads();
+  const Candidate none = {0, 0};
+  const int per_beam = a.chunks * a.keep;
+  const int64_t all = (int64_t)a.beams * per_beam;
+  int kept = 0;
+  for (int64_t q0 = 0; q0 < all; q0 += kThreads * kJoined) {
+    Candidate c[kJoined];
+    Candidate top = none;
+#pragma unroll
+    for (int i = 0; i < kJoined; ++i) {
+      const int64_t q = q0 + (int64_t)i * kThreads + threadIdx.x;
+      c[i] = none;
+      if (q < all) {
+        const int b = (int)(q / per_beam), rest = (int)(q - (int64_t)b * per_beam);
+        const float score = a.score[row0 + b];
+        if (score > -INFINITY) {
+          if (a.done && a.done[row0 + b]) {
+            if (rest == 0) c[i] = {order_of((double)score), (uint64_t)(uint32_t)~b << 32 | (uint32_t)~a.end_token};
+          } else {
+            const uint64_t k = a.lists[(int64_t)(row0 + b) * per_beam + rest];
+            if (k) c[i] = {order_of((double)score + ((double)value_of((uint32_t)(k >> 32)) - lse[b])), (uint64_t)(uint32_t)~b << 32 | (uint32_t)k};
+          }
+        }
+      }
+      if (greater(c[i], top)) top = c[i];
+    }
+#pragma unroll
+    for (int d = 1; d < kPerGroup; d *= 2) {
+      const Candidate other = {(uint64_t)__shfl_xor((unsigned long long)top.score, d), (uint64_t)__shfl_xor((unsigned long long)top.place, d)};
+      if (greater(other, top)) top = other;
+    }
+    if (threadIdx.x % kPerGroup == 0) groups[threadIdx.x / kPerGroup] = top;
+    __syncthreads();
+    // (candidates differ from each other, but for those that are none)
+    const Candidate mine = groups[lane];
+    const int at = lane_of_rank(a.keep - 1, [&](int j, int i) {
+      const Candidate other = groups[j];
+      return greater(other, mine) || (other.score == mine.score && other.place == mine.place && j < i);
+    });
+    const Candidate border = groups[at];
+#pragma unroll
+    for (int i = 0; i < kJoined; ++i)
+      if (c[i].score && !greater(border, c[i])) found[kept + atomicAdd(&listed, 1)] = c[i];
+    __syncthreads();
+    const int n = kept + listed;
+    best_of(found, n, a.keep, none, [](const Candidate& x, const Candidate& y) { return greater(x, y); }, [&](int i, const Candidate& k) { best[i] = k; });
+    __syncthreads();
+    kept = min(n, a.keep);
+    if ((int)threadIdx.x < kept) found[threadIdx.x] = best[threadIdx.x];
+    if (threadIdx.x == 0) listed = 0;
+    __syncthreads();
+  }
+  if ((int)threadIdx.x < a.keep) {
+    const bool there = (int)threadIdx.x < kept;
+    const Candidate k = there ? best[threadIdx.x] : none;
+    const int64_t at = (int64_t)blockIdx.x * a.keep + threadIdx.x;
+    const int beam = (int)~(uint32_t)(k.place >> 32), token = (int)~(uint32_t)k.place;
+    a.parent[at] = there ? row0 + beam : -1;
+    a.token[at] = there ? token : -1;
+    a.new_score[at] = there ? (float)score_of(k.score) : -INFINITY;
+    if (a.new_done) a.new_done[at] = there && ((a.done && a.done[row0 + beam]) || (token >= 0 && token == a.end_token));
+  }
+}
+
+// How a call is divided: chunks of 8192 logits where there are enough for every CU, else of 2048.
+struct BeamPlan { int32_t each, chunks; int64_t blocks; };
+BeamPlan plan_beam(int64_t rows, int32_t vocab) {
+  BeamPlan p;
+  p.each = rows * ((vocab + (int64_t)kThreads * 32 - 1) / (kThreads * 32)) >= 512 ? 32 : 8;
+  p.chunks = (int32_t)((vocab + (int64_t)kThreads * p.each - 1) / (kThreads * p.each));
+  p.blocks = rows * p.chunks;
+  return p;
+}
+size_t beam_bytes(const BeamPlan& p, int32_t keep) { return pad_to((size_t)p.blocks * keep * 8, 256) + pad_to((size_t)p.blocks * 8, 256) + pad_to((size_t)p.blocks * 4, 256); }
+
+int check_beam(const char* who, int32_t n_prompts, int32_t beams, int32_t vocab, int32_t keep) {
+  if (n_prompts < 0 || beams < 1 || vocab < 1 || keep < 1) return fail(FCP_ERR_INVALID_ARG, "%s: n_prompts must not be negative, beams, vocab and keep at least 1", who);
+  if (beams > FCP_BEAM_MAX_BEAMS || keep > FCP_BEAM_MAX_KEEP)
+    return fail(FCP_ERR_UNSUPPORTED, "%s: %d beams, %d kept; at most %d and %d", who, beams, keep, FCP_BEAM_MAX_BEAMS, FCP_BEAM_MAX_KEEP);
+  if (vocab > 1 << 30) return fail(FCP_ERR_UNSUPPORTED, "%s: a vocabulary of more than 2^30", who);
+  if ((int64_t)n_prompts * beams > INT32_MAX || !fits_axis(plan_beam((int64_t)n_prompts * beams, vocab).blocks, kThreads))
+    return fail(FCP_ERR_UNSUPPORTED, "%s: 2^24 chunks of logits or more", who);
+  return FCP_OK;
+}
+
+template <class T, int E>
+int launch_rows(const BeamArgs& a, const BeamPlan& p, hipStream_t st) {
+  static std::atomic<uint64_t> raised;
+  const int bytes = list_room(a.keep, E) * 8;
+  if (bytes > 60 * 1024)
+    if (int rc = raise_lds_limit(reinterpret_cast<const void*>(beam_rows_kernel<T, E>), bytes, raised)) return rc;
+  beam_rows_kernel<T, E><<<dim3((unsigned)p.blocks), dim3(kThreads), bytes, st>>>(a);
+  FCP_HIP_CHECK(hipGetLastError());
+  return FCP_OK;
+}
+
+}  // namespace
+}  // namespace fcp
+
+extern "C" size_t fcp_beam_scratch_bytes(int32_t n_prompts, int32_t beams, int32_t vocab, int32_t keep) {
+  using namespace fcp;
+  clear_error();
+  if (check_beam("fcp_beam_scratch_bytes", n_prompts, beams, vocab, keep)) return 0;
+  const size_t n = beam_bytes(plan_beam((int64_t)n_prompts * beams, vocab), keep);
+  return n ? n : 256;
+}
+
+extern "C" int fcp_beam_select(const void* logits, int32_t type, int64_t logits_row, int32_t n_prompts, int32_t beams, int32_t vocab, const float* score,
+                               const uint8_t* done, int32_t end_token, int32_t keep, int32_t* parent, int32_t* token, float* new_score,
+                               uint8_t* new_done, void* scratch, size_t scratch_bytes, void* stream) {
+  using namespace fcp;
+  clear_error();
+  const char* who = "fcp_beam_select";
+  if (int rc = check_beam(who, n_prompts, beams, vocab, keep)) return rc;
+  if (type != FCP_BF16 && type != FCP_F32) return fail(FCP_ERR_UNSUPPORTED, "%s: type %d is not known", who, type);
+  if (end_token < -1 || end_token >= vocab) return fail(FCP_ERR_INVALID_ARG, "%s: end_token %d is neither -1 nor a token", who, end_token);
+  if (n_prompts == 0) return FCP_OK;
+  if (!logits || !score || !parent || !token || !new_score) return fail(FCP_ERR_INVALID_ARG, "%s: null argument", who);
+  if (logits_row < vocab) return fail(FCP_ERR_INVALID_ARG, "%s: rows of logits overlap", who);
+  if ((uintptr_t)logits % (type == FCP_BF16 ? 2 : 4) || (uintptr_t)score % 4 || (uintptr_t)parent % 4 || (uintptr_t)token % 4 || (uintptr_t)new_score % 4)
+    return fail(FCP_ERR_INVALID_ARG, "%s: an argument is not aligned to its type", who);
+  if (new_score == score || (new_done && new_done == done)) return fail(FCP_ERR_INVALID_ARG, "%s: outputs must lie apart from inputs", who);
+  if (!scratch || (uintptr_t)scratch % 256) return fail(FCP_ERR_INVALID_ARG, "%s: scratch must be 256-byte aligned", who);
+  const BeamPlan p = plan_beam((int64_t)n_prompts * beams, vocab);
+  const size_t need = beam_bytes(p, keep);
+  if (scratch_bytes < need) return fail(FCP_ERR_CAPACITY, "%s: scratch has %zu bytes, %zu are needed", who, scratch_bytes, need);
+  BeamArgs a = {logits, logits_row, n_prompts * beams, beams, vocab, p.chunks, keep, end_token, score, done, parent, token, new_score, new_done};
+  char* const at = static_cast<char*>(scratch);
+  a.lists = reinterpret_cast<uint64_t*>(at);
+  a.sums = reinterpret_cast<double*>(at + pad_to((size_t)p.blocks * keep * 8, 256));
+  a.tops = reinterpret_cast<float*>(at + pad_to((size_t)p.blocks * keep * 8, 256) + pad_to((size_t)p.blocks * 8, 256));
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const bool bf16 = type == FCP_BF16;
+  if (int rc = p.each == 32 ? (bf16 ? launch_rows<__bf16, 32>(a, p, st) : launch_rows<float, 32>(a, p, st))
+                            : (bf16 ? launch_rows<__bf16, 8>(a, p, st) : launch_rows<float, 8>(a, p, st)))
+    return rc;
+  // candidates of a block's look lie in `keep` groups of four threads; the best so far beside them
+  static std::atomic<uint64_t> raised;
+  int room = 1;
+  while (room < keep + keep * kPerGroup * kJoined) room *= 2;
+  const int bytes = room * (int)sizeof(Candidate);
+  if (bytes > 48 * 1024)
+    if (int rc = raise_lds_limit(reinterpret_cast<const void*>(beam_join_kernel), bytes, raised)) return rc;
+  beam_join_kernel<<<dim3((unsigned)n_prompts), dim3(kThreads), bytes, st>>>(a);
+  FCP_HIP_CHECK(hipGetLastError());
+  return FCP_OK;
+}

@@ -752,7 +752,9 @@ int check_places(const char* who, const AttnPlan& p) {
 
 }  // namespace
 
-size_t evict_scratch_bytes(const char* who, const CacheView& c, int32_t n_seqs, int32_t max_pages);       // 0: refused
+// 0: refused
+size_t evict_scratch_bytes(const char* who, const CacheView& c, int32_t n_seqs, int32_t max_pages);
+size_t page_scratch_bytes(const char* who, const CacheView& c, bool fork, int32_t n_seqs, int32_t max_pages);
 
 }  // namespace fcp
 
@@ -761,9 +763,10 @@ extern "C" size_t fcp_cache_scratch_bytes(int which, const fcp_cache* cache, int
   clear_error();
   const char* who = "fcp_cache_scratch_bytes";
   CacheView c;
-  if (check_cache(who, cache, which != FCP_SCRATCH_CACHE_ATTN, &c)) return 0;
+  if (check_cache(who, cache, which == FCP_SCRATCH_CACHE_WEIGH || which == FCP_SCRATCH_CACHE_EVICT, &c)) return 0;
   if (check_sizes(who, c, n_seqs, max_pages, tq)) return 0;
   if (which == FCP_SCRATCH_CACHE_EVICT) return evict_scratch_bytes(who, c, n_seqs, max_pages);
+  if (which == FCP_SCRATCH_CACHE_FORK || which == FCP_SCRATCH_CACHE_COMPACT) return page_scratch_bytes(who, c, which == FCP_SCRATCH_CACHE_FORK, n_seqs, max_pages);
   if (which != FCP_SCRATCH_CACHE_ATTN && which != FCP_SCRATCH_CACHE_WEIGH) { fail(FCP_ERR_INVALID_ARG, "%s: which = %d is not known", who, which); return 0; }
   if (check_heads(who, c, hq)) return 0;
   const bool weigh = which == FCP_SCRATCH_CACHE_WEIGH;

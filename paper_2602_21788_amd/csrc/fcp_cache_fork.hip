@@ -1,0 +1,412 @@
+// fcp_cache_fork and fcp_cache_compact: who holds which page of the cache, kept on the device.
+//
+// A sequence that continues another one takes over its table; pages that are only read are shared, and a page that new tokens go into is copied for all of those who would write it but one.
+// Both calls look at all entries of the tables once and set bits, one a page; then one block counts through the bits for free pages, in increasing order, and lists the copies;
+// the last launch copies: 16 bytes a thread, a block for each (page, KV head), whose keys are one run of memory and whose values are another.
+// Small calls are chains of loads, large ones are bound by the memory.
+#include "fcp_cache.h"
+
+namespace fcp {
+namespace {
+
+constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64;
+
+struct Copy { int32_t from, to, tokens, pad; };
+
+struct PageArgs {
+  CacheView c;
+  SeqView s;                           // this step's sequences (no rows); rows of both tables are max_pages long
+  const int32_t* parent;               // fork: [n_new]
+  const int32_t* news;
+  int32_t n_new;
+  const uint8_t* busy;
+  int32_t* new_pages;
+  int32_t* new_len;
+  int32_t* counts;
+  // scratch
+  uint32_t* held;                      // a bit a page: sequences of this step (or others) hold it
+  uint32_t* read;                      // fork: sequences of the next step (or others) hold it and do not write it
+  int32_t* lowest;                     // fork: of the sequences of the next step that would write a page, the lowest; only entries of such pages mean something
+  int32_t* list;                       // fork: free pages; compact: pages that stay empty otherwise, in which others move
+  Copy* copies;
+  int32_t* n_copies;                   // compact
+  int32_t words;
+};
+
+__device__ inline int32_t cached(const PageArgs& a, int seq) {
+  const int64_t room = (int64_t)a.s.max_pages << a.c.log_page;
+  const int32_t n = max(a.s.kv_len[seq], 0);
+  return n < room ? n : (int32_t)room;
+}
+// A sequence of the next step: whom it continues (-1: nobody), tokens before and after, the place of the page in which both lie (-1: there is none).
+struct Next { int32_t parent, before, after, writes; };
+__device__ inline Next next_of(const PageArgs& a, int seq) {
+  const int32_t p = a.parent[seq], n = max(a.news[seq], 0);
+  const bool there = (uint32_t)p < (uint32_t)a.s.n_seqs;
+  const int32_t before = there ? cached(a, p) : 0;
+  const int64_t after = min((int64_t)before + n, (int64_t)a.s.max_pages << a.c.log_page);
+  return {there ? p : -1, before, (int32_t)after, after > before && (before & (a.c.page - 1)) ? before >> a.c.log_page : -1};
+}
+__device__ inline int32_t pages_for(const PageArgs& a, int32_t tokens) { return (int32_t)(((int64_t)tokens + a.c.page - 1) >> a.c.log_page); }
+__device__ inline int32_t entry(const PageArgs& a, int seq, int place) {
+  const int32_t p = a.s.pages[(int64_t)seq * a.s.max_pages + place];
+  return (uint32_t)p < (uint32_t)a.c.n_pages ? p : -1;
+}
+__device__ inline void set_bit(uint32_t* bits, int32_t page) { atomicOr(bits + (page >> 5), 1u << (page & 31)); }
+__device__ inline bool bit(const uint32_t* bits, int32_t page) { return bits[page >> 5] >> (page & 31) & 1; }
+
+// Sum over the block before this thread, and of all threads.  Every thread calls.
+struct Scan { int32_t before, all; };
+__device__ inline Scan block_scan(int32_t x, int32_t* sums) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int32_t upto = wave_prefix_sum(x);
+  if (lane == 63) sums[wave] = upto;
+  __syncthreads();
+  Scan r = {upto - x, 0};
+#pragma unroll
+  for (int w = 0; w < kPlanWaves; ++w) {
+    const int32_t n = sums[w];
+    r.before += w < wave ? n : 0;
+    r.all += n;
+  }
+  __syncthreads();
+  return r;
+}
+
+// ---- first launch: busy pages' bits, nothing else held; pages that are written have no writer yet -----------------
+template <bool Fork>
+__global__ __launch_bounds__(256) void clear_kernel(PageArgs a) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i < a.words) {
+    uint32_t w = 0;
+    if (a.busy)
+      for (int j = 0; j < 32 && i * 32 + j < a.c.n_pages; ++j) w |= (uint32_t)(a.busy[i * 32 + j] != 0) << j;
+    a.held[i] = Fork ? w : 0;
+    if (Fork) a.read[i] = w;
+  }
+  if (Fork && i < a.n_new) {
+    const Next x = next_of(a, i);
+    const int32_t page = x.writes >= 0 ? entry(a, x.parent, x.writes) : -1;
+    if (page >= 0) a.lowest[page] = INT32_MAX;
+    a.new_len[i] = x.after;
+  }
+}
+
+// ---- second launch: the bits of all entries, a wave for 64 places of a sequence -----------------------------------
+template <bool Fork>
+__global__ __launch_bounds__(256) void mark_kernel(PageArgs a) {
+  const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int per_seq = (a.s.max_pages + 63) / 64;
+  const int64_t seq = unit / per_seq;
+  const int place = (int)(unit % per_seq) * 64 + (threadIdx.x & 63);
+  if (place >= a.s.max_pages) return;
+  if (seq < a.s.n_seqs) {
+    if (place < pages_for(a, cached(a, (int)seq))) {
+      const int32_t page = entry(a, (int)seq, place);
+      if (page >= 0 && !bit(a.held, page)) set_bit(a.held, page);
+    }
+  } else if (Fork && seq - a.s.n_seqs < a.n_new) {
+    const int i = (int)(seq - a.s.n_seqs);
+    const Next x = next_of(a, i);
+    const int32_t page = place < pages_for(a, x.before) ? entry(a, x.parent, place) : -1;
+    a.new_pages[(int64_t)i * a.s.max_pages + place] = page;
+    if (page >= 0) {
+      if (place == x.writes) atomicMin(a.lowest + page, i);
+      else if (!bit(a.read, page)) set_bit(a.read, page);
+    }
+  }
+}
+
+// ---- third launch: one block hands out pages ----------------------------------------------------------------------
+__global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(PageArgs a) {
+  __shared__ int32_t sums[kPlanWaves];
+  // pages that are free now, and those that nobody holds but who writes them
+  int32_t need = 0, kept = 0;
+  auto copied = [&](int i, const Next& x, int32_t& page) {
+    page = x.writes >= 0 ? entry(a, x.parent, x.writes) : -1;
+    return page >= 0 && (bit(a.read, page) || a.lowest[page] != i);
+  };
+  for (int i = threadIdx.x; i < a.n_new; i += kPlanThreads) {
+    const Next x = next_of(a, i);
+    int32_t page;
+    const bool copy = copied(i, x, page);
+    need += copy + pages_for(a, x.after) - pages_for(a, x.before);
+    kept += page >= 0 && !copy;
+  }
+  need = block_scan(need, sums).all;
+  kept = block_scan(kept, sums).all;
+  int32_t listed = 0, held = 0;
+  for (int w0 = 0; w0 < a.words; w0 += kPlanThreads) {
+    const int w = w0 + threadIdx.x;
+    uint32_t free = w < a.words ? ~a.held[w] : 0u;
+    if (w == a.words - 1 && a.c.n_pages % 32) free &= (1u << (a.c.n_pages % 32)) - 1;
+    held += w < a.words ? __popc(a.read[w]) : 0;
+    const Scan at = block_scan(__popc(free), sums);
+    int32_t rank = listed + at.before;
+    for (; free && rank < need; free &= free - 1) a.list[rank++] = 32 * w + __builtin_ctz(free);
+    listed += at.all;
+  }
+  held = block_scan(held, sums).all;
+  const int32_t taken = min(need, listed);
+  if (threadIdx.x == 0) {
+    a.counts[0] = taken;
+    a.counts[1] = need - taken;
+    a.counts[2] = a.c.n_pages - held - kept - taken;
+  }
+  __threadfence_block();
+  int32_t before = 0;
+  for (int i0 = 0; i0 < a.n_new; i0 += kPlanThreads) {
+    const int i = i0 + threadIdx.x;
+    Next x = {};
+    int32_t page = -1;
+    bool copy = false;
+    if (i < a.n_new) {
+      x = next_of(a, i);
+      copy = copied(i, x, page);
+    }
+    const Scan at = block_scan(i < a.n_new ? copy + pages_for(a, x.after) - pages_for(a, x.before) : 0, sums);
+    if (i < a.n_new) {
+      int32_t rank = before + at.before;
+      int32_t* const table = a.new_pages + (int64_t)i * a.s.max_pages;
+      auto next = [&] { const int32_t r = rank++; return r < taken ? a.list[r] : -1; };
+      Copy c = {page, -1, 0, 0};
+      if (copy) {
+        c.to = table[x.writes] = next();
+        c.tokens = c.to >= 0 ? x.before & (a.c.page - 1) : 0;
+      }
+      a.copies[i] = c;
+      for (int place = pages_for(a, x.before); place < pages_for(a, x.after); ++place) table[place] = next();
+    }
+    before += at.all;
+  }
+}
+
+// The pages in use move to the lowest numbers that are not busy: `end` is the first number past these.
+__global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(PageArgs a) {
+  __shared__ int32_t sums[kPlanWaves];
+  __shared__ int32_t end_at, busy_end;
+  auto busy_bits = [&](int w) {
+    uint32_t b = 0;
+    if (a.busy)
+      for (int j = 0; j < 32 && w * 32 + j < a.c.n_pages; ++j) b |= (uint32_t)(a.busy[w * 32 + j] != 0) << j;
+    return b;
+  };
+  if (threadIdx.x == 0) end_at = busy_end = 0;
+  __syncthreads();
+  int32_t used = 0, all = 0;
+  for (int w = threadIdx.x; w < a.words; w += kPlanThreads) {
+    const uint32_t h = a.held[w], b = busy_bits(w);
+    used += __popc(h & ~b);
+    all += __popc(h);
+    if (b) atomicMax(&busy_end, 32 * w + 32 - __builtin_clz(b));
+  }
+  used = block_scan(used, sums).all;
+  all = block_scan(all, sums).all;
+  // the used-th page that is not busy
+  int32_t seen = 0;
+  for (int w0 = 0; w0 < a.words && seen < used; w0 += kPlanThreads) {
+    const int w = w0 + threadIdx.x;
+    uint32_t open = w < a.words ? ~busy_bits(w) : 0u;
+    const Scan at = block_scan(__popc(open), sums);
+    int32_t rank = seen + at.before;
+    if (rank < used && rank + __popc(open) >= used) {
+      for (; rank + 1 < used; ++rank) open &= open - 1;
+      end_at = 32 * w + __builtin_ctz(open) + 1;
+    }
+    seen += at.all;
+  }
+  __syncthreads();
+  const int32_t end = end_at;
+  int32_t holes = 0, movers = 0;
+  for (int w0 = 0; w0 < a.words; w0 += kPlanThreads) {
+    const int w = w0 + threadIdx.x;
+    uint32_t hole = 0, mover = 0;
+    if (w < a.words) {
+      const uint32_t h = a.held[w], b = busy_bits(w), low = 32 * w + 32 <= end ? ~0u : 32 * w >= end ? 0u : (1u << (end - 32 * w)) - 1;
+      hole = low & ~h & ~b;
+      mover = ~low & h & ~b;
+    }
+    const Scan hs = block_scan(__popc(hole), sums), ms = block_scan(__popc(mover), sums);
+    int32_t rank = holes + hs.before;
+    for (; hole; hole &= hole - 1) a.list[rank++] = 32 * w + __builtin_ctz(hole);
+    rank = movers + ms.before;
+    for (; mover; mover &= mover - 1) a.copies[rank++] = {32 * w + __builtin_ctz(mover), -1, a.c.page, 0};
+    holes += hs.all;
+    movers += ms.all;
+  }
+  __threadfence_block();
+  __syncthreads();
+  for (int i = threadIdx.x; i < movers; i += kPlanThreads) {
+    const int32_t from = a.copies[i].from, to = a.list[i];
+    a.copies[i].to = to;
+    a.lowest[from] = to;
+  }
+  if (threadIdx.x == 0) {
+    a.counts[0] = movers;
+    a.counts[1] = all;
+    a.counts[2] = max(end, busy_end);
+    a.n_copies[0] = movers;
+    a.n_copies[1] = end;
+  }
+}
+
+// ---- last launch --------------------------------------------------------------------------------------------------
+// The first `tokens` tokens of a (page, KV head), values in whole groups.
+__device__ inline void copy_page(const CacheView& c, int head_dim, const Copy& x, int head) {
+  const int64_t from = block_of(c, x.from, head), to = block_of(c, x.to, head);
+  const int row = head_dim / 16, keys = x.tokens * row, values = (x.tokens + kGroup - 1) / kGroup * kGroup * row;
+  const u32x4* const k0 = reinterpret_cast<const u32x4*>(c.k) + from * c.page * row;
+  const u32x4* const v0 = reinterpret_cast<const u32x4*>(c.v) + from * c.page * row;
+  u32x4* const k1 = reinterpret_cast<u32x4*>(c.k) + to * c.page * row;
+  u32x4* const v1 = reinterpret_cast<u32x4*>(c.v) + to * c.page * row;
+  for (int i = threadIdx.x; i < values; i += 256) {
+    const bool key = i < keys;
+    const u32x4 v = v0[i], k = k0[key ? i : 0];
+    v1[i] = v;
+    if (key) k1[i] = k;
+  }
+  if (c.weight && (int)threadIdx.x < x.tokens) c.weight[to * c.page + threadIdx.x] = c.weight[from * c.page + threadIdx.x];
+  if (threadIdx.x == 128) c.k_scale[to] = c.k_scale[from];
+  if (threadIdx.x == 129) c.v_scale[to] = c.v_scale[from];
+}
+__global__ __launch_bounds__(256) void fork_copy_kernel(PageArgs a, int head_dim) {
+  const Copy x = a.copies[blockIdx.x / a.c.hkv];
+  if (x.tokens > 0) copy_page(a.c, head_dim, x, blockIdx.x % a.c.hkv);
+}
+__global__ __launch_bounds__(256) void compact_copy_kernel(PageArgs a, int head_dim, int table_blocks) {
+  const int32_t end = a.n_copies[1];
+  if ((int)blockIdx.x < table_blocks) {
+    const int64_t all = (int64_t)a.s.n_seqs * a.s.max_pages;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)table_blocks * 256) {
+      const int seq = (int)(i / a.s.max_pages), place = (int)(i % a.s.max_pages);
+      int32_t page = place < pages_for(a, cached(a, seq)) ? entry(a, seq, place) : -1;
+      if (page >= end && !(a.busy && a.busy[page])) page = a.lowest[page];
+      a.new_pages[i] = page;
+    }
+    return;
+  }
+  const int64_t all = (int64_t)a.n_copies[0] * a.c.hkv;
+  for (int64_t u = blockIdx.x - table_blocks; u < all; u += gridDim.x - table_blocks) copy_page(a.c, head_dim, a.copies[u / a.c.hkv], (int)(u % a.c.hkv));
+}
+
+// ---- host ---------------------------------------------------------------------------------------------------------
+struct PageSpace { size_t held, read, lowest, list, copies, n_copies, bytes; int32_t words; };
+PageSpace page_space(const CacheView& c, int64_t n_copies) {
+  PageSpace s = {};
+  s.words = (int32_t)(((int64_t)c.n_pages + 31) / 32);
+  const size_t bits = pad_to((size_t)s.words * 4, 256), entries = pad_to((size_t)c.n_pages * 4, 256);
+  s.read = bits;
+  s.lowest = 2 * bits;
+  s.list = s.lowest + entries;
+  s.copies = s.list + entries;
+  s.n_copies = s.copies + pad_to((size_t)n_copies * sizeof(Copy), 256);
+  s.bytes = s.n_copies + 256;
+  return s;
+}
+void place_scratch(PageArgs& a, const PageSpace& s, void* scratch) {
+  char* const at = static_cast<char*>(scratch);
+  a.held = reinterpret_cast<uint32_t*>(at);
+  a.read = reinterpret_cast<uint32_t*>(at + s.read);
+  a.lowest = reinterpret_cast<int32_t*>(at + s.lowest);
+  a.list = reinterpret_cast<int32_t*>(at + s.list);
+  a.copies = reinterpret_cast<Copy*>(at + s.copies);
+  a.n_copies = reinterpret_cast<int32_t*>(at + s.n_copies);
+  a.words = s.words;
+}
+int check_page_sizes(const char* who, const CacheView& c, int32_t n_seqs, int32_t n_new, int32_t max_pages) {
+  if (int rc = check_sizes(who, c, n_seqs, max_pages, 0)) return rc;
+  if (int rc = check_sizes(who, c, n_new, max_pages, 0)) return rc;
+  if (!fits_axis((((int64_t)n_seqs + n_new) * ((max_pages + 63) / 64) + 3) / 4, 256) || !fits_axis((int64_t)n_new * c.hkv, 256))
+    return fail(FCP_ERR_UNSUPPORTED, "%s: 2^24 blocks of work or more", who);
+  return FCP_OK;
+}
+int check_scratch(const char* who, const void* scratch, size_t have, size_t need) {
+  if (!scratch || (uintptr_t)scratch % 256) return fail(FCP_ERR_INVALID_ARG, "%s: scratch must be 256-byte aligned", who);
+  if (have < need) return fail(FCP_ERR_CAPACITY, "%s: scratch has %zu bytes, %zu are needed", who, have, need);
+  return FCP_OK;
+}
+
+}  // namespace
+
+// 0: refused
+size_t page_scratch_bytes(const char* who, const CacheView& c, bool fork, int32_t n_seqs, int32_t max_pages) {
+  if (check_page_sizes(who, c, fork ? 0 : n_seqs, fork ? n_seqs : 0, max_pages)) return 0;
+  return page_space(c, fork ? n_seqs : c.n_pages).bytes;
+}
+
+}  // namespace fcp
+
+extern "C" int fcp_cache_fork(const fcp_cache* cache, const int32_t* pages, const int32_t* kv_len, int32_t n_seqs, int32_t max_pages, const int32_t* parent,
+                              const int32_t* news, int32_t n_new, const uint8_t* busy, int32_t* new_pages, int32_t* new_len, int32_t* counts,
+                              void* scratch, size_t scratch_bytes, void* stream) {
+  using namespace fcp;
+  clear_error();
+  const char* who = "fcp_cache_fork";
+  PageArgs a = {};
+  if (int rc = check_cache(who, cache, false, &a.c)) return rc;
+  if (int rc = check_page_sizes(who, a.c, n_seqs, n_new, max_pages)) return rc;
+  if (int rc = check_seqs(who, a.c, nullptr, false, kv_len, pages, n_seqs, max_pages, 0)) return rc;
+  if (!counts || (n_new > 0 && (!parent || !news || !new_len || (max_pages > 0 && !new_pages)))) return fail(FCP_ERR_INVALID_ARG, "%s: null argument", who);
+  if ((new_pages && new_pages == pages) || (new_len && new_len == kv_len)) return fail(FCP_ERR_INVALID_ARG, "%s: the new tables must lie apart from the old ones", who);
+  const PageSpace space = page_space(a.c, n_new);
+  if (int rc = check_scratch(who, scratch, scratch_bytes, space.bytes)) return rc;
+  a.s = {nullptr, kv_len, pages, n_seqs, max_pages, 0};
+  a.parent = parent;
+  a.news = news;
+  a.n_new = n_new;
+  a.busy = busy;
+  a.new_pages = new_pages;
+  a.new_len = new_len;
+  a.counts = counts;
+  place_scratch(a, space, scratch);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  clear_kernel<true><<<dim3((unsigned)((max(space.words, n_new) + 255) / 256)), dim3(256), 0, st>>>(a);
+  FCP_HIP_CHECK(hipGetLastError());
+  const int64_t units = ((int64_t)n_seqs + n_new) * ((max_pages + 63) / 64);
+  if (units > 0) {
+    mark_kernel<true><<<dim3((unsigned)((units + 3) / 4)), dim3(256), 0, st>>>(a);
+    FCP_HIP_CHECK(hipGetLastError());
+  }
+  fork_plan_kernel<<<dim3(1), dim3(kPlanThreads), 0, st>>>(a);
+  FCP_HIP_CHECK(hipGetLastError());
+  if (n_new > 0) {
+    fork_copy_kernel<<<dim3((unsigned)((int64_t)n_new * a.c.hkv)), dim3(256), 0, st>>>(a, cache->head_dim);
+    FCP_HIP_CHECK(hipGetLastError());
+  }
+  return FCP_OK;
+}
+
+extern "C" int fcp_cache_compact(const fcp_cache* cache, const int32_t* pages, const int32_t* kv_len, int32_t n_seqs, int32_t max_pages, const uint8_t* busy,
+                                 int32_t* new_pages, int32_t* counts, void* scratch, size_t scratch_bytes, void* stream) {
+  using namespace fcp;
+  clear_error();
+  const char* who = "fcp_cache_compact";
+  PageArgs a = {};
+  if (int rc = check_cache(who, cache, false, &a.c)) return rc;
+  if (int rc = check_page_sizes(who, a.c, n_seqs, 0, max_pages)) return rc;
+  if (int rc = check_seqs(who, a.c, nullptr, false, kv_len, pages, n_seqs, max_pages, 0)) return rc;
+  if (!counts || (n_seqs > 0 && max_pages > 0 && !new_pages)) return fail(FCP_ERR_INVALID_ARG, "%s: null argument", who);
+  const PageSpace space = page_space(a.c, a.c.n_pages);
+  if (int rc = check_scratch(who, scratch, scratch_bytes, space.bytes)) return rc;
+  a.s = {nullptr, kv_len, pages, n_seqs, max_pages, 0};
+  a.busy = busy;
+  a.new_pages = new_pages;
+  a.counts = counts;
+  place_scratch(a, space, scratch);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  clear_kernel<false><<<dim3((unsigned)((space.words + 255) / 256)), dim3(256), 0, st>>>(a);
+  FCP_HIP_CHECK(hipGetLastError());
+  const int64_t units = (int64_t)n_seqs * ((max_pages + 63) / 64), entries = (int64_t)n_seqs * max_pages;
+  if (units > 0) {
+    mark_kernel<false><<<dim3((unsigned)((units + 3) / 4)), dim3(256), 0, st>>>(a);
+    FCP_HIP_CHECK(hipGetLastError());
+  }
+  compact_plan_kernel<<<dim3(1), dim3(kPlanThreads), 0, st>>>(a);
+  FCP_HIP_CHECK(hipGetLastError());
+  const int table_blocks = (int)min((entries + 1023) / 1024, (int64_t)256), copy_blocks = (int)min(min((int64_t)a.c.n_pages, entries) * a.c.hkv, (int64_t)2048);
+  if (entries > 0) {
+    compact_copy_kernel<<<dim3((unsigned)(table_blocks + copy_blocks)), dim3(256), 0, st>>>(a, cache->head_dim, table_blocks);
+    FCP_HIP_CHECK(hipGetLastError());
+  }
+  return FCP_OK;
+}
