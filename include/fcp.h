@@ -478,6 +478,7 @@ typedef struct fcp_cache {
 #define FCP_SCRATCH_CACHE_ATTN 2
 #define FCP_SCRATCH_CACHE_WEIGH 3
 #define FCP_SCRATCH_CACHE_EVICT 4
+#define FCP_SCRATCH_CACHE_SHARED 5    /* for any number of groups                             */
 #define FCP_SCRATCH_CACHE_FORK 6      /* n_seqs: sequences of the next step; tq, hq not used */
 #define FCP_SCRATCH_CACHE_COMPACT 7   /* tq, hq not used                                      */
 size_t fcp_cache_scratch_bytes(int which, const fcp_cache* cache, int32_t n_seqs, int32_t max_pages, int32_t tq, int32_t hq);
@@ -571,6 +572,21 @@ int fcp_cache_fork(const fcp_cache* cache, const int32_t* pages, const int32_t* 
  */
 int fcp_cache_compact(const fcp_cache* cache, const int32_t* pages, const int32_t* kv_len, int32_t n_seqs, int32_t max_pages, const uint8_t* busy,
                       int32_t* new_pages, int32_t* counts, void* scratch, size_t scratch_bytes, void* stream);
+
+/*
+ * fcp_cache_attn_shared -- fcp_cache_attn (without weigh) for a batch whose sequences have common beginnings: beams or samples of a prompt, questions about a document.  The common tokens
+ * of a group are read and multiplied once for all of its rows, and every sequence's own tokens by themselves; the result is that of attention over the whole table, up to rounding.
+ *   groups [n_groups + 1] int32 device: the sequences groups[g] .. groups[g + 1] - 1 are group g; not falling, within 0 .. n_seqs (else the call does nothing, as where cu_seqlens falls).
+ *   Sequences outside all groups, and groups of one sequence with rows, are worked by themselves.
+ *   shared_len [n_groups] int32 device: tokens that the sequences of the group have in common: their tables name the same pages there, and those of the group's first sequence with rows are
+ *   read.  Less is taken where a row does not see as many: whole pages, at most the tokens before the new ones of every sequence.
+ *   n_groups from 0 to n_seqs.  scratch: fcp_cache_scratch_bytes(FCP_SCRATCH_CACHE_SHARED, ...).  Other arguments, results, limits and errors as in fcp_cache_attn.
+ * Scores, statistics and sums are held in 32 bits; probabilities are rounded to bf16 for the product with V, and for the parts that up to 32 rows on average see, of a group or of a sequence
+ * and KV head, what that leaves is multiplied too.  No atomics: results repeat bit for bit.
+ */
+int fcp_cache_attn_shared(const fcp_cache* cache, const void* q, int64_t q_row, int32_t tq, int32_t hq, const int32_t* cu_seqlens, const int32_t* kv_len,
+                          const int32_t* pages, int32_t n_seqs, int32_t max_pages, const int32_t* groups, const int32_t* shared_len, int32_t n_groups,
+                          float softmax_scale, void* o, float* lse, void* scratch, size_t scratch_bytes, void* stream);
 
 /*
  * fcp_beam_select -- the `keep` best continuations of every prompt.  A prompt has `beams` rows of logits; token t behind beam b has the score

@@ -19,7 +19,7 @@ LIB_PATH = os.path.join(_PKG, "libfcp.so")
 FCP_OK, FCP_ERR_INVALID_ARG, FCP_ERR_CAPACITY, FCP_ERR_UNSUPPORTED, FCP_ERR_HIP, FCP_ERR_STALLED = 0, -1, -2, -3, -4, -5
 FCP_SCRATCH_FWD, FCP_SCRATCH_BWD = 0, 1
 FCP_SCRATCH_CACHE_ATTN, FCP_SCRATCH_CACHE_WEIGH, FCP_SCRATCH_CACHE_EVICT = 2, 3, 4
-FCP_SCRATCH_CACHE_FORK, FCP_SCRATCH_CACHE_COMPACT = 6, 7
+FCP_SCRATCH_CACHE_SHARED, FCP_SCRATCH_CACHE_FORK, FCP_SCRATCH_CACHE_COMPACT = 5, 6, 7
 FCP_BEAM_MAX_BEAMS, FCP_BEAM_MAX_KEEP = 256, 64
 FCP_BF16, FCP_F32 = 0, 1
 FCP_ROTARY_HALF, FCP_ROTARY_PAIRS = 0, 1
@@ -39,7 +39,7 @@ EXPORTS = ["fcp_last_error", "fcp_shard_plan", "fcp_plan_groups", "fcp_scratch_b
            "fcp_group_shard_args", "fcp_attn_fwd_step_running", "fcp_shard_plan_mixed", "fcp_mask_tables", "fcp_attn_fwd_step_mixed", "fcp_attn_bwd_step_mixed",
            "fcp_attn_bwd_step_direct", "fcp_grad_finalize_direct", "fcp_attn_fwd_step_direct", "fcp_lse_merge_direct", "fcp_attn_fwd_step_static",
            "fcp_rotary_frequencies", "fcp_rotary", "fcp_cache_scratch_bytes", "fcp_cache_append", "fcp_cache_attn", "fcp_cache_weigh", "fcp_cache_evict",
-           "fcp_cache_fork", "fcp_cache_compact", "fcp_beam_scratch_bytes", "fcp_beam_select"]
+           "fcp_cache_fork", "fcp_cache_compact", "fcp_cache_attn_shared", "fcp_beam_scratch_bytes", "fcp_beam_select"]
 
 
 class FcpError(RuntimeError):
@@ -126,6 +126,8 @@ def lib() -> ctypes.CDLL:
         L.fcp_cache_fork.argtypes = [P, P, P, I32, I32, P, P, I32, P, P, P, P, P, SZ, P]
         L.fcp_cache_compact.restype = ctypes.c_int
         L.fcp_cache_compact.argtypes = [P, P, P, I32, I32, P, P, P, P, SZ, P]
+        L.fcp_cache_attn_shared.restype = ctypes.c_int
+        L.fcp_cache_attn_shared.argtypes = [P, P, I64, I32, I32, P, P, P, I32, I32, P, P, I32, F, P, P, P, SZ, P]
         L.fcp_beam_scratch_bytes.restype = SZ
         L.fcp_beam_scratch_bytes.argtypes = [I32, I32, I32, I32]
         L.fcp_beam_select.restype = ctypes.c_int
@@ -610,6 +612,17 @@ def fcp_cache_compact(cache, pages, kv_len, new_pages, counts, scratch, busy=Non
         raise ValueError("new_pages must have the shape of pages")
     _check(lib().fcp_cache_compact(ctypes.byref(cache), pg, kl, n, m, _bytes_ptr(busy, "busy", cache.n_pages), _int_ptr(new_pages, "new_pages"),
                                    _int_ptr(counts, "counts", 3), _dev_ptr(scratch), scratch.numel() * scratch.element_size(), _stream(stream)))
+
+
+def fcp_cache_attn_shared(cache, q, cu_seqlens, kv_len, pages, groups, shared_len, softmax_scale, o, lse, scratch, stream=None):
+    """fcp_cache_attn where the sequences groups[g] .. groups[g + 1] - 1 have their first shared_len[g] tokens in common; groups [n_groups + 1], shared_len [n_groups] int32."""
+    qp, qr, tq, hq = _queries(cache, q, lse)
+    if o.dtype is not _bf16 or o.shape != q.shape:
+        raise ValueError("o must be a bf16 tensor of q's shape")
+    cu, kl, pg, n, m = _seqs(cu_seqlens, kv_len, pages)
+    n_groups = shared_len.numel()
+    _check(lib().fcp_cache_attn_shared(ctypes.byref(cache), qp, qr, tq, hq, cu, kl, pg, n, m, _int_ptr(groups, "groups", n_groups + 1), _int_ptr(shared_len, "shared_len"), n_groups,
+                                       softmax_scale, _dev_ptr(o), _dev_ptr(lse), _dev_ptr(scratch), scratch.numel() * scratch.element_size(), _stream(stream)))
 
 
 def fcp_beam_scratch_bytes(n_prompts, beams, vocab, keep) -> int:

@@ -130,6 +130,10 @@ __device__ inline float wave_maxf(float x) {
 // Checks what every call of the cache checks, and fills the view.  needs_weight: the call reads or writes weights.  Sizes apart: those who only ask for scratch have no tables yet.
 int check_cache(const char* who, const fcp_cache* cache, bool needs_weight, CacheView* out);
 int check_sizes(const char* who, const CacheView& c, int32_t n_seqs, int32_t max_pages, int32_t n_rows);
+int check_heads(const char* who, const CacheView& c, int32_t hq);
+int check_scale(const char* who, float scale);
+int check_row_count(const char* who, int32_t tq, int32_t hq);
+int check_rows(const char* who, const fcp_cache* cache, const void* q, int64_t q_row, int32_t tq, int32_t hq);
 int check_seqs(const char* who, const CacheView& c, const int32_t* cu, bool needs_cu, const int32_t* kv_len, const int32_t* pages, int32_t n_seqs, int32_t max_pages, int32_t n_rows);
 
 }  // namespace fcp

@@ -130,6 +130,9 @@ static_assert(sizeof(Divided) == 32, "eight words");
 __host__ __device__ constexpr int slot_floats(int head_dim, int rows) { return rows * (head_dim + 2); }
 inline __device__ float* piece_slot(const AttnArgs& a, int block, int piece, int floats) { return a.part + (int64_t)(2 * (block + piece) + (piece == 0 ? 1 : 0)) * floats; }
 
+// Places are 32-bit numbers, and so is the one that a block of the weights' kernel, one of up to 2 kBlocks, steps to past the last.
+constexpr int64_t kMostPlaces = INT32_MAX - 2 * kBlocks;
+
 constexpr int kManyRows = 128;         // rows of a block in the kernel for many, or half of them
 
 int launch_attn_rows(const AttnArgs& a, int head_dim, int format, int rows, bool whole, hipStream_t st);

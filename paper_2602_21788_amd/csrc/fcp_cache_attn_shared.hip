@@ -1,0 +1,519 @@
+// fcp_cache_attn_shared: attention over the paged 8-bit cache where the sequences of a group have a common beginning.
+//
+// softmax over a sequence's tokens is put together from two parts: the common beginning, which all rows of the group see whole, and the sequence's own rest.  The group's rows are next
+// to each other, so the common part is attention of many rows over one run of keys: its bytes are read once for the group instead of once for every sequence, and where one token of a
+// sequence alone would leave the matrix units idle, a group's rows fill their tiles.  Partial results (sums, maximum, sum of exponentials) meet in the last launch.
+//   * First launch, one block: the parts and their places on two lines (csrc/fcp_cache_attn.h), one of all common parts, one of all own parts.
+//   * A launch for each line, with the kernels' bodies for few or for many rows as the rows of a group, and of a sequence, are on average.
+//   * A wave for each row joins the pieces of its two items.
+#include "fcp_cache_few.h"
+#include "fcp_cache_many.h"
+
+namespace fcp {
+namespace {
+
+enum { kCommon = 0, kOwn = 1 };
+
+// A run of cached tokens and the rows that attend over it.
+struct Part {
+  int32_t row0, rows;                  // rows of q, tokens; rows = 0: nothing to do
+  int32_t seq, page0;                  // its pages: those of the table's row from page0 on
+  int32_t len;                         // tokens
+  int32_t first_seen, each;            // row i of the part sees its tokens up to first_seen + each * i
+  int32_t group;                       // own parts: the common one of their rows, or -1
+};
+static_assert(sizeof(Part) == 32, "eight words");
+
+struct SharedArgs {
+  CacheView c;
+  SeqView s;
+  const int32_t* groups;
+  const int32_t* shared_len;
+  int32_t n_groups;
+  const __bf16* q;
+  int64_t q_row;
+  int32_t hq, group;
+  float scale;
+  __bf16* o;
+  float* lse;
+  Part* parts[2];                      // [n_groups], [n_seqs]
+  int32_t* before[2];                  // places of the parts before; one more entry: of all
+  int32_t rows[2], blocks[2];          // rows of a block, blocks that may share a line
+  float* slots[2];                     // two per block: pieces of divided items
+  float* whole[2];                     // items in one piece: [tq * hq][D + 2], sums, maximum, sum of exponentials
+  __device__ int32_t count(int kind) const { return kind == kCommon ? n_groups : s.n_seqs; }
+};
+
+__device__ inline int32_t places_of_part(const SharedArgs& a, const Part& p, int rows) {
+  return p.rows == 0 ? 0 : a.c.hkv * ((p.rows * a.group - 1) / rows + 1) * places_of<kItemLead>(p.len);
+}
+
+constexpr int kPartThreads = 1024;
+
+__global__ __launch_bounds__(kPartThreads) void parts_kernel(SharedArgs a) {
+  __shared__ int32_t sums[kPartThreads / 64], bad;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (threadIdx.x == 0) bad = 0;
+  __syncthreads();
+  bool falls = false;
+  for (int s = threadIdx.x; s < a.s.n_seqs; s += kPartThreads) {
+    falls |= a.s.cu[s + 1] < a.s.cu[s];
+    const SeqSizes z = seq_sizes(a.s, s, a.c.page);
+    a.parts[kOwn][s] = {z.row0, z.n, s, 0, z.len, z.len - z.n, 1, -1};
+  }
+  for (int g = threadIdx.x; g < a.n_groups; g += kPartThreads) falls |= a.groups[g] < 0 || a.groups[g + 1] < a.groups[g] || a.groups[g + 1] > a.s.n_seqs;
+  if (falls) bad = 1;
+  __syncthreads();
+  if (!bad)
+    for (int g = wave; g < a.n_groups; g += kPartThreads / 64) {
+      const int lo = a.groups[g], hi = a.groups[g + 1];
+      // what every row of the group sees; sequences without rows do not count
+      int least = INT32_MAX, first = INT32_MAX, rows = 0, seqs = 0, row0 = INT32_MAX;
+      for (int s = lo + lane; s < hi; s += 64) {
+        const SeqSizes z = seq_sizes(a.s, s, a.c.page);
+        if (z.n > 0) {
+          least = min(least, z.len - z.n);
+          first = min(first, s);
+          row0 = min(row0, z.row0);
+          rows += z.n;
+          ++seqs;
+        }
+      }
+#pragma unroll
+      for (int d = 32; d > 0; d >>= 1) {
+        least = min(least, __shfl_xor(least, d));
+        first = min(first, __shfl_xor(first, d));
+        row0 = min(row0, __shfl_xor(row0, d));
+        rows += __shfl_xor(rows, d);
+        seqs += __shfl_xor(seqs, d);
+      }
+      const int shared = seqs < 2 ? 0 : max(min(least, a.shared_len[g]), 0) & ~(a.c.page - 1);
+      if (lane == 0) a.parts[kCommon][g] = {row0, shared ? rows : 0, first, 0, shared, shared - 1, 0, -1};
+      if (shared)
+        for (int s = lo + lane; s < hi; s += 64) {
+          Part& p = a.parts[kOwn][s];
+          p.page0 = shared >> a.c.log_page;
+          p.len -= shared;
+          p.first_seen -= shared;
+          p.group = g;
+        }
+    }
+  __syncthreads();
+  for (int kind = 0; kind < 2; ++kind) {
+    const int n = a.count(kind);
+    int32_t total = 0;
+    for (int i0 = 0; i0 < n; i0 += kPartThreads) {
+      const int i = i0 + threadIdx.x;
+      const int32_t mine = i < n && !bad ? places_of_part(a, a.parts[kind][i], a.rows[kind]) : 0, upto = wave_prefix_sum(mine);
+      if (lane == 63) sums[wave] = upto;
+      __syncthreads();
+      int32_t at = total + upto - mine;
+      for (int w = 0; w < kPartThreads / 64; ++w) {
+        at += w < wave ? sums[w] : 0;
+        total += sums[w];
+      }
+      if (i < n) a.before[kind][i] = at;
+      __syncthreads();
+    }
+    if (threadIdx.x == 0) a.before[kind][n] = total;
+  }
+}
+
+// The last of v[0 .. n - 1], which do not fall, that is at most x (v[0] is); a wave looks at 64 at a time.
+template <class At>
+__device__ inline int last_up_to(int n, int x, At at) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0;
+  while (n > 1) {
+    const int step = (n + 63) / 64, i = lo + lane * step;
+    const bool below = i < lo + n && at(i) <= x;
+    const int k = max((int)__popcll(__ballot(below)) - 1, 0), next = lo + k * step;
+    n = min(step, lo + n - next);
+    lo = next;
+  }
+  return __builtin_amdgcn_readfirstlane(lo);
+}
+
+// A block's share of a line, item by item.
+struct Work {
+  Line line;
+  int32_t me, at, end, base;
+  int kind, index;
+  Part part;
+  // the piece at hand
+  int head, row_block, t0, t1, tiles, all_rows;
+  bool whole;
+  __device__ Work(const SharedArgs& a, int kind) : me(blockIdx.x), kind(kind) {
+    line = {};
+    line.total = __builtin_amdgcn_readfirstlane(a.before[kind][a.count(kind)]);
+    line.sharers = min(a.blocks[kind], (line.total + kLeastTiles - 1) / kLeastTiles);
+    at = end = 0;
+    if (me >= line.sharers) return;
+    at = line.begin(me);
+    end = line.begin(me + 1);
+    index = last_up_to(a.count(kind), at, [&](int i) { return a.before[kind][i]; });
+    take(a);
+  }
+  __device__ void take(const SharedArgs& a) {
+    const int32_t* const w = reinterpret_cast<const int32_t*>(a.parts[kind] + index);
+    auto uniform = [](int32_t x) { return __builtin_amdgcn_readfirstlane(x); };          // (scalar registers)
+    part = {uniform(w[0]), uniform(w[1]), uniform(w[2]), uniform(w[3]), uniform(w[4]), uniform(w[5]), uniform(w[6]), -1};
+    base = uniform(a.before[kind][index]);
+  }
+  __device__ bool next(const SharedArgs& a) {
+    while (at < end) {
+      const int rows = a.rows[kind];
+      while (at >= base + places_of_part(a, part, rows)) {
+        ++index;
+        take(a);
+      }
+      tiles = tiles_of(part.len);
+      all_rows = part.rows * a.group;
+      const int row_blocks = (all_rows + rows - 1) / rows, places = places_of<kItemLead>(part.len), item = (at - base) / places, from = (at - base) % places;
+      const Piece piece = piece_of<kItemLead>(tiles, from, end - at);
+      head = item / row_blocks;
+      row_block = item % row_blocks;
+      t0 = piece.first;
+      t1 = piece.last;
+      whole = t0 == 0 && t1 == tiles;
+      at += piece.places;
+      if (t0 < t1) return true;                            // (else the item's lead alone)
+    }
+    return false;
+  }
+  __device__ const int32_t* table(const SharedArgs& a) const { return a.s.pages + (int64_t)part.seq * a.s.max_pages + part.page0; }
+  __device__ float* slot(const SharedArgs& a, int floats) const { return a.slots[kind] + (int64_t)(2 * me + (t0 == 0 ? 1 : 0)) * floats; }
+  // last token that row `row` of the part (token and query head of the group) sees
+  __device__ int sees(int tok) const { return part.first_seen + part.each * tok; }
+  __device__ int64_t whole_row(const SharedArgs& a, int row) const { return (int64_t)(part.row0 + row / a.group) * a.hq + head * a.group + row % a.group; }
+};
+
+template <int D, int Fmt, int NB>
+__global__ __launch_bounds__(256, 2) void shared_few_kernel(SharedArgs a, int kind) {
+  constexpr int kRows = 16 * NB, kStride = D + 4;          // floats of a staged row: rows on different banks
+  __shared__ __align__(16) float stage[kWaves * kRows * kStride];
+  __shared__ float stage_m[kWaves * kRows], stage_l[kWaves * kRows];
+  __shared__ int32_t first_nan[kWaves][Fmt == kE4m3 ? D : 1];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
+  Work w(a, kind);
+  while (w.next(a)) {
+    int last[NB], first_seen = INT32_MAX;
+    bf16x8 q[NB][D / 32];
+    RowState<D> r[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const int my_row = w.row_block * kRows + 16 * b + n;
+      const bool live = my_row < w.all_rows;
+      const int my_tok = live ? my_row / a.group : 0;
+      last[b] = live ? w.sees(my_tok) : -1;
+      first_seen = min(first_seen, live ? last[b] : INT32_MAX);
+      const __bf16* x = a.q + (int64_t)(w.part.row0 + my_tok) * a.q_row + (w.head * a.group + (live ? my_row % a.group : 0)) * D + 16 * g;
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j) {
+        const bf16x8 y = *reinterpret_cast<const bf16x8*>(x + 64 * (j / 2) + 8 * (j % 2)), zero = {};
+        q[b][j] = live ? y : zero;
+      }
+      r[b].m = kLow;
+      r[b].l = 0.f;
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) r[b].o[i] = f32x4{0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int d = 8; d > 0; d >>= 1) first_seen = min(first_seen, __shfl_xor(first_seen, d));
+    const int rows = min(w.all_rows - w.row_block * kRows, kRows), seen = w.sees((w.row_block * kRows + rows - 1) / a.group);
+    const int t_end = min(w.t1, seen < 0 ? 0 : seen / kTile + 1);
+    walk<D, Fmt, false>(a.c, a.scale, w.table(a), w.head, w.part.len, w.t0 + wave, t_end, kWaves, q, last, first_seen, r, nullptr, rows, nullptr, first_nan[wave]);
+    float* const slot = w.slot(a, slot_floats(D, kRows));
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const int lr = 16 * b + n;
+      r[b].l = sum_over_groups(r[b].l);
+      if (g == 0) { stage_m[wave * kRows + lr] = r[b].m; stage_l[wave * kRows + lr] = r[b].l; }
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4*>(&stage[(wave * kRows + lr) * kStride + 16 * i + 4 * g]) = r[b].o[i];
+    }
+    __syncthreads();
+    for (int j = threadIdx.x; j < rows * (D / 4); j += 256) {
+      const int lr = j / (D / 4), ch = 4 * (j % (D / 4));
+      float m = kLow, l = 0.f;
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i) m = fmaxf(m, stage_m[i * kRows + lr]);
+      f32x4 o = {0, 0, 0, 0};
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i) {
+        const float f = __builtin_amdgcn_exp2f(stage_m[i * kRows + lr] - m);
+        l += f * stage_l[i * kRows + lr];
+        o += f * *reinterpret_cast<const f32x4*>(&stage[(i * kRows + lr) * kStride + ch]);
+      }
+      if (w.whole) {
+        float* const to = a.whole[kind] + w.whole_row(a, w.row_block * kRows + lr) * (D + 4);
+        *reinterpret_cast<f32x4*>(to + ch) = o;
+        if (ch == 0) { to[D] = m; to[D + 1] = l; }
+      } else {
+        *reinterpret_cast<f32x4*>(slot + lr * D + ch) = o;
+        if (ch == 0) { slot[kRows * D + lr] = m; slot[kRows * (D + 1) + lr] = l; }
+      }
+    }
+    __syncthreads();
+  }
+}
+
+template <int D, int Fmt, int kNB>
+__global__ __launch_bounds__(256, 2) void shared_many_kernel(SharedArgs a, int kind) {
+  constexpr int kRows = 64 * kNB;
+  extern __shared__ __align__(256) unsigned char lds[];    // two stages
+  __shared__ float key_scale[4][4];
+  __shared__ int32_t live[4][4], first_nan[2][D];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
+  const RowsLane at_lane = rows_lane<D>(lane, wave);
+  if (Fmt == kE4m3 && threadIdx.x < D) first_nan[1][threadIdx.x] = INT32_MAX;
+  int parity = 1;                                          // of the items that see a tile
+  Work w(a, kind);
+  while (w.next(a)) {
+    bf16x8 q[kNB][D / 32];
+    f32x4 o[kNB][D / 16];
+    float m[kNB], l[kNB];
+    int last[kNB];
+#pragma unroll
+    for (int b = 0; b < kNB; ++b) {
+      const int row = w.row_block * kRows + (wave * kNB + b) * 16 + n;
+      const bool there = row < w.all_rows;
+      const int tok = there ? row / a.group : 0;
+      last[b] = there ? w.sees(tok) : -1;
+      const __bf16* x = a.q + (int64_t)(w.part.row0 + tok) * a.q_row + (w.head * a.group + (there ? row % a.group : 0)) * D + 8 * g;
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j) {
+        const bf16x8 y = *reinterpret_cast<const bf16x8*>(x + 32 * j), zero = {};
+        q[b][j] = there ? y : zero;
+      }
+      m[b] = kLow;
+      l[b] = 0.f;
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) o[b][i] = f32x4{0, 0, 0, 0};
+    }
+    const int rows = min(w.all_rows - w.row_block * kRows, kRows), all_see = w.sees(w.row_block * kRows / a.group), seen = w.sees((w.row_block * kRows + rows - 1) / a.group);
+    const int t_end = min(w.t1, seen < 0 ? 0 : seen / kTile + 1);
+    if (w.t0 < t_end) {
+      walk_rows<D, Fmt, kNB>(a.c, a.scale, w.table(a), w.head, w.part.len, w.t0, t_end, q, last, all_see, o, m, l, lane, wave, at_lane, lds, key_scale, live, first_nan, parity);
+      parity ^= 1;
+    }
+#pragma unroll
+    for (int b = 0; b < kNB; ++b) l[b] = sum_over_groups(l[b]);
+    float* const slot = w.slot(a, slot_floats(D, kRows));
+#pragma unroll
+    for (int b = 0; b < kNB; ++b) {
+      const int lr = (wave * kNB + b) * 16 + n, row = w.row_block * kRows + lr;
+      if (!w.whole) {                                      // sums as they lie in the registers
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4*>(slot + (((wave * kNB + b) * (D / 16) + i) * 64 + lane) * 4) = o[b][i];
+        if (g == 0) { slot[kRows * D + lr] = m[b]; slot[kRows * (D + 1) + lr] = l[b]; }
+      } else if (row < w.all_rows) {
+        float* const to = a.whole[kind] + w.whole_row(a, row) * (D + 4);
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4*>(to + 16 * i + 4 * g) = o[b][i];
+        if (g == 0) { to[D] = m[b]; to[D + 1] = l[b]; }
+      }
+    }
+  }
+}
+
+template <int D>
+struct RowSum { float m, l, o[D / 64]; };
+
+// Joins the pieces of one item of row `row` of a part.
+template <int D>
+__device__ inline void join_item(const SharedArgs& a, int kind, int index, int row_tok, int h, RowSum<D>& r) {
+  constexpr int kCh = D / 64;
+  const Part p = a.parts[kind][index];
+  const int rows = a.rows[kind], row = (row_tok - p.row0) * a.group + h % a.group, head = h / a.group, all_rows = p.rows * a.group;
+  Line line = {};
+  line.total = a.before[kind][a.count(kind)];
+  line.sharers = min(a.blocks[kind], (line.total + kLeastTiles - 1) / kLeastTiles);
+  const int tiles = tiles_of(p.len), row_blocks = (all_rows + rows - 1) / rows, lr = row % rows;
+  const int32_t tile0 = a.before[kind][index] + (head * row_blocks + row / rows) * places_of<kItemLead>(p.len) + kItemLead;
+  const int first = line.owner(tile0), pieces = line.owner(tile0 + tiles - 1) - first + 1, ch = kCh * (threadIdx.x & 63);
+  const int floats = slot_floats(D, rows);
+  // channel ch of the row in a slot: rows of D channels, or, from many rows, as the sums lie in that kernel's registers
+  const int at = rows < 64 ? lr * D + ch : (((lr / 16) * (D / 16) + ch / 16) * 64 + ch % 16 / 4 * 16 + lr % 16) * 4 + ch % 4;
+  const float* const whole = a.whole[kind] + ((int64_t)row_tok * a.hq + h) * (D + 4);
+  constexpr int N = 4;
+  for (int p0 = 0; p0 < pieces; p0 += N) {
+    float pm[N], pl[N], po[N][kCh];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int piece = min(p0 + i, pieces - 1);
+      const float* const s = a.slots[kind] + (int64_t)(2 * (first + piece) + (piece == 0 ? 1 : 0)) * floats;
+      const float* const m = pieces == 1 ? whole + D : s + rows * D + lr;
+      pm[i] = *m;
+      pl[i] = pieces == 1 ? whole[D + 1] : m[rows];
+#pragma unroll
+      for (int c = 0; c < kCh; ++c) po[i][c] = pieces == 1 ? whole[ch + c] : s[at + c];
+    }
+    float top = r.m;
+#pragma unroll
+    for (int i = 0; i < N; ++i) top = fmaxf(top, pm[i]);   // (the last one again where there are no more)
+    const float f0 = __builtin_amdgcn_exp2f(r.m - top);
+    r.m = top;
+    r.l *= f0;
+#pragma unroll
+    for (int c = 0; c < kCh; ++c) r.o[c] *= f0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const bool there = p0 + i < pieces;
+      const float f = __builtin_amdgcn_exp2f(pm[i] - top);
+      r.l += there ? f * pl[i] : 0.f;
+#pragma unroll
+      for (int c = 0; c < kCh; ++c) r.o[c] += there ? f * po[i][c] : 0.f;
+    }
+  }
+}
+
+template <int D>
+__global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs a) {
+  constexpr int kCh = D / 64;
+  const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (unit >= (int64_t)a.s.n_rows * a.hq || a.before[kOwn][a.s.n_seqs] == 0) return;
+  const int tok = __builtin_amdgcn_readfirstlane((int)(unit / a.hq)), h = __builtin_amdgcn_readfirstlane((int)(unit % a.hq)), lane = threadIdx.x & 63;
+  if (a.s.cu[0] > tok || a.s.cu[a.s.n_seqs] <= tok) return;
+  const int seq = last_up_to(a.s.n_seqs, tok, [&](int i) { return a.s.cu[i]; });
+  const int group = a.parts[kOwn][seq].group;
+  RowSum<D> r = {kLow, 0.f, {}};
+  if (group >= 0) join_item<D>(a, kCommon, group, tok, h, r);
+  join_item<D>(a, kOwn, seq, tok, h, r);
+  const float inv = r.l == 0.f ? 0.f : 1.f / r.l;
+  __bf16* const to = a.o + ((int64_t)tok * a.hq + h) * D + kCh * lane;
+#pragma unroll
+  for (int c = 0; c < kCh; ++c) to[c] = (__bf16)(r.o[c] * inv);
+  if (lane == 0) a.lse[(int64_t)h * a.s.n_rows + tok] = r.l == 0.f ? -INFINITY : (r.m + __builtin_amdgcn_logf(r.l)) * kLn2;
+}
+
+// ---- host ---------------------------------------------------------------------------------------
+
+// Rows of a block, from the rows of a group or a sequence on average (as in fcp_cache_attn).
+int rows_form(int64_t all_rows, int64_t n) { return all_rows <= 16 * n ? 16 : all_rows <= 32 * n ? 32 : all_rows <= 64 * n ? 64 : 128; }
+
+struct SharedPlan { int rows[2]; int32_t blocks[2]; int64_t places[2]; };
+SharedPlan plan_shared(const CacheView& c, int32_t n_seqs, int32_t n_groups, int32_t max_pages, int32_t tq, int32_t hq) {
+  SharedPlan p;
+  const int64_t tiles = max(((int64_t)max_pages * c.page + kTile - 1) / kTile, (int64_t)1), all_rows = (int64_t)tq * (hq / c.hkv);
+  const int32_t n[2] = {n_groups, n_seqs};
+  for (int kind = 0; kind < 2; ++kind) {
+    p.rows[kind] = rows_form(all_rows, n[kind] > 0 ? n[kind] : 1);
+    p.places[kind] = (tiles + kItemLead) * c.hkv * (n[kind] + all_rows / p.rows[kind]);
+    p.blocks[kind] = (int32_t)min((p.places[kind] + kLeastTiles - 1) / kLeastTiles, (int64_t)kBlocks);
+  }
+  return p;
+}
+// Scratch: for any number of groups up to n_seqs.  The slots of common parts have room for the rows of one group.
+struct SharedSpace { size_t parts[2], before[2], slots[2], whole[2], bytes; };
+SharedSpace shared_space(const CacheView& c, int head_dim, int32_t n_seqs, int32_t max_pages, int32_t tq, int32_t hq) {
+  SharedSpace s;
+  const SharedPlan p = plan_shared(c, n_seqs, 1, max_pages, tq, hq);
+  size_t at = 0;
+  auto take = [&](size_t bytes) { const size_t here = at; at += pad_to(bytes, 256); return here; };
+  for (int kind = 0; kind < 2; ++kind) {
+    s.parts[kind] = take((size_t)n_seqs * sizeof(Part));
+    s.before[kind] = take(((size_t)n_seqs + 1) * 4);
+    s.slots[kind] = take((size_t)2 * kBlocks * slot_floats(head_dim, p.rows[kind]) * 4);
+    s.whole[kind] = take((size_t)tq * hq * (head_dim + 4) * 4);
+  }
+  s.bytes = at;
+  return s;
+}
+
+template <int D, int Fmt>
+int launch_line(const SharedArgs& a, int kind, hipStream_t st) {
+  const dim3 grid((unsigned)a.blocks[kind]), block(256);
+  if (a.rows[kind] <= 32) {
+    (a.rows[kind] == 16 ? shared_few_kernel<D, Fmt, 1> : shared_few_kernel<D, Fmt, 2>)<<<grid, block, 0, st>>>(a, kind);
+  } else {
+    constexpr int kLds = 2 * Stage<D>::kBytes;
+    static std::atomic<uint64_t> raised[2];
+    const bool half = a.rows[kind] == 64;
+    auto kernel = half ? shared_many_kernel<D, Fmt, 1> : shared_many_kernel<D, Fmt, 2>;
+    if (kLds > 64 * 1024 - 2048)
+      if (int rc = raise_lds_limit(reinterpret_cast<const void*>(kernel), kLds, raised[half])) return rc;
+    kernel<<<grid, block, kLds, st>>>(a, kind);
+  }
+  FCP_HIP_CHECK(hipGetLastError());
+  return FCP_OK;
+}
+
+template <int D, int Fmt>
+int launch_shared(const SharedArgs& a, hipStream_t st) {
+  parts_kernel<<<dim3(1), dim3(kPartThreads), 0, st>>>(a);
+  FCP_HIP_CHECK(hipGetLastError());
+  if (a.n_groups > 0)
+    if (int rc = launch_line<D, Fmt>(a, kCommon, st)) return rc;
+  if (int rc = launch_line<D, Fmt>(a, kOwn, st)) return rc;
+  shared_join_kernel<D><<<dim3((unsigned)(((int64_t)a.s.n_rows * a.hq + 3) / 4)), dim3(256), 0, st>>>(a);
+  FCP_HIP_CHECK(hipGetLastError());
+  return FCP_OK;
+}
+
+int check_shared(const char* who, const CacheView& c, int32_t n_seqs, int32_t max_pages, int32_t tq, int32_t hq) {
+  if (int rc = check_heads(who, c, hq)) return rc;
+  if (int rc = check_row_count(who, tq, hq)) return rc;
+  // (most places: with as many groups as sequences, rows in blocks of 16)
+  const int64_t tiles = max(((int64_t)max_pages * c.page + kTile - 1) / kTile, (int64_t)1);
+  if ((tiles + kItemLead) * c.hkv * (n_seqs + (int64_t)tq * (hq / c.hkv) / 16) > kMostPlaces || !fits_axis(((int64_t)tq * hq + 3) / 4, 256))
+    return fail(FCP_ERR_UNSUPPORTED, "%s: tables and rows that may make 2^31 tiles of work", who);
+  return FCP_OK;
+}
+
+}  // namespace
+
+// 0: refused
+size_t shared_scratch_bytes(const char* who, const CacheView& c, int head_dim, int32_t n_seqs, int32_t max_pages, int32_t tq, int32_t hq) {
+  if (check_shared(who, c, n_seqs, max_pages, tq, hq)) return 0;
+  return shared_space(c, head_dim, n_seqs, max_pages, tq, hq).bytes;
+}
+
+}  // namespace fcp
+
+extern "C" int fcp_cache_attn_shared(const fcp_cache* cache, const void* q, int64_t q_row, int32_t tq, int32_t hq, const int32_t* cu_seqlens, const int32_t* kv_len,
+                                     const int32_t* pages, int32_t n_seqs, int32_t max_pages, const int32_t* groups, const int32_t* shared_len, int32_t n_groups,
+                                     float softmax_scale, void* o, float* lse, void* scratch, size_t scratch_bytes, void* stream) {
+  using namespace fcp;
+  clear_error();
+  const char* who = "fcp_cache_attn_shared";
+  SharedArgs a = {};
+  if (int rc = check_cache(who, cache, false, &a.c)) return rc;
+  if (int rc = check_heads(who, a.c, hq)) return rc;
+  if (int rc = check_seqs(who, a.c, cu_seqlens, true, kv_len, pages, n_seqs, max_pages, tq)) return rc;
+  if (int rc = check_scale(who, softmax_scale)) return rc;
+  if (n_groups < 0 || n_groups > n_seqs || (n_groups > 0 && (!groups || !shared_len)))
+    return fail(FCP_ERR_INVALID_ARG, "%s: %d groups of %d sequences need their first sequences and lengths", who, n_groups, n_seqs);
+  if (tq == 0 || n_seqs == 0) return FCP_OK;
+  if (int rc = check_rows(who, cache, q, q_row, tq, hq)) return rc;
+  if (!o || !lse || (uintptr_t)o % 16 || (uintptr_t)lse % 4) return fail(FCP_ERR_INVALID_ARG, "%s: o and lse are required and must be aligned", who);
+  if (!scratch || (uintptr_t)scratch % 256) return fail(FCP_ERR_INVALID_ARG, "%s: scratch must be 256-byte aligned", who);
+  if (int rc = check_shared(who, a.c, n_seqs, max_pages, tq, hq)) return rc;
+  const SharedSpace space = shared_space(a.c, cache->head_dim, n_seqs, max_pages, tq, hq);
+  if (scratch_bytes < space.bytes) return fail(FCP_ERR_CAPACITY, "%s: scratch has %zu bytes, %zu are needed", who, scratch_bytes, space.bytes);
+  const SharedPlan p = plan_shared(a.c, n_seqs, n_groups, max_pages, tq, hq);
+  a.s = {cu_seqlens, kv_len, pages, n_seqs, max_pages, tq};
+  a.groups = groups;
+  a.shared_len = shared_len;
+  a.n_groups = n_groups;
+  a.q = static_cast<const __bf16*>(q);
+  a.q_row = q_row;
+  a.hq = hq;
+  a.group = hq / a.c.hkv;
+  a.scale = softmax_scale * kLog2e;
+  a.o = static_cast<__bf16*>(o);
+  a.lse = lse;
+  char* const at = static_cast<char*>(scratch);
+  for (int kind = 0; kind < 2; ++kind) {
+    a.parts[kind] = reinterpret_cast<Part*>(at + space.parts[kind]);
+    a.before[kind] = reinterpret_cast<int32_t*>(at + space.before[kind]);
+    a.slots[kind] = reinterpret_cast<float*>(at + space.slots[kind]);
+    a.whole[kind] = reinterpret_cast<float*>(at + space.whole[kind]);
+    a.rows[kind] = p.rows[kind];
+    a.blocks[kind] = p.blocks[kind];
+  }
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const bool e4m3 = cache->format == FCP_CACHE_E4M3;
+  return cache->head_dim == 128 ? (e4m3 ? launch_shared<128, kE4m3>(a, st) : launch_shared<128, kInt8>(a, st))
+                                : (e4m3 ? launch_shared<64, kE4m3>(a, st) : launch_shared<64, kInt8>(a, st));
+}
