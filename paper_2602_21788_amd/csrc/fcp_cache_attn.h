@@ -135,6 +135,7 @@ constexpr int64_t kMostPlaces = INT32_MAX - 2 * kBlocks;
 
 constexpr int kManyRows = 128;         // rows of a block in the kernel for many, or half of them
 
+size_t attn_scratch_bytes(const CacheView& c, int head_dim, int32_t n_seqs, int32_t max_pages, int32_t tq, int32_t hq);       // of fcp_cache_attn without weigh
 int launch_attn_rows(const AttnArgs& a, int head_dim, int format, int rows, bool whole, hipStream_t st);
 
 __device__ inline float max_over_groups(float x) {

@@ -533,6 +533,10 @@ size_t evict_scratch_bytes(const char* who, const CacheView& c, int32_t n_seqs, 
 size_t page_scratch_bytes(const char* who, const CacheView& c, bool fork, int32_t n_seqs, int32_t max_pages);
 size_t shared_scratch_bytes(const char* who, const CacheView& c, int head_dim, int32_t n_seqs, int32_t max_pages, int32_t tq, int32_t hq);
 
+size_t attn_scratch_bytes(const CacheView& c, int head_dim, int32_t n_seqs, int32_t max_pages, int32_t tq, int32_t hq) {
+  return attn_bytes(plan_attn(c, head_dim, n_seqs, max_pages, tq, hq, false));
+}
+
 }  // namespace fcp
 
 extern "C" size_t fcp_cache_scratch_bytes(int which, const fcp_cache* cache, int32_t n_seqs, int32_t max_pages, int32_t tq, int32_t hq) {

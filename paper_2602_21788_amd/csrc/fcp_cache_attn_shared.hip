@@ -303,9 +303,9 @@ __global__ __launch_bounds__(256, 2) void shared_many_kernel(SharedArgs a, int k
 #pragma unroll
     for (int b = 0; b < kNB; ++b) {
       const int lr = (wave * kNB + b) * 16 + n, row = w.row_block * kRows + lr;
-      if (!w.whole) {                                      // sums as they lie in the registers
+      if (!w.whole) {
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4*>(slot + (((wave * kNB + b) * (D / 16) + i) * 64 + lane) * 4) = o[b][i];
+        for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4*>(slot + lr * D + 16 * i + 4 * g) = o[b][i];
         if (g == 0) { slot[kRows * D + lr] = m[b]; slot[kRows * (D + 1) + lr] = l[b]; }
       } else if (row < w.all_rows) {
         float* const to = a.whole[kind] + w.whole_row(a, row) * (D + 4);
@@ -333,8 +333,7 @@ __device__ inline void join_item(const SharedArgs& a, int kind, int index, int r
   const int32_t tile0 = a.before[kind][index] + (head * row_blocks + row / rows) * places_of<kItemLead>(p.len) + kItemLead;
   const int first = line.owner(tile0), pieces = line.owner(tile0 + tiles - 1) - first + 1, ch = kCh * (threadIdx.x & 63);
   const int floats = slot_floats(D, rows);
-  // channel ch of the row in a slot: rows of D channels, or, from many rows, as the sums lie in that kernel's registers
-  const int at = rows < 64 ? lr * D + ch : (((lr / 16) * (D / 16) + ch / 16) * 64 + ch % 16 / 4 * 16 + lr % 16) * 4 + ch % 4;
+  const int at = lr * D + ch;
   const float* const whole = a.whole[kind] + ((int64_t)row_tok * a.hq + h) * (D + 4);
   constexpr int N = 4;
   for (int p0 = 0; p0 < pieces; p0 += N) {
@@ -406,6 +405,8 @@ SharedPlan plan_shared(const CacheView& c, int32_t n_seqs, int32_t n_groups, int
 }
 // Scratch: for any number of groups up to n_seqs.  The slots of common parts have room for the rows of one group.
 struct SharedSpace { size_t parts[2], before[2], slots[2], whole[2], bytes; };
+// Many rows of a sequence are attention of many rows already: the matrix units bound it, and the bytes that sequences share are read from the L2s.  Every sequence is worked by itself then.
+bool by_itself(const CacheView& c, int32_t n_seqs, int32_t tq, int32_t hq) { return (int64_t)tq * (hq / c.hkv) > (int64_t)64 * n_seqs; }
 SharedSpace shared_space(const CacheView& c, int head_dim, int32_t n_seqs, int32_t max_pages, int32_t tq, int32_t hq) {
   SharedSpace s;
   const SharedPlan p = plan_shared(c, n_seqs, 1, max_pages, tq, hq);
@@ -466,6 +467,7 @@ int check_shared(const char* who, const CacheView& c, int32_t n_seqs, int32_t ma
 // 0: refused
 size_t shared_scratch_bytes(const char* who, const CacheView& c, int head_dim, int32_t n_seqs, int32_t max_pages, int32_t tq, int32_t hq) {
   if (check_shared(who, c, n_seqs, max_pages, tq, hq)) return 0;
+  if (by_itself(c, n_seqs, tq, hq)) return attn_scratch_bytes(c, head_dim, n_seqs, max_pages, tq, hq);
   return shared_space(c, head_dim, n_seqs, max_pages, tq, hq).bytes;
 }
 
@@ -489,6 +491,11 @@ extern "C" int fcp_cache_attn_shared(const fcp_cache* cache, const void* q, int6
   if (!o || !lse || (uintptr_t)o % 16 || (uintptr_t)lse % 4) return fail(FCP_ERR_INVALID_ARG, "%s: o and lse are required and must be aligned", who);
   if (!scratch || (uintptr_t)scratch % 256) return fail(FCP_ERR_INVALID_ARG, "%s: scratch must be 256-byte aligned", who);
   if (int rc = check_shared(who, a.c, n_seqs, max_pages, tq, hq)) return rc;
+  if (by_itself(a.c, n_seqs, tq, hq)) {
+    const size_t need = attn_scratch_bytes(a.c, cache->head_dim, n_seqs, max_pages, tq, hq);
+    if (scratch_bytes < need) return fail(FCP_ERR_CAPACITY, "%s: scratch has %zu bytes, %zu are needed", who, scratch_bytes, need);
+    return fcp_cache_attn(cache, q, q_row, tq, hq, cu_seqlens, kv_len, pages, n_seqs, max_pages, softmax_scale, 0, o, lse, scratch, scratch_bytes, stream);
+  }
   const SharedSpace space = shared_space(a.c, cache->head_dim, n_seqs, max_pages, tq, hq);
   if (scratch_bytes < space.bytes) return fail(FCP_ERR_CAPACITY, "%s: scratch has %zu bytes, %zu are needed", who, scratch_bytes, space.bytes);
   const SharedPlan p = plan_shared(a.c, n_seqs, n_groups, max_pages, tq, hq);
