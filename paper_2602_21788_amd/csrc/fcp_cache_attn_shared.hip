@@ -37,23 +37,37 @@ struct SharedArgs {
   __bf16* o;
   float* lse;
   Part* parts[2];                      // [n_groups], [n_seqs]
-  int32_t* before[2];                  // places of the parts before; one more entry: of all
-  int32_t rows[2], blocks[2];          // rows of a block, blocks that may share a line
+  int32_t* before[2];                  // places of the parts before; two more entries: of all, and whether items are one place each (kWhole), or tiles and a lead
+  int32_t rows[2], sharers[2];         // rows of an item; blocks, or waves, that may share a line
   float* slots[2];                     // two per block: pieces of divided items
+  int32_t waves;                       // own parts: a wave works an item, else a block
   float* whole[2];                     // items in one piece: [tq * hq][D + 2], sums, maximum, sum of exponentials
   __device__ int32_t count(int kind) const { return kind == kCommon ? n_groups : s.n_seqs; }
 };
 
-__device__ inline int32_t places_of_part(const SharedArgs& a, const Part& p, int rows) {
-  return p.rows == 0 ? 0 : a.c.hkv * ((p.rows * a.group - 1) / rows + 1) * places_of<kItemLead>(p.len);
+__device__ inline int32_t places_of_item(const Part& p, bool whole) { return whole ? 1 : places_of<kItemLead>(p.len); }
+__device__ inline int32_t places_of_part(const SharedArgs& a, const Part& p, int rows, bool whole) {
+  return p.rows == 0 ? 0 : a.c.hkv * ((p.rows * a.group - 1) / rows + 1) * places_of_item(p, whole);
 }
 
 constexpr int kPartThreads = 1024;
+constexpr int kWholeLen = 16 * kTile;  // own parts up to this long are not divided
+constexpr int kSharers = kWaves * kBlocks;       // waves that share the line of own parts
+
+// How many share a line, and who: a share has a few places at least, where items are one place each one.
+__device__ inline Line line_of(const SharedArgs& a, int kind, bool& whole) {
+  const int32_t* const ends = a.before[kind] + a.count(kind);
+  Line line = {};
+  line.total = __builtin_amdgcn_readfirstlane(ends[0]);
+  whole = __builtin_amdgcn_readfirstlane(ends[1]);
+  line.sharers = min(a.sharers[kind], whole ? line.total : (line.total + kLeastTiles - 1) / kLeastTiles);
+  return line;
+}
 
 __global__ __launch_bounds__(kPartThreads) void parts_kernel(SharedArgs a) {
-  __shared__ int32_t sums[kPartThreads / 64], bad;
+  __shared__ int32_t sums[kPartThreads / 64], bad, longest;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  if (threadIdx.x == 0) bad = 0;
+  if (threadIdx.x == 0) bad = longest = 0;
   __syncthreads();
   bool falls = false;
   for (int s = threadIdx.x; s < a.s.n_seqs; s += kPartThreads) {
@@ -99,12 +113,18 @@ __global__ __launch_bounds__(kPartThreads) void parts_kernel(SharedArgs a) {
         }
     }
   __syncthreads();
+  int32_t most = 0;
+  for (int s = threadIdx.x; s < a.s.n_seqs; s += kPartThreads)
+    if (a.parts[kOwn][s].rows > 0) most = max(most, a.parts[kOwn][s].len);
+  atomicMax(&longest, wave_max(most));
+  __syncthreads();
   for (int kind = 0; kind < 2; ++kind) {
     const int n = a.count(kind);
+    const bool whole = kind == kOwn && a.waves && longest <= kWholeLen;
     int32_t total = 0;
     for (int i0 = 0; i0 < n; i0 += kPartThreads) {
       const int i = i0 + threadIdx.x;
-      const int32_t mine = i < n && !bad ? places_of_part(a, a.parts[kind][i], a.rows[kind]) : 0, upto = wave_prefix_sum(mine);
+      const int32_t mine = i < n && !bad ? places_of_part(a, a.parts[kind][i], a.rows[kind], whole) : 0, upto = wave_prefix_sum(mine);
       if (lane == 63) sums[wave] = upto;
       __syncthreads();
       int32_t at = total + upto - mine;
@@ -115,7 +135,7 @@ __global__ __launch_bounds__(kPartThreads) void parts_kernel(SharedArgs a) {
       if (i < n) a.before[kind][i] = at;
       __syncthreads();
     }
-    if (threadIdx.x == 0) a.before[kind][n] = total;
+    if (threadIdx.x == 0) a.before[kind][n] = total, a.before[kind][n + 1] = whole;
   }
 }
 
@@ -134,19 +154,18 @@ __device__ inline int last_up_to(int n, int x, At at) {
   return __builtin_amdgcn_readfirstlane(lo);
 }
 
-// A block's share of a line, item by item.
+// A block's or a wave's share of a line, item by item.
 struct Work {
   Line line;
   int32_t me, at, end, base;
   int kind, index;
+  bool undivided;                      // all items are in one piece
   Part part;
   // the piece at hand
   int head, row_block, t0, t1, tiles, all_rows;
   bool whole;
-  __device__ Work(const SharedArgs& a, int kind) : me(blockIdx.x), kind(kind) {
-    line = {};
-    line.total = __builtin_amdgcn_readfirstlane(a.before[kind][a.count(kind)]);
-    line.sharers = min(a.blocks[kind], (line.total + kLeastTiles - 1) / kLeastTiles);
+  __device__ Work(const SharedArgs& a, int kind, int me) : me(me), kind(kind) {
+    line = line_of(a, kind, undivided);
     at = end = 0;
     if (me >= line.sharers) return;
     at = line.begin(me);
@@ -163,14 +182,14 @@ struct Work {
   __device__ bool next(const SharedArgs& a) {
     while (at < end) {
       const int rows = a.rows[kind];
-      while (at >= base + places_of_part(a, part, rows)) {
+      while (at >= base + places_of_part(a, part, rows, undivided)) {
         ++index;
         take(a);
       }
       tiles = tiles_of(part.len);
       all_rows = part.rows * a.group;
-      const int row_blocks = (all_rows + rows - 1) / rows, places = places_of<kItemLead>(part.len), item = (at - base) / places, from = (at - base) % places;
-      const Piece piece = piece_of<kItemLead>(tiles, from, end - at);
+      const int row_blocks = (all_rows + rows - 1) / rows, places = places_of_item(part, undivided), item = (at - base) / places, from = (at - base) % places;
+      const Piece piece = undivided ? piece_of<kWhole>(tiles, from, end - at) : piece_of<kItemLead>(tiles, from, end - at);
       head = item / row_blocks;
       row_block = item % row_blocks;
       t0 = piece.first;
@@ -188,41 +207,50 @@ struct Work {
   __device__ int64_t whole_row(const SharedArgs& a, int row) const { return (int64_t)(part.row0 + row / a.group) * a.hq + head * a.group + row % a.group; }
 };
 
+// The rows of the piece at hand over its tiles t0 + first, t0 + first + step, ...
 template <int D, int Fmt, int NB>
-__global__ __launch_bounds__(256, 2) void shared_few_kernel(SharedArgs a, int kind) {
-  constexpr int kRows = 16 * NB, kStride = D + 4;          // floats of a staged row: rows on different banks
-  __shared__ __align__(16) float stage[kWaves * kRows * kStride];
-  __shared__ float stage_m[kWaves * kRows], stage_l[kWaves * kRows];
-  __shared__ int32_t first_nan[kWaves][Fmt == kE4m3 ? D : 1];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
-  Work w(a, kind);
-  while (w.next(a)) {
-    int last[NB], first_seen = INT32_MAX;
-    bf16x8 q[NB][D / 32];
-    RowState<D> r[NB];
+__device__ inline void walk_piece(const SharedArgs& a, const Work& w, int lane, int first, int step, RowState<D> (&r)[NB], int& rows, int32_t* first_nan) {
+  constexpr int kRows = 16 * NB;
+  const int n = lane & 15, g = lane >> 4;
+  int last[NB], first_seen = INT32_MAX;
+  bf16x8 q[NB][D / 32];
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      const int my_row = w.row_block * kRows + 16 * b + n;
-      const bool live = my_row < w.all_rows;
-      const int my_tok = live ? my_row / a.group : 0;
-      last[b] = live ? w.sees(my_tok) : -1;
-      first_seen = min(first_seen, live ? last[b] : INT32_MAX);
-      const __bf16* x = a.q + (int64_t)(w.part.row0 + my_tok) * a.q_row + (w.head * a.group + (live ? my_row % a.group : 0)) * D + 16 * g;
+  for (int b = 0; b < NB; ++b) {
+    const int my_row = w.row_block * kRows + 16 * b + n;
+    const bool live = my_row < w.all_rows;
+    const int my_tok = live ? my_row / a.group : 0;
+    last[b] = live ? w.sees(my_tok) : -1;
+    first_seen = min(first_seen, live ? last[b] : INT32_MAX);
+    const __bf16* x = a.q + (int64_t)(w.part.row0 + my_tok) * a.q_row + (w.head * a.group + (live ? my_row % a.group : 0)) * D + 16 * g;
 #pragma unroll
-      for (int j = 0; j < D / 32; ++j) {
-        const bf16x8 y = *reinterpret_cast<const bf16x8*>(x + 64 * (j / 2) + 8 * (j % 2)), zero = {};
-        q[b][j] = live ? y : zero;
-      }
-      r[b].m = kLow;
-      r[b].l = 0.f;
-#pragma unroll
-      for (int i = 0; i < D / 16; ++i) r[b].o[i] = f32x4{0, 0, 0, 0};
+    for (int j = 0; j < D / 32; ++j) {
+      const bf16x8 y = *reinterpret_cast<const bf16x8*>(x + 64 * (j / 2) + 8 * (j % 2)), zero = {};
+      q[b][j] = live ? y : zero;
     }
+    r[b].m = kLow;
+    r[b].l = 0.f;
 #pragma unroll
-    for (int d = 8; d > 0; d >>= 1) first_seen = min(first_seen, __shfl_xor(first_seen, d));
-    const int rows = min(w.all_rows - w.row_block * kRows, kRows), seen = w.sees((w.row_block * kRows + rows - 1) / a.group);
-    const int t_end = min(w.t1, seen < 0 ? 0 : seen / kTile + 1);
-    walk<D, Fmt, false>(a.c, a.scale, w.table(a), w.head, w.part.len, w.t0 + wave, t_end, kWaves, q, last, first_seen, r, nullptr, rows, nullptr, first_nan[wave]);
+    for (int i = 0; i < D / 16; ++i) r[b].o[i] = f32x4{0, 0, 0, 0};
+  }
+#pragma unroll
+  for (int d = 8; d > 0; d >>= 1) first_seen = min(first_seen, __shfl_xor(first_seen, d));
+  rows = min(w.all_rows - w.row_block * kRows, kRows);
+  const int seen = w.sees((w.row_block * kRows + rows - 1) / a.group);
+  const int t_end = min(w.t1, seen < 0 ? 0 : seen / kTile + 1);
+  walk<D, Fmt, false>(a.c, a.scale, w.table(a), w.head, w.part.len, w.t0 + first, t_end, step, q, last, first_seen, r, nullptr, rows, nullptr, first_nan);
+}
+
+template <int D, int Fmt, int NB>
+__device__ inline void few_rows(const SharedArgs& a, int kind, int lane, int wave, float* stage, int32_t* first_nan) {
+  constexpr int kRows = 16 * NB, kStride = D + 4;          // floats of a staged row: rows on different banks
+  float* const stage_m = stage + kWaves * kRows * kStride;
+  float* const stage_l = stage_m + kWaves * kRows;
+  const int n = lane & 15, g = lane >> 4;
+  Work w(a, kind, blockIdx.x);
+  while (w.next(a)) {
+    RowState<D> r[NB];
+    int rows;
+    walk_piece<D, Fmt, NB>(a, w, lane, wave, kWaves, r, rows, first_nan);
     float* const slot = w.slot(a, slot_floats(D, kRows));
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
@@ -258,17 +286,38 @@ __global__ __launch_bounds__(256, 2) void shared_few_kernel(SharedArgs a, int ki
   }
 }
 
+// Own parts of few rows: a wave works an item, or a piece of one, alone.  They are short as a rule - what was added behind the common beginning - and a block's waves would each have a tile or
+// none, and meet for it.
+template <int D, int Fmt>
+__device__ inline void own_rows(const SharedArgs& a, int lane, int wave, int32_t* first_nan) {
+  const int n = lane & 15, g = lane >> 4;
+  Work w(a, kOwn, kWaves * blockIdx.x + wave);
+  while (w.next(a)) {
+    RowState<D> r[1];
+    int rows;
+    walk_piece<D, Fmt, 1>(a, w, lane, 0, 1, r, rows, first_nan);
+    r[0].l = sum_over_groups(r[0].l);
+    if (n < rows) {
+      float* const to = w.whole ? a.whole[kOwn] + w.whole_row(a, 16 * w.row_block + n) * (D + 4) : w.slot(a, slot_floats(D, 16)) + n * D;
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4*>(to + 16 * i + 4 * g) = r[0].o[i];
+      if (g == 0) {
+        float* const m = w.whole ? to + D : w.slot(a, slot_floats(D, 16)) + 16 * D + n;
+        m[0] = r[0].m;
+        m[w.whole ? 1 : 16] = r[0].l;
+      }
+    }
+  }
+}
+
 template <int D, int Fmt, int kNB>
-__global__ __launch_bounds__(256, 2) void shared_many_kernel(SharedArgs a, int kind) {
+__device__ inline void many_rows(const SharedArgs& a, int kind, int lane, int wave, unsigned char* lds, float (&key_scale)[4][4], int32_t (&live)[4][4], int32_t (&first_nan)[2][D]) {
   constexpr int kRows = 64 * kNB;
-  extern __shared__ __align__(256) unsigned char lds[];    // two stages
-  __shared__ float key_scale[4][4];
-  __shared__ int32_t live[4][4], first_nan[2][D];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
+  const int n = lane & 15, g = lane >> 4;
   const RowsLane at_lane = rows_lane<D>(lane, wave);
   if (Fmt == kE4m3 && threadIdx.x < D) first_nan[1][threadIdx.x] = INT32_MAX;
   int parity = 1;                                          // of the items that see a tile
-  Work w(a, kind);
+  Work w(a, kind, blockIdx.x);
   while (w.next(a)) {
     bf16x8 q[kNB][D / 32];
     f32x4 o[kNB][D / 16];
@@ -317,6 +366,28 @@ __global__ __launch_bounds__(256, 2) void shared_many_kernel(SharedArgs a, int k
   }
 }
 
+// One launch works both lines (Own), or the line `kind`.  kRows: 16, 32, 64, 128 rows of an item.
+template <int D, int Fmt, int kRows, bool Own>
+__global__ __launch_bounds__(256, 2) void shared_kernel(SharedArgs a, int kind) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if constexpr (kRows <= 32) {
+    __shared__ __align__(16) float stage[kWaves * kRows * (D + 6)];
+    __shared__ int32_t first_nan[kWaves][Fmt == kE4m3 ? D : 1];
+    if constexpr (Own) own_rows<D, Fmt>(a, lane, wave, first_nan[wave]);
+    few_rows<D, Fmt, kRows / 16>(a, kind, lane, wave, stage, first_nan[wave]);
+  } else {
+    extern __shared__ __align__(256) unsigned char lds[];  // two stages
+    __shared__ float key_scale[4][4];
+    __shared__ int32_t live[4][4], first_nan[2][D];
+    // (the waves' own notes lie where the stages will)
+    if constexpr (Own) {
+      own_rows<D, Fmt>(a, lane, wave, reinterpret_cast<int32_t*>(lds) + wave * D);
+      __syncthreads();
+    }
+    many_rows<D, Fmt, kRows / 64>(a, kind, lane, wave, lds, key_scale, live, first_nan);
+  }
+}
+
 template <int D>
 struct RowSum { float m, l, o[D / 64]; };
 
@@ -326,12 +397,11 @@ __device__ inline void join_item(const SharedArgs& a, int kind, int index, int r
   constexpr int kCh = D / 64;
   const Part p = a.parts[kind][index];
   const int rows = a.rows[kind], row = (row_tok - p.row0) * a.group + h % a.group, head = h / a.group, all_rows = p.rows * a.group;
-  Line line = {};
-  line.total = a.before[kind][a.count(kind)];
-  line.sharers = min(a.blocks[kind], (line.total + kLeastTiles - 1) / kLeastTiles);
+  bool undivided;
+  const Line line = line_of(a, kind, undivided);
   const int tiles = tiles_of(p.len), row_blocks = (all_rows + rows - 1) / rows, lr = row % rows;
   const int32_t tile0 = a.before[kind][index] + (head * row_blocks + row / rows) * places_of<kItemLead>(p.len) + kItemLead;
-  const int first = line.owner(tile0), pieces = line.owner(tile0 + tiles - 1) - first + 1, ch = kCh * (threadIdx.x & 63);
+  const int first = undivided ? 0 : line.owner(tile0), pieces = undivided ? 1 : line.owner(tile0 + tiles - 1) - first + 1, ch = kCh * (threadIdx.x & 63);
   const int floats = slot_floats(D, rows);
   const int at = lr * D + ch;
   const float* const whole = a.whole[kind] + ((int64_t)row_tok * a.hq + h) * (D + 4);
@@ -391,51 +461,45 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs a) {
 // Rows of a block, from the rows of a group or a sequence on average (as in fcp_cache_attn).
 int rows_form(int64_t all_rows, int64_t n) { return all_rows <= 16 * n ? 16 : all_rows <= 32 * n ? 32 : all_rows <= 64 * n ? 64 : 128; }
 
-struct SharedPlan { int rows[2]; int32_t blocks[2]; int64_t places[2]; };
-SharedPlan plan_shared(const CacheView& c, int32_t n_seqs, int32_t n_groups, int32_t max_pages, int32_t tq, int32_t hq) {
+struct SharedPlan { int rows[2]; int32_t sharers[2]; bool waves; };
+SharedPlan plan_shared(const CacheView& c, int32_t n_seqs, int32_t n_groups, int32_t tq, int32_t hq) {
   SharedPlan p;
-  const int64_t tiles = max(((int64_t)max_pages * c.page + kTile - 1) / kTile, (int64_t)1), all_rows = (int64_t)tq * (hq / c.hkv);
-  const int32_t n[2] = {n_groups, n_seqs};
-  for (int kind = 0; kind < 2; ++kind) {
-    p.rows[kind] = rows_form(all_rows, n[kind] > 0 ? n[kind] : 1);
-    p.places[kind] = (tiles + kItemLead) * c.hkv * (n[kind] + all_rows / p.rows[kind]);
-    p.blocks[kind] = (int32_t)min((p.places[kind] + kLeastTiles - 1) / kLeastTiles, (int64_t)kBlocks);
-  }
+  const int64_t all_rows = (int64_t)tq * (hq / c.hkv);
+  p.rows[kCommon] = rows_form(all_rows, n_groups > 0 ? n_groups : 1);
+  p.rows[kOwn] = rows_form(all_rows, n_seqs);
+  p.waves = p.rows[kOwn] == 16;
+  p.sharers[kCommon] = kBlocks;
+  p.sharers[kOwn] = p.waves ? kSharers : kBlocks;
   return p;
 }
 // Scratch: for any number of groups up to n_seqs.  The slots of common parts have room for the rows of one group.
 struct SharedSpace { size_t parts[2], before[2], slots[2], whole[2], bytes; };
 // Many rows of a sequence are attention of many rows already: the matrix units bound it, and the bytes that sequences share are read from the L2s.  Every sequence is worked by itself then.
 bool by_itself(const CacheView& c, int32_t n_seqs, int32_t tq, int32_t hq) { return (int64_t)tq * (hq / c.hkv) > (int64_t)64 * n_seqs; }
-SharedSpace shared_space(const CacheView& c, int head_dim, int32_t n_seqs, int32_t max_pages, int32_t tq, int32_t hq) {
+SharedSpace shared_space(const CacheView& c, int head_dim, int32_t n_seqs, int32_t tq, int32_t hq) {
   SharedSpace s;
-  const SharedPlan p = plan_shared(c, n_seqs, 1, max_pages, tq, hq);
+  const SharedPlan p = plan_shared(c, n_seqs, 1, tq, hq);
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t here = at; at += pad_to(bytes, 256); return here; };
   for (int kind = 0; kind < 2; ++kind) {
     s.parts[kind] = take((size_t)n_seqs * sizeof(Part));
-    s.before[kind] = take(((size_t)n_seqs + 1) * 4);
-    s.slots[kind] = take((size_t)2 * kBlocks * slot_floats(head_dim, p.rows[kind]) * 4);
+    s.before[kind] = take(((size_t)n_seqs + 2) * 4);
+    s.slots[kind] = take((size_t)2 * p.sharers[kind] * slot_floats(head_dim, p.rows[kind]) * 4);
     s.whole[kind] = take((size_t)tq * hq * (head_dim + 4) * 4);
   }
   s.bytes = at;
   return s;
 }
 
-template <int D, int Fmt>
+template <int D, int Fmt, int kRows, bool Own>
 int launch_line(const SharedArgs& a, int kind, hipStream_t st) {
-  const dim3 grid((unsigned)a.blocks[kind]), block(256);
-  if (a.rows[kind] <= 32) {
-    (a.rows[kind] == 16 ? shared_few_kernel<D, Fmt, 1> : shared_few_kernel<D, Fmt, 2>)<<<grid, block, 0, st>>>(a, kind);
-  } else {
-    constexpr int kLds = 2 * Stage<D>::kBytes;
-    static std::atomic<uint64_t> raised[2];
-    const bool half = a.rows[kind] == 64;
-    auto kernel = half ? shared_many_kernel<D, Fmt, 1> : shared_many_kernel<D, Fmt, 2>;
-    if (kLds > 64 * 1024 - 2048)
-      if (int rc = raise_lds_limit(reinterpret_cast<const void*>(kernel), kLds, raised[half])) return rc;
-    kernel<<<grid, block, kLds, st>>>(a, kind);
+  constexpr int kLds = kRows <= 32 ? 0 : 2 * Stage<D>::kBytes;
+  auto kernel = shared_kernel<D, Fmt, kRows, Own>;
+  if (kLds > 64 * 1024 - 2048) {
+    static std::atomic<uint64_t> raised;
+    if (int rc = raise_lds_limit(reinterpret_cast<const void*>(kernel), kLds, raised)) return rc;
   }
+  kernel<<<dim3((unsigned)kBlocks), dim3(256), kLds, st>>>(a, kind);
   FCP_HIP_CHECK(hipGetLastError());
   return FCP_OK;
 }
@@ -444,9 +508,17 @@ template <int D, int Fmt>
 int launch_shared(const SharedArgs& a, hipStream_t st) {
   parts_kernel<<<dim3(1), dim3(kPartThreads), 0, st>>>(a);
   FCP_HIP_CHECK(hipGetLastError());
-  if (a.n_groups > 0)
-    if (int rc = launch_line<D, Fmt>(a, kCommon, st)) return rc;
-  if (int rc = launch_line<D, Fmt>(a, kOwn, st)) return rc;
+  const int common = a.rows[kCommon];
+  int rc;
+  if (a.waves) {
+    rc = common == 16 ? launch_line<D, Fmt, 16, true>(a, kCommon, st) : common == 32 ? launch_line<D, Fmt, 32, true>(a, kCommon, st)
+       : common == 64 ? launch_line<D, Fmt, 64, true>(a, kCommon, st) : launch_line<D, Fmt, 128, true>(a, kCommon, st);
+  } else {
+    rc = a.n_groups == 0 ? FCP_OK : common == 32 ? launch_line<D, Fmt, 32, false>(a, kCommon, st) : common == 64 ? launch_line<D, Fmt, 64, false>(a, kCommon, st)
+       : launch_line<D, Fmt, 128, false>(a, kCommon, st);
+    if (!rc) rc = a.rows[kOwn] == 32 ? launch_line<D, Fmt, 32, false>(a, kOwn, st) : launch_line<D, Fmt, 64, false>(a, kOwn, st);
+  }
+  if (rc) return rc;
   shared_join_kernel<D><<<dim3((unsigned)(((int64_t)a.s.n_rows * a.hq + 3) / 4)), dim3(256), 0, st>>>(a);
   FCP_HIP_CHECK(hipGetLastError());
   return FCP_OK;
@@ -468,7 +540,7 @@ int check_shared(const char* who, const CacheView& c, int32_t n_seqs, int32_t ma
 size_t shared_scratch_bytes(const char* who, const CacheView& c, int head_dim, int32_t n_seqs, int32_t max_pages, int32_t tq, int32_t hq) {
   if (check_shared(who, c, n_seqs, max_pages, tq, hq)) return 0;
   if (by_itself(c, n_seqs, tq, hq)) return attn_scratch_bytes(c, head_dim, n_seqs, max_pages, tq, hq);
-  return shared_space(c, head_dim, n_seqs, max_pages, tq, hq).bytes;
+  return shared_space(c, head_dim, n_seqs, tq, hq).bytes;
 }
 
 }  // namespace fcp
@@ -496,9 +568,9 @@ extern "C" int fcp_cache_attn_shared(const fcp_cache* cache, const void* q, int6
     if (scratch_bytes < need) return fail(FCP_ERR_CAPACITY, "%s: scratch has %zu bytes, %zu are needed", who, scratch_bytes, need);
     return fcp_cache_attn(cache, q, q_row, tq, hq, cu_seqlens, kv_len, pages, n_seqs, max_pages, softmax_scale, 0, o, lse, scratch, scratch_bytes, stream);
   }
-  const SharedSpace space = shared_space(a.c, cache->head_dim, n_seqs, max_pages, tq, hq);
+  const SharedSpace space = shared_space(a.c, cache->head_dim, n_seqs, tq, hq);
   if (scratch_bytes < space.bytes) return fail(FCP_ERR_CAPACITY, "%s: scratch has %zu bytes, %zu are needed", who, scratch_bytes, space.bytes);
-  const SharedPlan p = plan_shared(a.c, n_seqs, n_groups, max_pages, tq, hq);
+  const SharedPlan p = plan_shared(a.c, n_seqs, n_groups, tq, hq);
   a.s = {cu_seqlens, kv_len, pages, n_seqs, max_pages, tq};
   a.groups = groups;
   a.shared_len = shared_len;
@@ -517,8 +589,9 @@ extern "C" int fcp_cache_attn_shared(const fcp_cache* cache, const void* q, int6
     a.slots[kind] = reinterpret_cast<float*>(at + space.slots[kind]);
     a.whole[kind] = reinterpret_cast<float*>(at + space.whole[kind]);
     a.rows[kind] = p.rows[kind];
-    a.blocks[kind] = p.blocks[kind];
+    a.sharers[kind] = p.sharers[kind];
   }
+  a.waves = p.waves;
   hipStream_t st = static_cast<hipStream_t>(stream);
   const bool e4m3 = cache->format == FCP_CACHE_E4M3;
   return cache->head_dim == 128 ? (e4m3 ? launch_shared<128, kE4m3>(a, st) : launch_shared<128, kInt8>(a, st))
