@@ -14,15 +14,23 @@ namespace {
 
 enum { kCommon = 0, kOwn = 1 };
 
-// A run of cached tokens and the rows that attend over it.
-struct Part {
+// A run of cached tokens and the rows that attend over it, as the tables of parts hold it.
+struct Entry {
   int32_t row0, rows;                  // rows of q, tokens; rows = 0: nothing to do
-  int32_t seq, page0;                  // its pages: those of the table's row from page0 on
-  int32_t len;                         // tokens
-  int32_t first_seen, each;            // row i of the part sees its tokens up to first_seen + each * i
-  int32_t group;                       // own parts: the common one of their rows, or -1
+  int32_t other;                       // common: the sequence whose pages are read; own: the common part of the rows, or -1
+  int32_t len;                         // common: tokens; own: tokens of the sequence, common ones included
 };
-static_assert(sizeof(Part) == 32, "eight words");
+static_assert(sizeof(Entry) == 16, "four words");
+
+// In LDS or in scratch: the parts; the places of those before on their line, of all, and whether items are one place each (kWhole) or tiles and a lead.
+struct Tables {
+  Entry* common;
+  Entry* own;
+  int32_t* before_common;
+  int32_t* before_own;
+  __device__ Entry* e(int kind) const { return kind == kCommon ? common : own; }
+  __device__ int32_t* before(int kind) const { return kind == kCommon ? before_common : before_own; }
+};
 
 struct SharedArgs {
   CacheView c;
@@ -36,27 +44,35 @@ struct SharedArgs {
   float scale;
   __bf16* o;
   float* lse;
-  Part* parts[2];                      // [n_groups], [n_seqs]
-  int32_t* before[2];                  // places of the parts before; two more entries: of all, and whether items are one place each (kWhole), or tiles and a lead
+  Tables tables;                       // in scratch
   int32_t rows[2], sharers[2];         // rows of an item; blocks, or waves, that may share a line
   float* slots[2];                     // two per block: pieces of divided items
   int32_t waves;                       // own parts: a wave works an item, else a block
+  int32_t local;                       // blocks place the parts themselves
   float* whole[2];                     // items in one piece: [tq * hq][D + 2], sums, maximum, sum of exponentials
   __device__ int32_t count(int kind) const { return kind == kCommon ? n_groups : s.n_seqs; }
 };
 
+// A part, whole: its rows, its pages (those of the table's row from page0 on), tokens; row i sees those up to first_seen + each * i.
+struct Part { int32_t row0, rows, seq, page0, len, first_seen, each; };
+__device__ inline Part part_of(const SharedArgs& a, const Tables& t, int kind, int i) {
+  const Entry x = t.e(kind)[i];
+  if (kind == kCommon) return {x.row0, x.rows, x.other, 0, x.len, x.len - 1, 0};
+  const int32_t shared = x.other >= 0 ? t.common[x.other].len : 0, len = x.len - shared;
+  return {x.row0, x.rows, i, shared >> a.c.log_page, len, len - x.rows, 1};
+}
 __device__ inline int32_t places_of_item(const Part& p, bool whole) { return whole ? 1 : places_of<kItemLead>(p.len); }
 __device__ inline int32_t places_of_part(const SharedArgs& a, const Part& p, int rows, bool whole) {
   return p.rows == 0 ? 0 : a.c.hkv * ((p.rows * a.group - 1) / rows + 1) * places_of_item(p, whole);
 }
 
-constexpr int kPartThreads = 1024;
 constexpr int kWholeLen = 16 * kTile;  // own parts up to this long are not divided
 constexpr int kSharers = kWaves * kBlocks;       // waves that share the line of own parts
+constexpr int kLocal = 256;            // parts that a block places itself: one a thread
 
-// How many share a line, and who: a share has a few places at least, where items are one place each one.
-__device__ inline Line line_of(const SharedArgs& a, int kind, bool& whole) {
-  const int32_t* const ends = a.before[kind] + a.count(kind);
+// How many share a line: a share has a few places at least, where items are one place each one.
+__device__ inline Line line_of(const SharedArgs& a, const Tables& t, int kind, bool& whole) {
+  const int32_t* const ends = t.before(kind) + a.count(kind);
   Line line = {};
   line.total = __builtin_amdgcn_readfirstlane(ends[0]);
   whole = __builtin_amdgcn_readfirstlane(ends[1]);
@@ -64,79 +80,99 @@ __device__ inline Line line_of(const SharedArgs& a, int kind, bool& whole) {
   return line;
 }
 
-__global__ __launch_bounds__(kPartThreads) void parts_kernel(SharedArgs a) {
-  __shared__ int32_t sums[kPartThreads / 64], bad, longest;
+// Fills the tables.  Where cu_seqlens or groups fall, or groups name sequences that are not there, there are no places.
+template <int Threads>
+__device__ inline void place_parts(const SharedArgs& a, const Tables& t) {
+  __shared__ int32_t sums[Threads / 64], bad, longest;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   if (threadIdx.x == 0) bad = longest = 0;
   __syncthreads();
   bool falls = false;
-  for (int s = threadIdx.x; s < a.s.n_seqs; s += kPartThreads) {
+  for (int s = threadIdx.x; s < a.s.n_seqs; s += Threads) {
     falls |= a.s.cu[s + 1] < a.s.cu[s];
     const SeqSizes z = seq_sizes(a.s, s, a.c.page);
-    a.parts[kOwn][s] = {z.row0, z.n, s, 0, z.len, z.len - z.n, 1, -1};
+    t.own[s] = {z.row0, z.n, -1, z.len};
   }
-  for (int g = threadIdx.x; g < a.n_groups; g += kPartThreads) falls |= a.groups[g] < 0 || a.groups[g + 1] < a.groups[g] || a.groups[g + 1] > a.s.n_seqs;
+  for (int g = threadIdx.x; g < a.n_groups; g += Threads) falls |= a.groups[g] < 0 || a.groups[g + 1] < a.groups[g] || a.groups[g + 1] > a.s.n_seqs;
   if (falls) bad = 1;
   __syncthreads();
   if (!bad)
-    for (int g = wave; g < a.n_groups; g += kPartThreads / 64) {
-      const int lo = a.groups[g], hi = a.groups[g + 1];
+    for (int g0 = 0; g0 < a.n_groups; g0 += Threads / 8) {                // eight lanes a group
+      const int g = g0 + (int)threadIdx.x / 8, sub = threadIdx.x % 8;
+      const int lo = g < a.n_groups ? a.groups[g] : 0, hi = g < a.n_groups ? a.groups[g + 1] : 0;
       // what every row of the group sees; sequences without rows do not count
-      int least = INT32_MAX, first = INT32_MAX, rows = 0, seqs = 0, row0 = INT32_MAX;
-      for (int s = lo + lane; s < hi; s += 64) {
-        const SeqSizes z = seq_sizes(a.s, s, a.c.page);
-        if (z.n > 0) {
-          least = min(least, z.len - z.n);
+      int least = g < a.n_groups ? a.shared_len[g] : 0, first = INT32_MAX, rows = 0, seqs = 0, row0 = INT32_MAX;
+      for (int s = lo + sub; s < hi; s += 8) {
+        const Entry x = t.own[s];
+        t.own[s].other = g;
+        if (x.rows > 0) {
+          least = min(least, x.len - x.rows);
           first = min(first, s);
-          row0 = min(row0, z.row0);
-          rows += z.n;
+          row0 = min(row0, x.row0);
+          rows += x.rows;
           ++seqs;
         }
       }
 #pragma unroll
-      for (int d = 32; d > 0; d >>= 1) {
+      for (int d = 1; d < 8; d *= 2) {
         least = min(least, __shfl_xor(least, d));
         first = min(first, __shfl_xor(first, d));
         row0 = min(row0, __shfl_xor(row0, d));
         rows += __shfl_xor(rows, d);
         seqs += __shfl_xor(seqs, d);
       }
-      const int shared = seqs < 2 ? 0 : max(min(least, a.shared_len[g]), 0) & ~(a.c.page - 1);
-      if (lane == 0) a.parts[kCommon][g] = {row0, shared ? rows : 0, first, 0, shared, shared - 1, 0, -1};
-      if (shared)
-        for (int s = lo + lane; s < hi; s += 64) {
-          Part& p = a.parts[kOwn][s];
-          p.page0 = shared >> a.c.log_page;
-          p.len -= shared;
-          p.first_seen -= shared;
-          p.group = g;
-        }
+      const int shared = seqs < 2 ? 0 : max(least, 0) & ~(a.c.page - 1);
+      if (g < a.n_groups && sub == 0) t.common[g] = {row0, shared ? rows : 0, first, shared};
     }
   __syncthreads();
   int32_t most = 0;
-  for (int s = threadIdx.x; s < a.s.n_seqs; s += kPartThreads)
-    if (a.parts[kOwn][s].rows > 0) most = max(most, a.parts[kOwn][s].len);
-  atomicMax(&longest, wave_max(most));
+  if (!bad)
+    for (int s = threadIdx.x; s < a.s.n_seqs; s += Threads) {
+      const Part p = part_of(a, t, kOwn, s);
+      if (p.rows > 0) most = max(most, p.len);
+    }
+  most = wave_max(most);
+  if (lane == 0) atomicMax(&longest, most);
   __syncthreads();
   for (int kind = 0; kind < 2; ++kind) {
     const int n = a.count(kind);
     const bool whole = kind == kOwn && a.waves && longest <= kWholeLen;
     int32_t total = 0;
-    for (int i0 = 0; i0 < n; i0 += kPartThreads) {
+    for (int i0 = 0; i0 < n; i0 += Threads) {
       const int i = i0 + threadIdx.x;
-      const int32_t mine = i < n && !bad ? places_of_part(a, a.parts[kind][i], a.rows[kind], whole) : 0, upto = wave_prefix_sum(mine);
+      const int32_t mine = i < n && !bad ? places_of_part(a, part_of(a, t, kind, i), a.rows[kind], whole) : 0, upto = wave_prefix_sum(mine);
       if (lane == 63) sums[wave] = upto;
       __syncthreads();
       int32_t at = total + upto - mine;
-      for (int w = 0; w < kPartThreads / 64; ++w) {
+      for (int w = 0; w < Threads / 64; ++w) {
         at += w < wave ? sums[w] : 0;
         total += sums[w];
       }
-      if (i < n) a.before[kind][i] = at;
+      if (i < n) t.before(kind)[i] = at;
       __syncthreads();
     }
-    if (threadIdx.x == 0) a.before[kind][n] = total, a.before[kind][n + 1] = whole;
+    if (threadIdx.x == 0) t.before(kind)[n] = total, t.before(kind)[n + 1] = whole;
   }
+}
+
+constexpr int kPartThreads = 1024;
+__global__ __launch_bounds__(kPartThreads) void parts_kernel(SharedArgs a) { place_parts<kPartThreads>(a, a.tables); }
+
+// The tables that a block of a line's launch goes by, its own where there are few parts (a launch of one block takes 5 to 7 us, placing them in every block about 1); the first block leaves them
+// for the join.
+struct LocalTables { Entry e[2][kLocal]; int32_t before[2][kLocal + 2]; };
+__device__ inline Tables tables_of(const SharedArgs& a, LocalTables& own) {
+  if (!a.local) return a.tables;
+  const Tables t = {own.e[0], own.e[1], own.before[0], own.before[1]};
+  place_parts<256>(a, t);
+  __syncthreads();
+  if (blockIdx.x == 0)
+    for (int kind = 0; kind < 2; ++kind)
+      for (int i = threadIdx.x; i < a.count(kind) + 2; i += 256) {
+        if (i < a.count(kind)) a.tables.e(kind)[i] = t.e(kind)[i];
+        a.tables.before(kind)[i] = t.before(kind)[i];
+      }
+  return t;
 }
 
 // The last of v[0 .. n - 1], which do not fall, that is at most x (v[0] is); a wave looks at 64 at a time.
@@ -156,6 +192,7 @@ __device__ inline int last_up_to(int n, int x, At at) {
 
 // A block's or a wave's share of a line, item by item.
 struct Work {
+  const Tables& t;
   Line line;
   int32_t me, at, end, base;
   int kind, index;
@@ -164,20 +201,20 @@ struct Work {
   // the piece at hand
   int head, row_block, t0, t1, tiles, all_rows;
   bool whole;
-  __device__ Work(const SharedArgs& a, int kind, int me) : me(me), kind(kind) {
-    line = line_of(a, kind, undivided);
+  __device__ Work(const SharedArgs& a, const Tables& t, int kind, int me) : t(t), me(me), kind(kind) {
+    line = line_of(a, t, kind, undivided);
     at = end = 0;
     if (me >= line.sharers) return;
     at = line.begin(me);
     end = line.begin(me + 1);
-    index = last_up_to(a.count(kind), at, [&](int i) { return a.before[kind][i]; });
+    index = last_up_to(a.count(kind), at, [&](int i) { return t.before(kind)[i]; });
     take(a);
   }
   __device__ void take(const SharedArgs& a) {
-    const int32_t* const w = reinterpret_cast<const int32_t*>(a.parts[kind] + index);
+    const Part p = part_of(a, t, kind, index);
     auto uniform = [](int32_t x) { return __builtin_amdgcn_readfirstlane(x); };          // (scalar registers)
-    part = {uniform(w[0]), uniform(w[1]), uniform(w[2]), uniform(w[3]), uniform(w[4]), uniform(w[5]), uniform(w[6]), -1};
-    base = uniform(a.before[kind][index]);
+    part = {uniform(p.row0), uniform(p.rows), uniform(p.seq), uniform(p.page0), uniform(p.len), uniform(p.first_seen), p.each};
+    base = uniform(t.before(kind)[index]);
   }
   __device__ bool next(const SharedArgs& a) {
     while (at < end) {
@@ -241,12 +278,12 @@ __device__ inline void walk_piece(const SharedArgs& a, const Work& w, int lane, 
 }
 
 template <int D, int Fmt, int NB>
-__device__ inline void few_rows(const SharedArgs& a, int kind, int lane, int wave, float* stage, int32_t* first_nan) {
+__device__ inline void few_rows(const SharedArgs& a, const Tables& t, int kind, int lane, int wave, float* stage, int32_t* first_nan) {
   constexpr int kRows = 16 * NB, kStride = D + 4;          // floats of a staged row: rows on different banks
   float* const stage_m = stage + kWaves * kRows * kStride;
   float* const stage_l = stage_m + kWaves * kRows;
   const int n = lane & 15, g = lane >> 4;
-  Work w(a, kind, blockIdx.x);
+  Work w(a, t, kind, blockIdx.x);
   while (w.next(a)) {
     RowState<D> r[NB];
     int rows;
@@ -289,9 +326,9 @@ __device__ inline void few_rows(const SharedArgs& a, int kind, int lane, int wav
 // Own parts of few rows: a wave works an item, or a piece of one, alone.  They are short as a rule - what was added behind the common beginning - and a block's waves would each have a tile or
 // none, and meet for it.
 template <int D, int Fmt>
-__device__ inline void own_rows(const SharedArgs& a, int lane, int wave, int32_t* first_nan) {
+__device__ inline void own_rows(const SharedArgs& a, const Tables& t, int lane, int wave, int32_t* first_nan) {
   const int n = lane & 15, g = lane >> 4;
-  Work w(a, kOwn, kWaves * blockIdx.x + wave);
+  Work w(a, t, kOwn, kWaves * blockIdx.x + wave);
   while (w.next(a)) {
     RowState<D> r[1];
     int rows;
@@ -311,13 +348,13 @@ __device__ inline void own_rows(const SharedArgs& a, int lane, int wave, int32_t
 }
 
 template <int D, int Fmt, int kNB>
-__device__ inline void many_rows(const SharedArgs& a, int kind, int lane, int wave, unsigned char* lds, float (&key_scale)[4][4], int32_t (&live)[4][4], int32_t (&first_nan)[2][D]) {
+__device__ inline void many_rows(const SharedArgs& a, const Tables& t, int kind, int lane, int wave, unsigned char* lds, float (&key_scale)[4][4], int32_t (&live)[4][4], int32_t (&first_nan)[2][D]) {
   constexpr int kRows = 64 * kNB;
   const int n = lane & 15, g = lane >> 4;
   const RowsLane at_lane = rows_lane<D>(lane, wave);
   if (Fmt == kE4m3 && threadIdx.x < D) first_nan[1][threadIdx.x] = INT32_MAX;
   int parity = 1;                                          // of the items that see a tile
-  Work w(a, kind, blockIdx.x);
+  Work w(a, t, kind, blockIdx.x);
   while (w.next(a)) {
     bf16x8 q[kNB][D / 32];
     f32x4 o[kNB][D / 16];
@@ -369,91 +406,98 @@ __device__ inline void many_rows(const SharedArgs& a, int kind, int lane, int wa
 // One launch works both lines (Own), or the line `kind`.  kRows: 16, 32, 64, 128 rows of an item.
 template <int D, int Fmt, int kRows, bool Own>
 __global__ __launch_bounds__(256, 2) void shared_kernel(SharedArgs a, int kind) {
+  __shared__ LocalTables local;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Tables t = tables_of(a, local);
   if constexpr (kRows <= 32) {
     __shared__ __align__(16) float stage[kWaves * kRows * (D + 6)];
     __shared__ int32_t first_nan[kWaves][Fmt == kE4m3 ? D : 1];
-    if constexpr (Own) own_rows<D, Fmt>(a, lane, wave, first_nan[wave]);
-    few_rows<D, Fmt, kRows / 16>(a, kind, lane, wave, stage, first_nan[wave]);
+    if constexpr (Own) own_rows<D, Fmt>(a, t, lane, wave, first_nan[wave]);
+    few_rows<D, Fmt, kRows / 16>(a, t, kind, lane, wave, stage, first_nan[wave]);
   } else {
     extern __shared__ __align__(256) unsigned char lds[];  // two stages
     __shared__ float key_scale[4][4];
     __shared__ int32_t live[4][4], first_nan[2][D];
     // (the waves' own notes lie where the stages will)
     if constexpr (Own) {
-      own_rows<D, Fmt>(a, lane, wave, reinterpret_cast<int32_t*>(lds) + wave * D);
+      own_rows<D, Fmt>(a, t, lane, wave, reinterpret_cast<int32_t*>(lds) + wave * D);
       __syncthreads();
     }
-    many_rows<D, Fmt, kRows / 64>(a, kind, lane, wave, lds, key_scale, live, first_nan);
+    many_rows<D, Fmt, kRows / 64>(a, t, kind, lane, wave, lds, key_scale, live, first_nan);
   }
 }
 
-template <int D>
-struct RowSum { float m, l, o[D / 64]; };
-
-// Joins the pieces of one item of row `row` of a part.
-template <int D>
-__device__ inline void join_item(const SharedArgs& a, int kind, int index, int row_tok, int h, RowSum<D>& r) {
-  constexpr int kCh = D / 64;
-  const Part p = a.parts[kind][index];
-  const int rows = a.rows[kind], row = (row_tok - p.row0) * a.group + h % a.group, head = h / a.group, all_rows = p.rows * a.group;
+// The pieces of a row's item: the slots of blocks (waves) first, first + 1, ..., or, of one in one piece, its place among such rows.
+struct Pieces { int first, n, lr, rows; const float* whole; const float* slots; };
+__device__ inline Pieces pieces_of(const SharedArgs& a, int kind, int index, int tok, int h, int head_dim) {
+  const Tables& t = a.tables;
+  const Part p = part_of(a, t, kind, index);
+  const int rows = a.rows[kind], row = (tok - p.row0) * a.group + h % a.group, head = h / a.group, all_rows = p.rows * a.group;
   bool undivided;
-  const Line line = line_of(a, kind, undivided);
-  const int tiles = tiles_of(p.len), row_blocks = (all_rows + rows - 1) / rows, lr = row % rows;
-  const int32_t tile0 = a.before[kind][index] + (head * row_blocks + row / rows) * places_of<kItemLead>(p.len) + kItemLead;
-  const int first = undivided ? 0 : line.owner(tile0), pieces = undivided ? 1 : line.owner(tile0 + tiles - 1) - first + 1, ch = kCh * (threadIdx.x & 63);
-  const int floats = slot_floats(D, rows);
-  const int at = lr * D + ch;
-  const float* const whole = a.whole[kind] + ((int64_t)row_tok * a.hq + h) * (D + 4);
-  constexpr int N = 4;
-  for (int p0 = 0; p0 < pieces; p0 += N) {
-    float pm[N], pl[N], po[N][kCh];
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int piece = min(p0 + i, pieces - 1);
-      const float* const s = a.slots[kind] + (int64_t)(2 * (first + piece) + (piece == 0 ? 1 : 0)) * floats;
-      const float* const m = pieces == 1 ? whole + D : s + rows * D + lr;
-      pm[i] = *m;
-      pl[i] = pieces == 1 ? whole[D + 1] : m[rows];
-#pragma unroll
-      for (int c = 0; c < kCh; ++c) po[i][c] = pieces == 1 ? whole[ch + c] : s[at + c];
-    }
-    float top = r.m;
-#pragma unroll
-    for (int i = 0; i < N; ++i) top = fmaxf(top, pm[i]);   // (the last one again where there are no more)
-    const float f0 = __builtin_amdgcn_exp2f(r.m - top);
-    r.m = top;
-    r.l *= f0;
-#pragma unroll
-    for (int c = 0; c < kCh; ++c) r.o[c] *= f0;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const bool there = p0 + i < pieces;
-      const float f = __builtin_amdgcn_exp2f(pm[i] - top);
-      r.l += there ? f * pl[i] : 0.f;
-#pragma unroll
-      for (int c = 0; c < kCh; ++c) r.o[c] += there ? f * po[i][c] : 0.f;
-    }
-  }
+  const Line line = line_of(a, t, kind, undivided);
+  const int tiles = tiles_of(p.len), row_blocks = (all_rows + rows - 1) / rows;
+  const int32_t tile0 = t.before(kind)[index] + (head * row_blocks + row / rows) * places_of<kItemLead>(p.len) + kItemLead;
+  const int first = undivided ? 0 : line.owner(tile0), n = undivided ? 1 : line.owner(tile0 + tiles - 1) - first + 1;
+  return {first, n, row % rows, rows, a.whole[kind] + ((int64_t)tok * a.hq + h) * (head_dim + 4), a.slots[kind]};
 }
 
+// A wave for each row: the pieces of its items.  Lane i first looks at the maximum and the sum of piece i, so that all of these are asked for at once; then the sums follow, eight on their way.
 template <int D>
 __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs a) {
-  constexpr int kCh = D / 64;
-  const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (unit >= (int64_t)a.s.n_rows * a.hq || a.before[kOwn][a.s.n_seqs] == 0) return;
-  const int tok = __builtin_amdgcn_readfirstlane((int)(unit / a.hq)), h = __builtin_amdgcn_readfirstlane((int)(unit % a.hq)), lane = threadIdx.x & 63;
+  constexpr int kCh = D / 64, kAtOnce = 8;
+  const int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (unit >= (int64_t)a.s.n_rows * a.hq || a.tables.before_own[a.s.n_seqs] == 0) return;
+  const int tok = (int)(unit / a.hq), h = (int)(unit % a.hq), lane = threadIdx.x & 63;
   if (a.s.cu[0] > tok || a.s.cu[a.s.n_seqs] <= tok) return;
   const int seq = last_up_to(a.s.n_seqs, tok, [&](int i) { return a.s.cu[i]; });
-  const int group = a.parts[kOwn][seq].group;
-  RowSum<D> r = {kLow, 0.f, {}};
-  if (group >= 0) join_item<D>(a, kCommon, group, tok, h, r);
-  join_item<D>(a, kOwn, seq, tok, h, r);
-  const float inv = r.l == 0.f ? 0.f : 1.f / r.l;
-  __bf16* const to = a.o + ((int64_t)tok * a.hq + h) * D + kCh * lane;
+  const int group = a.tables.own[seq].other;
+  const Pieces own = pieces_of(a, kOwn, seq, tok, h, D);
+  Pieces common = {};
+  if (group >= 0 && a.tables.common[group].rows > 0) common = pieces_of(a, kCommon, group, tok, h, D);
+  const int all = __builtin_amdgcn_readfirstlane(common.n + own.n), ch = kCh * lane;
+  float m = kLow, l = 0.f, o[kCh] = {};
+  for (int p0 = 0; p0 < all; p0 += 64) {
+    const int mine = min(p0 + lane, all - 1);
+    const bool is_common = mine < common.n;
+    const Pieces x = is_common ? common : own;
+    const int piece = is_common ? mine : mine - common.n;
+    const float* const slot = x.slots + (int64_t)(2 * (x.first + piece) + (piece == 0 ? 1 : 0)) * slot_floats(D, x.rows);
+    const float* const sums = x.n == 1 ? x.whole : slot + x.lr * D;
+    const float* const stats = x.n == 1 ? x.whole + D : slot + x.rows * D + x.lr;
+    const float pm = stats[0], pl = stats[x.n == 1 ? 1 : x.rows];
+    const float top = fmaxf(m, wave_maxf(pm)), before = __builtin_amdgcn_exp2f(m - top);
+    const float f = p0 + lane < all ? __builtin_amdgcn_exp2f(pm - top) : 0.f;
+    m = top;
+    float part = p0 + lane < all ? f * pl : 0.f;
 #pragma unroll
-  for (int c = 0; c < kCh; ++c) to[c] = (__bf16)(r.o[c] * inv);
-  if (lane == 0) a.lse[(int64_t)h * a.s.n_rows + tok] = r.l == 0.f ? -INFINITY : (r.m + __builtin_amdgcn_logf(r.l)) * kLn2;
+    for (int d = 32; d > 0; d >>= 1) part += __shfl_xor(part, d);
+    l = l * before + part;
+#pragma unroll
+    for (int c = 0; c < kCh; ++c) o[c] *= before;
+    const int n = min(all - p0, 64);
+    const uint64_t at = (uint64_t)sums;
+    for (int j0 = 0; j0 < n; j0 += kAtOnce) {
+      float po[kAtOnce][kCh], pf[kAtOnce];
+#pragma unroll
+      for (int j = 0; j < kAtOnce; ++j) {
+        const int k = min(j0 + j, n - 1);
+        const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)at, k), hi = __builtin_amdgcn_readlane((int)(at >> 32), k);
+        const float* const from = reinterpret_cast<const float*>((uint64_t)hi << 32 | lo);
+        pf[j] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), k));
+#pragma unroll
+        for (int c = 0; c < kCh; ++c) po[j][c] = from[ch + c];
+      }
+#pragma unroll
+      for (int j = 0; j < kAtOnce; ++j)
+#pragma unroll
+        for (int c = 0; c < kCh; ++c) o[c] += j0 + j < n ? pf[j] * po[j][c] : 0.f;
+    }
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  __bf16* const to = a.o + ((int64_t)tok * a.hq + h) * D + ch;
+#pragma unroll
+  for (int c = 0; c < kCh; ++c) to[c] = (__bf16)(o[c] * inv);
+  if (lane == 0) a.lse[(int64_t)h * a.s.n_rows + tok] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 // ---- host ---------------------------------------------------------------------------------------
@@ -461,7 +505,7 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs a) {
 // Rows of a block, from the rows of a group or a sequence on average (as in fcp_cache_attn).
 int rows_form(int64_t all_rows, int64_t n) { return all_rows <= 16 * n ? 16 : all_rows <= 32 * n ? 32 : all_rows <= 64 * n ? 64 : 128; }
 
-struct SharedPlan { int rows[2]; int32_t sharers[2]; bool waves; };
+struct SharedPlan { int rows[2]; int32_t sharers[2]; bool waves, local; };
 SharedPlan plan_shared(const CacheView& c, int32_t n_seqs, int32_t n_groups, int32_t tq, int32_t hq) {
   SharedPlan p;
   const int64_t all_rows = (int64_t)tq * (hq / c.hkv);
@@ -470,6 +514,7 @@ SharedPlan plan_shared(const CacheView& c, int32_t n_seqs, int32_t n_groups, int
   p.waves = p.rows[kOwn] == 16;
   p.sharers[kCommon] = kBlocks;
   p.sharers[kOwn] = p.waves ? kSharers : kBlocks;
+  p.local = n_seqs <= kLocal;
   return p;
 }
 // Scratch: for any number of groups up to n_seqs.  The slots of common parts have room for the rows of one group.
@@ -482,7 +527,7 @@ SharedSpace shared_space(const CacheView& c, int head_dim, int32_t n_seqs, int32
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t here = at; at += pad_to(bytes, 256); return here; };
   for (int kind = 0; kind < 2; ++kind) {
-    s.parts[kind] = take((size_t)n_seqs * sizeof(Part));
+    s.parts[kind] = take((size_t)n_seqs * sizeof(Entry));
     s.before[kind] = take(((size_t)n_seqs + 2) * 4);
     s.slots[kind] = take((size_t)2 * p.sharers[kind] * slot_floats(head_dim, p.rows[kind]) * 4);
     s.whole[kind] = take((size_t)tq * hq * (head_dim + 4) * 4);
@@ -495,7 +540,7 @@ template <int D, int Fmt, int kRows, bool Own>
 int launch_line(const SharedArgs& a, int kind, hipStream_t st) {
   constexpr int kLds = kRows <= 32 ? 0 : 2 * Stage<D>::kBytes;
   auto kernel = shared_kernel<D, Fmt, kRows, Own>;
-  if (kLds > 64 * 1024 - 2048) {
+  if (kLds > 48 * 1024) {
     static std::atomic<uint64_t> raised;
     if (int rc = raise_lds_limit(reinterpret_cast<const void*>(kernel), kLds, raised)) return rc;
   }
@@ -506,8 +551,10 @@ int launch_line(const SharedArgs& a, int kind, hipStream_t st) {
 
 template <int D, int Fmt>
 int launch_shared(const SharedArgs& a, hipStream_t st) {
-  parts_kernel<<<dim3(1), dim3(kPartThreads), 0, st>>>(a);
-  FCP_HIP_CHECK(hipGetLastError());
+  if (!a.local) {
+    parts_kernel<<<dim3(1), dim3(kPartThreads), 0, st>>>(a);
+    FCP_HIP_CHECK(hipGetLastError());
+  }
   const int common = a.rows[kCommon];
   int rc;
   if (a.waves) {
@@ -583,15 +630,16 @@ extern "C" int fcp_cache_attn_shared(const fcp_cache* cache, const void* q, int6
   a.o = static_cast<__bf16*>(o);
   a.lse = lse;
   char* const at = static_cast<char*>(scratch);
+  a.tables = {reinterpret_cast<Entry*>(at + space.parts[kCommon]), reinterpret_cast<Entry*>(at + space.parts[kOwn]), reinterpret_cast<int32_t*>(at + space.before[kCommon]),
+              reinterpret_cast<int32_t*>(at + space.before[kOwn])};
   for (int kind = 0; kind < 2; ++kind) {
-    a.parts[kind] = reinterpret_cast<Part*>(at + space.parts[kind]);
-    a.before[kind] = reinterpret_cast<int32_t*>(at + space.before[kind]);
     a.slots[kind] = reinterpret_cast<float*>(at + space.slots[kind]);
     a.whole[kind] = reinterpret_cast<float*>(at + space.whole[kind]);
     a.rows[kind] = p.rows[kind];
     a.sharers[kind] = p.sharers[kind];
   }
   a.waves = p.waves;
+  a.local = p.local;
   hipStream_t st = static_cast<hipStream_t>(stream);
   const bool e4m3 = cache->format == FCP_CACHE_E4M3;
   return cache->head_dim == 128 ? (e4m3 ? launch_shared<128, kE4m3>(a, st) : launch_shared<128, kInt8>(a, st))
