@@ -70,14 +70,82 @@ constexpr int kWholeLen = 16 * kTile;  // own parts up to this long are not divi
 constexpr int kSharers = kWaves * kBlocks;       // waves that share the line of own parts
 constexpr int kLocal = 256;            // parts that a block places itself: one a thread
 
-// How many share a line: a share has a few places at least, where items are one place each one.
-__device__ inline Line line_of(const SharedArgs& a, const Tables& t, int kind, bool& whole) {
-  const int32_t* const ends = t.before(kind) + a.count(kind);
-  Line line = {};
-  line.total = __builtin_amdgcn_readfirstlane(ends[0]);
-  whole = __builtin_amdgcn_readfirstlane(ends[1]);
-  line.sharers = min(a.sharers[kind], whole ? line.total : (line.total + kLeastTiles - 1) / kLeastTiles);
-  return line;
+// Places 0 .. total - 1 in `n` shares that differ by one place at most.
+struct Even {
+  int32_t total, n;
+  __device__ int32_t begin(int32_t i) const { return i * (total / n) + min(i, total % n); }
+  __device__ int32_t owner(int32_t x) const {
+    const int32_t q = total / n, r = total % n, first = r * (q + 1);
+    return x < first ? x / (q + 1) : r + (x - first) / q;
+  }
+};
+// A line and its shares: a share has a few places at least, where items are one place each one.  Of the common line the last ones are smaller: their blocks begin with own parts, whose time is
+// that of `kOwnFirst` places of the common line for every item of a wave.
+struct Shares {
+  int32_t total, n;                    // places, shares
+  int32_t full, border;                // the first `full` shares have the places before `border`
+  bool whole;
+  __device__ int32_t begin(int32_t i) const { return i < full ? Even{border, full}.begin(i) : i == n ? total : border + Even{total - border, n - full}.begin(i - full); }
+  __device__ int32_t owner(int32_t x) const { return x < border ? Even{border, full}.owner(x) : full + Even{total - border, n - full}.owner(x - border); }
+};
+constexpr int own_first(int rows) { return rows == 128 ? 3 : 4; }
+__device__ inline Shares shares_of(const SharedArgs& a, const Tables& t, int kind) {
+  auto line = [&](int k) {
+    const int32_t* const ends = t.before(k) + a.count(k);
+    Shares s = {};
+    s.total = __builtin_amdgcn_readfirstlane(ends[0]);
+    s.whole = __builtin_amdgcn_readfirstlane(ends[1]);
+    s.n = min(a.sharers[k], s.whole ? s.total : (s.total + kLeastTiles - 1) / kLeastTiles);
+    s.full = s.n;
+    s.border = s.total;
+    return s;
+  };
+  Shares s = line(kind);
+  if (kind == kCommon && a.waves && s.n > 0) {
+    const Shares own = line(kOwn);
+    const int32_t rest = kBlocks - (own.n + kWaves - 1) / kWaves;         // blocks without own parts
+    if (s.n > rest) {
+      const int32_t items = own.whole ? (own.total + own.n - 1) / own.n : 1, less = own_first(a.rows[kCommon]) * items;
+      s.full = rest;
+      s.border = (int32_t)min((int64_t)s.total, rest * (((int64_t)s.total + (int64_t)(s.n - rest) * less) / s.n));
+    }
+  }
+  return s;
+}
+// Shares of the common line go to the blocks from the last one on, those of the own line from the first.
+__device__ inline int share_of_block(const SharedArgs& a, int kind) { return kind == kCommon && a.waves ? kBlocks - 1 - (int)blockIdx.x : (int)blockIdx.x; }
+
+// The common parts from the groups and the own parts' entries; these learn their group.
+struct Group { int32_t lo, hi, said; };
+template <int Threads, class F>
+__device__ inline void place_groups(const SharedArgs& a, const Tables& t, F group) {
+  for (int g0 = 0; g0 < a.n_groups; g0 += Threads / 8) {                // eight lanes a group
+    const int g = g0 + (int)threadIdx.x / 8, sub = threadIdx.x % 8;
+    const Group x = g < a.n_groups ? group(g) : Group{0, 0, 0};
+    // what every row of the group sees; sequences without rows do not count
+    int least = x.said, first = INT32_MAX, rows = 0, seqs = 0, row0 = INT32_MAX;
+    for (int s = x.lo + sub; s < x.hi; s += 8) {
+      const Entry y = t.own[s];
+      t.own[s].other = g;
+      if (y.rows > 0) {
+        least = min(least, y.len - y.rows);
+        first = min(first, s);
+        row0 = min(row0, y.row0);
+        rows += y.rows;
+        ++seqs;
+      }
+    }
+#pragma unroll
+    for (int d = 1; d < 8; d *= 2) {
+      least = min(least, __shfl_xor(least, d));
+      first = min(first, __shfl_xor(first, d));
+      row0 = min(row0, __shfl_xor(row0, d));
+      rows += __shfl_xor(rows, d);
+      seqs += __shfl_xor(seqs, d);
+    }
+    const int shared = seqs < 2 ? 0 : max(least, 0) & ~(a.c.page - 1);
+    if (g < a.n_groups && sub == 0) t.common[g] = {row0, shared ? rows : 0, first, shared};
+  }
 }
 
 // Fills the tables.  Where cu_seqlens or groups fall, or groups name sequences that are not there, there are no places.
@@ -97,33 +165,7 @@ __device__ inline void place_parts(const SharedArgs& a, const Tables& t) {
   if (falls) bad = 1;
   __syncthreads();
   if (!bad)
-    for (int g0 = 0; g0 < a.n_groups; g0 += Threads / 8) {                // eight lanes a group
-      const int g = g0 + (int)threadIdx.x / 8, sub = threadIdx.x % 8;
-      const int lo = g < a.n_groups ? a.groups[g] : 0, hi = g < a.n_groups ? a.groups[g + 1] : 0;
-      // what every row of the group sees; sequences without rows do not count
-      int least = g < a.n_groups ? a.shared_len[g] : 0, first = INT32_MAX, rows = 0, seqs = 0, row0 = INT32_MAX;
-      for (int s = lo + sub; s < hi; s += 8) {
-        const Entry x = t.own[s];
-        t.own[s].other = g;
-        if (x.rows > 0) {
-          least = min(least, x.len - x.rows);
-          first = min(first, s);
-          row0 = min(row0, x.row0);
-          rows += x.rows;
-          ++seqs;
-        }
-      }
-#pragma unroll
-      for (int d = 1; d < 8; d *= 2) {
-        least = min(least, __shfl_xor(least, d));
-        first = min(first, __shfl_xor(first, d));
-        row0 = min(row0, __shfl_xor(row0, d));
-        rows += __shfl_xor(rows, d);
-        seqs += __shfl_xor(seqs, d);
-      }
-      const int shared = seqs < 2 ? 0 : max(least, 0) & ~(a.c.page - 1);
-      if (g < a.n_groups && sub == 0) t.common[g] = {row0, shared ? rows : 0, first, shared};
-    }
+    place_groups<Threads>(a, t, [&](int g) { return Group{a.groups[g], a.groups[g + 1], a.shared_len[g]}; });
   __syncthreads();
   int32_t most = 0;
   if (!bad)
@@ -158,20 +200,68 @@ __device__ inline void place_parts(const SharedArgs& a, const Tables& t) {
 constexpr int kPartThreads = 1024;
 __global__ __launch_bounds__(kPartThreads) void parts_kernel(SharedArgs a) { place_parts<kPartThreads>(a, a.tables); }
 
-// The tables that a block of a line's launch goes by, its own where there are few parts (a launch of one block takes 5 to 7 us, placing them in every block about 1); the first block leaves them
-// for the join.
+// The same by every block of a line's launch, where there are up to kLocal sequences: a thread looks at a sequence and at a group, and everything is asked for at once.  (A launch of one block takes
+// 5 to 7 us.)  The first block leaves the tables for the join.
 struct LocalTables { Entry e[2][kLocal]; int32_t before[2][kLocal + 2]; };
 __device__ inline Tables tables_of(const SharedArgs& a, LocalTables& own) {
   if (!a.local) return a.tables;
+  __shared__ int32_t sums[3][4], longest[4], bad[4];
   const Tables t = {own.e[0], own.e[1], own.before[0], own.before[1]};
-  place_parts<256>(a, t);
+  const int i = threadIdx.x, lane = i & 63, wave = i >> 6;
+  const bool is_seq = i < a.s.n_seqs, is_group = i < a.n_groups;
+  const SeqSizes z = is_seq ? seq_sizes(a.s, i, a.c.page) : SeqSizes{};
+  bool falls = is_seq && a.s.cu[i + 1] < a.s.cu[i];
+  const int lo = is_group ? a.groups[i] : 0, hi = is_group ? a.groups[i + 1] : 0, said = is_group ? a.shared_len[i] : 0;
+  falls |= lo < 0 || hi < lo || hi > a.s.n_seqs;
+  if (is_seq) t.own[i] = {z.row0, z.n, -1, z.len};
+  if (is_group) t.common[i] = {lo, hi, said, 0};
+  falls = __ballot(falls);
+  if (lane == 0) bad[wave] = falls;
   __syncthreads();
-  if (blockIdx.x == 0)
-    for (int kind = 0; kind < 2; ++kind)
-      for (int i = threadIdx.x; i < a.count(kind) + 2; i += 256) {
-        if (i < a.count(kind)) a.tables.e(kind)[i] = t.e(kind)[i];
-        a.tables.before(kind)[i] = t.before(kind)[i];
-      }
+  const bool none = bad[0] | bad[1] | bad[2] | bad[3];
+  if (!none) place_groups<kLocal>(a, t, [&](int g) { const Entry x = t.common[g]; return Group{x.row0, x.rows, x.other}; });
+  __syncthreads();
+  // places of the thread's sequence if items are one place each, and if they are not; of its group
+  int32_t places[3] = {}, upto[3], most = 0;
+  if (is_seq && !none) {
+    const Part p = part_of(a, t, kOwn, i);
+    places[0] = places_of_part(a, p, a.rows[kOwn], false);
+    places[1] = places_of_part(a, p, a.rows[kOwn], true);
+    most = p.rows > 0 ? p.len : 0;
+  }
+  if (is_group && !none) places[2] = places_of_part(a, part_of(a, t, kCommon, i), a.rows[kCommon], false);
+  most = wave_max(most);
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    upto[k] = wave_prefix_sum(places[k]);
+    if (lane == 63) sums[k][wave] = upto[k];
+  }
+  if (lane == 0) longest[wave] = most;
+  __syncthreads();
+  const bool whole = a.waves && max(max(longest[0], longest[1]), max(longest[2], longest[3])) <= kWholeLen;
+  int32_t at[2] = {upto[2] - places[2], whole ? upto[1] - places[1] : upto[0] - places[0]}, total[2] = {};
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const int32_t common = sums[2][w], mine = whole ? sums[1][w] : sums[0][w];
+    at[0] += w < wave ? common : 0;
+    at[1] += w < wave ? mine : 0;
+    total[0] += common;
+    total[1] += mine;
+  }
+  if (is_group) t.before_common[i] = at[0];
+  if (is_seq) t.before_own[i] = at[1];
+  if (i == 0) {
+    t.before_common[a.n_groups] = total[0];
+    t.before_common[a.n_groups + 1] = 0;
+    t.before_own[a.s.n_seqs] = total[1];
+    t.before_own[a.s.n_seqs + 1] = whole;
+  }
+  __syncthreads();
+  if (blockIdx.x == 0) {
+    if (is_group) a.tables.common[i] = t.common[i], a.tables.before_common[i] = at[0];
+    if (is_seq) a.tables.own[i] = t.own[i], a.tables.before_own[i] = at[1];
+    if (i < 2) a.tables.before_common[a.n_groups + i] = t.before_common[a.n_groups + i], a.tables.before_own[a.s.n_seqs + i] = t.before_own[a.s.n_seqs + i];
+  }
   return t;
 }
 
@@ -192,8 +282,7 @@ __device__ inline int last_up_to(int n, int x, At at) {
 
 // A block's or a wave's share of a line, item by item.
 struct Work {
-  const Tables& t;
-  Line line;
+  Tables t;
   int32_t me, at, end, base;
   int kind, index;
   bool undivided;                      // all items are in one piece
@@ -202,11 +291,12 @@ struct Work {
   int head, row_block, t0, t1, tiles, all_rows;
   bool whole;
   __device__ Work(const SharedArgs& a, const Tables& t, int kind, int me) : t(t), me(me), kind(kind) {
-    line = line_of(a, t, kind, undivided);
+    const Shares shares = shares_of(a, t, kind);
+    undivided = shares.whole;
     at = end = 0;
-    if (me >= line.sharers) return;
-    at = line.begin(me);
-    end = line.begin(me + 1);
+    if (me >= shares.n) return;
+    at = shares.begin(me);
+    end = shares.begin(me + 1);
     index = last_up_to(a.count(kind), at, [&](int i) { return t.before(kind)[i]; });
     take(a);
   }
@@ -283,7 +373,7 @@ __device__ inline void few_rows(const SharedArgs& a, const Tables& t, int kind, 
   float* const stage_m = stage + kWaves * kRows * kStride;
   float* const stage_l = stage_m + kWaves * kRows;
   const int n = lane & 15, g = lane >> 4;
-  Work w(a, t, kind, blockIdx.x);
+  Work w(a, t, kind, share_of_block(a, kind));
   while (w.next(a)) {
     RowState<D> r[NB];
     int rows;
@@ -354,7 +444,7 @@ __device__ inline void many_rows(const SharedArgs& a, const Tables& t, int kind,
   const RowsLane at_lane = rows_lane<D>(lane, wave);
   if (Fmt == kE4m3 && threadIdx.x < D) first_nan[1][threadIdx.x] = INT32_MAX;
   int parity = 1;                                          // of the items that see a tile
-  Work w(a, t, kind, blockIdx.x);
+  Work w(a, t, kind, share_of_block(a, kind));
   while (w.next(a)) {
     bf16x8 q[kNB][D / 32];
     f32x4 o[kNB][D / 16];
@@ -433,11 +523,10 @@ __device__ inline Pieces pieces_of(const SharedArgs& a, int kind, int index, int
   const Tables& t = a.tables;
   const Part p = part_of(a, t, kind, index);
   const int rows = a.rows[kind], row = (tok - p.row0) * a.group + h % a.group, head = h / a.group, all_rows = p.rows * a.group;
-  bool undivided;
-  const Line line = line_of(a, t, kind, undivided);
+  const Shares shares = shares_of(a, t, kind);
   const int tiles = tiles_of(p.len), row_blocks = (all_rows + rows - 1) / rows;
   const int32_t tile0 = t.before(kind)[index] + (head * row_blocks + row / rows) * places_of<kItemLead>(p.len) + kItemLead;
-  const int first = undivided ? 0 : line.owner(tile0), n = undivided ? 1 : line.owner(tile0 + tiles - 1) - first + 1;
+  const int first = shares.whole ? 0 : shares.owner(tile0), n = shares.whole ? 1 : shares.owner(tile0 + tiles - 1) - first + 1;
   return {first, n, row % rows, rows, a.whole[kind] + ((int64_t)tok * a.hq + h) * (head_dim + 4), a.slots[kind]};
 }
 
