@@ -32,6 +32,9 @@ struct Tables {
   __device__ int32_t* before(int kind) const { return kind == kCommon ? before_common : before_own; }
 };
 
+// Where the pieces of a row's item lie: slots of blocks (waves) first, first + 1, ..; n = 1: in `whole`, n = 0: there is none.  lr: its row in a slot.
+struct RowPieces { int32_t first, n, lr, pad; };
+
 struct SharedArgs {
   CacheView c;
   SeqView s;
@@ -45,6 +48,7 @@ struct SharedArgs {
   __bf16* o;
   float* lse;
   Tables tables;                       // in scratch
+  struct RowPieces* pieces[2];         // [tq * hq], of all rows of sequences
   int32_t rows[2], sharers[2];         // rows of an item; blocks, or waves, that may share a line
   float* slots[2];                     // two per block: pieces of divided items
   int32_t waves;                       // own parts: a wave works an item, else a block
@@ -54,12 +58,12 @@ struct SharedArgs {
 };
 
 // A part, whole: its rows, its pages (those of the table's row from page0 on), tokens; row i sees those up to first_seen + each * i.
-struct Part { int32_t row0, rows, seq, page0, len, first_seen, each; };
+struct Part { int32_t row0, rows, seq, page0, len, first_seen, each, common; };       // common: own parts: their rows have a common part
 __device__ inline Part part_of(const SharedArgs& a, const Tables& t, int kind, int i) {
   const Entry x = t.e(kind)[i];
-  if (kind == kCommon) return {x.row0, x.rows, x.other, 0, x.len, x.len - 1, 0};
+  if (kind == kCommon) return {x.row0, x.rows, x.other, 0, x.len, x.len - 1, 0, 0};
   const int32_t shared = x.other >= 0 ? t.common[x.other].len : 0, len = x.len - shared;
-  return {x.row0, x.rows, i, shared >> a.c.log_page, len, len - x.rows, 1};
+  return {x.row0, x.rows, i, shared >> a.c.log_page, len, len - x.rows, 1, shared > 0};
 }
 __device__ inline int32_t places_of_item(const Part& p, bool whole) { return whole ? 1 : places_of<kItemLead>(p.len); }
 __device__ inline int32_t places_of_part(const SharedArgs& a, const Part& p, int rows, bool whole) {
@@ -79,40 +83,18 @@ struct Even {
     return x < first ? x / (q + 1) : r + (x - first) / q;
   }
 };
-// A line and its shares: a share has a few places at least, where items are one place each one.  Of the common line the last ones are smaller: their blocks begin with own parts, whose time is
-// that of `kOwnFirst` places of the common line for every item of a wave.
+// A line and its shares: a share has a few places at least, where items are one place each one.
 struct Shares {
-  int32_t total, n;                    // places, shares
-  int32_t full, border;                // the first `full` shares have the places before `border`
+  Even even;
   bool whole;
-  __device__ int32_t begin(int32_t i) const { return i < full ? Even{border, full}.begin(i) : i == n ? total : border + Even{total - border, n - full}.begin(i - full); }
-  __device__ int32_t owner(int32_t x) const { return x < border ? Even{border, full}.owner(x) : full + Even{total - border, n - full}.owner(x - border); }
 };
-constexpr int own_first(int rows) { return rows == 128 ? 3 : 4; }
 __device__ inline Shares shares_of(const SharedArgs& a, const Tables& t, int kind) {
-  auto line = [&](int k) {
-    const int32_t* const ends = t.before(k) + a.count(k);
-    Shares s = {};
-    s.total = __builtin_amdgcn_readfirstlane(ends[0]);
-    s.whole = __builtin_amdgcn_readfirstlane(ends[1]);
-    s.n = min(a.sharers[k], s.whole ? s.total : (s.total + kLeastTiles - 1) / kLeastTiles);
-    s.full = s.n;
-    s.border = s.total;
-    return s;
-  };
-  Shares s = line(kind);
-  if (kind == kCommon && a.waves && s.n > 0) {
-    const Shares own = line(kOwn);
-    const int32_t rest = kBlocks - (own.n + kWaves - 1) / kWaves;         // blocks without own parts
-    if (s.n > rest) {
-      const int32_t items = own.whole ? (own.total + own.n - 1) / own.n : 1, less = own_first(a.rows[kCommon]) * items;
-      s.full = rest;
-      s.border = (int32_t)min((int64_t)s.total, rest * (((int64_t)s.total + (int64_t)(s.n - rest) * less) / s.n));
-    }
-  }
-  return s;
+  const int32_t* const ends = t.before(kind) + a.count(kind);
+  const int32_t total = __builtin_amdgcn_readfirstlane(ends[0]);
+  const bool whole = __builtin_amdgcn_readfirstlane(ends[1]);
+  return {{total, min(a.sharers[kind], whole ? total : (total + kLeastTiles - 1) / kLeastTiles)}, whole};
 }
-// Shares of the common line go to the blocks from the last one on, those of the own line from the first.
+// Shares of the common line go to the blocks from the last one on, those of the own line from the first: where there are few, different blocks have them.
 __device__ inline int share_of_block(const SharedArgs& a, int kind) { return kind == kCommon && a.waves ? kBlocks - 1 - (int)blockIdx.x : (int)blockIdx.x; }
 
 // The common parts from the groups and the own parts' entries; these learn their group.
@@ -283,7 +265,7 @@ __device__ inline int last_up_to(int n, int x, At at) {
 // A block's or a wave's share of a line, item by item.
 struct Work {
   Tables t;
-  int32_t me, at, end, base;
+  int32_t me, at, end, base, item0;
   int kind, index;
   bool undivided;                      // all items are in one piece
   Part part;
@@ -294,17 +276,27 @@ struct Work {
     const Shares shares = shares_of(a, t, kind);
     undivided = shares.whole;
     at = end = 0;
-    if (me >= shares.n) return;
-    at = shares.begin(me);
-    end = shares.begin(me + 1);
+    if (me >= shares.even.n) return;
+    at = shares.even.begin(me);
+    end = shares.even.begin(me + 1);
     index = last_up_to(a.count(kind), at, [&](int i) { return t.before(kind)[i]; });
     take(a);
   }
   __device__ void take(const SharedArgs& a) {
     const Part p = part_of(a, t, kind, index);
     auto uniform = [](int32_t x) { return __builtin_amdgcn_readfirstlane(x); };          // (scalar registers)
-    part = {uniform(p.row0), uniform(p.rows), uniform(p.seq), uniform(p.page0), uniform(p.len), uniform(p.first_seen), p.each};
+    part = {uniform(p.row0), uniform(p.rows), uniform(p.seq), uniform(p.page0), uniform(p.len), uniform(p.first_seen), p.each, uniform(p.common)};
     base = uniform(t.before(kind)[index]);
+  }
+  // Rows of the piece at hand that begins its item: the join learns where their pieces lie.  `i` of `step` lanes.
+  __device__ void note_pieces(const SharedArgs& a, int i, int step) const {
+    if (t0 > 0) return;
+    const int rows = a.rows[kind], n = whole ? 1 : shares_of(a, t, kind).even.owner(item0 + kItemLead + tiles - 1) - me + 1;
+    for (int lr = i; lr < rows && row_block * rows + lr < all_rows; lr += step) {
+      const int64_t row = whole_row(a, row_block * rows + lr);
+      a.pieces[kind][row] = {me, n, lr, 0};
+      if (kind == kOwn && !part.common) a.pieces[kCommon][row] = {0, 0, 0, 0};
+    }
   }
   __device__ bool next(const SharedArgs& a) {
     while (at < end) {
@@ -322,6 +314,7 @@ struct Work {
       t0 = piece.first;
       t1 = piece.last;
       whole = t0 == 0 && t1 == tiles;
+      item0 = at - from;
       at += piece.places;
       if (t0 < t1) return true;                            // (else the item's lead alone)
     }
@@ -375,6 +368,7 @@ __device__ inline void few_rows(const SharedArgs& a, const Tables& t, int kind, 
   const int n = lane & 15, g = lane >> 4;
   Work w(a, t, kind, share_of_block(a, kind));
   while (w.next(a)) {
+    w.note_pieces(a, threadIdx.x, 256);
     RowState<D> r[NB];
     int rows;
     walk_piece<D, Fmt, NB>(a, w, lane, wave, kWaves, r, rows, first_nan);
@@ -420,6 +414,7 @@ __device__ inline void own_rows(const SharedArgs& a, const Tables& t, int lane, 
   const int n = lane & 15, g = lane >> 4;
   Work w(a, t, kOwn, kWaves * blockIdx.x + wave);
   while (w.next(a)) {
+    w.note_pieces(a, lane, 64);
     RowState<D> r[1];
     int rows;
     walk_piece<D, Fmt, 1>(a, w, lane, 0, 1, r, rows, first_nan);
@@ -446,6 +441,7 @@ __device__ inline void many_rows(const SharedArgs& a, const Tables& t, int kind,
   int parity = 1;                                          // of the items that see a tile
   Work w(a, t, kind, share_of_block(a, kind));
   while (w.next(a)) {
+    w.note_pieces(a, threadIdx.x, 256);
     bf16x8 q[kNB][D / 32];
     f32x4 o[kNB][D / 16];
     float m[kNB], l[kNB];
@@ -517,43 +513,29 @@ __global__ __launch_bounds__(256, 2) void shared_kernel(SharedArgs a, int kind) 
   }
 }
 
-// The pieces of a row's item: the slots of blocks (waves) first, first + 1, ..., or, of one in one piece, its place among such rows.
-struct Pieces { int first, n, lr, rows; const float* whole; const float* slots; };
-__device__ inline Pieces pieces_of(const SharedArgs& a, int kind, int index, int tok, int h, int head_dim) {
-  const Tables& t = a.tables;
-  const Part p = part_of(a, t, kind, index);
-  const int rows = a.rows[kind], row = (tok - p.row0) * a.group + h % a.group, head = h / a.group, all_rows = p.rows * a.group;
-  const Shares shares = shares_of(a, t, kind);
-  const int tiles = tiles_of(p.len), row_blocks = (all_rows + rows - 1) / rows;
-  const int32_t tile0 = t.before(kind)[index] + (head * row_blocks + row / rows) * places_of<kItemLead>(p.len) + kItemLead;
-  const int first = shares.whole ? 0 : shares.owner(tile0), n = shares.whole ? 1 : shares.owner(tile0 + tiles - 1) - first + 1;
-  return {first, n, row % rows, rows, a.whole[kind] + ((int64_t)tok * a.hq + h) * (head_dim + 4), a.slots[kind]};
-}
-
 // A wave for each row: the pieces of its items.  Lane i first looks at the maximum and the sum of piece i, so that all of these are asked for at once; then the sums follow, eight on their way.
 template <int D>
 __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs a) {
   constexpr int kCh = D / 64, kAtOnce = 8;
-  const int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (unit >= (int64_t)a.s.n_rows * a.hq || a.tables.before_own[a.s.n_seqs] == 0) return;
-  const int tok = (int)(unit / a.hq), h = (int)(unit % a.hq), lane = threadIdx.x & 63;
-  if (a.s.cu[0] > tok || a.s.cu[a.s.n_seqs] <= tok) return;
-  const int seq = last_up_to(a.s.n_seqs, tok, [&](int i) { return a.s.cu[i]; });
-  const int group = a.tables.own[seq].other;
-  const Pieces own = pieces_of(a, kOwn, seq, tok, h, D);
-  Pieces common = {};
-  if (group >= 0 && a.tables.common[group].rows > 0) common = pieces_of(a, kCommon, group, tok, h, D);
+  const int unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (unit >= a.s.n_rows * a.hq) return;
+  const int tok = unit / a.hq, h = unit - tok * a.hq;
+  // (all asked for at once)
+  const RowPieces common = a.pieces[kCommon][unit], own = a.pieces[kOwn][unit];
+  const int32_t places = a.tables.before_own[a.s.n_seqs], from_row = a.s.cu[0], to_row = a.s.cu[a.s.n_seqs];
+  if (places == 0 || tok < from_row || tok >= to_row) return;
   const int all = __builtin_amdgcn_readfirstlane(common.n + own.n), ch = kCh * lane;
   float m = kLow, l = 0.f, o[kCh] = {};
   for (int p0 = 0; p0 < all; p0 += 64) {
     const int mine = min(p0 + lane, all - 1);
     const bool is_common = mine < common.n;
-    const Pieces x = is_common ? common : own;
-    const int piece = is_common ? mine : mine - common.n;
-    const float* const slot = x.slots + (int64_t)(2 * (x.first + piece) + (piece == 0 ? 1 : 0)) * slot_floats(D, x.rows);
-    const float* const sums = x.n == 1 ? x.whole : slot + x.lr * D;
-    const float* const stats = x.n == 1 ? x.whole + D : slot + x.rows * D + x.lr;
-    const float pm = stats[0], pl = stats[x.n == 1 ? 1 : x.rows];
+    const RowPieces x = is_common ? common : own;
+    const int piece = is_common ? mine : mine - common.n, rows = is_common ? a.rows[kCommon] : a.rows[kOwn];
+    const float* const slot = (is_common ? a.slots[kCommon] : a.slots[kOwn]) + (int64_t)(2 * (x.first + piece) + (piece == 0 ? 1 : 0)) * slot_floats(D, rows);
+    const float* const whole = (is_common ? a.whole[kCommon] : a.whole[kOwn]) + (int64_t)unit * (D + 4);
+    const float* const sums = x.n == 1 ? whole : slot + x.lr * D;
+    const float* const stats = x.n == 1 ? whole + D : slot + rows * D + x.lr;
+    const float pm = stats[0], pl = stats[x.n == 1 ? 1 : rows];
     const float top = fmaxf(m, wave_maxf(pm)), before = __builtin_amdgcn_exp2f(m - top);
     const float f = p0 + lane < all ? __builtin_amdgcn_exp2f(pm - top) : 0.f;
     m = top;
@@ -607,7 +589,7 @@ SharedPlan plan_shared(const CacheView& c, int32_t n_seqs, int32_t n_groups, int
   return p;
 }
 // Scratch: for any number of groups up to n_seqs.  The slots of common parts have room for the rows of one group.
-struct SharedSpace { size_t parts[2], before[2], slots[2], whole[2], bytes; };
+struct SharedSpace { size_t parts[2], before[2], pieces[2], slots[2], whole[2], bytes; };
 // Many rows of a sequence are attention of many rows already: the matrix units bound it, and the bytes that sequences share are read from the L2s.  Every sequence is worked by itself then.
 bool by_itself(const CacheView& c, int32_t n_seqs, int32_t tq, int32_t hq) { return (int64_t)tq * (hq / c.hkv) > (int64_t)64 * n_seqs; }
 SharedSpace shared_space(const CacheView& c, int head_dim, int32_t n_seqs, int32_t tq, int32_t hq) {
@@ -618,6 +600,7 @@ SharedSpace shared_space(const CacheView& c, int head_dim, int32_t n_seqs, int32
   for (int kind = 0; kind < 2; ++kind) {
     s.parts[kind] = take((size_t)n_seqs * sizeof(Entry));
     s.before[kind] = take(((size_t)n_seqs + 2) * 4);
+    s.pieces[kind] = take((size_t)tq * hq * sizeof(RowPieces));
     s.slots[kind] = take((size_t)2 * p.sharers[kind] * slot_floats(head_dim, p.rows[kind]) * 4);
     s.whole[kind] = take((size_t)tq * hq * (head_dim + 4) * 4);
   }
@@ -722,6 +705,7 @@ extern "C" int fcp_cache_attn_shared(const fcp_cache* cache, const void* q, int6
   a.tables = {reinterpret_cast<Entry*>(at + space.parts[kCommon]), reinterpret_cast<Entry*>(at + space.parts[kOwn]), reinterpret_cast<int32_t*>(at + space.before[kCommon]),
               reinterpret_cast<int32_t*>(at + space.before[kOwn])};
   for (int kind = 0; kind < 2; ++kind) {
+    a.pieces[kind] = reinterpret_cast<RowPieces*>(at + space.pieces[kind]);
     a.slots[kind] = reinterpret_cast<float*>(at + space.slots[kind]);
     a.whole[kind] = reinterpret_cast<float*>(at + space.whole[kind]);
     a.rows[kind] = p.rows[kind];
