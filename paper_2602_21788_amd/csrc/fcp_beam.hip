@@ -4,7 +4,7 @@
 // logarithm is needed only to put beams beside each other.  Candidates of different beams can lie as near as they like: sums and scores are held in 64 bits.
 //
 // First launch: a block takes a chunk of a row, 32 neighbouring logits a thread (8 where there are few rows), which stay in registers for three looks:
-//   * the greatest of every four threads, 64 in all; the keep-th greatest of those 64, T: at least `keep` logits of the chunk are T or more;
+//   * the greatest of every four threads, 64 in all; the keep-th greatest of those 64, T, found bit by bit: at least `keep` logits of the chunk are T or more;
 //   * the sum of exp(x - greatest): the exponential as a polynomial in 64 bits, which this card multiplies as fast as 32;
 //   * logits beyond T, and those equal to it in T's four threads and earlier ones, go to a list in LDS.  Whatever the logits, they lie in `keep` groups of four threads, which bounds
 //     the list; as a rule it is little longer than `keep`.  The list is put in order by counting, where it is long by a bitonic sort.
@@ -46,25 +46,30 @@ __device__ inline uint64_t order_of(double x) {
 }
 __device__ inline double score_of(uint64_t order) { return __longlong_as_double((long long)(order >> 63 ? order & ~((uint64_t)1 << 63) : ~order)); }
 
-// A logit as it counts: NaN as -inf, +inf as the largest finite value, -0 as 0.
-__device__ inline float counted(float x) { return (x != x ? -INFINITY : fminf(x, FLT_MAX)) + 0.f; }
+// A constant in scalar registers: an instruction of the vector unit takes one, and the compiler would rather move it to vector registers every time.
+__device__ inline double scalar(double x) { asm volatile("" : "+s"(x)); return x; }
 
 // exp(x - top), x <= top: 2^n times a polynomial in f, n + f = (x - top) log2(e), |f| <= 1/2.  The coefficients are a least-squares fit on Chebyshev nodes with weights 2^-f; the
-// relative error is at most 4.1e-11, which is how far the logarithm of a sum may be off.  2^-1000 stands for everything below it.
-__device__ inline double exp_below(float x, double top) {
-  constexpr double kLog2E = 1.4426950408889634074, kShift = 6755399441055744.0;       // 1.5 * 2^52: the sum's low bits are the rounded number
-  const double t = fmax(((double)x - top) * kLog2E, -1000.0), shifted = t + kShift, f = t - (shifted - kShift);
-  double p = 0x1.fde1039ee67bfp-17;
-  p = __builtin_fma(p, f, 0x1.4469d4b220e3bp-13);
-  p = __builtin_fma(p, f, 0x1.5d8a9fcfc7546p-10);
-  p = __builtin_fma(p, f, 0x1.3b29dcb134a69p-7);
-  p = __builtin_fma(p, f, 0x1.c6b08a80840e9p-5);
-  p = __builtin_fma(p, f, 0x1.ebfbe0a416e10p-3);
-  p = __builtin_fma(p, f, 0x1.62e42ff12cfc5p-1);
-  p = __builtin_fma(p, f, 0x1.ffffffffac502p-1);
-  const int n = (int)(uint32_t)__double_as_longlong(shifted);
-  return __longlong_as_double(__double_as_longlong(p) + ((long long)n << 52));
-}
+// relative error is at most 4.1e-11, which is how far the logarithm of a sum may be off.  2^-1000 stands for everything below it, and for NaN.
+// Far: |top| is so large that its product with log2(e) must not be rounded before the difference.
+struct ExpBelow {
+  double log2e = scalar(1.4426950408889634074), shift = scalar(6755399441055744.0);      // 1.5 * 2^52: the sum's low bits are the rounded number
+  double c[8] = {scalar(0x1.ffffffffac502p-1), scalar(0x1.62e42ff12cfc5p-1), scalar(0x1.ebfbe0a416e10p-3), scalar(0x1.c6b08a80840e9p-5), scalar(0x1.3b29dcb134a69p-7),
+                 scalar(0x1.5d8a9fcfc7546p-10), scalar(0x1.4469d4b220e3bp-13), 0x1.fde1039ee67bfp-17};
+  double top, minus_top;
+  __device__ explicit ExpBelow(float t) : top(t), minus_top(-(double)t * 1.4426950408889634074) {}
+  template <bool Far>
+  __device__ double of(float x) const {
+    const double t = fmax(Far ? ((double)x - top) * log2e : __builtin_fma((double)x, log2e, minus_top), -1000.0), shifted = t + shift, f = t - (shifted - shift);
+    double p = c[7];
+#pragma unroll
+    for (int i = 6; i >= 0; --i) p = __builtin_fma(p, f, c[i]);
+    // 2^n: added to the exponent, in the upper word
+    u32x2 u = __builtin_bit_cast(u32x2, p);
+    u[1] += __builtin_bit_cast(u32x2, shifted)[0] << 20;
+    return __builtin_bit_cast(double, u);
+  }
+};
 
 __device__ inline double sum_of_wave(double x) {
 #pragma unroll
@@ -91,18 +96,22 @@ __device__ inline void load_row(const T* from, int there, float (&v)[E]) {
 #pragma unroll
     for (int i = 0; i < E; ++i) v[i] = i < there ? (float)from[i] : -INFINITY;
   }
-#pragma unroll
-  for (int i = 0; i < E; ++i) v[i] = counted(v[i]);
 }
 
-// One of the 64 elements that a wave holds, a lane each: the rank-th greatest, of equal ones the lowest lane first.  Returns its lane.
-template <class Greater>
-__device__ inline int lane_of_rank(int rank, Greater greater) {
-  const int lane = threadIdx.x & 63;
-  int above = 0;
-#pragma unroll 8
-  for (int j = 0; j < 64; ++j) above += greater(j, lane);
-  return __builtin_ctzll(__ballot(above == rank));
+__device__ inline float wave_top(float x) {
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) x = fmaxf(x, __shfl_xor(x, d));
+  return x;
+}
+
+// Of the 64 numbers that a wave holds, a lane each, the rank-th greatest (from 1), bit for bit from the top: as many as are set from the lowest one on are known.
+__device__ inline uint32_t greatest(uint32_t x, int rank, int lowest_bit) {
+  uint32_t found = 0;
+  for (int b = 31; b >= lowest_bit; --b) {
+    const uint32_t next = found | 1u << b;
+    if (__popcll(__ballot(x >= next)) >= rank) found = next;
+  }
+  return found;
 }
 
 // Puts list[0 .. n - 1], different from each other, in order, greatest first, as far as the first `keep`; the list has room for the next power of two.  Every thread calls.
@@ -154,32 +163,46 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(BeamArgs a) {
   const int first = chunk * (kThreads * E) + (int)threadIdx.x * E;
   float v[E];
   load_row<T, E>(static_cast<const T*>(a.logits) + (int64_t)row * a.row + first, a.vocab - first, v);
-  float top = v[0];
+  float top = -INFINITY;
 #pragma unroll
-  for (int i = 1; i < E; ++i) top = fmaxf(top, v[i]);
+  for (int i = 0; i < E; ++i) top = fmaxf(top, v[i]);      // (NaN is passed over)
   top = fmaxf(top, __shfl_xor(top, 1));
   top = fmaxf(top, __shfl_xor(top, 2));
   if (threadIdx.x % kPerGroup == 0) groups[threadIdx.x / kPerGroup] = top;
   if (threadIdx.x == 0) listed = 0;
   __syncthreads();
-  const float mine = groups[lane];
-  const int at = lane_of_rank(a.keep - 1, [&](int j, int i) {
-    const float other = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(mine), j));
-    return other > mine || (other == mine && j < i);
-  });
-  const float border = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(mine), at));
-  float most = mine;
+  const float unbounded = groups[lane], mine = fminf(unbounded, FLT_MAX) + 0.f;         // (-0 as 0)
+  const bool infinite = __ballot(unbounded == INFINITY);
+  if (infinite) {                                          // rare
 #pragma unroll
-  for (int d = 32; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
+    for (int i = 0; i < E; ++i) v[i] = v[i] == INFINITY ? FLT_MAX : v[i];
+  }
+  // the keep-th greatest group, of equal ones the lowest first.  (The lower half of a bf16 value is all zeros, in order_of all ones if it is negative.)
+  const uint32_t order = order_of(mine);
+  const bool half = sizeof(T) == 2 && !infinite;
+  uint32_t least = greatest(order, a.keep, half ? 16 : 0);
+  if (half && !(least >> 31)) least |= 0xffffu;
+  uint64_t equal = __ballot(order == least);
+  for (int k = a.keep - (int)__popcll(__ballot(order > least)); k > 1; --k) equal &= equal - 1;
+  const int at = __builtin_ctzll(equal);
+  const float border = value_of(least), most = wave_top(mine);
   double sum = 0;
   if (most > -INFINITY) {
+    const ExpBelow e(most);
+    if (fabsf(most) <= 65536.f) {
 #pragma unroll
-    for (int i = 0; i < E; ++i) sum += exp_below(v[i], (double)most);
-    const float equal = (int)threadIdx.x / kPerGroup <= at ? border : INFINITY;          // the border itself counts in its own group and earlier ones
+      for (int i = 0; i < E; ++i) sum += e.template of<false>(v[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < E; ++i) sum += e.template of<true>(v[i]);
+    }
+    const bool early = (int)threadIdx.x / kPerGroup <= at; // the border itself counts in its own group and earlier ones
 #pragma unroll
     for (int i = 0; i < E; ++i)
-      if ((v[i] > border || v[i] == equal) && v[i] > -INFINITY)
-        list[atomicAdd(&listed, 1)] = (uint64_t)order_of(v[i]) << 32 | (uint32_t)~(first + i);
+      if (__ballot(v[i] >= border)) {
+        const float x = v[i] + 0.f;
+        if ((x > border || (x == border && early)) && x > -INFINITY) list[atomicAdd(&listed, 1)] = (uint64_t)order_of(x) << 32 | (uint32_t)~(first + i);
+      }
   }
   sum = sum_of_wave(sum);
   if (lane == 0) sums[wave] = sum;
@@ -203,21 +226,41 @@ constexpr int kJoined = 8;             // candidates that a thread holds
 __global__ __launch_bounds__(kThreads) void beam_join_kernel(BeamArgs a) {
   extern __shared__ __align__(16) Candidate found[];       // the best so far, then those that may replace them
   __shared__ double lse[FCP_BEAM_MAX_BEAMS];
-  __shared__ Candidate groups[kGroups], best[FCP_BEAM_MAX_KEEP];
+  __shared__ uint32_t groups[kGroups];
+  __shared__ Candidate best[FCP_BEAM_MAX_KEEP];
   __shared__ int32_t listed;
   const int row0 = blockIdx.x * a.beams, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int per_beam = a.chunks * a.keep, all = a.beams * per_beam;      // (below 2^30: 2^24 chunks in all)
+  // what a thread holds of the lists, asked for before the sums are joined: a logit of a beam, or its score where it is done
+  uint64_t key[kJoined];
+  int beam[kJoined];
+  bool over[kJoined];
+  auto ask = [&](int q0) {
+#pragma unroll
+    for (int i = 0; i < kJoined; ++i) {
+      const int q = q0 + i * kThreads + (int)threadIdx.x, b = q < all ? q / per_beam : 0, rest = q - b * per_beam;
+      const float score = a.score[row0 + b];
+      const bool done = a.done && a.done[row0 + b];
+      const bool offers = q < all && score > -INFINITY;
+      const uint64_t k = a.lists[(int64_t)(row0 + b) * per_beam + (q < all ? rest : 0)];
+      beam[i] = b;
+      over[i] = done;
+      key[i] = !offers ? 0 : !done ? k : rest == 0 ? (uint64_t)(uint32_t)~a.end_token | (uint64_t)1 << 32 : 0;
+    }
+  };
+  ask(0);
   for (int b = wave; b < a.beams; b += kThreads / 64) {    // a wave joins the sums of a beam
     const float score = a.score[row0 + b];
     if (!(score > -INFINITY) || (a.done && a.done[row0 + b])) continue;
     const int64_t at = (int64_t)(row0 + b) * a.chunks;
-    float most = -INFINITY;
-    for (int c = lane; c < a.chunks; c += 64) most = fmaxf(most, a.tops[at + c]);
-#pragma unroll
-    for (int d = 32; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
+    float top = lane < a.chunks ? a.tops[at + lane] : -INFINITY;
+    const double first = lane < a.chunks ? a.sums[at + lane] : 0;
+    for (int c = lane + 64; c < a.chunks; c += 64) top = fmaxf(top, a.tops[at + c]);
+    const float most = wave_top(top);
     double sum = 0;
     for (int c = lane; c < a.chunks; c += 64) {
-      const float top = a.tops[at + c];
-      if (top > -INFINITY) sum += a.sums[at + c] * exp((double)top - (double)most);
+      const float here = c < 64 && a.chunks <= 64 ? top : a.tops[at + c];
+      if (here > -INFINITY) sum += (c < 64 ? first : a.sums[at + c]) * exp((double)here - (double)most);
     }
     sum = sum_of_wave(sum);
     if (lane == 0) lse[b] = (double)most + log(sum);
@@ -225,47 +268,28 @@ __global__ __launch_bounds__(kThreads) void beam_join_kernel(BeamArgs a) {
   if (threadIdx.x == 0) listed = 0;
   __syncthreads();
   const Candidate none = {0, 0};
-  const int per_beam = a.chunks * a.keep;
-  const int64_t all = (int64_t)a.beams * per_beam;
   int kept = 0;
-  for (int64_t q0 = 0; q0 < all; q0 += kThreads * kJoined) {
+  for (int q0 = 0; q0 < all; q0 += kThreads * kJoined) {
     Candidate c[kJoined];
-    Candidate top = none;
+    uint32_t top = 0;
 #pragma unroll
     for (int i = 0; i < kJoined; ++i) {
-      const int64_t q = q0 + (int64_t)i * kThreads + threadIdx.x;
-      c[i] = none;
-      if (q < all) {
-        const int b = (int)(q / per_beam), rest = (int)(q - (int64_t)b * per_beam);
-        const float score = a.score[row0 + b];
-        if (score > -INFINITY) {
-          if (a.done && a.done[row0 + b]) {
-            if (rest == 0) c[i] = {order_of((double)score), (uint64_t)(uint32_t)~b << 32 | (uint32_t)~a.end_token};
-          } else {
-            const uint64_t k = a.lists[(int64_t)(row0 + b) * per_beam + rest];
-            if (k) c[i] = {order_of((double)score + ((double)value_of((uint32_t)(k >> 32)) - lse[b])), (uint64_t)(uint32_t)~b << 32 | (uint32_t)k};
-          }
-        }
-      }
-      if (greater(c[i], top)) top = c[i];
+      const double score = a.score[row0 + beam[i]];
+      const double s = over[i] ? score : score + ((double)value_of((uint32_t)(key[i] >> 32)) - lse[beam[i]]);
+      c[i] = key[i] ? Candidate{order_of(s), (uint64_t)(uint32_t)~beam[i] << 32 | (uint32_t)key[i]} : none;
+      top = max(top, (uint32_t)(c[i].score >> 32));
     }
-#pragma unroll
-    for (int d = 1; d < kPerGroup; d *= 2) {
-      const Candidate other = {(uint64_t)__shfl_xor((unsigned long long)top.score, d), (uint64_t)__shfl_xor((unsigned long long)top.place, d)};
-      if (greater(other, top)) top = other;
-    }
+    if (q0 + kThreads * kJoined < all) ask(q0 + kThreads * kJoined);
+    // The border, by the upper words of the scores' orders (20 bits of a mantissa): whatever reaches it may be among the best.
+    top = max(top, (uint32_t)__shfl_xor((int)top, 1));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 2));
     if (threadIdx.x % kPerGroup == 0) groups[threadIdx.x / kPerGroup] = top;
     __syncthreads();
-    // (candidates differ from each other, but for those that are none)
-    const Candidate mine = groups[lane];
-    const int at = lane_of_rank(a.keep - 1, [&](int j, int i) {
-      const Candidate other = groups[j];
-      return greater(other, mine) || (other.score == mine.score && other.place == mine.place && j < i);
-    });
-    const Candidate border = groups[at];
+    const uint32_t border = max(greatest(groups[lane], a.keep, 0), 1u);
 #pragma unroll
     for (int i = 0; i < kJoined; ++i)
-      if (c[i].score && !greater(border, c[i])) found[kept + atomicAdd(&listed, 1)] = c[i];
+      if (__ballot((uint32_t)(c[i].score >> 32) >= border))
+        if ((uint32_t)(c[i].score >> 32) >= border) found[kept + atomicAdd(&listed, 1)] = c[i];
     __syncthreads();
     const int n = kept + listed;
     best_of(found, n, a.keep, none, [](const Candidate& x, const Candidate& y) { return greater(x, y); }, [&](int i, const Candidate& k) { best[i] = k; });
@@ -359,10 +383,10 @@ extern "C" int fcp_beam_select(const void* logits, int32_t type, int64_t logits_
   if (int rc = p.each == 32 ? (bf16 ? launch_rows<__bf16, 32>(a, p, st) : launch_rows<float, 32>(a, p, st))
                             : (bf16 ? launch_rows<__bf16, 8>(a, p, st) : launch_rows<float, 8>(a, p, st)))
     return rc;
-  // candidates of a block's look lie in `keep` groups of four threads; the best so far beside them
+  // all candidates of a block's look may have scores whose upper words are alike; the best so far beside them
   static std::atomic<uint64_t> raised;
-  int room = 1;
-  while (room < keep + keep * kPerGroup * kJoined) room *= 2;
+  int room = 2 * kThreads * kJoined;
+  static_assert(FCP_BEAM_MAX_KEEP <= kThreads * kJoined, "both fit");
   const int bytes = room * (int)sizeof(Candidate);
   if (bytes > 48 * 1024)
     if (int rc = raise_lds_limit(reinterpret_cast<const void*>(beam_join_kernel), bytes, raised)) return rc;
