@@ -599,7 +599,7 @@ int fcp_cache_attn_shared(const fcp_cache* cache, const void* q, int64_t q_row, 
  *   parent, token [n_prompts, keep] int32, new_score [n_prompts, keep] fp32, new_done [n_prompts, keep] bytes (or NULL): device out, best first.  parent: the row of the beam, what
  *   fcp_cache_fork takes; new_done: the beam is done, or token is end_token.  Where there are fewer candidates: -1, -1, -inf, 0.  Outputs lie apart from inputs.
  *   scratch: device, 256-byte aligned, fcp_beam_scratch_bytes (0 and fcp_last_error for arguments that the call would refuse); contents on entry irrelevant
- * Limits (FCP_ERR_UNSUPPORTED): beams, keep, vocab up to FCP_BEAM_MAX_BEAMS, FCP_BEAM_MAX_KEEP, 2^30; fewer than 2^24 chunks of 2048 logits of a row.
+ * Limits (FCP_ERR_UNSUPPORTED): beams, keep, vocab up to FCP_BEAM_MAX_BEAMS, FCP_BEAM_MAX_KEEP, 2^30; fewer than 2^24 chunks of 8192 logits of a row.
  */
 #define FCP_BEAM_MAX_BEAMS 256
 #define FCP_BEAM_MAX_KEEP 64

@@ -30,8 +30,7 @@ struct BeamArgs {
   float* new_score;
   uint8_t* new_done;
   uint64_t* lists;                     // [rows][chunks][keep]: ordered logit, then ~token; 0: none
-  double* sums;                        // [rows][chunks]: sum of exp(x - greatest)
-  float* tops;                         // [rows][chunks]: greatest logit, -inf: none
+  double* sums;                        // [rows][chunks]: sum of exp(x - reference), reference; a sum of 0: no logits
 };
 
 // Integers that order floats: greater value, greater integer (never 0).  No NaN, no -0.
@@ -49,25 +48,45 @@ __device__ inline double score_of(uint64_t order) { return __longlong_as_double(
 // A constant in scalar registers: an instruction of the vector unit takes one, and the compiler would rather move it to vector registers every time.
 __device__ inline double scalar(double x) { asm volatile("" : "+s"(x)); return x; }
 
-// exp(x - top), x <= top: 2^n times a polynomial in f, n + f = (x - top) log2(e), |f| <= 1/2.  The coefficients are a least-squares fit on Chebyshev nodes with weights 2^-f; the
-// relative error is at most 4.1e-11, which is how far the logarithm of a sum may be off.  2^-1000 stands for everything below it, and for NaN.
-// Far: |top| is so large that its product with log2(e) must not be rounded before the difference.
+// exp(x - top), x <= top, but for a factor that is the same for all x: 2^n times a polynomial in f, n + f = x log2(e), |f| <= 1/2, n counted from top's.  The integer part is found in 32 bits
+// (64-bit instructions take twice as long), the fraction in 64.  The coefficients are a least-squares fit on Chebyshev nodes with weights 2^-f; the relative error is at most 4.3e-11, which is how
+// far the logarithm of a sum may be off.  What lies more than 700 below the top, and NaN, counts as 700 below.
+// Far: |top| is so large that x log2(e) has no good integer part in 32 bits; there the difference is formed first.
 struct ExpBelow {
-  double log2e = scalar(1.4426950408889634074), shift = scalar(6755399441055744.0);      // 1.5 * 2^52: the sum's low bits are the rounded number
+  double log2e = scalar(1.4426950408889634074);
   double c[8] = {scalar(0x1.ffffffffac502p-1), scalar(0x1.62e42ff12cfc5p-1), scalar(0x1.ebfbe0a416e10p-3), scalar(0x1.c6b08a80840e9p-5), scalar(0x1.3b29dcb134a69p-7),
                  scalar(0x1.5d8a9fcfc7546p-10), scalar(0x1.4469d4b220e3bp-13), 0x1.fde1039ee67bfp-17};
-  double top, minus_top;
-  __device__ explicit ExpBelow(float t) : top(t), minus_top(-(double)t * 1.4426950408889634074) {}
-  template <bool Far>
-  __device__ double of(float x) const {
-    const double t = fmax(Far ? ((double)x - top) * log2e : __builtin_fma((double)x, log2e, minus_top), -1000.0), shifted = t + shift, f = t - (shifted - shift);
+  static constexpr float kShift = 12582912.f;              // 1.5 * 2^23: a sum's low bits are the rounded number
+  double top;
+  float lowest;
+  int32_t base;                                            // top's integer part, shifted
+  __device__ explicit ExpBelow(float t) : top(t), lowest(t - 700.f), base(__float_as_int(__builtin_fmaf(t, 1.44269504f, kShift))) {}
+  // 2^n p(f); n: shifted
+  __device__ double scaled(double f, int32_t n) const {
     double p = c[7];
 #pragma unroll
     for (int i = 6; i >= 0; --i) p = __builtin_fma(p, f, c[i]);
-    // 2^n: added to the exponent, in the upper word
     u32x2 u = __builtin_bit_cast(u32x2, p);
-    u[1] += __builtin_bit_cast(u32x2, shifted)[0] << 20;
+    u[1] += (uint32_t)n << 20;                             // (added to the exponent, in the upper word)
     return __builtin_bit_cast(double, u);
+  }
+  template <bool Far>
+  __device__ double of(float x) const {
+    if constexpr (Far) {
+      return of_difference((double)x - top);
+    } else {
+      x = fmaxf(x, lowest);
+      const float shifted = __builtin_fmaf(x, 1.44269504f, kShift);
+      return scaled(__builtin_fma((double)x, log2e, -(double)(shifted - kShift)), __float_as_int(shifted) - base);
+    }
+  }
+  // Sums of of(x) times exp(reference) are sums of exp(x).
+  template <bool Far>
+  __device__ double reference() const { return Far ? top : (double)(__int_as_float(base) - kShift) * 0.69314718055994530942; }
+  // exp(d), d <= 0
+  __device__ double of_difference(double d) const {
+    const double t = fmax(d, -700.0) * log2e, shifted = t + 6755399441055744.0;      // 1.5 * 2^52
+    return scaled(t - (shifted - 6755399441055744.0), (int32_t)__builtin_bit_cast(u32x2, shifted)[0]);
   }
 };
 
@@ -96,6 +115,8 @@ __device__ inline void load_row(const T* from, int there, float (&v)[E]) {
 #pragma unroll
     for (int i = 0; i < E; ++i) v[i] = i < there ? (float)from[i] : -INFINITY;
   }
+#pragma unroll
+  for (int i = 0; i < E; ++i) v[i] = __builtin_canonicalizef(v[i]);      // (no signalling NaN: each fmaxf would see to that anew)
 }
 
 __device__ inline float wave_top(float x) {
@@ -115,9 +136,9 @@ __device__ inline uint32_t greatest(uint32_t x, int rank, int lowest_bit) {
 }
 
 // Puts list[0 .. n - 1], different from each other, in order, greatest first, as far as the first `keep`; the list has room for the next power of two.  Every thread calls.
-template <class K, class Greater, class Out>
+template <int Threads, class K, class Greater, class Out>
 __device__ inline void best_of(K* list, int n, int keep, const K& least, Greater greater, Out out) {
-  if (n <= kThreads) {
+  if (n <= Threads) {
     if ((int)threadIdx.x < n) {
       const K mine = list[threadIdx.x];
       int above = 0;
@@ -129,11 +150,11 @@ __device__ inline void best_of(K* list, int n, int keep, const K& least, Greater
   }
   int size = 1;
   while (size < n) size *= 2;
-  for (int i = n + threadIdx.x; i < size; i += kThreads) list[i] = least;
+  for (int i = n + threadIdx.x; i < size; i += Threads) list[i] = least;
   __syncthreads();
   for (int run = 2; run <= size; run *= 2)
     for (int d = run / 2; d > 0; d /= 2) {
-      for (int i = threadIdx.x; i < size / 2; i += kThreads) {
+      for (int i = threadIdx.x; i < size / 2; i += Threads) {
         const int a = 2 * i - (i & (d - 1)), b = a + d;    // (the pair's lower place has the bit d clear)
         const K x = list[a], y = list[b];
         const bool falling = (a & run) == 0;
@@ -141,7 +162,7 @@ __device__ inline void best_of(K* list, int n, int keep, const K& least, Greater
       }
       __syncthreads();
     }
-  for (int i = threadIdx.x; i < min(keep, n); i += kThreads) out(i, list[i]);
+  for (int i = threadIdx.x; i < min(keep, n); i += Threads) out(i, list[i]);
 }
 
 // Room of the list of a block whose threads hold E elements: those of `keep` groups, and a power of two for the sort.
@@ -154,7 +175,10 @@ __host__ __device__ constexpr int list_room(int keep, int E) {
 template <class T, int E>
 __global__ __launch_bounds__(kThreads) void beam_rows_kernel(BeamArgs a) {
   extern __shared__ __align__(16) uint64_t list[];
+  constexpr int kStaged = 8;           // threads of a wave whose logits are looked at together
   __shared__ float groups[kGroups];
+  __shared__ __align__(16) float staged[kThreads / 64][kStaged * E];
+  __shared__ int32_t staged_by[kThreads / 64][kStaged];
   __shared__ double sums[kThreads / 64];
   __shared__ int32_t listed;
   const int row = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -166,6 +190,7 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(BeamArgs a) {
   float top = -INFINITY;
 #pragma unroll
   for (int i = 0; i < E; ++i) top = fmaxf(top, v[i]);      // (NaN is passed over)
+  const float own_top = fminf(top, FLT_MAX);
   top = fmaxf(top, __shfl_xor(top, 1));
   top = fmaxf(top, __shfl_xor(top, 2));
   if (threadIdx.x % kPerGroup == 0) groups[threadIdx.x / kPerGroup] = top;
@@ -186,34 +211,48 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(BeamArgs a) {
   for (int k = a.keep - (int)__popcll(__ballot(order > least)); k > 1; --k) equal &= equal - 1;
   const int at = __builtin_ctzll(equal);
   const float border = value_of(least), most = wave_top(mine);
-  double sum = 0;
+  double sum = 0, reference = 0;
   if (most > -INFINITY) {
     const ExpBelow e(most);
-    if (fabsf(most) <= 65536.f) {
+    const bool far = fabsf(most) > 1024.f;
+    reference = far ? e.template reference<true>() : e.template reference<false>();
+    if (!far) {
 #pragma unroll
       for (int i = 0; i < E; ++i) sum += e.template of<false>(v[i]);
     } else {
 #pragma unroll
       for (int i = 0; i < E; ++i) sum += e.template of<true>(v[i]);
     }
-    const bool early = (int)threadIdx.x / kPerGroup <= at; // the border itself counts in its own group and earlier ones
+    // Few threads have something for the list: the wave looks at all logits of eight of them at once.
+    for (uint64_t who = __ballot(own_top >= border); who;) {
+      const int place = (int)__popcll(who & (((uint64_t)1 << lane) - 1)), n = min((int)__popcll(who), kStaged);
+      if ((who >> lane & 1) && place < kStaged) {
 #pragma unroll
-    for (int i = 0; i < E; ++i)
-      if (__ballot(v[i] >= border)) {
-        const float x = v[i] + 0.f;
-        if ((x > border || (x == border && early)) && x > -INFINITY) list[atomicAdd(&listed, 1)] = (uint64_t)order_of(x) << 32 | (uint32_t)~(first + i);
+        for (int i = 0; i < E; i += 4) *reinterpret_cast<f32x4*>(&staged[wave][place * E + i]) = f32x4{v[i], v[i + 1], v[i + 2], v[i + 3]};
+        staged_by[wave][place] = threadIdx.x;
       }
+      wave_exchange();
+      for (int j = lane; j < n * E; j += 64) {
+        const float x = staged[wave][j] + 0.f;
+        const int by = staged_by[wave][j / E];
+        // (the border itself counts in its own group and earlier ones)
+        if ((x > border || (x == border && by / kPerGroup <= at)) && x > -INFINITY)
+          list[atomicAdd(&listed, 1)] = (uint64_t)order_of(x) << 32 | (uint32_t)~(chunk * (kThreads * E) + by * E + j % E);
+      }
+      wave_exchange();
+      for (int i = 0; i < n; ++i) who &= who - 1;
+    }
   }
   sum = sum_of_wave(sum);
   if (lane == 0) sums[wave] = sum;
   __syncthreads();
   const int n = listed;
   uint64_t* const out = a.lists + (int64_t)blockIdx.x * a.keep;
-  best_of(list, n, a.keep, (uint64_t)0, [](uint64_t x, uint64_t y) { return x > y; }, [&](int i, uint64_t k) { out[i] = k; });
+  best_of<kThreads>(list, n, a.keep, (uint64_t)0, [](uint64_t x, uint64_t y) { return x > y; }, [&](int i, uint64_t k) { out[i] = k; });
   if ((int)threadIdx.x >= n && (int)threadIdx.x < a.keep) out[threadIdx.x] = 0;
   if (threadIdx.x == 0) {
-    a.sums[blockIdx.x] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
-    a.tops[blockIdx.x] = most;
+    a.sums[2 * (int64_t)blockIdx.x] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+    a.sums[2 * (int64_t)blockIdx.x + 1] = reference;
   }
 }
 
@@ -221,14 +260,15 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(BeamArgs a) {
 struct Candidate { uint64_t score, place; };
 __device__ inline bool greater(const Candidate& x, const Candidate& y) { return x.score > y.score || (x.score == y.score && x.place > y.place); }
 
-constexpr int kJoined = 8;             // candidates that a thread holds
+constexpr int kJoinThreads = 1024, kJoined = 2;            // candidates that a thread holds
 
-__global__ __launch_bounds__(kThreads) void beam_join_kernel(BeamArgs a) {
+__global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a) {
   extern __shared__ __align__(16) Candidate found[];       // the best so far, then those that may replace them
   __shared__ double lse[FCP_BEAM_MAX_BEAMS];
   __shared__ uint32_t groups[kGroups];
   __shared__ Candidate best[FCP_BEAM_MAX_KEEP];
   __shared__ int32_t listed;
+  constexpr int kOfGroup = kJoinThreads / kGroups;
   const int row0 = blockIdx.x * a.beams, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int per_beam = a.chunks * a.keep, all = a.beams * per_beam;      // (below 2^30: 2^24 chunks in all)
   // what a thread holds of the lists, asked for before the sums are joined: a logit of a beam, or its score where it is done
@@ -238,7 +278,7 @@ __global__ __launch_bounds__(kThreads) void beam_join_kernel(BeamArgs a) {
   auto ask = [&](int q0) {
 #pragma unroll
     for (int i = 0; i < kJoined; ++i) {
-      const int q = q0 + i * kThreads + (int)threadIdx.x, b = q < all ? q / per_beam : 0, rest = q - b * per_beam;
+      const int q = q0 + i * kJoinThreads + (int)threadIdx.x, b = q < all ? q / per_beam : 0, rest = q - b * per_beam;
       const float score = a.score[row0 + b];
       const bool done = a.done && a.done[row0 + b];
       const bool offers = q < all && score > -INFINITY;
@@ -249,27 +289,26 @@ __global__ __launch_bounds__(kThreads) void beam_join_kernel(BeamArgs a) {
     }
   };
   ask(0);
-  for (int b = wave; b < a.beams; b += kThreads / 64) {    // a wave joins the sums of a beam
+  for (int b = wave; b < a.beams; b += kJoinThreads / 64) {    // a wave joins the sums of a beam
     const float score = a.score[row0 + b];
     if (!(score > -INFINITY) || (a.done && a.done[row0 + b])) continue;
-    const int64_t at = (int64_t)(row0 + b) * a.chunks;
-    float top = lane < a.chunks ? a.tops[at + lane] : -INFINITY;
-    const double first = lane < a.chunks ? a.sums[at + lane] : 0;
-    for (int c = lane + 64; c < a.chunks; c += 64) top = fmaxf(top, a.tops[at + c]);
-    const float most = wave_top(top);
-    double sum = 0;
-    for (int c = lane; c < a.chunks; c += 64) {
-      const float here = c < 64 && a.chunks <= 64 ? top : a.tops[at + c];
-      if (here > -INFINITY) sum += (c < 64 ? first : a.sums[at + c]) * exp((double)here - (double)most);
-    }
+    const double* const sums = a.sums + 2 * (int64_t)(row0 + b) * a.chunks;
+    double most = -INFINITY, sum = 0;
+    for (int c = lane; c < a.chunks; c += 64)
+      if (sums[2 * c] > 0) most = fmax(most, sums[2 * c + 1]);
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) most = fmax(most, __shfl_xor(most, d));
+    const ExpBelow e(0.f);
+    for (int c = lane; c < a.chunks; c += 64)
+      if (sums[2 * c] > 0) sum += sums[2 * c] * e.of_difference(sums[2 * c + 1] - most);
     sum = sum_of_wave(sum);
-    if (lane == 0) lse[b] = (double)most + log(sum);
+    if (lane == 0) lse[b] = most + log(sum);
   }
   if (threadIdx.x == 0) listed = 0;
   __syncthreads();
   const Candidate none = {0, 0};
   int kept = 0;
-  for (int q0 = 0; q0 < all; q0 += kThreads * kJoined) {
+  for (int q0 = 0; q0 < all; q0 += kJoinThreads * kJoined) {
     Candidate c[kJoined];
     uint32_t top = 0;
 #pragma unroll
@@ -279,11 +318,11 @@ __global__ __launch_bounds__(kThreads) void beam_join_kernel(BeamArgs a) {
       c[i] = key[i] ? Candidate{order_of(s), (uint64_t)(uint32_t)~beam[i] << 32 | (uint32_t)key[i]} : none;
       top = max(top, (uint32_t)(c[i].score >> 32));
     }
-    if (q0 + kThreads * kJoined < all) ask(q0 + kThreads * kJoined);
+    if (q0 + kJoinThreads * kJoined < all) ask(q0 + kJoinThreads * kJoined);
     // The border, by the upper words of the scores' orders (20 bits of a mantissa): whatever reaches it may be among the best.
-    top = max(top, (uint32_t)__shfl_xor((int)top, 1));
-    top = max(top, (uint32_t)__shfl_xor((int)top, 2));
-    if (threadIdx.x % kPerGroup == 0) groups[threadIdx.x / kPerGroup] = top;
+#pragma unroll
+    for (int d = 1; d < kOfGroup; d *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, d));
+    if (threadIdx.x % kOfGroup == 0) groups[threadIdx.x / kOfGroup] = top;
     __syncthreads();
     const uint32_t border = max(greatest(groups[lane], a.keep, 0), 1u);
 #pragma unroll
@@ -292,7 +331,7 @@ __global__ __launch_bounds__(kThreads) void beam_join_kernel(BeamArgs a) {
         if ((uint32_t)(c[i].score >> 32) >= border) found[kept + atomicAdd(&listed, 1)] = c[i];
     __syncthreads();
     const int n = kept + listed;
-    best_of(found, n, a.keep, none, [](const Candidate& x, const Candidate& y) { return greater(x, y); }, [&](int i, const Candidate& k) { best[i] = k; });
+    best_of<kJoinThreads>(found, n, a.keep, none, [](const Candidate& x, const Candidate& y) { return greater(x, y); }, [&](int i, const Candidate& k) { best[i] = k; });
     __syncthreads();
     kept = min(n, a.keep);
     if ((int)threadIdx.x < kept) found[threadIdx.x] = best[threadIdx.x];
@@ -311,24 +350,26 @@ __global__ __launch_bounds__(kThreads) void beam_join_kernel(BeamArgs a) {
   }
 }
 
-// How a call is divided: chunks of 8192 logits where there are enough for every CU, else of 2048.
+// How a call is divided: as many neighbouring logits a thread as leave four blocks, or two, for every CU; 8 where there are fewer.  (64 a thread: room for the list's worst case leaves one block a CU with
+// many kept.)
 struct BeamPlan { int32_t each, chunks; int64_t blocks; };
-BeamPlan plan_beam(int64_t rows, int32_t vocab) {
+BeamPlan plan_beam(int64_t rows, int32_t vocab, int32_t keep) {
+  auto chunks = [&](int64_t each) { return (vocab + kThreads * each - 1) / (kThreads * each); };
   BeamPlan p;
-  p.each = rows * ((vocab + (int64_t)kThreads * 32 - 1) / (kThreads * 32)) >= 512 ? 32 : 8;
-  p.chunks = (int32_t)((vocab + (int64_t)kThreads * p.each - 1) / (kThreads * p.each));
+  p.each = keep <= 16 && rows * chunks(64) >= 1024 ? 64 : rows * chunks(32) >= 512 ? 32 : 8;
+  p.chunks = (int32_t)chunks(p.each);
   p.blocks = rows * p.chunks;
   return p;
 }
-size_t beam_bytes(const BeamPlan& p, int32_t keep) { return pad_to((size_t)p.blocks * keep * 8, 256) + pad_to((size_t)p.blocks * 8, 256) + pad_to((size_t)p.blocks * 4, 256); }
+size_t beam_bytes(const BeamPlan& p, int32_t keep) { return pad_to((size_t)p.blocks * keep * 8, 256) + pad_to((size_t)p.blocks * 16, 256); }
 
 int check_beam(const char* who, int32_t n_prompts, int32_t beams, int32_t vocab, int32_t keep) {
   if (n_prompts < 0 || beams < 1 || vocab < 1 || keep < 1) return fail(FCP_ERR_INVALID_ARG, "%s: n_prompts must not be negative, beams, vocab and keep at least 1", who);
   if (beams > FCP_BEAM_MAX_BEAMS || keep > FCP_BEAM_MAX_KEEP)
     return fail(FCP_ERR_UNSUPPORTED, "%s: %d beams, %d kept; at most %d and %d", who, beams, keep, FCP_BEAM_MAX_BEAMS, FCP_BEAM_MAX_KEEP);
   if (vocab > 1 << 30) return fail(FCP_ERR_UNSUPPORTED, "%s: a vocabulary of more than 2^30", who);
-  if ((int64_t)n_prompts * beams > INT32_MAX || !fits_axis(plan_beam((int64_t)n_prompts * beams, vocab).blocks, kThreads))
-    return fail(FCP_ERR_UNSUPPORTED, "%s: 2^24 chunks of logits or more", who);
+  if ((int64_t)n_prompts * beams > INT32_MAX || !fits_axis((int64_t)n_prompts * beams * (((int64_t)vocab + 8191) / 8192), kThreads))
+    return fail(FCP_ERR_UNSUPPORTED, "%s: 2^24 chunks of 8192 logits or more", who);
   return FCP_OK;
 }
 
@@ -336,7 +377,7 @@ template <class T, int E>
 int launch_rows(const BeamArgs& a, const BeamPlan& p, hipStream_t st) {
   static std::atomic<uint64_t> raised;
   const int bytes = list_room(a.keep, E) * 8;
-  if (bytes > 60 * 1024)
+  if (bytes > 48 * 1024)
     if (int rc = raise_lds_limit(reinterpret_cast<const void*>(beam_rows_kernel<T, E>), bytes, raised)) return rc;
   beam_rows_kernel<T, E><<<dim3((unsigned)p.blocks), dim3(kThreads), bytes, st>>>(a);
   FCP_HIP_CHECK(hipGetLastError());
@@ -350,7 +391,7 @@ extern "C" size_t fcp_beam_scratch_bytes(int32_t n_prompts, int32_t beams, int32
   using namespace fcp;
   clear_error();
   if (check_beam("fcp_beam_scratch_bytes", n_prompts, beams, vocab, keep)) return 0;
-  const size_t n = beam_bytes(plan_beam((int64_t)n_prompts * beams, vocab), keep);
+  const size_t n = beam_bytes(plan_beam((int64_t)n_prompts * beams, vocab, keep), keep);
   return n ? n : 256;
 }
 
@@ -370,27 +411,27 @@ extern "C" int fcp_beam_select(const void* logits, int32_t type, int64_t logits_
     return fail(FCP_ERR_INVALID_ARG, "%s: an argument is not aligned to its type", who);
   if (new_score == score || (new_done && new_done == done)) return fail(FCP_ERR_INVALID_ARG, "%s: outputs must lie apart from inputs", who);
   if (!scratch || (uintptr_t)scratch % 256) return fail(FCP_ERR_INVALID_ARG, "%s: scratch must be 256-byte aligned", who);
-  const BeamPlan p = plan_beam((int64_t)n_prompts * beams, vocab);
+  const BeamPlan p = plan_beam((int64_t)n_prompts * beams, vocab, keep);
   const size_t need = beam_bytes(p, keep);
   if (scratch_bytes < need) return fail(FCP_ERR_CAPACITY, "%s: scratch has %zu bytes, %zu are needed", who, scratch_bytes, need);
   BeamArgs a = {logits, logits_row, n_prompts * beams, beams, vocab, p.chunks, keep, end_token, score, done, parent, token, new_score, new_done};
   char* const at = static_cast<char*>(scratch);
   a.lists = reinterpret_cast<uint64_t*>(at);
   a.sums = reinterpret_cast<double*>(at + pad_to((size_t)p.blocks * keep * 8, 256));
-  a.tops = reinterpret_cast<float*>(at + pad_to((size_t)p.blocks * keep * 8, 256) + pad_to((size_t)p.blocks * 8, 256));
   hipStream_t st = static_cast<hipStream_t>(stream);
   const bool bf16 = type == FCP_BF16;
-  if (int rc = p.each == 32 ? (bf16 ? launch_rows<__bf16, 32>(a, p, st) : launch_rows<float, 32>(a, p, st))
+  if (int rc = p.each == 64 ? (bf16 ? launch_rows<__bf16, 64>(a, p, st) : launch_rows<float, 64>(a, p, st))
+             : p.each == 32 ? (bf16 ? launch_rows<__bf16, 32>(a, p, st) : launch_rows<float, 32>(a, p, st))
                             : (bf16 ? launch_rows<__bf16, 8>(a, p, st) : launch_rows<float, 8>(a, p, st)))
     return rc;
   // all candidates of a block's look may have scores whose upper words are alike; the best so far beside them
   static std::atomic<uint64_t> raised;
-  int room = 2 * kThreads * kJoined;
-  static_assert(FCP_BEAM_MAX_KEEP <= kThreads * kJoined, "both fit");
+  int room = 2 * kJoinThreads * kJoined;
+  static_assert(FCP_BEAM_MAX_KEEP <= kJoinThreads * kJoined, "both fit");
   const int bytes = room * (int)sizeof(Candidate);
   if (bytes > 48 * 1024)
     if (int rc = raise_lds_limit(reinterpret_cast<const void*>(beam_join_kernel), bytes, raised)) return rc;
-  beam_join_kernel<<<dim3((unsigned)n_prompts), dim3(kThreads), bytes, st>>>(a);
+  beam_join_kernel<<<dim3((unsigned)n_prompts), dim3(kJoinThreads), bytes, st>>>(a);
   FCP_HIP_CHECK(hipGetLastError());
   return FCP_OK;
 }
