@@ -7,7 +7,7 @@
 //   * the greatest of every four threads, 64 in all; the keep-th greatest of those 64, T, found bit by bit: at least `keep` logits of the chunk are T or more;
 //   * the sum of exp(x - greatest): the exponential as a polynomial in 64 bits, which this card multiplies as fast as 32;
 //   * logits beyond T, and those equal to it in T's four threads and earlier ones, go to a list in LDS.  Whatever the logits, they lie in `keep` groups of four threads, which bounds
-//     the list; as a rule it is little longer than `keep`.  The list is put in order by counting, where it is long by a bitonic sort.
+//     the list; as a rule it is little longer than `keep`.  The list is put in order by counting, a few hundred at a time.
 // Second launch: a block for each prompt joins the sums and finds the best candidates of all lists the same way.
 #include <float.h>
 
@@ -135,46 +135,36 @@ __device__ inline uint32_t greatest(uint32_t x, int rank, int lowest_bit) {
   return found;
 }
 
-// Puts list[0 .. n - 1], different from each other, in order, greatest first, as far as the first `keep`; the list has room for the next power of two.  Every thread calls.
-template <int Threads, class K, class Greater, class Out>
-__device__ inline void best_of(K* list, int n, int keep, const K& least, Greater greater, Out out) {
-  if (n <= Threads) {
-    if ((int)threadIdx.x < n) {
-      const K mine = list[threadIdx.x];
+// The best `keep` of n elements that differ from each other, in order: best[0 .. min(n, keep) - 1].  Ranks by counting, Threads elements at a time, the best so far among them; at(i): element i.
+// room: Threads elements in LDS.  Every thread calls, best and room are free before, best is complete after.
+template <int Threads, class K, class Greater, class At>
+__device__ inline void best_of(K* best, K* room, int n, int keep, Greater greater, At at) {
+  int kept = 0;
+  for (int from = 0; from < n;) {
+    const int more = min(n - from, Threads - kept), all = kept + more, i = threadIdx.x;
+    K mine;
+    if (i < all) room[i] = mine = i < kept ? best[i] : at(from + i - kept);
+    __syncthreads();
+    if (i < all) {
       int above = 0;
 #pragma unroll 4
-      for (int j = 0; j < n; ++j) above += greater(list[j], mine);
-      if (above < keep) out(above, mine);
+      for (int j = 0; j < all; ++j) above += greater(room[j], mine);
+      if (above < keep) best[above] = mine;
     }
-    return;
+    __syncthreads();
+    kept = min(all, keep);
+    from += more;
   }
-  int size = 1;
-  while (size < n) size *= 2;
-  for (int i = n + threadIdx.x; i < size; i += Threads) list[i] = least;
-  __syncthreads();
-  for (int run = 2; run <= size; run *= 2)
-    for (int d = run / 2; d > 0; d /= 2) {
-      for (int i = threadIdx.x; i < size / 2; i += Threads) {
-        const int a = 2 * i - (i & (d - 1)), b = a + d;    // (the pair's lower place has the bit d clear)
-        const K x = list[a], y = list[b];
-        const bool falling = (a & run) == 0;
-        if (greater(y, x) == falling) { list[a] = y; list[b] = x; }
-      }
-      __syncthreads();
-    }
-  for (int i = threadIdx.x; i < min(keep, n); i += Threads) out(i, list[i]);
 }
 
-// Room of the list of a block whose threads hold E elements: those of `keep` groups, and a power of two for the sort.
-__host__ __device__ constexpr int list_room(int keep, int E) {
-  int n = 1;
-  while (n < keep) n *= 2;
-  return n * kPerGroup * E;
-}
+// Room of the list of a block whose threads hold E elements: those of `keep` groups.
+__host__ __device__ constexpr int list_room(int keep, int E) { return keep * kPerGroup * E; }
 
 template <class T, int E>
 __global__ __launch_bounds__(kThreads) void beam_rows_kernel(BeamArgs a) {
-  extern __shared__ __align__(16) uint64_t list[];
+  extern __shared__ __align__(16) uint16_t list[];         // places in the chunk
+  static_assert(kThreads * E <= 1 << 16, "they fit");
+  __shared__ uint64_t room[kThreads], best[FCP_BEAM_MAX_KEEP];
   constexpr int kStaged = 8;           // threads of a wave whose logits are looked at together
   __shared__ float groups[kGroups];
   __shared__ __align__(16) float staged[kThreads / 64][kStaged * E];
@@ -237,7 +227,7 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(BeamArgs a) {
         const int by = staged_by[wave][j / E];
         // (the border itself counts in its own group and earlier ones)
         if ((x > border || (x == border && by / kPerGroup <= at)) && x > -INFINITY)
-          list[atomicAdd(&listed, 1)] = (uint64_t)order_of(x) << 32 | (uint32_t)~(chunk * (kThreads * E) + by * E + j % E);
+          list[atomicAdd(&listed, 1)] = (uint16_t)(by * E + j % E);
       }
       wave_exchange();
       for (int i = 0; i < n; ++i) who &= who - 1;
@@ -247,9 +237,12 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(BeamArgs a) {
   if (lane == 0) sums[wave] = sum;
   __syncthreads();
   const int n = listed;
-  uint64_t* const out = a.lists + (int64_t)blockIdx.x * a.keep;
-  best_of<kThreads>(list, n, a.keep, (uint64_t)0, [](uint64_t x, uint64_t y) { return x > y; }, [&](int i, uint64_t k) { out[i] = k; });
-  if ((int)threadIdx.x >= n && (int)threadIdx.x < a.keep) out[threadIdx.x] = 0;
+  // (the logits themselves are read again: with them the list would take four times the LDS, and fewer blocks would run at once)
+  const int chunk0 = chunk * (kThreads * E);
+  const T* const x0 = static_cast<const T*>(a.logits) + (int64_t)row * a.row + chunk0;
+  best_of<kThreads>(best, room, n, a.keep, [](uint64_t x, uint64_t y) { return x > y; },
+                    [&](int i) { return (uint64_t)order_of(fminf((float)x0[list[i]], FLT_MAX) + 0.f) << 32 | (uint32_t)~(chunk0 + list[i]); });
+  if ((int)threadIdx.x < a.keep) a.lists[(int64_t)blockIdx.x * a.keep + threadIdx.x] = (int)threadIdx.x < n ? best[threadIdx.x] : 0;
   if (threadIdx.x == 0) {
     a.sums[2 * (int64_t)blockIdx.x] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
     a.sums[2 * (int64_t)blockIdx.x + 1] = reference;
@@ -263,7 +256,7 @@ __device__ inline bool greater(const Candidate& x, const Candidate& y) { return 
 constexpr int kJoinThreads = 1024, kJoined = 2;            // candidates that a thread holds
 
 __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a) {
-  extern __shared__ __align__(16) Candidate found[];       // the best so far, then those that may replace them
+  __shared__ Candidate found[FCP_BEAM_MAX_KEEP + kJoinThreads * kJoined], room[kJoinThreads];     // the best so far, then those that may replace them
   __shared__ double lse[FCP_BEAM_MAX_BEAMS];
   __shared__ uint32_t groups[kGroups];
   __shared__ Candidate best[FCP_BEAM_MAX_KEEP];
@@ -331,8 +324,7 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a) {
         if ((uint32_t)(c[i].score >> 32) >= border) found[kept + atomicAdd(&listed, 1)] = c[i];
     __syncthreads();
     const int n = kept + listed;
-    best_of<kJoinThreads>(found, n, a.keep, none, [](const Candidate& x, const Candidate& y) { return greater(x, y); }, [&](int i, const Candidate& k) { best[i] = k; });
-    __syncthreads();
+    best_of<kJoinThreads>(best, room, n, a.keep, [](const Candidate& x, const Candidate& y) { return greater(x, y); }, [&](int i) { return found[i]; });
     kept = min(n, a.keep);
     if ((int)threadIdx.x < kept) found[threadIdx.x] = best[threadIdx.x];
     if (threadIdx.x == 0) listed = 0;
@@ -350,13 +342,12 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a) {
   }
 }
 
-// How a call is divided: as many neighbouring logits a thread as leave four blocks, or two, for every CU; 8 where there are fewer.  (64 a thread: room for the list's worst case leaves one block a CU with
-// many kept.)
+// How a call is divided: as many neighbouring logits a thread as leave four blocks, or two, for every CU; 8 where there are fewer.
 struct BeamPlan { int32_t each, chunks; int64_t blocks; };
-BeamPlan plan_beam(int64_t rows, int32_t vocab, int32_t keep) {
+BeamPlan plan_beam(int64_t rows, int32_t vocab) {
   auto chunks = [&](int64_t each) { return (vocab + kThreads * each - 1) / (kThreads * each); };
   BeamPlan p;
-  p.each = keep <= 16 && rows * chunks(64) >= 1024 ? 64 : rows * chunks(32) >= 512 ? 32 : 8;
+  p.each = rows * chunks(64) >= 1024 ? 64 : rows * chunks(32) >= 512 ? 32 : 8;
   p.chunks = (int32_t)chunks(p.each);
   p.blocks = rows * p.chunks;
   return p;
@@ -375,10 +366,7 @@ int check_beam(const char* who, int32_t n_prompts, int32_t beams, int32_t vocab,
 
 template <class T, int E>
 int launch_rows(const BeamArgs& a, const BeamPlan& p, hipStream_t st) {
-  static std::atomic<uint64_t> raised;
-  const int bytes = list_room(a.keep, E) * 8;
-  if (bytes > 48 * 1024)
-    if (int rc = raise_lds_limit(reinterpret_cast<const void*>(beam_rows_kernel<T, E>), bytes, raised)) return rc;
+  const int bytes = list_room(a.keep, E) * 2;              // up to 32 KB
   beam_rows_kernel<T, E><<<dim3((unsigned)p.blocks), dim3(kThreads), bytes, st>>>(a);
   FCP_HIP_CHECK(hipGetLastError());
   return FCP_OK;
@@ -391,7 +379,7 @@ extern "C" size_t fcp_beam_scratch_bytes(int32_t n_prompts, int32_t beams, int32
   using namespace fcp;
   clear_error();
   if (check_beam("fcp_beam_scratch_bytes", n_prompts, beams, vocab, keep)) return 0;
-  const size_t n = beam_bytes(plan_beam((int64_t)n_prompts * beams, vocab, keep), keep);
+  const size_t n = beam_bytes(plan_beam((int64_t)n_prompts * beams, vocab), keep);
   return n ? n : 256;
 }
 
@@ -411,7 +399,7 @@ extern "C" int fcp_beam_select(const void* logits, int32_t type, int64_t logits_
     return fail(FCP_ERR_INVALID_ARG, "%s: an argument is not aligned to its type", who);
   if (new_score == score || (new_done && new_done == done)) return fail(FCP_ERR_INVALID_ARG, "%s: outputs must lie apart from inputs", who);
   if (!scratch || (uintptr_t)scratch % 256) return fail(FCP_ERR_INVALID_ARG, "%s: scratch must be 256-byte aligned", who);
-  const BeamPlan p = plan_beam((int64_t)n_prompts * beams, vocab, keep);
+  const BeamPlan p = plan_beam((int64_t)n_prompts * beams, vocab);
   const size_t need = beam_bytes(p, keep);
   if (scratch_bytes < need) return fail(FCP_ERR_CAPACITY, "%s: scratch has %zu bytes, %zu are needed", who, scratch_bytes, need);
   BeamArgs a = {logits, logits_row, n_prompts * beams, beams, vocab, p.chunks, keep, end_token, score, done, parent, token, new_score, new_done};
@@ -424,14 +412,7 @@ extern "C" int fcp_beam_select(const void* logits, int32_t type, int64_t logits_
              : p.each == 32 ? (bf16 ? launch_rows<__bf16, 32>(a, p, st) : launch_rows<float, 32>(a, p, st))
                             : (bf16 ? launch_rows<__bf16, 8>(a, p, st) : launch_rows<float, 8>(a, p, st)))
     return rc;
-  // all candidates of a block's look may have scores whose upper words are alike; the best so far beside them
-  static std::atomic<uint64_t> raised;
-  int room = 2 * kJoinThreads * kJoined;
-  static_assert(FCP_BEAM_MAX_KEEP <= kJoinThreads * kJoined, "both fit");
-  const int bytes = room * (int)sizeof(Candidate);
-  if (bytes > 48 * 1024)
-    if (int rc = raise_lds_limit(reinterpret_cast<const void*>(beam_join_kernel), bytes, raised)) return rc;
-  beam_join_kernel<<<dim3((unsigned)n_prompts), dim3(kJoinThreads), bytes, st>>>(a);
+  beam_join_kernel<<<dim3((unsigned)n_prompts), dim3(kJoinThreads), 0, st>>>(a);
   FCP_HIP_CHECK(hipGetLastError());
   return FCP_OK;
 }
