@@ -1,9 +1,9 @@
 // fcp_cache_fork and fcp_cache_compact: who holds which page of the cache, kept on the device.
 //
 // A sequence that continues another one takes over its table; pages that are only read are shared, and a page that new tokens go into is copied for all of those who would write it but one.
-// Both calls look at all entries of the tables once and set bits, one a page; then one block counts through the bits for free pages, in increasing order, and lists the copies;
-// the last launch copies: 16 bytes a thread, a block for each (page, KV head), whose keys are one run of memory and whose values are another.
-// Small calls are chains of loads, large ones are bound by the memory.
+// Every entry of this step's tables is looked at once, and marks its page; then one block counts through the marks for free pages, in increasing order, and lists the copies; the last launch copies,
+// 16 bytes a thread, a block for each (page, KV head), whose keys are one run of memory and whose values are another, and writes the tables.
+// Small calls are chains of loads and launches.  Where the tables are not large the block that plans marks too, bits in LDS: two launches; else four, with a byte a page.
 #include "fcp_cache.h"
 
 namespace fcp {
@@ -11,7 +11,7 @@ namespace {
 
 constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64;
 
-struct Copy { int32_t from, to, tokens, pad; };
+struct Copy { int32_t from, to, tokens, copied; };         // copied: fork, the entry is a copy's, whether there was a page for it or not
 
 struct PageArgs {
   CacheView c;
@@ -24,13 +24,13 @@ struct PageArgs {
   int32_t* new_len;
   int32_t* counts;
   // scratch
-  uint32_t* held;                      // a bit a page: sequences of this step (or others) hold it
-  uint32_t* read;                      // fork: sequences of the next step (or others) hold it and do not write it
-  int32_t* lowest;                     // fork: of the sequences of the next step that would write a page, the lowest; only entries of such pages mean something
-  int32_t* list;                       // fork: free pages; compact: pages that stay empty otherwise, in which others move
+  uint8_t* held;                       // large calls, a byte a page: sequences of this step (fork: or others) hold it
+  uint8_t* read;                       // fork: sequences of the next step (or others) hold it and do not write it
+  int32_t* lowest;                     // fork: of the sequences of the next step that would write a page, the lowest; compact: where a page moves.  Only entries of such pages mean something
+  int32_t* list;                       // fork: free pages; compact: pages in which others move
   Copy* copies;
-  int32_t* n_copies;                   // compact
-  int32_t words;
+  int32_t* n_copies;                   // compact: pages that move, and the first number past those in use afterwards
+  int32_t words;                       // of a bit a page
 };
 
 __device__ inline int32_t cached(const PageArgs& a, int seq) {
@@ -52,9 +52,6 @@ __device__ inline int32_t entry(const PageArgs& a, int seq, int place) {
   const int32_t p = a.s.pages[(int64_t)seq * a.s.max_pages + place];
   return (uint32_t)p < (uint32_t)a.c.n_pages ? p : -1;
 }
-__device__ inline void set_bit(uint32_t* bits, int32_t page) { atomicOr(bits + (page >> 5), 1u << (page & 31)); }
-__device__ inline bool bit(const uint32_t* bits, int32_t page) { return bits[page >> 5] >> (page & 31) & 1; }
-
 // Sum over the block before this thread, and of all threads.  Every thread calls.
 struct Scan { int32_t before, all; };
 __device__ inline Scan block_scan(int32_t x, int32_t* sums) {
@@ -73,26 +70,61 @@ __device__ inline Scan block_scan(int32_t x, int32_t* sums) {
   return r;
 }
 
-// ---- first launch: busy pages' bits, nothing else held; pages that are written have no writer yet -----------------
+// A word of bits, one for each of 32 bytes that is not 0 (behind n: 0).
+__device__ inline uint32_t bits_of(const uint8_t* bytes, int w, int32_t n) {
+  uint32_t bits = 0;
+  if (!bytes) return 0;
+  if (32 * w + 32 <= n) {
+    struct __attribute__((packed, aligned(1))) Words { uint32_t x[8]; };
+    const Words r = *reinterpret_cast<const Words*>(bytes + 32 * (int64_t)w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      uint32_t x = r.x[i];
+      x |= x >> 4;
+      x |= x >> 2;
+      x = (x | x >> 1) & 0x01010101u;
+      bits |= (x * 0x01020408u >> 24) << 4 * i;            // (the bytes' bits next to each other, the first one lowest)
+    }
+  } else {
+    for (int i = 32 * w; i < n; ++i) bits |= (uint32_t)(bytes[i] != 0) << (i - 32 * w);
+  }
+  return bits;
+}
+
+// The marks of pages, as bits in LDS or as bytes in scratch.
+struct LdsMarks {
+  uint32_t* held;
+  uint32_t* read;                      // (compact: busy)
+  __device__ uint32_t held_word(int w) const { return held[w]; }
+  __device__ uint32_t read_word(int w) const { return read[w]; }
+  __device__ bool is_read(int32_t page) const { return read[page >> 5] >> (page & 31) & 1; }
+};
+struct ByteMarks {
+  const uint8_t* held;
+  const uint8_t* read;
+  int32_t n;
+  __device__ uint32_t held_word(int w) const { return bits_of(held, w, n); }
+  __device__ uint32_t read_word(int w) const { return bits_of(read, w, n); }
+  __device__ bool is_read(int32_t page) const { return read && read[page]; }
+};
+
+// ---- large calls: marks ------------------------------------------------------------------------------------------
 template <bool Fork>
 __global__ __launch_bounds__(256) void clear_kernel(PageArgs a) {
   const int i = blockIdx.x * 256 + threadIdx.x;
-  if (i < a.words) {
-    uint32_t w = 0;
-    if (a.busy)
-      for (int j = 0; j < 32 && i * 32 + j < a.c.n_pages; ++j) w |= (uint32_t)(a.busy[i * 32 + j] != 0) << j;
-    a.held[i] = Fork ? w : 0;
-    if (Fork) a.read[i] = w;
+  for (int j = 4 * i; j < min(4 * i + 4, a.c.n_pages); ++j) {
+    const uint8_t b = a.busy ? a.busy[j] : 0;
+    a.held[j] = Fork ? b : 0;
+    if (Fork) a.read[j] = b;
   }
   if (Fork && i < a.n_new) {
     const Next x = next_of(a, i);
     const int32_t page = x.writes >= 0 ? entry(a, x.parent, x.writes) : -1;
     if (page >= 0) a.lowest[page] = INT32_MAX;
-    a.new_len[i] = x.after;
   }
 }
 
-// ---- second launch: the bits of all entries, a wave for 64 places of a sequence -----------------------------------
+// All entries, a wave for 64 places of a sequence.  (Who marks a page first does not matter: the same byte is written.)
 template <bool Fork>
 __global__ __launch_bounds__(256) void mark_kernel(PageArgs a) {
   const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -103,57 +135,138 @@ __global__ __launch_bounds__(256) void mark_kernel(PageArgs a) {
   if (seq < a.s.n_seqs) {
     if (place < pages_for(a, cached(a, (int)seq))) {
       const int32_t page = entry(a, (int)seq, place);
-      if (page >= 0 && !bit(a.held, page)) set_bit(a.held, page);
+      if (page >= 0) a.held[page] = 1;
     }
   } else if (Fork && seq - a.s.n_seqs < a.n_new) {
     const int i = (int)(seq - a.s.n_seqs);
     const Next x = next_of(a, i);
     const int32_t page = place < pages_for(a, x.before) ? entry(a, x.parent, place) : -1;
-    a.new_pages[(int64_t)i * a.s.max_pages + place] = page;
     if (page >= 0) {
       if (place == x.writes) atomicMin(a.lowest + page, i);
-      else if (!bit(a.read, page)) set_bit(a.read, page);
+      else a.read[page] = 1;
     }
   }
 }
 
-// ---- third launch: one block hands out pages ----------------------------------------------------------------------
-__global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(PageArgs a) {
+// ---- small calls: the block that plans marks -----------------------------------------------------------------------
+constexpr int kLdsPages = 1 << 18, kLdsSeqs = 4096, kLdsEntries = 1 << 17, kLdsNew = 8192;
+struct LdsTables { uint32_t *held, *read, *child, *part; int32_t* len; };
+__host__ __device__ inline size_t lds_bytes(int32_t words, int32_t n_seqs) { return (size_t)8 * words + 8 * ((n_seqs + 31) / 32) + 4 * (size_t)n_seqs; }
+__device__ inline LdsTables lds_tables(const PageArgs& a, unsigned char* lds) {
+  const int seq_words = (a.s.n_seqs + 31) / 32;
+  uint32_t* const held = reinterpret_cast<uint32_t*>(lds);
+  return {held, held + a.words, held + 2 * a.words, held + 2 * a.words + seq_words, reinterpret_cast<int32_t*>(held + 2 * a.words + 2 * seq_words)};
+}
+__device__ inline void set_bit(uint32_t* bits, int32_t i) { atomicOr(bits + (i >> 5), 1u << (i & 31)); }
+__device__ inline bool bit(const uint32_t* bits, int32_t i) { return bits[i >> 5] >> (i & 31) & 1; }
+
+// Marks this step's entries; fork: as read by others too, those of sequences with children, but the page in which new tokens go, which is marked if a child goes on without any.
+template <bool Fork>
+__device__ inline LdsMarks mark_in_lds(const PageArgs& a, unsigned char* lds) {
+  const LdsTables t = lds_tables(a, lds);
+  for (int w = threadIdx.x; w < a.words; w += kPlanThreads) {
+    const uint32_t b = bits_of(a.busy, w, a.c.n_pages);
+    t.held[w] = Fork ? b : 0;
+    t.read[w] = b;
+  }
+  for (int s = threadIdx.x; s < a.s.n_seqs; s += kPlanThreads) t.len[s] = cached(a, s);
+  for (int w = threadIdx.x; w < (a.s.n_seqs + 31) / 32; w += kPlanThreads) t.child[w] = t.part[w] = 0;
+  __syncthreads();
+  if (Fork) {
+    for (int i = threadIdx.x; i < a.n_new; i += kPlanThreads) {
+      const Next x = next_of(a, i);
+      if (x.parent < 0) continue;
+      if (!bit(t.child, x.parent)) set_bit(t.child, x.parent);
+      if (x.writes < 0 && !bit(t.part, x.parent)) set_bit(t.part, x.parent);
+      const int32_t page = x.writes >= 0 ? entry(a, x.parent, x.writes) : -1;
+      if (page >= 0) __hip_atomic_store(a.lowest + page, INT32_MAX, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __threadfence();
+    __syncthreads();
+    for (int i = threadIdx.x; i < a.n_new; i += kPlanThreads) {
+      const Next x = next_of(a, i);
+      const int32_t page = x.writes >= 0 ? entry(a, x.parent, x.writes) : -1;
+      if (page >= 0) atomicMin(a.lowest + page, i);
+    }
+  }
+  // a wave for 256 places of a sequence, four neighbouring entries a lane; four such units at once, so that their loads are on the way together
+  constexpr int kAtOnce = 4, kPlaces = 256;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, per_seq = (a.s.max_pages + kPlaces - 1) / kPlaces, units = a.s.n_seqs * per_seq;
+  for (int u0 = wave; u0 < units; u0 += kAtOnce * kPlanWaves) {
+    int32_t page[kAtOnce][4];
+    int seq[kAtOnce], place[kAtOnce], n[kAtOnce];
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const int u = u0 + k * kPlanWaves;
+      seq[k] = u < units ? u / per_seq : 0;
+      place[k] = u % per_seq * kPlaces + 4 * lane;
+      n[k] = u < units ? pages_for(a, t.len[seq[k]]) : 0;
+      const int32_t* const from = a.s.pages + (int64_t)seq[k] * a.s.max_pages + place[k];
+      struct __attribute__((packed, aligned(4))) Four { int32_t x[4]; };
+      if (place[k] + 4 <= n[k]) {
+        const Four f = *reinterpret_cast<const Four*>(from);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) page[k][j] = f.x[j];
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) page[k][j] = place[k] + j < n[k] ? from[j] : -1;
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      const bool reads = Fork && n[k] > 0 && bit(t.child, seq[k]), part = Fork && n[k] > 0 && bit(t.part, seq[k]);
+      const int full = t.len[seq[k]] >> a.c.log_page;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int32_t x = page[k][j];
+        if ((uint32_t)x >= (uint32_t)a.c.n_pages) continue;
+        set_bit(t.held, x);
+        if (reads && (place[k] + j < full || part)) set_bit(t.read, x);
+      }
+    }
+  }
+  __threadfence();
+  __syncthreads();
+  return {t.held, t.read};
+}
+
+// ---- one block hands out pages -------------------------------------------------------------------------------------
+template <class Marks>
+__device__ inline void plan_fork(const PageArgs& a, const Marks& marks) {
   __shared__ int32_t sums[kPlanWaves];
-  // pages that are free now, and those that nobody holds but who writes them
-  int32_t need = 0, kept = 0;
   auto copied = [&](int i, const Next& x, int32_t& page) {
     page = x.writes >= 0 ? entry(a, x.parent, x.writes) : -1;
-    return page >= 0 && (bit(a.read, page) || a.lowest[page] != i);
+    return page >= 0 && (marks.is_read(page) || __hip_atomic_load(a.lowest + page, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != i);
   };
+  // pages that are needed, and those that nobody holds but who writes them
+  int32_t need = 0, kept = 0;
   for (int i = threadIdx.x; i < a.n_new; i += kPlanThreads) {
     const Next x = next_of(a, i);
     int32_t page;
     const bool copy = copied(i, x, page);
     need += copy + pages_for(a, x.after) - pages_for(a, x.before);
     kept += page >= 0 && !copy;
+    a.new_len[i] = x.after;
   }
   need = block_scan(need, sums).all;
-  kept = block_scan(kept, sums).all;
-  int32_t listed = 0, held = 0;
+  int32_t listed = 0;
   for (int w0 = 0; w0 < a.words; w0 += kPlanThreads) {
     const int w = w0 + threadIdx.x;
-    uint32_t free = w < a.words ? ~a.held[w] : 0u;
+    uint32_t free = w < a.words ? ~marks.held_word(w) : 0u;
     if (w == a.words - 1 && a.c.n_pages % 32) free &= (1u << (a.c.n_pages % 32)) - 1;
-    held += w < a.words ? __popc(a.read[w]) : 0;
+    kept += w < a.words ? __popc(marks.read_word(w)) : 0;
     const Scan at = block_scan(__popc(free), sums);
     int32_t rank = listed + at.before;
     for (; free && rank < need; free &= free - 1) a.list[rank++] = 32 * w + __builtin_ctz(free);
     listed += at.all;
   }
-  held = block_scan(held, sums).all;
+  kept = block_scan(kept, sums).all;                       // (pages that the next step's sequences hold already, or others)
   const int32_t taken = min(need, listed);
   if (threadIdx.x == 0) {
     a.counts[0] = taken;
     a.counts[1] = need - taken;
-    a.counts[2] = a.c.n_pages - held - kept - taken;
+    a.counts[2] = a.c.n_pages - kept - taken;
   }
-  __threadfence_block();
   int32_t before = 0;
   for (int i0 = 0; i0 < a.n_new; i0 += kPlanThreads) {
     const int i = i0 + threadIdx.x;
@@ -169,7 +282,7 @@ __global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(PageArgs a) {
       int32_t rank = before + at.before;
       int32_t* const table = a.new_pages + (int64_t)i * a.s.max_pages;
       auto next = [&] { const int32_t r = rank++; return r < taken ? a.list[r] : -1; };
-      Copy c = {page, -1, 0, 0};
+      Copy c = {page, -1, 0, copy};
       if (copy) {
         c.to = table[x.writes] = next();
         c.tokens = c.to >= 0 ? x.before & (a.c.page - 1) : 0;
@@ -180,22 +293,23 @@ __global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(PageArgs a) {
     before += at.all;
   }
 }
+__global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(PageArgs a) { plan_fork(a, ByteMarks{a.held, a.read, a.c.n_pages}); }
+__global__ __launch_bounds__(kPlanThreads) void fork_small_kernel(PageArgs a) {
+  extern __shared__ __align__(16) unsigned char lds[];
+  plan_fork(a, mark_in_lds<true>(a, lds));
+}
 
 // The pages in use move to the lowest numbers that are not busy: `end` is the first number past these.
-__global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(PageArgs a) {
+template <class Marks>
+__device__ inline void plan_compact(const PageArgs& a, const Marks& marks) {
   __shared__ int32_t sums[kPlanWaves];
   __shared__ int32_t end_at, busy_end;
-  auto busy_bits = [&](int w) {
-    uint32_t b = 0;
-    if (a.busy)
-      for (int j = 0; j < 32 && w * 32 + j < a.c.n_pages; ++j) b |= (uint32_t)(a.busy[w * 32 + j] != 0) << j;
-    return b;
-  };
+  auto busy_bits = [&](int w) { return marks.read_word(w); };
   if (threadIdx.x == 0) end_at = busy_end = 0;
   __syncthreads();
   int32_t used = 0, all = 0;
   for (int w = threadIdx.x; w < a.words; w += kPlanThreads) {
-    const uint32_t h = a.held[w], b = busy_bits(w);
+    const uint32_t h = marks.held_word(w), b = busy_bits(w);
     used += __popc(h & ~b);
     all += __popc(h);
     if (b) atomicMax(&busy_end, 32 * w + 32 - __builtin_clz(b));
@@ -222,7 +336,7 @@ __global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(PageArgs a) 
     const int w = w0 + threadIdx.x;
     uint32_t hole = 0, mover = 0;
     if (w < a.words) {
-      const uint32_t h = a.held[w], b = busy_bits(w), low = 32 * w + 32 <= end ? ~0u : 32 * w >= end ? 0u : (1u << (end - 32 * w)) - 1;
+      const uint32_t h = marks.held_word(w), b = busy_bits(w), low = 32 * w + 32 <= end ? ~0u : 32 * w >= end ? 0u : (1u << (end - 32 * w)) - 1;
       hole = low & ~h & ~b;
       mover = ~low & h & ~b;
     }
@@ -249,6 +363,11 @@ __global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(PageArgs a) 
     a.n_copies[1] = end;
   }
 }
+__global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(PageArgs a) { plan_compact(a, ByteMarks{a.held, a.busy, a.c.n_pages}); }
+__global__ __launch_bounds__(kPlanThreads) void compact_small_kernel(PageArgs a) {
+  extern __shared__ __align__(16) unsigned char lds[];
+  plan_compact(a, mark_in_lds<false>(a, lds));
+}
 
 // ---- last launch --------------------------------------------------------------------------------------------------
 // The first `tokens` tokens of a (page, KV head), values in whole groups.
@@ -269,9 +388,24 @@ __device__ inline void copy_page(const CacheView& c, int head_dim, const Copy& x
   if (threadIdx.x == 128) c.k_scale[to] = c.k_scale[from];
   if (threadIdx.x == 129) c.v_scale[to] = c.v_scale[from];
 }
-__global__ __launch_bounds__(256) void fork_copy_kernel(PageArgs a, int head_dim) {
-  const Copy x = a.copies[blockIdx.x / a.c.hkv];
-  if (x.tokens > 0) copy_page(a.c, head_dim, x, blockIdx.x % a.c.hkv);
+// Copies, and the entries that are not fresh pages: those of the parent, and none behind the last one.
+__global__ __launch_bounds__(256) void fork_copy_kernel(PageArgs a, int head_dim, int table_blocks) {
+  if ((int)blockIdx.x >= table_blocks) {
+    const int u = blockIdx.x - table_blocks;
+    const Copy x = a.copies[u / a.c.hkv];
+    if (x.tokens > 0) copy_page(a.c, head_dim, x, u % a.c.hkv);
+    return;
+  }
+  const int per_seq = (a.s.max_pages + 255) / 256, i = blockIdx.x / per_seq, place = blockIdx.x % per_seq * 256 + threadIdx.x;
+  if (place >= a.s.max_pages) return;
+  const Next x = next_of(a, i);
+  int32_t* const to = a.new_pages + (int64_t)i * a.s.max_pages + place;
+  if (place < pages_for(a, x.before)) {
+    const int32_t page = entry(a, x.parent, place);
+    if (place != x.writes || !a.copies[i].copied) *to = page;
+  } else if (place >= pages_for(a, x.after)) {
+    *to = -1;
+  }
 }
 __global__ __launch_bounds__(256) void compact_copy_kernel(PageArgs a, int head_dim, int table_blocks) {
   const int32_t end = a.n_copies[1];
@@ -294,19 +428,31 @@ struct PageSpace { size_t held, read, lowest, list, copies, n_copies, bytes; int
 PageSpace page_space(const CacheView& c, int64_t n_copies) {
   PageSpace s = {};
   s.words = (int32_t)(((int64_t)c.n_pages + 31) / 32);
-  const size_t bits = pad_to((size_t)s.words * 4, 256), entries = pad_to((size_t)c.n_pages * 4, 256);
-  s.read = bits;
-  s.lowest = 2 * bits;
+  const size_t bytes = pad_to((size_t)c.n_pages, 256), entries = pad_to((size_t)c.n_pages * 4, 256);
+  s.read = bytes;
+  s.lowest = 2 * bytes;
   s.list = s.lowest + entries;
   s.copies = s.list + entries;
   s.n_copies = s.copies + pad_to((size_t)n_copies * sizeof(Copy), 256);
   s.bytes = s.n_copies + 256;
   return s;
 }
+// Whether one block marks and plans.
+bool small_call(const CacheView& c, int32_t n_seqs, int32_t max_pages, int32_t n_new) {
+  return c.n_pages <= kLdsPages && n_seqs <= kLdsSeqs && (int64_t)n_seqs * max_pages <= kLdsEntries && n_new <= kLdsNew;
+}
+template <class Kernel>
+int launch_small(Kernel kernel, const PageArgs& a, std::atomic<uint64_t>& raised, hipStream_t st) {
+  const size_t bytes = lds_bytes(a.words, a.s.n_seqs);
+  if (int rc = raise_lds_limit(reinterpret_cast<const void*>(kernel), (int)lds_bytes(kLdsPages / 32, kLdsSeqs), raised)) return rc;
+  kernel<<<dim3(1), dim3(kPlanThreads), bytes, st>>>(a);
+  FCP_HIP_CHECK(hipGetLastError());
+  return FCP_OK;
+}
 void place_scratch(PageArgs& a, const PageSpace& s, void* scratch) {
   char* const at = static_cast<char*>(scratch);
-  a.held = reinterpret_cast<uint32_t*>(at);
-  a.read = reinterpret_cast<uint32_t*>(at + s.read);
+  a.held = reinterpret_cast<uint8_t*>(at);
+  a.read = reinterpret_cast<uint8_t*>(at + s.read);
   a.lowest = reinterpret_cast<int32_t*>(at + s.lowest);
   a.list = reinterpret_cast<int32_t*>(at + s.list);
   a.copies = reinterpret_cast<Copy*>(at + s.copies);
@@ -316,7 +462,7 @@ void place_scratch(PageArgs& a, const PageSpace& s, void* scratch) {
 int check_page_sizes(const char* who, const CacheView& c, int32_t n_seqs, int32_t n_new, int32_t max_pages) {
   if (int rc = check_sizes(who, c, n_seqs, max_pages, 0)) return rc;
   if (int rc = check_sizes(who, c, n_new, max_pages, 0)) return rc;
-  if (!fits_axis((((int64_t)n_seqs + n_new) * ((max_pages + 63) / 64) + 3) / 4, 256) || !fits_axis((int64_t)n_new * c.hkv, 256))
+  if (!fits_axis((((int64_t)n_seqs + n_new) * ((max_pages + 63) / 64) + 3) / 4, 256) || !fits_axis((int64_t)n_new * (c.hkv + (max_pages + 255) / 256), 256))
     return fail(FCP_ERR_UNSUPPORTED, "%s: 2^24 blocks of work or more", who);
   return FCP_OK;
 }
@@ -360,17 +506,23 @@ extern "C" int fcp_cache_fork(const fcp_cache* cache, const int32_t* pages, cons
   a.counts = counts;
   place_scratch(a, space, scratch);
   hipStream_t st = static_cast<hipStream_t>(stream);
-  clear_kernel<true><<<dim3((unsigned)((max(space.words, n_new) + 255) / 256)), dim3(256), 0, st>>>(a);
-  FCP_HIP_CHECK(hipGetLastError());
-  const int64_t units = ((int64_t)n_seqs + n_new) * ((max_pages + 63) / 64);
-  if (units > 0) {
-    mark_kernel<true><<<dim3((unsigned)((units + 3) / 4)), dim3(256), 0, st>>>(a);
+  if (small_call(a.c, n_seqs, max_pages, n_new)) {
+    static std::atomic<uint64_t> raised;
+    if (int rc = launch_small(fork_small_kernel, a, raised, st)) return rc;
+  } else {
+    clear_kernel<true><<<dim3((unsigned)((max((a.c.n_pages + 3) / 4, n_new) + 255) / 256)), dim3(256), 0, st>>>(a);
+    FCP_HIP_CHECK(hipGetLastError());
+    const int64_t units = ((int64_t)n_seqs + n_new) * ((max_pages + 63) / 64);
+    if (units > 0) {
+      mark_kernel<true><<<dim3((unsigned)((units + 3) / 4)), dim3(256), 0, st>>>(a);
+      FCP_HIP_CHECK(hipGetLastError());
+    }
+    fork_plan_kernel<<<dim3(1), dim3(kPlanThreads), 0, st>>>(a);
     FCP_HIP_CHECK(hipGetLastError());
   }
-  fork_plan_kernel<<<dim3(1), dim3(kPlanThreads), 0, st>>>(a);
-  FCP_HIP_CHECK(hipGetLastError());
   if (n_new > 0) {
-    fork_copy_kernel<<<dim3((unsigned)((int64_t)n_new * a.c.hkv)), dim3(256), 0, st>>>(a, cache->head_dim);
+    const int64_t tables = (int64_t)n_new * ((max_pages + 255) / 256);
+    fork_copy_kernel<<<dim3((unsigned)(tables + (int64_t)n_new * a.c.hkv)), dim3(256), 0, st>>>(a, cache->head_dim, (int)tables);
     FCP_HIP_CHECK(hipGetLastError());
   }
   return FCP_OK;
@@ -394,15 +546,21 @@ extern "C" int fcp_cache_compact(const fcp_cache* cache, const int32_t* pages, c
   a.counts = counts;
   place_scratch(a, space, scratch);
   hipStream_t st = static_cast<hipStream_t>(stream);
-  clear_kernel<false><<<dim3((unsigned)((space.words + 255) / 256)), dim3(256), 0, st>>>(a);
-  FCP_HIP_CHECK(hipGetLastError());
-  const int64_t units = (int64_t)n_seqs * ((max_pages + 63) / 64), entries = (int64_t)n_seqs * max_pages;
-  if (units > 0) {
-    mark_kernel<false><<<dim3((unsigned)((units + 3) / 4)), dim3(256), 0, st>>>(a);
+  const int64_t entries = (int64_t)n_seqs * max_pages;
+  if (small_call(a.c, n_seqs, max_pages, 0)) {
+    static std::atomic<uint64_t> raised;
+    if (int rc = launch_small(compact_small_kernel, a, raised, st)) return rc;
+  } else {
+    clear_kernel<false><<<dim3((unsigned)(((a.c.n_pages + 3) / 4 + 255) / 256)), dim3(256), 0, st>>>(a);
+    FCP_HIP_CHECK(hipGetLastError());
+    const int64_t units = (int64_t)n_seqs * ((max_pages + 63) / 64);
+    if (units > 0) {
+      mark_kernel<false><<<dim3((unsigned)((units + 3) / 4)), dim3(256), 0, st>>>(a);
+      FCP_HIP_CHECK(hipGetLastError());
+    }
+    compact_plan_kernel<<<dim3(1), dim3(kPlanThreads), 0, st>>>(a);
     FCP_HIP_CHECK(hipGetLastError());
   }
-  compact_plan_kernel<<<dim3(1), dim3(kPlanThreads), 0, st>>>(a);
-  FCP_HIP_CHECK(hipGetLastError());
   const int table_blocks = (int)min((entries + 1023) / 1024, (int64_t)256), copy_blocks = (int)min(min((int64_t)a.c.n_pages, entries) * a.c.hkv, (int64_t)2048);
   if (entries > 0) {
     compact_copy_kernel<<<dim3((unsigned)(table_blocks + copy_blocks)), dim3(256), 0, st>>>(a, cache->head_dim, table_blocks);

@@ -203,6 +203,13 @@ def _compact(pool, pages, lens, busy=None, in_place=False):
     return want
 
 
+def _padded(pages, lens, large):
+    """large: thousands of sequences without tokens behind the others, so that the call is worked as large ones are."""
+    if not large:
+        return pages, lens
+    return np.concatenate([pages, np.full((4100, pages.shape[1]), -1, np.int32)]), np.concatenate([lens, np.zeros(4100, np.int32)])
+
+
 def _tables(rng, n, m, n_pages, P, busy):
     """Sequences of any length, some with a common beginning."""
     lens = rng.integers(0, m * P + 1, n)
@@ -222,13 +229,14 @@ def _tables(rng, n, m, n_pages, P, busy):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("large", [False, True])
 @pytest.mark.parametrize("P, hkv, D, fmt, weight", [(16, 2, 64, "int8", True), (32, 3, 128, "e4m3", False), (64, 1, 128, "int8", True), (128, 5, 64, "e4m3", True)])
-@pytest.mark.parametrize("n, n_new, m, n_pages", [(1, 8, 4, 40), (8, 8, 5, 90), (70, 130, 3, 700), (5, 3, 130, 900), (3, 0, 2, 9), (0, 4, 2, 9)])
-def test_fork(P, hkv, D, fmt, weight, n, n_new, m, n_pages):
+@pytest.mark.parametrize("n, n_new, m, n_pages", [(1, 8, 4, 40), (8, 8, 5, 90), (70, 130, 3, 700), (5, 3, 130, 900), (2, 9, 600, 1200), (3, 0, 2, 9), (0, 4, 2, 9)])
+def test_fork(P, hkv, D, fmt, weight, n, n_new, m, n_pages, large):
     rng = np.random.default_rng(n * 1000 + n_new + P)
     busy = (rng.random(n_pages) < 0.1).astype(np.uint8)
     pool = Pool(rng, n_pages, P, hkv, D, fmt, weight)
-    pages, lens = _tables(rng, n, m, n_pages, P, busy)
+    pages, lens = _padded(*_tables(rng, n, m, n_pages, P, busy), large)
     parent = rng.integers(-1, n + 1, n_new)                  # (some of nobody)
     for news in (np.ones(n_new), np.zeros(n_new), rng.integers(-1, 2 * P, n_new)):
         _fork(pool, pages, lens, parent, news.astype(np.int32), busy)
@@ -236,12 +244,14 @@ def test_fork(P, hkv, D, fmt, weight, n, n_new, m, n_pages):
 
 
 @pytest.mark.gpu
-def test_fork_keeps_a_page_that_others_read_or_hold():
+@pytest.mark.parametrize("large", [False, True])
+def test_fork_keeps_a_page_that_others_read_or_hold(large):
     """A sequence goes on in a page of which another one has more tokens, of which another one reads as many, that is busy, that a table names twice."""
     rng = np.random.default_rng(7)
     pool = Pool(rng, 30, 32)
     pages = np.array([[4, 9, -1], [4, 9, 2], [4, 9, -1], [7, 7, -1], [8, -1, -1]], np.int32)
     lens = np.array([50, 70, 50, 40, 3], np.int32)
+    pages, lens = _padded(pages, lens, large)
     busy = np.zeros(30, np.uint8)
     busy[8] = 1
     for parent, news in (([0, 1], [1, 1]), ([0, 2], [1, 0]), ([2, 0, 0], [5, 1, 40]), ([3, 3], [1, 1]), ([4], [1]), ([4, 4], [0, 0]), ([1, 1, 0, 2, 3, 4], [1] * 6)):
@@ -250,24 +260,26 @@ def test_fork_keeps_a_page_that_others_read_or_hold():
 
 
 @pytest.mark.gpu
-def test_fork_with_too_few_pages_and_entries_that_are_no_page():
+@pytest.mark.parametrize("large", [False, True])
+def test_fork_with_too_few_pages_and_entries_that_are_no_page(large):
     rng = np.random.default_rng(8)
     pool = Pool(rng, 6, 16)
     pages = np.array([[0, 1, -1, -1], [2, 99, 3, -1], [-7, -1, -1, -1]], np.int32)
     for lens in ([20, 40, 10], [32, 48, 16], [1000, 17, -3], [0, 0, 0]):
         for parent in ([0, 0, 0, 0], [1, 1, 0], [2, 2, 2], [0, 1, 2, 3, -1]):
             for new in (1, 20, 1 << 30):
-                _fork(pool, pages, np.array(lens, np.int32), np.array(parent), np.full(len(parent), new))
+                _fork(pool, *_padded(pages, np.array(lens, np.int32), large), np.array(parent), np.full(len(parent), new))
 
 
 @pytest.mark.gpu
-def test_fork_many():
-    """More sequences and pages than a block looks at once."""
+@pytest.mark.parametrize("n, m, n_pages, n_new", [(2500, 9, 70001, 3001), (4100, 3, 30011, 1000), (300, 4, 20000, 8200), (600, 300, 262160, 20)])
+def test_fork_many(n, m, n_pages, n_new):
+    """More sequences and pages than a block looks at once; more than are worked by one block."""
     rng = np.random.default_rng(9)
-    pool = Pool(rng, 70001, 16, hkv=1)
-    pages, lens = _tables(rng, 2500, 9, 70001, 16, np.zeros(70001))
-    parent = rng.integers(0, 2500, 3001)
-    w = _fork(pool, pages, lens, parent, rng.integers(0, 40, 3001))
+    pool = Pool(rng, n_pages, 16, hkv=1)
+    pages, lens = _tables(rng, n, m, n_pages, 16, np.zeros(n_pages))
+    parent = rng.integers(0, n, n_new)
+    w = _fork(pool, pages, lens, parent, rng.integers(0, 40, n_new))
     _compact(pool, w[0], w[1])
 
 
@@ -290,9 +302,10 @@ def test_steps_one_after_the_other():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("large", [False, True])
 @pytest.mark.parametrize("P, hkv, D, fmt, weight", [(16, 2, 64, "int8", True), (128, 3, 128, "e4m3", False)])
 @pytest.mark.parametrize("n, m, n_pages, share", [(1, 1, 1, 0), (1, 5, 33, 0.2), (9, 6, 64, 0.0), (40, 7, 900, 0.3), (0, 3, 40, 0.5), (3, 0, 9, 0.5), (300, 5, 4000, 0.02)])
-def test_compact(P, hkv, D, fmt, weight, n, m, n_pages, share):
+def test_compact(P, hkv, D, fmt, weight, n, m, n_pages, share, large):
     rng = np.random.default_rng(n + n_pages)
     busy = (rng.random(n_pages) < share).astype(np.uint8)
     pool = Pool(rng, n_pages, P, hkv, D, fmt, weight)
@@ -300,6 +313,7 @@ def test_compact(P, hkv, D, fmt, weight, n, m, n_pages, share):
     if n > 5:
         busy[pages[pages >= 0][:3]] = 1                      # pages in use that stay
         pages[2, 0], lens[3] = 10 ** 6, -1
+    pages, lens = _padded(pages, lens, large)
     w = _compact(pool, pages, lens, busy)
     _compact(pool, w[0], lens, busy, in_place=True)          # (nothing moves any more)
     if not busy.any():
