@@ -97,7 +97,6 @@ struct LdsMarks {
   uint32_t* read;                      // (compact: busy)
   __device__ uint32_t held_word(int w) const { return held[w]; }
   __device__ uint32_t read_word(int w) const { return read[w]; }
-  __device__ bool is_read(int32_t page) const { return read[page >> 5] >> (page & 31) & 1; }
 };
 struct ByteMarks {
   const uint8_t* held;
@@ -149,7 +148,7 @@ __global__ __launch_bounds__(256) void mark_kernel(PageArgs a) {
 }
 
 // ---- small calls: the block that plans marks -----------------------------------------------------------------------
-constexpr int kLdsPages = 1 << 18, kLdsSeqs = 4096, kLdsEntries = 1 << 17, kLdsNew = 8192;
+constexpr int kLdsPages = 1 << 18, kLdsSeqs = 4096, kLdsEntries = 1 << 17, kLdsNew = kPlanThreads;      // (a new sequence a thread)
 struct LdsTables { uint32_t *held, *read, *child, *part; int32_t* len; };
 __host__ __device__ inline size_t lds_bytes(int32_t words, int32_t n_seqs) { return (size_t)8 * words + 8 * ((n_seqs + 31) / 32) + 4 * (size_t)n_seqs; }
 __device__ inline LdsTables lds_tables(const PageArgs& a, unsigned char* lds) {
@@ -160,10 +159,9 @@ __device__ inline LdsTables lds_tables(const PageArgs& a, unsigned char* lds) {
 __device__ inline void set_bit(uint32_t* bits, int32_t i) { atomicOr(bits + (i >> 5), 1u << (i & 31)); }
 __device__ inline bool bit(const uint32_t* bits, int32_t i) { return bits[i >> 5] >> (i & 31) & 1; }
 
-// Marks this step's entries; fork: as read by others too, those of sequences with children, but the page in which new tokens go, which is marked if a child goes on without any.
+// Clears the marks but those of busy pages, and looks up the lengths.
 template <bool Fork>
-__device__ inline LdsMarks mark_in_lds(const PageArgs& a, unsigned char* lds) {
-  const LdsTables t = lds_tables(a, lds);
+__device__ inline void begin_marks(const PageArgs& a, const LdsTables& t) {
   for (int w = threadIdx.x; w < a.words; w += kPlanThreads) {
     const uint32_t b = bits_of(a.busy, w, a.c.n_pages);
     t.held[w] = Fork ? b : 0;
@@ -171,26 +169,12 @@ __device__ inline LdsMarks mark_in_lds(const PageArgs& a, unsigned char* lds) {
   }
   for (int s = threadIdx.x; s < a.s.n_seqs; s += kPlanThreads) t.len[s] = cached(a, s);
   for (int w = threadIdx.x; w < (a.s.n_seqs + 31) / 32; w += kPlanThreads) t.child[w] = t.part[w] = 0;
-  __syncthreads();
-  if (Fork) {
-    for (int i = threadIdx.x; i < a.n_new; i += kPlanThreads) {
-      const Next x = next_of(a, i);
-      if (x.parent < 0) continue;
-      if (!bit(t.child, x.parent)) set_bit(t.child, x.parent);
-      if (x.writes < 0 && !bit(t.part, x.parent)) set_bit(t.part, x.parent);
-      const int32_t page = x.writes >= 0 ? entry(a, x.parent, x.writes) : -1;
-      if (page >= 0) __hip_atomic_store(a.lowest + page, INT32_MAX, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
-    __threadfence();
-    __syncthreads();
-    for (int i = threadIdx.x; i < a.n_new; i += kPlanThreads) {
-      const Next x = next_of(a, i);
-      const int32_t page = x.writes >= 0 ? entry(a, x.parent, x.writes) : -1;
-      if (page >= 0) atomicMin(a.lowest + page, i);
-    }
-  }
-  // a wave for 256 places of a sequence, four neighbouring entries a lane; four such units at once, so that their loads are on the way together
-  constexpr int kAtOnce = 4, kPlaces = 256;
+}
+// Marks this step's entries; fork: as read by others too, those of sequences with children, but the page in which new tokens go, which is marked if a child goes on without any.
+template <bool Fork>
+__device__ inline void mark_in_lds(const PageArgs& a, const LdsTables& t) {
+  // a wave for 256 places of a sequence, four neighbouring entries a lane; eight such units at once, so that their loads are on the way together
+  constexpr int kAtOnce = 8, kPlaces = 256;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, per_seq = (a.s.max_pages + kPlaces - 1) / kPlaces, units = a.s.n_seqs * per_seq;
   for (int u0 = wave; u0 < units; u0 += kAtOnce * kPlanWaves) {
     int32_t page[kAtOnce][4];
@@ -225,9 +209,6 @@ __device__ inline LdsMarks mark_in_lds(const PageArgs& a, unsigned char* lds) {
       }
     }
   }
-  __threadfence();
-  __syncthreads();
-  return {t.held, t.read};
 }
 
 // ---- one block hands out pages -------------------------------------------------------------------------------------
@@ -294,9 +275,73 @@ __device__ inline void plan_fork(const PageArgs& a, const Marks& marks) {
   }
 }
 __global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(PageArgs a) { plan_fork(a, ByteMarks{a.held, a.read, a.c.n_pages}); }
+
+// A new sequence a thread, whose numbers stay in registers; free pages in LDS as far as they fit.  (What this takes is loads that wait for each other, 0.7 us each.)
 __global__ __launch_bounds__(kPlanThreads) void fork_small_kernel(PageArgs a) {
+  constexpr int kListed = 2 * kPlanThreads;
   extern __shared__ __align__(16) unsigned char lds[];
-  plan_fork(a, mark_in_lds<true>(a, lds));
+  __shared__ int32_t sums[kPlanWaves], list[kListed];
+  __shared__ __align__(16) int32_t written[kPlanThreads];  // pages that the sequences would write, or -1
+  const LdsTables t = lds_tables(a, lds);
+  const int i = threadIdx.x;
+  const bool there = i < a.n_new;
+  const int32_t said = there ? a.parent[i] : -1, news = there ? max(a.news[i], 0) : 0;
+  begin_marks<true>(a, t);
+  __syncthreads();
+  const int32_t parent = (uint32_t)said < (uint32_t)a.s.n_seqs ? said : -1, tokens = parent >= 0 ? t.len[parent] : 0;
+  const int32_t after = (int32_t)min((int64_t)tokens + news, (int64_t)a.s.max_pages << a.c.log_page), writes = after > tokens && (tokens & (a.c.page - 1)) ? tokens >> a.c.log_page : -1;
+  const int32_t page = writes >= 0 ? entry(a, parent, writes) : -1;
+  if (parent >= 0) {
+    if (!bit(t.child, parent)) set_bit(t.child, parent);
+    if (writes < 0 && !bit(t.part, parent)) set_bit(t.part, parent);
+  }
+  written[i] = page;
+  __syncthreads();
+  mark_in_lds<true>(a, t);
+  // whether one before it would write the page too
+  bool copy = false;
+  if (page >= 0) {
+    int j = 0;
+    for (; j + 4 <= i; j += 4) {
+      const i32x4 w = *reinterpret_cast<const i32x4*>(written + j);
+      copy |= w[0] == page || w[1] == page || w[2] == page || w[3] == page;
+    }
+    for (; j < i; ++j) copy |= written[j] == page;
+  }
+  __syncthreads();
+  copy |= page >= 0 && bit(t.read, page);
+  const Scan mine = block_scan(copy + pages_for(a, after) - pages_for(a, tokens), sums);
+  const int32_t need = mine.all;
+  int32_t listed = 0, held = page >= 0 && !copy;
+  for (int w0 = 0; w0 < a.words; w0 += kPlanThreads) {
+    const int w = w0 + i;
+    uint32_t free = w < a.words ? ~t.held[w] : 0u;
+    if (w == a.words - 1 && a.c.n_pages % 32) free &= (1u << (a.c.n_pages % 32)) - 1;
+    held += w < a.words ? __popc(t.read[w]) : 0;
+    const Scan at = block_scan(__popc(free), sums);
+    int32_t rank = listed + at.before;
+    for (; free && rank < need; free &= free - 1, ++rank) (rank < kListed ? list : a.list)[rank] = 32 * w + __builtin_ctz(free);
+    listed += at.all;
+  }
+  held = block_scan(held, sums).all;
+  const int32_t taken = min(need, listed);
+  if (i == 0) {
+    a.counts[0] = taken;
+    a.counts[1] = need - taken;
+    a.counts[2] = a.c.n_pages - held - taken;
+  }
+  if (!there) return;
+  int32_t rank = mine.before;
+  int32_t* const table = a.new_pages + (int64_t)i * a.s.max_pages;
+  auto next = [&] { const int32_t r = rank++; return r >= taken ? -1 : r < kListed ? list[r] : a.list[r]; };
+  Copy c = {page, -1, 0, copy};
+  if (copy) {
+    c.to = table[writes] = next();
+    c.tokens = c.to >= 0 ? tokens & (a.c.page - 1) : 0;
+  }
+  a.copies[i] = c;
+  a.new_len[i] = after;
+  for (int place = pages_for(a, tokens); place < pages_for(a, after); ++place) table[place] = next();
 }
 
 // The pages in use move to the lowest numbers that are not busy: `end` is the first number past these.
@@ -366,7 +411,12 @@ __device__ inline void plan_compact(const PageArgs& a, const Marks& marks) {
 __global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(PageArgs a) { plan_compact(a, ByteMarks{a.held, a.busy, a.c.n_pages}); }
 __global__ __launch_bounds__(kPlanThreads) void compact_small_kernel(PageArgs a) {
   extern __shared__ __align__(16) unsigned char lds[];
-  plan_compact(a, mark_in_lds<false>(a, lds));
+  const LdsTables t = lds_tables(a, lds);
+  begin_marks<false>(a, t);
+  __syncthreads();
+  mark_in_lds<false>(a, t);
+  __syncthreads();
+  plan_compact(a, LdsMarks{t.held, t.read});
 }
 
 // ---- last launch --------------------------------------------------------------------------------------------------
