@@ -92,11 +92,27 @@ __device__ inline uint32_t bits_of(const uint8_t* bytes, int w, int32_t n) {
 }
 
 // The marks of pages, as bits in LDS or as bytes in scratch.
+// In LDS two bits a page, 16 pages a word: held, read (compact: busy), so that an entry is marked with one addition of bits.
+__device__ inline uint32_t even_bits(uint32_t x) {         // bits 0, 2, 4, .. next to each other
+  x &= 0x55555555u;
+  x = (x | x >> 1) & 0x33333333u;
+  x = (x | x >> 2) & 0x0f0f0f0fu;
+  x = (x | x >> 4) & 0x00ff00ffu;
+  return (x | x >> 8) & 0xffffu;
+}
+__device__ inline uint32_t spread_bits(uint32_t x) {       // 16 bits to bits 0, 2, 4, ..
+  x &= 0xffffu;
+  x = (x | x << 8) & 0x00ff00ffu;
+  x = (x | x << 4) & 0x0f0f0f0fu;
+  x = (x | x << 2) & 0x33333333u;
+  return (x | x << 1) & 0x55555555u;
+}
+constexpr uint32_t kHeld = 1, kRead = 2;
 struct LdsMarks {
-  uint32_t* held;
-  uint32_t* read;                      // (compact: busy)
-  __device__ uint32_t held_word(int w) const { return held[w]; }
-  __device__ uint32_t read_word(int w) const { return read[w]; }
+  uint32_t* two;
+  __device__ uint32_t held_word(int w) const { return even_bits(two[2 * w]) | even_bits(two[2 * w + 1]) << 16; }
+  __device__ uint32_t read_word(int w) const { return even_bits(two[2 * w] >> 1) | even_bits(two[2 * w + 1] >> 1) << 16; }
+  __device__ bool is_read(int32_t page) const { return two[page >> 4] >> 2 * (page & 15) & kRead; }
 };
 struct ByteMarks {
   const uint8_t* held;
@@ -149,12 +165,16 @@ __global__ __launch_bounds__(256) void mark_kernel(PageArgs a) {
 
 // ---- small calls: the block that plans marks -----------------------------------------------------------------------
 constexpr int kLdsPages = 1 << 18, kLdsSeqs = 4096, kLdsEntries = 1 << 17, kLdsNew = kPlanThreads;      // (a new sequence a thread)
-struct LdsTables { uint32_t *held, *read, *child, *part; int32_t* len; };
-__host__ __device__ inline size_t lds_bytes(int32_t words, int32_t n_seqs) { return (size_t)8 * words + 8 * ((n_seqs + 31) / 32) + 4 * (size_t)n_seqs; }
+// Per page: marks, and whether somebody writes it; per sequence of this step: whether it has children, whether one of them goes on without new tokens in a page that is begun, its tokens, the
+// lowest child that writes its last page.
+struct LdsTables { LdsMarks marks; uint32_t *written, *child, *part; int32_t *len, *low; };
+__host__ __device__ inline size_t lds_bytes(int32_t words, int32_t n_seqs) { return (size_t)12 * words + 8 * ((n_seqs + 31) / 32) + 8 * (size_t)n_seqs; }
 __device__ inline LdsTables lds_tables(const PageArgs& a, unsigned char* lds) {
   const int seq_words = (a.s.n_seqs + 31) / 32;
-  uint32_t* const held = reinterpret_cast<uint32_t*>(lds);
-  return {held, held + a.words, held + 2 * a.words, held + 2 * a.words + seq_words, reinterpret_cast<int32_t*>(held + 2 * a.words + 2 * seq_words)};
+  uint32_t* const two = reinterpret_cast<uint32_t*>(lds);
+  uint32_t* const child = two + 3 * a.words;
+  int32_t* const len = reinterpret_cast<int32_t*>(child + 2 * seq_words);
+  return {{two}, two + 2 * a.words, child, child + seq_words, len, len + a.s.n_seqs};
 }
 __device__ inline void set_bit(uint32_t* bits, int32_t i) { atomicOr(bits + (i >> 5), 1u << (i & 31)); }
 __device__ inline bool bit(const uint32_t* bits, int32_t i) { return bits[i >> 5] >> (i & 31) & 1; }
@@ -164,51 +184,61 @@ template <bool Fork>
 __device__ inline void begin_marks(const PageArgs& a, const LdsTables& t) {
   for (int w = threadIdx.x; w < a.words; w += kPlanThreads) {
     const uint32_t b = bits_of(a.busy, w, a.c.n_pages);
-    t.held[w] = Fork ? b : 0;
-    t.read[w] = b;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) t.marks.two[2 * w + half] = spread_bits(b >> 16 * half) * (Fork ? kHeld | kRead : kRead);
+    if (Fork) t.written[w] = 0;
   }
-  for (int s = threadIdx.x; s < a.s.n_seqs; s += kPlanThreads) t.len[s] = cached(a, s);
+  for (int s = threadIdx.x; s < a.s.n_seqs; s += kPlanThreads) {
+    t.len[s] = cached(a, s);
+    if (Fork) t.low[s] = INT32_MAX;
+  }
   for (int w = threadIdx.x; w < (a.s.n_seqs + 31) / 32; w += kPlanThreads) t.child[w] = t.part[w] = 0;
 }
 // Marks this step's entries; fork: as read by others too, those of sequences with children, but the page in which new tokens go, which is marked if a child goes on without any.
 template <bool Fork>
 __device__ inline void mark_in_lds(const PageArgs& a, const LdsTables& t) {
-  // a wave for 256 places of a sequence, four neighbouring entries a lane; eight such units at once, so that their loads are on the way together
+  // a wave for 256 places of a sequence, four neighbouring entries a lane; of eight sequences at once, so that their loads are on the way together, and then the looks at the marks
   constexpr int kAtOnce = 8, kPlaces = 256;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, per_seq = (a.s.max_pages + kPlaces - 1) / kPlaces, units = a.s.n_seqs * per_seq;
-  for (int u0 = wave; u0 < units; u0 += kAtOnce * kPlanWaves) {
-    int32_t page[kAtOnce][4];
-    int seq[kAtOnce], place[kAtOnce], n[kAtOnce];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  for (int first = 0; first < a.s.max_pages; first += kPlaces)
+    for (int s0 = wave; s0 < a.s.n_seqs; s0 += kAtOnce * kPlanWaves) {
+      const int place = first + 4 * lane;
+      int32_t page[kAtOnce][4];
 #pragma unroll
-    for (int k = 0; k < kAtOnce; ++k) {
-      const int u = u0 + k * kPlanWaves;
-      seq[k] = u < units ? u / per_seq : 0;
-      place[k] = u % per_seq * kPlaces + 4 * lane;
-      n[k] = u < units ? pages_for(a, t.len[seq[k]]) : 0;
-      const int32_t* const from = a.s.pages + (int64_t)seq[k] * a.s.max_pages + place[k];
-      struct __attribute__((packed, aligned(4))) Four { int32_t x[4]; };
-      if (place[k] + 4 <= n[k]) {
-        const Four f = *reinterpret_cast<const Four*>(from);
+      for (int k = 0; k < kAtOnce; ++k) {
+        const int seq = s0 + k * kPlanWaves, n = seq < a.s.n_seqs ? pages_for(a, t.len[seq]) : 0;
+        const int32_t* const from = a.s.pages + (int64_t)(n > 0 ? seq : 0) * a.s.max_pages + place;
+        struct __attribute__((packed, aligned(4))) Four { int32_t x[4]; };
+        Four f = {{-1, -1, -1, -1}};
+        if (place + 4 <= n) {
+          f = *reinterpret_cast<const Four*>(from);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 3; ++j) f.x[j] = place + j < n ? from[j] : -1;
+        }
 #pragma unroll
         for (int j = 0; j < 4; ++j) page[k][j] = f.x[j];
-      } else {
+      }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) page[k][j] = place[k] + j < n[k] ? from[j] : -1;
+      for (int k = 0; k < kAtOnce; ++k) {
+        const int seq = s0 + k * kPlanWaves;
+        if (seq >= a.s.n_seqs) break;
+        const int32_t len = t.len[seq], full = len >> a.c.log_page;
+        if (first >= pages_for(a, len)) continue;
+        const bool reads = Fork && bit(t.child, seq), part = Fork && bit(t.part, seq);
+        uint32_t bits[4], before[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int32_t x = page[k][j];
+          const bool there = (uint32_t)x < (uint32_t)a.c.n_pages;
+          bits[j] = there ? (reads && (place + j < full || part) ? kHeld | kRead : kHeld) << 2 * (x & 15) : 0u;
+          before[j] = t.marks.two[there ? x >> 4 : 0];
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if ((before[j] & bits[j]) != bits[j]) atomicOr(t.marks.two + (page[k][j] >> 4), bits[j]);      // (many sequences name the same pages)
       }
     }
-#pragma unroll
-    for (int k = 0; k < kAtOnce; ++k) {
-      const bool reads = Fork && n[k] > 0 && bit(t.child, seq[k]), part = Fork && n[k] > 0 && bit(t.part, seq[k]);
-      const int full = t.len[seq[k]] >> a.c.log_page;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int32_t x = page[k][j];
-        if ((uint32_t)x >= (uint32_t)a.c.n_pages) continue;
-        set_bit(t.held, x);
-        if (reads && (place[k] + j < full || part)) set_bit(t.read, x);
-      }
-    }
-  }
 }
 
 // ---- one block hands out pages -------------------------------------------------------------------------------------
@@ -280,8 +310,7 @@ __global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(PageArgs a) { p
 __global__ __launch_bounds__(kPlanThreads) void fork_small_kernel(PageArgs a) {
   constexpr int kListed = 2 * kPlanThreads;
   extern __shared__ __align__(16) unsigned char lds[];
-  __shared__ int32_t sums[kPlanWaves], list[kListed];
-  __shared__ __align__(16) int32_t written[kPlanThreads];  // pages that the sequences would write, or -1
+  __shared__ int32_t sums[kPlanWaves], list[kListed], written[kPlanThreads], several;           // written: pages that the sequences would write, or -1
   const LdsTables t = lds_tables(a, lds);
   const int i = threadIdx.x;
   const bool there = i < a.n_new;
@@ -294,30 +323,28 @@ __global__ __launch_bounds__(kPlanThreads) void fork_small_kernel(PageArgs a) {
   if (parent >= 0) {
     if (!bit(t.child, parent)) set_bit(t.child, parent);
     if (writes < 0 && !bit(t.part, parent)) set_bit(t.part, parent);
+    if (page >= 0) atomicMin(t.low + parent, i);
   }
   written[i] = page;
+  if (i == 0) several = 0;
   __syncthreads();
   mark_in_lds<true>(a, t);
-  // whether one before it would write the page too
-  bool copy = false;
-  if (page >= 0) {
-    int j = 0;
-    for (; j + 4 <= i; j += 4) {
-      const i32x4 w = *reinterpret_cast<const i32x4*>(written + j);
-      copy |= w[0] == page || w[1] == page || w[2] == page || w[3] == page;
-    }
-    for (; j < i; ++j) copy |= written[j] == page;
-  }
+  const bool lowest = page >= 0 && t.low[parent] == i;
+  if (lowest && (atomicOr(t.written + (page >> 5), 1u << (page & 31)) >> (page & 31) & 1)) several = 1;    // two parents have begun the same page
   __syncthreads();
-  copy |= page >= 0 && bit(t.read, page);
+  // whether one before it would write the page too
+  bool copy = page >= 0 && !lowest;
+  if (several)
+    for (int j = 0; page >= 0 && j < i; ++j) copy |= written[j] == page;
+  copy |= page >= 0 && t.marks.is_read(page);
   const Scan mine = block_scan(copy + pages_for(a, after) - pages_for(a, tokens), sums);
   const int32_t need = mine.all;
   int32_t listed = 0, held = page >= 0 && !copy;
   for (int w0 = 0; w0 < a.words; w0 += kPlanThreads) {
     const int w = w0 + i;
-    uint32_t free = w < a.words ? ~t.held[w] : 0u;
+    uint32_t free = w < a.words ? ~t.marks.held_word(w) : 0u;
     if (w == a.words - 1 && a.c.n_pages % 32) free &= (1u << (a.c.n_pages % 32)) - 1;
-    held += w < a.words ? __popc(t.read[w]) : 0;
+    held += w < a.words ? __popc(t.marks.read_word(w)) : 0;
     const Scan at = block_scan(__popc(free), sums);
     int32_t rank = listed + at.before;
     for (; free && rank < need; free &= free - 1, ++rank) (rank < kListed ? list : a.list)[rank] = 32 * w + __builtin_ctz(free);
@@ -416,7 +443,7 @@ __global__ __launch_bounds__(kPlanThreads) void compact_small_kernel(PageArgs a)
   __syncthreads();
   mark_in_lds<false>(a, t);
   __syncthreads();
-  plan_compact(a, LdsMarks{t.held, t.read});
+  plan_compact(a, t.marks);
 }
 
 // ---- last launch --------------------------------------------------------------------------------------------------
