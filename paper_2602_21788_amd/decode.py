@@ -3,8 +3,10 @@
 Only buffers and tables live here (which pages a sequence owns, how long it is, which position comes next); every step of the path runs in the library's own kernels:
   fcp_rotary -> fcp_cache_append -> fcp_cache_attn (weigh) for new tokens; fcp_attn_fwd_step_direct for prompts, whose keys then go into the cache and whose
   weights fcp_cache_weigh adds up; fcp_cache_evict when a sequence outgrows its budget.
+Several continuations of every prompt (BeamDecoder):
+  fcp_beam_select -> fcp_cache_fork -> fcp_rotary -> fcp_cache_append -> fcp_cache_attn_shared; fcp_cache_compact when the pool is to shrink.
 
-    python -m paper_2602_21788_amd.decode        # a small run: prompts, tokens, eviction
+    python -m paper_2602_21788_amd.decode        # a small run: prompts, tokens, eviction; beams
 """
 from __future__ import annotations
 
@@ -168,6 +170,88 @@ class CacheDecoder:
         return kept
 
 
+class BeamDecoder:
+    """`beams` continuations of each of n_prompts prompts, one layer.  The tables live on the device: a step needs nothing from the host but the rows.
+
+        dec.prefill(q, k, v, lens)                      # the prompts
+        loop: tokens, parents = dec.select(logits)      # logits [n_prompts, vocab] after the prompts, then [n_prompts * beams, vocab]
+              o, lse = dec.step(q, k, v)                # the rows of these tokens, one for each beam
+        dec.sequences()                                 # what each beam says
+    """
+
+    def __init__(self, n_prompts, beams, n_pages, max_pages, hq, hkv, head_dim, end_token=-1, **kw):
+        self.prompts = CacheDecoder(n_prompts, n_pages, max_pages, hq, hkv, head_dim, **kw)
+        self.n, self.beams, self.end = n_prompts, beams, end_token
+        self.cache, self.device, self.scale = self.prompts.cache, self.prompts.device, self.prompts.scale
+        i32 = lambda *shape: torch.empty(*shape, dtype=torch.int32, device=self.device)
+        rows = n_prompts * beams
+        self._tables = [(i32(rows, max_pages), i32(rows)) for _ in range(2)]           # this step's and the next one's, in turn
+        self.counts = i32(3)
+        up = self.prompts._to
+        self._ones, self._cu, self._groups = up(np.ones(rows)), up(np.arange(rows + 1)), up(np.arange(n_prompts + 1) * beams)
+        self._fork_scratch = torch.empty(B.fcp_cache_scratch_bytes(B.FCP_SCRATCH_CACHE_FORK, self.cache, rows, max_pages), dtype=torch.uint8, device=self.device)
+        self._attn_scratch = torch.empty(B.fcp_cache_scratch_bytes(B.FCP_SCRATCH_CACHE_SHARED, self.cache, rows, max_pages, rows, hq), dtype=torch.uint8, device=self.device)
+        self._beam_scratch = None
+
+    def prefill(self, q, k, v, lens):
+        """The prompts, as CacheDecoder.prefill."""
+        out = self.prompts.prefill(q, k, v, lens)
+        self.pages, self.kv_len = self.prompts.pages_d, self.prompts.kv_len_d
+        self._shared = self.prompts._to(np.asarray(lens) // self.prompts.P * self.prompts.P)     # (the page in which a prompt ends is every beam's own)
+        self.score, self.done = torch.zeros(self.n, device=self.device), torch.zeros(self.n, dtype=torch.uint8, device=self.device)
+        self.chosen, self.history, self.steps = None, [], 0
+        return out
+
+    def select(self, logits):
+        """The best tokens behind the beams so far: (tokens, parents) [n_prompts, beams], best first; parents are rows of the logits, -1 where there is no candidate.  self.score, self.done follow."""
+        width = 1 if not self.history else self.beams
+        mk = lambda dt: torch.empty(self.n, self.beams, dtype=dt, device=self.device)
+        parent, token, score, done = mk(torch.int32), mk(torch.int32), mk(torch.float32), mk(torch.uint8)
+        n = B.fcp_beam_scratch_bytes(self.n, width, logits.shape[1], self.beams)
+        if self._beam_scratch is None or self._beam_scratch.numel() < n:
+            self._beam_scratch = torch.empty(n, dtype=torch.uint8, device=self.device)
+        B.fcp_beam_select(logits, self.score, width, parent, token, score, self._beam_scratch, self.done, self.end, done)
+        self.score, self.done, self.chosen = score.view(-1), done.view(-1), parent.view(-1)
+        self.history.append((parent, token))
+        return token, parent
+
+    def step(self, q, k, v, check=True):
+        """The rows of the chosen tokens, bf16 [n_prompts * beams, heads, D] (turned in place): O, LSE.  check: raises MemoryError, and leaves the beams as they were, where the pool has too few
+        pages, for which the host waits; without it the tokens that found no page are seen by nobody."""
+        if self.chosen is None:
+            raise ValueError("select() chooses the tokens whose rows step() takes")
+        dec, rows = self.prompts, self.n * self.beams
+        dec._fit(q, k, v, rows)
+        o, lse = torch.empty(q.shape, dtype=torch.bfloat16, device=self.device), torch.empty(dec.hq, rows, dtype=torch.float32, device=self.device)
+        pages, kv_len = self._tables[self.steps % 2]
+        B.fcp_cache_fork(self.cache, self.pages, self.kv_len, self.chosen, self._ones, pages, kv_len, self.counts, self._fork_scratch)
+        if check and int(self.counts[1]):
+            raise MemoryError("no page left")
+        if dec.rot_dim:
+            dec._rotate(q, k, kv_len - 1)                    # (the new token is the last one)
+        B.fcp_cache_append(self.cache, k, v, self._cu, kv_len, pages)
+        B.fcp_cache_attn_shared(self.cache, q, self._cu, kv_len, pages, self._groups, self._shared, self.scale, o, lse, self._attn_scratch)
+        self.pages, self.kv_len, self.chosen = pages, kv_len, None
+        self.steps += 1
+        return o, lse
+
+    def compact(self):
+        """Moves the pages in use to the pool's beginning: (pages moved, in use, first number past them).  The host waits."""
+        n = B.fcp_cache_scratch_bytes(B.FCP_SCRATCH_CACHE_COMPACT, self.cache, *self.pages.shape)
+        B.fcp_cache_compact(self.cache, self.pages, self.kv_len, self.pages, self.counts, torch.empty(n, dtype=torch.uint8, device=self.device))
+        return tuple(self.counts.tolist())
+
+    def sequences(self):
+        """[n_prompts, beams, selections] int64: the tokens of every beam, from the choices and whom they continue; -1 where a beam had no candidate.  The host waits."""
+        out = np.full((self.n, self.beams, len(self.history)), -1, np.int64)
+        row = np.arange(self.n * self.beams)
+        for t in range(len(self.history) - 1, -1, -1):
+            parent, token = (x.cpu().numpy().reshape(-1) for x in self.history[t])
+            out.reshape(-1, len(self.history))[:, t] = np.where(row >= 0, token[row], -1)
+            row = np.where(row >= 0, parent[row], -1)
+        return out
+
+
 def main():
     g = torch.Generator(device="cuda").manual_seed(0)
     lens, hq, hkv, D = [700, 150, 33, 1200], 32, 8, 128
@@ -183,6 +267,12 @@ def main():
     print("cut to 512: cached", dec.kv_len.tolist(), "head 0 of sequence 0 keeps", kept[0, 0, :8].tolist(), "...; pages in use:", int((dec.pages >= 0).sum()))
     o, lse = dec.step(rows(9, hq), rows(9, hkv), rows(9, hkv), [1, 5, 0, 3])
     print("1, 5, 0 and 3 tokens more: cached", dec.kv_len.tolist(), "mean LSE %.3f" % float(lse.mean()))
+    beams = BeamDecoder(len(lens), 4, 256, 64, hq, hkv, D, turns=turns, magnitude=magnitude)
+    beams.prefill(rows(sum(lens), hq), rows(sum(lens), hkv), rows(sum(lens), hkv), lens)
+    for t in range(8):
+        beams.select(3 * torch.randn(len(lens) * (4 if t else 1), 32000, generator=g, device="cuda"))
+        o, lse = beams.step(rows(4 * len(lens), hq), rows(4 * len(lens), hkv), rows(4 * len(lens), hkv))
+    print("4 beams each, 8 tokens: the best of the first prompt", beams.sequences()[0, 0].tolist(), "at %.2f;" % float(beams.score[0]), "pages moved, in use, end:", beams.compact())
 
 
 if __name__ == "__main__":
