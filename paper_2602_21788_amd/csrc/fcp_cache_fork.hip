@@ -197,22 +197,28 @@ __device__ inline void begin_marks(const PageArgs& a, const LdsTables& t) {
 // Marks this step's entries; fork: as read by others too, those of sequences with children, but the page in which new tokens go, which is marked if a child goes on without any.
 template <bool Fork>
 __device__ inline void mark_in_lds(const PageArgs& a, const LdsTables& t) {
-  // a wave for 256 places of a sequence, four neighbouring entries a lane; of eight sequences at once, so that their loads are on the way together, and then the looks at the marks
-  constexpr int kAtOnce = 8, kPlaces = 256;
+  // Four neighbouring entries a lane, 16 to 64 lanes a sequence, as the tables are long; a wave looks at eight such lots at once, so that their loads are on the way together.  Instructions bound
+  // this where there are thousands of entries for each wave, so there are few for an entry: a mark is made whether it is there or not.
+  constexpr int kAtOnce = 8;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  for (int first = 0; first < a.s.max_pages; first += kPlaces)
-    for (int s0 = wave; s0 < a.s.n_seqs; s0 += kAtOnce * kPlanWaves) {
-      const int place = first + 4 * lane;
+  const int log_lanes = a.s.max_pages > 128 ? 6 : a.s.max_pages > 64 ? 5 : 4, of_lot = 64 >> log_lanes, sub = lane >> log_lanes;
+  for (int first = 0; first < a.s.max_pages; first += 4 << log_lanes)
+    for (int lot = wave; lot * of_lot < a.s.n_seqs; lot += kAtOnce * kPlanWaves) {
+      const int place = first + 4 * (lane & ((1 << log_lanes) - 1));
       int32_t page[kAtOnce][4];
+      int readable[kAtOnce];                               // places before this one are read by others
 #pragma unroll
       for (int k = 0; k < kAtOnce; ++k) {
-        const int seq = s0 + k * kPlanWaves, n = seq < a.s.n_seqs ? pages_for(a, t.len[seq]) : 0;
-        const int32_t* const from = a.s.pages + (int64_t)(n > 0 ? seq : 0) * a.s.max_pages + place;
+        const int seq = (lot + k * kPlanWaves) * of_lot + sub;
+        const bool there = seq < a.s.n_seqs;
+        const int32_t len = there ? t.len[seq] : 0, n = pages_for(a, len);
+        readable[k] = Fork && there && bit(t.child, seq) ? (bit(t.part, seq) ? n : len >> a.c.log_page) : 0;
+        const int32_t* const from = a.s.pages + (int64_t)(there ? seq : 0) * a.s.max_pages + place;
         struct __attribute__((packed, aligned(4))) Four { int32_t x[4]; };
         Four f = {{-1, -1, -1, -1}};
         if (place + 4 <= n) {
           f = *reinterpret_cast<const Four*>(from);
-        } else {
+        } else if (place < n) {
 #pragma unroll
           for (int j = 0; j < 3; ++j) f.x[j] = place + j < n ? from[j] : -1;
         }
@@ -220,24 +226,12 @@ __device__ inline void mark_in_lds(const PageArgs& a, const LdsTables& t) {
         for (int j = 0; j < 4; ++j) page[k][j] = f.x[j];
       }
 #pragma unroll
-      for (int k = 0; k < kAtOnce; ++k) {
-        const int seq = s0 + k * kPlanWaves;
-        if (seq >= a.s.n_seqs) break;
-        const int32_t len = t.len[seq], full = len >> a.c.log_page;
-        if (first >= pages_for(a, len)) continue;
-        const bool reads = Fork && bit(t.child, seq), part = Fork && bit(t.part, seq);
-        uint32_t bits[4], before[4];
+      for (int k = 0; k < kAtOnce; ++k)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const int32_t x = page[k][j];
-          const bool there = (uint32_t)x < (uint32_t)a.c.n_pages;
-          bits[j] = there ? (reads && (place + j < full || part) ? kHeld | kRead : kHeld) << 2 * (x & 15) : 0u;
-          before[j] = t.marks.two[there ? x >> 4 : 0];
+          const uint32_t x = page[k][j];
+          if (x < (uint32_t)a.c.n_pages) atomicOr(t.marks.two + (x >> 4), (place + j < readable[k] ? kHeld | kRead : kHeld) << (2 * x & 31));
         }
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if ((before[j] & bits[j]) != bits[j]) atomicOr(t.marks.two + (page[k][j] >> 4), bits[j]);      // (many sequences name the same pages)
-      }
     }
 }
 
