@@ -541,7 +541,7 @@ int fcp_cache_evict(const fcp_cache* cache, const int32_t* pages, const int32_t*
  * Answering a prompt with several continuations: fcp_beam_select says which beams go on with which tokens, fcp_cache_fork gives every one of them its table.
  *
  * fcp_cache_fork -- the tables of the next step's sequences out of those of this step's.  Sequence i of the next step has the tokens of sequence parent[i] (a number outside
- * 0 .. n_seqs - 1: none) and room for news[i] more (negative: 0); new_len[i] counts both, at most max_pages * page_tokens.  One sequence may have several children (beams, samples; a
+ * 0 .. n_seqs - 1: none) and room for news[i] more (negative: 0); new_len[i] counts both, at most max_pages * page_tokens: tokens past that have no room, and are not to be appended.  One sequence may have several children (beams, samples; a
  * prompt's first continuations), one child (it goes on) or none (it ends).
  *   - Pages that are only read are shared.
  *   - A page that holds tokens of the parent and gets new ones must belong to one sequence: where several would write it the lowest keeps it, but none does if others only read it or it is

@@ -196,7 +196,9 @@ class BeamDecoder:
     def prefill(self, q, k, v, lens):
         """The prompts, as CacheDecoder.prefill."""
         out = self.prompts.prefill(q, k, v, lens)
+        self.prompts._upload()                               # (prompts may all be empty)
         self.pages, self.kv_len = self.prompts.pages_d, self.prompts.kv_len_d
+        self._longest = int(np.max(lens, initial=0))         # tokens of the longest sequence
         self._shared = self.prompts._to(np.asarray(lens) // self.prompts.P * self.prompts.P)     # (the page in which a prompt ends is every beam's own)
         self.score, self.done = torch.zeros(self.n, device=self.device), torch.zeros(self.n, dtype=torch.uint8, device=self.device)
         self.chosen, self.history, self.steps = None, [], 0
@@ -204,6 +206,8 @@ class BeamDecoder:
 
     def select(self, logits):
         """The best tokens behind the beams so far: (tokens, parents) [n_prompts, beams], best first; parents are rows of the logits, -1 where there is no candidate.  self.score, self.done follow."""
+        if self.chosen is not None:
+            raise ValueError("step() takes the rows of the tokens that were chosen before the next ones are")
         width = 1 if not self.history else self.beams
         mk = lambda dt: torch.empty(self.n, self.beams, dtype=dt, device=self.device)
         parent, token, score, done = mk(torch.int32), mk(torch.int32), mk(torch.float32), mk(torch.uint8)
@@ -222,6 +226,8 @@ class BeamDecoder:
             raise ValueError("select() chooses the tokens whose rows step() takes")
         dec, rows = self.prompts, self.n * self.beams
         dec._fit(q, k, v, rows)
+        if self._longest == dec.pages.shape[1] * dec.P:
+            raise MemoryError("a sequence's table is full")
         o, lse = torch.empty(q.shape, dtype=torch.bfloat16, device=self.device), torch.empty(dec.hq, rows, dtype=torch.float32, device=self.device)
         pages, kv_len = self._tables[self.steps % 2]
         B.fcp_cache_fork(self.cache, self.pages, self.kv_len, self.chosen, self._ones, pages, kv_len, self.counts, self._fork_scratch)
@@ -233,6 +239,7 @@ class BeamDecoder:
         B.fcp_cache_attn_shared(self.cache, q, self._cu, kv_len, pages, self._groups, self._shared, self.scale, o, lse, self._attn_scratch)
         self.pages, self.kv_len, self.chosen = pages, kv_len, None
         self.steps += 1
+        self._longest += 1
         return o, lse
 
     def compact(self):

@@ -100,6 +100,42 @@ def test_too_few_pages_leave_the_beams_as_they_were():
 
 
 @pytest.mark.gpu
+def test_calls_out_of_turn_and_full_tables_are_refused():
+    """Two choices without a step between them; a step where the longest sequence's table is full, which would write over its last token."""
+    import torch
+    from paper_2602_21788_amd.decode import BeamDecoder
+    rows = lambda n, h: torch.randn(n, h, 64, device="cuda").to(torch.bfloat16)
+    dec = BeamDecoder(2, 2, 40, 2, 2, 2, 64, page_tokens=16)
+    dec.prefill(rows(33, 2), rows(33, 2), rows(33, 2), [30, 3])
+    for t in range(3):
+        dec.select(torch.randn(4 if t else 2, 50, device="cuda"))
+        with pytest.raises(ValueError):
+            dec.select(torch.randn(4, 50, device="cuda"))
+        if t < 2:
+            dec.step(rows(4, 2), rows(4, 2), rows(4, 2))
+    codes, pages = dec.cache.k.view(torch.int8).clone(), dec.pages.clone()
+    with pytest.raises(MemoryError):
+        dec.step(rows(4, 2), rows(4, 2), rows(4, 2))
+    assert torch.equal(dec.cache.k.view(torch.int8), codes) and torch.equal(dec.pages, pages) and dec.kv_len.tolist() == [32, 32, 5, 5]
+
+
+@pytest.mark.gpu
+def test_prompts_without_tokens():
+    import torch
+    from paper_2602_21788_amd.decode import BeamDecoder
+    rows = lambda n, h: torch.randn(n, h, 64, device="cuda").to(torch.bfloat16)
+    for lens in ([0, 0], [0, 20]):
+        dec = BeamDecoder(2, 2, 40, 2, 2, 2, 64, page_tokens=16, rot_dim=0)
+        dec.prefill(rows(sum(lens), 2), rows(sum(lens), 2), rows(sum(lens), 2), lens)
+        dec.select(torch.randn(2, 50, device="cuda"))
+        v = rows(4, 2)
+        o, lse = dec.step(rows(4, 2), rows(4, 2), v.clone())
+        assert dec.kv_len.tolist() == [m + 1 for m in lens for _ in range(2)]
+        # a token alone sees its own value, in e4m3 (half a step of 2^-3), which a bf16 rounding of O follows
+        assert float((o[:2].float() - v[:2].float()).abs().max()) <= float(v[:2].abs().max()) * (2.0 ** -4 + 2.0 ** -8)
+
+
+@pytest.mark.gpu
 def test_ended_beams_and_beams_without_candidates():
     """A vocabulary of two tokens, one of which ends a beam: fewer candidates than beams at first, then finished ones stay at their score."""
     import torch
