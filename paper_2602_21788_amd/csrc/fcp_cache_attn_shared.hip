@@ -183,7 +183,7 @@ constexpr int kPartThreads = 1024;
 __global__ __launch_bounds__(kPartThreads) void parts_kernel(SharedArgs a) { place_parts<kPartThreads>(a, a.tables); }
 
 // The same by every block of a line's launch, where there are up to kLocal sequences: a thread looks at a sequence and at a group, and everything is asked for at once.  (A launch of one block takes
-// 5 to 7 us.)  The first block leaves the tables for the join.
+// 5 to 7 us.)  The join learns from the first block whether there is anything to do.
 struct LocalTables { Entry e[2][kLocal]; int32_t before[2][kLocal + 2]; };
 __device__ inline Tables tables_of(const SharedArgs& a, LocalTables& own) {
   if (!a.local) return a.tables;
@@ -239,11 +239,7 @@ __device__ inline Tables tables_of(const SharedArgs& a, LocalTables& own) {
     t.before_own[a.s.n_seqs + 1] = whole;
   }
   __syncthreads();
-  if (blockIdx.x == 0) {
-    if (is_group) a.tables.common[i] = t.common[i], a.tables.before_common[i] = at[0];
-    if (is_seq) a.tables.own[i] = t.own[i], a.tables.before_own[i] = at[1];
-    if (i < 2) a.tables.before_common[a.n_groups + i] = t.before_common[a.n_groups + i], a.tables.before_own[a.s.n_seqs + i] = t.before_own[a.s.n_seqs + i];
-  }
+  if (blockIdx.x == 0 && i == 0) a.tables.before_own[a.s.n_seqs] = total[1];
   return t;
 }
 

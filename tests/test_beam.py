@@ -130,6 +130,15 @@ def test_sizes(dtype, prompts, beams, vocab, keep, pad):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("prompts, beams, vocab, keep, pad", [(260, 4, 16385, 5, 3), (128, 8, 17000, 64, 0), (40, 8, 70001, 33, 1), (1030, 1, 5001, 1, 0)])
+def test_sizes_of_chunks_of_16384(dtype, prompts, beams, vocab, keep, pad):
+    rng = np.random.default_rng(vocab + keep)
+    x = rng.standard_normal((prompts * beams, vocab)) * 2.5
+    _check(x, _scores(rng, prompts * beams), beams, keep, dtype=dtype, pad=pad)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("rows", [6, 600])                     # chunks of 2048, of 8192
 @pytest.mark.parametrize("kind", ["equal", "rising", "falling", "two", "steps", "one_high", "zeros"])
 def test_orders(rows, kind):

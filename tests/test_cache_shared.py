@@ -113,6 +113,29 @@ def test_sizes(P, D, hq, hkv, groups, fmt):
     assert np.array_equal(w, b.ref.weight.astype(np.float32))
 
 
+# more sequences than a block has threads; own parts that are divided, alone and beside short ones; both
+MANY_OR_LONG = [
+    (16, 64, 2, 2, [(48, one(1, 20)) for _ in range(150)]), (32, 64, 4, 1, [(100, one(*[i % 40 + 1 for i in range(600)])), (0, one(3)), (64, [(5, 0), (9, 1)] * 300)]),
+    (16, 64, 16, 1, [(40, [(20, 3), (9, 2), (4, 4)]) for _ in range(100)]), (64, 128, 8, 2, [(200, one(1100, 5, 3000)), (64, one(1025, 1))]), (128, 64, 4, 4, [(1000, one(2500, 1030))]),
+    (64, 64, 2, 2, [(64, one(*[1400 if i == 77 else i % 9 + 1 for i in range(300)]))]), (64, 128, 40, 8, [(130, [(1300, 9), (1200, 3)])])]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("P, D, hq, hkv, groups", MANY_OR_LONG)
+def test_many_sequences_and_long_ones(P, D, hq, hkv, groups):
+    Batch(P, D, hq, hkv, groups, "int8" if P == 64 else "e4m3").check()
+
+
+@pytest.mark.gpu
+def test_many_sequences_whose_tables_fall():
+    b = Batch(16, 64, 2, 2, [(48, one(1, 20)) for _ in range(150)], "int8")
+    for name, at, to in (("cu", 200, 2 ** 31 - 1), ("cu", 299, 0), ("groups", 100, 301), ("groups", 70, 1), ("groups", 0, -1)):
+        table = getattr(b, name).copy()
+        table[at] = to
+        o, lse = b.run(fill=7.0, **{name: table})
+        assert (o == 7).all() and (lse == 7).all(), (name, at)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("fmt", FORMATS)
 def test_less_is_shared_than_said(fmt):
