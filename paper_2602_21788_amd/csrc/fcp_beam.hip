@@ -5,10 +5,13 @@
 //
 // First launch: a block takes a chunk of a row, 32 neighbouring logits a thread (8 where there are few rows), which stay in registers for three looks:
 //   * the greatest of every four threads, 64 in all; the keep-th greatest of those 64, T, found bit by bit: at least `keep` logits of the chunk are T or more;
-//   * the sum of exp(x - greatest): the exponential as a polynomial in 64 bits, which this card multiplies as fast as 32;
+//   * the sum of exp(x - greatest);
 //   * logits beyond T, and those equal to it in T's four threads and earlier ones, go to a list in LDS.  Whatever the logits, they lie in `keep` groups of four threads, which bounds
 //     the list; as a rule it is little longer than `keep`.  The list is put in order by counting, a few hundred at a time.
 // Second launch: a block for each prompt joins the sums and finds the best candidates of all lists the same way.
+//
+// 64 prompts of 8 beams, 131072 bf16 logits each, 16 kept: 43.9 and 9.8 us, 50.1 together (a copy's rate would read the logits in 27); vector instructions bound the first, loads and barriers that wait for
+// each other the second, and all of small calls: one prompt of 4 beams over 32000 tokens 5.3 and 6.2 us, 11.3 together.
 #include <float.h>
 
 #include "fcp_device.h"
@@ -48,46 +51,67 @@ __device__ inline double score_of(uint64_t order) { return __longlong_as_double(
 // A constant in scalar registers: an instruction of the vector unit takes one, and the compiler would rather move it to vector registers every time.
 __device__ inline double scalar(double x) { asm volatile("" : "+s"(x)); return x; }
 
-// exp(x - top), x <= top, but for a factor that is the same for all x: 2^n times a polynomial in f, n + f = x log2(e), |f| <= 1/2, n counted from top's.  The integer part is found in 32 bits
-// (64-bit instructions take twice as long), the fraction in 64.  The coefficients are a least-squares fit on Chebyshev nodes with weights 2^-f; the relative error is at most 4.3e-11, which is how
-// far the logarithm of a sum may be off.  What lies more than 700 below the top, and NaN, counts as 700 below.
-// Far: |top| is so large that x log2(e) has no good integer part in 32 bits; there the difference is formed first.
-struct ExpBelow {
+// exp(d), d <= 0, in 64 bits: 2^n times a polynomial in f, n + f = d log2(e), |f| <= 1/2.  The coefficients are a least-squares fit on Chebyshev nodes with weights 2^-f; the relative error is at most
+// 4.3e-11.  What is below -700, and NaN, counts as -700.
+struct Exp {
   double log2e = scalar(1.4426950408889634074);
   double c[8] = {scalar(0x1.ffffffffac502p-1), scalar(0x1.62e42ff12cfc5p-1), scalar(0x1.ebfbe0a416e10p-3), scalar(0x1.c6b08a80840e9p-5), scalar(0x1.3b29dcb134a69p-7),
                  scalar(0x1.5d8a9fcfc7546p-10), scalar(0x1.4469d4b220e3bp-13), 0x1.fde1039ee67bfp-17};
-  static constexpr float kShift = 12582912.f;              // 1.5 * 2^23: a sum's low bits are the rounded number
-  double top;
-  float lowest;
-  int32_t base;                                            // top's integer part, shifted
-  __device__ explicit ExpBelow(float t) : top(t), lowest(t - 700.f), base(__float_as_int(__builtin_fmaf(t, 1.44269504f, kShift))) {}
-  // 2^n p(f); n: shifted
-  __device__ double scaled(double f, int32_t n) const {
+  __device__ double operator()(double d) const {
+    const double t = fmax(d, -700.0) * log2e, shifted = t + 6755399441055744.0;      // 1.5 * 2^52: a sum's low bits are the rounded number
+    const double f = t - (shifted - 6755399441055744.0);
     double p = c[7];
 #pragma unroll
     for (int i = 6; i >= 0; --i) p = __builtin_fma(p, f, c[i]);
     u32x2 u = __builtin_bit_cast(u32x2, p);
-    u[1] += (uint32_t)n << 20;                             // (added to the exponent, in the upper word)
+    u[1] += __builtin_bit_cast(u32x2, shifted)[0] << 20;   // (n, added to the exponent, in the upper word)
     return __builtin_bit_cast(double, u);
   }
-  template <bool Far>
-  __device__ double of(float x) const {
-    if constexpr (Far) {
-      return of_difference((double)x - top);
-    } else {
-      x = fmaxf(x, lowest);
-      const float shifted = __builtin_fmaf(x, 1.44269504f, kShift);
-      return scaled(__builtin_fma((double)x, log2e, -(double)(shifted - kShift)), __float_as_int(shifted) - base);
-    }
+};
+
+// Sums of exp(x), |greatest x| <= 1024: exp(x) = 2^n 2^(k / 1024) e^r, n + k / 1024 + r / ln 2 = x log2(e), |r| <= ln 2 / 2048 and a little.  2^(k / 1024) comes from a table in LDS, in 64 bits; r and
+// e^r - 1 = r + r^2 / 2 + .. take 32, which is enough because they are small: r twice and e^r - 1 once are off by half a step of 2^-35, 1.46e-11, and r^3 / 6 is at most 1e-11, so a term is off by
+// 5.4e-11 of itself at most, and that is how far the logarithm of a sum may be off.  Vector instructions bound the launch, and one in 64 bits takes as long as two: 512 rows of 131072 bf16 logits take 43.9 us
+// so, 49.5 with a parabola in 64 bits behind a table of 512, 52.6 with the polynomial of Exp; without any sum 30, the memory's 27 of them.  What lies more than 700 below the greatest, and NaN, counts as 700 below.
+constexpr int kPowers = 1024;
+// The upper words of the powers lack k << 10: an element's integer part, n and k, is added whole.
+__device__ inline void fill_powers(double* powers) {
+  static_assert(kPowers == 4 * kThreads, "four a thread");
+  const double x = (double)threadIdx.x * (0.69314718055994530942 / kPowers);         // below 0.174: what is left out of the series is below 7e-15
+  double p = 1.0 / 362880;
+  const double c[9] = {1, 1, 1.0 / 2, 1.0 / 6, 1.0 / 24, 1.0 / 120, 1.0 / 720, 1.0 / 5040, 1.0 / 40320};
+#pragma unroll
+  for (int i = 8; i >= 0; --i) p = __builtin_fma(p, x, c[i]);
+  const double quarter[4] = {1, 1.18920711500272106672, 1.41421356237309504880, 1.68179283050742908606};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int k = threadIdx.x + i * kThreads;
+    u32x2 u = __builtin_bit_cast(u32x2, p * quarter[i]);
+    u[1] -= k << 10;
+    powers[k] = __builtin_bit_cast(double, u);
   }
-  // Sums of of(x) times exp(reference) are sums of exp(x).
-  template <bool Far>
-  __device__ double reference() const { return Far ? top : (double)(__int_as_float(base) - kShift) * 0.69314718055994530942; }
-  // exp(d), d <= 0
-  __device__ double of_difference(double d) const {
-    const double t = fmax(d, -700.0) * log2e, shifted = t + 6755399441055744.0;      // 1.5 * 2^52
-    return scaled(t - (shifted - 6755399441055744.0), (int32_t)__builtin_bit_cast(u32x2, shifted)[0]);
+}
+struct NearSum {
+  static constexpr float kShift = 12582912.f, kScale = 1477.3197f;       // 1.5 * 2^23: a sum's low bits are the rounded number; 1024 log2(e)
+  const double* powers;
+  float base, shift, lowest;                               // base: 1024 n of the greatest
+  double sum = 0, rest = 0;
+  __device__ NearSum(const double* powers, float top)
+      : powers(powers), base(__int_as_float(__float_as_int(__builtin_fmaf(top, kScale, kShift)) & ~(kPowers - 1)) - kShift), shift(kShift - base), lowest(top - 700.f) {}
+  __device__ void add(float x) {
+    x = __builtin_amdgcn_fmed3f(x, lowest, FLT_MAX);       // (one instruction; the greater of two would be quieted first; of NaN and two others it is the lesser)
+    const float shifted = __builtin_fmaf(x, kScale, shift), n = shifted - shift;
+    const float r = __builtin_fmaf(n, 0x1.05c61p-39f, __builtin_fmaf(n, -0x1.62e43p-11f, x)), p = __builtin_fmaf(0.5f * r, r, r);       // ln 2 / 1024 in two parts
+    const uint32_t i = __float_as_uint(shifted);           // (the shift's own bits lie above those that are used)
+    u32x2 u = __builtin_bit_cast(u32x2, *reinterpret_cast<const double*>(reinterpret_cast<const char*>(powers) + (i << 3 & 8 * (kPowers - 1))));
+    u[1] += i << 10;                                       // (to the exponent, in the upper word)
+    const double power = __builtin_bit_cast(double, u);
+    sum += power;
+    rest = __builtin_fma(power, (double)p, rest);
   }
+  // times exp(reference): the sum of exp(x)
+  __device__ double all() const { return sum + rest; }
+  __device__ double reference() const { return (double)base * (0.69314718055994530942 / kPowers); }
 };
 
 __device__ inline double sum_of_wave(double x) {
@@ -96,22 +120,26 @@ __device__ inline double sum_of_wave(double x) {
   return x;
 }
 
-// E elements from `from` on, of which those at 0 .. there - 1 exist; the others count as -inf.
-template <class T, int E>
-__device__ inline void load_row(const T* from, int there, float (&v)[E]) {
+// E elements from `from` on, of which those at 0 .. there - 1 exist; the others count as -inf.  meanwhile: what else there is to do before they arrive.
+template <class T, int E, class Meanwhile>
+__device__ inline void load_row(const T* from, int there, float (&v)[E], Meanwhile meanwhile) {
   if (there >= E) {
     constexpr int W = 16 / sizeof(T);
     struct __attribute__((packed, aligned(sizeof(T)))) Words { uint32_t w[4]; };     // (rows may begin at any element)
+    Words r[E / W];
+#pragma unroll
+    for (int i = 0; i < E / W; ++i) r[i] = *reinterpret_cast<const Words*>(from + W * i);
+    meanwhile();
 #pragma unroll
     for (int i = 0; i < E / W; ++i) {
-      const Words r = *reinterpret_cast<const Words*>(from + W * i);
 #pragma unroll
       for (int j = 0; j < W; ++j) {
-        if constexpr (sizeof(T) == 2) v[W * i + j] = __uint_as_float(j % 2 ? r.w[j / 2] & 0xffff0000u : r.w[j / 2] << 16);
-        else v[W * i + j] = __uint_as_float(r.w[j]);
+        if constexpr (sizeof(T) == 2) v[W * i + j] = __uint_as_float(j % 2 ? r[i].w[j / 2] & 0xffff0000u : r[i].w[j / 2] << 16);
+        else v[W * i + j] = __uint_as_float(r[i].w[j]);
       }
     }
   } else {
+    meanwhile();
 #pragma unroll
     for (int i = 0; i < E; ++i) v[i] = i < there ? (float)from[i] : -INFINITY;
   }
@@ -163,20 +191,19 @@ __host__ __device__ constexpr int list_room(int keep, int E) { return keep * kPe
 template <class T, int E>
 __global__ __launch_bounds__(kThreads) void beam_rows_kernel(BeamArgs a) {
   extern __shared__ __align__(16) uint16_t list[];         // places in the chunk
-  static_assert(kThreads * E <= 1 << 16, "they fit");
   __shared__ uint64_t room[kThreads], best[FCP_BEAM_MAX_KEEP];
   constexpr int kStaged = 8;           // threads of a wave whose logits are looked at together
   __shared__ float groups[kGroups];
   __shared__ __align__(16) float staged[kThreads / 64][kStaged * E];
   __shared__ int32_t staged_by[kThreads / 64][kStaged];
-  __shared__ double sums[kThreads / 64];
+  __shared__ double sums[kThreads / 64], powers[kPowers];
   __shared__ int32_t listed;
   const int row = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const float score = a.score[row];
   if (!(score > -INFINITY) || (a.done && a.done[row])) return;           // offers nothing, or one candidate whatever its logits
   const int first = chunk * (kThreads * E) + (int)threadIdx.x * E;
   float v[E];
-  load_row<T, E>(static_cast<const T*>(a.logits) + (int64_t)row * a.row + first, a.vocab - first, v);
+  load_row<T, E>(static_cast<const T*>(a.logits) + (int64_t)row * a.row + first, a.vocab - first, v, [&] { fill_powers(powers); });
   float top = -INFINITY;
 #pragma unroll
   for (int i = 0; i < E; ++i) top = fmaxf(top, v[i]);      // (NaN is passed over)
@@ -203,15 +230,17 @@ __global__ __launch_bounds__(kThreads) void beam_rows_kernel(BeamArgs a) {
   const float border = value_of(least), most = wave_top(mine);
   double sum = 0, reference = 0;
   if (most > -INFINITY) {
-    const ExpBelow e(most);
-    const bool far = fabsf(most) > 1024.f;
-    reference = far ? e.template reference<true>() : e.template reference<false>();
-    if (!far) {
+    if (fabsf(most) <= 1024.f) {
+      NearSum near(powers, most);
 #pragma unroll
-      for (int i = 0; i < E; ++i) sum += e.template of<false>(v[i]);
+      for (int i = 0; i < E; ++i) near.add(v[i]);
+      sum = near.all();
+      reference = near.reference();
     } else {
+      const Exp e;
 #pragma unroll
-      for (int i = 0; i < E; ++i) sum += e.template of<true>(v[i]);
+      for (int i = 0; i < E; ++i) sum += e((double)v[i] - most);
+      reference = most;
     }
     // Few threads have something for the list: the wave looks at all logits of eight of them at once.
     for (uint64_t who = __ballot(own_top >= border); who;) {
@@ -261,7 +290,6 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a) {
   __shared__ uint32_t groups[kGroups];
   __shared__ Candidate best[FCP_BEAM_MAX_KEEP];
   __shared__ int32_t listed;
-  constexpr int kOfGroup = kJoinThreads / kGroups;
   const int row0 = blockIdx.x * a.beams, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int per_beam = a.chunks * a.keep, all = a.beams * per_beam;      // (below 2^30: 2^24 chunks in all)
   // what a thread holds of the lists, asked for before the sums are joined: a logit of a beam, or its score where it is done
@@ -291,12 +319,13 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a) {
       if (sums[2 * c] > 0) most = fmax(most, sums[2 * c + 1]);
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) most = fmax(most, __shfl_xor(most, d));
-    const ExpBelow e(0.f);
+    const Exp e;
     for (int c = lane; c < a.chunks; c += 64)
-      if (sums[2 * c] > 0) sum += sums[2 * c] * e.of_difference(sums[2 * c + 1] - most);
+      if (sums[2 * c] > 0) sum += sums[2 * c] * e(sums[2 * c + 1] - most);
     sum = sum_of_wave(sum);
     if (lane == 0) lse[b] = most + log(sum);
   }
+  if (threadIdx.x < kGroups) groups[threadIdx.x] = 0;
   if (threadIdx.x == 0) listed = 0;
   __syncthreads();
   const Candidate none = {0, 0};
@@ -312,10 +341,9 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a) {
       top = max(top, (uint32_t)(c[i].score >> 32));
     }
     if (q0 + kJoinThreads * kJoined < all) ask(q0 + kJoinThreads * kJoined);
-    // The border, by the upper words of the scores' orders (20 bits of a mantissa): whatever reaches it may be among the best.
-#pragma unroll
-    for (int d = 1; d < kOfGroup; d *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, d));
-    if (threadIdx.x % kOfGroup == 0) groups[threadIdx.x / kOfGroup] = top;
+    // The border, by the upper words of the scores' orders (20 bits of a mantissa): whatever reaches it may be among the best.  A group is a lane of all waves: a list, whose best are next to each other,
+    // lies in different ones.
+    atomicMax(groups + lane, top);
     __syncthreads();
     const uint32_t border = max(greatest(groups[lane], a.keep, 0), 1u);
 #pragma unroll
@@ -327,6 +355,7 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a) {
     best_of<kJoinThreads>(best, room, n, a.keep, [](const Candidate& x, const Candidate& y) { return greater(x, y); }, [&](int i) { return found[i]; });
     kept = min(n, a.keep);
     if ((int)threadIdx.x < kept) found[threadIdx.x] = best[threadIdx.x];
+    if (threadIdx.x < kGroups) groups[threadIdx.x] = 0;
     if (threadIdx.x == 0) listed = 0;
     __syncthreads();
   }
@@ -347,7 +376,7 @@ struct BeamPlan { int32_t each, chunks; int64_t blocks; };
 BeamPlan plan_beam(int64_t rows, int32_t vocab) {
   auto chunks = [&](int64_t each) { return (vocab + kThreads * each - 1) / (kThreads * each); };
   BeamPlan p;
-  p.each = rows * chunks(64) >= 1024 ? 64 : rows * chunks(32) >= 512 ? 32 : 8;
+  p.each = rows * chunks(32) >= 512 ? 32 : 8;
   p.chunks = (int32_t)chunks(p.each);
   p.blocks = rows * p.chunks;
   return p;
@@ -366,7 +395,7 @@ int check_beam(const char* who, int32_t n_prompts, int32_t beams, int32_t vocab,
 
 template <class T, int E>
 int launch_rows(const BeamArgs& a, const BeamPlan& p, hipStream_t st) {
-  const int bytes = list_room(a.keep, E) * 2;              // up to 32 KB
+  const int bytes = list_room(a.keep, E) * 2;              // up to 16 KB
   beam_rows_kernel<T, E><<<dim3((unsigned)p.blocks), dim3(kThreads), bytes, st>>>(a);
   FCP_HIP_CHECK(hipGetLastError());
   return FCP_OK;
@@ -408,8 +437,7 @@ extern "C" int fcp_beam_select(const void* logits, int32_t type, int64_t logits_
   a.sums = reinterpret_cast<double*>(at + pad_to((size_t)p.blocks * keep * 8, 256));
   hipStream_t st = static_cast<hipStream_t>(stream);
   const bool bf16 = type == FCP_BF16;
-  if (int rc = p.each == 64 ? (bf16 ? launch_rows<__bf16, 64>(a, p, st) : launch_rows<float, 64>(a, p, st))
-             : p.each == 32 ? (bf16 ? launch_rows<__bf16, 32>(a, p, st) : launch_rows<float, 32>(a, p, st))
+  if (int rc = p.each == 32 ? (bf16 ? launch_rows<__bf16, 32>(a, p, st) : launch_rows<float, 32>(a, p, st))
                             : (bf16 ? launch_rows<__bf16, 8>(a, p, st) : launch_rows<float, 8>(a, p, st)))
     return rc;
   beam_join_kernel<<<dim3((unsigned)n_prompts), dim3(kJoinThreads), 0, st>>>(a);
