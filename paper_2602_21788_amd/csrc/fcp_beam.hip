@@ -141,7 +141,10 @@ __device__ inline void load_row(const T* from, int there, float (&v)[E], Meanwhi
   } else {
     meanwhile();
 #pragma unroll
-    for (int i = 0; i < E; ++i) v[i] = i < there ? (float)from[i] : -INFINITY;
+    for (int i = 0; i < E; ++i) {                          // (those behind the row's last logit ask for that one: a load under a condition is waited for before the next is asked for)
+      const float x = (float)from[min(i, there - 1)];
+      v[i] = i < there ? x : -INFINITY;
+    }
   }
 #pragma unroll
   for (int i = 0; i < E; ++i) v[i] = __builtin_canonicalizef(v[i]);      // (no signalling NaN: each fmaxf would see to that anew)
@@ -291,22 +294,23 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a) {
   __shared__ Candidate best[FCP_BEAM_MAX_KEEP];
   __shared__ int32_t listed;
   const int row0 = blockIdx.x * a.beams, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int per_beam = a.chunks * a.keep, all = a.beams * per_beam;      // (below 2^30: 2^24 chunks in all)
-  // what a thread holds of the lists, asked for before the sums are joined: a logit of a beam, or its score where it is done
+  const int lists = a.beams * a.chunks, all = lists * a.keep;            // (below 2^30: 2^24 chunks in all)
+  // What a thread holds of the lists, asked for before the sums are joined: a logit of a beam, or its score where it is done.  All lists' best come first, then all lists' second best, and so on: what
+  // follows a round is less than what was in it.
   uint64_t key[kJoined];
   int beam[kJoined];
   bool over[kJoined];
   auto ask = [&](int q0) {
 #pragma unroll
     for (int i = 0; i < kJoined; ++i) {
-      const int q = q0 + i * kJoinThreads + (int)threadIdx.x, b = q < all ? q / per_beam : 0, rest = q - b * per_beam;
+      const uint32_t q = q0 + i * kJoinThreads + (int)threadIdx.x, rank = q < all ? q / (uint32_t)lists : 0, l = q < all ? q - rank * lists : 0, b = l / (uint32_t)a.chunks;
       const float score = a.score[row0 + b];
       const bool done = a.done && a.done[row0 + b];
       const bool offers = q < all && score > -INFINITY;
-      const uint64_t k = a.lists[(int64_t)(row0 + b) * per_beam + (q < all ? rest : 0)];
+      const uint64_t k = a.lists[((int64_t)row0 * a.chunks + l) * a.keep + rank];
       beam[i] = b;
       over[i] = done;
-      key[i] = !offers ? 0 : !done ? k : rest == 0 ? (uint64_t)(uint32_t)~a.end_token | (uint64_t)1 << 32 : 0;
+      key[i] = !offers ? 0 : !done ? k : rank == 0 && l == b * a.chunks ? (uint64_t)(uint32_t)~a.end_token | (uint64_t)1 << 32 : 0;
     }
   };
   ask(0);
@@ -341,17 +345,18 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a) {
       top = max(top, (uint32_t)(c[i].score >> 32));
     }
     if (q0 + kJoinThreads * kJoined < all) ask(q0 + kJoinThreads * kJoined);
-    // The border, by the upper words of the scores' orders (20 bits of a mantissa): whatever reaches it may be among the best.  A group is a lane of all waves: a list, whose best are next to each other,
-    // lies in different ones.
-    atomicMax(groups + lane, top);
+    // The border, by the upper words of the scores' orders (20 bits of a mantissa): whatever reaches it may be among the best.  Groups are made so that a list's
+    // elements, `lists` threads apart, lie in different ones, as far as that goes.
+    atomicMax(groups + (lane + 5 * wave & kGroups - 1), top);
     __syncthreads();
-    const uint32_t border = max(greatest(groups[lane], a.keep, 0), 1u);
+    const uint32_t border = max(max(greatest(groups[lane], a.keep, 0), 1u), kept == a.keep ? (uint32_t)(best[kept - 1].score >> 32) : 0u);
 #pragma unroll
     for (int i = 0; i < kJoined; ++i)
       if (__ballot((uint32_t)(c[i].score >> 32) >= border))
         if ((uint32_t)(c[i].score >> 32) >= border) found[kept + atomicAdd(&listed, 1)] = c[i];
     __syncthreads();
     const int n = kept + listed;
+    if (n == kept && lists <= kJoinThreads * kJoined) break;             // (nor does anything follow)
     best_of<kJoinThreads>(best, room, n, a.keep, [](const Candidate& x, const Candidate& y) { return greater(x, y); }, [&](int i) { return found[i]; });
     kept = min(n, a.keep);
     if ((int)threadIdx.x < kept) found[threadIdx.x] = best[threadIdx.x];
