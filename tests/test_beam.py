@@ -139,6 +139,21 @@ def test_many_rows_of_long_chunks(dtype, prompts, beams, vocab, keep, pad):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [6, 600])                     # chunks of 2048, of 8192
+@pytest.mark.parametrize("first, last, keep", [(0, 1000, 64), (4000, 5500, 30), (8191, 8193, 3), (16000, 16700, 10), (100, 164, 64), (2047, 9000, 64)])
+def test_masks_that_leave_a_run_of_tokens(rows, dtype, first, last, keep):
+    """Few of a block's threads hold anything, or as few groups as are kept: more logits than a block lists may be among the best.  Beams of different masks beside each other, values that repeat."""
+    rng = np.random.default_rng(first + keep)
+    x = np.full((rows, 16700), -np.inf)
+    x[:, first:last] = np.round(rng.standard_normal((rows, last - first)) * 4, 1)
+    x[1] = np.where(rng.random(16700) < 0.01, x[1], -np.inf)
+    x[2, first:last] = 1.5
+    x[3, first:last] = np.where(np.arange(first, last) % 3 == 0, -7.0, -np.inf)
+    _check(x, _scores(rng, rows), 2, keep, dtype=dtype)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("rows", [7, 700])                     # chunks of 2048, of 8192
 @pytest.mark.parametrize("spread", [0.0, 1e-3, 5.0, 200.0, 900.0])
 def test_logarithm_of_the_sum(rows, spread):
