@@ -3,15 +3,16 @@
 // The score of token t behind beam b is score_b + x_bt - ln sum_u exp x_bu.  The order of a beam's tokens is that of its logits, so a beam offers its `keep` greatest logits, and the
 // logarithm is needed only to put beams beside each other.  Candidates of different beams can lie as near as they like: sums and scores are held in 64 bits.
 //
-// First launch: a block takes a chunk of a row, 32 neighbouring logits a thread (8 where there are few rows), which stay in registers for three looks:
-//   * the greatest of every four threads, 64 in all; the keep-th greatest of those 64, T, found bit by bit: at least `keep` logits of the chunk are T or more;
+// First launch: a block takes a chunk of a row, up to 32 neighbouring logits a thread (8 where there are few rows), which stay in registers for three looks:
+//   * the greatest of every four threads, 64 in all (of each of the 256 threads, if more than 32 are kept); the keep-th greatest of those, T, found bit by bit: at least `keep` logits of the chunk are T
+//     or more, and as a rule few others;
 //   * the sum of exp(x - greatest);
-//   * logits beyond T, and those equal to it in T's four threads and earlier ones, go to a list in LDS.  Whatever the logits, they lie in `keep` groups of four threads, which bounds
-//     the list; as a rule it is little longer than `keep`.  The list is put in order by counting, a few hundred at a time.
-// Second launch: a block for each prompt joins the sums and finds the best candidates of all lists the same way.
+//   * logits beyond T, and those equal to it in T's threads and earlier ones, go to a list in LDS, which is put in order by counting how many are beyond each.  Where there are more than the list has
+//     places, T becomes the keep-th greatest logit itself.
+// Second launch: a block for each prompt joins the sums and finds the best candidates of all lists the same way, all lists' best first.
 //
-// 64 prompts of 8 beams, 131072 bf16 logits each, 16 kept: 43.9 and 9.8 us, 50.1 together (a copy's rate would read the logits in 27); vector instructions bound the first, loads and barriers that wait for
-// each other the second, and all of small calls: one prompt of 4 beams over 32000 tokens 5.3 and 6.2 us, 11.3 together.
+// 64 prompts of 8 beams, 131072 bf16 logits each, 16 kept: 44.5 and 7.6 us, 48.4 together (a copy's rate would read the logits in 27); vector instructions bound the first, loads and barriers that wait
+// for each other the second, and all of small calls: one prompt of 4 beams over 32000 tokens 5.5 and 6.3 us, 11.5 together.
 #include <float.h>
 
 #include "fcp_device.h"
@@ -25,7 +26,7 @@ constexpr int kPerGroup = kThreads / kGroups;
 struct BeamArgs {
   const void* logits;
   int64_t row;
-  int32_t rows, beams, vocab, chunks, keep, end_token;
+  int32_t rows, beams, vocab, chunks, each, keep, end_token;       // each: logits of a thread
   const float* score;
   const uint8_t* done;
   int32_t* parent;
@@ -120,9 +121,9 @@ __device__ inline double sum_of_wave(double x) {
   return x;
 }
 
-// E elements from `from` on, of which those at 0 .. there - 1 exist; the others count as -inf.  meanwhile: what else there is to do before they arrive.
+// E elements from `from` on, of which the first `each` are the thread's and those at 0 .. there - 1 exist; the others count as -inf.  meanwhile: what else there is to do before they arrive.
 template <class T, int E, class Meanwhile>
-__device__ inline void load_row(const T* from, int there, float (&v)[E], Meanwhile meanwhile) {
+__device__ inline void load_row(const T* from, int there, int each, float (&v)[E], Meanwhile meanwhile) {
   if (there >= E) {
     constexpr int W = 16 / sizeof(T);
     struct __attribute__((packed, aligned(sizeof(T)))) Words { uint32_t w[4]; };     // (rows may begin at any element)
@@ -138,12 +139,16 @@ __device__ inline void load_row(const T* from, int there, float (&v)[E], Meanwhi
         else v[W * i + j] = __uint_as_float(r[i].w[j]);
       }
     }
+    if (each < E) {
+#pragma unroll
+      for (int i = 1; i < E; ++i) v[i] = i < each ? v[i] : -INFINITY;
+    }
   } else {
     meanwhile();
 #pragma unroll
     for (int i = 0; i < E; ++i) {                          // (those behind the row's last logit ask for that one: a load under a condition is waited for before the next is asked for)
       const float x = (float)from[min(i, there - 1)];
-      v[i] = i < there ? x : -INFINITY;
+      v[i] = i < min(there, each) ? x : -INFINITY;
     }
   }
 #pragma unroll
@@ -156,14 +161,16 @@ __device__ inline float wave_top(float x) {
   return x;
 }
 
-// Of the 64 numbers that a wave holds, a lane each, the rank-th greatest (from 1), bit for bit from the top: as many as are set from the lowest one on are known.
-__device__ inline uint32_t greatest(uint32_t x, int rank, int lowest_bit) {
+// The rank-th greatest (from 1) of the numbers that a wave holds, bit for bit from the top; reach(x): how many are x or more.  The bits below the lowest one to be looked at are ones where the sign's,
+// the highest, is not set, else zeros: such are the orders of bf16 numbers.
+template <class Reach>
+__device__ inline uint32_t greatest(Reach reach, int rank, int lowest_bit) {
   uint32_t found = 0;
   for (int b = 31; b >= lowest_bit; --b) {
     const uint32_t next = found | 1u << b;
-    if (__popcll(__ballot(x >= next)) >= rank) found = next;
+    if (reach(next) >= rank) found = next;
   }
-  return found;
+  return found >> 31 ? found : found | ((1u << lowest_bit) - 1);
 }
 
 // The best `keep` of n elements that differ from each other, in order: best[0 .. min(n, keep) - 1].  Ranks by counting, Threads elements at a time, the best so far among them, several threads an element where
@@ -190,17 +197,17 @@ __device__ inline void best_of(K* best, K* room, int n, int keep, Greater greate
   }
 }
 
-constexpr int kListed = 512;           // places of the list: as long as counting takes no longer than looking for the least logit that is offered
+constexpr int kListed = 512;           // places of the list: counting takes about as long for so many as looking for the least logit that is offered
 
 // Where more logits may be among the best than the list has places - a mask leaves few groups something, or logits are equal: the keep-th greatest logit, bit by bit, over all that the block holds; then
 // exactly those beyond it, and of those equal to it the first.  How many are in the list.  reach: zeros.  (The logits are read again: kept in registers until here they
 // cost all blocks, 512 rows of 131072 logits 48.5 us instead of 44.5.)
 template <class T, int E>
-__device__ inline int list_best(const T* from, int there, int keep, uint16_t* list, int32_t* reach, int32_t* sums_before, int32_t& listed) {
+__device__ inline int list_best(const T* from, int there, int each, int keep, uint16_t* list, int32_t* reach, int32_t* sums_before, int32_t& listed) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   uint32_t order[E], least = 0;
   float v[E];
-  load_row<T, E>(from, there, v, [] {});
+  load_row<T, E>(from, there, each, v, [] {});
 #pragma unroll
   for (int i = 0; i < E; ++i) order[i] = v[i] > -INFINITY ? order_of(fminf(v[i], FLT_MAX) + 0.f) : 0;
   for (int b = 31; b >= 0; --b) {
@@ -210,7 +217,9 @@ __device__ inline int list_best(const T* from, int there, int keep, uint16_t* li
     for (int i = 0; i < E; ++i) n += (int)__popcll(__ballot(order[i] >= next));
     if (lane == 0) atomicAdd(reach + b, n);
     __syncthreads();
-    if (reach[b] >= keep) least = next;
+    const int all = reach[b];
+    if (all >= keep) least = next;
+    if (all == keep) break;
   }
   int beyond = 0, equal = 0;
 #pragma unroll
@@ -235,7 +244,7 @@ __device__ inline int list_best(const T* from, int there, int keep, uint16_t* li
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < E; ++i) {
-    const uint16_t place = (uint16_t)(threadIdx.x * E + i);
+    const uint16_t place = (uint16_t)(threadIdx.x * each + i);
     if (order[i] > least) list[atomicAdd(&listed, 1)] = place;
     else if (order[i] == least && least > 0 && rank < keep) list[rank++] = place;
   }
@@ -247,7 +256,7 @@ template <class T, int E>
 __global__ __launch_bounds__(kThreads, 7) void beam_rows_kernel(BeamArgs a) {
   __shared__ uint64_t room[kThreads], best[FCP_BEAM_MAX_KEEP];
   constexpr int kStaged = 8;           // threads of a wave whose logits are looked at together
-  __shared__ float groups[kGroups];
+  __shared__ __align__(16) float tops[kThreads];
   __shared__ __align__(16) float staged[kThreads / 64][kStaged * E];
   __shared__ int32_t staged_by[kThreads / 64][kStaged];
   __shared__ double sums[kThreads / 64], powers[kPowers];
@@ -257,34 +266,60 @@ __global__ __launch_bounds__(kThreads, 7) void beam_rows_kernel(BeamArgs a) {
   const int row = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const float score = a.score[row];
   if (!(score > -INFINITY) || (a.done && a.done[row])) return;           // offers nothing, or one candidate whatever its logits
-  const int first = chunk * (kThreads * E) + (int)threadIdx.x * E;
+  const int chunk0 = chunk * (kThreads * a.each), first = chunk0 + (int)threadIdx.x * a.each;
   float v[E];
   const T* const x = static_cast<const T*>(a.logits) + (int64_t)row * a.row + first;
-  load_row<T, E>(x, a.vocab - first, v, [&] { fill_powers(powers); });
+  load_row<T, E>(x, a.vocab - first, a.each, v, [&] { fill_powers(powers); });
   float top = -INFINITY;
 #pragma unroll
   for (int i = 0; i < E; ++i) top = fmaxf(top, v[i]);      // (NaN is passed over)
   const float own_top = fminf(top, FLT_MAX);
-  top = fmaxf(top, __shfl_xor(top, 1));
-  top = fmaxf(top, __shfl_xor(top, 2));
-  if (threadIdx.x % kPerGroup == 0) groups[threadIdx.x / kPerGroup] = top;
+  tops[threadIdx.x] = top;
   if (threadIdx.x == 0) listed = 0;
   if (threadIdx.x < 32) reach[threadIdx.x] = 0;
   __syncthreads();
-  const float unbounded = groups[lane], mine = fminf(unbounded, FLT_MAX) + 0.f;         // (-0 as 0)
+  const f32x4 four = *reinterpret_cast<const f32x4*>(tops + kPerGroup * lane);
+  const float unbounded = fmaxf(fmaxf(four[0], four[1]), fmaxf(four[2], four[3])), mine = fminf(unbounded, FLT_MAX) + 0.f;         // (-0 as 0)
   const bool infinite = __ballot(unbounded == INFINITY);
   if (infinite) {                                          // rare
 #pragma unroll
     for (int i = 0; i < E; ++i) v[i] = v[i] == INFINITY ? FLT_MAX : v[i];
   }
-  // the keep-th greatest group, of equal ones the lowest first.  (The lower half of a bf16 value is all zeros, in order_of all ones if it is negative.)
-  const uint32_t order = order_of(mine);
-  const bool half = sizeof(T) == 2 && !infinite;
-  uint32_t least = greatest(order, a.keep, half ? 16 : 0);
-  if (half && !(least >> 31)) least |= 0xffffu;
-  uint64_t equal = __ballot(order == least);
-  for (int k = a.keep - (int)__popcll(__ballot(order > least)); k > 1; --k) equal &= equal - 1;
-  const int at = __builtin_ctzll(equal);
+  // the keep-th greatest of the groups, or of the threads, of equal ones the lowest first, and its last thread
+  const int lowest_bit = sizeof(T) == 2 && !infinite ? 16 : 0;
+  uint32_t least;
+  int at;
+  // (of threads costs more, and leaves fewer to be counted: 96 rows of 32000, 64 kept, 49 us with groups, 22 so; with up to 32 kept about as many are left)
+  if (a.keep <= kGroups / 2) {
+    const uint32_t order = order_of(mine);
+    least = greatest([&](uint32_t x) { return (int)__popcll(__ballot(order >= x)); }, a.keep, lowest_bit);
+    uint64_t equal = __ballot(order == least);
+    for (int k = a.keep - (int)__popcll(__ballot(order > least)); k > 1; --k) equal &= equal - 1;
+    at = kPerGroup * __builtin_ctzll(equal) + kPerGroup - 1;
+  } else {
+    uint32_t order[kPerGroup];
+#pragma unroll
+    for (int i = 0; i < kPerGroup; ++i) order[i] = order_of(fminf(four[i], FLT_MAX) + 0.f);
+    auto reach = [&](uint32_t x) {
+      int n = 0;
+#pragma unroll
+      for (int i = 0; i < kPerGroup; ++i) n += (int)__popcll(__ballot(order[i] >= x));
+      return n;
+    };
+    least = greatest(reach, a.keep, lowest_bit);
+    int equal = 0, need = a.keep;                          // of the lane; of all lanes
+#pragma unroll
+    for (int i = 0; i < kPerGroup; ++i) {
+      equal += order[i] == least;
+      need -= (int)__popcll(__ballot(order[i] > least));
+    }
+    const int upto = wave_prefix_sum(equal);
+    const int found = __builtin_ctzll(__ballot(upto >= need));           // the lane that has the last one
+    int last = 0, k = need - (upto - equal);
+#pragma unroll
+    for (int i = kPerGroup - 1; i >= 0; --i) last = order[i] == least && equal-- == k ? i : last;
+    at = kPerGroup * found + __builtin_amdgcn_readlane(last, found);
+  }
   const float border = value_of(least), most = wave_top(mine);
   double sum = 0, reference = 0;
   if (most > -INFINITY) {
@@ -313,9 +348,9 @@ __global__ __launch_bounds__(kThreads, 7) void beam_rows_kernel(BeamArgs a) {
         const float x = staged[wave][j] + 0.f;
         const int by = staged_by[wave][j / E];
         // (the border itself counts in its own group and earlier ones)
-        if ((x > border || (x == border && by / kPerGroup <= at)) && x > -INFINITY) {
+        if ((x > border || (x == border && by <= at)) && x > -INFINITY) {
           const int k = atomicAdd(&listed, 1);
-          if (k < kListed) list[k] = (uint16_t)(by * E + j % E);
+          if (k < kListed) list[k] = (uint16_t)(by * a.each + j % E);
         }
       }
       wave_exchange();
@@ -326,9 +361,8 @@ __global__ __launch_bounds__(kThreads, 7) void beam_rows_kernel(BeamArgs a) {
   if (lane == 0) sums[wave] = sum;
   __syncthreads();
   int n = listed;
-  if (__builtin_expect(n > kListed, false)) n = list_best<T, E>(x, a.vocab - first, a.keep, list, reach, sums_before, listed);
+  if (__builtin_expect(n > kListed, false)) n = list_best<T, E>(x, a.vocab - first, a.each, a.keep, list, reach, sums_before, listed);
   // (the logits themselves are read again: with them the list would take four times the LDS, and fewer blocks would run at once)
-  const int chunk0 = chunk * (kThreads * E);
   const T* const x0 = static_cast<const T*>(a.logits) + (int64_t)row * a.row + chunk0;
   best_of<kThreads, false>(best, room, n, a.keep, [](uint64_t x, uint64_t y) { return x > y; },
                     [&](int i) { return (uint64_t)order_of(fminf((float)x0[list[i]], FLT_MAX) + 0.f) << 32 | (uint32_t)~(chunk0 + list[i]); });
@@ -409,7 +443,8 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a) {
     // elements, `lists` threads apart, lie in different ones, as far as that goes.
     atomicMax(groups + (lane + 5 * wave & kGroups - 1), top);
     __syncthreads();
-    const uint32_t border = max(max(greatest(groups[lane], a.keep, 0), 1u), kept == a.keep ? (uint32_t)(best[kept - 1].score >> 32) : 0u);
+    const uint32_t of_group = groups[lane];
+    const uint32_t border = max(max(greatest([&](uint32_t x) { return (int)__popcll(__ballot(of_group >= x)); }, a.keep, 0), 1u), kept == a.keep ? (uint32_t)(best[kept - 1].score >> 32) : 0u);
 #pragma unroll
     for (int i = 0; i < kJoined; ++i)
       if (__ballot((uint32_t)(c[i].score >> 32) >= border))
@@ -436,13 +471,15 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a) {
   }
 }
 
-// How a call is divided: as many neighbouring logits a thread as leave four blocks, or two, for every CU; 8 where there are fewer.
-struct BeamPlan { int32_t each, chunks; int64_t blocks; };
+// How a call is divided: chunks of up to 8192 logits where they make three blocks for two CUs, else of up to 2048; all chunks of a row are alike but for the last one's end.  2048 / 8192, bf16 but for the
+// second: 4 rows of 32000 10.8 / 12.4 us, 8 prompts of 5 over 50001 fp32 13.8 / 14.2, 8 of 8 over 32000 13.9 / 14.1, 12 13.9 / 13.7, 16 17.6 / 15.1, 64 34.5 / 24.1.
+struct BeamPlan { int32_t room, chunks, each; int64_t blocks; };        // room: logits that a thread has registers for
 BeamPlan plan_beam(int64_t rows, int32_t vocab) {
   auto chunks = [&](int64_t each) { return (vocab + kThreads * each - 1) / (kThreads * each); };
   BeamPlan p;
-  p.each = rows * chunks(32) >= 512 ? 32 : 8;
-  p.chunks = (int32_t)chunks(p.each);
+  p.room = rows * chunks(32) >= 384 ? 32 : 8;
+  p.chunks = (int32_t)chunks(p.room);
+  p.each = (int32_t)((vocab + (int64_t)kThreads * p.chunks - 1) / ((int64_t)kThreads * p.chunks));
   p.blocks = rows * p.chunks;
   return p;
 }
@@ -495,13 +532,13 @@ extern "C" int fcp_beam_select(const void* logits, int32_t type, int64_t logits_
   const BeamPlan p = plan_beam((int64_t)n_prompts * beams, vocab);
   const size_t need = beam_bytes(p, keep);
   if (scratch_bytes < need) return fail(FCP_ERR_CAPACITY, "%s: scratch has %zu bytes, %zu are needed", who, scratch_bytes, need);
-  BeamArgs a = {logits, logits_row, n_prompts * beams, beams, vocab, p.chunks, keep, end_token, score, done, parent, token, new_score, new_done};
+  BeamArgs a = {logits, logits_row, n_prompts * beams, beams, vocab, p.chunks, p.each, keep, end_token, score, done, parent, token, new_score, new_done};
   char* const at = static_cast<char*>(scratch);
   a.lists = reinterpret_cast<uint64_t*>(at);
   a.sums = reinterpret_cast<double*>(at + pad_to((size_t)p.blocks * keep * 8, 256));
   hipStream_t st = static_cast<hipStream_t>(stream);
   const bool bf16 = type == FCP_BF16;
-  if (int rc = p.each == 32 ? (bf16 ? launch_rows<__bf16, 32>(a, p, st) : launch_rows<float, 32>(a, p, st))
+  if (int rc = p.room == 32 ? (bf16 ? launch_rows<__bf16, 32>(a, p, st) : launch_rows<float, 32>(a, p, st))
                             : (bf16 ? launch_rows<__bf16, 8>(a, p, st) : launch_rows<float, 8>(a, p, st)))
     return rc;
   beam_join_kernel<<<dim3((unsigned)n_prompts), dim3(kJoinThreads), 0, st>>>(a);
