@@ -576,8 +576,9 @@ int fcp_cache_compact(const fcp_cache* cache, const int32_t* pages, const int32_
 /*
  * fcp_cache_attn_shared -- fcp_cache_attn (without weigh) for a batch whose sequences have common beginnings: beams or samples of a prompt, questions about a document.  The common tokens
  * of a group are read and multiplied once for all of its rows, and every sequence's own tokens by themselves; the result is that of attention over the whole table, up to rounding.
- *   groups [n_groups + 1] int32 device: the sequences groups[g] .. groups[g + 1] - 1 are group g; not falling, within 0 .. n_seqs (else the call does nothing, as where cu_seqlens falls).
- *   Sequences outside all groups, and groups of one sequence with rows, are worked by themselves.
+ *   groups [n_groups + 1] int32 device: the sequences groups[g] .. groups[g + 1] - 1 are group g; not falling, within 0 .. n_seqs.  Sequences outside all groups, and groups of one
+ *   sequence with rows, are worked by themselves; so are all, whatever groups and shared_len hold, where the tables are too small to gain by it, or sequences have more than 64 rows for a KV head on
+ *   average.  Else the call does nothing where groups fall or leave 0 .. n_seqs, as where cu_seqlens falls.
  *   shared_len [n_groups] int32 device: tokens that the sequences of the group have in common: their tables name the same pages there, and those of the group's first sequence with rows are
  *   read.  Less is taken where a row does not see as many: whole pages, at most the tokens before the new ones of every sequence.
  *   n_groups from 0 to n_seqs.  scratch: fcp_cache_scratch_bytes(FCP_SCRATCH_CACHE_SHARED, ...).  Other arguments, results, limits and errors as in fcp_cache_attn.

@@ -3,9 +3,13 @@
 // softmax over a sequence's tokens is put together from two parts: the common beginning, which all rows of the group see whole, and the sequence's own rest.  The group's rows are next
 // to each other, so the common part is attention of many rows over one run of keys: its bytes are read once for the group instead of once for every sequence, and where one token of a
 // sequence alone would leave the matrix units idle, a group's rows fill their tiles.  Partial results (sums, maximum, sum of exponentials) meet in the last launch.
-//   * First launch, one block: the parts and their places on two lines (csrc/fcp_cache_attn.h), one of all common parts, one of all own parts.
-//   * A launch for each line, with the kernels' bodies for few or for many rows as the rows of a group, and of a sequence, are on average.
-//   * A wave for each row joins the pieces of its two items.
+//   * All common parts are one line of tiles, all own parts another (csrc/fcp_cache_attn.h).  Every block places the parts by itself where they are few; else a launch of one block does.
+//   * One launch works both lines, the common one with the bodies for few or for many rows, as the rows of a group are on average; a wave works an own part alone.  Where sequences have more than 16 rows
+//     for a KV head on average each line has a launch of its own.
+//   * A wave for each row joins the pieces of its two items, whose places their workers left for it.
+// 64 samples of a prompt of up to 16384 tokens, e4m3, 32 query heads over 8 KV heads of 128: 44.2 and 9.5 us, 51 together, fcp_cache_attn 174; the products of the common part would take a large product's rate
+// 14 us, the blocks begin them 11 us after the launch does (places 4.2, own parts and the first loads the rest), and partial results are 34 MB.  16 prompts of up to 8000 tokens, 8 beams each, int8: 39 and
+// 6.7 us, 50.5 together, where reading every key once takes 24.
 #include "fcp_cache_few.h"
 #include "fcp_cache_many.h"
 
@@ -70,7 +74,9 @@ __device__ inline int32_t places_of_part(const SharedArgs& a, const Part& p, int
   return p.rows == 0 ? 0 : a.c.hkv * ((p.rows * a.group - 1) / rows + 1) * places_of_item(p, whole);
 }
 
-constexpr int kWholeLen = 16 * kTile;  // own parts up to this long are not divided
+// Own parts up to this long are not divided, where all are.  4 / 8 / 16 tiles: 64 of a group with up to 600 own tokens 60.2 / 60.1 / 59.7 us, 8 with 1000 39.4 / 39.1 / 55.2, 16 groups of two with 1000
+// 35.4 / 35.4 / 44.2, 64 with 300 57.9 / 53.6 / 54.0.
+constexpr int kWholeLen = 8 * kTile;
 constexpr int kSharers = kWaves * kBlocks;       // waves that share the line of own parts
 constexpr int kLocal = 256;            // parts that a block places itself: one a thread
 
@@ -572,7 +578,7 @@ struct SharedPlan { int rows[2]; int32_t sharers[2]; bool waves, local; };
 SharedPlan plan_shared(const CacheView& c, int32_t n_seqs, int32_t n_groups, int32_t tq, int32_t hq) {
   SharedPlan p;
   const int64_t all_rows = (int64_t)tq * (hq / c.hkv);
-  p.rows[kCommon] = rows_form(all_rows, n_groups > 0 ? n_groups : 1);
+  p.rows[kCommon] = rows_form(all_rows, n_groups);
   p.rows[kOwn] = rows_form(all_rows, n_seqs);
   p.waves = p.rows[kOwn] == 16;
   p.sharers[kCommon] = kBlocks;
@@ -582,8 +588,15 @@ SharedPlan plan_shared(const CacheView& c, int32_t n_seqs, int32_t n_groups, int
 }
 // Scratch: for any number of groups up to n_seqs.  The slots of common parts have room for the rows of one group.
 struct SharedSpace { size_t parts[2], before[2], pieces[2], slots[2], whole[2], bytes; };
-// Many rows of a sequence are attention of many rows already: the matrix units bound it, and the bytes that sequences share are read from the L2s.  Every sequence is worked by itself then.
-bool by_itself(const CacheView& c, int32_t n_seqs, int32_t tq, int32_t hq) { return (int64_t)tq * (hq / c.hkv) > (int64_t)64 * n_seqs; }
+// Whether every sequence is worked by itself, as fcp_cache_attn does.  Many rows of a sequence are attention of many rows already: the matrix units bound it, and the bytes that sequences share are read from
+// the L2s (8 questions of 256 tokens about 4000: 221 us so, 328 in groups).  Else what groups gain is bytes, and what they cost is the second part and its joining, 8 to 15 us of a call, more with two
+// launches.  How long the common parts are only the device knows; what they may save at most follows from the tables' size.  Itself / in groups, e4m3, 32 query heads over 8 KV heads, MB that may be saved:
+// one row of a sequence 4 MB 8 / 18 us, 63 19.8 / 19.4, 73 20 / 26, 135 28 / 28, 249 48 / 39, 1000 94 / 52, 2200 174 / 54; 32 rows of a KV head 123 MB 39 / 55, 478 85 / 79, 985 133 / 140, 2200 222 / 193;
+// 64 rows 63 MB 37 / 55, 478 134 / 119, 2200 456 / 338.
+bool by_itself(const CacheView& c, int head_dim, int32_t n_seqs, int32_t n_groups, int32_t max_pages, int32_t tq, int32_t hq) {
+  const int64_t rows = (int64_t)tq * (hq / c.hkv), saved = n_groups == 0 ? 0 : (int64_t)(n_seqs - n_groups) * max_pages * c.page * c.hkv * 2 * head_dim;
+  return rows > (int64_t)64 * n_seqs || saved < (int64_t)(rows <= (int64_t)16 * n_seqs ? 96 : 384) << 20;
+}
 SharedSpace shared_space(const CacheView& c, int head_dim, int32_t n_seqs, int32_t tq, int32_t hq) {
   SharedSpace s;
   const SharedPlan p = plan_shared(c, n_seqs, 1, tq, hq);
@@ -625,7 +638,7 @@ int launch_shared(const SharedArgs& a, hipStream_t st) {
     rc = common == 16 ? launch_line<D, Fmt, 16, true>(a, kCommon, st) : common == 32 ? launch_line<D, Fmt, 32, true>(a, kCommon, st)
        : common == 64 ? launch_line<D, Fmt, 64, true>(a, kCommon, st) : launch_line<D, Fmt, 128, true>(a, kCommon, st);
   } else {
-    rc = a.n_groups == 0 ? FCP_OK : common == 32 ? launch_line<D, Fmt, 32, false>(a, kCommon, st) : common == 64 ? launch_line<D, Fmt, 64, false>(a, kCommon, st)
+    rc = common == 32 ? launch_line<D, Fmt, 32, false>(a, kCommon, st) : common == 64 ? launch_line<D, Fmt, 64, false>(a, kCommon, st)
        : launch_line<D, Fmt, 128, false>(a, kCommon, st);
     if (!rc) rc = a.rows[kOwn] == 32 ? launch_line<D, Fmt, 32, false>(a, kOwn, st) : launch_line<D, Fmt, 64, false>(a, kOwn, st);
   }
@@ -650,8 +663,9 @@ int check_shared(const char* who, const CacheView& c, int32_t n_seqs, int32_t ma
 // 0: refused
 size_t shared_scratch_bytes(const char* who, const CacheView& c, int head_dim, int32_t n_seqs, int32_t max_pages, int32_t tq, int32_t hq) {
   if (check_shared(who, c, n_seqs, max_pages, tq, hq)) return 0;
-  if (by_itself(c, n_seqs, tq, hq)) return attn_scratch_bytes(c, head_dim, n_seqs, max_pages, tq, hq);
-  return shared_space(c, head_dim, n_seqs, tq, hq).bytes;
+  const size_t itself = attn_scratch_bytes(c, head_dim, n_seqs, max_pages, tq, hq);
+  if (by_itself(c, head_dim, n_seqs, 1, max_pages, tq, hq)) return itself;
+  return max(itself, shared_space(c, head_dim, n_seqs, tq, hq).bytes);         // (with more groups less may be saved)
 }
 
 }  // namespace fcp
@@ -674,13 +688,11 @@ extern "C" int fcp_cache_attn_shared(const fcp_cache* cache, const void* q, int6
   if (!o || !lse || (uintptr_t)o % 16 || (uintptr_t)lse % 4) return fail(FCP_ERR_INVALID_ARG, "%s: o and lse are required and must be aligned", who);
   if (!scratch || (uintptr_t)scratch % 256) return fail(FCP_ERR_INVALID_ARG, "%s: scratch must be 256-byte aligned", who);
   if (int rc = check_shared(who, a.c, n_seqs, max_pages, tq, hq)) return rc;
-  if (by_itself(a.c, n_seqs, tq, hq)) {
-    const size_t need = attn_scratch_bytes(a.c, cache->head_dim, n_seqs, max_pages, tq, hq);
-    if (scratch_bytes < need) return fail(FCP_ERR_CAPACITY, "%s: scratch has %zu bytes, %zu are needed", who, scratch_bytes, need);
+  const size_t need = shared_scratch_bytes(who, a.c, cache->head_dim, n_seqs, max_pages, tq, hq);
+  if (scratch_bytes < need) return fail(FCP_ERR_CAPACITY, "%s: scratch has %zu bytes, %zu are needed", who, scratch_bytes, need);
+  if (by_itself(a.c, cache->head_dim, n_seqs, n_groups, max_pages, tq, hq))
     return fcp_cache_attn(cache, q, q_row, tq, hq, cu_seqlens, kv_len, pages, n_seqs, max_pages, softmax_scale, 0, o, lse, scratch, scratch_bytes, stream);
-  }
   const SharedSpace space = shared_space(a.c, cache->head_dim, n_seqs, tq, hq);
-  if (scratch_bytes < space.bytes) return fail(FCP_ERR_CAPACITY, "%s: scratch has %zu bytes, %zu are needed", who, scratch_bytes, space.bytes);
   const SharedPlan p = plan_shared(a.c, n_seqs, n_groups, tq, hq);
   a.s = {cu_seqlens, kv_len, pages, n_seqs, max_pages, tq};
   a.groups = groups;

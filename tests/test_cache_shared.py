@@ -46,14 +46,22 @@ def test_refusals_come_before_any_device_work():
 
 
 # ---- GPU ------------------------------------------------------------------------------------------------------------------------------------
+def wide(n_seqs, n_groups, P, D, hkv):
+    """Pages of a table with which groups may save 384 MB, so that they are worked together."""
+    return (384 << 20) // ((n_seqs - n_groups) * P * hkv * 2 * D) + 1
+
+
 class Batch:
-    """groups: [(common tokens, [(own tokens, new rows), ..]), ..]; the common pages of a group are the first ones of all of its tables.  A sequence's length is common + own."""
-    def __init__(self, P, D, hq, hkv, groups, fmt, seed=0, scale=None):
+    """groups: [(common tokens, [(own tokens, new rows), ..]), ..]; the common pages of a group are the first ones of all of its tables.  A sequence's length is common + own.
+    narrow: tables of which every sequence is worked by itself."""
+    def __init__(self, P, D, hq, hkv, groups, fmt, seed=0, scale=None, narrow=False):
         import torch
         rng = np.random.default_rng(seed + P + D + hq)
         self.kv_len = np.array([c + own for c, seqs in groups for own, _ in seqs], np.int32)
         self.news = [n for _, seqs in groups for _, n in seqs]
         width = max(-(-int(self.kv_len.max()) // P), 1) + 1
+        if not narrow:
+            width = max(width, wide(len(self.news), len(groups) if len(self.news) > len(groups) else 0, P, D, hkv))
         count = sum(c // P + sum(-(-(c % P + own) // P) for own, _ in seqs) for c, seqs in groups)
         order = list(rng.permutation(count + 2))
         self.pages = np.full((len(self.news), width), -1, np.int32)
@@ -107,6 +115,7 @@ CASES = [  # P, D, hq, hkv, groups
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("P, D, hq, hkv, groups", CASES)
 def test_sizes(P, D, hq, hkv, groups, fmt):
+    Batch(P, D, hq, hkv, groups, fmt, narrow=True).check()
     b = Batch(P, D, hq, hkv, groups, fmt)
     b.check()
     w = R.check_content(b.cache, b.ref)
@@ -273,17 +282,32 @@ def test_pages_past_the_32nd_bit(fmt, least):
             to[n - used:] = x
         ones = torch.ones(n, hkv, device="cuda") / 64
         cache = B.Cache(view(k), view(v), ones, ones)
-        pages = dev(np.array([[5, 0, 3, 7, -1], [5, 0, 3, 1, 9], [2, 8, -1, -1, -1]], np.int32)) + (n - used)
+        pages = torch.full((3, wide(3, 1, P, D, hkv)), -1, dtype=torch.int32, device="cuda")
+        pages[:, :5] = dev(np.array([[5, 0, 3, 7, -1], [5, 0, 3, 1, 9], [2, 8, -1, -1, -1]], np.int32)) + (n - used)
         for cu in ([0, 1, 2, 3], [0, 20, 40, 41]):
             m = cu[-1]
             o, lse = torch.empty(m, hq, D, dtype=torch.bfloat16, device="cuda"), torch.empty(hq, m, device="cuda")
-            w = torch.empty(B.fcp_cache_scratch_bytes(B.FCP_SCRATCH_CACHE_SHARED, cache, 3, 5, m, hq), dtype=torch.uint8, device="cuda")
+            w = torch.empty(B.fcp_cache_scratch_bytes(B.FCP_SCRATCH_CACHE_SHARED, cache, *pages.shape, m, hq), dtype=torch.uint8, device="cuda")
             B.fcp_cache_attn_shared(cache, q[:m].contiguous(), dev(cu), dev([500, 600, 200]), pages, dev([0, 2]), dev([384]), 0.05, o, lse, w)
             results.append((o, lse))
         del cache, k, v
     for a, b in zip(results[:2], results[2:]):
         assert torch.equal(a[0].view(torch.int16), b[0].view(torch.int16)) and torch.equal(a[1].view(torch.int32), b[1].view(torch.int32))
         assert torch.isfinite(a[1]).all() == (fmt == "int8" or least == 0)
+
+
+@pytest.mark.gpu
+def test_small_tables_are_worked_by_themselves():
+    """Whatever groups and shared_len hold: bit for bit what fcp_cache_attn gives."""
+    import torch
+    b = Batch(32, 64, 8, 2, [(192, one(3, 4, 5)), (64, one(1, 2))], "e4m3", narrow=True)
+    q, cu, lens, pages = dev_bf16(b.q), dev(b.cu), dev(b.kv_len), dev(b.pages)
+    o, lse = torch.empty_like(q), torch.empty(8, len(b.q), device="cuda")
+    w = torch.empty(B.fcp_cache_scratch_bytes(B.FCP_SCRATCH_CACHE_ATTN, b.cache, len(b.kv_len), b.pages.shape[1], len(b.q), 8), dtype=torch.uint8, device="cuda")
+    B.fcp_cache_attn(b.cache, q, cu, lens, pages, b.scale, o, lse, w)
+    for kw in (dict(), dict(groups=[0, 4, 2]), dict(groups=[-5, 9, 9]), dict(shared=[10 ** 6, -3]), dict(groups=[0], shared=[])):
+        got = b.run(**kw)
+        assert np.array_equal(got[0], o.double().cpu().numpy()) and np.array_equal(got[1], lse.double().cpu().numpy())
 
 
 @pytest.mark.gpu

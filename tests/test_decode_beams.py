@@ -17,15 +17,16 @@ def rows_of(cache, table, n, P, fmt):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("fmt, P, D, hq, hkv, beams, lens, rot", [("e4m3", 64, 128, 8, 2, 4, [150, 3, 64], 128), ("int8", 16, 64, 4, 4, 3, [33, 16, 1, 47], 0), ("int8", 32, 64, 10, 2, 8, [100], 32)])
-def test_beams_are_sequences(fmt, P, D, hq, hkv, beams, lens, rot):
+@pytest.mark.parametrize("fmt, P, D, hq, hkv, beams, lens, rot, width", [
+    ("e4m3", 64, 128, 8, 2, 4, [150, 3, 64], 128, 400), ("int8", 16, 64, 4, 4, 3, [33, 16, 1, 47], 0, 16), ("int8", 32, 64, 10, 2, 8, [100], 32, 2000), ("e4m3", 64, 128, 8, 2, 4, [150, 3, 64], 128, 16)])
+def test_beams_are_sequences(fmt, P, D, hq, hkv, beams, lens, rot, width):
     """The cached tokens of every beam are, code for code, those of a sequence that was appended alone, whatever beams forked from each other; attention is that over its own table."""
     import torch
     from paper_2602_21788_amd.decode import BeamDecoder, CacheDecoder
     g = torch.Generator(device="cuda").manual_seed(P)
     rows = lambda n, h: torch.randn(n, h, D, generator=g, device="cuda").to(torch.bfloat16)
     n, steps, vocab = len(lens), 2 * P // 3 + 3, 500
-    dec = BeamDecoder(n, beams, 200, 16, hq, hkv, D, end_token=7, page_tokens=P, fmt=fmt, rot_dim=rot)
+    dec = BeamDecoder(n, beams, 200, width, hq, hkv, D, end_token=7, page_tokens=P, fmt=fmt, rot_dim=rot)
     alone = CacheDecoder(n * beams, 400, 16, hq, hkv, D, page_tokens=P, fmt=fmt, rot_dim=rot)
     q, k, v = rows(sum(lens), hq), rows(sum(lens), hkv), rows(sum(lens), hkv)
     again = [torch.cat([x[a: a + m] for a, m in zip(np.cumsum([0] + lens), lens) for _ in range(beams)]).contiguous() for x in (q, k, v)]
@@ -43,7 +44,7 @@ def test_beams_are_sequences(fmt, P, D, hq, hkv, beams, lens, rot):
             assert end == used
         # attention over every beam's own table, all of it
         ordinary = torch.empty_like(o), torch.empty_like(lse)
-        work = torch.empty(B.fcp_cache_scratch_bytes(B.FCP_SCRATCH_CACHE_ATTN, dec.cache, n * beams, 16, n * beams, hq), dtype=torch.uint8, device="cuda")
+        work = torch.empty(B.fcp_cache_scratch_bytes(B.FCP_SCRATCH_CACHE_ATTN, dec.cache, n * beams, width, n * beams, hq), dtype=torch.uint8, device="cuda")
         qr = given[-1][0].clone()
         dec.prompts._rotate(qr, given[-1][1].clone(), dec.prompts._to(np.repeat(np.array(lens) + t, beams)))
         B.fcp_cache_attn(dec.cache, qr, dec._cu, dec.kv_len, dec.pages, dec.scale, *ordinary, work)
@@ -162,7 +163,7 @@ def test_two_steps_in_a_graph():
     import torch
     from paper_2602_21788_amd.decode import CacheDecoder
     g = torch.Generator(device="cuda").manual_seed(9)
-    n, beams, hq, hkv, D, P, vocab, m = 3, 4, 8, 2, 128, 32, 3001, 8
+    n, beams, hq, hkv, D, P, vocab, m = 3, 4, 8, 2, 128, 32, 3001, 800          # (tables with which a prompt's beams are worked together)
     rows = n * beams
     draw = lambda r, h: torch.randn(r, h, D, generator=g, device="cuda").to(torch.bfloat16)
     lens = [100, 33, 64]
