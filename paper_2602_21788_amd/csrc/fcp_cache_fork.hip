@@ -4,6 +4,9 @@
 // Every entry of this step's tables is looked at once, and marks its page; then one block counts through the marks for free pages, in increasing order, and lists the copies; the last launch copies,
 // 16 bytes a thread, a block for each (page, KV head), whose keys are one run of memory and whose values are another, and writes the tables.
 // Small calls are chains of loads and launches.  Where the tables are not large the block that plans marks too, bits in LDS: two launches; else four, with a byte a page.
+//
+// A step of 8 beams 11.0 us, of 32 prompts' 256 over up to 8001 tokens 14.5 (planning 7 and 10 of them); 1024 beams that begin, of 64 prompts, 38 (planning 16, copying 19: 136 MB read and
+// written); 8 sequences compacted 12.8, 64 of up to 16384 tokens 146 (planning 15, copying 129: 635 MB read and written, a copy's rate).
 #include "fcp_cache.h"
 
 namespace fcp {
@@ -164,7 +167,9 @@ __global__ __launch_bounds__(256) void mark_kernel(PageArgs a) {
 }
 
 // ---- small calls: the block that plans marks -----------------------------------------------------------------------
-constexpr int kLdsPages = 1 << 18, kLdsSeqs = 4096, kLdsEntries = 1 << 17, kLdsNew = kPlanThreads;      // (a new sequence a thread)
+// One block / many, us, tables all but full, fork and compact: 8 sequences of 64 entries 9.1 / 13.7 and 9.1 / 12.6, 64 of 256 12.3 / 16.0 and 11.6 / 15.0, 256 of 127 14.5 / 16.1, of 256 20.1 / 14.9 and
+// 17.5 / 12.4, 1024 of 128 35.4 / 17.5 and 29.6 / 13.2; 64 of 64 in a pool of 200000 pages 16.8 / 24.2 and 20.2 / 25.0.  The others are what LDS has room for, and a thread for each new sequence.
+constexpr int kLdsPages = 1 << 18, kLdsSeqs = 4096, kLdsEntries = 1 << 15, kLdsNew = kPlanThreads;
 // Per page: marks, and whether somebody writes it; per sequence of this step: whether it has children, whether one of them goes on without new tokens in a page that is begun, its tokens, the
 // lowest child that writes its last page.
 struct LdsTables { LdsMarks marks; uint32_t *written, *child, *part; int32_t *len, *low; };
@@ -198,7 +203,7 @@ __device__ inline void begin_marks(const PageArgs& a, const LdsTables& t) {
 template <bool Fork>
 __device__ inline void mark_in_lds(const PageArgs& a, const LdsTables& t) {
   // Four neighbouring entries a lane, 16 to 64 lanes a sequence, as the tables are long; a wave looks at eight such lots at once, so that their loads are on the way together.  Instructions bound
-  // this where there are thousands of entries for each wave, so there are few for an entry: a mark is made whether it is there or not.
+  // this where there are thousands of entries for each wave, so there are few for an entry: a mark is made whether it is there or not (256 beams 14.4 us; 22.9 with a look before).
   constexpr int kAtOnce = 8;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int log_lanes = a.s.max_pages > 128 ? 6 : a.s.max_pages > 64 ? 5 : 4, of_lot = 64 >> log_lanes, sub = lane >> log_lanes;
