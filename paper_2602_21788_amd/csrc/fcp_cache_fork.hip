@@ -5,8 +5,8 @@
 // 16 bytes a thread, a block for each (page, KV head), whose keys are one run of memory and whose values are another, and writes the tables.
 // Small calls are chains of loads and launches.  Where the tables are not large the block that plans marks too, bits in LDS: two launches; else four, with a byte a page.
 //
-// A step of 8 beams 11.0 us, of 32 prompts' 256 over up to 8001 tokens 14.5 (planning 7 and 10 of them); 1024 beams that begin, of 64 prompts, 38 (planning 16, copying 19: 136 MB read and
-// written); 8 sequences compacted 12.8, 64 of up to 16384 tokens 146 (planning 15, copying 129: 635 MB read and written, a copy's rate).
+// A step of 8 beams 11.0 us, of 32 prompts' 256 over up to 8001 tokens 14.4 (planning 7 and 10 of them); 1024 beams that begin, of 64 prompts, 38 (planning 16, copying 19: 136 MB read and
+// written); 8 sequences compacted 12.3, 64 of up to 16384 tokens 145 (planning 14, copying 129: 635 MB read and written, a copy's rate).
 #include "fcp_cache.h"
 
 namespace fcp {
@@ -71,6 +71,12 @@ __device__ inline Scan block_scan(int32_t x, int32_t* sums) {
   }
   __syncthreads();
   return r;
+}
+
+// Two counts of up to 33 a thread, in the halves of a word: the block's are below 2^16.
+struct Pair { Scan low, high; };
+__device__ inline Pair pair_of(const Scan& x) {
+  return {{x.before & 0xffff, x.all & 0xffff}, {(int32_t)((uint32_t)x.before >> 16), (int32_t)((uint32_t)x.all >> 16)}};
 }
 
 // A word of bits, one for each of 32 bytes that is not 0 (behind n: 0).
@@ -167,8 +173,8 @@ __global__ __launch_bounds__(256) void mark_kernel(PageArgs a) {
 }
 
 // ---- small calls: the block that plans marks -----------------------------------------------------------------------
-// One block / many, us, tables all but full, fork and compact: 8 sequences of 64 entries 9.1 / 13.7 and 9.1 / 12.6, 64 of 256 12.3 / 16.0 and 11.6 / 15.0, 256 of 127 14.5 / 16.1, of 256 20.1 / 14.9 and
-// 17.5 / 12.4, 1024 of 128 35.4 / 17.5 and 29.6 / 13.2; 64 of 64 in a pool of 200000 pages 16.8 / 24.2 and 20.2 / 25.0.  The others are what LDS has room for, and a thread for each new sequence.
+// One block / many, us, tables all but full, fork and compact: 8 sequences of 64 entries 8.8 / 13.7 and 8.5 / 12.0, 64 of 256 12.2 / 16.0 and 11.0 / 14.4, 256 of 127 14.4 / 16.1, of 256 20.1 / 14.4 and
+// 16.9 / 11.8, 1024 of 128 35.4 / 17.6 and 29.0 / 12.4; 64 of 64 in a pool of 200000 pages 17.2 / 24.2 and 19.5 / 24.4.  The others are what LDS has room for, and a thread for each new sequence.
 constexpr int kLdsPages = 1 << 18, kLdsSeqs = 4096, kLdsEntries = 1 << 15, kLdsNew = kPlanThreads;
 // Per page: marks, and whether somebody writes it; per sequence of this step: whether it has children, whether one of them goes on without new tokens in a page that is begun, its tokens, the
 // lowest child that writes its last page.
@@ -322,12 +328,13 @@ __global__ __launch_bounds__(kPlanThreads) void fork_small_kernel(PageArgs a) {
   if (parent >= 0) {
     if (!bit(t.child, parent)) set_bit(t.child, parent);
     if (writes < 0 && !bit(t.part, parent)) set_bit(t.part, parent);
-    if (page >= 0) atomicMin(t.low + parent, i);
   }
-  written[i] = page;
   if (i == 0) several = 0;
   __syncthreads();
   mark_in_lds<true>(a, t);
+  if (page >= 0) atomicMin(t.low + parent, i);             // (the page was asked for before the marks' entries, and is waited for with them)
+  written[i] = page;
+  __syncthreads();
   const bool lowest = page >= 0 && t.low[parent] == i;
   if (lowest && (atomicOr(t.written + (page >> 5), 1u << (page & 31)) >> (page & 31) & 1)) several = 1;    // two parents have begun the same page
   __syncthreads();
@@ -338,18 +345,19 @@ __global__ __launch_bounds__(kPlanThreads) void fork_small_kernel(PageArgs a) {
   copy |= page >= 0 && t.marks.is_read(page);
   const Scan mine = block_scan(copy + pages_for(a, after) - pages_for(a, tokens), sums);
   const int32_t need = mine.all;
-  int32_t listed = 0, held = page >= 0 && !copy;
+  int32_t listed = 0, held = 0;
   for (int w0 = 0; w0 < a.words; w0 += kPlanThreads) {
     const int w = w0 + i;
     uint32_t free = w < a.words ? ~t.marks.held_word(w) : 0u;
     if (w == a.words - 1 && a.c.n_pages % 32) free &= (1u << (a.c.n_pages % 32)) - 1;
-    held += w < a.words ? __popc(t.marks.read_word(w)) : 0;
-    const Scan at = block_scan(__popc(free), sums);
-    int32_t rank = listed + at.before;
+    const int32_t kept = (w < a.words ? __popc(t.marks.read_word(w)) : 0) + (w0 == 0 && page >= 0 && !copy);
+    const Pair at = pair_of(block_scan(__popc(free) | kept << 16, sums));
+    int32_t rank = listed + at.low.before;
     for (; free && rank < need; free &= free - 1, ++rank) (rank < kListed ? list : a.list)[rank] = 32 * w + __builtin_ctz(free);
-    listed += at.all;
+    listed += at.low.all;
+    held += at.high.all;
   }
-  held = block_scan(held, sums).all;
+  __syncthreads();                                         // (the list is written)
   const int32_t taken = min(need, listed);
   if (i == 0) {
     a.counts[0] = taken;
@@ -379,14 +387,14 @@ __device__ inline void plan_compact(const PageArgs& a, const Marks& marks) {
   if (threadIdx.x == 0) end_at = busy_end = 0;
   __syncthreads();
   int32_t used = 0, all = 0;
-  for (int w = threadIdx.x; w < a.words; w += kPlanThreads) {
-    const uint32_t h = marks.held_word(w), b = busy_bits(w);
-    used += __popc(h & ~b);
-    all += __popc(h);
+  for (int w0 = 0; w0 < a.words; w0 += kPlanThreads) {
+    const int w = w0 + threadIdx.x;
+    const uint32_t h = w < a.words ? marks.held_word(w) : 0u, b = w < a.words ? busy_bits(w) : 0u;
     if (b) atomicMax(&busy_end, 32 * w + 32 - __builtin_clz(b));
+    const Pair n = pair_of(block_scan(__popc(h & ~b) | __popc(h) << 16, sums));
+    used += n.low.all;
+    all += n.high.all;
   }
-  used = block_scan(used, sums).all;
-  all = block_scan(all, sums).all;
   // the used-th page that is not busy
   int32_t seen = 0;
   for (int w0 = 0; w0 < a.words && seen < used; w0 += kPlanThreads) {
@@ -411,13 +419,13 @@ __device__ inline void plan_compact(const PageArgs& a, const Marks& marks) {
       hole = low & ~h & ~b;
       mover = ~low & h & ~b;
     }
-    const Scan hs = block_scan(__popc(hole), sums), ms = block_scan(__popc(mover), sums);
-    int32_t rank = holes + hs.before;
+    const Pair n = pair_of(block_scan(__popc(hole) | __popc(mover) << 16, sums));
+    int32_t rank = holes + n.low.before;
     for (; hole; hole &= hole - 1) a.list[rank++] = 32 * w + __builtin_ctz(hole);
-    rank = movers + ms.before;
+    rank = movers + n.high.before;
     for (; mover; mover &= mover - 1) a.copies[rank++] = {32 * w + __builtin_ctz(mover), -1, a.c.page, 0};
-    holes += hs.all;
-    movers += ms.all;
+    holes += n.low.all;
+    movers += n.high.all;
   }
   __threadfence_block();
   __syncthreads();
