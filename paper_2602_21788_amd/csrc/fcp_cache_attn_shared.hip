@@ -7,8 +7,8 @@
 //   * One launch works both lines, the common one with the bodies for few or for many rows, as the rows of a group are on average; a wave works an own part alone.  Where sequences have more than 16 rows
 //     for a KV head on average each line has a launch of its own.
 //   * A wave for each row joins the pieces of its two items, whose places their workers left for it.
-// 64 samples of a prompt of up to 16384 tokens, e4m3, 32 query heads over 8 KV heads of 128: 44.2 and 9.5 us, 51 together, fcp_cache_attn 174; the products of the common part would take a large product's rate
-// 14 us, the blocks begin them 11 us after the launch does (places 4.2, own parts and the first loads the rest), and partial results are 34 MB.  16 prompts of up to 8000 tokens, 8 beams each, int8: 39 and
+// 64 samples of a prompt of up to 16384 tokens, e4m3, 32 query heads over 8 KV heads of 128: 43.5 and 9.6 us, 50 together, fcp_cache_attn 174; the products of the common part would take a large product's rate
+// 14 us, the blocks begin them 10 us after the launch does (places 3.4, own parts and the first loads the rest), and partial results are 34 MB.  16 prompts of up to 8000 tokens, 8 beams each, int8: 39 and
 // 6.7 us, 50.5 together, where reading every key once takes 24.
 #include "fcp_cache_few.h"
 #include "fcp_cache_many.h"
@@ -53,7 +53,7 @@ struct SharedArgs {
   float* lse;
   Tables tables;                       // in scratch
   struct RowPieces* pieces[2];         // [tq * hq], of all rows of sequences
-  int32_t rows[2], sharers[2];         // rows of an item; blocks, or waves, that may share a line
+  int32_t log_rows[2], log_sharers[2]; // rows of an item; blocks, or waves, that may share a line
   float* slots[2];                     // two per block: pieces of divided items
   int32_t waves;                       // own parts: a wave works an item, else a block
   int32_t local;                       // blocks place the parts themselves
@@ -70,9 +70,8 @@ __device__ inline Part part_of(const SharedArgs& a, const Tables& t, int kind, i
   return {x.row0, x.rows, i, shared >> a.c.log_page, len, len - x.rows, 1, shared > 0};
 }
 __device__ inline int32_t places_of_item(const Part& p, bool whole) { return whole ? 1 : places_of<kItemLead>(p.len); }
-__device__ inline int32_t places_of_part(const SharedArgs& a, const Part& p, int rows, bool whole) {
-  return p.rows == 0 ? 0 : a.c.hkv * ((p.rows * a.group - 1) / rows + 1) * places_of_item(p, whole);
-}
+__device__ inline int32_t row_blocks_of(const SharedArgs& a, const Part& p, int kind) { return ((p.rows * a.group - 1) >> a.log_rows[kind]) + 1; }
+__device__ inline int32_t places_of_part(const SharedArgs& a, const Part& p, int kind, bool whole) { return p.rows == 0 ? 0 : a.c.hkv * row_blocks_of(a, p, kind) * places_of_item(p, whole); }
 
 // Own parts up to this long are not divided, where all are.  4 / 8 / 16 tiles: 64 of a group with up to 600 own tokens 60.2 / 60.1 / 59.7 us, 8 with 1000 39.4 / 39.1 / 55.2, 16 groups of two with 1000
 // 35.4 / 35.4 / 44.2, 64 with 300 57.9 / 53.6 / 54.0.
@@ -82,11 +81,15 @@ constexpr int kLocal = 256;            // parts that a block places itself: one 
 
 // Places 0 .. total - 1 in `n` shares that differ by one place at most.
 struct Even {
-  int32_t total, n;
-  __device__ int32_t begin(int32_t i) const { return i * (total / n) + min(i, total % n); }
+  int32_t total, n, log_most;          // n: up to 2^log_most
+  __device__ int32_t each() const { return n >> log_most ? total >> log_most : (int32_t)((uint32_t)total / (uint32_t)n); }
+  __device__ int32_t begin(int32_t i) const {
+    const int32_t q = each();
+    return i * q + min(i, total - n * q);
+  }
   __device__ int32_t owner(int32_t x) const {
-    const int32_t q = total / n, r = total % n, first = r * (q + 1);
-    return x < first ? x / (q + 1) : r + (x - first) / q;
+    const int32_t q = each(), r = total - n * q, first = r * (q + 1);
+    return x < first ? (int32_t)((uint32_t)x / (uint32_t)(q + 1)) : r + (int32_t)((uint32_t)(x - first) / (uint32_t)q);
   }
 };
 // A line and its shares: a share has a few places at least, where items are one place each one.
@@ -98,41 +101,53 @@ __device__ inline Shares shares_of(const SharedArgs& a, const Tables& t, int kin
   const int32_t* const ends = t.before(kind) + a.count(kind);
   const int32_t total = __builtin_amdgcn_readfirstlane(ends[0]);
   const bool whole = __builtin_amdgcn_readfirstlane(ends[1]);
-  return {{total, min(a.sharers[kind], whole ? total : (total + kLeastTiles - 1) / kLeastTiles)}, whole};
+  return {{total, min(1 << a.log_sharers[kind], whole ? total : (total + kLeastTiles - 1) / kLeastTiles), a.log_sharers[kind]}, whole};
 }
 // Shares of the common line go to the blocks from the last one on, those of the own line from the first: where there are few, different blocks have them.
 __device__ inline int share_of_block(const SharedArgs& a, int kind) { return kind == kCommon && a.waves ? kBlocks - 1 - (int)blockIdx.x : (int)blockIdx.x; }
 
 // The common parts from the groups and the own parts' entries; these learn their group.
 struct Group { int32_t lo, hi, said; };
+// What every row of a group sees, at most `said`, its first sequence and row, its rows and sequences: of some of its sequences.  Those without rows do not count.
+struct Seen { int32_t least, first, row0, rows, seqs; };
+__device__ inline Seen look_at(const Tables& t, const Group& x, int g, int sub, int lanes) {
+  Seen r = {max(x.said, 0), INT32_MAX, INT32_MAX, 0, 0};
+  for (int s = x.lo + sub; s < x.hi; s += lanes) {
+    const Entry y = t.own[s];
+    t.own[s].other = g;
+    if (y.rows > 0) {
+      r.least = min(r.least, max(y.len - y.rows, 0));
+      r.first = min(r.first, s);
+      r.row0 = min(r.row0, y.row0);
+      r.rows += y.rows;
+      ++r.seqs;
+    }
+  }
+  return r;
+}
+__device__ inline Entry common_of(const Seen& x, int page) {
+  const int32_t shared = x.seqs < 2 ? 0 : x.least & ~(page - 1);
+  return {x.row0, shared ? x.rows : 0, x.first, shared};
+}
 template <int Threads, class F>
 __device__ inline void place_groups(const SharedArgs& a, const Tables& t, F group) {
+  if (a.n_groups <= Threads / 64) {                                     // a wave a group (300 sequences of one group: 48 us, 56 with eight lanes)
+    const int g = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (g >= a.n_groups) return;
+    Seen x = look_at(t, group(g), g, lane, 64);
+    auto least_of = [](int32_t v) { return INT32_MAX - wave_max(INT32_MAX - v); };
+    auto sum_of = [](int32_t v) { return __builtin_amdgcn_readlane(wave_prefix_sum(v), 63); };
+    x = {least_of(x.least), least_of(x.first), least_of(x.row0), sum_of(x.rows), sum_of(x.seqs)};
+    if (lane == 0) t.common[g] = common_of(x, a.c.page);
+    return;
+  }
   for (int g0 = 0; g0 < a.n_groups; g0 += Threads / 8) {                // eight lanes a group
     const int g = g0 + (int)threadIdx.x / 8, sub = threadIdx.x % 8;
-    const Group x = g < a.n_groups ? group(g) : Group{0, 0, 0};
-    // what every row of the group sees; sequences without rows do not count
-    int least = x.said, first = INT32_MAX, rows = 0, seqs = 0, row0 = INT32_MAX;
-    for (int s = x.lo + sub; s < x.hi; s += 8) {
-      const Entry y = t.own[s];
-      t.own[s].other = g;
-      if (y.rows > 0) {
-        least = min(least, y.len - y.rows);
-        first = min(first, s);
-        row0 = min(row0, y.row0);
-        rows += y.rows;
-        ++seqs;
-      }
-    }
+    Seen x = look_at(t, g < a.n_groups ? group(g) : Group{0, 0, 0}, g, sub, 8);
 #pragma unroll
-    for (int d = 1; d < 8; d *= 2) {
-      least = min(least, __shfl_xor(least, d));
-      first = min(first, __shfl_xor(first, d));
-      row0 = min(row0, __shfl_xor(row0, d));
-      rows += __shfl_xor(rows, d);
-      seqs += __shfl_xor(seqs, d);
-    }
-    const int shared = seqs < 2 ? 0 : max(least, 0) & ~(a.c.page - 1);
-    if (g < a.n_groups && sub == 0) t.common[g] = {row0, shared ? rows : 0, first, shared};
+    for (int d = 1; d < 8; d *= 2)
+      x = {min(x.least, __shfl_xor(x.least, d)), min(x.first, __shfl_xor(x.first, d)), min(x.row0, __shfl_xor(x.row0, d)), x.rows + __shfl_xor(x.rows, d), x.seqs + __shfl_xor(x.seqs, d)};
+    if (g < a.n_groups && sub == 0) t.common[g] = common_of(x, a.c.page);
   }
 }
 
@@ -170,7 +185,7 @@ __device__ inline void place_parts(const SharedArgs& a, const Tables& t) {
     int32_t total = 0;
     for (int i0 = 0; i0 < n; i0 += Threads) {
       const int i = i0 + threadIdx.x;
-      const int32_t mine = i < n && !bad ? places_of_part(a, part_of(a, t, kind, i), a.rows[kind], whole) : 0, upto = wave_prefix_sum(mine);
+      const int32_t mine = i < n && !bad ? places_of_part(a, part_of(a, t, kind, i), kind, whole) : 0, upto = wave_prefix_sum(mine);
       if (lane == 63) sums[wave] = upto;
       __syncthreads();
       int32_t at = total + upto - mine;
@@ -213,11 +228,11 @@ __device__ inline Tables tables_of(const SharedArgs& a, LocalTables& own) {
   int32_t places[3] = {}, upto[3], most = 0;
   if (is_seq && !none) {
     const Part p = part_of(a, t, kOwn, i);
-    places[0] = places_of_part(a, p, a.rows[kOwn], false);
-    places[1] = places_of_part(a, p, a.rows[kOwn], true);
+    places[0] = places_of_part(a, p, kOwn, false);
+    places[1] = places_of_part(a, p, kOwn, true);
     most = p.rows > 0 ? p.len : 0;
   }
-  if (is_group && !none) places[2] = places_of_part(a, part_of(a, t, kCommon, i), a.rows[kCommon], false);
+  if (is_group && !none) places[2] = places_of_part(a, part_of(a, t, kCommon, i), kCommon, false);
   most = wave_max(most);
 #pragma unroll
   for (int k = 0; k < 3; ++k) {
@@ -293,26 +308,26 @@ struct Work {
   // Rows of the piece at hand that begins its item: the join learns where their pieces lie.  `i` of `step` lanes.
   __device__ void note_pieces(const SharedArgs& a, int i, int step) const {
     if (t0 > 0) return;
-    const int rows = a.rows[kind], n = whole ? 1 : shares_of(a, t, kind).even.owner(item0 + kItemLead + tiles - 1) - me + 1;
-    for (int lr = i; lr < rows && row_block * rows + lr < all_rows; lr += step) {
-      const int64_t row = whole_row(a, row_block * rows + lr);
+    const int row0 = row_block << a.log_rows[kind], rows = min(1 << a.log_rows[kind], all_rows - row0), n = whole ? 1 : shares_of(a, t, kind).even.owner(item0 + kItemLead + tiles - 1) - me + 1;
+    for (int lr = i; lr < rows; lr += step) {
+      const int64_t row = whole_row(a, row0 + lr);
       a.pieces[kind][row] = {me, n, lr, 0};
       if (kind == kOwn && !part.common) a.pieces[kCommon][row] = {0, 0, 0, 0};
     }
   }
   __device__ bool next(const SharedArgs& a) {
     while (at < end) {
-      const int rows = a.rows[kind];
-      while (at >= base + places_of_part(a, part, rows, undivided)) {
+      while (at >= base + places_of_part(a, part, kind, undivided)) {
         ++index;
         take(a);
       }
       tiles = tiles_of(part.len);
       all_rows = part.rows * a.group;
-      const int row_blocks = (all_rows + rows - 1) / rows, places = places_of_item(part, undivided), item = (at - base) / places, from = (at - base) % places;
+      const int row_blocks = row_blocks_of(a, part, kind), places = places_of_item(part, undivided), item = undivided ? at - base : __builtin_amdgcn_readfirstlane((uint32_t)(at - base) / (uint32_t)places),
+                from = at - base - item * places;
       const Piece piece = undivided ? piece_of<kWhole>(tiles, from, end - at) : piece_of<kItemLead>(tiles, from, end - at);
-      head = item / row_blocks;
-      row_block = item % row_blocks;
+      head = row_blocks == 1 ? item : __builtin_amdgcn_readfirstlane((uint32_t)item / (uint32_t)row_blocks);
+      row_block = item - head * row_blocks;
       t0 = piece.first;
       t1 = piece.last;
       whole = t0 == 0 && t1 == tiles;
@@ -528,7 +543,7 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs a) {
     const int mine = min(p0 + lane, all - 1);
     const bool is_common = mine < common.n;
     const RowPieces x = is_common ? common : own;
-    const int piece = is_common ? mine : mine - common.n, rows = is_common ? a.rows[kCommon] : a.rows[kOwn];
+    const int piece = is_common ? mine : mine - common.n, rows = 1 << (is_common ? a.log_rows[kCommon] : a.log_rows[kOwn]);
     const float* const slot = (is_common ? a.slots[kCommon] : a.slots[kOwn]) + (int64_t)(2 * (x.first + piece) + (piece == 0 ? 1 : 0)) * slot_floats(D, rows);
     const float* const whole = (is_common ? a.whole[kCommon] : a.whole[kOwn]) + (int64_t)unit * (D + 4);
     const float* const sums = x.n == 1 ? whole : slot + x.lr * D;
@@ -591,11 +606,11 @@ struct SharedSpace { size_t parts[2], before[2], pieces[2], slots[2], whole[2], 
 // Whether every sequence is worked by itself, as fcp_cache_attn does.  Many rows of a sequence are attention of many rows already: the matrix units bound it, and the bytes that sequences share are read from
 // the L2s (8 questions of 256 tokens about 4000: 221 us so, 328 in groups).  Else what groups gain is bytes, and what they cost is the second part and its joining, 8 to 15 us of a call, more with two
 // launches.  How long the common parts are only the device knows; what they may save at most follows from the tables' size.  Itself / in groups, e4m3, 32 query heads over 8 KV heads, MB that may be saved:
-// one row of a sequence 4 MB 8 / 18 us, 63 19.8 / 19.4, 73 20 / 26, 135 28 / 28, 249 48 / 39, 1000 94 / 52, 2200 174 / 54; 32 rows of a KV head 123 MB 39 / 55, 478 85 / 79, 985 133 / 140, 2200 222 / 193;
+// 4 rows for a KV head 4 MB 8 / 18 us, 63 19.8 / 19.4, 73 20 / 26, 135 28 / 28, 249 48 / 39, 1000 94 / 52, 2200 174 / 54; 16 rows 123 MB 29 / 36, 1000 99 / 75, 2200 185 / 117; 32 rows 123 MB 39 / 55, 478 85 / 79, 985 133 / 140, 2200 222 / 193;
 // 64 rows 63 MB 37 / 55, 478 134 / 119, 2200 456 / 338.
 bool by_itself(const CacheView& c, int head_dim, int32_t n_seqs, int32_t n_groups, int32_t max_pages, int32_t tq, int32_t hq) {
   const int64_t rows = (int64_t)tq * (hq / c.hkv), saved = n_groups == 0 ? 0 : (int64_t)(n_seqs - n_groups) * max_pages * c.page * c.hkv * 2 * head_dim;
-  return rows > (int64_t)64 * n_seqs || saved < (int64_t)(rows <= (int64_t)16 * n_seqs ? 96 : 384) << 20;
+  return rows > (int64_t)64 * n_seqs || saved < (int64_t)(rows <= (int64_t)8 * n_seqs ? 1 : rows <= (int64_t)16 * n_seqs ? 2 : 3) << 27;
 }
 SharedSpace shared_space(const CacheView& c, int head_dim, int32_t n_seqs, int32_t tq, int32_t hq) {
   SharedSpace s;
@@ -632,7 +647,7 @@ int launch_shared(const SharedArgs& a, hipStream_t st) {
     parts_kernel<<<dim3(1), dim3(kPartThreads), 0, st>>>(a);
     FCP_HIP_CHECK(hipGetLastError());
   }
-  const int common = a.rows[kCommon];
+  const int common = 1 << a.log_rows[kCommon];
   int rc;
   if (a.waves) {
     rc = common == 16 ? launch_line<D, Fmt, 16, true>(a, kCommon, st) : common == 32 ? launch_line<D, Fmt, 32, true>(a, kCommon, st)
@@ -640,7 +655,7 @@ int launch_shared(const SharedArgs& a, hipStream_t st) {
   } else {
     rc = common == 32 ? launch_line<D, Fmt, 32, false>(a, kCommon, st) : common == 64 ? launch_line<D, Fmt, 64, false>(a, kCommon, st)
        : launch_line<D, Fmt, 128, false>(a, kCommon, st);
-    if (!rc) rc = a.rows[kOwn] == 32 ? launch_line<D, Fmt, 32, false>(a, kOwn, st) : launch_line<D, Fmt, 64, false>(a, kOwn, st);
+    if (!rc) rc = a.log_rows[kOwn] == 5 ? launch_line<D, Fmt, 32, false>(a, kOwn, st) : launch_line<D, Fmt, 64, false>(a, kOwn, st);
   }
   if (rc) return rc;
   shared_join_kernel<D><<<dim3((unsigned)(((int64_t)a.s.n_rows * a.hq + 3) / 4)), dim3(256), 0, st>>>(a);
@@ -712,8 +727,8 @@ extern "C" int fcp_cache_attn_shared(const fcp_cache* cache, const void* q, int6
     a.pieces[kind] = reinterpret_cast<RowPieces*>(at + space.pieces[kind]);
     a.slots[kind] = reinterpret_cast<float*>(at + space.slots[kind]);
     a.whole[kind] = reinterpret_cast<float*>(at + space.whole[kind]);
-    a.rows[kind] = p.rows[kind];
-    a.sharers[kind] = p.sharers[kind];
+    a.log_rows[kind] = __builtin_ctz(p.rows[kind]);
+    a.log_sharers[kind] = __builtin_ctz(p.sharers[kind]);
   }
   a.waves = p.waves;
   a.local = p.local;

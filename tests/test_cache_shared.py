@@ -146,6 +146,20 @@ def test_many_sequences_whose_tables_fall():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("count", [1, 3, 5, 200])
+@pytest.mark.parametrize("new", [1, 9])
+def test_common_pages_are_read_once(count, new):
+    """Those of the group's first sequence with rows: what the others' tables say there is not looked at."""
+    b = Batch(16, 64, 8, 2, [(48 + 16 * (g % 3), [(5, 0), (new + g % 2, new), (new + 30, new), (new, new)]) for g in range(count)], "int8")
+    want = b.want()
+    for g in range(count):
+        pages = 3 + g % 3
+        b.pages[4 * g, :pages] = -1                          # (no rows)
+        b.pages[4 * g + 2, :pages], b.pages[4 * g + 3, :pages] = -1, b.pages[(4 * g + 17) % (4 * count), 0]
+    check_attn(b.run(), want)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("fmt", FORMATS)
 def test_less_is_shared_than_said(fmt):
     """Lengths that no page ends at, rows that do not see all that is said to be common, negative ones, sequences outside groups, groups of one sequence or of none."""

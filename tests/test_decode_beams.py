@@ -18,7 +18,7 @@ def rows_of(cache, table, n, P, fmt):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("fmt, P, D, hq, hkv, beams, lens, rot, width", [
-    ("e4m3", 64, 128, 8, 2, 4, [150, 3, 64], 128, 400), ("int8", 16, 64, 4, 4, 3, [33, 16, 1, 47], 0, 16), ("int8", 32, 64, 10, 2, 8, [100], 32, 2000), ("e4m3", 64, 128, 8, 2, 4, [150, 3, 64], 128, 16)])
+    ("e4m3", 64, 128, 8, 2, 4, [150, 3, 64], 128, 600), ("int8", 16, 64, 4, 4, 3, [33, 16, 1, 47], 0, 16), ("int8", 32, 64, 10, 2, 8, [100], 32, 3000), ("e4m3", 64, 128, 8, 2, 4, [150, 3, 64], 128, 16)])
 def test_beams_are_sequences(fmt, P, D, hq, hkv, beams, lens, rot, width):
     """The cached tokens of every beam are, code for code, those of a sequence that was appended alone, whatever beams forked from each other; attention is that over its own table."""
     import torch
@@ -163,7 +163,7 @@ def test_two_steps_in_a_graph():
     import torch
     from paper_2602_21788_amd.decode import CacheDecoder
     g = torch.Generator(device="cuda").manual_seed(9)
-    n, beams, hq, hkv, D, P, vocab, m = 3, 4, 8, 2, 128, 32, 3001, 800          # (tables with which a prompt's beams are worked together)
+    n, beams, hq, hkv, D, P, vocab, m = 3, 4, 8, 2, 128, 32, 3001, 1200          # (tables with which a prompt's beams are worked together)
     rows = n * beams
     draw = lambda r, h: torch.randn(r, h, D, generator=g, device="cuda").to(torch.bfloat16)
     lens = [100, 33, 64]
