@@ -26,7 +26,7 @@ constexpr int kPerGroup = kThreads / kGroups;
 struct BeamArgs {
   const void* logits;
   int64_t row;
-  int32_t rows, beams, vocab, chunks, each, keep, end_token;       // each: logits of a thread
+  int32_t rows, beams, vocab, chunks, length, each, keep, end_token;         // length: logits of a chunk (of a row's last one a few less); each: of a thread
   const float* score;
   const uint8_t* done;
   int32_t* parent;
@@ -121,10 +121,10 @@ __device__ inline double sum_of_wave(double x) {
   return x;
 }
 
-// E elements from `from` on, of which the first `each` are the thread's and those at 0 .. there - 1 exist; the others count as -inf.  meanwhile: what else there is to do before they arrive.
+// E elements from `from` on, of which the first `each` are the thread's and those at 0 .. there - 1 the chunk's; the others count as -inf.  The row has those at 0 .. row_end - 1.  meanwhile: what else there is to do before they arrive.
 template <class T, int E, class Meanwhile>
-__device__ inline void load_row(const T* from, int there, int each, float (&v)[E], Meanwhile meanwhile) {
-  if (there >= E) {
+__device__ inline void load_row(const T* from, int there, int row_end, int each, float (&v)[E], Meanwhile meanwhile) {
+  if (there >= each && row_end >= E) {
     constexpr int W = 16 / sizeof(T);
     struct __attribute__((packed, aligned(sizeof(T)))) Words { uint32_t w[4]; };     // (rows may begin at any element)
     Words r[E / W];
@@ -147,7 +147,7 @@ __device__ inline void load_row(const T* from, int there, int each, float (&v)[E
     meanwhile();
 #pragma unroll
     for (int i = 0; i < E; ++i) {                          // (those behind the row's last logit ask for that one: a load under a condition is waited for before the next is asked for)
-      const float x = (float)from[min(i, there - 1)];
+      const float x = (float)from[min(i, row_end - 1)];
       v[i] = i < min(there, each) ? x : -INFINITY;
     }
   }
@@ -203,11 +203,11 @@ constexpr int kListed = 512;           // places of the list: counting takes abo
 // exactly those beyond it, and of those equal to it the first.  How many are in the list.  reach: zeros.  (The logits are read again: kept in registers until here they
 // cost all blocks, 512 rows of 131072 logits 48.5 us instead of 44.5.)
 template <class T, int E>
-__device__ inline int list_best(const T* from, int there, int each, int keep, uint16_t* list, int32_t* reach, int32_t* sums_before, int32_t& listed) {
+__device__ inline int list_best(const T* from, int there, int row_end, int each, int keep, uint16_t* list, int32_t* reach, int32_t* sums_before, int32_t& listed) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   uint32_t order[E], least = 0;
   float v[E];
-  load_row<T, E>(from, there, each, v, [] {});
+  load_row<T, E>(from, there, row_end, each, v, [] {});
 #pragma unroll
   for (int i = 0; i < E; ++i) order[i] = v[i] > -INFINITY ? order_of(fminf(v[i], FLT_MAX) + 0.f) : 0;
   for (int b = 31; b >= 0; --b) {
@@ -266,10 +266,10 @@ __global__ __launch_bounds__(kThreads, 7) void beam_rows_kernel(BeamArgs a) {
   const int row = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const float score = a.score[row];
   if (!(score > -INFINITY) || (a.done && a.done[row])) return;           // offers nothing, or one candidate whatever its logits
-  const int chunk0 = chunk * (kThreads * a.each), first = chunk0 + (int)threadIdx.x * a.each;
+  const int chunk0 = chunk * a.length, first = (int)threadIdx.x * a.each, there = min(a.length, a.vocab - chunk0) - first;
   float v[E];
-  const T* const x = static_cast<const T*>(a.logits) + (int64_t)row * a.row + first;
-  load_row<T, E>(x, a.vocab - first, a.each, v, [&] { fill_powers(powers); });
+  const T* const x = static_cast<const T*>(a.logits) + (int64_t)row * a.row + chunk0 + first;
+  load_row<T, E>(x, there, a.vocab - chunk0 - first, a.each, v, [&] { fill_powers(powers); });
   float top = -INFINITY;
 #pragma unroll
   for (int i = 0; i < E; ++i) top = fmaxf(top, v[i]);      // (NaN is passed over)
@@ -361,7 +361,7 @@ __global__ __launch_bounds__(kThreads, 7) void beam_rows_kernel(BeamArgs a) {
   if (lane == 0) sums[wave] = sum;
   __syncthreads();
   int n = listed;
-  if (__builtin_expect(n > kListed, false)) n = list_best<T, E>(x, a.vocab - first, a.each, a.keep, list, reach, sums_before, listed);
+  if (__builtin_expect(n > kListed, false)) n = list_best<T, E>(x, there, a.vocab - chunk0 - first, a.each, a.keep, list, reach, sums_before, listed);
   // (the logits themselves are read again: with them the list would take four times the LDS, and fewer blocks would run at once)
   const T* const x0 = static_cast<const T*>(a.logits) + (int64_t)row * a.row + chunk0;
   best_of<kThreads, false>(best, room, n, a.keep, [](uint64_t x, uint64_t y) { return x > y; },
@@ -471,15 +471,17 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a) {
   }
 }
 
-// How a call is divided: chunks of up to 8192 logits where they make three blocks for two CUs, else of up to 2048; all chunks of a row are alike but for the last one's end.  2048 / 8192, bf16 but for the
+// How a call is divided: chunks of up to 8192 logits where they make three blocks for two CUs, else of up to 2048; all chunks of a row are alike, so that every one has
+// something for nearly all of its threads (1024 rows of 256000, 32 kept: 916 us where the last chunk had a quarter of the others').  2048 / 8192, bf16 but for the
 // second: 4 rows of 32000 10.8 / 12.4 us, 8 prompts of 5 over 50001 fp32 13.8 / 14.2, 8 of 8 over 32000 13.9 / 14.1, 12 13.9 / 13.7, 16 17.6 / 15.1, 64 34.5 / 24.1.
-struct BeamPlan { int32_t room, chunks, each; int64_t blocks; };        // room: logits that a thread has registers for
+struct BeamPlan { int32_t room, chunks, length, each; int64_t blocks; };        // room: logits that a thread has registers for
 BeamPlan plan_beam(int64_t rows, int32_t vocab) {
   auto chunks = [&](int64_t each) { return (vocab + kThreads * each - 1) / (kThreads * each); };
   BeamPlan p;
   p.room = rows * chunks(32) >= 384 ? 32 : 8;
   p.chunks = (int32_t)chunks(p.room);
-  p.each = (int32_t)((vocab + (int64_t)kThreads * p.chunks - 1) / ((int64_t)kThreads * p.chunks));
+  p.length = (int32_t)((vocab + (int64_t)p.chunks - 1) / p.chunks);
+  p.each = (p.length + kThreads - 1) / kThreads;
   p.blocks = rows * p.chunks;
   return p;
 }
@@ -532,7 +534,7 @@ extern "C" int fcp_beam_select(const void* logits, int32_t type, int64_t logits_
   const BeamPlan p = plan_beam((int64_t)n_prompts * beams, vocab);
   const size_t need = beam_bytes(p, keep);
   if (scratch_bytes < need) return fail(FCP_ERR_CAPACITY, "%s: scratch has %zu bytes, %zu are needed", who, scratch_bytes, need);
-  BeamArgs a = {logits, logits_row, n_prompts * beams, beams, vocab, p.chunks, p.each, keep, end_token, score, done, parent, token, new_score, new_done};
+  BeamArgs a = {logits, logits_row, n_prompts * beams, beams, vocab, p.chunks, p.length, p.each, keep, end_token, score, done, parent, token, new_score, new_done};
   char* const at = static_cast<char*>(scratch);
   a.lists = reinterpret_cast<uint64_t*>(at);
   a.sums = reinterpret_cast<double*>(at + pad_to((size_t)p.blocks * keep * 8, 256));
