@@ -471,14 +471,15 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(BeamArgs a) {
   }
 }
 
-// How a call is divided: chunks of up to 8192 logits where they make three blocks for two CUs, else of up to 2048; all chunks of a row are alike, so that every one has
+// How a call is divided: chunks of up to 8192 logits where a row has more than 2048 and they make three blocks for two CUs, else of up to 2048; all chunks of a row are alike, so that every one has
 // something for nearly all of its threads (1024 rows of 256000, 32 kept: 916 us where the last chunk had a quarter of the others').  2048 / 8192, bf16 but for the
-// second: 4 rows of 32000 10.8 / 12.4 us, 8 prompts of 5 over 50001 fp32 13.8 / 14.2, 8 of 8 over 32000 13.9 / 14.1, 12 13.9 / 13.7, 16 17.6 / 15.1, 64 34.5 / 24.1.
+// second: 4 rows of 32000 10.8 / 12.4 us, 8 prompts of 5 over 50001 fp32 13.8 / 14.2, 8 of 8 over 32000 13.9 / 14.1, 12 13.9 / 13.7, 16 17.6 / 15.1, 64 34.5 / 24.1; 4096 rows
+// of 2000 25.6 / 34.7, of 5000 48.8 / 36.4.
 struct BeamPlan { int32_t room, chunks, length, each; int64_t blocks; };        // room: logits that a thread has registers for
 BeamPlan plan_beam(int64_t rows, int32_t vocab) {
   auto chunks = [&](int64_t each) { return (vocab + kThreads * each - 1) / (kThreads * each); };
   BeamPlan p;
-  p.room = rows * chunks(32) >= 384 ? 32 : 8;
+  p.room = chunks(8) > 1 && rows * chunks(32) >= 384 ? 32 : 8;
   p.chunks = (int32_t)chunks(p.room);
   p.length = (int32_t)((vocab + (int64_t)p.chunks - 1) / p.chunks);
   p.each = (p.length + kThreads - 1) / kThreads;
