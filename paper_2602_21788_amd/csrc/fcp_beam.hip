@@ -263,7 +263,9 @@ __global__ __launch_bounds__(kThreads, 7) void beam_rows_kernel(BeamArgs a) {
   __shared__ int32_t listed;
   __shared__ uint16_t list[kListed];   // places in the chunk
   __shared__ int32_t reach[32], sums_before[kThreads / 64];
-  const int row = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  // (The blocks of a die are every eighth: a row begins with its own number's chunk, so that chunks that a mask leaves more than others do not meet
+  // in one die.  512 rows of 131072 with a mask that leaves tokens 4000 to 5500: 79 us, 230 else.)
+  const int row = blockIdx.x / a.chunks, chunk = (blockIdx.x + row) % a.chunks, unit = row * a.chunks + chunk, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const float score = a.score[row];
   if (!(score > -INFINITY) || (a.done && a.done[row])) return;           // offers nothing, or one candidate whatever its logits
   const int chunk0 = chunk * a.length, first = (int)threadIdx.x * a.each, there = min(a.length, a.vocab - chunk0) - first;
@@ -366,10 +368,10 @@ __global__ __launch_bounds__(kThreads, 7) void beam_rows_kernel(BeamArgs a) {
   const T* const x0 = static_cast<const T*>(a.logits) + (int64_t)row * a.row + chunk0;
   best_of<kThreads, false>(best, room, n, a.keep, [](uint64_t x, uint64_t y) { return x > y; },
                     [&](int i) { return (uint64_t)order_of(fminf((float)x0[list[i]], FLT_MAX) + 0.f) << 32 | (uint32_t)~(chunk0 + list[i]); });
-  if ((int)threadIdx.x < a.keep) a.lists[(int64_t)blockIdx.x * a.keep + threadIdx.x] = (int)threadIdx.x < n ? best[threadIdx.x] : 0;
+  if ((int)threadIdx.x < a.keep) a.lists[(int64_t)unit * a.keep + threadIdx.x] = (int)threadIdx.x < n ? best[threadIdx.x] : 0;
   if (threadIdx.x == 0) {
-    a.sums[2 * (int64_t)blockIdx.x] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
-    a.sums[2 * (int64_t)blockIdx.x + 1] = reference;
+    a.sums[2 * (int64_t)unit] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+    a.sums[2 * (int64_t)unit + 1] = reference;
   }
 }
 
