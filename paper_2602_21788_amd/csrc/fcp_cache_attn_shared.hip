@@ -537,8 +537,17 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs a) {
   const RowPieces common = a.pieces[kCommon][unit], own = a.pieces[kOwn][unit];
   const int32_t places = a.tables.before_own[a.s.n_seqs], from_row = a.s.cu[0], to_row = a.s.cu[a.s.n_seqs];
   if (places == 0 || tok < from_row || tok >= to_row) return;
-  const int all = __builtin_amdgcn_readfirstlane(common.n + own.n), ch = kCh * lane;
+  // an own part in one piece, as most are, is asked for with the stats of the others
+  const bool one = __builtin_amdgcn_readfirstlane(own.n) == 1;
+  const int all = __builtin_amdgcn_readfirstlane(common.n + (one ? 0 : own.n)), ch = kCh * lane;
   float m = kLow, l = 0.f, o[kCh] = {};
+  if (one) {
+    const float* const from = a.whole[kOwn] + (int64_t)unit * (D + 4);
+    m = from[D];
+    l = from[D + 1];
+#pragma unroll
+    for (int c = 0; c < kCh; ++c) o[c] = from[ch + c];
+  }
   for (int p0 = 0; p0 < all; p0 += 64) {
     const int mine = min(p0 + lane, all - 1);
     const bool is_common = mine < common.n;
