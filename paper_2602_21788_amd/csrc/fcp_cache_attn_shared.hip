@@ -7,9 +7,9 @@
 //   * One launch works both lines, the common one with the bodies for few or for many rows, as the rows of a group are on average; a wave works an own part alone.  Where sequences have more than 16 rows
 //     for a KV head on average each line has a launch of its own.
 //   * A wave for each row joins the pieces of its two items, whose places their workers left for it.
-// 64 samples of a prompt of up to 16384 tokens, e4m3, 32 query heads over 8 KV heads of 128: 43.5 and 9.6 us, 50 together, fcp_cache_attn 174; the products of the common part would take a large product's rate
+// 64 samples of a prompt of up to 16384 tokens, e4m3, 32 query heads over 8 KV heads of 128: 43.6 and 9.2 us, 49.8 together, fcp_cache_attn 174; the products of the common part would take a large product's rate
 // 14 us, the blocks begin them 10 us after the launch does (places 3.4, own parts and the first loads the rest), and partial results are 34 MB.  16 prompts of up to 8000 tokens, 8 beams each, int8: 39 and
-// 6.7 us, 50.5 together, where reading every key once takes 24.
+// 6.5 us, 50.1 together, where reading every key once takes 24.
 #include "fcp_cache_few.h"
 #include "fcp_cache_many.h"
 
@@ -526,7 +526,7 @@ __global__ __launch_bounds__(256, 2) void shared_kernel(SharedArgs a, int kind) 
   }
 }
 
-// A wave for each row: the pieces of its items.  Lane i first looks at the maximum and the sum of piece i, so that all of these are asked for at once; then the sums follow, eight on their way.
+// A wave for each row: the pieces of its items.  Lane i looks at the maximum and the sum of piece i, so that all of these are asked for at once; the sums of eight pieces are on their way beside them, then of eight more.
 template <int D>
 __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs a) {
   constexpr int kCh = D / 64, kAtOnce = 8;
@@ -558,6 +558,20 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs a) {
     const float* const sums = x.n == 1 ? whole : slot + x.lr * D;
     const float* const stats = x.n == 1 ? whole + D : slot + rows * D + x.lr;
     const float pm = stats[0], pl = stats[x.n == 1 ? 1 : rows];
+    const int n = min(all - p0, 64);
+    const uint64_t at = (uint64_t)sums;
+    float po[kAtOnce][kCh], next[kAtOnce][kCh];
+    auto ask = [&](int j0, float (&to)[kAtOnce][kCh]) {
+#pragma unroll
+      for (int j = 0; j < kAtOnce; ++j) {
+        const int k = min(j0 + j, n - 1);
+        const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)at, k), hi = __builtin_amdgcn_readlane((int)(at >> 32), k);
+        const float* const from = reinterpret_cast<const float*>((uint64_t)hi << 32 | lo);
+#pragma unroll
+        for (int c = 0; c < kCh; ++c) to[j][c] = from[ch + c];
+      }
+    };
+    ask(0, po);
     const float top = fmaxf(m, wave_maxf(pm)), before = __builtin_amdgcn_exp2f(m - top);
     const float f = p0 + lane < all ? __builtin_amdgcn_exp2f(pm - top) : 0.f;
     m = top;
@@ -567,23 +581,17 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs a) {
     l = l * before + part;
 #pragma unroll
     for (int c = 0; c < kCh; ++c) o[c] *= before;
-    const int n = min(all - p0, 64);
-    const uint64_t at = (uint64_t)sums;
     for (int j0 = 0; j0 < n; j0 += kAtOnce) {
-      float po[kAtOnce][kCh], pf[kAtOnce];
+      if (j0 + kAtOnce < n) ask(j0 + kAtOnce, next);
 #pragma unroll
       for (int j = 0; j < kAtOnce; ++j) {
-        const int k = min(j0 + j, n - 1);
-        const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)at, k), hi = __builtin_amdgcn_readlane((int)(at >> 32), k);
-        const float* const from = reinterpret_cast<const float*>((uint64_t)hi << 32 | lo);
-        pf[j] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), k));
+        const float pf = j0 + j < n ? __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), min(j0 + j, n - 1))) : 0.f;
 #pragma unroll
-        for (int c = 0; c < kCh; ++c) po[j][c] = from[ch + c];
+        for (int c = 0; c < kCh; ++c) {
+          o[c] += j0 + j < n ? pf * po[j][c] : 0.f;
+          po[j][c] = next[j][c];
+        }
       }
-#pragma unroll
-      for (int j = 0; j < kAtOnce; ++j)
-#pragma unroll
-        for (int c = 0; c < kCh; ++c) o[c] += j0 + j < n ? pf[j] * po[j][c] : 0.f;
     }
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
