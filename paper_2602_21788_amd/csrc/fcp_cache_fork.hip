@@ -59,18 +59,19 @@ __device__ inline int32_t entry(const PageArgs& a, int seq, int place) {
 struct Scan { int32_t before, all; };
 __device__ inline Scan block_scan(int32_t x, int32_t* sums) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int32_t upto = wave_prefix_sum(x);
+  // (two counts in a word may reach its sign)
+  const uint32_t upto = wave_prefix(x, [](int32_t a, int32_t b) { return (int32_t)((uint32_t)a + (uint32_t)b); });
   if (lane == 63) sums[wave] = upto;
   __syncthreads();
-  Scan r = {upto - x, 0};
+  uint32_t before = upto - (uint32_t)x, all = 0;
 #pragma unroll
   for (int w = 0; w < kPlanWaves; ++w) {
-    const int32_t n = sums[w];
-    r.before += w < wave ? n : 0;
-    r.all += n;
+    const uint32_t n = sums[w];
+    before += w < wave ? n : 0;
+    all += n;
   }
   __syncthreads();
-  return r;
+  return {(int32_t)before, (int32_t)all};
 }
 
 // Two counts of up to 33 a thread, in the halves of a word: the block's are below 2^16.
@@ -351,7 +352,7 @@ __global__ __launch_bounds__(kPlanThreads) void fork_small_kernel(PageArgs a) {
     uint32_t free = w < a.words ? ~t.marks.held_word(w) : 0u;
     if (w == a.words - 1 && a.c.n_pages % 32) free &= (1u << (a.c.n_pages % 32)) - 1;
     const int32_t kept = (w < a.words ? __popc(t.marks.read_word(w)) : 0) + (w0 == 0 && page >= 0 && !copy);
-    const Pair at = pair_of(block_scan(__popc(free) | kept << 16, sums));
+    const Pair at = pair_of(block_scan((int32_t)(__popc(free) | (uint32_t)kept << 16), sums));
     int32_t rank = listed + at.low.before;
     for (; free && rank < need; free &= free - 1, ++rank) (rank < kListed ? list : a.list)[rank] = 32 * w + __builtin_ctz(free);
     listed += at.low.all;
@@ -391,7 +392,7 @@ __device__ inline void plan_compact(const PageArgs& a, const Marks& marks) {
     const int w = w0 + threadIdx.x;
     const uint32_t h = w < a.words ? marks.held_word(w) : 0u, b = w < a.words ? busy_bits(w) : 0u;
     if (b) atomicMax(&busy_end, 32 * w + 32 - __builtin_clz(b));
-    const Pair n = pair_of(block_scan(__popc(h & ~b) | __popc(h) << 16, sums));
+    const Pair n = pair_of(block_scan((int32_t)(__popc(h & ~b) | (uint32_t)__popc(h) << 16), sums));
     used += n.low.all;
     all += n.high.all;
   }
@@ -419,7 +420,7 @@ __device__ inline void plan_compact(const PageArgs& a, const Marks& marks) {
       hole = low & ~h & ~b;
       mover = ~low & h & ~b;
     }
-    const Pair n = pair_of(block_scan(__popc(hole) | __popc(mover) << 16, sums));
+    const Pair n = pair_of(block_scan((int32_t)(__popc(hole) | (uint32_t)__popc(mover) << 16), sums));
     int32_t rank = holes + n.low.before;
     for (; hole; hole &= hole - 1) a.list[rank++] = 32 * w + __builtin_ctz(hole);
     rank = movers + n.high.before;

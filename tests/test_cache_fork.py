@@ -284,6 +284,35 @@ def test_fork_many(n, m, n_pages, n_new):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("n, m, n_pages, n_new", [(300, 9, 70001, 1000), (20, 30, 262144, 1024), (1000, 30, 40000, 1024), (64, 30, 65569, 700)])
+def test_one_block_over_many_pages(n, m, n_pages, n_new):
+    """Pools of more pages than a block's threads look at once, where one block marks and plans; more fresh pages than LDS lists; some busy."""
+    rng = np.random.default_rng(n)
+    pool = Pool(rng, n_pages, 16, hkv=1)
+    busy = (rng.random(n_pages) < 0.3).astype(np.uint8)
+    pages, lens = _tables(rng, n, m, n_pages, 16, busy)
+    for high in (20, 150):
+        w = _fork(pool, pages, lens, rng.integers(-1, n, n_new), rng.integers(0, high, n_new), busy)
+        _compact(pool, w[0], w[1], busy)
+
+
+@pytest.mark.gpu
+def test_every_page_of_a_block_held():
+    """32768 pages, all of them held, and read by sequences that go on; then all but one, which moves."""
+    rng = np.random.default_rng(1)
+    pool = Pool(rng, 32768, 16, hkv=1)
+    pages, lens = rng.permutation(32768).astype(np.int32).reshape(1024, 32), np.full(1024, 512, np.int32)
+    w = _fork(pool, pages, lens, np.arange(1024), np.zeros(1024, np.int32))
+    assert w[2] == [0, 0, 0]
+    assert _compact(pool, pages, lens)[1] == [0, 32768, 32768]
+    at = tuple(np.argwhere(pages == 5)[0])
+    pages[at] = -1
+    assert _compact(pool, pages, lens)[1] == [1, 32767, 32767]
+    w = _fork(pool, pages, lens - 3, np.arange(1024), np.ones(1024, np.int32))
+    assert w[2] == [0, 0, 1]
+
+
+@pytest.mark.gpu
 def test_steps_one_after_the_other():
     """A prompt, its beams, and then every step's tables out of those before; compacted in between."""
     rng = np.random.default_rng(10)
