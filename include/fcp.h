@@ -582,8 +582,8 @@ int fcp_cache_compact(const fcp_cache* cache, const int32_t* pages, const int32_
  *   shared_len [n_groups] int32 device: tokens that the sequences of the group have in common: their tables name the same pages there, and those of the group's first sequence with rows are
  *   read.  Less is taken where a row does not see as many: whole pages, at most the tokens before the new ones of every sequence.
  *   n_groups from 0 to n_seqs.  scratch: fcp_cache_scratch_bytes(FCP_SCRATCH_CACHE_SHARED, ...).  Other arguments, results, limits and errors as in fcp_cache_attn.
- * Scores, statistics and sums are held in 32 bits; probabilities are rounded to bf16 for the product with V, and for the parts that up to 32 rows on average see, of a group or of a sequence
- * and KV head, what that leaves is multiplied too.  No atomics: results repeat bit for bit.
+ * Precision as in fcp_cache_attn for the same sequences, whatever the groups: scores, statistics and sums are held in 32 bits; probabilities are rounded to bf16 for the product with V, and with
+ * up to 32 rows per sequence and KV head on average what that leaves is multiplied too.  No atomics: results repeat bit for bit.
  */
 int fcp_cache_attn_shared(const fcp_cache* cache, const void* q, int64_t q_row, int32_t tq, int32_t hq, const int32_t* cu_seqlens, const int32_t* kv_len,
                           const int32_t* pages, int32_t n_seqs, int32_t max_pages, const int32_t* groups, const int32_t* shared_len, int32_t n_groups,

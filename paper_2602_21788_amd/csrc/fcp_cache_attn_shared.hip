@@ -7,8 +7,8 @@
 //   * One launch works both lines, the common one with the bodies for few or for many rows, as the rows of a group are on average; a wave works an own part alone.  Where sequences have more than 16 rows
 //     for a KV head on average each line has a launch of its own.
 //   * A wave for each row joins the pieces of its two items, whose places their workers left for it.
-// 64 samples of a prompt of up to 16384 tokens, e4m3, 32 query heads over 8 KV heads of 128: 43.6 and 9.2 us, 49.8 together, fcp_cache_attn 174; the products of the common part would take a large product's rate
-// 14 us, the blocks begin them 10 us after the launch does (places 3.4, own parts and the first loads the rest), and partial results are 34 MB.  16 prompts of up to 8000 tokens, 8 beams each, int8: 39 and
+// 64 samples of a prompt of up to 16384 tokens, e4m3, 32 query heads over 8 KV heads of 128: 59 us, fcp_cache_attn 174; the products of the common part would take a large product's rate
+// 14 us (21 with probabilities in two parts), the blocks begin them 10 us after the launch does (places 3.4, own parts and the first loads the rest), and partial results are 34 MB.  16 prompts of up to 8000 tokens, 8 beams each, int8: 39 and
 // 6.5 us, 50.1 together, where reading every key once takes 24.
 #include "fcp_cache_few.h"
 #include "fcp_cache_many.h"
@@ -448,7 +448,7 @@ __device__ inline void own_rows(const SharedArgs& a, const Tables& t, int lane, 
   }
 }
 
-template <int D, int Fmt, int kNB>
+template <int D, int Fmt, int kNB, bool Rest>
 __device__ inline void many_rows(const SharedArgs& a, const Tables& t, int kind, int lane, int wave, unsigned char* lds, float (&key_scale)[4][4], int32_t (&live)[4][4], int32_t (&first_nan)[2][D]) {
   constexpr int kRows = 64 * kNB;
   const int n = lane & 15, g = lane >> 4;
@@ -479,7 +479,7 @@ __device__ inline void many_rows(const SharedArgs& a, const Tables& t, int kind,
     const int rows = min(w.all_rows - w.row_block * kRows, kRows), all_see = w.sees(w.row_block * kRows / a.group), seen = w.sees((w.row_block * kRows + rows - 1) / a.group);
     const int t_end = min(w.t1, seen < 0 ? 0 : seen / kTile + 1);
     if (w.t0 < t_end) {
-      walk_rows<D, Fmt, kNB>(a.c, a.scale, w.table(a), w.head, w.part.len, w.t0, t_end, q, last, all_see, o, m, l, lane, wave, at_lane, lds, key_scale, live, first_nan, parity);
+      walk_rows<D, Fmt, kNB, Rest>(a.c, a.scale, w.table(a), w.head, w.part.len, w.t0, t_end, q, last, all_see, o, m, l, lane, wave, at_lane, lds, key_scale, live, first_nan, parity);
       parity ^= 1;
     }
 #pragma unroll
@@ -502,8 +502,8 @@ __device__ inline void many_rows(const SharedArgs& a, const Tables& t, int kind,
   }
 }
 
-// One launch works both lines (Own), or the line `kind`.  kRows: 16, 32, 64, 128 rows of an item.
-template <int D, int Fmt, int kRows, bool Own>
+// One launch works both lines (Own), or the line `kind`.  kRows: 16, 32, 64, 128 rows of an item.  Rest: of 64 and 128 (others always): probabilities in two parts.
+template <int D, int Fmt, int kRows, bool Own, bool Rest>
 __global__ __launch_bounds__(256, 2) void shared_kernel(SharedArgs a, int kind) {
   __shared__ LocalTables local;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -522,7 +522,7 @@ __global__ __launch_bounds__(256, 2) void shared_kernel(SharedArgs a, int kind) 
       own_rows<D, Fmt>(a, t, lane, wave, reinterpret_cast<int32_t*>(lds) + wave * D);
       __syncthreads();
     }
-    many_rows<D, Fmt, kRows / 64>(a, t, kind, lane, wave, lds, key_scale, live, first_nan);
+    many_rows<D, Fmt, kRows / 64, Rest>(a, t, kind, lane, wave, lds, key_scale, live, first_nan);
   }
 }
 
@@ -645,10 +645,10 @@ SharedSpace shared_space(const CacheView& c, int head_dim, int32_t n_seqs, int32
   return s;
 }
 
-template <int D, int Fmt, int kRows, bool Own>
+template <int D, int Fmt, int kRows, bool Own, bool Rest>
 int launch_line(const SharedArgs& a, int kind, hipStream_t st) {
   constexpr int kLds = kRows <= 32 ? 0 : 2 * Stage<D>::kBytes;
-  auto kernel = shared_kernel<D, Fmt, kRows, Own>;
+  auto kernel = shared_kernel<D, Fmt, kRows, Own, Rest>;
   if (kLds > 48 * 1024) {
     static std::atomic<uint64_t> raised;
     if (int rc = raise_lds_limit(reinterpret_cast<const void*>(kernel), kLds, raised)) return rc;
@@ -666,13 +666,17 @@ int launch_shared(const SharedArgs& a, hipStream_t st) {
   }
   const int common = 1 << a.log_rows[kCommon];
   int rc;
+  // Probabilities are as exact as fcp_cache_attn has them for the same sequences: in two parts, however many rows a group brings together, but where sequences have more than 32 rows.
   if (a.waves) {
-    rc = common == 16 ? launch_line<D, Fmt, 16, true>(a, kCommon, st) : common == 32 ? launch_line<D, Fmt, 32, true>(a, kCommon, st)
-       : common == 64 ? launch_line<D, Fmt, 64, true>(a, kCommon, st) : launch_line<D, Fmt, 128, true>(a, kCommon, st);
+    rc = common == 16 ? launch_line<D, Fmt, 16, true, true>(a, kCommon, st) : common == 32 ? launch_line<D, Fmt, 32, true, true>(a, kCommon, st)
+       : common == 64 ? launch_line<D, Fmt, 64, true, true>(a, kCommon, st) : launch_line<D, Fmt, 128, true, true>(a, kCommon, st);
+  } else if (a.log_rows[kOwn] == 5) {
+    rc = common == 32 ? launch_line<D, Fmt, 32, false, true>(a, kCommon, st) : common == 64 ? launch_line<D, Fmt, 64, false, true>(a, kCommon, st)
+       : launch_line<D, Fmt, 128, false, true>(a, kCommon, st);
+    if (!rc) rc = launch_line<D, Fmt, 32, false, true>(a, kOwn, st);
   } else {
-    rc = common == 32 ? launch_line<D, Fmt, 32, false>(a, kCommon, st) : common == 64 ? launch_line<D, Fmt, 64, false>(a, kCommon, st)
-       : launch_line<D, Fmt, 128, false>(a, kCommon, st);
-    if (!rc) rc = a.log_rows[kOwn] == 5 ? launch_line<D, Fmt, 32, false>(a, kOwn, st) : launch_line<D, Fmt, 64, false>(a, kOwn, st);
+    rc = common == 64 ? launch_line<D, Fmt, 64, false, false>(a, kCommon, st) : launch_line<D, Fmt, 128, false, false>(a, kCommon, st);
+    if (!rc) rc = launch_line<D, Fmt, 64, false, false>(a, kOwn, st);
   }
   if (rc) return rc;
   shared_join_kernel<D><<<dim3((unsigned)(((int64_t)a.s.n_rows * a.hq + 3) / 4)), dim3(256), 0, st>>>(a);
