@@ -554,8 +554,8 @@ int fcp_cache_evict(const fcp_cache* cache, const int32_t* pages, const int32_t*
  *   busy [n_pages] bytes, device, or NULL: not 0 for pages that others hold, sequences outside the call say
  *   counts [3] int32 device out: pages handed out, pages that were lacking, pages that neither the new tables nor others hold
  *   scratch: device, 256-byte aligned, fcp_cache_scratch_bytes(FCP_SCRATCH_CACHE_FORK, cache, n_new, max_pages, ...); contents on entry irrelevant
- * While the call runs nobody else may write the pages of its sequences or use free ones.  2^24 blocks of work or more (one for 256 entries of a table, one for each (new sequence, KV head))
- * are FCP_ERR_UNSUPPORTED.
+ * While the call runs nobody else may write the pages of its sequences or use free ones.  2^24 blocks of work or more (one for 256 entries of a table, one for each (new sequence, KV head)),
+ * and new tables of 2^31 entries or more, are FCP_ERR_UNSUPPORTED.
  */
 int fcp_cache_fork(const fcp_cache* cache, const int32_t* pages, const int32_t* kv_len, int32_t n_seqs, int32_t max_pages, const int32_t* parent,
                    const int32_t* news, int32_t n_new, const uint8_t* busy, int32_t* new_pages, int32_t* new_len, int32_t* counts,
@@ -568,7 +568,7 @@ int fcp_cache_fork(const fcp_cache* cache, const int32_t* pages, const int32_t* 
  *   busy as above: such pages stay where they are
  *   counts [3] int32 device out: pages moved, pages in use, the first number past all pages that are in use or busy
  *   scratch: fcp_cache_scratch_bytes(FCP_SCRATCH_CACHE_COMPACT, cache, n_seqs, max_pages, ...)
- * Old pages keep their contents until somebody writes them.  Limits as above.
+ * Old pages keep their contents until somebody writes them.  2^24 blocks of work or more are FCP_ERR_UNSUPPORTED.
  */
 int fcp_cache_compact(const fcp_cache* cache, const int32_t* pages, const int32_t* kv_len, int32_t n_seqs, int32_t max_pages, const uint8_t* busy,
                       int32_t* new_pages, int32_t* counts, void* scratch, size_t scratch_bytes, void* stream);

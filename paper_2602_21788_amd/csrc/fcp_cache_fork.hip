@@ -549,6 +549,8 @@ int check_page_sizes(const char* who, const CacheView& c, int32_t n_seqs, int32_
   if (int rc = check_sizes(who, c, n_new, max_pages, 0)) return rc;
   if (!fits_axis((((int64_t)n_seqs + n_new) * ((max_pages + 63) / 64) + 3) / 4, 256) || !fits_axis((int64_t)n_new * (c.hkv + (max_pages + 255) / 256), 256))
     return fail(FCP_ERR_UNSUPPORTED, "%s: 2^24 blocks of work or more", who);
+  // (the pages that new sequences need are added up in 32 bits: at most one for each entry)
+  if ((int64_t)n_new * max_pages > INT32_MAX) return fail(FCP_ERR_UNSUPPORTED, "%s: new tables of 2^31 entries or more", who);
   return FCP_OK;
 }
 int check_scratch(const char* who, const void* scratch, size_t have, size_t need) {
