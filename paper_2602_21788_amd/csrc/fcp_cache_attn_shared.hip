@@ -36,8 +36,9 @@ struct Tables {
   __device__ int32_t* before(int kind) const { return kind == kCommon ? before_common : before_own; }
 };
 
-// Where the pieces of a row's item lie: slots of blocks (waves) first, first + 1, ..; n = 1: in `whole`, n = 0: there is none.  lr: its row in a slot.
-struct RowPieces { int32_t first, n, lr, pad; };
+// Where the pieces of a row's item lie: slots of blocks (waves) first, first + 1, ..; n = 1: in `whole`.  lr: its row in a slot.  common: own parts: the row has a common part too (else what the
+// common part's worker noted for the row does not count).
+struct RowPieces { int32_t first, n, lr, common; };
 
 struct SharedArgs {
   CacheView c;
@@ -108,18 +109,20 @@ __device__ inline int share_of_block(const SharedArgs& a, int kind) { return kin
 
 // The common parts from the groups and the own parts' entries; these learn their group.
 struct Group { int32_t lo, hi, said; };
-// What every row of a group sees, at most `said`, its first sequence and row, its rows and sequences: of some of its sequences.  Those without rows do not count.
-struct Seen { int32_t least, first, row0, rows, seqs; };
-__device__ inline Seen look_at(const Tables& t, const Group& x, int g, int sub, int lanes) {
+// What every row of a group sees, at most `said`, its first sequence, its first row and the one behind its last, its sequences: of some of its sequences.  Those without rows do not count, nor do those
+// with a row that does not see a page before the new ones (a beam that has just begun): these are worked by themselves, and do not keep the others from what they have in common.  Where the rows of
+// such a sequence lie between the others' they are worked with them, and nobody looks at what comes out.
+struct Seen { int32_t least, first, row0, end, seqs; };
+__device__ inline Seen look_at(const Tables& t, const Group& x, int g, int sub, int lanes, int page) {
   Seen r = {max(x.said, 0), INT32_MAX, INT32_MAX, 0, 0};
   for (int s = x.lo + sub; s < x.hi; s += lanes) {
     const Entry y = t.own[s];
-    t.own[s].other = g;
-    if (y.rows > 0) {
-      r.least = min(r.least, max(y.len - y.rows, 0));
+    if (y.rows > 0 && y.len - y.rows >= page) {
+      t.own[s].other = g;
+      r.least = min(r.least, y.len - y.rows);
       r.first = min(r.first, s);
       r.row0 = min(r.row0, y.row0);
-      r.rows += y.rows;
+      r.end = max(r.end, y.row0 + y.rows);
       ++r.seqs;
     }
   }
@@ -127,26 +130,26 @@ __device__ inline Seen look_at(const Tables& t, const Group& x, int g, int sub, 
 }
 __device__ inline Entry common_of(const Seen& x, int page) {
   const int32_t shared = x.seqs < 2 ? 0 : x.least & ~(page - 1);
-  return {x.row0, shared ? x.rows : 0, x.first, shared};
+  return {x.row0, shared ? x.end - x.row0 : 0, x.first, shared};
 }
 template <int Threads, class F>
 __device__ inline void place_groups(const SharedArgs& a, const Tables& t, F group) {
   if (a.n_groups <= Threads / 64) {                                     // a wave a group (300 sequences of one group: 48 us, 56 with eight lanes)
     const int g = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     if (g >= a.n_groups) return;
-    Seen x = look_at(t, group(g), g, lane, 64);
+    Seen x = look_at(t, group(g), g, lane, 64, a.c.page);
     auto least_of = [](int32_t v) { return INT32_MAX - wave_max(INT32_MAX - v); };
     auto sum_of = [](int32_t v) { return __builtin_amdgcn_readlane(wave_prefix_sum(v), 63); };
-    x = {least_of(x.least), least_of(x.first), least_of(x.row0), sum_of(x.rows), sum_of(x.seqs)};
+    x = {least_of(x.least), least_of(x.first), least_of(x.row0), wave_max(x.end), sum_of(x.seqs)};
     if (lane == 0) t.common[g] = common_of(x, a.c.page);
     return;
   }
   for (int g0 = 0; g0 < a.n_groups; g0 += Threads / 8) {                // eight lanes a group
     const int g = g0 + (int)threadIdx.x / 8, sub = threadIdx.x % 8;
-    Seen x = look_at(t, g < a.n_groups ? group(g) : Group{0, 0, 0}, g, sub, 8);
+    Seen x = look_at(t, g < a.n_groups ? group(g) : Group{0, 0, 0}, g, sub, 8, a.c.page);
 #pragma unroll
     for (int d = 1; d < 8; d *= 2)
-      x = {min(x.least, __shfl_xor(x.least, d)), min(x.first, __shfl_xor(x.first, d)), min(x.row0, __shfl_xor(x.row0, d)), x.rows + __shfl_xor(x.rows, d), x.seqs + __shfl_xor(x.seqs, d)};
+      x = {min(x.least, __shfl_xor(x.least, d)), min(x.first, __shfl_xor(x.first, d)), min(x.row0, __shfl_xor(x.row0, d)), max(x.end, __shfl_xor(x.end, d)), x.seqs + __shfl_xor(x.seqs, d)};
     if (g < a.n_groups && sub == 0) t.common[g] = common_of(x, a.c.page);
   }
 }
@@ -311,8 +314,7 @@ struct Work {
     const int row0 = row_block << a.log_rows[kind], rows = min(1 << a.log_rows[kind], all_rows - row0), n = whole ? 1 : shares_of(a, t, kind).even.owner(item0 + kItemLead + tiles - 1) - me + 1;
     for (int lr = i; lr < rows; lr += step) {
       const int64_t row = whole_row(a, row0 + lr);
-      a.pieces[kind][row] = {me, n, lr, 0};
-      if (kind == kOwn && !part.common) a.pieces[kCommon][row] = {0, 0, 0, 0};
+      a.pieces[kind][row] = {me, n, lr, part.common};
     }
   }
   __device__ bool next(const SharedArgs& a) {
@@ -534,9 +536,11 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs a) {
   if (unit >= a.s.n_rows * a.hq) return;
   const int tok = unit / a.hq, h = unit - tok * a.hq;
   // (all asked for at once)
-  const RowPieces common = a.pieces[kCommon][unit], own = a.pieces[kOwn][unit];
+  RowPieces common = a.pieces[kCommon][unit];
+  const RowPieces own = a.pieces[kOwn][unit];
   const int32_t places = a.tables.before_own[a.s.n_seqs], from_row = a.s.cu[0], to_row = a.s.cu[a.s.n_seqs];
   if (places == 0 || tok < from_row || tok >= to_row) return;
+  if (!own.common) common.n = 0;
   // an own part in one piece, as most are, is asked for with the stats of the others
   const bool one = __builtin_amdgcn_readfirstlane(own.n) == 1;
   const int all = __builtin_amdgcn_readfirstlane(common.n + (one ? 0 : own.n)), ch = kCh * lane;
