@@ -579,9 +579,11 @@ int fcp_cache_compact(const fcp_cache* cache, const int32_t* pages, const int32_
  *   groups [n_groups + 1] int32 device: the sequences groups[g] .. groups[g + 1] - 1 are group g; not falling, within 0 .. n_seqs.  Sequences outside all groups, and groups of one
  *   sequence with rows, are worked by themselves; so are all, whatever groups and shared_len hold, where the tables are too small to gain by it, or sequences have more than 64 rows for a KV head on
  *   average.  Else the call does nothing where groups fall or leave 0 .. n_seqs, as where cu_seqlens falls.
- *   shared_len [n_groups] int32 device: tokens that the sequences of the group have in common: their tables name the same pages there, and those of the group's first sequence with rows are
- *   read.  Less is taken where a row does not see as many: whole pages, at most the tokens before the new ones of every sequence.  Sequences with less than a page before their new tokens
+ *   shared_len [n_groups] int32 device: tokens that the sequences of the group have in common: their tables name the same pages there, and those of the group's first sequence with rows and a
+ *   whole page before them are read.  Less is taken where a row does not see as many: whole pages, at most the tokens before the new ones of every sequence.  Sequences with less than a page before their new tokens
  *   do not count: they have nothing in common with the others, and are worked by themselves.
+ * What it gains is bytes: it pays where what is common is long beside a sequence's own tokens.  fcp_cache_attn is as fast or faster where own parts are as long as the common ones (64 sequences of
+ * 512 + 3000 tokens 79 us, 102 here) and for 17 to 32 rows per sequence and KV head; only the device knows the lengths, and the sizes that the host looks at are those of the tables, full or not.
  *   n_groups from 0 to n_seqs.  scratch: fcp_cache_scratch_bytes(FCP_SCRATCH_CACHE_SHARED, ...).  Other arguments, results, limits and errors as in fcp_cache_attn.
  * Precision as in fcp_cache_attn for the same sequences, whatever the groups: scores, statistics and sums are held in 32 bits; probabilities are rounded to bf16 for the product with V, and with
  * up to 32 rows per sequence and KV head on average what that leaves is multiplied too.  No atomics: results repeat bit for bit.

@@ -627,11 +627,12 @@ struct SharedSpace { size_t parts[2], before[2], pieces[2], slots[2], whole[2], 
 // Whether every sequence is worked by itself, as fcp_cache_attn does.  Many rows of a sequence are attention of many rows already: the matrix units bound it, and the bytes that sequences share are read from
 // the L2s (8 questions of 256 tokens about 4000: 221 us so, 328 in groups).  Else what groups gain is bytes, and what they cost is the second part and its joining, 8 to 15 us of a call, more with two
 // launches.  How long the common parts are only the device knows; what they may save at most follows from the tables' size.  Itself / in groups, e4m3, 32 query heads over 8 KV heads, MB that may be saved:
-// 4 rows for a KV head 4 MB 8 / 18 us, 63 19.8 / 19.4, 73 20 / 26, 135 28 / 28, 249 48 / 39, 1000 94 / 52, 2200 174 / 54; 16 rows 123 MB 29 / 36, 1000 99 / 75, 2200 185 / 117; 32 rows 123 MB 39 / 55, 478 85 / 79, 985 133 / 140, 2200 222 / 193;
-// 64 rows 63 MB 37 / 55, 478 134 / 119, 2200 456 / 338.
+// 4 rows for a KV head 4 MB 8 / 18 us, 63 19.8 / 19.4, 73 20 / 26, 135 28 / 30, 251 43 / 30 and 33 / 27, 500 58 / 36, 2200 174 / 64; 8 rows 251 MB 46 / 36 and 34 / 36, 520 54 / 46; 16 rows 123 MB 29 / 36, 503 80 / 57 and
+// 54 / 65, 1000 92 / 79, 2200 188 / 144; 64 rows 63 MB 37 / 55, 478 134 / 119, 2200 456 / 338.  17 to 32 rows gain little or nothing, since both ways multiply probabilities in two parts and the products are
+// what bounds them: 32 rows 123 MB 39 / 55, 478 92 / 92, 985 118 / 144, 2200 230 / 242.
 bool by_itself(const CacheView& c, int head_dim, int32_t n_seqs, int32_t n_groups, int32_t max_pages, int32_t tq, int32_t hq) {
   const int64_t rows = (int64_t)tq * (hq / c.hkv), saved = n_groups == 0 ? 0 : (int64_t)(n_seqs - n_groups) * max_pages * c.page * c.hkv * 2 * head_dim;
-  return rows > (int64_t)64 * n_seqs || saved < (int64_t)(rows <= (int64_t)8 * n_seqs ? 1 : rows <= (int64_t)16 * n_seqs ? 2 : 3) << 27;
+  return rows > (int64_t)64 * n_seqs || saved < (int64_t)(rows <= (int64_t)8 * n_seqs ? 1 : 3) << 27;
 }
 SharedSpace shared_space(const CacheView& c, int head_dim, int32_t n_seqs, int32_t tq, int32_t hq) {
   SharedSpace s;
