@@ -547,7 +547,8 @@ int fcp_cache_evict(const fcp_cache* cache, const int32_t* pages, const int32_t*
  *   - A page that holds tokens of the parent and gets new ones must belong to one sequence: where several would write it the lowest keeps it, but none does if others only read it or it is
  *     busy.  The others get a copy of the parent's tokens in it: codes (values in whole groups of 16 tokens), scales, weights if the cache has them.
  *   - Fresh pages, for copies and for new tokens, are handed out in increasing order to the sequences in order, and within one in the order of its table: the lowest numbers that no sequence of
- *     this step holds and that are not busy.  If there are too few the rest of the entries are -1 (such tokens are not written, and seen by nobody).
+ *     this step holds and that are not busy.  If there are too few the rest of the entries are -1 (such tokens are not written, and seen by nobody; where a copy finds no page that goes for the
+ *     parent's tokens in it too).  An entry that is no page's number already stays -1 and is not counted as lacking, also where new tokens would go.
  *   - Pages that only sequences without children held are free afterwards, for the next call: this one does not write them.
  * Entries of parents' tables that are no page's number become -1.  Entries behind a sequence's last page are -1.
  *   pages [n_seqs][max_pages], kv_len [n_seqs];  parent, news [n_new];  new_pages [n_new][max_pages], new_len [n_new] out, apart from the old tables: int32 device

@@ -171,7 +171,8 @@ class CacheDecoder:
 
 
 class BeamDecoder:
-    """`beams` continuations of each of n_prompts prompts, one layer.  The tables live on the device: a step needs nothing from the host but the rows.
+    """`beams` continuations of each of n_prompts prompts, one layer.  The tables live on the device: a step needs nothing from the host but the rows, and the host waits for it only to learn whether
+    there were pages enough (check).
 
         dec.prefill(q, k, v, lens)                      # the prompts
         loop: tokens, parents = dec.select(logits)      # logits [n_prompts, vocab] after the prompts, then [n_prompts * beams, vocab]
@@ -202,6 +203,7 @@ class BeamDecoder:
         self._shared = self.prompts._to(np.asarray(lens) // self.prompts.P * self.prompts.P)     # (the page in which a prompt ends is every beam's own)
         self.score, self.done = torch.zeros(self.n, device=self.device), torch.zeros(self.n, dtype=torch.uint8, device=self.device)
         self.chosen, self.history, self.steps = None, [], 0
+        self._unchecked = False                              # whether a step may have found too few pages
         return out
 
     def select(self, logits):
@@ -221,7 +223,8 @@ class BeamDecoder:
 
     def step(self, q, k, v, check=True):
         """The rows of the chosen tokens, bf16 [n_prompts * beams, heads, D] (turned in place): O, LSE.  check: raises MemoryError, and leaves the beams as they were, where the pool has too few
-        pages, for which the host waits; without it the tokens that found no page are seen by nobody."""
+        pages, or a new token would go into one that was lacking in an earlier step; the host waits for this.  Without it tokens that found no page are seen by nobody, and if the page would
+        have been a copy of one that is begun, neither are the beam's earlier tokens in it nor its next ones, until that page ends."""
         if self.chosen is None:
             raise ValueError("select() chooses the tokens whose rows step() takes")
         dec, rows = self.prompts, self.n * self.beams
@@ -233,11 +236,14 @@ class BeamDecoder:
         B.fcp_cache_fork(self.cache, self.pages, self.kv_len, self.chosen, self._ones, pages, kv_len, self.counts, self._fork_scratch)
         if check and int(self.counts[1]):
             raise MemoryError("no page left")
+        if check and self._unchecked and bool((pages.gather(1, (kv_len - 1).long()[:, None] // dec.P) < 0).any()):
+            raise MemoryError("a beam has no page for its next token: an earlier step without check found none")
         if dec.rot_dim:
             dec._rotate(q, k, kv_len - 1)                    # (the new token is the last one)
         B.fcp_cache_append(self.cache, k, v, self._cu, kv_len, pages)
         B.fcp_cache_attn_shared(self.cache, q, self._cu, kv_len, pages, self._groups, self._shared, self.scale, o, lse, self._attn_scratch)
         self.pages, self.kv_len, self.chosen = pages, kv_len, None
+        self._unchecked |= not check
         self.steps += 1
         self._longest += 1
         return o, lse
