@@ -199,7 +199,8 @@ class BeamDecoder:
         out = self.prompts.prefill(q, k, v, lens)
         self.prompts._upload()                               # (prompts may all be empty)
         self.pages, self.kv_len = self.prompts.pages_d, self.prompts.kv_len_d
-        self._longest = int(np.max(lens, initial=0))         # tokens of the longest sequence
+        self._lens = np.asarray(lens, np.int64)
+        self._longest = int(np.max(lens, initial=0))         # tokens of the longest sequence that goes on, or more
         self._shared = self.prompts._to(np.asarray(lens) // self.prompts.P * self.prompts.P)     # (the page in which a prompt ends is every beam's own)
         self.score, self.done = torch.zeros(self.n, device=self.device), torch.zeros(self.n, dtype=torch.uint8, device=self.device)
         self.chosen, self.history, self.steps = None, [], 0
@@ -221,27 +222,36 @@ class BeamDecoder:
         self.history.append((parent, token))
         return token, parent
 
+    def _going(self):
+        """[n_prompts, 1] bool: prompts of which a chosen beam goes on.  The others' have all ended, or there was no candidate; this stays so."""
+        return ((self.done == 0) & (self.chosen >= 0)).view(self.n, self.beams).any(1, keepdim=True)
+
     def step(self, q, k, v, check=True):
         """The rows of the chosen tokens, bf16 [n_prompts * beams, heads, D] (turned in place): O, LSE.  check: raises MemoryError, and leaves the beams as they were, where the pool has too few
         pages, or a new token would go into one that was lacking in an earlier step; the host waits for this.  Without it tokens that found no page are seen by nobody, and if the page would
-        have been a copy of one that is begun, neither are the beam's earlier tokens in it nor its next ones, until that page ends."""
+        have been a copy of one that is begun, neither are the beam's earlier tokens in it nor its next ones, until that page ends.
+        Prompts whose beams have all ended stay as they are: their rows are not appended and take no pages, O is 0 and LSE -inf for them.  (With an end token this takes 7 small launches a step.)"""
         if self.chosen is None:
             raise ValueError("select() chooses the tokens whose rows step() takes")
         dec, rows = self.prompts, self.n * self.beams
         dec._fit(q, k, v, rows)
-        if self._longest == dec.pages.shape[1] * dec.P:
-            raise MemoryError("a sequence's table is full")
+        if self._longest == dec.pages.shape[1] * dec.P:      # (the host waits here alone: prompts may have ended)
+            self._longest = int(np.max(self._lens[self._going().cpu().numpy()[:, 0]] + self.steps, initial=0))
+            if self._longest == dec.pages.shape[1] * dec.P:
+                raise MemoryError("a sequence's table is full")
         o, lse = torch.empty(q.shape, dtype=torch.bfloat16, device=self.device), torch.empty(dec.hq, rows, dtype=torch.float32, device=self.device)
         pages, kv_len = self._tables[self.steps % 2]
-        B.fcp_cache_fork(self.cache, self.pages, self.kv_len, self.chosen, self._ones, pages, kv_len, self.counts, self._fork_scratch)
+        news = self._ones if self.end < 0 else self._going().expand(-1, self.beams).reshape(-1).int()
+        B.fcp_cache_fork(self.cache, self.pages, self.kv_len, self.chosen, news, pages, kv_len, self.counts, self._fork_scratch)
         if check and int(self.counts[1]):
             raise MemoryError("no page left")
-        if check and self._unchecked and bool((pages.gather(1, (kv_len - 1).long()[:, None] // dec.P) < 0).any()):
+        if check and self._unchecked and bool(((pages.gather(1, (kv_len - 1).clamp(min=0).long()[:, None] // dec.P)[:, 0] < 0) & (news > 0)).any()):
             raise MemoryError("a beam has no page for its next token: an earlier step without check found none")
         if dec.rot_dim:
             dec._rotate(q, k, kv_len - 1)                    # (the new token is the last one)
-        B.fcp_cache_append(self.cache, k, v, self._cu, kv_len, pages)
-        B.fcp_cache_attn_shared(self.cache, q, self._cu, kv_len, pages, self._groups, self._shared, self.scale, o, lse, self._attn_scratch)
+        tokens = kv_len if self.end < 0 else kv_len * news   # (a row of a sequence of no tokens is not appended, and sees nothing)
+        B.fcp_cache_append(self.cache, k, v, self._cu, tokens, pages)
+        B.fcp_cache_attn_shared(self.cache, q, self._cu, tokens, pages, self._groups, self._shared, self.scale, o, lse, self._attn_scratch)
         self.pages, self.kv_len, self.chosen = pages, kv_len, None
         self._unchecked |= not check
         self.steps += 1
