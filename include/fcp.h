@@ -551,10 +551,11 @@ int fcp_cache_evict(const fcp_cache* cache, const int32_t* pages, const int32_t*
  *     parent's tokens in it too).  An entry that is no page's number already stays -1 and is not counted as lacking, also where new tokens would go.
  *   - Pages that only sequences without children held are free afterwards, for the next call: this one does not write them.
  * Entries of parents' tables that are no page's number become -1.  Entries behind a sequence's last page are -1.
- *   pages [n_seqs][max_pages], kv_len [n_seqs];  parent, news [n_new];  new_pages [n_new][max_pages], new_len [n_new] out, apart from the old tables: int32 device
+ *   pages [n_seqs][max_pages], kv_len [n_seqs];  parent, news [n_new];  new_pages [n_new][max_pages], new_len [n_new] out: int32 device
  *   busy [n_pages] bytes, device, or NULL: not 0 for pages that others hold, sequences outside the call say
  *   counts [3] int32 device out: pages handed out, pages that were lacking, pages that neither the new tables nor others hold
  *   scratch: device, 256-byte aligned, fcp_cache_scratch_bytes(FCP_SCRATCH_CACHE_FORK, cache, n_new, max_pages, ...); contents on entry irrelevant
+ * Outputs and scratch lie apart from inputs and from each other (FCP_ERR_INVALID_ARG), here and in the two calls that say so below.
  * While the call runs nobody else may write the pages of its sequences or use free ones.  2^24 blocks of work or more (one for 256 entries of a table, one for each (new sequence, KV head)),
  * and new tables of 2^31 entries or more, are FCP_ERR_UNSUPPORTED.
  */
@@ -568,7 +569,7 @@ int fcp_cache_fork(const fcp_cache* cache, const int32_t* pages, const int32_t* 
  *   new_pages [n_seqs][max_pages] int32 device out (may be pages itself): the tables with the new numbers, -1 where there is no cached token or no page
  *   busy as above: such pages stay where they are
  *   counts [3] int32 device out: pages moved, pages in use, the first number past all pages that are in use or busy
- *   scratch: fcp_cache_scratch_bytes(FCP_SCRATCH_CACHE_COMPACT, cache, n_seqs, max_pages, ...)
+ *   scratch: fcp_cache_scratch_bytes(FCP_SCRATCH_CACHE_COMPACT, cache, n_seqs, max_pages, ...);  what else is written lies apart, as above
  * Old pages keep their contents until somebody writes them.  2^24 blocks of work or more are FCP_ERR_UNSUPPORTED.
  */
 int fcp_cache_compact(const fcp_cache* cache, const int32_t* pages, const int32_t* kv_len, int32_t n_seqs, int32_t max_pages, const uint8_t* busy,
@@ -602,7 +603,7 @@ int fcp_cache_attn_shared(const fcp_cache* cache, const void* q, int64_t q_row, 
  *   logits [n_prompts * beams, vocab] FCP_BF16 or FCP_F32 device, rows logits_row elements apart, aligned to their type
  *   score [n_prompts * beams] fp32 device;  done [n_prompts * beams] bytes device, or NULL;  end_token: the token that ends a beam, or -1
  *   parent, token [n_prompts, keep] int32, new_score [n_prompts, keep] fp32, new_done [n_prompts, keep] bytes (or NULL): device out, best first.  parent: the row of the beam, what
- *   fcp_cache_fork takes; new_done: the beam is done, or token is end_token.  Where there are fewer candidates: -1, -1, -inf, 0.  Outputs lie apart from inputs.
+ *   fcp_cache_fork takes; new_done: the beam is done, or token is end_token.  Where there are fewer candidates: -1, -1, -inf, 0.  Outputs and scratch lie apart, as above.
  *   scratch: device, 256-byte aligned, fcp_beam_scratch_bytes (0 and fcp_last_error for arguments that the call would refuse); contents on entry irrelevant
  * Limits (FCP_ERR_UNSUPPORTED): beams, keep, vocab up to FCP_BEAM_MAX_BEAMS, FCP_BEAM_MAX_KEEP, 2^30; fewer than 2^24 chunks of 8192 logits of a row.
  */

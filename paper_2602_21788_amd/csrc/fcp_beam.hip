@@ -532,11 +532,14 @@ extern "C" int fcp_beam_select(const void* logits, int32_t type, int64_t logits_
   if (logits_row < vocab) return fail(FCP_ERR_INVALID_ARG, "%s: rows of logits overlap", who);
   if ((uintptr_t)logits % (type == FCP_BF16 ? 2 : 4) || (uintptr_t)score % 4 || (uintptr_t)parent % 4 || (uintptr_t)token % 4 || (uintptr_t)new_score % 4)
     return fail(FCP_ERR_INVALID_ARG, "%s: an argument is not aligned to its type", who);
-  if (new_score == score || (new_done && new_done == done)) return fail(FCP_ERR_INVALID_ARG, "%s: outputs must lie apart from inputs", who);
   if (!scratch || (uintptr_t)scratch % 256) return fail(FCP_ERR_INVALID_ARG, "%s: scratch must be 256-byte aligned", who);
   const BeamPlan p = plan_beam((int64_t)n_prompts * beams, vocab);
   const size_t need = beam_bytes(p, keep);
   if (scratch_bytes < need) return fail(FCP_ERR_CAPACITY, "%s: scratch has %zu bytes, %zu are needed", who, scratch_bytes, need);
+  const int64_t rows = (int64_t)n_prompts * beams, kept = (int64_t)n_prompts * keep, element = type == FCP_BF16 ? 2 : 4;
+  if (int rc = check_apart(who, {{parent, 4 * kept}, {token, 4 * kept}, {new_score, 4 * kept}, {new_done, kept}, {scratch, (int64_t)need}},
+                           {{logits, vocab * element, rows, rows > 1 ? logits_row * element : 0}, {score, 4 * rows}, {done, rows}}))
+    return rc;
   BeamArgs a = {logits, logits_row, n_prompts * beams, beams, vocab, p.chunks, p.length, p.each, keep, end_token, score, done, parent, token, new_score, new_done};
   char* const at = static_cast<char*>(scratch);
   a.lists = reinterpret_cast<uint64_t*>(at);

@@ -724,6 +724,7 @@ extern "C" int fcp_cache_attn_shared(const fcp_cache* cache, const void* q, int6
   if (int rc = check_scale(who, softmax_scale)) return rc;
   if (n_groups < 0 || n_groups > n_seqs || (n_groups > 0 && (!groups || !shared_len)))
     return fail(FCP_ERR_INVALID_ARG, "%s: %d groups of %d sequences need their first sequences and lengths", who, n_groups, n_seqs);
+  if (int rc = check_int_pointers(who, {groups, shared_len})) return rc;
   if (tq == 0 || n_seqs == 0) return FCP_OK;
   if (int rc = check_rows(who, cache, q, q_row, tq, hq)) return rc;
   if (!o || !lse || (uintptr_t)o % 16 || (uintptr_t)lse % 4) return fail(FCP_ERR_INVALID_ARG, "%s: o and lse are required and must be aligned", who);

@@ -580,9 +580,13 @@ extern "C" int fcp_cache_fork(const fcp_cache* cache, const int32_t* pages, cons
   if (int rc = check_page_sizes(who, a.c, n_seqs, n_new, max_pages)) return rc;
   if (int rc = check_seqs(who, a.c, nullptr, false, kv_len, pages, n_seqs, max_pages, 0)) return rc;
   if (!counts || (n_new > 0 && (!parent || !news || !new_len || (max_pages > 0 && !new_pages)))) return fail(FCP_ERR_INVALID_ARG, "%s: null argument", who);
-  if ((new_pages && new_pages == pages) || (new_len && new_len == kv_len)) return fail(FCP_ERR_INVALID_ARG, "%s: the new tables must lie apart from the old ones", who);
+  if (int rc = check_int_pointers(who, {pages, kv_len, parent, news, new_pages, new_len, counts})) return rc;
   const PageSpace space = page_space(a.c, n_new);
   if (int rc = check_scratch(who, scratch, scratch_bytes, space.bytes)) return rc;
+  const int64_t row = (int64_t)4 * max_pages;
+  if (int rc = check_apart(who, {{new_pages, n_new * row}, {new_len, (int64_t)4 * n_new}, {counts, 12}, {scratch, (int64_t)space.bytes}},
+                           {{pages, n_seqs * row}, {kv_len, (int64_t)4 * n_seqs}, {parent, (int64_t)4 * n_new}, {news, (int64_t)4 * n_new}, {busy, a.c.n_pages}}))
+    return rc;
   a.s = {nullptr, kv_len, pages, n_seqs, max_pages, 0};
   a.parent = parent;
   a.news = news;
@@ -625,8 +629,12 @@ extern "C" int fcp_cache_compact(const fcp_cache* cache, const int32_t* pages, c
   if (int rc = check_page_sizes(who, a.c, n_seqs, 0, max_pages)) return rc;
   if (int rc = check_seqs(who, a.c, nullptr, false, kv_len, pages, n_seqs, max_pages, 0)) return rc;
   if (!counts || (n_seqs > 0 && max_pages > 0 && !new_pages)) return fail(FCP_ERR_INVALID_ARG, "%s: null argument", who);
+  if (int rc = check_int_pointers(who, {pages, kv_len, new_pages, counts})) return rc;
   const PageSpace space = page_space(a.c, a.c.n_pages);
   if (int rc = check_scratch(who, scratch, scratch_bytes, space.bytes)) return rc;
+  const int64_t tables = (int64_t)4 * n_seqs * max_pages;
+  const Span old = {new_pages == pages ? nullptr : pages, tables};       // (the new tables may be the old ones)
+  if (int rc = check_apart(who, {{new_pages, tables}, {counts, 12}, {scratch, (int64_t)space.bytes}}, {old, {kv_len, (int64_t)4 * n_seqs}, {busy, a.c.n_pages}})) return rc;
   a.s = {nullptr, kv_len, pages, n_seqs, max_pages, 0};
   a.busy = busy;
   a.new_pages = new_pages;

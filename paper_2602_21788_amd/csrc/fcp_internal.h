@@ -4,6 +4,7 @@
 #include <stdint.h>
 
 #include <atomic>
+#include <initializer_list>
 #include "fcp.h"
 #include "fcp_sizes.h"
 
@@ -22,6 +23,34 @@ void clear_error();
 
 // A launch has fewer than 2^32 threads along an axis; HIP refuses larger ones, which a call that has launched something before would find out too late.
 inline bool fits_axis(int64_t blocks, int threads) { return blocks < ((int64_t)1 << 32) / threads; }
+
+// Memory that a call reads or writes: `rows` runs of `bytes` that are `stride` bytes apart.  No address: nothing.
+struct Span {
+  const void* p;
+  int64_t bytes, rows = 1, stride = 0;
+};
+inline bool meet(const Span& run, const Span& rows) {      // one run, and rows
+  if (!run.p || !rows.p || run.bytes <= 0 || rows.bytes <= 0 || rows.rows <= 0) return false;
+  const intptr_t at = (intptr_t)run.p - (intptr_t)rows.p, end = (intptr_t)((rows.rows - 1) * rows.stride + rows.bytes);
+  if (at + run.bytes <= 0 || at >= end) return false;
+  if (at < 0 || rows.rows == 1) return true;
+  return at % rows.stride < rows.bytes || at % rows.stride + run.bytes > rows.stride;
+}
+// What a call writes must lie apart from what it reads, and from what else it writes.
+inline int check_apart(const char* who, std::initializer_list<Span> out, std::initializer_list<Span> in) {
+  for (const Span& x : out) {
+    for (const Span& y : in)
+      if (meet(x, y)) return fail(FCP_ERR_INVALID_ARG, "%s: outputs and scratch must lie apart from inputs", who);
+    for (const Span& y : out)
+      if (&x != &y && meet(x, y)) return fail(FCP_ERR_INVALID_ARG, "%s: outputs and scratch must lie apart from each other", who);
+  }
+  return FCP_OK;
+}
+inline int check_int_pointers(const char* who, std::initializer_list<const void*> pointers) {
+  for (const void* p : pointers)
+    if ((uintptr_t)p % 4) return fail(FCP_ERR_INVALID_ARG, "%s: an argument is not aligned to its type", who);
+  return FCP_OK;
+}
 
 // A kernel that uses more than 64 KB of dynamic LDS needs its limit raised once per device; `done` keeps one bit
 // per device (devices past 63 raise it on every call).  Safe to call from several threads.
