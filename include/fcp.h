@@ -599,7 +599,8 @@ int fcp_cache_attn_shared(const fcp_cache* cache, const void* q, int64_t q_row, 
  *   score_b + x_bt - ln sum_u exp x_bu.
  * NaN counts as -inf and +inf as the largest finite value; a logit of -inf is no candidate (a grammar's mask), nor is any of a beam whose score is -inf or NaN (beams that begin with the same
  * tokens: all but one).  Of a beam at most its `keep` greatest logits are candidates, among equal ones the lowest tokens.  A beam that is done has one candidate, end_token, at its score.
- * Sums and scores are held and compared in 64 bits; among equal scores the lowest beam comes first, then the lowest token.
+ * Sums and scores are held and compared in 64 bits, and the logarithm is off by 1e-10 at most: candidates of different beams whose scores lie within 2e-10 of each other may come in either order, those
+ * of one beam come in the order of its logits.  Among equal scores the lowest beam comes first, then the lowest token.
  *   logits [n_prompts * beams, vocab] FCP_BF16 or FCP_F32 device, rows logits_row elements apart, aligned to their type
  *   score [n_prompts * beams] fp32 device;  done [n_prompts * beams] bytes device, or NULL;  end_token: the token that ends a beam, or -1
  *   parent, token [n_prompts, keep] int32, new_score [n_prompts, keep] fp32, new_done [n_prompts, keep] bytes (or NULL): device out, best first.  parent: the row of the beam, what

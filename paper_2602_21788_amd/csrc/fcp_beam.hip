@@ -1,7 +1,8 @@
 // fcp_beam_select: the best continuations of every prompt, over its beams and the vocabulary.
 //
 // The score of token t behind beam b is score_b + x_bt - ln sum_u exp x_bu.  The order of a beam's tokens is that of its logits, so a beam offers its `keep` greatest logits, and the
-// logarithm is needed only to put beams beside each other.  Candidates of different beams can lie as near as they like: sums and scores are held in 64 bits.
+// logarithm is needed only to put beams beside each other.  Sums and scores are held in 64 bits, and the logarithm is off by 1e-10 at most: by 5.4e-11 from the terms of a chunk's sum (NearSum), and where
+// a row has several by 4.3e-11 from bringing their sums together (Exp).  Candidates of different beams that lie nearer than 2e-10 may come in either order.
 //
 // First launch: a block takes a chunk of a row, up to 32 neighbouring logits a thread (8 where there are few rows), which stay in registers for three looks:
 //   * the greatest of every four threads, 64 in all (of each of the 256 threads, if more than 32 are kept); the keep-th greatest of those, T, found bit by bit: at least `keep` logits of the chunk are T
@@ -11,8 +12,8 @@
 //     places, T becomes the keep-th greatest logit itself.
 // Second launch: a block for each prompt joins the sums and finds the best candidates of all lists the same way, all lists' best first.
 //
-// 64 prompts of 8 beams, 131072 bf16 logits each, 16 kept: 44.5 and 7.6 us, 48.4 together (a copy's rate would read the logits in 27); vector instructions bound the first, loads and barriers that wait
-// for each other the second, and all of small calls: one prompt of 4 beams over 32000 tokens 5.5 and 6.3 us, 11.5 together.
+// 64 prompts of 8 beams, 131072 bf16 logits each, 16 kept: 48.5 us (43 and 7.7 under a profiler; a copy's rate would read the logits in 27); vector instructions bound the first, loads and barriers that
+// wait for each other the second, and all of small calls: one prompt of 4 beams over 32000 tokens 11.8 us (6 to 7, and 6.2).
 #include <float.h>
 
 #include "fcp_device.h"
@@ -72,7 +73,7 @@ struct Exp {
 
 // Sums of exp(x), |greatest x| <= 1024: exp(x) = 2^n 2^(k / 1024) e^r, n + k / 1024 + r / ln 2 = x log2(e), |r| <= ln 2 / 2048 and a little.  2^(k / 1024) comes from a table in LDS, in 64 bits; r and
 // e^r - 1 = r + r^2 / 2 + .. take 32, which is enough because they are small: r twice and e^r - 1 once are off by half a step of 2^-35, 1.46e-11, and r^3 / 6 is at most 1e-11, so a term is off by
-// 5.4e-11 of itself at most, and that is how far the logarithm of a sum may be off.  Vector instructions bound the launch, and one in 64 bits takes as long as two: 512 rows of 131072 bf16 logits take 43.9 us
+// 5.4e-11 of itself at most, and that is how far the logarithm of a chunk's sum may be off.  Vector instructions bound the launch, and one in 64 bits takes as long as two: 512 rows of 131072 bf16 logits take 43.9 us
 // so, 49.5 with a parabola in 64 bits behind a table of 512, 52.6 with the polynomial of Exp; without any sum 30, the memory's 27 of them.  What lies more than 700 below the greatest, and NaN, counts as 700 below.
 constexpr int kPowers = 1024;
 // The upper words of the powers lack k << 10: an element's integer part, n and k, is added whole.

@@ -7,9 +7,9 @@
 //   * One launch works both lines, the common one with the bodies for few or for many rows, as the rows of a group are on average; a wave works an own part alone.  Where sequences have more than 16 rows
 //     for a KV head on average each line has a launch of its own.
 //   * A wave for each row joins the pieces of its two items, whose places their workers left for it.
-// 64 samples of a prompt of up to 16384 tokens, e4m3, 32 query heads over 8 KV heads of 128: 59 us, fcp_cache_attn 174; the products of the common part would take a large product's rate
-// 14 us (21 with probabilities in two parts), the blocks begin them 10 us after the launch does (places 3.4, own parts and the first loads the rest), and partial results are 34 MB.  16 prompts of up to 8000 tokens, 8 beams each, int8: 39 and
-// 6.5 us, 50.1 together, where reading every key once takes 24.
+// 64 samples of a prompt of up to 16384 tokens, e4m3, 32 query heads over 8 KV heads of 128: 59 us, 52 and 9.4 of them the launches under a
+// profiler, fcp_cache_attn 174; the products of the common part would take a large product's rate 14 us (21 with probabilities in two parts), the blocks begin them 10 us after the launch does (places 3.4, own
+// parts and the first loads the rest), and partial results are 34 MB.  16 prompts of up to 8000 tokens, 8 beams each, int8: 50 us, 44 and 6.6 under a profiler, where reading every key once takes 24.
 #include "fcp_cache_few.h"
 #include "fcp_cache_many.h"
 
@@ -347,8 +347,8 @@ struct Work {
 };
 
 // The rows of the piece at hand over its tiles t0 + first, t0 + first + step, ...
-// (Matrix rows behind the last have the queries of the head's first row, and nobody reads their sums.  Zeros instead would be waited for where the queries are asked for: the launch of 16 prompts of
-// 8 beams over up to 8000 tokens 39.2 us, 40.7 so.)
+// (Matrix rows behind the last have the queries of the head's first row, and nobody reads their sums.  Zeros instead would be waited for where the queries are asked for: 16 prompts of 8 beams over
+// up to 8000 tokens 50.5 us, 51.7 so.)
 template <int D, int Fmt, int NB>
 __device__ inline void walk_piece(const SharedArgs& a, const Work& w, int lane, int first, int step, RowState<D> (&r)[NB], int& rows, int32_t* first_nan) {
   constexpr int kRows = 16 * NB;
