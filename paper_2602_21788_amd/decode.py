@@ -189,7 +189,7 @@ class BeamDecoder:
         self._tables = [(i32(rows, max_pages), i32(rows)) for _ in range(2)]           # this step's and the next one's, in turn
         self.counts = i32(3)
         up = self.prompts._to
-        self._ones, self._cu, self._groups = up(np.ones(rows)), up(np.arange(rows + 1)), up(np.arange(n_prompts + 1) * beams)
+        self._ones, self._none, self._cu, self._groups = up(np.ones(rows)), up(np.zeros((1, 1))), up(np.arange(rows + 1)), up(np.arange(n_prompts + 1) * beams)
         self._fork_scratch = torch.empty(B.fcp_cache_scratch_bytes(B.FCP_SCRATCH_CACHE_FORK, self.cache, rows, max_pages), dtype=torch.uint8, device=self.device)
         self._attn_scratch = torch.empty(B.fcp_cache_scratch_bytes(B.FCP_SCRATCH_CACHE_SHARED, self.cache, rows, max_pages, rows, hq), dtype=torch.uint8, device=self.device)
         self._beam_scratch = None
@@ -222,26 +222,27 @@ class BeamDecoder:
         self.history.append((parent, token))
         return token, parent
 
-    def _going(self):
-        """[n_prompts, 1] bool: prompts of which a chosen beam goes on.  The others' have all ended, or there was no candidate; this stays so."""
-        return ((self.done == 0) & (self.chosen >= 0)).view(self.n, self.beams).any(1, keepdim=True)
+    def _over(self):
+        """[n_prompts, 1] bool: prompts of which no chosen beam goes on: they have all ended, or there was no candidate.  This stays so."""
+        return torch.logical_or(self.done, self.chosen < 0).view(self.n, self.beams).all(1, keepdim=True)
 
     def step(self, q, k, v, check=True):
         """The rows of the chosen tokens, bf16 [n_prompts * beams, heads, D] (turned in place): O, LSE.  check: raises MemoryError, and leaves the beams as they were, where the pool has too few
         pages, or a new token would go into one that was lacking in an earlier step; the host waits for this.  Without it tokens that found no page are seen by nobody, and if the page would
         have been a copy of one that is begun, neither are the beam's earlier tokens in it nor its next ones, until that page ends.
-        Prompts whose beams have all ended stay as they are: their rows are not appended and take no pages, O is 0 and LSE -inf for them.  (With an end token this takes 7 small launches a step.)"""
+        Prompts whose beams have all ended stay as they are: their rows are not appended and take no pages, O is 0 and LSE -inf for them.  (With an end token this takes 5 small launches, some 18 us
+        of a step of 16 prompts' 8 beams that takes 89 without.)"""
         if self.chosen is None:
             raise ValueError("select() chooses the tokens whose rows step() takes")
         dec, rows = self.prompts, self.n * self.beams
         dec._fit(q, k, v, rows)
         if self._longest == dec.pages.shape[1] * dec.P:      # (the host waits here alone: prompts may have ended)
-            self._longest = int(np.max(self._lens[self._going().cpu().numpy()[:, 0]] + self.steps, initial=0))
+            self._longest = int(np.max(self._lens[~self._over().cpu().numpy()[:, 0]] + self.steps, initial=0))
             if self._longest == dec.pages.shape[1] * dec.P:
                 raise MemoryError("a sequence's table is full")
         o, lse = torch.empty(q.shape, dtype=torch.bfloat16, device=self.device), torch.empty(dec.hq, rows, dtype=torch.float32, device=self.device)
         pages, kv_len = self._tables[self.steps % 2]
-        news = self._ones if self.end < 0 else self._going().expand(-1, self.beams).reshape(-1).int()
+        news = self._ones if self.end < 0 else torch.where(self._over(), self._none, self._ones.view(self.n, self.beams)).view(-1)
         B.fcp_cache_fork(self.cache, self.pages, self.kv_len, self.chosen, news, pages, kv_len, self.counts, self._fork_scratch)
         if check and int(self.counts[1]):
             raise MemoryError("no page left")
