@@ -74,8 +74,7 @@ __device__ inline int32_t places_of_item(const Part& p, bool whole) { return who
 __device__ inline int32_t row_blocks_of(const SharedArgs& a, const Part& p, int kind) { return ((p.rows * a.group - 1) >> a.log_rows[kind]) + 1; }
 __device__ inline int32_t places_of_part(const SharedArgs& a, const Part& p, int kind, bool whole) { return p.rows == 0 ? 0 : a.c.hkv * row_blocks_of(a, p, kind) * places_of_item(p, whole); }
 
-// Own parts up to this long are not divided, where all are.  4 / 8 / 16 tiles: 64 of a group with up to 600 own tokens 60.2 / 60.1 / 59.7 us, 8 with 1000 39.4 / 39.1 / 55.2, 16 groups of two with 1000
-// 35.4 / 35.4 / 44.2, 64 with 300 57.9 / 53.6 / 54.0.
+// Own parts up to this long are not divided, where all are.  4 / 8 / 16 tiles: 64 of a group with 600 own tokens 67.9 / 68.3 / 68.1 us, with 300 62.8 / 59.8 / 59.9, 8 with 1000 36.5 / 36.4 / 51.6.
 constexpr int kWholeLen = 8 * kTile;
 constexpr int kSharers = kWaves * kBlocks;       // waves that share the line of own parts
 constexpr int kLocal = 256;            // parts that a block places itself: one a thread
@@ -134,7 +133,7 @@ __device__ inline Entry common_of(const Seen& x, int page) {
 }
 template <int Threads, class F>
 __device__ inline void place_groups(const SharedArgs& a, const Tables& t, F group) {
-  if (a.n_groups <= Threads / 64) {                                     // a wave a group (300 sequences of one group: 48 us, 56 with eight lanes)
+  if (a.n_groups <= Threads / 64) {                                     // a wave a group (300 sequences of one group: 52 us, 58 with eight lanes)
     const int g = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     if (g >= a.n_groups) return;
     Seen x = look_at(t, group(g), g, lane, 64, a.c.page);
